@@ -448,3 +448,18 @@ class StencilPlan:
             self.destroy()
         except Exception:
             pass
+
+
+# The sequence operators (sequence.py) under the package's own name, loaded
+# when first asked for: importing the package does not import torch.
+_SEQUENCE = ("short_conv", "short_conv_grad", "short_conv_step", "state_scan",
+             "state_scan_grad", "state_scan_step")
+
+
+def __getattr__(name):
+    if name in _SEQUENCE:
+        from . import sequence
+        for n in _SEQUENCE:
+            globals()[n] = getattr(sequence, n)
+        return globals()[name]
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

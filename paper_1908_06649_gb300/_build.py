@@ -18,9 +18,16 @@ UNITS = ["tcu_dft.cu", "host_tables.cu", "noalloc.cu", "grid_plan.cu",
          "kernels_mixed_r8.cu", "kernels_mixed_r16.cu", "kernels_mixed_r32.cu",
          "kernels_bf16_r8.cu", "kernels_bf16_r16.cu", "kernels_bf16_r32.cu",
          "grid_kernels.cu"]
+# the sequence operators: no index checks of their own, so both variants link
+# the same objects
+SEQ_UNITS = ["short_conv.cu", "state_scan.cu", "state_scan_f32.cu",
+             "state_scan_bf16.cu", "state_scan_f16.cu"]
 HEADERS = ["tcgen05.cuh", "group_kernel.cuh", "launch.h",
-           "launch_impl.cuh", "host_plan.h"]
-HDR = os.path.join(os.path.dirname(HERE), "include", "tcu_dft.h")
+           "launch_impl.cuh", "host_plan.h", "seq_common.cuh",
+           "state_scan.cuh", "state_scan_impl.cuh"]
+INCLUDE = os.path.join(os.path.dirname(HERE), "include")
+HDR = os.path.join(INCLUDE, "tcu_dft.h")
+SEQ_HDR = os.path.join(INCLUDE, "tcu_seq.h")
 LIB_PATH = os.path.join(HERE, "libtcu_dft.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 # the bounds-checked variant: every shared-memory, tensor-memory and global
@@ -45,8 +52,8 @@ def nvcc() -> str:
 
 
 def _sources():
-    return ([os.path.join(CSRC, u) for u in UNITS]
-            + [os.path.join(CSRC, h) for h in HEADERS] + [HDR])
+    return ([os.path.join(CSRC, u) for u in UNITS + SEQ_UNITS]
+            + [os.path.join(CSRC, h) for h in HEADERS] + [HDR, SEQ_HDR])
 
 
 def build_variants(names=("release",), force: bool = False,
@@ -56,6 +63,7 @@ def build_variants(names=("release",), force: bool = False,
     newest = max(os.path.getmtime(f) for f in _sources())
     cc = nvcc()
     jobs = []
+    shared = {}  # object path -> (unit, compiler) of the units both variants link
     for name in names:
         defs, lib_path, build_dir = VARIANTS[name]
         if (not force and os.path.exists(lib_path)
@@ -69,6 +77,16 @@ def build_variants(names=("release",), force: bool = False,
             if verbose:
                 cmd.insert(1, "-Xptxas=-v")
             procs.append((u, subprocess.Popen(cmd)))
+            objs.append(obj)
+        os.makedirs(BUILD_DIR, exist_ok=True)
+        for u in SEQ_UNITS:
+            obj = os.path.join(BUILD_DIR, u.replace(".cu", ".o"))
+            if obj not in shared:
+                cmd = [cc, *ARCH, *FLAGS, "-c", "-o", obj, os.path.join(CSRC, u)]
+                if verbose:
+                    cmd.insert(1, "-Xptxas=-v")
+                shared[obj] = (u, subprocess.Popen(cmd))
+            procs.append(shared[obj])
             objs.append(obj)
         jobs.append((name, lib_path, procs, objs))
     for name, lib_path, procs, objs in jobs:

@@ -1,0 +1,146 @@
+// state_scan_impl.cuh -- launches of the scan kernels for one element type.
+#pragma once
+#include "state_scan.cuh"
+
+namespace tcu {
+namespace seq {
+
+template <typename T>
+ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, bool grad) {
+  ScanArgs<T> a{};
+  a.u = rows_of<const T>(s.u);
+  a.dt = rows_of<const T>(s.dt);
+  a.gate = rows_of<const T>(s.gate);
+  a.B = rows_of<const T>(s.B);
+  a.C = rows_of<const T>(s.C);
+  a.A = s.A;
+  a.skip = s.skip;
+  a.dt_bias = s.dt_bias;
+  a.state = s.state;
+  a.last = s.last;
+  a.marks = s.marks;
+  a.offsets = s.offsets;
+  a.slots = s.slots;
+  a.rows = s.rows;
+  a.channels = s.channels;
+  a.num_slots = s.num_slots;
+  a.chunk_rows = p.chunk_rows;
+  a.states = (int)s.states;
+  a.groups = s.groups;
+  a.per_group = p.per_group;
+  a.group_blocks = p.group_blocks;
+  a.sequences = s.sequences;
+  a.batches = (int)p.batches;
+  a.chunks = p.chunks;
+  a.softplus = s.softplus;
+  if (!grad) a.y = rows_of<T>(s.y);
+  float *w = static_cast<float *>(s.workspace);
+  a.carry = w;
+  a.sum_d = a.carry + p.carry;
+  a.row_seq = s.offsets ? reinterpret_cast<int32_t *>(a.sum_d + p.sum_d) : nullptr;
+  if (grad) {
+    a.dy = rows_of<const T>(s.dy);
+    a.du = rows_of<T>(s.du);
+    a.ddt = rows_of<T>(s.ddt);
+    a.dgate = rows_of<T>(s.dgate);
+    a.dB = rows_of<T>(s.dB);
+    a.dC = rows_of<T>(s.dC);
+    a.dlast = s.dlast;
+    a.dstate = s.dstate;
+    a.bc_parts = a.sum_d + p.sum_d + p.row_seq;
+    a.A_parts = a.bc_parts + p.bc_parts;
+    a.skip_parts = s.dskip ? a.A_parts + p.A_parts : nullptr;
+    a.bias_parts = s.ddt_bias ? a.A_parts + p.A_parts + p.vec_parts : nullptr;
+  }
+  return a;
+}
+
+template <auto *kernel, typename T>
+int start(int64_t blocks, int floats, const ScanArgs<T> &a, cudaStream_t st) {
+  if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  const int bytes = floats * 4;
+  if (bytes > 48 * 1024 &&
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) !=
+          cudaSuccess) {
+    cudaGetLastError();
+    return TCU_DFT_ERR_CUDA;
+  }
+  kernel<<<(unsigned)blocks, kScanThreads, bytes, st>>>(a);
+  return launched();
+}
+
+template <typename T, int LS, bool kPacked>
+int forward(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
+  using P = Shape<LS, scan_ch(LS)>;
+  constexpr int floats = kTile * (P::kChannels * 2 + P::kStates * 2);
+  const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
+  if (p.chunks > 1) {
+    if (const int rc = start<scan_kernel<T, P, kPacked, true>>(blocks, floats, a, st)) return rc;
+    const int64_t count = a.channels * a.states * p.batches;
+    carry_kernel<T, false><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
+    if (const int rc = launched()) return rc;
+  }
+  return start<scan_kernel<T, P, kPacked, false>>(blocks, floats, a, st);
+}
+
+template <typename T, int LS, bool kPacked>
+int gradient(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
+  using P = Shape<LS, grad_ch(LS)>;
+  const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
+  if (p.chunks > 1) {
+    constexpr int floats = kTile * (P::kChannels * 2 + P::kStates);
+    if (const int rc = start<adjoint_kernel<T, P, kPacked>>(blocks, floats, a, st)) return rc;
+    const int64_t count = a.channels * a.states * p.batches;
+    carry_kernel<T, true><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
+    if (const int rc = launched()) return rc;
+  }
+  return start<scan_grad_kernel<T, P, kPacked>>(blocks, grad_floats<P>(), a, st);
+}
+
+template <typename T, int LS>
+int by_lanes(ScanCall call, const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
+  if (call == kScanStep) {
+    const int64_t count = a.channels * a.sequences * LS;
+    const int64_t blocks = (count + kScanThreads - 1) / kScanThreads;
+    if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+    scan_step_kernel<T, LS><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
+    return launched();
+  }
+  if (call == kScan)
+    return a.row_seq ? forward<T, LS, true>(p, a, st) : forward<T, LS, false>(p, a, st);
+  return a.row_seq ? gradient<T, LS, true>(p, a, st) : gradient<T, LS, false>(p, a, st);
+}
+
+template <typename T>
+int run_scan(ScanCall call, const tcu_state_scan_args &s, cudaStream_t st) {
+  const ScanPlan p = plan_of(s, call == kScanGrad);
+  const ScanArgs<T> a = args_of<T>(s, p, call == kScanGrad);
+  if (call != kScanStep && s.offsets && s.rows > 0) {
+    row_sequence_kernel<<<(unsigned)((s.rows + 127) / 128), 128, 0, st>>>(
+        a.row_seq, s.offsets, s.sequences, s.rows);
+    if (const int rc = launched()) return rc;
+  }
+  int rc = TCU_DFT_ERR_UNSUPPORTED;
+  const bool none = call != kScanStep && (p.batches == 0 || s.rows == 0);
+  if (none) rc = TCU_DFT_OK;
+  else switch (p.ls) {
+    case 1: rc = by_lanes<T, 1>(call, p, a, st); break;
+    case 2: rc = by_lanes<T, 2>(call, p, a, st); break;
+    case 4: rc = by_lanes<T, 4>(call, p, a, st); break;
+    case 8: rc = by_lanes<T, 8>(call, p, a, st); break;
+    case 16: rc = by_lanes<T, 16>(call, p, a, st); break;
+    case 32: rc = by_lanes<T, 32>(call, p, a, st); break;
+  }
+  if (rc != TCU_DFT_OK || call != kScanGrad) return rc;
+  const int64_t bc = p.batches * s.rows * s.groups * 2 * s.states;
+  if (bc > 0) sum_bc_kernel<T><<<(unsigned)((bc + 127) / 128), 128, 0, st>>>(a);
+  if ((rc = launched())) return rc;
+  const int64_t parts = none ? 0 : p.batches * p.chunks;
+  if ((rc = sum_parts(s.dA, a.A_parts, parts, s.channels * s.states, st))) return rc;
+  if (s.dskip && (rc = sum_parts(s.dskip, a.skip_parts, parts, s.channels, st))) return rc;
+  if (s.ddt_bias && (rc = sum_parts(s.ddt_bias, a.bias_parts, parts, s.channels, st))) return rc;
+  return TCU_DFT_OK;
+}
+
+}  // namespace seq
+}  // namespace tcu
