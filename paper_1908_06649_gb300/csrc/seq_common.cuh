@@ -56,14 +56,134 @@ __device__ __forceinline__ float exp2_fast(float x) {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+__device__ __forceinline__ float rcp_fast(float x) {  // 1 / inf = 0
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 __device__ __forceinline__ float sigmoid(float v) {
-  return __fdividef(1.f, 1.f + exp2_fast(-kLog2e * v));
+  return rcp_fast(1.f + exp2_fast(-kLog2e * v));
 }
 __device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
+__device__ __forceinline__ float2 silu2(float2 v) {
+  const float2 e = __fmul2_rn(v, make_float2(-kLog2e, -kLog2e));
+  const float2 w = __fadd2_rn(make_float2(exp2_fast(e.x), exp2_fast(e.y)), make_float2(1.f, 1.f));
+  return __fmul2_rn(v, make_float2(rcp_fast(w.x), rcp_fast(w.y)));
+}
 __device__ __forceinline__ float dsilu(float v) {
   const float s = sigmoid(v);
   return s * (1.f + v * (1.f - s));
 }
+
+// log(1 + exp(v)) of two values: max(v, 0) + log1p(e), e = exp(-|v|) <= 1, and
+// log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3.  2 artanh(s) / s is a
+// polynomial of degree 4 in s^2, fitted at the Chebyshev nodes of [0, 1/9]
+// (relative error 7.6e-9), so that small e keep their relative accuracy, which
+// log(1 + e) would lose.
+__device__ __forceinline__ float2 softplus2(float2 v) {
+  const float2 e = make_float2(exp2_fast(-kLog2e * fabsf(v.x)), exp2_fast(-kLog2e * fabsf(v.y)));
+  const float2 w = __fadd2_rn(e, make_float2(2.f, 2.f));
+  const float2 s = __fmul2_rn(e, make_float2(rcp_fast(w.x), rcp_fast(w.y)));
+  const float2 q = __fmul2_rn(s, s);
+  float2 p = make_float2(0.28157779f, 0.28157779f);
+  p = __ffma2_rn(p, q, make_float2(0.27965158f, 0.27965158f));
+  p = __ffma2_rn(p, q, make_float2(0.40024596f, 0.40024596f));
+  p = __ffma2_rn(p, q, make_float2(0.66666323f, 0.66666323f));
+  p = __ffma2_rn(p, q, make_float2(2.f, 2.f));
+  return __ffma2_rn(s, p, make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)));
+}
+
+// Two adjacent values of a type in 32-bit words, and back.
+template <typename T>
+struct Pair;
+template <>
+struct Pair<float> {
+  static constexpr int kWords = 2;
+  static __device__ __forceinline__ float2 get(const uint32_t *w) {
+    return make_float2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  }
+  static __device__ __forceinline__ void put(uint32_t *w, float2 v) {
+    w[0] = __float_as_uint(v.x);
+    w[1] = __float_as_uint(v.y);
+  }
+};
+template <>
+struct Pair<bf16> {
+  static constexpr int kWords = 1;
+  static __device__ __forceinline__ float2 get(const uint32_t *w) {
+    return make_float2(__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u));
+  }
+  static __device__ __forceinline__ void put(uint32_t *w, float2 v) {
+    const __nv_bfloat162 p = __float22bfloat162_rn(v);
+    w[0] = *reinterpret_cast<const uint32_t *>(&p);
+  }
+};
+template <>
+struct Pair<f16> {
+  static constexpr int kWords = 1;
+  static __device__ __forceinline__ float2 get(const uint32_t *w) {
+    return __half22float2(*reinterpret_cast<const __half2 *>(w));
+  }
+  static __device__ __forceinline__ void put(uint32_t *w, float2 v) {
+    const __half2 p = __float22half2_rn(v);
+    w[0] = *reinterpret_cast<const uint32_t *>(&p);
+  }
+};
+
+// V adjacent values (V even) as they lie in memory, in words so that nothing
+// waits for them before they are used: loads and stores of up to 16 bytes
+// where kWide, value by value otherwise; those from `count` on are neither
+// read nor written (kWide: count is V or at most 0).
+template <typename T, int V>
+struct Raw {
+  static constexpr int kPairWords = Pair<T>::kWords, kWords = V / 2 * kPairWords;
+  static constexpr int kStep = kWords % 4 == 0 ? 4 : kWords % 2 == 0 ? 2 : 1;
+  uint32_t w[kWords];
+  __device__ __forceinline__ float2 pair(int i) const { return Pair<T>::get(w + i * kPairWords); }
+  __device__ __forceinline__ void set(int i, float2 v) { Pair<T>::put(w + i * kPairWords, v); }
+  template <bool kWide>
+  __device__ __forceinline__ void load(const T *p, int count) {
+    if constexpr (kWide) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = 0;
+      if (count > 0) {
+#pragma unroll
+        for (int i = 0; i < kWords / kStep; ++i) {
+          const Vec<uint32_t, kStep> v = reinterpret_cast<const Vec<uint32_t, kStep> *>(p)[i];
+#pragma unroll
+          for (int j = 0; j < kStep; ++j) w[i * kStep + j] = v.v[j];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i)
+        set(i, make_float2(2 * i < count ? to_f(p[2 * i]) : 0.f,
+                           2 * i + 1 < count ? to_f(p[2 * i + 1]) : 0.f));
+    }
+  }
+  template <bool kWide>
+  __device__ __forceinline__ void store(T *p, int count) const {
+    if constexpr (kWide) {
+      if (count > 0) {
+#pragma unroll
+        for (int i = 0; i < kWords / kStep; ++i) {
+          Vec<uint32_t, kStep> v;
+#pragma unroll
+          for (int j = 0; j < kStep; ++j) v.v[j] = w[i * kStep + j];
+          reinterpret_cast<Vec<uint32_t, kStep> *>(p)[i] = v;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) {
+        const float2 v = pair(i);
+        if (2 * i < count) p[2 * i] = from_f<T>(v.x);
+        if (2 * i + 1 < count) p[2 * i + 1] = from_f<T>(v.y);
+      }
+    }
+  }
+};
 
 // A row tensor of element type T.
 template <typename T>

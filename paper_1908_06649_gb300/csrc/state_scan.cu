@@ -16,14 +16,15 @@ ScanPlan plan_of(const tcu_state_scan_args &a, bool grad) {
   ScanPlan p{};
   p.batches = a.offsets ? 1 : a.sequences;
   p.ls = lanes_of(a.states);
-  p.db = block_channels(p.ls, grad ? grad_ch(p.ls) : scan_ch(p.ls));
+  p.db = grad ? block_channels(p.ls, grad_ch(p.ls)) : scan_channels(p.ls);
   p.per_group = (int)(a.channels / a.groups);
   p.group_blocks = (p.per_group + p.db - 1) / p.db;
   const int64_t blocks = p.batches * a.groups * p.group_blocks;
   const int64_t tiles = (a.rows + kTile - 1) / kTile;
-  // enough blocks for four on every SM, where there are rows to split
-  const int64_t want = 4 * (int64_t)num_sms();
-  int64_t chunks = blocks == 0 || blocks * 2 >= want ? 1 : (want + blocks - 1) / blocks;
+  // Where the blocks leave more than half of the card's slots empty, rows are
+  // split so that all blocks run at once.
+  const int64_t slots = (grad ? 3 : scan_resident(p.ls)) * (int64_t)num_sms();
+  int64_t chunks = blocks == 0 || blocks * 2 > slots ? 1 : slots / blocks;
   chunks = std::max<int64_t>(1, std::min(chunks, tiles / 2));
   const int64_t chunk_tiles = std::max<int64_t>(1, (tiles + chunks - 1) / chunks);
   p.chunk_rows = chunk_tiles * kTile;

@@ -65,6 +65,9 @@ struct ScanArgs {
   int64_t chunk_rows;
   int states, groups, per_group, group_blocks;
   int sequences, batches, chunks, softplus;
+  // whether states, and B and C, are read in words of four values
+  int wide_states, wide_bc;
+  int wide;  // whether rows are, in words of 16 bytes
 };
 
 // The channels a block of the given kernel covers, and its rows.
@@ -90,9 +93,7 @@ struct Place {
   }
 };
 
-__device__ __forceinline__ float softplus(float v) {
-  return fmaxf(v, 0.f) + log1pf(exp2_fast(-kLog2e * fabsf(v)));
-}
+__device__ __forceinline__ float softplus(float v) { return softplus2(make_float2(v, v)).x; }
 
 // Four states of one channel, from / to an array [..][states].
 __device__ __forceinline__ void load4(float (&h)[4], const float *p, int n, int states) {
@@ -189,134 +190,404 @@ __device__ __forceinline__ float step_of(const ScanArgs<T> &a, float dt, float b
   return a.softplus ? softplus(v) : v;
 }
 
-// The scan of a chunk.  kLocal: from a zero start, leaving its final state
-// and sum of d for the carry; otherwise from the carried state, with outputs.
-template <typename T, class P, bool kPacked, bool kLocal>
-__global__ void __launch_bounds__(kScanThreads) scan_kernel(ScanArgs<T> a) {
-  constexpr int LS = P::LS, CH = P::CH, NP = P::kStates, DB = P::kChannels;
-  extern __shared__ __align__(16) float smem[];
-  float *sd = smem, *sx = sd + kTile * DB, *sB = sx + kTile * DB, *sC = sB + kTile * NP;
-  const Place<DB, T> w(a);
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int sl = lane % LS, n0 = sl * 4;
-  const int ch0 = warp * P::kWarpChannels + lane / LS * CH;  // of the block
-  float A2[CH][4], h[CH][4], dsum[CH];
-  const int64_t state0 = (w.b * a.chunks + w.k) * a.channels + w.c0;
+// ------------------------------------------------------------------ forward
+// How the forward kernels are laid out.  A block is pairs of warps over
+// adjacent channels of one group, each pair by itself.  Its first warp runs
+// the recurrence of WC channels, LS lanes over the states, CH channels a
+// thread; the second turns the rows u, dt into d, d u for it one piece of RP
+// rows ahead, and its sums into y one piece behind, a lane owning V adjacent
+// channels of a row.  With 16 values a lane there are too few recurrences to
+// hide each other's latencies, and the two halves are about equally long.
+// The first warps come first, so that each SM quarter gets as many of either
+// kind.  What the inner loop draws from shared memory, whose pipe returns 32
+// words a clock whatever lanes share, is 2 CH + 2 * 4 words for CH * 4 states.
+constexpr int kRing = 4;  // pieces of raw rows: one behind, the current one, two ahead
+constexpr int scan_ch(int ls) { return ls == 2 ? 2 : 4; }
+constexpr int scan_pairs(int ls) { return ls <= 8 ? 4 : ls == 16 ? 2 : 1; }
+constexpr int scan_channels(int ls) { return scan_pairs(ls) * (32 / ls) * scan_ch(ls); }
+// blocks that registers and shared memory let an SM hold
+constexpr int scan_resident(int ls) { return ls <= 4 ? 2 : ls == 32 ? 2 : 1; }
+template <int LS_, typename T>
+struct Lay {
+  static constexpr int LS = LS_, CH = scan_ch(LS), NP = 4 * LS;
+  static constexpr int kPairs = scan_pairs(LS), kBlock = 64 * kPairs;
+  static constexpr int WC = 32 / LS * CH, V = WC < 8 ? WC : 8, DB = kPairs * WC;
+  static constexpr int COLS = WC / V, RP = 32 / COLS;
+  static constexpr int kRow = WC + 4;  // pitch of d, d u
+  // pitches of the lanes' shares of o: 8 lanes' 16-byte accesses miss each
+  // other's banks
+  static constexpr int kYLane = LS == 2 ? 48 : LS == 4 ? 40 : LS == 32 ? 4 : WC + 4;
+  static constexpr int kYRow = LS * kYLane + 4;
+  static constexpr int kRaw = Raw<T, V>::kWords;
+  // shared memory, in floats
+  static constexpr int kBC = RP * NP;  // a piece of B or C
+  static constexpr int kPairFloats =
+      4 * kBC + 2 * WC + 2 * (2 * RP * kRow + RP * kYRow) + kRing * 3 * 32 * kRaw;
+  static constexpr int kFloats = kPairs * kPairFloats;
+};
+
+// The two warps of a pair meet.
+__device__ __forceinline__ void meet(int pair) {
+  asm volatile("bar.sync %0, 64;" ::"r"(pair + 1) : "memory");
+}
+
+__device__ __forceinline__ void copy_async(uint32_t *to, const void *from, int bytes) {
+  const uint32_t s = (uint32_t)__cvta_generic_to_shared(to);
+  if (bytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from) : "memory");
+  else if (bytes == 8)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(s), "l"(from) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(from) : "memory");
+}
+
+// Four states of CH channels (pairs of channels packed) from / to an array
+// [channels][states], channels from c on of which `count` exist.
+template <typename T, int PAIRS>
+__device__ __forceinline__ void load_states(float2 (&h)[PAIRS][4], const ScanArgs<T> &a,
+                                            const float *base, int n0, int count) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const bool in = ch0 + c < w.nc;
-    dsum[c] = 0.f;
+  for (int p = 0; p < PAIRS; ++p) {
+    float v[2][4] = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) A2[c][i] = h[c][i] = 0.f;
-    if (!in) continue;
-    load4(A2[c], a.A + (w.c0 + ch0 + c) * a.states, n0, a.states);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) A2[c][i] *= kLog2e;
-    if (!kPacked && w.k == 0) {
-      if (a.state)
-        load4(h[c], a.state + (w.b * a.channels + w.c0 + ch0 + c) * a.states, n0, a.states);
-    } else if (!kLocal && w.k > 0) {
-      load4(h[c], a.carry + (state0 + ch0 + c) * a.states, n0, a.states);
+    for (int j = 0; j < 2; ++j) {
+      if (!base || 2 * p + j >= count) continue;
+      const float *q = base + (int64_t)(2 * p + j) * a.states;
+      if (a.wide_states) {
+        const float4 w = n0 < a.states ? *reinterpret_cast<const float4 *>(q + n0)
+                                       : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[j][0] = w.x, v[j][1] = w.y, v[j][2] = w.z, v[j][3] = w.w;
+      } else {
+        load4(v[j], q, n0, a.states);
+      }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[p][i] = make_float2(v[0][i], v[1][i]);
   }
-  for (int64_t row0 = w.r0; row0 < w.r1; row0 += kTile) {
-    const int rows = (int)min((int64_t)kTile, w.r1 - row0);
-    __syncthreads();
-    for (int e = threadIdx.x; e < kTile * DB; e += kScanThreads) {
-      const int t = e / DB, c = e % DB;
-      float d = 0.f, x = 0.f;
-      if (t < rows && c < w.nc) {
-        const float bias = a.dt_bias ? a.dt_bias[w.c0 + c] : 0.f;
-        d = step_of(a, to_f(a.dt.at(w.b, row0 + t)[w.c0 + c]), bias);
-        x = d * to_f(a.u.at(w.b, row0 + t)[w.c0 + c]);
+}
+template <typename T, int PAIRS>
+__device__ __forceinline__ void store_states(const float2 (&h)[PAIRS][4], const ScanArgs<T> &a,
+                                             float *base, int n0, int count) {
+#pragma unroll
+  for (int p = 0; p < PAIRS; ++p)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (2 * p + j >= count) continue;
+      float *q = base + (int64_t)(2 * p + j) * a.states;
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = j ? h[p][i].y : h[p][i].x;
+      if (a.wide_states) {
+        if (n0 < a.states) *reinterpret_cast<float4 *>(q + n0) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+        store4(q, v, n0, a.states);
       }
-      sd[e] = d;
-      sx[e] = x;
     }
-    stage_bc<NP>(a, w.b, w.g, row0, rows, sB, kLocal ? nullptr : sC);
-    const uint32_t opens = kPacked ? opens_mask(a, row0, lane) : 0;
-    __syncthreads();
-    if (!kLocal && a.marks) {
-      const int64_t marks = (a.rows + kTile - 1) / kTile;
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-        if (ch0 + c < w.nc)
-          store4(a.marks + ((w.b * marks + row0 / kTile) * a.channels + w.c0 + ch0 + c) * a.states,
-                 h[c], n0, a.states);
+}
+
+// The scan of a chunk.  kLocal: from a zero start, leaving the chunk's final
+// state and its sum of d for the carry; otherwise from the carried state,
+// with outputs.  kWide: rows in words of V values.
+template <typename T, int LS, bool kPacked, bool kLocal, bool kWide>
+__global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
+    scan_kernel(ScanArgs<T> a) {
+  using L = Lay<LS, T>;
+  constexpr int CH = L::CH, PAIRS = CH / 2, V = L::V, RP = L::RP;
+  extern __shared__ __align__(16) float smem[];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int pair = warp % L::kPairs;
+  float *sbc = smem + pair * L::kPairFloats;           // [2][B, C][RP][states]
+  float *sbias = sbc + 4 * L::kBC, *sskip = sbias + L::WC;
+  float *sdx = sskip + L::WC;                          // [2][d, x][RP][kRow]
+  float *sy = sdx + 4 * RP * L::kRow;                  // [2][RP][kYRow]
+  uint32_t *ring = reinterpret_cast<uint32_t *>(sy + 2 * RP * L::kYRow);
+  const Place<L::DB, T> w(a);
+  const int64_t c0 = w.c0 + pair * L::WC;
+  const int nc = w.nc - pair * L::WC;
+  if (nc <= 0) return;  // both warps of the pair
+  const int pieces = (int)((w.r1 - w.r0 + RP - 1) / RP);
+
+  if (warp >= L::kPairs) {
+    // ---- rows into d, d u; sums into y
+    const int vr = lane / L::COLS, vc = lane % L::COLS * V, vcount = min(V, nc - vc);
+    for (int c = lane; c < L::WC; c += 32) {
+      sbias[c] = a.dt_bias && c < nc ? a.dt_bias[c0 + c] : 0.f;
+      sskip[c] = a.skip && c < nc ? a.skip[c0 + c] : 0.f;
     }
-    for (int t = 0; t < rows; ++t) {
-      if (kPacked && (opens >> t & 1)) {
-        const int64_t r = row0 + t;
-        const int s = a.row_seq[r], before = r > 0 ? a.row_seq[r - 1] : -1;
+    __syncwarp();
+    const float *bias = sbias + vc, *skip = sskip + vc;
+    const T *pu = a.u.at(w.b, w.r0 + vr) + c0 + vc, *pd = a.dt.at(w.b, w.r0 + vr) + c0 + vc;
+    const T *pz = a.gate.p && !kLocal ? a.gate.at(w.b, w.r0 + vr) + c0 + vc : nullptr;
+    T *py = kLocal ? nullptr : a.y.at(w.b, w.r0 + vr) + c0 + vc;
+    const int64_t su = RP * a.u.row, sdt = RP * a.dt.row, sz = RP * a.gate.row, so = RP * a.y.row;
+    const int last = (int)(w.r1 - w.r0) - vr;  // this lane's row is in piece i if i RP < last
+    auto slot = [&](int i, int which) { return ring + ((i % kRing * 3 + which) * 32 + lane) * L::kRaw; };
+    // piece i of u, dt, gate on its way to the ring
+    Raw<T, V> hold[3];
+    auto fetch = [&](int i) {
+      const bool in = i * RP < last && vcount > 0;
+      if constexpr (kWide) {
+        if (in) {
+          constexpr int word = L::kRaw % 4 == 0 ? 4 : L::kRaw % 2 == 0 ? 2 : 1;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          if (ch0 + c >= w.nc) continue;
-          const int64_t at = w.c0 + ch0 + c;
-          if (!kLocal && a.last && before >= 0)
-            store4(a.last + (before * a.channels + at) * a.states, h[c], n0, a.states);
-          dsum[c] = 0.f;
+          for (int j = 0; j < L::kRaw; j += word) {
+            copy_async(slot(i, 0) + j, reinterpret_cast<const uint32_t *>(pu) + j, word * 4);
+            copy_async(slot(i, 1) + j, reinterpret_cast<const uint32_t *>(pd) + j, word * 4);
+            if (pz) copy_async(slot(i, 2) + j, reinterpret_cast<const uint32_t *>(pz) + j, word * 4);
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      } else {
+        hold[0].template load<false>(pu, in ? vcount : 0);
+        hold[1].template load<false>(pd, in ? vcount : 0);
+        if (pz) hold[2].template load<false>(pz, in ? vcount : 0);
+      }
+      pu += su;
+      pd += sdt;
+      if (pz) pz += sz;
+    };
+    auto landed = [&](int i) {  // what fetch(i) loaded by value
+      if constexpr (!kWide) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) h[c][i] = 0.f;
-          if (a.state && s >= 0)
-            load4(h[c], a.state + (s * a.channels + at) * a.states, n0, a.states);
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+          for (int j = 0; j < L::kRaw; ++j) slot(i, k)[j] = hold[k].w[j];
+      }
+    };
+    auto take = [&](int i, int which) {
+      Raw<T, V> r;
+#pragma unroll
+      for (int j = 0; j < L::kRaw; ++j) r.w[j] = slot(i, which)[j];
+      return r;
+    };
+    // B and C of a piece: quads of states
+    constexpr int kItems = RP * LS, kBatch = kItems < 64 ? 1 : 2;
+    Raw<T, 4> qb[kBatch], qc[kBatch];
+    auto load_bc = [&](int i, int base) {
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int item = base + j * 32 + lane, n = item % LS * 4;
+        const int64_t r = w.r0 + (int64_t)i * RP + item / LS;
+        const int count = item < kItems && r < w.r1 ? min(4, a.states - n) : 0;
+        const T *from = a.B.at(w.b, r) + (int64_t)w.g * a.states + n;
+        if (a.wide_bc) qb[j].template load<true>(from, count);
+        else qb[j].template load<false>(from, count);
+        if (kLocal) continue;
+        from = a.C.at(w.b, r) + (int64_t)w.g * a.states + n;
+        if (a.wide_bc) qc[j].template load<true>(from, count);
+        else qc[j].template load<false>(from, count);
+      }
+    };
+    auto store_bc = [&](int i, int base) {
+      float4 *to = reinterpret_cast<float4 *>(sbc + i % 2 * 2 * L::kBC);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int item = base + j * 32 + lane;
+        if (item >= kItems) continue;  // fewer than one a lane
+        float2 v0 = qb[j].pair(0), v1 = qb[j].pair(1);
+        to[item] = make_float4(v0.x, v0.y, v1.x, v1.y);
+        if (kLocal) continue;
+        v0 = qc[j].pair(0), v1 = qc[j].pair(1);
+        to[kItems + item] = make_float4(v0.x, v0.y, v1.x, v1.y);
+      }
+    };
+    auto stage = [&](int i) {
+      const Raw<T, V> u = take(i, 0), dt = take(i, 1);
+      float *od = sdx + i % 2 * 2 * RP * L::kRow + vr * L::kRow + vc, *ox = od + RP * L::kRow;
+      float2 d[V / 2], x[V / 2];
+#pragma unroll
+      for (int v = 0; v < V / 2; ++v) {
+        d[v] = __fadd2_rn(dt.pair(v), *reinterpret_cast<const float2 *>(bias + 2 * v));
+        if (a.softplus) d[v] = softplus2(d[v]);
+        x[v] = __fmul2_rn(d[v], u.pair(v));
+      }
+#pragma unroll
+      for (int v = 0; v < V / 2; v += 2) {
+        *reinterpret_cast<float4 *>(od + 2 * v) = make_float4(d[v].x, d[v].y, d[v + 1].x, d[v + 1].y);
+        *reinterpret_cast<float4 *>(ox + 2 * v) = make_float4(x[v].x, x[v].y, x[v + 1].x, x[v + 1].y);
+      }
+    };
+    auto finish = [&](int i) {
+      const Raw<T, V> u = take(i, 0), z = take(i, 2);
+      const float *from = sy + i % 2 * RP * L::kYRow + vr * L::kYRow + vc;
+      float2 o[V / 2];
+#pragma unroll
+      for (int v = 0; v < V / 2; ++v)
+        o[v] = __fmul2_rn(*reinterpret_cast<const float2 *>(skip + 2 * v), u.pair(v));
+#pragma unroll
+      for (int q = 0; q < LS; ++q)
+#pragma unroll
+        for (int v = 0; v < V / 2; v += 2) {
+          const float4 y4 = *reinterpret_cast<const float4 *>(from + q * L::kYLane + 2 * v);
+          o[v] = __fadd2_rn(o[v], make_float2(y4.x, y4.y));
+          o[v + 1] = __fadd2_rn(o[v + 1], make_float2(y4.z, y4.w));
+        }
+      Raw<T, V> out;
+#pragma unroll
+      for (int v = 0; v < V / 2; ++v) {
+        if (pz) o[v] = __fmul2_rn(o[v], silu2(z.pair(v)));
+        out.set(v, o[v]);
+      }
+      out.template store<kWide>(py, i * RP < last ? vcount : 0);
+      py += so;
+    };
+    auto ready = [&]() {
+      if constexpr (kWide) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    };
+#pragma unroll 1
+    for (int i = 0; i < kRing - 1; ++i) {
+      fetch(i);
+      landed(i);
+    }
+    load_bc(0, 0);
+    ready();
+    stage(0);
+#pragma unroll 1
+    for (int base = 0; base < kItems; base += kBatch * 32) {
+      if (base > 0) load_bc(0, base);
+      store_bc(0, base);
+    }
+    meet(pair);
+#pragma unroll 1
+    for (int i = 0; i <= pieces; ++i) {
+      const bool more = i + 1 < pieces;
+      if (more) load_bc(i + 1, 0);
+      if (!kLocal && i > 0) finish(i - 1);
+      fetch(i + kRing - 1);
+      if (more) {
+        ready();
+        stage(i + 1);
+#pragma unroll 1
+        for (int base = 0; base < kItems; base += kBatch * 32) {
+          if (base > 0) load_bc(i + 1, base);
+          store_bc(i + 1, base);
         }
       }
-      float y[CH];
-      const float4 B4 = *reinterpret_cast<const float4 *>(sB + t * NP + n0);
+      landed(i + kRing - 1);
+      meet(pair);
+    }
+    return;
+  }
+
+  // ---- the recurrence
+  const int sl = lane % LS, n0 = sl * 4, ch0 = lane / LS * CH, count = nc - ch0;
+  const int64_t at = c0 + ch0, state0 = (w.b * a.chunks + w.k) * a.channels + at;
+  float2 A2[PAIRS][4], h[PAIRS][4], dsum[PAIRS];
+  load_states(A2, a, a.A + at * a.states, n0, count);
+#pragma unroll
+  for (int p = 0; p < PAIRS; ++p) {
+    dsum[p] = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) A2[p][i] = __fmul2_rn(A2[p][i], make_float2(kLog2e, kLog2e));
+  }
+  const float *start = nullptr;
+  if (!kPacked && w.k == 0) start = a.state ? a.state + (w.b * a.channels + at) * a.states : nullptr;
+  else if (!kLocal && w.k > 0) start = a.carry + state0 * a.states;
+  load_states(h, a, start, n0, count);
+  uint32_t opens = 0;
+  meet(pair);
+#pragma unroll 1
+  for (int i = 0; i <= pieces; ++i) {
+    if (i == pieces) {
+      meet(pair);
+      break;
+    }
+    const int64_t row0 = w.r0 + (int64_t)i * RP;
+    const int rows = (int)min((int64_t)RP, w.r1 - row0);
+    const int in_tile = (int)(row0 % kTile);
+    if (in_tile == 0) {
+      if (kPacked) opens = opens_mask(a, row0, lane);
+      if (!kLocal && a.marks) {
+        const int64_t marks = (a.rows + kTile - 1) / kTile;
+        store_states(h, a, a.marks + ((w.b * marks + row0 / kTile) * a.channels + at) * a.states, n0,
+                     count);
+      }
+    }
+    const float *sd = sdx + i % 2 * 2 * RP * L::kRow + ch0, *sx = sd + RP * L::kRow;
+    const float4 *sB = reinterpret_cast<const float4 *>(sbc + i % 2 * 2 * L::kBC) + sl,
+                 *sC = sB + RP * LS;
+    float *to = sy + i % 2 * RP * L::kYRow + sl * L::kYLane + ch0;
+    auto open = [&](int t) {
+      const int64_t r = row0 + t;
+      const int s = a.row_seq[r], before = r > 0 ? a.row_seq[r - 1] : -1;
+      if (!kLocal && a.last && before >= 0)
+        store_states(h, a, a.last + (before * a.channels + at) * a.states, n0, count);
+      load_states(h, a, a.state && s >= 0 ? a.state + (s * a.channels + at) * a.states : nullptr,
+                  n0, count);
+#pragma unroll
+      for (int p = 0; p < PAIRS; ++p) dsum[p] = make_float2(0.f, 0.f);
+    };
+    auto step = [&](int t, float2 (&y)[PAIRS]) {
+      float2 d[PAIRS], x[PAIRS];
+      if constexpr (CH == 4) {
+        const float4 d4 = *reinterpret_cast<const float4 *>(sd + t * L::kRow);
+        const float4 x4 = *reinterpret_cast<const float4 *>(sx + t * L::kRow);
+        d[0] = make_float2(d4.x, d4.y), d[PAIRS - 1] = make_float2(d4.z, d4.w);
+        x[0] = make_float2(x4.x, x4.y), x[PAIRS - 1] = make_float2(x4.z, x4.w);
+      } else {
+        d[0] = *reinterpret_cast<const float2 *>(sd + t * L::kRow);
+        x[0] = *reinterpret_cast<const float2 *>(sx + t * L::kRow);
+      }
+      const float4 B4 = sB[t * LS];
       const float B[4] = {B4.x, B4.y, B4.z, B4.w};
-      float C[4] = {};
-      if (!kLocal) {
-        const float4 C4 = *reinterpret_cast<const float4 *>(sC + t * NP + n0);
-        C[0] = C4.x, C[1] = C4.y, C[2] = C4.z, C[3] = C4.w;
-      }
+      float4 C4 = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (!kLocal) C4 = sC[t * LS];
+      const float C[4] = {C4.x, C4.y, C4.z, C4.w};
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const float d = sd[t * DB + ch0 + c], x = sx[t * DB + ch0 + c];
-        y[c] = 0.f;
-        if (kLocal) dsum[c] += d;
+      for (int p = 0; p < PAIRS; ++p) {
+        if (kLocal) dsum[p] = __fadd2_rn(dsum[p], d[p]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h[c][i] = fmaf(exp2_fast(d * A2[c][i]), h[c][i], x * B[i]);
-          if (!kLocal) y[c] = fmaf(C[i], h[c][i], y[c]);
+        for (int j = 0; j < 4; ++j) {
+          const float2 e = __fmul2_rn(d[p], A2[p][j]);
+          h[p][j] = __ffma2_rn(make_float2(exp2_fast(e.x), exp2_fast(e.y)), h[p][j],
+                               __fmul2_rn(x[p], make_float2(B[j], B[j])));
+          if (kLocal) continue;
+          const float2 c = make_float2(C[j], C[j]);
+          y[p] = j == 0 ? __fmul2_rn(c, h[p][j]) : __ffma2_rn(c, h[p][j], y[p]);
         }
       }
-      if (!kLocal) {
-        reduce_scatter<CH, LS, 1>(y, lane);
-        __syncwarp();
-        constexpr int held = CH > LS ? CH / LS : 1;
-        if (owner_of<CH, LS>(sl)) {
-          const int at = t * DB + ch0 + first_of<CH, LS>(sl);
+    };
+    auto share = [&](int t, const float2 (&y)[PAIRS]) {
+      if constexpr (CH == 4)
+        *reinterpret_cast<float4 *>(to + t * L::kYRow) =
+            make_float4(y[0].x, y[0].y, y[PAIRS - 1].x, y[PAIRS - 1].y);
+      else
+        *reinterpret_cast<float2 *>(to + t * L::kYRow) = y[0];
+    };
+    if (rows < RP || (kPacked && (opens >> in_tile) << (32 - RP) != 0)) {
+      for (int t = 0; t < rows; ++t) {
+        if (kPacked && (opens >> (in_tile + t) & 1)) open(t);
+        float2 y[PAIRS];
+        step(t, y);
+        if (!kLocal) share(t, y);
+      }
+    } else {
+      // a few rows at a time, their loads ahead of all stores
+      constexpr int R = 4;
+#pragma unroll 1
+      for (int t = 0; t < RP; t += R) {
+        float2 y[R][PAIRS];
 #pragma unroll
-          for (int i = 0; i < held; ++i) sx[at + i] = y[i];
+        for (int j = 0; j < R; ++j) step(t + j, y[j]);
+        if constexpr (!kLocal) {
+#pragma unroll
+          for (int j = 0; j < R; ++j) share(t + j, y[j]);
         }
       }
     }
-    if (kLocal) continue;
-    __syncthreads();
-    for (int e = threadIdx.x; e < rows * DB; e += kScanThreads) {
-      const int t = e / DB, c = e % DB;
-      if (c >= w.nc) continue;
-      float o = sx[e];
-      if (a.skip) o = fmaf(a.skip[w.c0 + c], to_f(a.u.at(w.b, row0 + t)[w.c0 + c]), o);
-      if (a.gate.p) o *= silu(to_f(a.gate.at(w.b, row0 + t)[w.c0 + c]));
-      a.y.at(w.b, row0 + t)[w.c0 + c] = from_f<T>(o);
-    }
+    meet(pair);
   }
   if (kLocal) {
+    store_states(h, a, a.carry + state0 * a.states, n0, count);
+    if (sl == 0)
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      if (ch0 + c >= w.nc) continue;
-      store4(a.carry + (state0 + ch0 + c) * a.states, h[c], n0, a.states);
-      if (sl == 0) a.sum_d[state0 + ch0 + c] = dsum[c];
-    }
+      for (int p = 0; p < PAIRS; ++p) {
+        if (2 * p < count) a.sum_d[state0 + 2 * p] = dsum[p].x;
+        if (2 * p + 1 < count) a.sum_d[state0 + 2 * p + 1] = dsum[p].y;
+      }
   } else if (a.last && w.r1 == a.rows) {
     const int s = kPacked ? a.row_seq[a.rows - 1] : (int)w.b;
-    if (s >= 0) {
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-        if (ch0 + c < w.nc)
-          store4(a.last + (s * a.channels + w.c0 + ch0 + c) * a.states, h[c], n0, a.states);
-    }
+    if (s >= 0) store_states(h, a, a.last + (s * a.channels + at) * a.states, n0, count);
   }
 }
 
@@ -757,13 +1028,12 @@ __global__ void sum_bc_kernel(ScanArgs<T> a) {
 // ------------------------------------------------------------- host side
 enum ScanCall { kScan, kScanGrad, kScanStep };
 
-// The channels of a block by the lanes over the states: forward and gradient.
-constexpr int scan_ch(int ls) { return ls < 4 ? ls : 4; }
-constexpr int grad_ch(int ls) { return ls < 2 ? 1 : 2; }
+// The channels of a gradient block by the lanes over the states.
+constexpr int grad_ch(int) { return 2; }
 constexpr int block_channels(int ls, int ch) { return kWarps * (32 / ls) * ch; }
 
 inline int lanes_of(int64_t states) {
-  int ls = 1;
+  int ls = 2;
   while (ls * 4 < states) ls *= 2;
   return ls;
 }

@@ -34,6 +34,17 @@ ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, bool grad) 
   a.chunks = p.chunks;
   a.softplus = s.softplus;
   if (!grad) a.y = rows_of<T>(s.y);
+  auto whole = [&](const void *q) { return (uintptr_t)q % 16 == 0; };
+  a.wide_states = s.states % 4 == 0 && whole(s.A) && whole(s.state) && whole(s.last) &&
+                  whole(s.marks) && whole(s.workspace) && whole(s.dlast) && whole(s.dstate);
+  const int64_t batches = p.batches, rows = s.rows;
+  a.wide_bc = s.states % 4 == 0 && rows_aligned(s.B, s.type, batches, rows, 4 * sizeof(T)) &&
+              rows_aligned(s.C, s.type, batches, rows, 4 * sizeof(T));
+  constexpr int most = 8;  // values of a word of rows, at most 16 bytes
+  const int word = std::min<int>(16, most * sizeof(T));
+  a.wide = p.per_group % most == 0;
+  for (const tcu_seq_rows *r : {&s.u, &s.dt, &s.gate, &s.y})
+    a.wide = a.wide && rows_aligned(*r, s.type, batches, rows, word);
   float *w = static_cast<float *>(s.workspace);
   a.carry = w;
   a.sum_d = a.carry + p.carry;
@@ -56,7 +67,7 @@ ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, bool grad) 
 }
 
 template <auto *kernel, typename T>
-int start(int64_t blocks, int floats, const ScanArgs<T> &a, cudaStream_t st) {
+int start(int64_t blocks, int threads, int floats, const ScanArgs<T> &a, cudaStream_t st) {
   if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
   const int bytes = floats * 4;
   if (bytes > 48 * 1024 &&
@@ -65,22 +76,23 @@ int start(int64_t blocks, int floats, const ScanArgs<T> &a, cudaStream_t st) {
     cudaGetLastError();
     return TCU_DFT_ERR_CUDA;
   }
-  kernel<<<(unsigned)blocks, kScanThreads, bytes, st>>>(a);
+  kernel<<<(unsigned)blocks, threads, bytes, st>>>(a);
   return launched();
 }
 
-template <typename T, int LS, bool kPacked>
+template <typename T, int LS, bool kPacked, bool kWide>
 int forward(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
-  using P = Shape<LS, scan_ch(LS)>;
-  constexpr int floats = kTile * (P::kChannels * 2 + P::kStates * 2);
   const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
+  constexpr int floats = Lay<LS, T>::kFloats;
   if (p.chunks > 1) {
-    if (const int rc = start<scan_kernel<T, P, kPacked, true>>(blocks, floats, a, st)) return rc;
+    if (const int rc = start<scan_kernel<T, LS, kPacked, true, kWide>>(blocks, Lay<LS, T>::kBlock, floats,
+                                                                      a, st))
+      return rc;
     const int64_t count = a.channels * a.states * p.batches;
     carry_kernel<T, false><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
     if (const int rc = launched()) return rc;
   }
-  return start<scan_kernel<T, P, kPacked, false>>(blocks, floats, a, st);
+  return start<scan_kernel<T, LS, kPacked, false, kWide>>(blocks, Lay<LS, T>::kBlock, floats, a, st);
 }
 
 template <typename T, int LS, bool kPacked>
@@ -89,12 +101,12 @@ int gradient(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
   const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
   if (p.chunks > 1) {
     constexpr int floats = kTile * (P::kChannels * 2 + P::kStates);
-    if (const int rc = start<adjoint_kernel<T, P, kPacked>>(blocks, floats, a, st)) return rc;
+    if (const int rc = start<adjoint_kernel<T, P, kPacked>>(blocks, kScanThreads, floats, a, st)) return rc;
     const int64_t count = a.channels * a.states * p.batches;
     carry_kernel<T, true><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
     if (const int rc = launched()) return rc;
   }
-  return start<scan_grad_kernel<T, P, kPacked>>(blocks, grad_floats<P>(), a, st);
+  return start<scan_grad_kernel<T, P, kPacked>>(blocks, kScanThreads, grad_floats<P>(), a, st);
 }
 
 template <typename T, int LS>
@@ -106,8 +118,11 @@ int by_lanes(ScanCall call, const ScanPlan &p, const ScanArgs<T> &a, cudaStream_
     scan_step_kernel<T, LS><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
     return launched();
   }
-  if (call == kScan)
-    return a.row_seq ? forward<T, LS, true>(p, a, st) : forward<T, LS, false>(p, a, st);
+  if (call == kScan) {
+    if (a.row_seq)
+      return a.wide ? forward<T, LS, true, true>(p, a, st) : forward<T, LS, true, false>(p, a, st);
+    return a.wide ? forward<T, LS, false, true>(p, a, st) : forward<T, LS, false, false>(p, a, st);
+  }
   return a.row_seq ? gradient<T, LS, true>(p, a, st) : gradient<T, LS, false>(p, a, st);
 }
 
@@ -124,7 +139,6 @@ int run_scan(ScanCall call, const tcu_state_scan_args &s, cudaStream_t st) {
   const bool none = call != kScanStep && (p.batches == 0 || s.rows == 0);
   if (none) rc = TCU_DFT_OK;
   else switch (p.ls) {
-    case 1: rc = by_lanes<T, 1>(call, p, a, st); break;
     case 2: rc = by_lanes<T, 2>(call, p, a, st); break;
     case 4: rc = by_lanes<T, 4>(call, p, a, st); break;
     case 8: rc = by_lanes<T, 8>(call, p, a, st); break;
