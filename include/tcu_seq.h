@@ -97,7 +97,7 @@ int tcu_short_conv_step(const tcu_short_conv_args *a, void *stream);
  * entries x ceil(rows / TCU_SEQ_MARK) x channels x states (batch entries:
  * sequences when dense, 1 when packed), written by the scan when not NULL
  * and read by its gradient. */
-enum { TCU_SEQ_MARK = 32 };
+enum { TCU_SEQ_MARK = 16 };
 typedef struct {
   int32_t type, softplus, sequences, groups;
   int64_t rows, channels, states;

@@ -16,27 +16,29 @@ ScanPlan plan_of(const tcu_state_scan_args &a, bool grad) {
   ScanPlan p{};
   p.batches = a.offsets ? 1 : a.sequences;
   p.ls = lanes_of(a.states);
-  p.db = grad ? block_channels(p.ls, grad_ch(p.ls)) : scan_channels(p.ls);
+  p.db = grad ? grad_channels(p.ls) : scan_channels(p.ls);
   p.per_group = (int)(a.channels / a.groups);
   p.group_blocks = (p.per_group + p.db - 1) / p.db;
   const int64_t blocks = p.batches * a.groups * p.group_blocks;
   const int64_t tiles = (a.rows + kTile - 1) / kTile;
   // Where the blocks leave more than half of the card's slots empty, rows are
   // split so that all blocks run at once.
-  const int64_t slots = (grad ? 3 : scan_resident(p.ls)) * (int64_t)num_sms();
+  const int64_t slots = (grad ? grad_resident(p.ls) : scan_resident(p.ls)) * (int64_t)num_sms();
   int64_t chunks = blocks == 0 || blocks * 2 > slots ? 1 : slots / blocks;
   chunks = std::max<int64_t>(1, std::min(chunks, tiles / 2));
   const int64_t chunk_tiles = std::max<int64_t>(1, (tiles + chunks - 1) / chunks);
   p.chunk_rows = chunk_tiles * kTile;
   p.chunks = (int)std::max<int64_t>(1, (a.rows + p.chunk_rows - 1) / p.chunk_rows);
   const int64_t parts = p.batches * p.chunks * a.channels;
-  p.carry = p.chunks > 1 ? parts * a.states : 0;
-  p.sum_d = p.chunks > 1 ? parts : 0;
-  p.row_seq = a.offsets ? a.rows : 0;
+  // each a multiple of 16 bytes, so that all are aligned if the workspace is
+  auto whole = [](int64_t floats) { return (floats + 3) / 4 * 4; };
+  p.carry = p.chunks > 1 ? whole(parts * a.states) : 0;
+  p.sum_d = p.chunks > 1 ? whole(parts) : 0;
+  p.row_seq = a.offsets ? whole(a.rows) : 0;
   if (grad) {
-    p.bc_parts = p.batches * a.rows * a.groups * 2 * a.states * p.group_blocks;
-    p.A_parts = parts * a.states;
-    p.vec_parts = parts;
+    p.bc_parts = whole(p.batches * a.rows * a.groups * 2 * a.states * p.group_blocks);
+    p.A_parts = whole(parts * a.states);
+    p.vec_parts = whole(parts);
   }
   return p;
 }

@@ -37,15 +37,15 @@
 #include <algorithm>
 
 #include "seq_common.cuh"
+#include "tcgen05.cuh"
 
 namespace tcu {
 namespace seq {
 
 constexpr int kWarps = 4;
 constexpr int kScanThreads = 32 * kWarps;
-constexpr int kTile = TCU_SEQ_MARK;  // rows of a tile: a warp's ballot covers it
-constexpr int kSub = 4;              // rows whose states a gradient thread holds
-static_assert(kTile == 32, "masks of a tile's rows are 32-bit");
+constexpr int kTile = 32;             // rows of a forward tile: a warp's ballot
+constexpr int kMark = TCU_SEQ_MARK;   // rows of a gradient tile
 
 template <typename T>
 struct ScanArgs {
@@ -57,7 +57,7 @@ struct ScanArgs {
   float *carry;    // [batch][chunk][channels][states]: state that enters a chunk
   float *sum_d;    // [batch][chunk][channels]
   int32_t *row_seq;
-  float *bc_parts;  // [channel block of a group][batch][row][group][dB, dC][states]
+  float *bc_parts;  // [block of a group's channels][batch][row][group][dB, dC][states]
   float *A_parts;   // [batch][chunk][channels][states]
   float *skip_parts, *bias_parts;  // [batch][chunk][channels]
   const int32_t *offsets, *slots;
@@ -497,16 +497,16 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     const int in_tile = (int)(row0 % kTile);
     if (in_tile == 0) {
       if (kPacked) opens = opens_mask(a, row0, lane);
-      if (!kLocal && a.marks) {
-        const int64_t marks = (a.rows + kTile - 1) / kTile;
-        store_states(h, a, a.marks + ((w.b * marks + row0 / kTile) * a.channels + at) * a.states, n0,
-                     count);
-      }
     }
     const float *sd = sdx + i % 2 * 2 * RP * L::kRow + ch0, *sx = sd + RP * L::kRow;
     const float4 *sB = reinterpret_cast<const float4 *>(sbc + i % 2 * 2 * L::kBC) + sl,
                  *sC = sB + RP * LS;
     float *to = sy + i % 2 * RP * L::kYRow + sl * L::kYLane + ch0;
+    auto mark = [&](int t) {
+      if (kLocal || !a.marks || (in_tile + t) % kMark != 0) return;
+      const int64_t marks = (a.rows + kMark - 1) / kMark, m = (row0 + t) / kMark;
+      store_states(h, a, a.marks + ((w.b * marks + m) * a.channels + at) * a.states, n0, count);
+    };
     auto open = [&](int t) {
       const int64_t r = row0 + t;
       const int s = a.row_seq[r], before = r > 0 ? a.row_seq[r - 1] : -1;
@@ -556,6 +556,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     };
     if (rows < RP || (kPacked && (opens >> in_tile) << (32 - RP) != 0)) {
       for (int t = 0; t < rows; ++t) {
+        mark(t);
         if (kPacked && (opens >> (in_tile + t) & 1)) open(t);
         float2 y[PAIRS];
         step(t, y);
@@ -566,6 +567,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       constexpr int R = 4;
 #pragma unroll 1
       for (int t = 0; t < RP; t += R) {
+        mark(t);
         float2 y[R][PAIRS];
 #pragma unroll
         for (int j = 0; j < R; ++j) step(t + j, y[j]);
@@ -734,280 +736,424 @@ __global__ void __launch_bounds__(kScanThreads) adjoint_kernel(ScanArgs<T> a) {
   }
 }
 
-// Shared memory of the gradient kernel, in floats.
-template <class P>
-constexpr int grad_floats() {
-  return kTile * P::kChannels * 3 + kTile * P::kStates * 2 +
-         kTile / kSub * P::CH * 4 * kScanThreads + kWarps * kTile * P::kStates * 2;
+// How the gradient kernel is laid out: blocks of four pairs of warps, as the
+// forward kernel's, over tiles of kMark rows from the last to the first.  The
+// first warp of a pair recomputes a tile's states from its mark, down the
+// rows, and puts each into tensor memory, its own lane's columns -- 16 rows x
+// 16 states of fp32 a thread are more than its registers or shared memory hold
+// -- then walks the adjoint up.  The second warp turns u, dt, gate, dy into d,
+// d u, q for the next tile and the sums o, r, v (in their places) into du,
+// ddt, dgate for the one before.  Two blocks fill an SM and its tensor memory.
+template <int LS_, typename T>
+struct GradLay {
+  static constexpr int LS = LS_, CH = scan_ch(LS), NP = 4 * LS, E = 4 * CH, CL = 32 / LS;
+  static constexpr int kPairs = 4, kBlock = 64 * kPairs;
+  static constexpr int WC = CL * CH, DB = kPairs * WC;
+  static constexpr int V = LS <= 8 ? 8 : LS == 16 ? 4 : 2;
+  static constexpr int COLS = WC / V, RP = 32 / COLS, PASSES = kMark / RP;
+  static constexpr int kColumns = kMark * E;  // of tensor memory
+  // shared memory, in floats
+  static constexpr int kRow = WC + 4;
+  static constexpr int kPlane = kMark * kRow;         // d, d u or q of a tile
+  static constexpr int kBC = kMark * NP;              // B or C of a tile
+  static constexpr int kPairFloats = 2 * (3 * kPlane + 2 * kBC) + 2 * WC;
+  static constexpr int kThreadFloats = 2 * E;         // a first warp's thread: mark, sum of dA
+  static constexpr int kFloats = 4 + 4 * kBC + kPairs * (kPairFloats + 32 * kThreadFloats);
+};
+constexpr int kFlush = 16;  // tiles whose shares of dA are summed before they join the rest
+constexpr int grad_channels(int ls) { return 4 * (32 / ls) * scan_ch(ls); }
+constexpr int grad_resident(int ls) { return ls <= 8 ? 2 : 1; }
+
+template <int E>
+__device__ __forceinline__ void tmem_put(uint32_t at, const float2 (&h)[E / 8][4]) {
+  float v[E];
+#pragma unroll
+  for (int i = 0; i < E / 2; ++i) v[2 * i] = h[i / 4][i % 4].x, v[2 * i + 1] = h[i / 4][i % 4].y;
+  if constexpr (E == 16) tmem_st16(at, v);
+  else tmem_st8u(at, reinterpret_cast<const uint32_t *>(v));
+}
+template <int E>
+__device__ __forceinline__ void tmem_get(uint32_t at, float2 (&h)[E / 8][4]) {
+  float v[E];
+  if constexpr (E == 16) tmem_ld16(at, v);
+  else tmem_ld8(at, v);
+#pragma unroll
+  for (int i = 0; i < E / 2; ++i) h[i / 4][i % 4] = make_float2(v[2 * i], v[2 * i + 1]);
 }
 
-// The gradient over a chunk.  Tiles from the last to the first: the states of
-// a tile are recomputed from its mark, keeping every kSub-th in shared memory
-// (each thread its own); then kSub rows at a time from those, with states and
-// decays in registers, the adjoint walks up.
-template <typename T, class P, bool kPacked>
-__global__ void __launch_bounds__(kScanThreads) scan_grad_kernel(ScanArgs<T> a) {
-  constexpr int LS = P::LS, CH = P::CH, NP = P::kStates, DB = P::kChannels;
-  constexpr int CL = 32 / LS, E = CH * 4;
+template <typename T, int LS, bool kPacked, bool kWide>
+__global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanArgs<T> a) {
+  using L = GradLay<LS, T>;
+  constexpr int CH = L::CH, PAIRS = CH / 2, V = L::V, E = L::E;
   extern __shared__ __align__(16) float smem[];
-  float *sd = smem, *sx = sd + kTile * DB, *sq = sx + kTile * DB, *sB = sq + kTile * DB,
-        *sC = sB + kTile * NP, *snap = sC + kTile * NP, *sbc = snap + kTile / kSub * E * kScanThreads;
-  const Place<DB, T> w(a);
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int sl = lane % LS, n0 = sl * 4;
-  const int ch0 = warp * P::kWarpChannels + lane / LS * CH;
-  float A2[CH][4], dA[CH][4], e[CH][4];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, pair = warp % L::kPairs;
+  float *sBC = smem + 4;                                       // [2][B, C][row][states]
+  float *own = sBC + 4 * L::kBC + pair * L::kPairFloats;
+  float *sdxq = own;                                           // [2][d, x, q][row][kRow]
+  float *ssum = own + 6 * L::kPlane;                           // [2][row][dB, dC][states]
+  float *sbias = ssum + 4 * L::kBC, *sskip = sbias + L::WC;
+  const Place<L::DB, T> w(a);
+  const int64_t c0 = w.c0 + pair * L::WC;
+  const int nc = w.nc - pair * L::WC;
+  const int tiles = (int)((w.r1 - w.r0 + kMark - 1) / kMark);
   const int64_t part = w.b * a.chunks + w.k;
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) A2[c][i] = e[c][i] = dA[c][i] = 0.f;
-    if (ch0 + c >= w.nc) continue;
-    const int64_t at = w.c0 + ch0 + c;
-    load4(A2[c], a.A + at * a.states, n0, a.states);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) A2[c][i] *= kLog2e;
-    if (w.r1 < a.rows)
-      load4(e[c], a.carry + (part * a.channels + at) * a.states, n0, a.states);
-    else if (!kPacked && a.dlast)
-      load4(e[c], a.dlast + (w.b * a.channels + at) * a.states, n0, a.states);
-  }
-  // the epilogue's thread owns one channel (or shares it with others, DB < threads)
-  const int ec = threadIdx.x % DB;
-  float dskip = 0.f, dbias = 0.f;
-  const int64_t marks = (a.rows + kTile - 1) / kTile;
-  const int64_t tiles = (w.r1 - w.r0 + kTile - 1) / kTile;
-  for (int64_t tile = tiles - 1; tile >= 0; --tile) {
-    const int64_t row0 = w.r0 + tile * kTile;
-    const int rows = (int)min((int64_t)kTile, w.r1 - row0);
-    __syncthreads();
-    for (int i = threadIdx.x; i < kTile * DB; i += kScanThreads) {
-      const int t = i / DB, c = i % DB;
-      float d = 0.f, x = 0.f, q = 0.f;
-      if (t < rows && c < w.nc) {
-        d = step_of(a, to_f(a.dt.at(w.b, row0 + t)[w.c0 + c]),
-                    a.dt_bias ? a.dt_bias[w.c0 + c] : 0.f);
-        x = d * to_f(a.u.at(w.b, row0 + t)[w.c0 + c]);
-        q = to_f(a.dy.at(w.b, row0 + t)[w.c0 + c]);
-        if (a.gate.p) q *= silu(to_f(a.gate.at(w.b, row0 + t)[w.c0 + c]));
-      }
-      sd[i] = d;
-      sx[i] = x;
-      sq[i] = q;
+  // the i-th tile of the walk up, and its rows
+  auto row_of = [&](int i) { return w.r0 + (int64_t)(tiles - 1 - i) * kMark; };
+  if (warp == 0) tmem_alloc(smem_u32(smem), L::kColumns);
+
+  if (warp >= L::kPairs) {
+    // ---- rows in and out
+    const int vr = lane / L::COLS, vc = lane % L::COLS * V, vcount = min(V, nc - vc);
+    const int me = threadIdx.x - 32 * L::kPairs;  // of the second warps
+    for (int c = lane; c < L::WC; c += 32) {
+      sbias[c] = a.dt_bias && c < nc ? a.dt_bias[c0 + c] : 0.f;
+      sskip[c] = a.skip && c < nc ? a.skip[c0 + c] : 0.f;
     }
-    stage_bc<NP>(a, w.b, w.g, row0, rows, sB, sC);
+    __syncwarp();
+    const float *bias = sbias + vc, *skip = sskip + vc;
+    const bool gated = a.gate.p != nullptr;
+    float2 dskip[V / 2], dbias[V / 2];
+#pragma unroll
+    for (int v = 0; v < V / 2; ++v) dskip[v] = dbias[v] = make_float2(0.f, 0.f);
+    struct {
+      Raw<T, V> u, dt, z, dy;
+    } in;
+    auto load = [&](int i, int pass) {
+      const int64_t r = row_of(i) + pass * L::RP + vr;
+      const int count = r < w.r1 ? vcount : 0;
+      in.u.template load<kWide>(a.u.at(w.b, r) + c0 + vc, count);
+      in.dt.template load<kWide>(a.dt.at(w.b, r) + c0 + vc, count);
+      if (gated) in.z.template load<kWide>(a.gate.at(w.b, r) + c0 + vc, count);
+      in.dy.template load<kWide>(a.dy.at(w.b, r) + c0 + vc, count);
+    };
+    auto stage = [&](int i, int pass) {
+      float *o = sdxq + i % 2 * 3 * L::kPlane + (pass * L::RP + vr) * L::kRow + vc;
+#pragma unroll
+      for (int v = 0; v < V / 2; ++v) {
+        float2 d = __fadd2_rn(in.dt.pair(v), *reinterpret_cast<const float2 *>(bias + 2 * v));
+        if (a.softplus) d = softplus2(d);
+        float2 q = in.dy.pair(v);
+        if (gated) q = __fmul2_rn(q, silu2(in.z.pair(v)));
+        *reinterpret_cast<float2 *>(o + 2 * v) = d;
+        *reinterpret_cast<float2 *>(o + L::kPlane + 2 * v) = __fmul2_rn(d, in.u.pair(v));
+        *reinterpret_cast<float2 *>(o + 2 * L::kPlane + 2 * v) = q;
+      }
+    };
+    auto finish = [&](int i, int pass) {
+      const float *from = sdxq + i % 2 * 3 * L::kPlane + (pass * L::RP + vr) * L::kRow + vc;
+      const int64_t r = row_of(i) + pass * L::RP + vr;
+      const int count = r < w.r1 ? vcount : 0;
+      Raw<T, V> du, ddt, dz;
+#pragma unroll
+      for (int k = 0; k < V / 2; ++k) {
+        const float2 v = *reinterpret_cast<const float2 *>(from + 2 * k);
+        const float2 o = *reinterpret_cast<const float2 *>(from + L::kPlane + 2 * k);
+        const float2 rr = *reinterpret_cast<const float2 *>(from + 2 * L::kPlane + 2 * k);
+        const float2 s2 = *reinterpret_cast<const float2 *>(skip + 2 * k);
+        const float2 u = in.u.pair(k), dy = in.dy.pair(k);
+        const float2 raw = __fadd2_rn(in.dt.pair(k), *reinterpret_cast<const float2 *>(bias + 2 * k));
+        const float2 d = a.softplus ? softplus2(raw) : raw;
+        float2 q = dy;
+        if (gated) {
+          const float2 z = in.z.pair(k);
+          const float2 s = make_float2(sigmoid(z.x), sigmoid(z.y));
+          const float2 zs = __fmul2_rn(z, s);
+          q = __fmul2_rn(dy, zs);
+          // (z s)' = s + z s (1 - s)
+          const float2 ds = __ffma2_rn(zs, make_float2(1.f - s.x, 1.f - s.y), s);
+          dz.set(k, __fmul2_rn(__fmul2_rn(dy, __ffma2_rn(s2, u, o)), ds));
+        }
+        // v carries log2 e from A2
+        float2 g = __ffma2_rn(rr, u, __fmul2_rn(v, make_float2(kLn2, kLn2)));
+        if (a.softplus) g = __fmul2_rn(g, make_float2(sigmoid(raw.x), sigmoid(raw.y)));
+        du.set(k, __ffma2_rn(rr, d, __fmul2_rn(s2, q)));
+        ddt.set(k, g);
+        if (count > 0) {
+          dskip[k] = __ffma2_rn(q, u, dskip[k]);
+          dbias[k] = __fadd2_rn(dbias[k], g);
+        }
+      }
+      du.template store<kWide>(a.du.at(w.b, r) + c0 + vc, count);
+      ddt.template store<kWide>(a.ddt.at(w.b, r) + c0 + vc, count);
+      if (gated && a.dgate.p) dz.template store<kWide>(a.dgate.at(w.b, r) + c0 + vc, count);
+    };
+    auto stage_bc = [&](int i) {
+      constexpr int items = kMark * LS;  // quads of B, then of C
+      const int64_t row0 = row_of(i);
+      for (int item = me; item < 2 * items; item += 32 * L::kPairs) {
+        const int which = item / items, t = item % items / LS, n = item % LS * 4;
+        const Rows<const T> &src = which ? a.C : a.B;
+        const int64_t r = row0 + t;
+        const int count = r < w.r1 ? min(4, a.states - n) : 0;
+        const T *from = src.at(w.b, r) + (int64_t)w.g * a.states + n;
+        Raw<T, 4> q;
+        if (a.wide_bc) q.template load<true>(from, count);
+        else q.template load<false>(from, count);
+        const float2 v0 = q.pair(0), v1 = q.pair(1);
+        reinterpret_cast<float4 *>(sBC + i % 2 * 2 * L::kBC)[item] =
+            make_float4(v0.x, v0.y, v1.x, v1.y);
+      }
+    };
+    // the block's shares of dB, dC: its four first warps' sums, in order
+    auto share_bc = [&](int i) {
+      const int64_t row0 = row_of(i);
+      const int rows = (int)min((int64_t)kMark, w.r1 - row0);
+      const float *from = sBC + 4 * L::kBC + 6 * L::kPlane + i % 2 * 2 * L::kBC;
+      const int live = min(L::kPairs, (w.nc + L::WC - 1) / L::WC);
+      for (int j = me; j < rows * 2 * L::NP; j += 32 * L::kPairs) {
+        const int n = j % L::NP, which = j / L::NP % 2, t = j / (2 * L::NP);
+        if (n >= a.states) continue;
+        float s = 0.f;
+        for (int k = 0; k < live; ++k) s += from[k * L::kPairFloats + j];
+        a.bc_parts[((((int64_t)w.cb * a.batches + w.b) * a.rows + row0 + t) * a.groups + w.g) * 2 *
+                       a.states + which * a.states + n] = s;
+      }
+    };
+#pragma unroll 1
+    for (int p = 0; p < L::PASSES; ++p) {
+      load(0, p);
+      stage(0, p);
+    }
+    stage_bc(0);
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i <= tiles; ++i) {
+      if (i > 0) {
+#pragma unroll 1
+        for (int p = 0; p < L::PASSES; ++p) {
+          load(i - 1, p);
+          finish(i - 1, p);
+        }
+        share_bc(i - 1);
+      }
+      if (i + 1 < tiles) {
+#pragma unroll 1
+        for (int p = 0; p < L::PASSES; ++p) {
+          load(i + 1, p);
+          stage(i + 1, p);
+        }
+        stage_bc(i + 1);
+      }
+      __syncthreads();
+    }
+    // a channel's shares lie in the lanes of its column
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) {
+#pragma unroll
+      for (int s = L::COLS; s < 32; s *= 2) {
+        dskip[k].x += __shfl_xor_sync(~0u, dskip[k].x, s);
+        dskip[k].y += __shfl_xor_sync(~0u, dskip[k].y, s);
+        dbias[k].x += __shfl_xor_sync(~0u, dbias[k].x, s);
+        dbias[k].y += __shfl_xor_sync(~0u, dbias[k].y, s);
+      }
+      if (vr != 0) continue;
+      const int64_t at = part * a.channels + c0 + vc + 2 * k;
+      if (2 * k < vcount && a.skip_parts) a.skip_parts[at] = dskip[k].x;
+      if (2 * k + 1 < vcount && a.skip_parts) a.skip_parts[at + 1] = dskip[k].y;
+      if (2 * k < vcount && a.bias_parts) a.bias_parts[at] = dbias[k].x;
+      if (2 * k + 1 < vcount && a.bias_parts) a.bias_parts[at + 1] = dbias[k].y;
+    }
+    return;
+  }
+
+  // ---- states down, adjoint up
+  const int sl = lane % LS, n0 = sl * 4, ch0 = lane / LS * CH, count = nc - ch0;
+  const int64_t at = c0 + ch0;
+  // this thread's 16-byte slots: its mark, then its sum of dA
+  float4 *slots = reinterpret_cast<float4 *>(sBC + 4 * L::kBC + L::kPairs * L::kPairFloats) +
+                  warp * 32 * (L::kThreadFloats / 4) + lane;
+  float4 *asum = slots + 32 * (E / 4);
+  float2 A2[PAIRS][4], e[PAIRS][4], dA[PAIRS][4];
+  load_states(A2, a, a.A + at * a.states, n0, count);
+  const float *below = nullptr;
+  if (w.r1 < a.rows) below = a.carry + (part * a.channels + at) * a.states;
+  else if (!kPacked && a.dlast) below = a.dlast + (w.b * a.channels + at) * a.states;
+  load_states(e, a, below, n0, count);
+#pragma unroll
+  for (int p = 0; p < PAIRS; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      A2[p][i] = __fmul2_rn(A2[p][i], make_float2(kLog2e, kLog2e));
+      dA[p][i] = make_float2(0.f, 0.f);
+    }
+#pragma unroll
+  for (int j = 0; j < E / 4; ++j) asum[32 * j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto flush = [&]() {
+#pragma unroll
+    for (int p = 0; p < PAIRS; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        float4 *s = asum + 32 * (p * 2 + i / 2);
+        const float4 v = *s;
+        *s = make_float4(v.x + dA[p][i].x, v.y + dA[p][i].y, v.z + dA[p][i + 1].x,
+                         v.w + dA[p][i + 1].y);
+        dA[p][i] = dA[p][i + 1] = make_float2(0.f, 0.f);
+      }
+  };
+  const int64_t marks = (a.rows + kMark - 1) / kMark;
+  auto mark_of = [&](int i) {
+    return a.marks + ((w.b * marks + row_of(i) / kMark) * a.channels + at) * a.states;
+  };
+  // the mark of the i-th tile on its way, one 16-byte copy a channel
+  auto fetch_mark = [&](int i) {
+    if (!a.wide_states) return;
+    if (i < tiles && n0 < a.states) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (c < count)
+          copy_async(reinterpret_cast<uint32_t *>(slots + 32 * c),
+                     mark_of(i) + (int64_t)c * a.states + n0, 16);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int c = 0; c < CH; ++c) slots[32 * c] = make_float4(0.f, 0.f, 0.f, 0.f);
+  fetch_mark(0);
+  __syncthreads();
+  const uint32_t column = *reinterpret_cast<volatile uint32_t *>(smem) + ((uint32_t)warp << 21);
+#pragma unroll 1
+  for (int i = 0; i <= tiles; ++i) {
+    if (i == tiles) {
+      __syncthreads();
+      break;
+    }
+    const int64_t row0 = row_of(i);
+    const int rows = (int)min((int64_t)kMark, w.r1 - row0);
     const uint32_t opens = kPacked ? opens_mask(a, row0, lane) : 0;
     const uint32_t closes = kPacked ? closes_mask(a, row0, lane) : 0;
-    float h[CH][4];
+    float *sd = sdxq + i % 2 * 3 * L::kPlane, *sx = sd + L::kPlane, *sq = sx + L::kPlane;
+    const float4 *sB = reinterpret_cast<const float4 *>(sBC + i % 2 * 2 * L::kBC) + sl,
+                 *sC = sB + kMark * LS;
+    float *sum = ssum + i % 2 * 2 * L::kBC;
+    float2 h[PAIRS][4];
+    if (a.wide_states) {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[c][i] = 0.f;
-      if (ch0 + c < w.nc)
-        load4(h[c], a.marks + ((w.b * marks + row0 / kTile) * a.channels + w.c0 + ch0 + c) * a.states,
-              n0, a.states);
+      for (int p = 0; p < PAIRS; ++p) {
+        const float4 v0 = slots[32 * 2 * p], v1 = slots[32 * (2 * p + 1)];
+        h[p][0] = make_float2(v0.x, v1.x), h[p][1] = make_float2(v0.y, v1.y);
+        h[p][2] = make_float2(v0.z, v1.z), h[p][3] = make_float2(v0.w, v1.w);
+      }
+    } else {
+      load_states(h, a, mark_of(i), n0, count);
     }
-    __syncthreads();
-    auto open = [&](int t) {  // the state a sequence starts from
+    auto load2 = [&](float2 (&v)[PAIRS], const float *from, int t) {
+      if constexpr (CH == 4) {
+        const float4 q = *reinterpret_cast<const float4 *>(from + t * L::kRow + ch0);
+        v[0] = make_float2(q.x, q.y), v[PAIRS - 1] = make_float2(q.z, q.w);
+      } else {
+        v[0] = *reinterpret_cast<const float2 *>(from + t * L::kRow + ch0);
+      }
+    };
+    auto open_state = [&](float2 (&to)[PAIRS][4], int t) {
       const int s = a.row_seq[row0 + t];
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[c][i] = 0.f;
-        if (a.state && s >= 0 && ch0 + c < w.nc)
-          load4(h[c], a.state + (s * a.channels + w.c0 + ch0 + c) * a.states, n0, a.states);
-      }
+      load_states(to, a, a.state && s >= 0 ? a.state + (s * a.channels + at) * a.states : nullptr,
+                  n0, count);
     };
-    auto keep = [&](int sub) {
+    // down the rows: column block t holds the state that enters row t
+#pragma unroll 4
+    for (int t = 0; t < rows; ++t) {
+      tmem_put<E>(column + t * E, h);
+      if (kPacked && (opens >> t & 1)) open_state(h, t);
+      float2 d[PAIRS], x[PAIRS];
+      load2(d, sd, t);
+      load2(x, sx, t);
+      const float4 B4 = sB[t * LS];
+      const float B[4] = {B4.x, B4.y, B4.z, B4.w};
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
+      for (int p = 0; p < PAIRS; ++p)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          snap[(sub * E + c * 4 + i) * kScanThreads + threadIdx.x] = h[c][i];
-    };
-    const int subs = (rows + kSub - 1) / kSub;
-    for (int sub = 0; sub < subs; ++sub) {
-      keep(sub);
-      if (sub == subs - 1) break;
-#pragma unroll
-      for (int j = 0; j < kSub; ++j) {
-        const int t = sub * kSub + j;
-        if (kPacked && (opens >> t & 1)) open(t);
-        const float4 B4 = *reinterpret_cast<const float4 *>(sB + t * NP + n0);
-        const float B[4] = {B4.x, B4.y, B4.z, B4.w};
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const float d = sd[t * DB + ch0 + c], x = sx[t * DB + ch0 + c];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            h[c][i] = fmaf(exp2_fast(d * A2[c][i]), h[c][i], x * B[i]);
+        for (int j = 0; j < 4; ++j) {
+          const float2 z = __fmul2_rn(d[p], A2[p][j]);
+          h[p][j] = __ffma2_rn(make_float2(exp2_fast(z.x), exp2_fast(z.y)), h[p][j],
+                               __fmul2_rn(x[p], make_float2(B[j], B[j])));
         }
+    }
+    tmem_wait_st();
+    fetch_mark(i + 1);
+    // up the rows
+#pragma unroll 1
+    for (int t = rows - 1; t >= 0; --t) {
+      float2 before[PAIRS][4];  // the state that enters row t
+      tmem_get<E>(column + t * E, before);
+      if (kPacked && (closes >> t & 1)) {
+        const int s = a.row_seq[row0 + t];
+        load_states(e, a, a.dlast && s >= 0 ? a.dlast + (s * a.channels + at) * a.states : nullptr,
+                    n0, count);
+      }
+      const bool opening = kPacked && (opens >> t & 1);
+      float2 d[PAIRS], x[PAIRS], q[PAIRS];
+      load2(d, sd, t);
+      load2(x, sx, t);
+      load2(q, sq, t);
+      const float4 B4 = sB[t * LS], C4 = sC[t * LS];
+      const float B[4] = {B4.x, B4.y, B4.z, B4.w}, C[4] = {C4.x, C4.y, C4.z, C4.w};
+      float bc[8], o[CH], r[CH], v[CH];
+      float2 bb[4], cc[4];
+      float2 start[PAIRS][4];
+      if (kPacked && opening) open_state(start, t);
+#pragma unroll
+      for (int p = 0; p < PAIRS; ++p) {
+        float2 oo, rr, vv;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 Bj = make_float2(B[j], B[j]), Cj = make_float2(C[j], C[j]);
+          const float2 z = __fmul2_rn(d[p], A2[p][j]);
+          const float2 ee = __ffma2_rn(Cj, q[p], e[p][j]);
+          bb[j] = p == 0 ? __fmul2_rn(x[p], ee) : __ffma2_rn(x[p], ee, bb[j]);
+          cc[j] = p == 0 ? __fmul2_rn(q[p], h[p][j]) : __ffma2_rn(q[p], h[p][j], cc[j]);
+          rr = j == 0 ? __fmul2_rn(ee, Bj) : __ffma2_rn(ee, Bj, rr);
+          oo = j == 0 ? __fmul2_rn(h[p][j], Cj) : __ffma2_rn(h[p][j], Cj, oo);
+          e[p][j] = __fmul2_rn(make_float2(exp2_fast(z.x), exp2_fast(z.y)), ee);
+          const float2 g = __fmul2_rn(e[p][j], kPacked && opening ? start[p][j] : before[p][j]);
+          vv = j == 0 ? __fmul2_rn(g, A2[p][j]) : __ffma2_rn(g, A2[p][j], vv);
+          dA[p][j] = __ffma2_rn(g, d[p], dA[p][j]);
+          h[p][j] = before[p][j];
+        }
+        o[2 * p] = oo.x, o[2 * p + 1] = oo.y;
+        r[2 * p] = rr.x, r[2 * p + 1] = rr.y;
+        v[2 * p] = vv.x, v[2 * p + 1] = vv.y;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) bc[j] = bb[j].x + bb[j].y, bc[4 + j] = cc[j].x + cc[j].y;
+      if (kPacked && opening && a.dstate && a.row_seq[row0 + t] >= 0)
+        store_states(e, a, a.dstate + ((int64_t)a.row_seq[row0 + t] * a.channels + at) * a.states,
+                     n0, count);
+      reduce_scatter<CH, LS, 1>(o, lane);
+      reduce_scatter<CH, LS, 1>(r, lane);
+      reduce_scatter<CH, LS, 1>(v, lane);
+      reduce_scatter<8, L::CL, LS>(bc, lane);
+      __syncwarp();  // the row's d, x, q have been read by all
+      if (owner_of<CH, LS>(sl)) {
+        constexpr int held = CH > LS ? CH / LS : 1;
+        const int to = t * L::kRow + ch0 + first_of<CH, LS>(sl);
+#pragma unroll
+        for (int k = 0; k < held; ++k) sd[to + k] = v[k], sx[to + k] = o[k], sq[to + k] = r[k];
+      }
+      if (owner_of<8, L::CL>(lane / LS)) {
+        constexpr int held = 8 > L::CL ? 8 / L::CL : 1;
+        const int f = first_of<8, L::CL>(lane / LS);
+#pragma unroll
+        for (int k = 0; k < held; ++k)
+          sum[(t * 2 + (f + k) / 4) * L::NP + n0 + (f + k) % 4] = bc[k];
       }
     }
-    for (int sub = subs - 1; sub >= 0; --sub) {
-      float hs[kSub][CH][4], as[kSub][CH][4];
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          h[c][i] = snap[(sub * E + c * 4 + i) * kScanThreads + threadIdx.x];
-#pragma unroll
-      for (int j = 0; j < kSub; ++j) {
-        // rows past the end have d = x = 0: the state stays
-        const int t = sub * kSub + j;
-        if (kPacked && (opens >> t & 1)) open(t);
-        const float4 B4 = *reinterpret_cast<const float4 *>(sB + t * NP + n0);
-        const float B[4] = {B4.x, B4.y, B4.z, B4.w};
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const float d = sd[t * DB + ch0 + c], x = sx[t * DB + ch0 + c];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            as[j][c][i] = exp2_fast(d * A2[c][i]);
-            h[c][i] = fmaf(as[j][c][i], h[c][i], x * B[i]);
-            hs[j][c][i] = h[c][i];
-          }
-        }
-      }
-#pragma unroll
-      for (int j = kSub - 1; j >= 0; --j) {
-        const int t = sub * kSub + j;
-        if (kPacked && (closes >> t & 1)) {
-          const int s = a.row_seq[row0 + t];
-#pragma unroll
-          for (int c = 0; c < CH; ++c) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[c][i] = 0.f;
-            if (ch0 + c < w.nc && a.dlast && s >= 0)
-              load4(e[c], a.dlast + (s * a.channels + w.c0 + ch0 + c) * a.states, n0, a.states);
-          }
-        }
-        // h <- the state before row t
-        if (kPacked && (opens >> t & 1)) {
-          open(t);
-        } else {
-#pragma unroll
-          for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              h[c][i] = j > 0 ? hs[j > 0 ? j - 1 : 0][c][i]
-                              : snap[(sub * E + c * 4 + i) * kScanThreads + threadIdx.x];
-        }
-        const float4 B4 = *reinterpret_cast<const float4 *>(sB + t * NP + n0);
-        const float4 C4 = *reinterpret_cast<const float4 *>(sC + t * NP + n0);
-        const float B[4] = {B4.x, B4.y, B4.z, B4.w}, C[4] = {C4.x, C4.y, C4.z, C4.w};
-        float bc[8] = {};
-        float o[CH], r[CH], v[CH];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const float d = sd[t * DB + ch0 + c], x = sx[t * DB + ch0 + c], q = sq[t * DB + ch0 + c];
-          o[c] = r[c] = v[c] = 0.f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float ee = fmaf(C[i], q, e[c][i]);
-            bc[i] = fmaf(x, ee, bc[i]);
-            bc[4 + i] = fmaf(q, hs[j][c][i], bc[4 + i]);
-            r[c] = fmaf(ee, B[i], r[c]);
-            o[c] = fmaf(hs[j][c][i], C[i], o[c]);
-            e[c][i] = as[j][c][i] * ee;
-            const float p = e[c][i] * h[c][i];
-            v[c] = fmaf(p, A2[c][i], v[c]);
-            dA[c][i] = fmaf(p, d, dA[c][i]);
-          }
-        }
-        if (kPacked && (opens >> t & 1) && a.dstate && a.row_seq[row0 + t] >= 0) {
-#pragma unroll
-          for (int c = 0; c < CH; ++c)
-            if (ch0 + c < w.nc)
-              store4(a.dstate + (a.row_seq[row0 + t] * a.channels + w.c0 + ch0 + c) * a.states,
-                     e[c], n0, a.states);
-        }
-        // sums over states: one channel's o, r, v to its owner, in place of
-        // the row's x, q, d (read by this warp only, and for the last time)
-        reduce_scatter<CH, LS, 1>(o, lane);
-        reduce_scatter<CH, LS, 1>(r, lane);
-        reduce_scatter<CH, LS, 1>(v, lane);
-        __syncwarp();
-        if (owner_of<CH, LS>(sl)) {
-          constexpr int held = CH > LS ? CH / LS : 1;
-          const int at = t * DB + ch0 + first_of<CH, LS>(sl);
-#pragma unroll
-          for (int i = 0; i < held; ++i) {
-            sx[at + i] = o[i];
-            sq[at + i] = r[i];
-            sd[at + i] = v[i];
-          }
-        }
-        // sums over the warp's channels
-        reduce_scatter<8, CL, LS>(bc, lane);
-        if (owner_of<8, CL>(lane / LS)) {
-          constexpr int held = 8 > CL ? 8 / CL : 1;
-          const int f = first_of<8, CL>(lane / LS);
-#pragma unroll
-          for (int i = 0; i < held; ++i) {
-            const int which = (f + i) / 4, n = n0 + (f + i) % 4;
-            sbc[((warp * kTile + t) * 2 + which) * NP + n] = bc[i];
-          }
-        }
-      }
-    }
+    if (i % kFlush == kFlush - 1) flush();
     __syncthreads();
-    for (int i = threadIdx.x; i < rows * 2 * NP; i += kScanThreads) {
-      const int n = i % NP;
-      if (n >= a.states) continue;
-      float s = 0.f;
+  }
+  flush();
 #pragma unroll
-      for (int k = 0; k < kWarps; ++k) s += sbc[k * kTile * 2 * NP + i];
-      const int t = i / (2 * NP), which = i / NP % 2;
-      a.bc_parts[((((int64_t)w.cb * a.batches + w.b) * a.rows + row0 + t) * a.groups + w.g) * 2 *
-                     a.states + which * a.states + n] = s;
-    }
-    if (ec < w.nc) {
-      const int64_t c = w.c0 + ec;
-      const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
-      for (int t = threadIdx.x / DB; t < rows; t += kScanThreads / DB) {
-        const int64_t r = row0 + t;
-        const float u = to_f(a.u.at(w.b, r)[c]), dt = to_f(a.dt.at(w.b, r)[c]) + bias;
-        const float dy = to_f(a.dy.at(w.b, r)[c]);
-        const float d = a.softplus ? softplus(dt) : dt;
-        const float o = sx[t * DB + ec], rr = sq[t * DB + ec], v = sd[t * DB + ec] * kLn2;
-        float q = dy;
-        if (a.gate.p) {
-          const float z = to_f(a.gate.at(w.b, r)[c]);
-          q *= silu(z);
-          if (a.dgate.p) a.dgate.at(w.b, r)[c] = from_f<T>(dy * fmaf(skip, u, o) * dsilu(z));
-        }
-        float g = fmaf(rr, u, v);
-        if (a.softplus) g *= sigmoid(dt);
-        a.du.at(w.b, r)[c] = from_f<T>(fmaf(rr, d, skip * q));
-        a.ddt.at(w.b, r)[c] = from_f<T>(g);
-        dskip = fmaf(q, u, dskip);
-        dbias += g;
-      }
-    }
-  }
+  for (int p = 0; p < PAIRS; ++p)
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    if (ch0 + c >= w.nc) continue;
-    const int64_t at = w.c0 + ch0 + c;
-    store4(a.A_parts + (part * a.channels + at) * a.states, dA[c], n0, a.states);
-    if (!kPacked && a.dstate && w.k == 0)
-      store4(a.dstate + (w.b * a.channels + at) * a.states, e[c], n0, a.states);
-  }
-  __syncthreads();
-  sd[threadIdx.x] = dskip;
-  sx[threadIdx.x] = dbias;
-  __syncthreads();
-  if (threadIdx.x < w.nc) {
-    float s = 0.f, bsum = 0.f;
-    for (int i = threadIdx.x; i < kScanThreads; i += DB) {
-      s += sd[i];
-      bsum += sx[i];
+    for (int i = 0; i < 4; i += 2) {
+      const float4 v = asum[32 * (p * 2 + i / 2)];
+      dA[p][i] = make_float2(v.x, v.y), dA[p][i + 1] = make_float2(v.z, v.w);
     }
-    const int64_t at = part * a.channels + w.c0 + threadIdx.x;
-    if (a.skip_parts) a.skip_parts[at] = s;
-    if (a.bias_parts) a.bias_parts[at] = bsum;
-  }
+  store_states(dA, a, a.A_parts + (part * a.channels + at) * a.states, n0, count);
+  if (!kPacked && a.dstate && w.k == 0)
+    store_states(e, a, a.dstate + (w.b * a.channels + at) * a.states, n0, count);
+  asm volatile("bar.sync 1, %0;" ::"r"(32 * L::kPairs) : "memory");  // the first warps
+  if (warp == 0) tmem_dealloc(*reinterpret_cast<volatile uint32_t *>(smem), L::kColumns);
 }
 
 // dB and dC from the channel blocks' shares, in order.
@@ -1028,8 +1174,8 @@ __global__ void sum_bc_kernel(ScanArgs<T> a) {
 // ------------------------------------------------------------- host side
 enum ScanCall { kScan, kScanGrad, kScanStep };
 
-// The channels of a gradient block by the lanes over the states.
-constexpr int grad_ch(int) { return 2; }
+// The channels of a block of the adjoint kernel by the lanes over the states.
+constexpr int adjoint_ch(int) { return 2; }
 constexpr int block_channels(int ls, int ch) { return kWarps * (32 / ls) * ch; }
 
 inline int lanes_of(int64_t states) {

@@ -43,8 +43,12 @@ ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, bool grad) 
   constexpr int most = 8;  // values of a word of rows, at most 16 bytes
   const int word = std::min<int>(16, most * sizeof(T));
   a.wide = p.per_group % most == 0;
-  for (const tcu_seq_rows *r : {&s.u, &s.dt, &s.gate, &s.y})
+  for (const tcu_seq_rows *r : {&s.u, &s.dt, &s.gate})
     a.wide = a.wide && rows_aligned(*r, s.type, batches, rows, word);
+  if (!grad) a.wide = a.wide && rows_aligned(s.y, s.type, batches, rows, word);
+  else
+    for (const tcu_seq_rows *r : {&s.dy, &s.du, &s.ddt, &s.dgate})
+      a.wide = a.wide && rows_aligned(*r, s.type, batches, rows, word);
   float *w = static_cast<float *>(s.workspace);
   a.carry = w;
   a.sum_d = a.carry + p.carry;
@@ -95,18 +99,23 @@ int forward(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
   return start<scan_kernel<T, LS, kPacked, false, kWide>>(blocks, Lay<LS, T>::kBlock, floats, a, st);
 }
 
-template <typename T, int LS, bool kPacked>
+template <typename T, int LS, bool kPacked, bool kWide>
 int gradient(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
-  using P = Shape<LS, grad_ch(LS)>;
-  const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
   if (p.chunks > 1) {
+    using P = Shape<LS, adjoint_ch(LS)>;
     constexpr int floats = kTile * (P::kChannels * 2 + P::kStates);
-    if (const int rc = start<adjoint_kernel<T, P, kPacked>>(blocks, kScanThreads, floats, a, st)) return rc;
+    ScanArgs<T> c = a;
+    c.group_blocks = (a.per_group + P::kChannels - 1) / P::kChannels;
+    const int64_t blocks = p.batches * p.chunks * a.groups * c.group_blocks;
+    if (const int rc = start<adjoint_kernel<T, P, kPacked>>(blocks, kScanThreads, floats, c, st))
+      return rc;
     const int64_t count = a.channels * a.states * p.batches;
     carry_kernel<T, true><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
     if (const int rc = launched()) return rc;
   }
-  return start<scan_grad_kernel<T, P, kPacked>>(blocks, kScanThreads, grad_floats<P>(), a, st);
+  using L = GradLay<LS, T>;
+  const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
+  return start<scan_grad_kernel<T, LS, kPacked, kWide>>(blocks, L::kBlock, L::kFloats, a, st);
 }
 
 template <typename T, int LS>
@@ -123,7 +132,9 @@ int by_lanes(ScanCall call, const ScanPlan &p, const ScanArgs<T> &a, cudaStream_
       return a.wide ? forward<T, LS, true, true>(p, a, st) : forward<T, LS, true, false>(p, a, st);
     return a.wide ? forward<T, LS, false, true>(p, a, st) : forward<T, LS, false, false>(p, a, st);
   }
-  return a.row_seq ? gradient<T, LS, true>(p, a, st) : gradient<T, LS, false>(p, a, st);
+  if (a.row_seq)
+    return a.wide ? gradient<T, LS, true, true>(p, a, st) : gradient<T, LS, true, false>(p, a, st);
+  return a.wide ? gradient<T, LS, false, true>(p, a, st) : gradient<T, LS, false, false>(p, a, st);
 }
 
 template <typename T>

@@ -24,7 +24,7 @@ from . import OK, TcuDftError, lib
 
 MAX_WIDTH = 8
 MAX_STATES = 128
-MARK = 32
+MARK = 16  # rows from one state that the gradient resumes from to the next
 
 SYMBOLS = (
     "tcu_short_conv", "tcu_short_conv_grad", "tcu_short_conv_grad_workspace",
