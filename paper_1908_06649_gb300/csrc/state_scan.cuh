@@ -42,8 +42,7 @@
 namespace tcu {
 namespace seq {
 
-constexpr int kWarps = 4;
-constexpr int kScanThreads = 32 * kWarps;
+constexpr int kScanThreads = 128;     // of the single-token kernel
 constexpr int kTile = 32;             // rows of a forward tile: a warp's ballot
 constexpr int kMark = TCU_SEQ_MARK;   // rows of a gradient tile
 
@@ -158,31 +157,6 @@ __device__ __forceinline__ uint32_t closes_mask(const ScanArgs<T> &a, int64_t ro
 __global__ void row_sequence_kernel(int32_t *row_seq, const int32_t *offsets, int count,
                                     int64_t rows);
 
-// Shape of a kernel: LS lanes over the states, CH channels a thread.
-template <int LS_, int CH_>
-struct Shape {
-  static constexpr int LS = LS_, CH = CH_;
-  static constexpr int kStates = 4 * LS;            // states, padded
-  static constexpr int kWarpChannels = 32 / LS * CH;
-  static constexpr int kChannels = kWarps * kWarpChannels;
-};
-
-// Stages a tile of B and C ([row][padded states], zeros past the end).
-template <int NP, typename T>
-__device__ __forceinline__ void stage_bc(const ScanArgs<T> &a, int64_t b, int g, int64_t row0,
-                                         int rows, float *sB, float *sC) {
-  for (int e = threadIdx.x; e < kTile * NP; e += kScanThreads) {
-    const int t = e / NP, n = e % NP;
-    float vb = 0.f, vc = 0.f;
-    if (t < rows && n < a.states) {
-      vb = to_f(a.B.at(b, row0 + t)[(int64_t)g * a.states + n]);
-      if (sC) vc = to_f(a.C.at(b, row0 + t)[(int64_t)g * a.states + n]);
-    }
-    sB[e] = vb;
-    if (sC) sC[e] = vc;
-  }
-}
-
 // d of one value.
 template <typename T>
 __device__ __forceinline__ float step_of(const ScanArgs<T> &a, float dt, float bias) {
@@ -285,14 +259,18 @@ __device__ __forceinline__ void store_states(const float2 (&h)[PAIRS][4], const 
     }
 }
 
-// The scan of a chunk.  kLocal: from a zero start, leaving the chunk's final
-// state and its sum of d for the carry; otherwise from the carried state,
-// with outputs.  kWide: rows in words of V values.
-template <typename T, int LS, bool kPacked, bool kLocal, bool kWide>
+// The scan of a chunk.  kOutputs: from the carried state, with outputs.
+// kState: from a zero start, leaving the chunk's final state and its sum of d
+// for the carry.  kAdjoint: the same for the adjoint, whose recurrence is the
+// scan's from the last row to the first, with q for d u and C for B, and the
+// decay after the sum: c <- a (c + q C).  kWide: rows in words of V values.
+enum ScanMode { kOutputs, kState, kAdjoint };
+template <typename T, int LS, bool kPacked, ScanMode kMode, bool kWide>
 __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     scan_kernel(ScanArgs<T> a) {
   using L = Lay<LS, T>;
   constexpr int CH = L::CH, PAIRS = CH / 2, V = L::V, RP = L::RP;
+  constexpr bool kLocal = kMode != kOutputs, kBack = kMode == kAdjoint;
   extern __shared__ __align__(16) float smem[];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int pair = warp % L::kPairs;
@@ -306,6 +284,10 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
   const int nc = w.nc - pair * L::WC;
   if (nc <= 0) return;  // both warps of the pair
   const int pieces = (int)((w.r1 - w.r0 + RP - 1) / RP);
+  // row t of piece i
+  auto row_of = [&](int i, int t) {
+    return kBack ? w.r1 - 1 - ((int64_t)i * RP + t) : w.r0 + (int64_t)i * RP + t;
+  };
 
   if (warp >= L::kPairs) {
     // ---- rows into d, d u; sums into y
@@ -316,10 +298,13 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     }
     __syncwarp();
     const float *bias = sbias + vc, *skip = sskip + vc;
-    const T *pu = a.u.at(w.b, w.r0 + vr) + c0 + vc, *pd = a.dt.at(w.b, w.r0 + vr) + c0 + vc;
-    const T *pz = a.gate.p && !kLocal ? a.gate.at(w.b, w.r0 + vr) + c0 + vc : nullptr;
-    T *py = kLocal ? nullptr : a.y.at(w.b, w.r0 + vr) + c0 + vc;
-    const int64_t su = RP * a.u.row, sdt = RP * a.dt.row, sz = RP * a.gate.row, so = RP * a.y.row;
+    const Rows<const T> &ru = kBack ? a.dy : a.u;
+    const int64_t first = row_of(0, vr);
+    const T *pu = ru.at(w.b, first) + c0 + vc, *pd = a.dt.at(w.b, first) + c0 + vc;
+    const T *pz = a.gate.p && kMode != kState ? a.gate.at(w.b, first) + c0 + vc : nullptr;
+    T *py = kLocal ? nullptr : a.y.at(w.b, first) + c0 + vc;
+    constexpr int64_t way = kBack ? -RP : RP;
+    const int64_t su = way * ru.row, sdt = way * a.dt.row, sz = way * a.gate.row, so = way * a.y.row;
     const int last = (int)(w.r1 - w.r0) - vr;  // this lane's row is in piece i if i RP < last
     auto slot = [&](int i, int which) { return ring + ((i % kRing * 3 + which) * 32 + lane) * L::kRaw; };
     // piece i of u, dt, gate on its way to the ring
@@ -367,9 +352,9 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
         const int item = base + j * 32 + lane, n = item % LS * 4;
-        const int64_t r = w.r0 + (int64_t)i * RP + item / LS;
-        const int count = item < kItems && r < w.r1 ? min(4, a.states - n) : 0;
-        const T *from = a.B.at(w.b, r) + (int64_t)w.g * a.states + n;
+        const int64_t r = row_of(i, item / LS);
+        const int count = item < kItems && r >= w.r0 && r < w.r1 ? min(4, a.states - n) : 0;
+        const T *from = (kBack ? a.C : a.B).at(w.b, r) + (int64_t)w.g * a.states + n;
         if (a.wide_bc) qb[j].template load<true>(from, count);
         else qb[j].template load<false>(from, count);
         if (kLocal) continue;
@@ -399,7 +384,9 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       for (int v = 0; v < V / 2; ++v) {
         d[v] = __fadd2_rn(dt.pair(v), *reinterpret_cast<const float2 *>(bias + 2 * v));
         if (a.softplus) d[v] = softplus2(d[v]);
-        x[v] = __fmul2_rn(d[v], u.pair(v));
+        x[v] = u.pair(v);
+        if (!kBack) x[v] = __fmul2_rn(d[v], x[v]);
+        else if (pz) x[v] = __fmul2_rn(x[v], silu2(take(i, 2).pair(v)));
       }
 #pragma unroll
       for (int v = 0; v < V / 2; v += 2) {
@@ -481,10 +468,12 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     for (int i = 0; i < 4; ++i) A2[p][i] = __fmul2_rn(A2[p][i], make_float2(kLog2e, kLog2e));
   }
   const float *start = nullptr;
-  if (!kPacked && w.k == 0) start = a.state ? a.state + (w.b * a.channels + at) * a.states : nullptr;
-  else if (!kLocal && w.k > 0) start = a.carry + state0 * a.states;
+  const float *ends = kBack ? a.dlast : a.state;  // what sequences start from
+  if (!kPacked && (kBack ? w.r1 == a.rows : w.k == 0))
+    start = ends ? ends + (w.b * a.channels + at) * a.states : nullptr;
+  else if (!kLocal && w.k > 0)
+    start = a.carry + state0 * a.states;
   load_states(h, a, start, n0, count);
-  uint32_t opens = 0;
   meet(pair);
 #pragma unroll 1
   for (int i = 0; i <= pieces; ++i) {
@@ -492,28 +481,32 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       meet(pair);
       break;
     }
-    const int64_t row0 = w.r0 + (int64_t)i * RP;
-    const int rows = (int)min((int64_t)RP, w.r1 - row0);
-    const int in_tile = (int)(row0 % kTile);
-    if (in_tile == 0) {
-      if (kPacked) opens = opens_mask(a, row0, lane);
+    const int64_t row0 = row_of(i, 0);
+    const int rows = (int)min((int64_t)RP, w.r1 - w.r0 - (int64_t)i * RP);
+    uint32_t opens = 0;  // rows of the piece where a sequence opens (going back: ends)
+    if (kPacked) {
+      const int64_t r = row_of(i, lane);
+      bool o = lane < rows;
+      if (kBack) o = o && (r + 1 == a.rows || a.row_seq[r] != a.row_seq[r + 1]);
+      else o = o && (r == 0 || a.row_seq[r] != a.row_seq[r - 1]);
+      opens = __ballot_sync(~0u, o);
     }
     const float *sd = sdx + i % 2 * 2 * RP * L::kRow + ch0, *sx = sd + RP * L::kRow;
     const float4 *sB = reinterpret_cast<const float4 *>(sbc + i % 2 * 2 * L::kBC) + sl,
                  *sC = sB + RP * LS;
     float *to = sy + i % 2 * RP * L::kYRow + sl * L::kYLane + ch0;
     auto mark = [&](int t) {
-      if (kLocal || !a.marks || (in_tile + t) % kMark != 0) return;
+      if (kLocal || !a.marks || (uint32_t)(row0 + t) % kMark != 0) return;
       const int64_t marks = (a.rows + kMark - 1) / kMark, m = (row0 + t) / kMark;
       store_states(h, a, a.marks + ((w.b * marks + m) * a.channels + at) * a.states, n0, count);
     };
     auto open = [&](int t) {
-      const int64_t r = row0 + t;
-      const int s = a.row_seq[r], before = r > 0 ? a.row_seq[r - 1] : -1;
+      const int64_t r = row_of(i, t);
+      const int s = a.row_seq[r], before = !kBack && r > 0 ? a.row_seq[r - 1] : -1;
       if (!kLocal && a.last && before >= 0)
         store_states(h, a, a.last + (before * a.channels + at) * a.states, n0, count);
-      load_states(h, a, a.state && s >= 0 ? a.state + (s * a.channels + at) * a.states : nullptr,
-                  n0, count);
+      load_states(h, a, ends && s >= 0 ? ends + (s * a.channels + at) * a.states : nullptr, n0,
+                  count);
 #pragma unroll
       for (int p = 0; p < PAIRS; ++p) dsum[p] = make_float2(0.f, 0.f);
     };
@@ -539,8 +532,10 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float2 e = __fmul2_rn(d[p], A2[p][j]);
-          h[p][j] = __ffma2_rn(make_float2(exp2_fast(e.x), exp2_fast(e.y)), h[p][j],
-                               __fmul2_rn(x[p], make_float2(B[j], B[j])));
+          const float2 decay = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+          const float2 b = make_float2(B[j], B[j]);
+          h[p][j] = kBack ? __fmul2_rn(decay, __ffma2_rn(x[p], b, h[p][j]))
+                          : __ffma2_rn(decay, h[p][j], __fmul2_rn(x[p], b));
           if (kLocal) continue;
           const float2 c = make_float2(C[j], C[j]);
           y[p] = j == 0 ? __fmul2_rn(c, h[p][j]) : __ffma2_rn(c, h[p][j], y[p]);
@@ -554,10 +549,10 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       else
         *reinterpret_cast<float2 *>(to + t * L::kYRow) = y[0];
     };
-    if (rows < RP || (kPacked && (opens >> in_tile) << (32 - RP) != 0)) {
+    if (rows < RP || opens != 0) {
       for (int t = 0; t < rows; ++t) {
         mark(t);
-        if (kPacked && (opens >> (in_tile + t) & 1)) open(t);
+        if (kPacked && (opens >> t & 1)) open(t);
         float2 y[PAIRS];
         step(t, y);
         if (!kLocal) share(t, y);
@@ -655,87 +650,6 @@ __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(ScanArgs<T> a) 
 }
 
 // ---------------------------------------------------------------- gradient
-// The adjoint of a chunk from a zero start below it: its contribution to the
-// adjoint above it and its sum of d.
-template <typename T, class P, bool kPacked>
-__global__ void __launch_bounds__(kScanThreads) adjoint_kernel(ScanArgs<T> a) {
-  constexpr int LS = P::LS, CH = P::CH, NP = P::kStates, DB = P::kChannels;
-  extern __shared__ __align__(16) float smem[];
-  float *sd = smem, *sq = sd + kTile * DB, *sC = sq + kTile * DB;
-  const Place<DB, T> w(a);
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int sl = lane % LS, n0 = sl * 4;
-  const int ch0 = warp * P::kWarpChannels + lane / LS * CH;
-  float A2[CH][4], e[CH][4], dsum[CH];
-  const int64_t state0 = (w.b * a.chunks + w.k) * a.channels + w.c0;
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    dsum[c] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) A2[c][i] = e[c][i] = 0.f;
-    if (ch0 + c >= w.nc) continue;
-    const int64_t at = w.c0 + ch0 + c;
-    load4(A2[c], a.A + at * a.states, n0, a.states);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) A2[c][i] *= kLog2e;
-    if (!kPacked && w.r1 == a.rows && a.dlast)
-      load4(e[c], a.dlast + (w.b * a.channels + at) * a.states, n0, a.states);
-  }
-  const int64_t tiles = (w.r1 - w.r0 + kTile - 1) / kTile;
-  for (int64_t tile = tiles - 1; tile >= 0; --tile) {
-    const int64_t row0 = w.r0 + tile * kTile;
-    const int rows = (int)min((int64_t)kTile, w.r1 - row0);
-    __syncthreads();
-    for (int i = threadIdx.x; i < kTile * DB; i += kScanThreads) {
-      const int t = i / DB, c = i % DB;
-      float d = 0.f, q = 0.f;
-      if (t < rows && c < w.nc) {
-        d = step_of(a, to_f(a.dt.at(w.b, row0 + t)[w.c0 + c]),
-                    a.dt_bias ? a.dt_bias[w.c0 + c] : 0.f);
-        q = to_f(a.dy.at(w.b, row0 + t)[w.c0 + c]);
-        if (a.gate.p) q *= silu(to_f(a.gate.at(w.b, row0 + t)[w.c0 + c]));
-      }
-      sd[i] = d;
-      sq[i] = q;
-    }
-    for (int i = threadIdx.x; i < kTile * NP; i += kScanThreads) {
-      const int t = i / NP, n = i % NP;
-      sC[i] = t < rows && n < a.states
-                  ? to_f(a.C.at(w.b, row0 + t)[(int64_t)w.g * a.states + n])
-                  : 0.f;
-    }
-    const uint32_t closes = kPacked ? closes_mask(a, row0, lane) : 0;
-    __syncthreads();
-    for (int t = rows - 1; t >= 0; --t) {
-      if (kPacked && (closes >> t & 1)) {
-        const int s = a.row_seq[row0 + t];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) e[c][i] = 0.f;
-          if (ch0 + c < w.nc && a.dlast && s >= 0)
-            load4(e[c], a.dlast + (s * a.channels + w.c0 + ch0 + c) * a.states, n0, a.states);
-        }
-      }
-      const float4 C4 = *reinterpret_cast<const float4 *>(sC + t * NP + n0);
-      const float C[4] = {C4.x, C4.y, C4.z, C4.w};
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const float d = sd[t * DB + ch0 + c], q = sq[t * DB + ch0 + c];
-        dsum[c] += d;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[c][i] = exp2_fast(d * A2[c][i]) * fmaf(C[i], q, e[c][i]);
-      }
-    }
-  }
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    if (ch0 + c >= w.nc) continue;
-    store4(a.carry + (state0 + ch0 + c) * a.states, e[c], n0, a.states);
-    if (sl == 0) a.sum_d[state0 + ch0 + c] = dsum[c];
-  }
-}
-
 // How the gradient kernel is laid out: blocks of four pairs of warps, as the
 // forward kernel's, over tiles of kMark rows from the last to the first.  The
 // first warp of a pair recomputes a tile's states from its mark, down the
@@ -815,18 +729,25 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
     float2 dskip[V / 2], dbias[V / 2];
 #pragma unroll
     for (int v = 0; v < V / 2; ++v) dskip[v] = dbias[v] = make_float2(0.f, 0.f);
-    struct {
+    struct In {
       Raw<T, V> u, dt, z, dy;
-    } in;
-    auto load = [&](int i, int pass) {
-      const int64_t r = row_of(i) + pass * L::RP + vr;
-      const int count = r < w.r1 ? vcount : 0;
-      in.u.template load<kWide>(a.u.at(w.b, r) + c0 + vc, count);
-      in.dt.template load<kWide>(a.dt.at(w.b, r) + c0 + vc, count);
-      if (gated) in.z.template load<kWide>(a.gate.at(w.b, r) + c0 + vc, count);
-      in.dy.template load<kWide>(a.dy.at(w.b, r) + c0 + vc, count);
     };
-    auto stage = [&](int i, int pass) {
+    // this lane's first row of the tile that the first warps are at
+    const int64_t row = row_of(0) + vr;
+    const T *pu = a.u.at(w.b, row) + c0 + vc, *pd = a.dt.at(w.b, row) + c0 + vc,
+            *pz = gated ? a.gate.at(w.b, row) + c0 + vc : nullptr,
+            *py = a.dy.at(w.b, row) + c0 + vc;
+    // pass `pass` of the tile `to` tiles further up
+    auto load = [&](In &in, int i, int to, int pass) {
+      const int up = to * kMark - pass * L::RP;
+      const int64_t r = row_of(i + to) + pass * L::RP + vr;
+      const int count = i + to >= 0 && i + to < tiles && r < w.r1 ? vcount : 0;
+      in.u.template load<kWide>(pu - up * a.u.row, count);
+      in.dt.template load<kWide>(pd - up * a.dt.row, count);
+      if (gated) in.z.template load<kWide>(pz - up * a.gate.row, count);
+      in.dy.template load<kWide>(py - up * a.dy.row, count);
+    };
+    auto stage = [&](const In &in, int i, int pass) {
       float *o = sdxq + i % 2 * 3 * L::kPlane + (pass * L::RP + vr) * L::kRow + vc;
 #pragma unroll
       for (int v = 0; v < V / 2; ++v) {
@@ -839,7 +760,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
         *reinterpret_cast<float2 *>(o + 2 * L::kPlane + 2 * v) = q;
       }
     };
-    auto finish = [&](int i, int pass) {
+    auto finish = [&](const In &in, int i, int pass) {
       const float *from = sdxq + i % 2 * 3 * L::kPlane + (pass * L::RP + vr) * L::kRow + vc;
       const int64_t r = row_of(i) + pass * L::RP + vr;
       const int count = r < w.r1 ? vcount : 0;
@@ -909,31 +830,33 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
                        a.states + which * a.states + n] = s;
       }
     };
-#pragma unroll 1
+    // the passes of an iteration: those of the tile behind, then those of the
+    // one ahead, each loaded while the one before is worked on
+    In in[2];
+#pragma unroll
     for (int p = 0; p < L::PASSES; ++p) {
-      load(0, p);
-      stage(0, p);
+      load(in[0], 0, 0, p);
+      stage(in[0], 0, p);
     }
     stage_bc(0);
     __syncthreads();
 #pragma unroll 1
     for (int i = 0; i <= tiles; ++i) {
-      if (i > 0) {
-#pragma unroll 1
-        for (int p = 0; p < L::PASSES; ++p) {
-          load(i - 1, p);
-          finish(i - 1, p);
-        }
-        share_bc(i - 1);
+      constexpr int jobs = 2 * L::PASSES;
+      load(in[0], i, -1, 0);
+#pragma unroll
+      for (int j = 0; j < jobs; ++j) {
+        const int to = j < L::PASSES ? -1 : 1, pass = j % L::PASSES;
+        if (j + 1 < jobs) load(in[(j + 1) % 2], i, j + 1 < L::PASSES ? -1 : 1, (j + 1) % L::PASSES);
+        if (to < 0 && i > 0) finish(in[j % 2], i - 1, pass);
+        if (to > 0 && i + 1 < tiles) stage(in[j % 2], i + 1, pass);
       }
-      if (i + 1 < tiles) {
-#pragma unroll 1
-        for (int p = 0; p < L::PASSES; ++p) {
-          load(i + 1, p);
-          stage(i + 1, p);
-        }
-        stage_bc(i + 1);
-      }
+      if (i > 0) share_bc(i - 1);
+      if (i + 1 < tiles) stage_bc(i + 1);
+      pu -= kMark * a.u.row;
+      pd -= kMark * a.dt.row;
+      if (gated) pz -= kMark * a.gate.row;
+      py -= kMark * a.dy.row;
       __syncthreads();
     }
     // a channel's shares lie in the lanes of its column
@@ -1071,10 +994,8 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
     }
     tmem_wait_st();
     fetch_mark(i + 1);
-    // up the rows
-#pragma unroll 1
-    for (int t = rows - 1; t >= 0; --t) {
-      float2 before[PAIRS][4];  // the state that enters row t
+    // up the rows: h the state after row t, before the one that enters it
+    auto up = [&](int t, const float2 (&h)[PAIRS][4], float2 (&before)[PAIRS][4]) {
       tmem_get<E>(column + t * E, before);
       if (kPacked && (closes >> t & 1)) {
         const int s = a.row_seq[row0 + t];
@@ -1090,8 +1011,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       const float B[4] = {B4.x, B4.y, B4.z, B4.w}, C[4] = {C4.x, C4.y, C4.z, C4.w};
       float bc[8], o[CH], r[CH], v[CH];
       float2 bb[4], cc[4];
-      float2 start[PAIRS][4];
-      if (kPacked && opening) open_state(start, t);
+      if (kPacked && opening) open_state(before, t);  // the state the sequence starts from
 #pragma unroll
       for (int p = 0; p < PAIRS; ++p) {
         float2 oo, rr, vv;
@@ -1105,10 +1025,9 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
           rr = j == 0 ? __fmul2_rn(ee, Bj) : __ffma2_rn(ee, Bj, rr);
           oo = j == 0 ? __fmul2_rn(h[p][j], Cj) : __ffma2_rn(h[p][j], Cj, oo);
           e[p][j] = __fmul2_rn(make_float2(exp2_fast(z.x), exp2_fast(z.y)), ee);
-          const float2 g = __fmul2_rn(e[p][j], kPacked && opening ? start[p][j] : before[p][j]);
+          const float2 g = __fmul2_rn(e[p][j], before[p][j]);
           vv = j == 0 ? __fmul2_rn(g, A2[p][j]) : __ffma2_rn(g, A2[p][j], vv);
           dA[p][j] = __ffma2_rn(g, d[p], dA[p][j]);
-          h[p][j] = before[p][j];
         }
         o[2 * p] = oo.x, o[2 * p + 1] = oo.y;
         r[2 * p] = rr.x, r[2 * p + 1] = rr.y;
@@ -1116,6 +1035,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) bc[j] = bb[j].x + bb[j].y, bc[4 + j] = cc[j].x + cc[j].y;
+      if (kPacked && opening) tmem_get<E>(column + t * E, before);  // the last one's end again
       if (kPacked && opening && a.dstate && a.row_seq[row0 + t] >= 0)
         store_states(e, a, a.dstate + ((int64_t)a.row_seq[row0 + t] * a.channels + at) * a.states,
                      n0, count);
@@ -1137,7 +1057,15 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
         for (int k = 0; k < held; ++k)
           sum[(t * 2 + (f + k) / 4) * L::NP + n0 + (f + k) % 4] = bc[k];
       }
+    };
+    float2 other[PAIRS][4];
+    int t = rows - 1;
+#pragma unroll 1
+    for (; t > 0; t -= 2) {
+      up(t, h, other);
+      up(t - 1, other, h);
     }
+    if (t == 0) up(0, h, other);
     if (i % kFlush == kFlush - 1) flush();
     __syncthreads();
   }
@@ -1173,10 +1101,6 @@ __global__ void sum_bc_kernel(ScanArgs<T> a) {
 
 // ------------------------------------------------------------- host side
 enum ScanCall { kScan, kScanGrad, kScanStep };
-
-// The channels of a block of the adjoint kernel by the lanes over the states.
-constexpr int adjoint_ch(int) { return 2; }
-constexpr int block_channels(int ls, int ch) { return kWarps * (32 / ls) * ch; }
 
 inline int lanes_of(int64_t states) {
   int ls = 2;

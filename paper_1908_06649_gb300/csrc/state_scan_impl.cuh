@@ -89,25 +89,25 @@ int forward(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
   const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
   constexpr int floats = Lay<LS, T>::kFloats;
   if (p.chunks > 1) {
-    if (const int rc = start<scan_kernel<T, LS, kPacked, true, kWide>>(blocks, Lay<LS, T>::kBlock, floats,
+    if (const int rc = start<scan_kernel<T, LS, kPacked, kState, kWide>>(blocks, Lay<LS, T>::kBlock, floats,
                                                                       a, st))
       return rc;
     const int64_t count = a.channels * a.states * p.batches;
     carry_kernel<T, false><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
     if (const int rc = launched()) return rc;
   }
-  return start<scan_kernel<T, LS, kPacked, false, kWide>>(blocks, Lay<LS, T>::kBlock, floats, a, st);
+  return start<scan_kernel<T, LS, kPacked, kOutputs, kWide>>(blocks, Lay<LS, T>::kBlock, floats, a, st);
 }
 
 template <typename T, int LS, bool kPacked, bool kWide>
 int gradient(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
   if (p.chunks > 1) {
-    using P = Shape<LS, adjoint_ch(LS)>;
-    constexpr int floats = kTile * (P::kChannels * 2 + P::kStates);
+    using F = Lay<LS, T>;
     ScanArgs<T> c = a;
-    c.group_blocks = (a.per_group + P::kChannels - 1) / P::kChannels;
+    c.group_blocks = (a.per_group + F::DB - 1) / F::DB;
     const int64_t blocks = p.batches * p.chunks * a.groups * c.group_blocks;
-    if (const int rc = start<adjoint_kernel<T, P, kPacked>>(blocks, kScanThreads, floats, c, st))
+    if (const int rc = start<scan_kernel<T, LS, kPacked, kAdjoint, kWide>>(blocks, F::kBlock,
+                                                                        F::kFloats, c, st))
       return rc;
     const int64_t count = a.channels * a.states * p.batches;
     carry_kernel<T, true><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
