@@ -28,25 +28,11 @@ template <>
 __device__ __forceinline__ f16 from_f<f16>(float v) { return __float2half_rn(v); }
 
 // V adjacent values, accessed as one word of V * sizeof(T) <= 16 bytes; the
-// address is aligned to that (vector_width below).
+// address is aligned to that.
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Vec {
   T v[V];
 };
-template <typename T, int V>
-__device__ __forceinline__ void load_vec(float (&out)[V], const T *p) {
-  const Vec<T, V> w = *reinterpret_cast<const Vec<T, V> *>(p);
-#pragma unroll
-  for (int i = 0; i < V; ++i) out[i] = to_f(w.v[i]);
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_vec(T *p, const float (&in)[V]) {
-  Vec<T, V> w;
-#pragma unroll
-  for (int i = 0; i < V; ++i) w.v[i] = from_f<T>(in[i]);
-  *reinterpret_cast<Vec<T, V> *>(p) = w;
-}
-
 // 2^x by the special function unit (relative error 2^-22; 2^-inf = 0).
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -66,14 +52,16 @@ __device__ __forceinline__ float sigmoid(float v) {
   return rcp_fast(1.f + exp2_fast(-kLog2e * v));
 }
 __device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
-__device__ __forceinline__ float2 silu2(float2 v) {
+__device__ __forceinline__ float2 sigmoid2(float2 v) {
   const float2 e = __fmul2_rn(v, make_float2(-kLog2e, -kLog2e));
   const float2 w = __fadd2_rn(make_float2(exp2_fast(e.x), exp2_fast(e.y)), make_float2(1.f, 1.f));
-  return __fmul2_rn(v, make_float2(rcp_fast(w.x), rcp_fast(w.y)));
+  return make_float2(rcp_fast(w.x), rcp_fast(w.y));
 }
-__device__ __forceinline__ float dsilu(float v) {
-  const float s = sigmoid(v);
-  return s * (1.f + v * (1.f - s));
+__device__ __forceinline__ float2 silu2(float2 v) { return __fmul2_rn(v, sigmoid2(v)); }
+// (v sigma(v))' = s + v s (1 - s)
+__device__ __forceinline__ float2 dsilu2(float2 v) {
+  const float2 s = sigmoid2(v), vs = __fmul2_rn(v, s);
+  return __ffma2_rn(vs, __ffma2_rn(s, make_float2(-1.f, -1.f), make_float2(1.f, 1.f)), s);
 }
 
 // log(1 + exp(v)) of two values: max(v, 0) + log1p(e), e = exp(-|v|) <= 1, and
@@ -131,19 +119,40 @@ struct Pair<f16> {
   }
 };
 
-// V adjacent values (V even) as they lie in memory, in words so that nothing
-// waits for them before they are used: loads and stores of up to 16 bytes
-// where kWide, value by value otherwise; those from `count` on are neither
-// read nor written (kWide: count is V or at most 0).
-template <typename T, int V>
+// One value as it lies in memory, in a word of its own, and back.
+__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ uint32_t bits_of(bf16 v) { return __bfloat16_as_ushort(v); }
+__device__ __forceinline__ uint32_t bits_of(f16 v) { return __half_as_ushort(v); }
+template <typename T>
+__device__ __forceinline__ float of_bits(uint32_t w);
+template <>
+__device__ __forceinline__ float of_bits<float>(uint32_t w) { return __uint_as_float(w); }
+template <>
+__device__ __forceinline__ float of_bits<bf16>(uint32_t w) { return __uint_as_float(w << 16); }
+template <>
+__device__ __forceinline__ float of_bits<f16>(uint32_t w) {
+  return __half2float(__ushort_as_half((unsigned short)w));
+}
+
+// V values (V even) as they lie in memory, in words (kApart: one value each)
+// so that nothing waits for them before they are used: adjacent ones in loads and stores of up to 16
+// bytes where kWide, value by value at a pitch of `gap` otherwise; those from
+// `count` on are neither read nor written (kWide: count is V or at most 0).
+template <typename T, int V, bool kApart = false>
 struct Raw {
-  static constexpr int kPairWords = Pair<T>::kWords, kWords = V / 2 * kPairWords;
+  static constexpr int kPairWords = kApart ? 2 : Pair<T>::kWords, kWords = V / 2 * kPairWords;
   static constexpr int kStep = kWords % 4 == 0 ? 4 : kWords % 2 == 0 ? 2 : 1;
   uint32_t w[kWords];
-  __device__ __forceinline__ float2 pair(int i) const { return Pair<T>::get(w + i * kPairWords); }
-  __device__ __forceinline__ void set(int i, float2 v) { Pair<T>::put(w + i * kPairWords, v); }
+  __device__ __forceinline__ float2 pair(int i) const {
+    if constexpr (kApart) return make_float2(of_bits<T>(w[2 * i]), of_bits<T>(w[2 * i + 1]));
+    else return Pair<T>::get(w + i * kPairWords);
+  }
+  __device__ __forceinline__ void set(int i, float2 v) {
+    if constexpr (kApart) w[2 * i] = bits_of(from_f<T>(v.x)), w[2 * i + 1] = bits_of(from_f<T>(v.y));
+    else Pair<T>::put(w + i * kPairWords, v);
+  }
   template <bool kWide>
-  __device__ __forceinline__ void load(const T *p, int count) {
+  __device__ __forceinline__ void load(const T *p, int count, int64_t gap = 1) {
     if constexpr (kWide) {
 #pragma unroll
       for (int i = 0; i < kWords; ++i) w[i] = 0;
@@ -155,15 +164,18 @@ struct Raw {
           for (int j = 0; j < kStep; ++j) w[i * kStep + j] = v.v[j];
         }
       }
+    } else if constexpr (kApart) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) w[i] = i < count ? bits_of(p[i * gap]) : 0;
     } else {
 #pragma unroll
       for (int i = 0; i < V / 2; ++i)
-        set(i, make_float2(2 * i < count ? to_f(p[2 * i]) : 0.f,
-                           2 * i + 1 < count ? to_f(p[2 * i + 1]) : 0.f));
+        set(i, make_float2(2 * i < count ? to_f(p[2 * i * gap]) : 0.f,
+                           2 * i + 1 < count ? to_f(p[(2 * i + 1) * gap]) : 0.f));
     }
   }
   template <bool kWide>
-  __device__ __forceinline__ void store(T *p, int count) const {
+  __device__ __forceinline__ void store(T *p, int count, int64_t gap = 1) const {
     if constexpr (kWide) {
       if (count > 0) {
 #pragma unroll
@@ -178,8 +190,8 @@ struct Raw {
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) {
         const float2 v = pair(i);
-        if (2 * i < count) p[2 * i] = from_f<T>(v.x);
-        if (2 * i + 1 < count) p[2 * i + 1] = from_f<T>(v.y);
+        if (2 * i < count) p[2 * i * gap] = from_f<T>(v.x);
+        if (2 * i + 1 < count) p[(2 * i + 1) * gap] = from_f<T>(v.y);
       }
     }
   }
@@ -244,10 +256,15 @@ inline int num_sms() {
   return n;
 }
 
-// Sums partial[p][i] over p < parts in order, one value per thread: the
-// second step of the parameter gradients (the same result in every run).
-__global__ void sum_parts_kernel(float *out, const float *partial, int64_t parts, int64_t count);
-int sum_parts(float *out, const float *partial, int64_t parts, int64_t count, cudaStream_t st);
+// The second step of the parameter gradients: out[i] = sum over p < parts of
+// parts[p * stride + i], always in the same order; up to three at once.  A
+// stride of 0 is each sum's own count.
+struct Sum {
+  float *out;
+  const float *parts;
+  int64_t count;
+};
+int sum_parts(const Sum *sums, int count, int64_t parts, int64_t stride, cudaStream_t st);
 
 }  // namespace seq
 }  // namespace tcu

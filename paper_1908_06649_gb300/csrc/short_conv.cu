@@ -26,18 +26,21 @@ struct ConvArgs {
   const float *weight, *bias;
   const T *state, *dlast;
   T *last, *dstate;
-  float *parts;  // gradient: [run][channels][W] then [run][channels]
-  float *bias_parts;
+  float *parts;  // gradient: [run]{[channels][W], [channels]}
   const int32_t *offsets;
   const int32_t *slots;
   int64_t rows, channels, num_slots;
   int sequences, batches, silu;
-  int64_t runs;  // runs of kBlockRows * blocks rows in a batch entry
+  int64_t runs;  // of kBlockRows * blocks rows in a batch entry
   int blocks;
 };
 
 constexpr int kThreads = 128;
 constexpr int kBlockRows = 8;
+// Rows whose loads are on their way while as many are worked on: a multiple
+// of the width, so that slots are known, near eight.
+template <int W>
+constexpr int kAhead = W * (8 / W);
 
 // One sequence as rows [lo, hi) of a batch entry; span_of holds t itself
 // whatever the offsets are.
@@ -54,306 +57,395 @@ __device__ __forceinline__ Span span_of(const ConvArgs<T> &a, int64_t b, int64_t
   return {max((int64_t)a.offsets[s], (int64_t)0),
           max(min((int64_t)a.offsets[s + 1], a.rows), t + 1), s};
 }
-
-// Row i of a sequence, from the state where i < 0.
-template <typename T, int V, int W>
-__device__ __forceinline__ void row_value(const ConvArgs<T> &a, int64_t b, const Span &s,
-                                          int64_t i, int64_t c, float (&out)[V]) {
-  if (i >= 0) {
-    load_vec<T, V>(out, a.x.at(b, s.lo + i) + c);
-  } else if (a.state && s.seq >= 0) {
-    load_vec<T, V>(out, a.state + ((int64_t)s.seq * (W - 1) + (W - 1) + i) * a.channels + c);
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; ++v) out[v] = 0.f;
-  }
+// Sequence s itself, empty ones too.
+template <typename T>
+__device__ __forceinline__ Span span_at(const ConvArgs<T> &a, int64_t s) {
+  if (!a.offsets) return {0, a.rows, (int)s};
+  const int64_t lo = min(max((int64_t)a.offsets[s], (int64_t)0), a.rows);
+  return {lo, min(max((int64_t)a.offsets[s + 1], lo), a.rows), (int)s};
 }
 
-template <typename T, int V, int W>
-__device__ __forceinline__ void load_params(const ConvArgs<T> &a, int64_t c, float (&w)[W][V],
-                                            float (&bias)[V]) {
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    bias[v] = a.bias ? a.bias[c + v] : 0.f;
-#pragma unroll
-    for (int k = 0; k < W; ++k) w[k][v] = a.weight[(c + v) * W + k];
-  }
-}
+// What a thread owns: V channels, of which `count` exist, as pairs for packed
+// arithmetic.  kWide: adjacent ones, read in words (count is V); otherwise one
+// of each V-th part of the channels, so that lanes read adjacent values.
+template <typename T, int V, int W, bool kWide>
+struct Own {
+  static constexpr int P = V / 2;
+  using Row = Raw<T, V, !kWide>;
+  const ConvArgs<T> &a;
+  int64_t b, c, gap;
+  int count;
+  float2 w[W][P], bias[P];
 
-// p_i from the definition, row by row: where the fast path's window would
-// leave the sequence.
-template <typename T, int V, int W>
-__device__ __forceinline__ void pre_at(const ConvArgs<T> &a, int64_t b, const Span &s, int64_t i,
-                                       int64_t c, const float (&w)[W][V], const float (&bias)[V],
-                                       float (&p)[V]) {
-#pragma unroll
-  for (int v = 0; v < V; ++v) p[v] = bias[v];
-#pragma unroll
-  for (int k = 0; k < W; ++k) {
-    float x[V];
-    row_value<T, V, W>(a, b, s, i - (W - 1) + k, c, x);
-#pragma unroll
-    for (int v = 0; v < V; ++v) p[v] = fmaf(w[k][v], x[v], p[v]);
+  // The `which`-th of `all` threads that share a row.
+  __device__ __forceinline__ Own(const ConvArgs<T> &args, int64_t which, int64_t all) : a(args) {
+    c = kWide ? which * V : which;
+    gap = kWide ? 1 : all;
+    count = kWide ? V : (int)((a.channels - c + gap - 1) / gap);
   }
-}
-
-// The W-1 rows that a continuation of sequence s needs.
-template <typename T, int V, int W>
-__device__ __forceinline__ void write_last(const ConvArgs<T> &a, int64_t item, int64_t cv) {
-  if constexpr (W > 1) {
-    const int k = item % (W - 1);
-    const int64_t s = item / (W - 1);
-    Span sp;
-    sp.seq = (int)s;
-    if (a.offsets) {
-      sp.lo = min(max((int64_t)a.offsets[s], (int64_t)0), a.rows);
-      sp.hi = min(max((int64_t)a.offsets[s + 1], sp.lo), a.rows);
-    } else {
-      sp.lo = 0;
-      sp.hi = a.rows;
+  __device__ __forceinline__ void params() {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const bool in = kWide || v < count;
+      float *to = reinterpret_cast<float *>(bias);
+      to[v] = a.bias && in ? a.bias[c + v * gap] : 0.f;
+#pragma unroll
+      for (int k = 0; k < W; ++k)
+        reinterpret_cast<float *>(w[k])[v] = in ? a.weight[(c + v * gap) * W + k] : 0.f;
     }
-    float x[V];
-    row_value<T, V, W>(a, a.offsets ? 0 : s, sp, sp.hi - sp.lo - (W - 1) + k, cv, x);
-    store_vec<T, V>(a.last + (s * (W - 1) + k) * a.channels + cv, x);
   }
-}
+  __device__ __forceinline__ Row row(const T *p) const {
+    Row r;
+    r.template load<kWide>(p, count, gap);
+    return r;
+  }
+  __device__ __forceinline__ void put(T *p, const float2 (&v)[P]) const {
+    Row r;
+#pragma unroll
+    for (int i = 0; i < P; ++i) r.set(i, v[i]);
+    r.template store<kWide>(p, count, gap);
+  }
+  // Row i of a sequence, from the state where i < 0.
+  __device__ __forceinline__ Row value(const Span &s, int64_t i) const {
+    if (i >= 0) return row(a.x.at(b, s.lo + i) + c);
+    if (a.state && s.seq >= 0)
+      return row(a.state + ((int64_t)s.seq * (W - 1) + (W - 1) + i) * a.channels + c);
+    Row zero;
+#pragma unroll
+    for (int j = 0; j < Row::kWords; ++j) zero.w[j] = 0;
+    return zero;
+  }
+  // p of the row in slot j of a window whose slots are rows mod W.
+  __device__ __forceinline__ void pre(const float2 (&x)[W][P], int j, float2 (&p)[P]) const {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      p[i] = bias[i];
+#pragma unroll
+      for (int k = 0; k < W; ++k) p[i] = __ffma2_rn(w[k][i], x[(j + 1 + k) % W][i], p[i]);
+    }
+  }
+  // dp of that row from its dy.
+  __device__ __forceinline__ void dpre(const float2 (&x)[W][P], int j, const Row &dy,
+                                       float2 (&dp)[P]) const {
+    float2 p[P];
+    if (a.silu) pre(x, j, p);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      dp[i] = dy.pair(i);
+      if (a.silu) dp[i] = __fmul2_rn(dp[i], dsilu2(p[i]));
+    }
+  }
+  // The window before row i of a sequence, i in slot 0.
+  __device__ __forceinline__ void window(const Span &s, int64_t i, float2 (&x)[W][P]) const {
+#pragma unroll
+    for (int k = 1; k < W; ++k) {
+      const Row r = value(s, i - W + k);
+#pragma unroll
+      for (int j = 0; j < P; ++j) x[k % W][j] = r.pair(j);
+    }
+  }
+};
 
 // y: one thread per V channels and run of rows; the threads past the runs
-// write `last`.
-template <typename T, int V, int W>
+// write `last`, the W-1 rows that a continuation needs.  A thread walks down
+// its rows with the last W of them in registers, slot r mod W each, and the
+// next W on their way.
+template <typename T, int V, int W, bool kWide>
 __global__ void __launch_bounds__(kThreads) conv_kernel(ConvArgs<T> a) {
-  const int64_t cvs = a.channels / V;
+  const int64_t cvs = (a.channels + V - 1) / V;
   const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t c = id % cvs * V;
   const int64_t item = id / cvs, runs = a.runs * a.batches;
+  Own<T, V, W, kWide> own(a, id % cvs, cvs);
+  using Row = typename Own<T, V, W, kWide>::Row;
+  constexpr int P = V / 2;
+  const int64_t c = own.c;
   if (item >= runs) {
-    if (a.last && item - runs < (int64_t)a.sequences * (W - 1))
-      write_last<T, V, W>(a, item - runs, c);
+    const int64_t rest = item - runs;
+    if (!a.last || rest >= (int64_t)a.sequences * (W - 1)) return;
+    constexpr int kPast = W > 1 ? W - 1 : 1;  // W == 1 has no past and returned
+    const Span s = span_at(a, rest / kPast);
+    own.b = a.offsets ? 0 : s.seq;
+    const Row r = own.value(s, s.hi - s.lo - (W - 1) + rest % kPast);
+    r.template store<kWide>(a.last + rest * a.channels + c, own.count, own.gap);
     return;
   }
-  const int64_t b = item / a.runs, t0 = item % a.runs * (kBlockRows * a.blocks);
+  const int64_t b = own.b = item / a.runs, t0 = item % a.runs * (kBlockRows * a.blocks);
   const int64_t t1 = min(t0 + kBlockRows * a.blocks, a.rows);
-  float w[W][V], bias[V];
-  load_params<T, V, W>(a, c, w, bias);
-  Span s = span_of(a, b, t0);
-  for (int64_t t = t0; t < t1; t += kBlockRows) {
-    if (t >= s.lo + (W - 1) && t + kBlockRows <= min(s.hi, t1)) {
-      Vec<T, V> in[kBlockRows + W - 1];
+  own.params();
+  for (int64_t lo = t0; lo < t1;) {
+    const Span s = span_of(a, b, lo);
+    const int64_t hi = min(s.hi, t1);
+    float2 x[W][P];
+    own.window(s, lo - s.lo, x);
+    const T *from = a.x.at(b, lo) + c;
+    T *to = a.y.at(b, lo) + c;
+    auto row = [&](int j, const Row &r) {
 #pragma unroll
-      for (int r = 0; r < kBlockRows + W - 1; ++r)
-        in[r] = *reinterpret_cast<const Vec<T, V> *>(a.x.at(b, t - (W - 1) + r) + c);
+      for (int i = 0; i < P; ++i) x[j][i] = r.pair(i);
+      float2 p[P];
+      own.pre(x, j, p);
 #pragma unroll
-      for (int r = 0; r < kBlockRows; ++r) {
-        float p[V];
+      for (int i = 0; i < P; ++i)
+        if (a.silu) p[i] = silu2(p[i]);
+      own.put(to, p);
+      to += a.y.row;
+    };
+    int left = (int)(hi - lo);
+    constexpr int G = kAhead<W>;
+    Row next[G];
+    if (left >= G) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          p[v] = bias[v];
+      for (int j = 0; j < G; ++j, from += a.x.row) next[j] = own.row(from);
+    }
+    for (; left >= G; left -= G) {
+      Row now[G];
 #pragma unroll
-          for (int k = 0; k < W; ++k) p[v] = fmaf(w[k][v], to_f(in[r + k].v[v]), p[v]);
-          if (a.silu) p[v] = silu(p[v]);
-        }
-        store_vec<T, V>(a.y.at(b, t + r) + c, p);
+      for (int j = 0; j < G; ++j) now[j] = next[j];
+      if (left >= 2 * G) {
+#pragma unroll
+        for (int j = 0; j < G; ++j, from += a.x.row) next[j] = own.row(from);
       }
-      continue;
+#pragma unroll
+      for (int j = 0; j < G; ++j) row(j % W, now[j]);
     }
-    const int64_t te = min(t + kBlockRows, t1);
-    for (int64_t r = t; r < te; ++r) {
-      if (r >= s.hi) s = span_of(a, b, r);
-      float p[V];
-      pre_at<T, V, W>(a, b, s, r - s.lo, c, w, bias, p);
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (a.silu) p[v] = silu(p[v]);
-      store_vec<T, V>(a.y.at(b, r) + c, p);
+    for (int j = 0; j < G - 1; ++j) {
+      if (j >= left) break;
+      row(j % W, own.row(from));
+      from += a.x.row;
     }
-    if (te < t1 && te >= s.hi) s = span_of(a, b, te);
-  }
-}
-
-// dp_i from the definition.
-template <typename T, int V, int W>
-__device__ __forceinline__ void dpre_at(const ConvArgs<T> &a, int64_t b, const Span &s, int64_t i,
-                                        int64_t c, const float (&w)[W][V], const float (&bias)[V],
-                                        float (&dp)[V]) {
-  load_vec<T, V>(dp, a.dy.at(b, s.lo + i) + c);
-  if (!a.silu) return;
-  float p[V];
-  pre_at<T, V, W>(a, b, s, i, c, w, bias, p);
-#pragma unroll
-  for (int v = 0; v < V; ++v) dp[v] *= dsilu(p[v]);
-}
-
-// The gradient of row i of a sequence, i >= -(W-1).
-template <typename T, int V, int W>
-__device__ __forceinline__ void drow_at(const ConvArgs<T> &a, int64_t b, const Span &s, int64_t i,
-                                        int64_t c, const float (&w)[W][V], const float (&bias)[V],
-                                        float (&dx)[V]) {
-  const int64_t len = s.hi - s.lo, tail = i - (len - (W - 1));
-  if (tail >= 0 && a.dlast && s.seq >= 0) {
-    load_vec<T, V>(dx, a.dlast + ((int64_t)s.seq * (W - 1) + tail) * a.channels + c);
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; ++v) dx[v] = 0.f;
-  }
-#pragma unroll
-  for (int k = 0; k < W; ++k) {
-    const int64_t j = i + (W - 1) - k;
-    if (j < 0 || j >= len) continue;
-    float dp[V];
-    dpre_at<T, V, W>(a, b, s, j, c, w, bias, dp);
-#pragma unroll
-    for (int v = 0; v < V; ++v) dx[v] = fmaf(w[k][v], dp[v], dx[v]);
+    lo = hi;
   }
 }
 
 // dx and each run's share of dw and dbias: one thread per V channels and run;
-// the threads past the runs write dstate.
-template <typename T, int V, int W>
+// the threads past the runs write dstate.  A thread walks down its rows (and,
+// for the last of them, W-1 rows on) with the last W rows of x and of dp in
+// registers: row r gives p_r, dp_r, its terms of dw, and
+// dx_{r-(W-1)} = sum_k w_k dp_{r-k}.
+template <typename T, int V, int W, bool kWide>
 __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
-  const int64_t cvs = a.channels / V;
+  const int64_t cvs = (a.channels + V - 1) / V;
   const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t c = id % cvs * V;
   const int64_t item = id / cvs, runs = a.runs * a.batches;
-  float w[W][V], bias[V];
+  Own<T, V, W, kWide> own(a, id % cvs, cvs);
+  using Row = typename Own<T, V, W, kWide>::Row;
+  constexpr int P = V / 2;
+  const int64_t c = own.c;
+  // dlast of the row that lies i before the end of what sequence s would
+  // continue to, or zeros
+  auto after = [&](const Span &s, int64_t i, float2 (&dx)[P]) {
+    if (!a.dlast || s.seq < 0) return;
+    const Row r = own.row(a.dlast + ((int64_t)s.seq * (W - 1) + i) * a.channels + c);
+#pragma unroll
+    for (int j = 0; j < P; ++j) dx[j] = r.pair(j);
+  };
   if (item >= runs) {
+    // row i = k - (W-1) < 0 of sequence s: taps of its first rows
     const int64_t rest = item - runs;
     if (!a.dstate || rest >= (int64_t)a.sequences * (W - 1)) return;
-    load_params<T, V, W>(a, c, w, bias);
-    constexpr int kPast = W > 1 ? W - 1 : 1;  // W == 1 has no past and returned
-    const int64_t sq = rest / kPast, k = rest % kPast;
-    Span s{0, a.rows, (int)sq};
-    if (a.offsets) {
-      s.lo = min(max((int64_t)a.offsets[sq], (int64_t)0), a.rows);
-      s.hi = min(max((int64_t)a.offsets[sq + 1], s.lo), a.rows);
+    constexpr int kPast = W > 1 ? W - 1 : 1;
+    const Span s = span_at(a, rest / kPast);
+    own.b = a.offsets ? 0 : s.seq;
+    own.params();
+    const int64_t i = rest % kPast - (W - 1), len = s.hi - s.lo;
+    float2 x[W][P], dp[P], dx[P] = {};
+    if (i >= len - (W - 1)) after(s, i - (len - (W - 1)), dx);
+    own.window(s, 0, x);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+      if (j > i + (W - 1) || j >= len) break;
+      const Row r = own.value(s, j);
+#pragma unroll
+      for (int n = 0; n < P; ++n) x[j][n] = r.pair(n);
+      own.dpre(x, j, own.row(a.dy.at(own.b, s.lo + j) + c), dp);
+      const int64_t k = i + (W - 1) - j;  // the tap of row i in row j
+#pragma unroll
+      for (int m = 0; m < W; ++m)
+        if (m == k)
+#pragma unroll
+          for (int n = 0; n < P; ++n) dx[n] = __ffma2_rn(own.w[m][n], dp[n], dx[n]);
     }
-    float dx[V];
-    drow_at<T, V, W>(a, a.offsets ? 0 : sq, s, k - (W - 1), c, w, bias, dx);
-    store_vec<T, V>(a.dstate + rest * a.channels + c, dx);
+    own.put(a.dstate + rest * a.channels + c, dx);
     return;
   }
-  load_params<T, V, W>(a, c, w, bias);
-  const int64_t b = item / a.runs, t0 = item % a.runs * (kBlockRows * a.blocks);
+  const int64_t b = own.b = item / a.runs, t0 = item % a.runs * (kBlockRows * a.blocks);
   const int64_t t1 = min(t0 + kBlockRows * a.blocks, a.rows);
-  float dw[W][V], db[V];
+  own.params();
+  float2 dw[W][P] = {}, db[P] = {};
+  for (int64_t lo = t0; lo < t1;) {
+    const Span s = span_of(a, b, lo);
+    const int64_t hi = min(s.hi, t1);
+    float2 x[W][P], dp[W][P] = {};
+    own.window(s, lo - s.lo, x);
+    const T *px = a.x.at(b, lo) + c, *py = a.dy.at(b, lo) + c;
+    T *to = a.dx.at(b, lo - (W - 1)) + c;  // of the row that the next one completes
+    auto fill = [&](int j, const Row &r) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    db[v] = 0.f;
+      for (int i = 0; i < P; ++i) x[j][i] = r.pair(i);
+    };
+    auto weigh = [&](int j) {
 #pragma unroll
-    for (int k = 0; k < W; ++k) dw[k][v] = 0.f;
-  }
-  Span s = span_of(a, b, t0);
-  for (int64_t r = t0; r < t1; ++r) {
-    if (r >= s.hi) s = span_of(a, b, r);
-    const int64_t i = r - s.lo;
-    float g[V];
-    drow_at<T, V, W>(a, b, s, i, c, w, bias, g);
-    store_vec<T, V>(a.dx.at(b, r) + c, g);
-    dpre_at<T, V, W>(a, b, s, i, c, w, bias, g);
+      for (int i = 0; i < P; ++i) {
+        db[i] = __fadd2_rn(db[i], dp[j][i]);
 #pragma unroll
-    for (int k = 0; k < W; ++k) {
-      float x[V];
-      row_value<T, V, W>(a, b, s, i - (W - 1) + k, c, x);
+        for (int k = 0; k < W; ++k) dw[k][i] = __ffma2_rn(dp[j][i], x[(j + 1 + k) % W][i], dw[k][i]);
+      }
+    };
+    auto emit = [&](int j, bool store, float2 (&dx)[P]) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) dw[k][v] = fmaf(g[v], x[v], dw[k][v]);
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int k = 0; k < W; ++k) dx[i] = __ffma2_rn(own.w[k][i], dp[(j + W - k) % W][i], dx[i]);
+      if (store) own.put(to, dx);
+      to += a.dx.row;
+    };
+    const int n = (int)(hi - lo);
+    int r0 = 0;  // rows done
+    constexpr int G = kAhead<W>;
+    Row nx[G], ny[G];
+    auto fetch = [&]() {
+#pragma unroll
+      for (int j = 0; j < G; ++j, px += a.x.row, py += a.dy.row) nx[j] = own.row(px), ny[j] = own.row(py);
+    };
+    if (n >= G) fetch();
+    for (; r0 + G <= n; r0 += G) {
+      Row xs[G], ys[G];
+#pragma unroll
+      for (int j = 0; j < G; ++j) xs[j] = nx[j], ys[j] = ny[j];
+      if (r0 + 2 * G <= n) fetch();
+#pragma unroll
+      for (int j = 0; j < G; ++j) {
+        float2 dx[P] = {};
+        fill(j % W, xs[j]);
+        own.dpre(x, j % W, ys[j], dp[j % W]);
+        weigh(j % W);
+        emit(j % W, r0 + j >= W - 1, dx);
+      }
     }
+    // the rows left, and the W-1 beyond them that the last rows' dx still need
+    const int end = (int)(s.hi - lo);  // of the sequence
+#pragma unroll 1
+    for (; r0 < n + W - 1; r0 += W) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) db[v] += g[v];
+      for (int j = 0; j < W; ++j) {
+        const int r = r0 + j;
+        if (r >= n + W - 1) break;
+        float2 dx[P] = {};
+        if (r < end) {
+          fill(j, own.row(px));
+          own.dpre(x, j, own.row(py), dp[j]);
+          px += a.x.row;
+          py += a.dy.row;
+          if (r < n) weigh(j);
+        } else {
+#pragma unroll
+          for (int i = 0; i < P; ++i) dp[j][i] = make_float2(0.f, 0.f);
+          after(s, r - end, dx);
+        }
+        emit(j, r >= W - 1, dx);
+      }
+    }
+    lo = hi;
   }
+  float *share = a.parts + item * a.channels * (W + 1);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if (a.bias_parts) a.bias_parts[item * a.channels + c + v] = db[v];
+    if (!kWide && v >= own.count) continue;
+    share[a.channels * W + c + v * own.gap] = reinterpret_cast<const float *>(db)[v];
 #pragma unroll
-    for (int k = 0; k < W; ++k) a.parts[(item * a.channels + c + v) * W + k] = dw[k][v];
+    for (int k = 0; k < W; ++k) share[(c + v * own.gap) * W + k] = reinterpret_cast<const float *>(dw[k])[v];
   }
 }
 
 // One token: one thread per V channels and batch entry.
-template <typename T, int V, int W>
+template <typename T, int V, int W, bool kWide>
 __global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs<T> a) {
-  const int64_t cvs = a.channels / V;
+  const int64_t cvs = (a.channels + V - 1) / V;
   const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t c = id % cvs * V, b = id / cvs;
+  const int64_t b = id / cvs;
   if (b >= a.sequences) return;
-  const int64_t slot = a.slots ? a.slots[b] : b;
-  float p[V];
-  if (slot < 0 || slot >= a.num_slots) {
+  Own<T, V, W, kWide> own(a, id % cvs, cvs);
+  using Row = typename Own<T, V, W, kWide>::Row;
+  constexpr int P = V / 2;
+  const int64_t c = own.c, slot = a.slots ? a.slots[b] : b;
+  float2 p[P] = {};
+  if (slot >= 0 && slot < a.num_slots) {
+    T *cache = a.last + slot * (W - 1) * a.channels + c;
+    Row r[W];
 #pragma unroll
-    for (int v = 0; v < V; ++v) p[v] = 0.f;
-    store_vec<T, V>(a.y.at(b, 0) + c, p);
-    return;
+    for (int k = 0; k < W - 1; ++k) r[k] = own.row(cache + k * a.channels);
+    r[W - 1] = own.row(a.x.at(b, 0) + c);
+    own.params();
+    float2 x[W][P];
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      if (k > 0) r[k].template store<kWide>(cache + (k - 1) * a.channels, own.count, own.gap);
+#pragma unroll
+      for (int i = 0; i < P; ++i) x[k][i] = r[k].pair(i);
+    }
+    own.pre(x, W - 1, p);
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (a.silu) p[i] = silu2(p[i]);
   }
-  Vec<T, V> x[W];
-  T *cache = a.last + slot * (W - 1) * a.channels + c;
-#pragma unroll
-  for (int k = 0; k < W - 1; ++k)
-    x[k] = *reinterpret_cast<const Vec<T, V> *>(cache + k * a.channels);
-  x[W - 1] = *reinterpret_cast<const Vec<T, V> *>(a.x.at(b, 0) + c);
-  float w[W][V], bias[V];
-  load_params<T, V, W>(a, c, w, bias);
-#pragma unroll
-  for (int k = 0; k < W - 1; ++k) *reinterpret_cast<Vec<T, V> *>(cache + k * a.channels) = x[k + 1];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    p[v] = bias[v];
-#pragma unroll
-    for (int k = 0; k < W; ++k) p[v] = fmaf(w[k][v], to_f(x[k].v[v]), p[v]);
-    if (a.silu) p[v] = silu(p[v]);
-  }
-  store_vec<T, V>(a.y.at(b, 0) + c, p);
+  own.put(a.y.at(b, 0) + c, p);
 }
 
 // ------------------------------------------------------------- host side
 enum Call { kForward, kGrad, kStep };
 
-template <typename T, int V, int W>
-int launch(Call call, const ConvArgs<T> &a, cudaStream_t st) {
-  const int64_t cvs = a.channels / V;
+template <Call kCall, typename T, int V, int W, bool kWide>
+int launch(const ConvArgs<T> &a, cudaStream_t st) {
+  const int64_t cvs = (a.channels + V - 1) / V;
   int64_t items = a.runs * a.batches;
-  if (call == kStep) items = a.sequences;
-  else if (call == kForward ? a.last != nullptr : a.dstate != nullptr)
+  if (kCall == kStep) items = a.sequences;
+  else if (kCall == kForward ? a.last != nullptr : a.dstate != nullptr)
     items += (int64_t)a.sequences * (W - 1);
   const int64_t blocks = (items * cvs + kThreads - 1) / kThreads;
   if (blocks == 0) return TCU_DFT_OK;
   if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
-  if (call == kForward) conv_kernel<T, V, W><<<(unsigned)blocks, kThreads, 0, st>>>(a);
-  else if (call == kGrad) conv_grad_kernel<T, V, W><<<(unsigned)blocks, kThreads, 0, st>>>(a);
-  else conv_step_kernel<T, V, W><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+  const dim3 grid((unsigned)blocks);
+  if constexpr (kCall == kForward) conv_kernel<T, V, W, kWide><<<grid, kThreads, 0, st>>>(a);
+  else if constexpr (kCall == kGrad) conv_grad_kernel<T, V, W, kWide><<<grid, kThreads, 0, st>>>(a);
+  else conv_step_kernel<T, V, W, kWide><<<grid, kThreads, 0, st>>>(a);
   return launched();
 }
 
-template <typename T, int V>
-int by_width(Call call, int width, const ConvArgs<T> &a, cudaStream_t st) {
+template <Call kCall, typename T, int V, bool kWide>
+int by_width(int width, const ConvArgs<T> &a, cudaStream_t st) {
   switch (width) {
-    case 1: return launch<T, V, 1>(call, a, st);
-    case 2: return launch<T, V, 2>(call, a, st);
-    case 3: return launch<T, V, 3>(call, a, st);
-    case 4: return launch<T, V, 4>(call, a, st);
-    case 5: return launch<T, V, 5>(call, a, st);
-    case 6: return launch<T, V, 6>(call, a, st);
-    case 7: return launch<T, V, 7>(call, a, st);
-    case 8: return launch<T, V, 8>(call, a, st);
+    case 1: return launch<kCall, T, V, 1, kWide>(a, st);
+    case 2: return launch<kCall, T, V, 2, kWide>(a, st);
+    case 3: return launch<kCall, T, V, 3, kWide>(a, st);
+    case 4: return launch<kCall, T, V, 4, kWide>(a, st);
+    case 5: return launch<kCall, T, V, 5, kWide>(a, st);
+    case 6: return launch<kCall, T, V, 6, kWide>(a, st);
+    case 7: return launch<kCall, T, V, 7, kWide>(a, st);
+    case 8: return launch<kCall, T, V, 8, kWide>(a, st);
   }
   return TCU_DFT_ERR_UNSUPPORTED;
 }
 
 struct Shape {
-  int64_t batches, rows, runs;
-  int blocks;
+  int64_t batches, runs;
+  int blocks;  // of kBlockRows rows in a run
 };
 
-Shape shape_of(const tcu_short_conv_args &a) {
+// Runs as long as eight blocks, so that few rows are read twice and few shares
+// of dw written, but short enough to give every SM its 1024 threads.
+Shape shape_of(const tcu_short_conv_args &a, int values) {
   Shape s;
   s.batches = a.offsets ? 1 : a.sequences;
-  s.rows = a.rows;
-  s.blocks = 4;
-  s.runs = (a.rows + kBlockRows * s.blocks - 1) / (kBlockRows * s.blocks);
+  const int64_t tall = (a.rows + kBlockRows - 1) / kBlockRows;
+  const int64_t threads = s.batches * tall * ((a.channels + values - 1) / values);
+  s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(16, threads / (1024 * num_sms())));
+  s.runs = (tall + s.blocks - 1) / s.blocks;
   return s;
 }
 
-int64_t grad_parts(const tcu_short_conv_args &a) {
-  const Shape s = shape_of(a);
-  return s.runs * s.batches;
-}
+// Values a thread of the gradient owns: rows in words of 8 or 16 bytes.
+constexpr int kGradValues = 2;
 
 int check_sizes(const tcu_short_conv_args *a) {
   if (!a || a->type < TCU_SEQ_F32 || a->type > TCU_SEQ_F16 || a->sequences < 0 || a->rows < 0 ||
@@ -366,7 +458,10 @@ int check_sizes(const tcu_short_conv_args *a) {
 
 template <typename T>
 int dispatch(Call call, const tcu_short_conv_args &s, cudaStream_t st) {
-  const Shape sh = shape_of(s);
+  constexpr int most = 4;
+  const int V = call == kGrad ? kGradValues : most;
+  const Shape sh = shape_of(s, V);
+  const int word = V * sizeof(T);
   ConvArgs<T> a{};
   a.x = rows_of<const T>(s.x);
   a.y = rows_of<T>(s.y);
@@ -388,25 +483,27 @@ int dispatch(Call call, const tcu_short_conv_args &s, cudaStream_t st) {
   a.silu = s.silu;
   a.runs = sh.runs;
   a.blocks = sh.blocks;
-  const int64_t parts = sh.runs * sh.batches;
-  if (call == kGrad) {
-    a.parts = static_cast<float *>(s.workspace);
-    a.bias_parts = s.dbias ? a.parts + parts * s.channels * s.width : nullptr;
-  }
-  constexpr int V = 16 / sizeof(T);
-  bool wide = s.channels % V == 0 && rows_aligned(s.x, s.type, sh.batches, s.rows, 16);
+  if (call == kGrad) a.parts = static_cast<float *>(s.workspace);
+  const int64_t batches = call == kStep ? s.sequences : sh.batches;
+  bool wide = s.channels % V == 0 && rows_aligned(s.x, s.type, batches, s.rows, word);
   if (call == kGrad)
-    wide = wide && rows_aligned(s.dy, s.type, sh.batches, s.rows, 16) &&
-           rows_aligned(s.dx, s.type, sh.batches, s.rows, 16);
+    wide = wide && rows_aligned(s.dy, s.type, batches, s.rows, word) &&
+           rows_aligned(s.dx, s.type, batches, s.rows, word);
   else
-    wide = wide && rows_aligned(s.y, s.type, sh.batches, s.rows, 16);
+    wide = wide && rows_aligned(s.y, s.type, batches, s.rows, word);
   for (const void *p : {s.state, s.dlast, (const void *)s.last, (const void *)s.dstate})
-    wide = wide && (uintptr_t)p % 16 == 0;
-  const int rc = wide ? by_width<T, V>(call, s.width, a, st) : by_width<T, 1>(call, s.width, a, st);
-  if (rc != TCU_DFT_OK || call != kGrad) return rc;
-  const int rw = sum_parts(s.dweight, a.parts, parts, s.channels * s.width, st);
-  if (rw != TCU_DFT_OK || !s.dbias) return rw;
-  return sum_parts(s.dbias, a.bias_parts, parts, s.channels, st);
+    wide = wide && (uintptr_t)p % word == 0;
+  if (call == kForward)
+    return wide ? by_width<kForward, T, most, true>(s.width, a, st)
+                : by_width<kForward, T, 2, false>(s.width, a, st);
+  if (call == kStep)
+    return wide ? by_width<kStep, T, most, true>(s.width, a, st) : by_width<kStep, T, 2, false>(s.width, a, st);
+  const int rc = wide ? by_width<kGrad, T, kGradValues, true>(s.width, a, st)
+                      : by_width<kGrad, T, 2, false>(s.width, a, st);
+  if (rc != TCU_DFT_OK) return rc;
+  const int64_t weights = s.channels * s.width;
+  const Sum sums[] = {{s.dweight, a.parts, weights}, {s.dbias, a.parts + weights, s.channels}};
+  return sum_parts(sums, s.dbias ? 2 : 1, sh.runs * sh.batches, weights + s.channels, st);
 }
 
 int by_type(Call call, const tcu_short_conv_args &a, cudaStream_t st) {
@@ -419,17 +516,40 @@ int by_type(Call call, const tcu_short_conv_args &a, cudaStream_t st) {
 
 }  // namespace
 
-__global__ void sum_parts_kernel(float *out, const float *partial, int64_t parts, int64_t count) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i >= count) return;
+// A block sums 32 adjacent values, eight threads each, the eight in order.
+struct Sums {
+  Sum s[3];
+};
+__global__ void __launch_bounds__(256) sum_parts_kernel(Sums sums, int count, int64_t parts,
+                                                        int64_t stride) {
+  __shared__ float part[8][33];
+  int64_t i = (int64_t)blockIdx.x * 32 + threadIdx.x % 32;
+  const int y = threadIdx.x / 32;
+  int k = 0;
+  while (k < count && i >= sums.s[k].count) i -= sums.s[k++].count;
   float s = 0.f;
-  for (int64_t p = 0; p < parts; ++p) s += partial[p * count + i];
-  out[i] = s;
+  if (k < count) {
+    const float *from = sums.s[k].parts + i;
+#pragma unroll 8
+    for (int64_t p = y; p < parts; p += 8) s += from[p * (stride > 0 ? stride : sums.s[k].count)];
+  }
+  part[y][threadIdx.x % 32] = s;
+  __syncthreads();
+  if (y > 0 || k >= count) return;
+#pragma unroll
+  for (int j = 1; j < 8; ++j) s += part[j][threadIdx.x % 32];
+  sums.s[k].out[i] = s;
 }
 
-int sum_parts(float *out, const float *partial, int64_t parts, int64_t count, cudaStream_t st) {
-  if (count == 0) return TCU_DFT_OK;
-  sum_parts_kernel<<<(unsigned)((count + 127) / 128), 128, 0, st>>>(out, partial, parts, count);
+int sum_parts(const Sum *sums, int count, int64_t parts, int64_t stride, cudaStream_t st) {
+  Sums a{};
+  int64_t n = 0;
+  for (int k = 0; k < count; ++k) {
+    a.s[k] = sums[k];
+    n += sums[k].count;
+  }
+  if (n == 0) return TCU_DFT_OK;
+  sum_parts_kernel<<<(unsigned)((n + 31) / 32), 256, 0, st>>>(a, count, parts, stride);
   return launched();
 }
 
@@ -440,7 +560,8 @@ using namespace tcu::seq;
 
 extern "C" int64_t tcu_short_conv_grad_workspace(const tcu_short_conv_args *a) {
   if (check_sizes(a) != TCU_DFT_OK) return -1;
-  return grad_parts(*a) * a->channels * (a->width + 1) * 4;
+  const Shape s = shape_of(*a, kGradValues);
+  return s.runs * s.batches * a->channels * (a->width + 1) * 4;
 }
 
 extern "C" int tcu_short_conv(const tcu_short_conv_args *a, void *stream) {

@@ -181,7 +181,7 @@ constexpr int scan_pairs(int ls) { return ls <= 8 ? 4 : ls == 16 ? 2 : 1; }
 constexpr int scan_channels(int ls) { return scan_pairs(ls) * (32 / ls) * scan_ch(ls); }
 // blocks that registers and shared memory let an SM hold
 constexpr int scan_resident(int ls) { return ls <= 4 ? 2 : ls == 32 ? 2 : 1; }
-template <int LS_, typename T>
+template <int LS_, typename T, bool kWide>
 struct Lay {
   static constexpr int LS = LS_, CH = scan_ch(LS), NP = 4 * LS;
   static constexpr int kPairs = scan_pairs(LS), kBlock = 64 * kPairs;
@@ -192,7 +192,7 @@ struct Lay {
   // other's banks
   static constexpr int kYLane = LS == 2 ? 48 : LS == 4 ? 40 : LS == 32 ? 4 : WC + 4;
   static constexpr int kYRow = LS * kYLane + 4;
-  static constexpr int kRaw = Raw<T, V>::kWords;
+  static constexpr int kRaw = Raw<T, V, !kWide>::kWords;
   // shared memory, in floats
   static constexpr int kBC = RP * NP;  // a piece of B or C
   static constexpr int kPairFloats =
@@ -268,7 +268,8 @@ enum ScanMode { kOutputs, kState, kAdjoint };
 template <typename T, int LS, bool kPacked, ScanMode kMode, bool kWide>
 __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     scan_kernel(ScanArgs<T> a) {
-  using L = Lay<LS, T>;
+  using L = Lay<LS, T, kWide>;
+  using Row = Raw<T, L::V, !kWide>;
   constexpr int CH = L::CH, PAIRS = CH / 2, V = L::V, RP = L::RP;
   constexpr bool kLocal = kMode != kOutputs, kBack = kMode == kAdjoint;
   extern __shared__ __align__(16) float smem[];
@@ -308,7 +309,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     const int last = (int)(w.r1 - w.r0) - vr;  // this lane's row is in piece i if i RP < last
     auto slot = [&](int i, int which) { return ring + ((i % kRing * 3 + which) * 32 + lane) * L::kRaw; };
     // piece i of u, dt, gate on its way to the ring
-    Raw<T, V> hold[3];
+    Row hold[3];
     auto fetch = [&](int i) {
       const bool in = i * RP < last && vcount > 0;
       if constexpr (kWide) {
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       }
     };
     auto take = [&](int i, int which) {
-      Raw<T, V> r;
+      Row r;
 #pragma unroll
       for (int j = 0; j < L::kRaw; ++j) r.w[j] = slot(i, which)[j];
       return r;
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       }
     };
     auto stage = [&](int i) {
-      const Raw<T, V> u = take(i, 0), dt = take(i, 1);
+      const Row u = take(i, 0), dt = take(i, 1);
       float *od = sdx + i % 2 * 2 * RP * L::kRow + vr * L::kRow + vc, *ox = od + RP * L::kRow;
       float2 d[V / 2], x[V / 2];
 #pragma unroll
@@ -395,7 +396,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       }
     };
     auto finish = [&](int i) {
-      const Raw<T, V> u = take(i, 0), z = take(i, 2);
+      const Row u = take(i, 0), z = take(i, 2);
       const float *from = sy + i % 2 * RP * L::kYRow + vr * L::kYRow + vc;
       float2 o[V / 2];
 #pragma unroll
@@ -409,7 +410,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
           o[v] = __fadd2_rn(o[v], make_float2(y4.x, y4.y));
           o[v + 1] = __fadd2_rn(o[v + 1], make_float2(y4.z, y4.w));
         }
-      Raw<T, V> out;
+      Row out;
 #pragma unroll
       for (int v = 0; v < V / 2; ++v) {
         if (pz) o[v] = __fmul2_rn(o[v], silu2(z.pair(v)));
@@ -730,7 +731,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
 #pragma unroll
     for (int v = 0; v < V / 2; ++v) dskip[v] = dbias[v] = make_float2(0.f, 0.f);
     struct In {
-      Raw<T, V> u, dt, z, dy;
+      Raw<T, V, !kWide> u, dt, z, dy;
     };
     // this lane's first row of the tile that the first warps are at
     const int64_t row = row_of(0) + vr;
@@ -764,7 +765,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       const float *from = sdxq + i % 2 * 3 * L::kPlane + (pass * L::RP + vr) * L::kRow + vc;
       const int64_t r = row_of(i) + pass * L::RP + vr;
       const int count = r < w.r1 ? vcount : 0;
-      Raw<T, V> du, ddt, dz;
+      Raw<T, V, !kWide> du, ddt, dz;
 #pragma unroll
       for (int k = 0; k < V / 2; ++k) {
         const float2 v = *reinterpret_cast<const float2 *>(from + 2 * k);

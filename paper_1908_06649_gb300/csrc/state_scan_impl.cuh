@@ -87,22 +87,22 @@ int start(int64_t blocks, int threads, int floats, const ScanArgs<T> &a, cudaStr
 template <typename T, int LS, bool kPacked, bool kWide>
 int forward(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
   const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
-  constexpr int floats = Lay<LS, T>::kFloats;
+  constexpr int floats = Lay<LS, T, kWide>::kFloats;
   if (p.chunks > 1) {
-    if (const int rc = start<scan_kernel<T, LS, kPacked, kState, kWide>>(blocks, Lay<LS, T>::kBlock, floats,
+    if (const int rc = start<scan_kernel<T, LS, kPacked, kState, kWide>>(blocks, Lay<LS, T, kWide>::kBlock, floats,
                                                                       a, st))
       return rc;
     const int64_t count = a.channels * a.states * p.batches;
     carry_kernel<T, false><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
     if (const int rc = launched()) return rc;
   }
-  return start<scan_kernel<T, LS, kPacked, kOutputs, kWide>>(blocks, Lay<LS, T>::kBlock, floats, a, st);
+  return start<scan_kernel<T, LS, kPacked, kOutputs, kWide>>(blocks, Lay<LS, T, kWide>::kBlock, floats, a, st);
 }
 
 template <typename T, int LS, bool kPacked, bool kWide>
 int gradient(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
   if (p.chunks > 1) {
-    using F = Lay<LS, T>;
+    using F = Lay<LS, T, kWide>;
     ScanArgs<T> c = a;
     c.group_blocks = (a.per_group + F::DB - 1) / F::DB;
     const int64_t blocks = p.batches * p.chunks * a.groups * c.group_blocks;
@@ -161,10 +161,11 @@ int run_scan(ScanCall call, const tcu_state_scan_args &s, cudaStream_t st) {
   if (bc > 0) sum_bc_kernel<T><<<(unsigned)((bc + 127) / 128), 128, 0, st>>>(a);
   if ((rc = launched())) return rc;
   const int64_t parts = none ? 0 : p.batches * p.chunks;
-  if ((rc = sum_parts(s.dA, a.A_parts, parts, s.channels * s.states, st))) return rc;
-  if (s.dskip && (rc = sum_parts(s.dskip, a.skip_parts, parts, s.channels, st))) return rc;
-  if (s.ddt_bias && (rc = sum_parts(s.ddt_bias, a.bias_parts, parts, s.channels, st))) return rc;
-  return TCU_DFT_OK;
+  Sum sums[3] = {{s.dA, a.A_parts, s.channels * s.states}};
+  int count = 1;
+  if (s.dskip) sums[count++] = {s.dskip, a.skip_parts, s.channels};
+  if (s.ddt_bias) sums[count++] = {s.ddt_bias, a.bias_parts, s.channels};
+  return sum_parts(sums, count, parts, 0, st);
 }
 
 }  // namespace seq
