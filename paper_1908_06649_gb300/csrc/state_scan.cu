@@ -23,7 +23,7 @@ ScanPlan plan_of(const tcu_state_scan_args &a, bool grad) {
   const int64_t tiles = (a.rows + kTile - 1) / kTile;
   // Where the blocks leave more than half of the card's slots empty, rows are
   // split so that all blocks run at once.
-  const int64_t slots = (grad ? grad_resident(p.ls) : scan_resident(p.ls)) * (int64_t)num_sms();
+  const int64_t slots = (grad ? grad_resident(p.ls) : kResident) * (int64_t)num_sms();
   int64_t chunks = blocks == 0 || blocks * 2 > slots ? 1 : slots / blocks;
   chunks = std::max<int64_t>(1, std::min(chunks, tiles / 2));
   const int64_t chunk_tiles = std::max<int64_t>(1, (tiles + chunks - 1) / chunks);

@@ -175,28 +175,30 @@ __device__ __forceinline__ float step_of(const ScanArgs<T> &a, float dt, float b
 // The first warps come first, so that each SM quarter gets as many of either
 // kind.  What the inner loop draws from shared memory, whose pipe returns 32
 // words a clock whatever lanes share, is 2 CH + 2 * 4 words for CH * 4 states.
-constexpr int kRing = 4;  // pieces of raw rows: one behind, the current one, two ahead
 constexpr int scan_ch(int ls) { return ls == 2 ? 2 : 4; }
-constexpr int scan_pairs(int ls) { return ls <= 8 ? 4 : ls == 16 ? 2 : 1; }
-constexpr int scan_channels(int ls) { return scan_pairs(ls) * (32 / ls) * scan_ch(ls); }
-// blocks that registers and shared memory let an SM hold
-constexpr int scan_resident(int ls) { return ls <= 4 ? 2 : ls == 32 ? 2 : 1; }
+constexpr int kPairs = 4;
+constexpr int scan_channels(int ls) { return kPairs * (32 / ls) * scan_ch(ls); }
+constexpr int kResident = 2;  // blocks that registers and shared memory let an SM hold
 template <int LS_, typename T, bool kWide>
 struct Lay {
   static constexpr int LS = LS_, CH = scan_ch(LS), NP = 4 * LS;
-  static constexpr int kPairs = scan_pairs(LS), kBlock = 64 * kPairs;
-  static constexpr int WC = 32 / LS * CH, V = WC < 8 ? WC : 8, DB = kPairs * WC;
-  static constexpr int COLS = WC / V, RP = 32 / COLS;
+  static constexpr int kBlock = 64 * kPairs;
+  static constexpr int WC = 32 / LS * CH, DB = kPairs * WC;
+  static constexpr int RP = 8, V = WC >= 8 ? WC / 4 : 2;
+  static constexpr int COLS = WC / V, kActive = RP * COLS;  // lanes that own values
   static constexpr int kRow = WC + 4;  // pitch of d, d u
   // pitches of the lanes' shares of o: 8 lanes' 16-byte accesses miss each
   // other's banks
   static constexpr int kYLane = LS == 2 ? 48 : LS == 4 ? 40 : LS == 32 ? 4 : WC + 4;
   static constexpr int kYRow = LS * kYLane + 4;
   static constexpr int kRaw = Raw<T, V, !kWide>::kWords;
+  // pieces of raw rows: one behind, the current one, and two ahead, or one
+  // where they would leave no room for a second block
+  static constexpr int kRing = kRaw * V > 32 ? 3 : 4;
   // shared memory, in floats
   static constexpr int kBC = RP * NP;  // a piece of B or C
   static constexpr int kPairFloats =
-      4 * kBC + 2 * WC + 2 * (2 * RP * kRow + RP * kYRow) + kRing * 3 * 32 * kRaw;
+      4 * kBC + 2 * WC + 2 * (2 * RP * kRow + RP * kYRow) + kRing * 3 * kActive * kRaw;
   static constexpr int kFloats = kPairs * kPairFloats;
 };
 
@@ -266,15 +268,15 @@ __device__ __forceinline__ void store_states(const float2 (&h)[PAIRS][4], const 
 // decay after the sum: c <- a (c + q C).  kWide: rows in words of V values.
 enum ScanMode { kOutputs, kState, kAdjoint };
 template <typename T, int LS, bool kPacked, ScanMode kMode, bool kWide>
-__global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
+__global__ void __launch_bounds__(64 * kPairs, kResident)
     scan_kernel(ScanArgs<T> a) {
   using L = Lay<LS, T, kWide>;
   using Row = Raw<T, L::V, !kWide>;
-  constexpr int CH = L::CH, PAIRS = CH / 2, V = L::V, RP = L::RP;
+  constexpr int kRing = L::kRing, CH = L::CH, PAIRS = CH / 2, V = L::V, RP = L::RP;
   constexpr bool kLocal = kMode != kOutputs, kBack = kMode == kAdjoint;
   extern __shared__ __align__(16) float smem[];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int pair = warp % L::kPairs;
+  const int pair = warp % kPairs;
   float *sbc = smem + pair * L::kPairFloats;           // [2][B, C][RP][states]
   float *sbias = sbc + 4 * L::kBC, *sskip = sbias + L::WC;
   float *sdx = sskip + L::WC;                          // [2][d, x][RP][kRow]
@@ -290,9 +292,10 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     return kBack ? w.r1 - 1 - ((int64_t)i * RP + t) : w.r0 + (int64_t)i * RP + t;
   };
 
-  if (warp >= L::kPairs) {
+  if (warp >= kPairs) {
     // ---- rows into d, d u; sums into y
-    const int vr = lane / L::COLS, vc = lane % L::COLS * V, vcount = min(V, nc - vc);
+    const int vr = lane / L::COLS, vc = lane % L::COLS * V;
+    const int vcount = lane < L::kActive ? min(V, nc - vc) : 0;
     for (int c = lane; c < L::WC; c += 32) {
       sbias[c] = a.dt_bias && c < nc ? a.dt_bias[c0 + c] : 0.f;
       sskip[c] = a.skip && c < nc ? a.skip[c0 + c] : 0.f;
@@ -307,7 +310,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     constexpr int64_t way = kBack ? -RP : RP;
     const int64_t su = way * ru.row, sdt = way * a.dt.row, sz = way * a.gate.row, so = way * a.y.row;
     const int last = (int)(w.r1 - w.r0) - vr;  // this lane's row is in piece i if i RP < last
-    auto slot = [&](int i, int which) { return ring + ((i % kRing * 3 + which) * 32 + lane) * L::kRaw; };
+    auto slot = [&](int i, int which) { return ring + ((i % kRing * 3 + which) * L::kActive + lane) * L::kRaw; };
     // piece i of u, dt, gate on its way to the ring
     Row hold[3];
     auto fetch = [&](int i) {
@@ -334,6 +337,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
     };
     auto landed = [&](int i) {  // what fetch(i) loaded by value
       if constexpr (!kWide) {
+        if (lane >= L::kActive) return;
 #pragma unroll
         for (int k = 0; k < 3; ++k)
 #pragma unroll
@@ -378,6 +382,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       }
     };
     auto stage = [&](int i) {
+      if (lane >= L::kActive) return;
       const Row u = take(i, 0), dt = take(i, 1);
       float *od = sdx + i % 2 * 2 * RP * L::kRow + vr * L::kRow + vc, *ox = od + RP * L::kRow;
       float2 d[V / 2], x[V / 2];
@@ -390,12 +395,18 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
         else if (pz) x[v] = __fmul2_rn(x[v], silu2(take(i, 2).pair(v)));
       }
 #pragma unroll
-      for (int v = 0; v < V / 2; v += 2) {
-        *reinterpret_cast<float4 *>(od + 2 * v) = make_float4(d[v].x, d[v].y, d[v + 1].x, d[v + 1].y);
-        *reinterpret_cast<float4 *>(ox + 2 * v) = make_float4(x[v].x, x[v].y, x[v + 1].x, x[v + 1].y);
+      for (int v = 0; v < V / 2; ++v) {
+        if constexpr (V == 2) {
+          *reinterpret_cast<float2 *>(od) = d[0];
+          *reinterpret_cast<float2 *>(ox) = x[0];
+        } else if (v % 2 == 0) {
+          *reinterpret_cast<float4 *>(od + 2 * v) = make_float4(d[v].x, d[v].y, d[v + 1].x, d[v + 1].y);
+          *reinterpret_cast<float4 *>(ox + 2 * v) = make_float4(x[v].x, x[v].y, x[v + 1].x, x[v + 1].y);
+        }
       }
     };
     auto finish = [&](int i) {
+      if (lane >= L::kActive) return;
       const Row u = take(i, 0), z = take(i, 2);
       const float *from = sy + i % 2 * RP * L::kYRow + vr * L::kYRow + vc;
       float2 o[V / 2];
@@ -405,10 +416,14 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
 #pragma unroll
       for (int q = 0; q < LS; ++q)
 #pragma unroll
-        for (int v = 0; v < V / 2; v += 2) {
-          const float4 y4 = *reinterpret_cast<const float4 *>(from + q * L::kYLane + 2 * v);
-          o[v] = __fadd2_rn(o[v], make_float2(y4.x, y4.y));
-          o[v + 1] = __fadd2_rn(o[v + 1], make_float2(y4.z, y4.w));
+        for (int v = 0; v < V / 2; ++v) {
+          if constexpr (V == 2) {
+            o[0] = __fadd2_rn(o[0], *reinterpret_cast<const float2 *>(from + q * L::kYLane));
+          } else if (v % 2 == 0) {
+            const float4 y4 = *reinterpret_cast<const float4 *>(from + q * L::kYLane + 2 * v);
+            o[v] = __fadd2_rn(o[v], make_float2(y4.x, y4.y));
+            o[v + 1] = __fadd2_rn(o[v + 1], make_float2(y4.z, y4.w));
+          }
         }
       Row out;
 #pragma unroll
@@ -420,7 +435,7 @@ __global__ void __launch_bounds__(64 * scan_pairs(LS), scan_resident(LS))
       py += so;
     };
     auto ready = [&]() {
-      if constexpr (kWide) asm volatile("cp.async.wait_group 2;" ::: "memory");
+      if constexpr (kWide) asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
     };
 #pragma unroll 1
     for (int i = 0; i < kRing - 1; ++i) {
@@ -613,39 +628,49 @@ __global__ void carry_kernel(ScanArgs<T> a) {
   }
 }
 
-// One token: LS lanes per channel, 4 states each, the cache in place.
-template <typename T, int LS>
+// One token: LS lanes per channel, 4 states each, the cache in place.  The
+// cache read and written is nearly all it does: 16 bytes a lane either way.
+template <typename T, int LS, bool kWide>
 __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(ScanArgs<T> a) {
   const int64_t id = ((int64_t)blockIdx.x * kScanThreads + threadIdx.x) / LS;
-  const int sl = threadIdx.x % LS, n0 = sl * 4;
+  const int sl = threadIdx.x % LS, n0 = sl * 4, n = min(4, a.states - n0);
   const bool in = id < a.channels * a.sequences;
   const int64_t b = in ? id / a.channels : 0, c = in ? id % a.channels : 0;
   const int64_t slot = a.slots ? a.slots[b] : b;
   const bool live = in && slot >= 0 && slot < a.num_slots;
-  float o = 0.f, u = 0.f;
+  float o = 0.f, u = 0.f, z = 0.f;
   if (live) {
+    float *cache = a.last + (slot * a.channels + c) * a.states + n0;
+    const float *rate = a.A + c * a.states + n0;
+    const int64_t g = c / a.per_group * a.states + n0;
+    Raw<float, 4> h, A;
+    Raw<T, 4> B, C;
+    h.template load<kWide>(cache, n);
+    A.template load<kWide>(rate, n);
+    B.template load<kWide>(a.B.at(b, 0) + g, n);
+    C.template load<kWide>(a.C.at(b, 0) + g, n);
     u = to_f(a.u.at(b, 0)[c]);
+    if (a.gate.p) z = to_f(a.gate.at(b, 0)[c]);
     const float d = step_of(a, to_f(a.dt.at(b, 0)[c]), a.dt_bias ? a.dt_bias[c] : 0.f);
-    const float x = d * u;
-    float A[4], h[4];
-    load4(A, a.A + c * a.states, n0, a.states);
-    float *cache = a.last + (slot * a.channels + c) * a.states;
-    load4(h, cache, n0, a.states);
-    const int64_t g = c / a.per_group * a.states;
+    const float2 x = make_float2(d * u, d * u), e = make_float2(d * kLog2e, d * kLog2e);
+    float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (n0 + i >= a.states) continue;
-      h[i] = fmaf(exp2_fast(d * (A[i] * kLog2e)), h[i], x * to_f(a.B.at(b, 0)[g + n0 + i]));
-      o = fmaf(to_f(a.C.at(b, 0)[g + n0 + i]), h[i], o);
+    for (int i = 0; i < 2; ++i) {
+      const float2 r = __fmul2_rn(e, A.pair(i));
+      const float2 v = __ffma2_rn(make_float2(exp2_fast(r.x), exp2_fast(r.y)), h.pair(i),
+                                  __fmul2_rn(x, B.pair(i)));
+      h.set(i, v);
+      sum = __ffma2_rn(C.pair(i), v, sum);
     }
-    store4(cache, h, n0, a.states);
+    o = sum.x + sum.y;
+    h.template store<kWide>(cache, n);
   }
 #pragma unroll
   for (int s = LS / 2; s > 0; s /= 2) o += __shfl_xor_sync(~0u, o, s);
   if (!in || sl != 0) return;
   if (live) {
     if (a.skip) o = fmaf(a.skip[c], u, o);
-    if (a.gate.p) o *= silu(to_f(a.gate.at(b, 0)[c]));
+    if (a.gate.p) o *= silu(z);
   }
   a.y.at(b, 0)[c] = from_f<T>(live ? o : 0.f);
 }
@@ -662,7 +687,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(ScanArgs<T> a) 
 template <int LS_, typename T>
 struct GradLay {
   static constexpr int LS = LS_, CH = scan_ch(LS), NP = 4 * LS, E = 4 * CH, CL = 32 / LS;
-  static constexpr int kPairs = 4, kBlock = 64 * kPairs;
+  static constexpr int kBlock = 64 * kPairs;
   static constexpr int WC = CL * CH, DB = kPairs * WC;
   static constexpr int V = LS <= 8 ? 8 : LS == 16 ? 4 : 2;
   static constexpr int COLS = WC / V, RP = 32 / COLS, PASSES = kMark / RP;
@@ -701,7 +726,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   using L = GradLay<LS, T>;
   constexpr int CH = L::CH, PAIRS = CH / 2, V = L::V, E = L::E;
   extern __shared__ __align__(16) float smem[];
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, pair = warp % L::kPairs;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, pair = warp % kPairs;
   float *sBC = smem + 4;                                       // [2][B, C][row][states]
   float *own = sBC + 4 * L::kBC + pair * L::kPairFloats;
   float *sdxq = own;                                           // [2][d, x, q][row][kRow]
@@ -716,10 +741,10 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   auto row_of = [&](int i) { return w.r0 + (int64_t)(tiles - 1 - i) * kMark; };
   if (warp == 0) tmem_alloc(smem_u32(smem), L::kColumns);
 
-  if (warp >= L::kPairs) {
+  if (warp >= kPairs) {
     // ---- rows in and out
     const int vr = lane / L::COLS, vc = lane % L::COLS * V, vcount = min(V, nc - vc);
-    const int me = threadIdx.x - 32 * L::kPairs;  // of the second warps
+    const int me = threadIdx.x - 32 * kPairs;  // of the second warps
     for (int c = lane; c < L::WC; c += 32) {
       sbias[c] = a.dt_bias && c < nc ? a.dt_bias[c0 + c] : 0.f;
       sskip[c] = a.skip && c < nc ? a.skip[c0 + c] : 0.f;
@@ -802,7 +827,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
     auto stage_bc = [&](int i) {
       constexpr int items = kMark * LS;  // quads of B, then of C
       const int64_t row0 = row_of(i);
-      for (int item = me; item < 2 * items; item += 32 * L::kPairs) {
+      for (int item = me; item < 2 * items; item += 32 * kPairs) {
         const int which = item / items, t = item % items / LS, n = item % LS * 4;
         const Rows<const T> &src = which ? a.C : a.B;
         const int64_t r = row0 + t;
@@ -821,8 +846,8 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       const int64_t row0 = row_of(i);
       const int rows = (int)min((int64_t)kMark, w.r1 - row0);
       const float *from = sBC + 4 * L::kBC + 6 * L::kPlane + i % 2 * 2 * L::kBC;
-      const int live = min(L::kPairs, (w.nc + L::WC - 1) / L::WC);
-      for (int j = me; j < rows * 2 * L::NP; j += 32 * L::kPairs) {
+      const int live = min(kPairs, (w.nc + L::WC - 1) / L::WC);
+      for (int j = me; j < rows * 2 * L::NP; j += 32 * kPairs) {
         const int n = j % L::NP, which = j / L::NP % 2, t = j / (2 * L::NP);
         if (n >= a.states) continue;
         float s = 0.f;
@@ -884,7 +909,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   const int sl = lane % LS, n0 = sl * 4, ch0 = lane / LS * CH, count = nc - ch0;
   const int64_t at = c0 + ch0;
   // this thread's 16-byte slots: its mark, then its sum of dA
-  float4 *slots = reinterpret_cast<float4 *>(sBC + 4 * L::kBC + L::kPairs * L::kPairFloats) +
+  float4 *slots = reinterpret_cast<float4 *>(sBC + 4 * L::kBC + kPairs * L::kPairFloats) +
                   warp * 32 * (L::kThreadFloats / 4) + lane;
   float4 *asum = slots + 32 * (E / 4);
   float2 A2[PAIRS][4], e[PAIRS][4], dA[PAIRS][4];
@@ -1081,7 +1106,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   store_states(dA, a, a.A_parts + (part * a.channels + at) * a.states, n0, count);
   if (!kPacked && a.dstate && w.k == 0)
     store_states(e, a, a.dstate + (w.b * a.channels + at) * a.states, n0, count);
-  asm volatile("bar.sync 1, %0;" ::"r"(32 * L::kPairs) : "memory");  // the first warps
+  asm volatile("bar.sync 1, %0;" ::"r"(32 * kPairs) : "memory");  // the first warps
   if (warp == 0) tmem_dealloc(*reinterpret_cast<volatile uint32_t *>(smem), L::kColumns);
 }
 

@@ -6,7 +6,8 @@ namespace tcu {
 namespace seq {
 
 template <typename T>
-ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, bool grad) {
+ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, ScanCall call) {
+  const bool grad = call == kScanGrad, step = call == kScanStep;
   ScanArgs<T> a{};
   a.u = rows_of<const T>(s.u);
   a.dt = rows_of<const T>(s.dt);
@@ -37,7 +38,7 @@ ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, bool grad) 
   auto whole = [&](const void *q) { return (uintptr_t)q % 16 == 0; };
   a.wide_states = s.states % 4 == 0 && whole(s.A) && whole(s.state) && whole(s.last) &&
                   whole(s.marks) && whole(s.workspace) && whole(s.dlast) && whole(s.dstate);
-  const int64_t batches = p.batches, rows = s.rows;
+  const int64_t batches = step ? s.sequences : p.batches, rows = s.rows;
   a.wide_bc = s.states % 4 == 0 && rows_aligned(s.B, s.type, batches, rows, 4 * sizeof(T)) &&
               rows_aligned(s.C, s.type, batches, rows, 4 * sizeof(T));
   constexpr int most = 8;  // values of a word of rows, at most 16 bytes
@@ -124,7 +125,10 @@ int by_lanes(ScanCall call, const ScanPlan &p, const ScanArgs<T> &a, cudaStream_
     const int64_t count = a.channels * a.sequences * LS;
     const int64_t blocks = (count + kScanThreads - 1) / kScanThreads;
     if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
-    scan_step_kernel<T, LS><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
+    if (a.wide_states && a.wide_bc)
+      scan_step_kernel<T, LS, true><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
+    else
+      scan_step_kernel<T, LS, false><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
     return launched();
   }
   if (call == kScan) {
@@ -140,7 +144,7 @@ int by_lanes(ScanCall call, const ScanPlan &p, const ScanArgs<T> &a, cudaStream_
 template <typename T>
 int run_scan(ScanCall call, const tcu_state_scan_args &s, cudaStream_t st) {
   const ScanPlan p = plan_of(s, call == kScanGrad);
-  const ScanArgs<T> a = args_of<T>(s, p, call == kScanGrad);
+  const ScanArgs<T> a = args_of<T>(s, p, call);
   if (call != kScanStep && s.offsets && s.rows > 0) {
     row_sequence_kernel<<<(unsigned)((s.rows + 127) / 128), 128, 0, st>>>(
         a.row_seq, s.offsets, s.sequences, s.rows);

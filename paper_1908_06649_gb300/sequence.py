@@ -16,6 +16,7 @@ calls are what that runs; the ``_step`` calls have no gradient.
 from __future__ import annotations
 
 import ctypes
+import struct
 from collections import namedtuple
 
 import torch
@@ -69,7 +70,15 @@ class _ScanArgs(ctypes.Structure):
                 ("slots", _vp), ("num_slots", _i64)]
 
 
+# The same structures for struct.pack: what a call costs on the host counts
+# where a token's kernel takes a few microseconds.
+_CONV = struct.Struct("4i2qP" + "P2q" * 4 + "P" * 8 + "Pq" * 2)
+_SCAN = struct.Struct("4i3qP" + "P2q" * 6 + "P" * 8 + "P2q" * 6 + "P" * 3 + "Pq" * 2)
+assert _CONV.size == ctypes.sizeof(_ConvArgs) and _SCAN.size == ctypes.sizeof(_ScanArgs)
+_NO_ROWS = (0, 0, 0)
+
 _bound = None
+_calls = {}
 
 
 def _lib():
@@ -81,34 +90,45 @@ def _lib():
             args = ctypes.POINTER(_ConvArgs if "conv" in name else _ScanArgs)
             f.argtypes = [args] if name.endswith("workspace") else [args, _vp]
             f.restype = _i64 if name.endswith("workspace") else ctypes.c_int
+            f = _calls[name] = L[name]  # the same entry, for packed arguments
+            f.argtypes = [ctypes.c_char_p] if name.endswith("workspace") else [ctypes.c_char_p, _vp]
+            f.restype = _i64 if name.endswith("workspace") else ctypes.c_int
         _bound = L
     return _bound
 
 
-def _call(name, args, stream):
-    rc = getattr(_lib(), name)(args, stream)
+def _call(name, packed, stream):
+    f = _calls.get(name)
+    if f is None:
+        _lib()
+        f = _calls[name]
+    rc = f(packed, stream)
     if rc != OK:
         raise TcuDftError(rc, name)
+
+
+_current_device = torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 class _On:
     """The device and stream of a call, current while it allocates and
     launches: memory that a call takes for itself belongs to its stream."""
 
-    def __init__(self, device, stream):
+    def __init__(self, index, stream):
         self.stream = stream
-        self.guards = []
-        if device.index != torch.cuda.current_device():
-            self.guards.append(torch.cuda.device(device))
-        if stream is not None:
-            self.guards.append(torch.cuda.stream(stream))
-        self.device = device
+        self.index = index
+        self.guards = ()
+        if stream is not None or index != _current_device():
+            self.guards = [torch.cuda.device(index)]
+            if stream is not None:
+                self.guards.append(torch.cuda.stream(stream))
 
     def __enter__(self):
         for g in self.guards:
             g.__enter__()
-        s = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
-        return s.cuda_stream
+        return _raw_stream(self.index) if self.stream is None else self.stream.cuda_stream
 
     def __exit__(self, *exc):
         for g in reversed(self.guards):
@@ -120,35 +140,53 @@ def _tensor(t, name):
         raise TypeError("%s must be a torch tensor" % name)
 
 
-def _rows(t, name, like, shape):
-    """t as a row tensor of the type and device of `like`: (ptr, strides)."""
-    _tensor(t, name)
-    if t.dtype != like.dtype:
-        raise TypeError("%s must be %s, not %s" % (name, like.dtype, t.dtype))
-    if t.device != like.device:
-        raise ValueError("%s must be on %s" % (name, like.device))
-    if t.shape != shape:
-        raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-    st = t.stride()
-    # B and C: groups and states adjacent
-    if (st[-1] != 1 and shape[-1] != 1) or (
-            len(shape) > like.dim() and shape[-2] > 1 and st[-2] != shape[-1]):
-        raise ValueError("the values of a row of %s must be adjacent" % name)
-    if like.dim() == 3:
-        return _Rows(t.data_ptr(), st[0], st[1])
-    return _Rows(t.data_ptr(), 0, st[0])
-
-
-def _flat(t, name, dtype, device, shape):
-    """t as a contiguous array, or None: its address."""
-    if t is None:
-        return None
+def _wrong(t, name, dtype, index, shape, why):
+    """Raises what is wrong with t."""
     _tensor(t, name)
     if t.dtype != dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
-    if t.device != device or not t.is_contiguous() or t.shape != shape:
-        raise ValueError("%s must be contiguous, of shape %s, on %s"
-                         % (name, tuple(shape), device))
+    if t.get_device() != index:
+        raise ValueError("%s must be on cuda:%d, not %s" % (name, index, t.device))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+    raise ValueError("%s must %s" % (name, why))
+
+
+_ADJACENT = "hold the values of a row next to each other"
+
+
+def _rows(t, name, dtype, index, shape):
+    """t, (batch, rows, values) or (rows, values), as a row tensor: (pointer,
+    batch stride, row stride)."""
+    if not isinstance(t, torch.Tensor):
+        _tensor(t, name)
+    st = t.stride()
+    if (t.dtype is not dtype or t.shape != shape or t.get_device() != index
+            or (st[-1] != 1 and shape[-1] > 1)):
+        _wrong(t, name, dtype, index, shape, _ADJACENT)
+    return (t.data_ptr(), st[0], st[1]) if len(st) == 3 else (t.data_ptr(), 0, st[0])
+
+
+def _grouped_rows(t, name, dtype, index, shape):
+    """The same for (..., groups, states)."""
+    if not isinstance(t, torch.Tensor):
+        _tensor(t, name)
+    st = t.stride()
+    if (t.dtype is not dtype or t.shape != shape or t.get_device() != index
+            or (st[-1] != 1 and shape[-1] > 1) or (st[-2] != shape[-1] and shape[-2] > 1)):
+        _wrong(t, name, dtype, index, shape, _ADJACENT)
+    return (t.data_ptr(), st[0], st[1]) if len(st) == 4 else (t.data_ptr(), 0, st[0])
+
+
+def _flat(t, name, dtype, index, shape):
+    """t as a contiguous array: its address, or 0 for None."""
+    if t is None:
+        return 0
+    if not isinstance(t, torch.Tensor):
+        _tensor(t, name)
+    if (t.dtype is not dtype or t.shape != shape or t.get_device() != index
+            or not t.is_contiguous()):
+        _wrong(t, name, dtype, index, shape, "be contiguous")
     return t.data_ptr()
 
 
@@ -163,7 +201,7 @@ def _layout(x, name, offsets):
     if offsets is None:
         if len(shape) != 3:
             raise ValueError("%s must be (batch, length, channels)" % name)
-        return shape[0], shape[1], shape[2], None
+        return shape[0], shape[1], shape[2], 0
     if len(shape) != 2:
         raise ValueError("%s must be (rows, channels) with offsets" % name)
     _tensor(offsets, "offsets")
@@ -174,26 +212,24 @@ def _layout(x, name, offsets):
     return offsets.shape[0] - 1, shape[0], shape[1], offsets.data_ptr()
 
 
-def _slots(slots, batch, device):
-    if slots is None:
-        return None
-    return _flat(slots, "slots", torch.int32, device, (batch,))
-
-
-def _cache(state, slots, batch, tail, dtype, device):
-    """The address and entry count of a cache that a step advances."""
+def _cache(state, slots, batch, tail, dtype, index):
+    """(address, entries, address of slots) of a cache that a step advances."""
     _tensor(state, "state")
     if state.dim() != 1 + len(tail):
         raise ValueError("state must have shape (entries, %s)" % ", ".join(map(str, tail)))
     n = state.shape[0]
-    ptr = _flat(state, "state", dtype, device, (n,) + tail)
+    ptr = _flat(state, "state", dtype, index, (n,) + tail)
     if slots is None and n < batch:
         raise ValueError("state has %d entries for %d rows" % (n, batch))
-    return ptr, n
+    return ptr, n, _flat(slots, "slots", torch.int32, index, (batch,))
 
 
 def _wants_grad(*tensors):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _no_grad(*tensors):
@@ -201,30 +237,42 @@ def _no_grad(*tensors):
         raise ValueError("the single-token calls have no gradient")
 
 
+def _adjacent(t):
+    return t if t.shape[-1] == 1 or t.stride(-1) == 1 else t.contiguous()
+
+
+def _workspace(name, packed, device):
+    _lib()
+    n = _calls[name](packed)
+    if n < 0:
+        raise TcuDftError(2, name)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None, n
+
+
 # --------------------------------------------------------- short convolution
-def _conv_args(x, weight, bias, silu, state, offsets):
-    seqs, rows, ch, off = _layout(x, "x", offsets)
+def _width(weight):
     _tensor(weight, "weight")
     if weight.dim() != 2 or not 1 <= weight.shape[1] <= MAX_WIDTH:
         raise ValueError("weight must be (channels, width) with 1 <= width <= %d" % MAX_WIDTH)
-    width, f32, dev = weight.shape[1], torch.float32, x.device
-    a = _ConvArgs(type=_TYPES[x.dtype], width=width, silu=bool(silu), sequences=seqs,
-                  rows=rows, channels=ch, offsets=off, x=_rows(x, "x", x, x.shape),
-                  weight=_flat(weight, "weight", f32, dev, (ch, width)),
-                  bias=_flat(bias, "bias", f32, dev, (ch,)),
-                  state=_flat(state, "state", x.dtype, dev, (seqs, width - 1, ch)))
-    return a, (seqs, width - 1, ch)
+    return weight.shape[1]
 
 
 def _conv(x, weight, bias, silu, state, offsets, out, stream):
-    a, tail = _conv_args(x, weight, bias, silu, state, offsets)
-    with _On(x.device, stream) as st:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-        last = torch.empty(tail, dtype=x.dtype, device=x.device)
-        a.y = _rows(y, "out", x, x.shape)
-        a.last = last.data_ptr()
-        if a.channels:
-            _call("tcu_short_conv", a, st)
+    seqs, rows, ch, off = _layout(x, "x", offsets)
+    width, dtype, index = _width(weight), x.dtype, x.get_device()
+    tail = (seqs, width - 1, ch)
+    px = _rows(x, "x", dtype, index, x.shape)
+    pw = _flat(weight, "weight", torch.float32, index, (ch, width))
+    pb = _flat(bias, "bias", torch.float32, index, (ch,))
+    ps = _flat(state, "state", dtype, index, tail)
+    with _On(index, stream) as st:
+        y = torch.empty(x.shape, dtype=dtype, device=x.device) if out is None else out
+        last = torch.empty(tail, dtype=dtype, device=x.device)
+        py = _rows(y, "out", dtype, index, x.shape)
+        if ch:
+            _call("tcu_short_conv", _CONV.pack(
+                _TYPES[dtype], width, bool(silu), seqs, rows, ch, off, *px, *py, *_NO_ROWS,
+                *_NO_ROWS, pw, pb, ps, 0, last.data_ptr(), 0, 0, 0, 0, 0, 0, 0), st)
     return y, last
 
 
@@ -242,10 +290,6 @@ class _ShortConv(torch.autograd.Function):
         g = short_conv_grad(_adjacent(dy), x, weight, bias, silu=ctx.silu, state=state,
                             offsets=offsets, dlast=dlast.contiguous(), stream=ctx.stream)
         return g.x, g.weight, g.bias, g.state, None, None, None
-
-
-def _adjacent(t):
-    return t if t.shape[-1] == 1 or t.stride(-1) == 1 else t.contiguous()
 
 
 def short_conv(x, weight, bias=None, *, silu=False, state=None, offsets=None, out=None,
@@ -269,32 +313,33 @@ def short_conv_grad(dy, x, weight, bias=None, *, silu=False, state=None, offsets
                     dlast=None, stream=None):
     """Gradients of short_conv's (y, last) under dy and dlast (zeros if None):
     ConvGrads(x, weight, bias, state), the last two None where the argument is."""
-    a, tail = _conv_args(x, weight, bias, silu, state, offsets)
-    f32, dev = torch.float32, x.device
-    with _On(dev, stream) as st:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        dw = torch.empty(weight.shape, dtype=f32, device=dev)
-        db = torch.empty(bias.shape, dtype=f32, device=dev) if bias is not None else None
-        ds = torch.empty(tail, dtype=x.dtype, device=dev) if state is not None else None
-        a.dy, a.dx = _rows(dy, "dy", x, x.shape), _rows(dx, "dx", x, x.shape)
-        a.dlast = _flat(dlast, "dlast", x.dtype, dev, tail)
-        a.dweight = dw.data_ptr()
-        a.dbias = db.data_ptr() if db is not None else None
-        a.dstate = ds.data_ptr() if ds is not None else None
-        if a.channels:
-            work = _workspace("tcu_short_conv_grad_workspace", a, dev)
-            _call("tcu_short_conv_grad", a, st)
+    seqs, rows, ch, off = _layout(x, "x", offsets)
+    width, dtype, index, dev = _width(weight), x.dtype, x.get_device(), x.device
+    tail, f32 = (seqs, width - 1, ch), torch.float32
+    px = _rows(x, "x", dtype, index, x.shape)
+    pdy = _rows(dy, "dy", dtype, index, x.shape)
+    pw = _flat(weight, "weight", f32, index, (ch, width))
+    pb = _flat(bias, "bias", f32, index, (ch,))
+    ps = _flat(state, "state", dtype, index, tail)
+    pl = _flat(dlast, "dlast", dtype, index, tail)
+    with _On(index, stream) as st:
+        dx = torch.empty(x.shape, dtype=dtype, device=dev)
+        dw = torch.empty((ch, width), dtype=f32, device=dev)
+        db = torch.empty((ch,), dtype=f32, device=dev) if bias is not None else None
+        ds = torch.empty(tail, dtype=dtype, device=dev) if state is not None else None
+
+        def packed(work, size):
+            return _CONV.pack(
+                _TYPES[dtype], width, bool(silu), seqs, rows, ch, off, *px, *_NO_ROWS, *pdy,
+                *_rows(dx, "dx", dtype, index, x.shape), pw, pb, ps, pl, 0,
+                ds.data_ptr() if ds is not None else 0, dw.data_ptr(),
+                db.data_ptr() if db is not None else 0, work, size, 0, 0)
+
+        if ch:
+            work, n = _workspace("tcu_short_conv_grad_workspace", packed(0, 0), dev)
+            _call("tcu_short_conv_grad", packed(work.data_ptr() if n else 0, n), st)
             del work
     return ConvGrads(dx, dw, db, ds)
-
-
-def _workspace(name, a, device):
-    n = getattr(_lib(), name)(a)
-    if n < 0:
-        raise TcuDftError(2, name)
-    w = torch.empty(n, dtype=torch.uint8, device=device)
-    a.workspace, a.workspace_bytes = w.data_ptr(), n
-    return w
 
 
 def short_conv_step(x, state, weight, bias=None, *, silu=False, slots=None, out=None,
@@ -303,32 +348,24 @@ def short_conv_step(x, state, weight, bias=None, *, silu=False, slots=None, out=
     ``state`` (entries, width - 1, channels) is advanced in place, at entry
     slots[b] (int32) for row b, or entry b.  A slot outside the cache gives a
     row of zeros; no two rows may name the same one."""
-    _no_grad(x, weight, bias)
     _tensor(x, "x")
-    _tensor(weight, "weight")
     if x.dim() != 2 or x.dtype not in _TYPES or not x.is_cuda:
         raise ValueError("x must be a float32, bfloat16 or float16 CUDA tensor (batch, channels)")
-    if weight.dim() != 2 or not 1 <= weight.shape[1] <= MAX_WIDTH:
-        raise ValueError("weight must be (channels, width) with 1 <= width <= %d" % MAX_WIDTH)
+    _no_grad(x, weight, bias)
     batch, ch = x.shape
-    width, f32, dev = weight.shape[1], torch.float32, x.device
-    ptr, entries = _cache(state, slots, batch, (width - 1, ch), x.dtype, dev)
-    with _On(dev, stream) as st:
-        y = torch.empty((batch, ch), dtype=x.dtype, device=dev) if out is None else out
-        a = _ConvArgs(type=_TYPES[x.dtype], width=width, silu=bool(silu), sequences=batch, rows=1,
-                      channels=ch, x=_step_rows(x, "x", x, x.shape),
-                      y=_step_rows(y, "out", x, x.shape),
-                      weight=_flat(weight, "weight", f32, dev, (ch, width)),
-                      bias=_flat(bias, "bias", f32, dev, (ch,)), last=ptr,
-                      slots=_slots(slots, batch, dev), num_slots=entries)
+    width, dtype, index = _width(weight), x.dtype, x.get_device()
+    cache, entries, ps = _cache(state, slots, batch, (width - 1, ch), dtype, index)
+    px = _rows(x, "x", dtype, index, x.shape)
+    pw = _flat(weight, "weight", torch.float32, index, (ch, width))
+    pb = _flat(bias, "bias", torch.float32, index, (ch,))
+    with _On(index, stream) as st:
+        y = torch.empty((batch, ch), dtype=dtype, device=x.device) if out is None else out
+        py = _rows(y, "out", dtype, index, x.shape)
         if ch:
-            _call("tcu_short_conv_step", a, st)
+            _call("tcu_short_conv_step", _CONV.pack(
+                _TYPES[dtype], width, bool(silu), batch, 1, ch, 0, px[0], px[2], 0, py[0], py[2],
+                0, *_NO_ROWS, *_NO_ROWS, pw, pb, 0, 0, cache, 0, 0, 0, 0, 0, ps, entries), st)
     return y
-
-
-def _step_rows(t, name, like, shape):
-    r = _rows(t, name, like, shape)
-    return _Rows(r.ptr, r.row_stride, 0)
 
 
 # ------------------------------------------------------------ selective scan
@@ -343,49 +380,56 @@ def _grouped(t, name, x):
     return t
 
 
-def _scan_args(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets):
-    seqs, rows, ch, off = _layout(u, "u", offsets)
-    B, C = _grouped(B, "B", u), _grouped(C, "C", u)
+def _groups(B, ch):
     groups, states = B.shape[-2:]
     if not 1 <= states <= MAX_STATES:
         raise ValueError("B must have 1 to %d states" % MAX_STATES)
     if groups < 1 or ch % groups:
         raise ValueError("the %d channels must divide into the %d groups of B" % (ch, groups))
-    f32, dev, lead = torch.float32, u.device, tuple(u.shape[:-1])
-    bc = torch.Size(lead + (groups, states))
-    a = _ScanArgs(type=_TYPES[u.dtype], softplus=bool(softplus), sequences=seqs, groups=groups,
-                  rows=rows, channels=ch, states=states, offsets=off,
-                  u=_rows(u, "u", u, u.shape), dt=_rows(dt, "dt", u, u.shape),
-                  B=_rows(B, "B", u, bc), C=_rows(C, "C", u, bc),
-                  A=_flat(A, "A", f32, dev, (ch, states)),
-                  skip=_flat(skip, "skip", f32, dev, (ch,)),
-                  dt_bias=_flat(dt_bias, "dt_bias", f32, dev, (ch,)),
-                  state=_flat(state, "state", f32, dev, (seqs, ch, states)))
-    if gate is not None:
-        a.gate = _rows(gate, "gate", u, u.shape)
-    return a, (seqs, ch, states)
+    return groups, states
 
 
-def _marks_shape(u, offsets, states):
-    batch, rows = (u.shape[0], u.shape[1]) if offsets is None else (1, u.shape[0])
-    return (batch, -(-rows // MARK), u.shape[-1], states)
+class _ScanCall:
+    """The checked arguments that the scan and its gradient share."""
+
+    def __init__(self, u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets):
+        seqs, rows, ch, off = _layout(u, "u", offsets)
+        B, C = _grouped(B, "B", u), _grouped(C, "C", u)
+        groups, states = _groups(B, ch)
+        f32, dtype, index, shape = torch.float32, u.dtype, u.get_device(), u.shape
+        bc = shape[:-1] + (groups, states)
+        self.index, self.dtype, self.channels, self.tail = index, dtype, ch, (seqs, ch, states)
+        self.head = (_TYPES[dtype], bool(softplus), seqs, groups, rows, ch, states, off,
+                     *_rows(u, "u", dtype, index, shape), *_rows(dt, "dt", dtype, index, shape),
+                     *(_rows(gate, "gate", dtype, index, shape) if gate is not None else _NO_ROWS))
+        self.bc = (*_grouped_rows(B, "B", dtype, index, bc), *_grouped_rows(C, "C", dtype, index, bc))
+        self.params = (_flat(A, "A", f32, index, (ch, states)),
+                       _flat(skip, "skip", f32, index, (ch,)),
+                       _flat(dt_bias, "dt_bias", f32, index, (ch,)),
+                       _flat(state, "state", f32, index, self.tail))
+        batch = shape[0] if off == 0 and offsets is None else 1
+        self.marks = (batch, -(-rows // MARK), ch, states)
+
+
+_NO_GRADS = _NO_ROWS * 6 + (0, 0, 0)
 
 
 def _scan(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets, marks, out, stream):
-    a, tail = _scan_args(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets)
+    c = _ScanCall(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets)
     f32, dev = torch.float32, u.device
-    with _On(dev, stream) as st:
+    with _On(c.index, stream) as st:
         y = torch.empty(u.shape, dtype=u.dtype, device=dev) if out is None else out
-        last = torch.empty(tail, dtype=f32, device=dev)
-        a.y = _rows(y, "out", u, u.shape)
-        a.last = last.data_ptr()
-        kept = None
-        if marks:
-            kept = torch.empty(_marks_shape(u, offsets, tail[2]), dtype=f32, device=dev)
-            a.marks = kept.data_ptr()
-        if a.channels:
-            work = _workspace("tcu_state_scan_workspace", a, dev)
-            _call("tcu_state_scan", a, st)
+        last = torch.empty(c.tail, dtype=f32, device=dev)
+        py = _rows(y, "out", c.dtype, c.index, u.shape)
+        kept = torch.empty(c.marks, dtype=f32, device=dev) if marks else None
+
+        def packed(work, size):
+            return _SCAN.pack(*c.head, *py, *c.bc, *c.params, 0, last.data_ptr(), 0,
+                              kept.data_ptr() if marks else 0, *_NO_GRADS, work, size, 0, 0)
+
+        if c.channels:
+            work, n = _workspace("tcu_state_scan_workspace", packed(0, 0), dev)
+            _call("tcu_state_scan", packed(work.data_ptr() if n else 0, n), st)
             del work
     return y, last, kept
 
@@ -440,30 +484,38 @@ def state_scan_grad(dy, u, dt, A, B, C, *, marks, skip=None, gate=None, dt_bias=
     """Gradients of state_scan's (y, last) under dy and dlast (zeros if None),
     from the marks that state_scan kept of the same arguments: ScanGrads(u, dt,
     A, B, C, skip, gate, dt_bias, state), None where the argument is."""
-    a, tail = _scan_args(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets)
-    f32, dev = torch.float32, u.device
-    with _On(dev, stream) as st:
-        def like(t, dtype):
-            return None if t is None else torch.empty(t.shape, dtype=dtype, device=dev)
+    c = _ScanCall(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets)
+    f32, dev, dtype, index, shape = torch.float32, u.device, c.dtype, c.index, u.shape
+    pdy = _rows(dy, "dy", dtype, index, shape)
+    pm = _flat(marks, "marks", f32, index, c.marks)
+    pl = _flat(dlast, "dlast", f32, index, c.tail)
+    with _On(index, stream) as st:
+        def like(t, kind):
+            return None if t is None else torch.empty(t.shape, dtype=kind, device=dev)
 
-        g = ScanGrads(like(u, u.dtype), like(dt, u.dtype), like(A, f32), like(B, u.dtype),
-                      like(C, u.dtype), like(skip, f32), like(gate, u.dtype),
-                      like(dt_bias, f32), like(state, f32))
-        a.dy = _rows(dy, "dy", u, u.shape)
-        a.marks = _flat(marks, "marks", f32, dev, _marks_shape(u, offsets, tail[2]))
-        a.dlast = _flat(dlast, "dlast", f32, dev, tail)
-        a.du, a.ddt = _rows(g.u, "du", u, u.shape), _rows(g.dt, "ddt", u, u.shape)
-        for name, t in (("dB", g.B), ("dC", g.C)):
-            t = _grouped(t, name, u)
-            setattr(a, name, _rows(t, name, u, t.shape))
-        if gate is not None:
-            a.dgate = _rows(g.gate, "dgate", u, u.shape)
-        for name, t in (("dA", g.A), ("dskip", g.skip), ("ddt_bias", g.dt_bias),
-                        ("dstate", g.state)):
-            setattr(a, name, t.data_ptr() if t is not None else None)
-        if a.channels:
-            work = _workspace("tcu_state_scan_grad_workspace", a, dev)
-            _call("tcu_state_scan_grad", a, st)
+        def ptr(t):
+            return 0 if t is None else t.data_ptr()
+
+        def rows(t):
+            return _rows(t, "gradient", dtype, index, shape) if t is not None else _NO_ROWS
+
+        def grouped(t):
+            t = _grouped(t, "gradient", u)
+            return _grouped_rows(t, "gradient", dtype, index, t.shape)
+
+        g = ScanGrads(like(u, dtype), like(dt, dtype), like(A, f32), like(B, dtype),
+                      like(C, dtype), like(skip, f32), like(gate, dtype), like(dt_bias, f32),
+                      like(state, f32))
+        outs = (*pdy, *rows(g.u), *rows(g.dt), *rows(g.gate), *grouped(g.B), *grouped(g.C),
+                ptr(g.A), ptr(g.skip), ptr(g.dt_bias))
+
+        def packed(work, size):
+            return _SCAN.pack(*c.head, *_NO_ROWS, *c.bc, *c.params, pl, 0, ptr(g.state), pm, *outs,
+                              work, size, 0, 0)
+
+        if c.channels:
+            work, n = _workspace("tcu_state_scan_grad_workspace", packed(0, 0), dev)
+            _call("tcu_state_scan_grad", packed(ptr(work), n), st)
             del work
     return g
 
@@ -475,32 +527,29 @@ def state_scan_step(u, dt, A, B, C, state, *, skip=None, gate=None, dt_bias=None
     ``state`` (entries, channels, states) is advanced in place, at entry
     slots[b] (int32) for row b, or entry b.  A slot outside the cache gives a
     row of zeros; no two rows may name the same one."""
-    _no_grad(u, dt, A, B, C, skip, gate, dt_bias)
     _tensor(u, "u")
     if u.dim() != 2 or u.dtype not in _TYPES or not u.is_cuda:
         raise ValueError("u must be a float32, bfloat16 or float16 CUDA tensor (batch, channels)")
-    batch, ch = u.shape
+    _no_grad(u, dt, A, B, C, skip, gate, dt_bias)
+    batch, ch = shape = u.shape
     B, C = _grouped(B, "B", u), _grouped(C, "C", u)
-    groups, states = B.shape[-2:]
-    if not 1 <= states <= MAX_STATES:
-        raise ValueError("B must have 1 to %d states" % MAX_STATES)
-    if groups < 1 or ch % groups:
-        raise ValueError("the %d channels must divide into the %d groups of B" % (ch, groups))
-    f32, dev = torch.float32, u.device
-    bc = torch.Size((batch, groups, states))
-    ptr, entries = _cache(state, slots, batch, (ch, states), f32, dev)
-    with _On(dev, stream) as st:
-        y = torch.empty((batch, ch), dtype=u.dtype, device=dev) if out is None else out
-        a = _ScanArgs(type=_TYPES[u.dtype], softplus=bool(softplus), sequences=batch,
-                      groups=groups, rows=1, channels=ch, states=states,
-                      u=_step_rows(u, "u", u, u.shape), dt=_step_rows(dt, "dt", u, u.shape),
-                      y=_step_rows(y, "out", u, u.shape), B=_step_rows(B, "B", u, bc),
-                      C=_step_rows(C, "C", u, bc), A=_flat(A, "A", f32, dev, (ch, states)),
-                      skip=_flat(skip, "skip", f32, dev, (ch,)),
-                      dt_bias=_flat(dt_bias, "dt_bias", f32, dev, (ch,)), last=ptr,
-                      slots=_slots(slots, batch, dev), num_slots=entries)
-        if gate is not None:
-            a.gate = _step_rows(gate, "gate", u, u.shape)
+    groups, states = _groups(B, ch)
+    f32, dtype, index = torch.float32, u.dtype, u.get_device()
+    bc = (batch, groups, states)
+    cache, entries, ps = _cache(state, slots, batch, (ch, states), f32, index)
+    pu, pd = _rows(u, "u", dtype, index, shape), _rows(dt, "dt", dtype, index, shape)
+    pz = _rows(gate, "gate", dtype, index, shape) if gate is not None else _NO_ROWS
+    pB, pC = _grouped_rows(B, "B", dtype, index, bc), _grouped_rows(C, "C", dtype, index, bc)
+    pA = _flat(A, "A", f32, index, (ch, states))
+    pk = _flat(skip, "skip", f32, index, (ch,))
+    pi = _flat(dt_bias, "dt_bias", f32, index, (ch,))
+    with _On(index, stream) as st:
+        y = torch.empty((batch, ch), dtype=dtype, device=u.device) if out is None else out
+        py = _rows(y, "out", dtype, index, shape)
         if ch:
-            _call("tcu_state_scan_step", a, st)
+            _call("tcu_state_scan_step", _SCAN.pack(
+                _TYPES[dtype], bool(softplus), batch, groups, 1, ch, states, 0,
+                pu[0], pu[2], 0, pd[0], pd[2], 0, pz[0], pz[2], 0, py[0], py[2], 0,
+                pB[0], pB[2], 0, pC[0], pC[2], 0, pA, pk, pi, 0, 0, cache, 0, 0, *_NO_GRADS,
+                0, 0, ps, entries), st)
     return y
