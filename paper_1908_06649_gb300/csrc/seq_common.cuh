@@ -201,14 +201,17 @@ struct Raw {
 template <typename T>
 struct Rows {
   T *p;
-  int64_t batch, row;
-  __device__ __forceinline__ T *at(int64_t b, int64_t t) const { return p + b * batch + t * row; }
+  int64_t batch;
+  int32_t row;  // one 32-bit product for a row's address (row_fits)
+  __device__ __forceinline__ T *at(int64_t b, int32_t t) const {
+    return p + b * batch + (int64_t)t * row;
+  }
 };
 
 // The sequence that holds row t of a packed tensor: the last s with
 // offsets[s] <= t < offsets[s + 1], -1 if t is in none (values out of order
 // still give -1 <= s < count).
-__device__ __forceinline__ int sequence_of(const int32_t *offsets, int count, int64_t t) {
+__device__ __forceinline__ int sequence_of(const int32_t *offsets, int count, int t) {
   int lo = 0, hi = count;  // offsets[lo] <= t unless lo == 0
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
@@ -233,6 +236,11 @@ inline bool rows_aligned(const tcu_seq_rows &r, int type, int64_t batches, int64
 inline bool row_ok(const tcu_seq_rows &r, int size) {
   return r.ptr && (uintptr_t)r.ptr % size == 0;
 }
+// Rows, and a row's pitch, within 32 bits, with room to step past the end.
+constexpr int64_t kMostRows = INT32_MAX - 4096;
+inline bool row_fits(const tcu_seq_rows &r) {
+  return r.row_stride >= INT32_MIN && r.row_stride <= INT32_MAX;
+}
 inline bool f32_ok(const void *p) { return p && (uintptr_t)p % 4 == 0; }
 inline bool opt_ok(const void *p, int size) { return (uintptr_t)p % size == 0; }
 
@@ -242,7 +250,7 @@ inline int launched() {
 
 template <typename T>
 inline Rows<T> rows_of(const tcu_seq_rows &r) {
-  return {static_cast<T *>(r.ptr), r.batch_stride, r.row_stride};
+  return {static_cast<T *>(r.ptr), r.batch_stride, (int32_t)r.row_stride};
 }
 
 // Streaming multiprocessors of the current device.

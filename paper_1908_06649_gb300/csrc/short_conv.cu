@@ -29,8 +29,8 @@ struct ConvArgs {
   float *parts;  // gradient: [run]{[channels][W], [channels]}
   const int32_t *offsets;
   const int32_t *slots;
-  int64_t rows, channels, num_slots;
-  int sequences, batches, silu;
+  int64_t channels, num_slots;
+  int rows, sequences, batches, silu;
   int64_t runs;  // of kBlockRows * blocks rows in a batch entry
   int blocks;
 };
@@ -45,24 +45,23 @@ constexpr int kAhead = W * (8 / W);
 // One sequence as rows [lo, hi) of a batch entry; span_of holds t itself
 // whatever the offsets are.
 struct Span {
-  int64_t lo, hi;
+  int lo, hi;
   int seq;
 };
 
 template <typename T>
-__device__ __forceinline__ Span span_of(const ConvArgs<T> &a, int64_t b, int64_t t) {
+__device__ __forceinline__ Span span_of(const ConvArgs<T> &a, int64_t b, int t) {
   if (!a.offsets) return {0, a.rows, (int)b};
   const int s = sequence_of(a.offsets, a.sequences, t);
   if (s < 0) return {t, t + 1, -1};
-  return {max((int64_t)a.offsets[s], (int64_t)0),
-          max(min((int64_t)a.offsets[s + 1], a.rows), t + 1), s};
+  return {max(a.offsets[s], 0), max(min(a.offsets[s + 1], a.rows), t + 1), s};
 }
 // Sequence s itself, empty ones too.
 template <typename T>
 __device__ __forceinline__ Span span_at(const ConvArgs<T> &a, int64_t s) {
   if (!a.offsets) return {0, a.rows, (int)s};
-  const int64_t lo = min(max((int64_t)a.offsets[s], (int64_t)0), a.rows);
-  return {lo, min(max((int64_t)a.offsets[s + 1], lo), a.rows), (int)s};
+  const int lo = min(max(a.offsets[s], 0), a.rows);
+  return {lo, min(max(a.offsets[s + 1], lo), a.rows), (int)s};
 }
 
 // What a thread owns: V channels, of which `count` exist, as pairs for packed
@@ -106,7 +105,7 @@ struct Own {
     r.template store<kWide>(p, count, gap);
   }
   // Row i of a sequence, from the state where i < 0.
-  __device__ __forceinline__ Row value(const Span &s, int64_t i) const {
+  __device__ __forceinline__ Row value(const Span &s, int i) const {
     if (i >= 0) return row(a.x.at(b, s.lo + i) + c);
     if (a.state && s.seq >= 0)
       return row(a.state + ((int64_t)s.seq * (W - 1) + (W - 1) + i) * a.channels + c);
@@ -136,7 +135,7 @@ struct Own {
     }
   }
   // The window before row i of a sequence, i in slot 0.
-  __device__ __forceinline__ void window(const Span &s, int64_t i, float2 (&x)[W][P]) const {
+  __device__ __forceinline__ void window(const Span &s, int i, float2 (&x)[W][P]) const {
 #pragma unroll
     for (int k = 1; k < W; ++k) {
       const Row r = value(s, i - W + k);
@@ -165,16 +164,16 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(ConvArgs<T> a) {
     constexpr int kPast = W > 1 ? W - 1 : 1;  // W == 1 has no past and returned
     const Span s = span_at(a, rest / kPast);
     own.b = a.offsets ? 0 : s.seq;
-    const Row r = own.value(s, s.hi - s.lo - (W - 1) + rest % kPast);
+    const Row r = own.value(s, s.hi - s.lo - (W - 1) + (int)(rest % kPast));
     r.template store<kWide>(a.last + rest * a.channels + c, own.count, own.gap);
     return;
   }
-  const int64_t b = own.b = item / a.runs, t0 = item % a.runs * (kBlockRows * a.blocks);
-  const int64_t t1 = min(t0 + kBlockRows * a.blocks, a.rows);
+  const int64_t b = own.b = item / a.runs, run = item % a.runs;
+  const int t0 = (int)run * (kBlockRows * a.blocks), t1 = min(t0 + kBlockRows * a.blocks, a.rows);
   own.params();
-  for (int64_t lo = t0; lo < t1;) {
+  for (int lo = t0; lo < t1;) {
     const Span s = span_of(a, b, lo);
-    const int64_t hi = min(s.hi, t1);
+    const int hi = min(s.hi, t1);
     float2 x[W][P];
     own.window(s, lo - s.lo, x);
     const T *from = a.x.at(b, lo) + c;
@@ -190,7 +189,7 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(ConvArgs<T> a) {
       own.put(to, p);
       to += a.y.row;
     };
-    int left = (int)(hi - lo);
+    int left = hi - lo;
     constexpr int G = kAhead<W>;
     Row next[G];
     if (left >= G) {
@@ -234,7 +233,7 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
   const int64_t c = own.c;
   // dlast of the row that lies i before the end of what sequence s would
   // continue to, or zeros
-  auto after = [&](const Span &s, int64_t i, float2 (&dx)[P]) {
+  auto after = [&](const Span &s, int i, float2 (&dx)[P]) {
     if (!a.dlast || s.seq < 0) return;
     const Row r = own.row(a.dlast + ((int64_t)s.seq * (W - 1) + i) * a.channels + c);
 #pragma unroll
@@ -248,7 +247,7 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
     const Span s = span_at(a, rest / kPast);
     own.b = a.offsets ? 0 : s.seq;
     own.params();
-    const int64_t i = rest % kPast - (W - 1), len = s.hi - s.lo;
+    const int i = (int)(rest % kPast) - (W - 1), len = s.hi - s.lo;
     float2 x[W][P], dp[P], dx[P] = {};
     if (i >= len - (W - 1)) after(s, i - (len - (W - 1)), dx);
     own.window(s, 0, x);
@@ -259,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
 #pragma unroll
       for (int n = 0; n < P; ++n) x[j][n] = r.pair(n);
       own.dpre(x, j, own.row(a.dy.at(own.b, s.lo + j) + c), dp);
-      const int64_t k = i + (W - 1) - j;  // the tap of row i in row j
+      const int k = i + (W - 1) - j;  // the tap of row i in row j
 #pragma unroll
       for (int m = 0; m < W; ++m)
         if (m == k)
@@ -269,13 +268,13 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
     own.put(a.dstate + rest * a.channels + c, dx);
     return;
   }
-  const int64_t b = own.b = item / a.runs, t0 = item % a.runs * (kBlockRows * a.blocks);
-  const int64_t t1 = min(t0 + kBlockRows * a.blocks, a.rows);
+  const int64_t b = own.b = item / a.runs, run = item % a.runs;
+  const int t0 = (int)run * (kBlockRows * a.blocks), t1 = min(t0 + kBlockRows * a.blocks, a.rows);
   own.params();
   float2 dw[W][P] = {}, db[P] = {};
-  for (int64_t lo = t0; lo < t1;) {
+  for (int lo = t0; lo < t1;) {
     const Span s = span_of(a, b, lo);
-    const int64_t hi = min(s.hi, t1);
+    const int hi = min(s.hi, t1);
     float2 x[W][P], dp[W][P] = {};
     own.window(s, lo - s.lo, x);
     const T *px = a.x.at(b, lo) + c, *py = a.dy.at(b, lo) + c;
@@ -300,7 +299,7 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
       if (store) own.put(to, dx);
       to += a.dx.row;
     };
-    const int n = (int)(hi - lo);
+    const int n = hi - lo;
     int r0 = 0;  // rows done
     constexpr int G = kAhead<W>;
     Row nx[G], ny[G];
@@ -324,7 +323,7 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
       }
     }
     // the rows left, and the W-1 beyond them that the last rows' dx still need
-    const int end = (int)(s.hi - lo);  // of the sequence
+    const int end = s.hi - lo;  // of the sequence
 #pragma unroll 1
     for (; r0 < n + W - 1; r0 += W) {
 #pragma unroll
@@ -451,7 +450,8 @@ int check_sizes(const tcu_short_conv_args *a) {
   if (!a || a->type < TCU_SEQ_F32 || a->type > TCU_SEQ_F16 || a->sequences < 0 || a->rows < 0 ||
       a->channels < 1 || a->width < 1)
     return TCU_DFT_ERR_INVALID;
-  if (a->width > TCU_SEQ_MAX_WIDTH || a->rows > INT32_MAX || a->channels > INT32_MAX)
+  if (a->width > TCU_SEQ_MAX_WIDTH || a->rows > kMostRows || a->channels > INT32_MAX ||
+      !row_fits(a->x) || !row_fits(a->y) || !row_fits(a->dy) || !row_fits(a->dx))
     return TCU_DFT_ERR_UNSUPPORTED;
   return TCU_DFT_OK;
 }
@@ -475,7 +475,7 @@ int dispatch(Call call, const tcu_short_conv_args &s, cudaStream_t st) {
   a.dstate = static_cast<T *>(s.dstate);
   a.offsets = s.offsets;
   a.slots = s.slots;
-  a.rows = s.rows;
+  a.rows = (int)s.rows;
   a.channels = s.channels;
   a.num_slots = s.num_slots;
   a.sequences = s.sequences;

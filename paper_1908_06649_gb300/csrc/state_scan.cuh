@@ -60,8 +60,8 @@ struct ScanArgs {
   float *A_parts;   // [batch][chunk][channels][states]
   float *skip_parts, *bias_parts;  // [batch][chunk][channels]
   const int32_t *offsets, *slots;
-  int64_t rows, channels, num_slots;
-  int64_t chunk_rows;
+  int64_t channels, num_slots;
+  int rows, chunk_rows;
   int states, groups, per_group, group_blocks;
   int sequences, batches, chunks, softplus;
   // whether states, and B and C, are read in words of four values
@@ -72,22 +72,22 @@ struct ScanArgs {
 // The channels a block of the given kernel covers, and its rows.
 template <int DB, typename T>
 struct Place {
-  int64_t b, k, r0, r1;
-  int g, cb;
-  int64_t c0;
-  int nc;
-  __device__ __forceinline__ explicit Place(const ScanArgs<T> &a) {
+  int64_t b, k, c0;
+  int r0, r1;  // rows
+  int g, cb, nc;
+  // of `chunks` chunks from `first` on
+  __device__ __forceinline__ explicit Place(const ScanArgs<T> &a, int chunks, int first) {
     const int blocks = a.groups * a.group_blocks;
     const int64_t id = blockIdx.x;
     const int blk = (int)(id % blocks);
     const int64_t bk = id / blocks;
-    k = bk % a.chunks;
-    b = bk / a.chunks;
+    k = first + bk % chunks;
+    b = bk / chunks;
     g = blk / a.group_blocks;
     cb = blk % a.group_blocks;
     c0 = (int64_t)g * a.per_group + cb * DB;
     nc = min(DB, a.per_group - cb * DB);
-    r0 = k * a.chunk_rows;
+    r0 = (int)k * a.chunk_rows;
     r1 = min(r0 + a.chunk_rows, a.rows);
   }
 };
@@ -142,20 +142,20 @@ __device__ __forceinline__ bool owner_of(int q) {
 
 // Bits of the tile's rows that open (or, closes, end) a sequence.
 template <typename T>
-__device__ __forceinline__ uint32_t opens_mask(const ScanArgs<T> &a, int64_t row0, int lane) {
-  const int64_t r = row0 + lane;
+__device__ __forceinline__ uint32_t opens_mask(const ScanArgs<T> &a, int row0, int lane) {
+  const int r = row0 + lane;
   const bool o = r < a.rows && (r == 0 || a.row_seq[r] != a.row_seq[r - 1]);
   return __ballot_sync(~0u, o);
 }
 template <typename T>
-__device__ __forceinline__ uint32_t closes_mask(const ScanArgs<T> &a, int64_t row0, int lane) {
-  const int64_t r = row0 + lane;
+__device__ __forceinline__ uint32_t closes_mask(const ScanArgs<T> &a, int row0, int lane) {
+  const int r = row0 + lane;
   const bool c = r < a.rows && (r + 1 == a.rows || a.row_seq[r] != a.row_seq[r + 1]);
   return __ballot_sync(~0u, c);
 }
 
 __global__ void row_sequence_kernel(int32_t *row_seq, const int32_t *offsets, int count,
-                                    int64_t rows);
+                                    int rows);
 
 // d of one value.
 template <typename T>
@@ -215,6 +215,16 @@ __device__ __forceinline__ void copy_async(uint32_t *to, const void *from, int b
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(s), "l"(from) : "memory");
   else
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(from) : "memory");
+}
+
+// h <- 2^e h + b.  The decays come out of the special function unit one by one;
+// packing them for one product costs more moves than two products do.
+__device__ __forceinline__ float2 decay_add(float2 e, float2 h, float2 b) {
+  return make_float2(fmaf(exp2_fast(e.x), h.x, b.x), fmaf(exp2_fast(e.y), h.y, b.y));
+}
+// 2^e h
+__device__ __forceinline__ float2 decay(float2 e, float2 h) {
+  return __fmul2_rn(make_float2(exp2_fast(e.x), exp2_fast(e.y)), h);
 }
 
 // Four states of CH channels (pairs of channels packed) from / to an array
@@ -282,14 +292,15 @@ __global__ void __launch_bounds__(64 * kPairs, kResident)
   float *sdx = sskip + L::WC;                          // [2][d, x][RP][kRow]
   float *sy = sdx + 4 * RP * L::kRow;                  // [2][RP][kYRow]
   uint32_t *ring = reinterpret_cast<uint32_t *>(sy + 2 * RP * L::kYRow);
-  const Place<L::DB, T> w(a);
+  // the last chunk's own final state (first, going back) is of no use
+  const Place<L::DB, T> w(a, a.chunks - kLocal, kBack);
   const int64_t c0 = w.c0 + pair * L::WC;
   const int nc = w.nc - pair * L::WC;
   if (nc <= 0) return;  // both warps of the pair
-  const int pieces = (int)((w.r1 - w.r0 + RP - 1) / RP);
+  const int pieces = (w.r1 - w.r0 + RP - 1) / RP;
   // row t of piece i
   auto row_of = [&](int i, int t) {
-    return kBack ? w.r1 - 1 - ((int64_t)i * RP + t) : w.r0 + (int64_t)i * RP + t;
+    return kBack ? w.r1 - 1 - (i * RP + t) : w.r0 + i * RP + t;
   };
 
   if (warp >= kPairs) {
@@ -303,13 +314,13 @@ __global__ void __launch_bounds__(64 * kPairs, kResident)
     __syncwarp();
     const float *bias = sbias + vc, *skip = sskip + vc;
     const Rows<const T> &ru = kBack ? a.dy : a.u;
-    const int64_t first = row_of(0, vr);
+    const int first = row_of(0, vr);
     const T *pu = ru.at(w.b, first) + c0 + vc, *pd = a.dt.at(w.b, first) + c0 + vc;
     const T *pz = a.gate.p && kMode != kState ? a.gate.at(w.b, first) + c0 + vc : nullptr;
     T *py = kLocal ? nullptr : a.y.at(w.b, first) + c0 + vc;
     constexpr int64_t way = kBack ? -RP : RP;
     const int64_t su = way * ru.row, sdt = way * a.dt.row, sz = way * a.gate.row, so = way * a.y.row;
-    const int last = (int)(w.r1 - w.r0) - vr;  // this lane's row is in piece i if i RP < last
+    const int last = w.r1 - w.r0 - vr;  // this lane's row is in piece i if i RP < last
     auto slot = [&](int i, int which) { return ring + ((i % kRing * 3 + which) * L::kActive + lane) * L::kRaw; };
     // piece i of u, dt, gate on its way to the ring
     Row hold[3];
@@ -350,22 +361,34 @@ __global__ void __launch_bounds__(64 * kPairs, kResident)
       for (int j = 0; j < L::kRaw; ++j) r.w[j] = slot(i, which)[j];
       return r;
     };
-    // B and C of a piece: quads of states
-    constexpr int kItems = RP * LS, kBatch = kItems < 64 ? 1 : 2;
+    // B and C of a piece: quads of states, each of a lane's 32 / LS rows
+    // further down than the one before
+    constexpr int kItems = RP * LS, kBatch = kItems < 64 ? 1 : 2, kDown = 32 / LS;
     Raw<T, 4> qb[kBatch], qc[kBatch];
+    const int qr = lane / LS, qn = lane % LS * 4, rows = w.r1 - w.r0;
+    const int quad = lane < kItems ? min(4, a.states - qn) : 0;
+    const int64_t of_group = (int64_t)w.g * a.states + qn;
+    const Rows<const T> &rb = kBack ? a.C : a.B;
+    const T *pb = rb.at(w.b, row_of(0, qr)) + of_group;
+    const T *pc = kLocal ? nullptr : a.C.at(w.b, row_of(0, qr)) + of_group;
+    const int64_t sb = way * rb.row, sc = way * a.C.row;
+    // in order of i and base, so that the pointers follow
     auto load_bc = [&](int i, int base) {
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const int item = base + j * 32 + lane, n = item % LS * 4;
-        const int64_t r = row_of(i, item / LS);
-        const int count = item < kItems && r >= w.r0 && r < w.r1 ? min(4, a.states - n) : 0;
-        const T *from = (kBack ? a.C : a.B).at(w.b, r) + (int64_t)w.g * a.states + n;
+        const int down = (base / 32 + j) * kDown;
+        const int count = i * RP + qr + down < rows ? quad : 0;
+        const T *from = pb + (kBack ? -down : down) * (int64_t)rb.row;
         if (a.wide_bc) qb[j].template load<true>(from, count);
         else qb[j].template load<false>(from, count);
         if (kLocal) continue;
-        from = a.C.at(w.b, r) + (int64_t)w.g * a.states + n;
+        from = pc + (kBack ? -down : down) * (int64_t)a.C.row;
         if (a.wide_bc) qc[j].template load<true>(from, count);
         else qc[j].template load<false>(from, count);
+      }
+      if (base + kBatch * 32 >= kItems) {
+        pb += sb;
+        if (!kLocal) pc += sc;
       }
     };
     auto store_bc = [&](int i, int base) {
@@ -497,11 +520,11 @@ __global__ void __launch_bounds__(64 * kPairs, kResident)
       meet(pair);
       break;
     }
-    const int64_t row0 = row_of(i, 0);
-    const int rows = (int)min((int64_t)RP, w.r1 - w.r0 - (int64_t)i * RP);
+    const int row0 = row_of(i, 0);
+    const int rows = min(RP, w.r1 - w.r0 - i * RP);
     uint32_t opens = 0;  // rows of the piece where a sequence opens (going back: ends)
     if (kPacked) {
-      const int64_t r = row_of(i, lane);
+      const int r = row_of(i, lane);
       bool o = lane < rows;
       if (kBack) o = o && (r + 1 == a.rows || a.row_seq[r] != a.row_seq[r + 1]);
       else o = o && (r == 0 || a.row_seq[r] != a.row_seq[r - 1]);
@@ -513,11 +536,11 @@ __global__ void __launch_bounds__(64 * kPairs, kResident)
     float *to = sy + i % 2 * RP * L::kYRow + sl * L::kYLane + ch0;
     auto mark = [&](int t) {
       if (kLocal || !a.marks || (uint32_t)(row0 + t) % kMark != 0) return;
-      const int64_t marks = (a.rows + kMark - 1) / kMark, m = (row0 + t) / kMark;
+      const int64_t marks = (a.rows + kMark - 1) / kMark, m = (uint32_t)(row0 + t) / kMark;
       store_states(h, a, a.marks + ((w.b * marks + m) * a.channels + at) * a.states, n0, count);
     };
     auto open = [&](int t) {
-      const int64_t r = row_of(i, t);
+      const int r = row_of(i, t);
       const int s = a.row_seq[r], before = !kBack && r > 0 ? a.row_seq[r - 1] : -1;
       if (!kLocal && a.last && before >= 0)
         store_states(h, a, a.last + (before * a.channels + at) * a.states, n0, count);
@@ -548,10 +571,9 @@ __global__ void __launch_bounds__(64 * kPairs, kResident)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float2 e = __fmul2_rn(d[p], A2[p][j]);
-          const float2 decay = make_float2(exp2_fast(e.x), exp2_fast(e.y));
           const float2 b = make_float2(B[j], B[j]);
-          h[p][j] = kBack ? __fmul2_rn(decay, __ffma2_rn(x[p], b, h[p][j]))
-                          : __ffma2_rn(decay, h[p][j], __fmul2_rn(x[p], b));
+          h[p][j] = kBack ? decay(e, __ffma2_rn(x[p], b, h[p][j]))
+                          : decay_add(e, h[p][j], __fmul2_rn(x[p], b));
           if (kLocal) continue;
           const float2 c = make_float2(C[j], C[j]);
           y[p] = j == 0 ? __fmul2_rn(c, h[p][j]) : __ffma2_rn(c, h[p][j], y[p]);
@@ -576,7 +598,7 @@ __global__ void __launch_bounds__(64 * kPairs, kResident)
     } else {
       // a few rows at a time, their loads ahead of all stores
       constexpr int R = 4;
-#pragma unroll 1
+#pragma unroll
       for (int t = 0; t < RP; t += R) {
         mark(t);
         float2 y[R][PAIRS];
@@ -616,8 +638,13 @@ __global__ void carry_kernel(ScanArgs<T> a) {
   float h = 0.f;
   for (int j = 0; j < a.chunks; ++j) {
     const int k = kBack ? a.chunks - 1 - j : j;
-    const int64_t r0 = k * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
+    const int r0 = k * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
     float *p = a.carry + (b * a.chunks + k) * per + at;
+    // the last chunk of the walk has left nothing, and nothing needs it
+    if (j == a.chunks - 1) {
+      *p = h;
+      break;
+    }
     const float own = *p, decay = exp2_fast(A2 * a.sum_d[(b * a.chunks + k) * a.channels + c]);
     // does a sequence open (close, going back) within the chunk?
     bool cut;
@@ -630,49 +657,64 @@ __global__ void carry_kernel(ScanArgs<T> a) {
 
 // One token: LS lanes per channel, 4 states each, the cache in place.  The
 // cache read and written is nearly all it does: 16 bytes a lane either way.
-template <typename T, int LS, bool kWide>
+// NB batch entries a thread, on their way at once, for one load of A.
+template <typename T, int LS, int NB, bool kWide>
 __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(ScanArgs<T> a) {
   const int64_t id = ((int64_t)blockIdx.x * kScanThreads + threadIdx.x) / LS;
   const int sl = threadIdx.x % LS, n0 = sl * 4, n = min(4, a.states - n0);
-  const bool in = id < a.channels * a.sequences;
-  const int64_t b = in ? id / a.channels : 0, c = in ? id % a.channels : 0;
-  const int64_t slot = a.slots ? a.slots[b] : b;
-  const bool live = in && slot >= 0 && slot < a.num_slots;
-  float o = 0.f, u = 0.f, z = 0.f;
-  if (live) {
-    float *cache = a.last + (slot * a.channels + c) * a.states + n0;
-    const float *rate = a.A + c * a.states + n0;
-    const int64_t g = c / a.per_group * a.states + n0;
-    Raw<float, 4> h, A;
-    Raw<T, 4> B, C;
-    h.template load<kWide>(cache, n);
-    A.template load<kWide>(rate, n);
-    B.template load<kWide>(a.B.at(b, 0) + g, n);
-    C.template load<kWide>(a.C.at(b, 0) + g, n);
-    u = to_f(a.u.at(b, 0)[c]);
-    if (a.gate.p) z = to_f(a.gate.at(b, 0)[c]);
-    const float d = step_of(a, to_f(a.dt.at(b, 0)[c]), a.dt_bias ? a.dt_bias[c] : 0.f);
-    const float2 x = make_float2(d * u, d * u), e = make_float2(d * kLog2e, d * kLog2e);
+  const int64_t batches = (a.sequences + NB - 1) / NB;
+  const bool in = id < a.channels * batches;
+  const int64_t b0 = in ? id / a.channels : 0, c = in ? id % a.channels : 0;
+  const int64_t g = c / a.per_group * a.states + n0;
+  Raw<float, 4> h[NB], A;
+  Raw<T, 4> B[NB], C[NB];
+  float *cache[NB];
+  float u[NB], dt[NB], z[NB], o[NB];
+  A.template load<kWide>(a.A + c * a.states + n0, in ? n : 0);
+  const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int64_t b = b0 + i * batches;
+    const bool row = in && b < a.sequences;
+    const int64_t slot = !row ? -1 : a.slots ? a.slots[b] : b;
+    const bool live = slot >= 0 && slot < a.num_slots;
+    cache[i] = live ? a.last + (slot * a.channels + c) * a.states + n0 : nullptr;
+    h[i].template load<kWide>(cache[i], live ? n : 0);
+    B[i].template load<kWide>(a.B.at(b, 0) + g, live ? n : 0);
+    C[i].template load<kWide>(a.C.at(b, 0) + g, live ? n : 0);
+    u[i] = live ? to_f(a.u.at(b, 0)[c]) : 0.f;
+    dt[i] = live ? to_f(a.dt.at(b, 0)[c]) : 0.f;
+    z[i] = live && a.gate.p ? to_f(a.gate.at(b, 0)[c]) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const float d = step_of(a, dt[i], bias);
+    const float2 x = make_float2(d * u[i], d * u[i]), e = make_float2(d * kLog2e, d * kLog2e);
     float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float2 r = __fmul2_rn(e, A.pair(i));
-      const float2 v = __ffma2_rn(make_float2(exp2_fast(r.x), exp2_fast(r.y)), h.pair(i),
-                                  __fmul2_rn(x, B.pair(i)));
-      h.set(i, v);
-      sum = __ffma2_rn(C.pair(i), v, sum);
+    for (int j = 0; j < 2; ++j) {
+      const float2 r = __fmul2_rn(e, A.pair(j));
+      const float2 v = __ffma2_rn(make_float2(exp2_fast(r.x), exp2_fast(r.y)), h[i].pair(j),
+                                  __fmul2_rn(x, B[i].pair(j)));
+      h[i].set(j, v);
+      sum = __ffma2_rn(C[i].pair(j), v, sum);
     }
-    o = sum.x + sum.y;
-    h.template store<kWide>(cache, n);
+    o[i] = sum.x + sum.y;
+    if (cache[i]) h[i].template store<kWide>(cache[i], n);
   }
 #pragma unroll
-  for (int s = LS / 2; s > 0; s /= 2) o += __shfl_xor_sync(~0u, o, s);
+  for (int s = LS / 2; s > 0; s /= 2)
+#pragma unroll
+    for (int i = 0; i < NB; ++i) o[i] += __shfl_xor_sync(~0u, o[i], s);
   if (!in || sl != 0) return;
-  if (live) {
-    if (a.skip) o = fmaf(a.skip[c], u, o);
-    if (a.gate.p) o *= silu(z);
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int64_t b = b0 + i * batches;
+    if (b >= a.sequences) break;
+    float y = fmaf(skip, u[i], o[i]);
+    if (a.gate.p) y *= silu(z[i]);
+    a.y.at(b, 0)[c] = from_f<T>(cache[i] ? y : 0.f);
   }
-  a.y.at(b, 0)[c] = from_f<T>(live ? o : 0.f);
 }
 
 // ---------------------------------------------------------------- gradient
@@ -687,7 +729,7 @@ __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(ScanArgs<T> a) 
 template <int LS_, typename T>
 struct GradLay {
   static constexpr int LS = LS_, CH = scan_ch(LS), NP = 4 * LS, E = 4 * CH, CL = 32 / LS;
-  static constexpr int kBlock = 64 * kPairs;
+  static constexpr int kPairs = 4, kBlock = 64 * kPairs;
   static constexpr int WC = CL * CH, DB = kPairs * WC;
   static constexpr int V = LS <= 8 ? 8 : LS == 16 ? 4 : 2;
   static constexpr int COLS = WC / V, RP = 32 / COLS, PASSES = kMark / RP;
@@ -726,25 +768,25 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   using L = GradLay<LS, T>;
   constexpr int CH = L::CH, PAIRS = CH / 2, V = L::V, E = L::E;
   extern __shared__ __align__(16) float smem[];
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, pair = warp % kPairs;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, pair = warp % L::kPairs;
   float *sBC = smem + 4;                                       // [2][B, C][row][states]
   float *own = sBC + 4 * L::kBC + pair * L::kPairFloats;
   float *sdxq = own;                                           // [2][d, x, q][row][kRow]
   float *ssum = own + 6 * L::kPlane;                           // [2][row][dB, dC][states]
   float *sbias = ssum + 4 * L::kBC, *sskip = sbias + L::WC;
-  const Place<L::DB, T> w(a);
+  const Place<L::DB, T> w(a, a.chunks, 0);
   const int64_t c0 = w.c0 + pair * L::WC;
   const int nc = w.nc - pair * L::WC;
-  const int tiles = (int)((w.r1 - w.r0 + kMark - 1) / kMark);
+  const int tiles = (w.r1 - w.r0 + kMark - 1) / kMark;
   const int64_t part = w.b * a.chunks + w.k;
   // the i-th tile of the walk up, and its rows
-  auto row_of = [&](int i) { return w.r0 + (int64_t)(tiles - 1 - i) * kMark; };
+  auto row_of = [&](int i) { return w.r0 + (tiles - 1 - i) * kMark; };
   if (warp == 0) tmem_alloc(smem_u32(smem), L::kColumns);
 
-  if (warp >= kPairs) {
+  if (warp >= L::kPairs) {
     // ---- rows in and out
     const int vr = lane / L::COLS, vc = lane % L::COLS * V, vcount = min(V, nc - vc);
-    const int me = threadIdx.x - 32 * kPairs;  // of the second warps
+    const int me = threadIdx.x - 32 * L::kPairs;  // of the second warps
     for (int c = lane; c < L::WC; c += 32) {
       sbias[c] = a.dt_bias && c < nc ? a.dt_bias[c0 + c] : 0.f;
       sskip[c] = a.skip && c < nc ? a.skip[c0 + c] : 0.f;
@@ -759,19 +801,19 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       Raw<T, V, !kWide> u, dt, z, dy;
     };
     // this lane's first row of the tile that the first warps are at
-    const int64_t row = row_of(0) + vr;
+    const int row = row_of(0) + vr;
     const T *pu = a.u.at(w.b, row) + c0 + vc, *pd = a.dt.at(w.b, row) + c0 + vc,
             *pz = gated ? a.gate.at(w.b, row) + c0 + vc : nullptr,
             *py = a.dy.at(w.b, row) + c0 + vc;
     // pass `pass` of the tile `to` tiles further up
     auto load = [&](In &in, int i, int to, int pass) {
       const int up = to * kMark - pass * L::RP;
-      const int64_t r = row_of(i + to) + pass * L::RP + vr;
+      const int r = row_of(i + to) + pass * L::RP + vr;
       const int count = i + to >= 0 && i + to < tiles && r < w.r1 ? vcount : 0;
-      in.u.template load<kWide>(pu - up * a.u.row, count);
-      in.dt.template load<kWide>(pd - up * a.dt.row, count);
-      if (gated) in.z.template load<kWide>(pz - up * a.gate.row, count);
-      in.dy.template load<kWide>(py - up * a.dy.row, count);
+      in.u.template load<kWide>(pu - (int64_t)up * a.u.row, count);
+      in.dt.template load<kWide>(pd - (int64_t)up * a.dt.row, count);
+      if (gated) in.z.template load<kWide>(pz - (int64_t)up * a.gate.row, count);
+      in.dy.template load<kWide>(py - (int64_t)up * a.dy.row, count);
     };
     auto stage = [&](const In &in, int i, int pass) {
       float *o = sdxq + i % 2 * 3 * L::kPlane + (pass * L::RP + vr) * L::kRow + vc;
@@ -788,7 +830,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
     };
     auto finish = [&](const In &in, int i, int pass) {
       const float *from = sdxq + i % 2 * 3 * L::kPlane + (pass * L::RP + vr) * L::kRow + vc;
-      const int64_t r = row_of(i) + pass * L::RP + vr;
+      const int r = row_of(i) + pass * L::RP + vr;
       const int count = r < w.r1 ? vcount : 0;
       Raw<T, V, !kWide> du, ddt, dz;
 #pragma unroll
@@ -826,11 +868,11 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
     };
     auto stage_bc = [&](int i) {
       constexpr int items = kMark * LS;  // quads of B, then of C
-      const int64_t row0 = row_of(i);
-      for (int item = me; item < 2 * items; item += 32 * kPairs) {
+      const int row0 = row_of(i);
+      for (int item = me; item < 2 * items; item += 32 * L::kPairs) {
         const int which = item / items, t = item % items / LS, n = item % LS * 4;
         const Rows<const T> &src = which ? a.C : a.B;
-        const int64_t r = row0 + t;
+        const int r = row0 + t;
         const int count = r < w.r1 ? min(4, a.states - n) : 0;
         const T *from = src.at(w.b, r) + (int64_t)w.g * a.states + n;
         Raw<T, 4> q;
@@ -842,18 +884,26 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       }
     };
     // the block's shares of dB, dC: its four first warps' sums, in order
+    // A lane's values keep their column where a row has at most 128 of them.
+    constexpr int kCols = 2 * L::NP, kLanes = 32 * L::kPairs;
+    const int live = min(L::kPairs, (w.nc + L::WC - 1) / L::WC);
+    const int64_t pitch = (int64_t)a.groups * 2 * a.states;
+    float *shares = a.bc_parts + (((int64_t)w.cb * a.batches + w.b) * a.rows) * pitch +
+                    (int64_t)w.g * 2 * a.states;
     auto share_bc = [&](int i) {
-      const int64_t row0 = row_of(i);
-      const int rows = (int)min((int64_t)kMark, w.r1 - row0);
+      const int row0 = row_of(i), rows = min(kMark, w.r1 - row0);
       const float *from = sBC + 4 * L::kBC + 6 * L::kPlane + i % 2 * 2 * L::kBC;
-      const int live = min(kPairs, (w.nc + L::WC - 1) / L::WC);
-      for (int j = me; j < rows * 2 * L::NP; j += 32 * kPairs) {
-        const int n = j % L::NP, which = j / L::NP % 2, t = j / (2 * L::NP);
+      for (int col = me % kCols; col < kCols; col += kLanes) {
+        const int n = col % L::NP, which = col / L::NP;
         if (n >= a.states) continue;
-        float s = 0.f;
-        for (int k = 0; k < live; ++k) s += from[k * L::kPairFloats + j];
-        a.bc_parts[((((int64_t)w.cb * a.batches + w.b) * a.rows + row0 + t) * a.groups + w.g) * 2 *
-                       a.states + which * a.states + n] = s;
+        float *to = shares + row0 * pitch + which * a.states + n;
+        for (int t = me / kCols; t < rows; t += kCols < kLanes ? kLanes / kCols : 1) {
+          float s = 0.f;
+#pragma unroll
+          for (int k = 0; k < L::kPairs; ++k)
+            if (k < live) s += from[k * L::kPairFloats + t * kCols + col];
+          to[t * pitch] = s;
+        }
       }
     };
     // the passes of an iteration: those of the tile behind, then those of the
@@ -879,10 +929,10 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       }
       if (i > 0) share_bc(i - 1);
       if (i + 1 < tiles) stage_bc(i + 1);
-      pu -= kMark * a.u.row;
-      pd -= kMark * a.dt.row;
-      if (gated) pz -= kMark * a.gate.row;
-      py -= kMark * a.dy.row;
+      pu -= (int64_t)kMark * a.u.row;
+      pd -= (int64_t)kMark * a.dt.row;
+      if (gated) pz -= (int64_t)kMark * a.gate.row;
+      py -= (int64_t)kMark * a.dy.row;
       __syncthreads();
     }
     // a channel's shares lie in the lanes of its column
@@ -909,7 +959,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   const int sl = lane % LS, n0 = sl * 4, ch0 = lane / LS * CH, count = nc - ch0;
   const int64_t at = c0 + ch0;
   // this thread's 16-byte slots: its mark, then its sum of dA
-  float4 *slots = reinterpret_cast<float4 *>(sBC + 4 * L::kBC + kPairs * L::kPairFloats) +
+  float4 *slots = reinterpret_cast<float4 *>(sBC + 4 * L::kBC + L::kPairs * L::kPairFloats) +
                   warp * 32 * (L::kThreadFloats / 4) + lane;
   float4 *asum = slots + 32 * (E / 4);
   float2 A2[PAIRS][4], e[PAIRS][4], dA[PAIRS][4];
@@ -941,7 +991,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   };
   const int64_t marks = (a.rows + kMark - 1) / kMark;
   auto mark_of = [&](int i) {
-    return a.marks + ((w.b * marks + row_of(i) / kMark) * a.channels + at) * a.states;
+    return a.marks + ((w.b * marks + (uint32_t)row_of(i) / kMark) * a.channels + at) * a.states;
   };
   // the mark of the i-th tile on its way, one 16-byte copy a channel
   auto fetch_mark = [&](int i) {
@@ -966,8 +1016,8 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       __syncthreads();
       break;
     }
-    const int64_t row0 = row_of(i);
-    const int rows = (int)min((int64_t)kMark, w.r1 - row0);
+    const int row0 = row_of(i);
+    const int rows = min(kMark, w.r1 - row0);
     const uint32_t opens = kPacked ? opens_mask(a, row0, lane) : 0;
     const uint32_t closes = kPacked ? closes_mask(a, row0, lane) : 0;
     float *sd = sdxq + i % 2 * 3 * L::kPlane, *sx = sd + L::kPlane, *sq = sx + L::kPlane;
@@ -1000,7 +1050,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
                   n0, count);
     };
     // down the rows: column block t holds the state that enters row t
-#pragma unroll 4
+#pragma unroll 8
     for (int t = 0; t < rows; ++t) {
       tmem_put<E>(column + t * E, h);
       if (kPacked && (opens >> t & 1)) open_state(h, t);
@@ -1014,8 +1064,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float2 z = __fmul2_rn(d[p], A2[p][j]);
-          h[p][j] = __ffma2_rn(make_float2(exp2_fast(z.x), exp2_fast(z.y)), h[p][j],
-                               __fmul2_rn(x[p], make_float2(B[j], B[j])));
+          h[p][j] = decay_add(z, h[p][j], __fmul2_rn(x[p], make_float2(B[j], B[j])));
         }
     }
     tmem_wait_st();
@@ -1050,7 +1099,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
           cc[j] = p == 0 ? __fmul2_rn(q[p], h[p][j]) : __ffma2_rn(q[p], h[p][j], cc[j]);
           rr = j == 0 ? __fmul2_rn(ee, Bj) : __ffma2_rn(ee, Bj, rr);
           oo = j == 0 ? __fmul2_rn(h[p][j], Cj) : __ffma2_rn(h[p][j], Cj, oo);
-          e[p][j] = __fmul2_rn(make_float2(exp2_fast(z.x), exp2_fast(z.y)), ee);
+          e[p][j] = decay(z, ee);
           const float2 g = __fmul2_rn(e[p][j], before[p][j]);
           vv = j == 0 ? __fmul2_rn(g, A2[p][j]) : __ffma2_rn(g, A2[p][j], vv);
           dA[p][j] = __ffma2_rn(g, d[p], dA[p][j]);
@@ -1106,20 +1155,21 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   store_states(dA, a, a.A_parts + (part * a.channels + at) * a.states, n0, count);
   if (!kPacked && a.dstate && w.k == 0)
     store_states(e, a, a.dstate + (w.b * a.channels + at) * a.states, n0, count);
-  asm volatile("bar.sync 1, %0;" ::"r"(32 * kPairs) : "memory");  // the first warps
+  asm volatile("bar.sync 1, %0;" ::"r"(32 * L::kPairs) : "memory");  // the first warps
   if (warp == 0) tmem_dealloc(*reinterpret_cast<volatile uint32_t *>(smem), L::kColumns);
 }
 
 // dB and dC from the channel blocks' shares, in order.
 template <typename T>
 __global__ void sum_bc_kernel(ScanArgs<T> a) {
-  const int64_t per = (int64_t)a.groups * 2 * a.states, count = a.batches * a.rows * per;
+  const int64_t per = (int64_t)a.groups * 2 * a.states, count = (int64_t)a.batches * a.rows * per;
   const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (id >= count) return;
   float s = 0.f;
   for (int k = 0; k < a.group_blocks; ++k) s += a.bc_parts[k * count + id];
   const int64_t row = id / per, in = id % per;
-  const int64_t b = row / a.rows, t = row % a.rows;
+  const int64_t b = row / a.rows;
+  const int t = (int)(row % a.rows);
   const int g = (int)(in / (2 * a.states)), which = (int)(in / a.states % 2), n = (int)(in % a.states);
   const Rows<T> &out = which ? a.dC : a.dB;
   out.at(b, t)[(int64_t)g * a.states + n] = from_f<T>(s);

@@ -22,10 +22,10 @@ ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, ScanCall ca
   a.marks = s.marks;
   a.offsets = s.offsets;
   a.slots = s.slots;
-  a.rows = s.rows;
+  a.rows = (int)s.rows;
   a.channels = s.channels;
   a.num_slots = s.num_slots;
-  a.chunk_rows = p.chunk_rows;
+  a.chunk_rows = (int)p.chunk_rows;
   a.states = (int)s.states;
   a.groups = s.groups;
   a.per_group = p.per_group;
@@ -87,17 +87,17 @@ int start(int64_t blocks, int threads, int floats, const ScanArgs<T> &a, cudaStr
 
 template <typename T, int LS, bool kPacked, bool kWide>
 int forward(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
-  const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
+  const int64_t blocks = p.batches * a.groups * p.group_blocks;
   constexpr int floats = Lay<LS, T, kWide>::kFloats;
   if (p.chunks > 1) {
-    if (const int rc = start<scan_kernel<T, LS, kPacked, kState, kWide>>(blocks, Lay<LS, T, kWide>::kBlock, floats,
+    if (const int rc = start<scan_kernel<T, LS, kPacked, kState, kWide>>(blocks * (p.chunks - 1), Lay<LS, T, kWide>::kBlock, floats,
                                                                       a, st))
       return rc;
     const int64_t count = a.channels * a.states * p.batches;
     carry_kernel<T, false><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
     if (const int rc = launched()) return rc;
   }
-  return start<scan_kernel<T, LS, kPacked, kOutputs, kWide>>(blocks, Lay<LS, T, kWide>::kBlock, floats, a, st);
+  return start<scan_kernel<T, LS, kPacked, kOutputs, kWide>>(blocks * p.chunks, Lay<LS, T, kWide>::kBlock, floats, a, st);
 }
 
 template <typename T, int LS, bool kPacked, bool kWide>
@@ -106,7 +106,7 @@ int gradient(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
     using F = Lay<LS, T, kWide>;
     ScanArgs<T> c = a;
     c.group_blocks = (a.per_group + F::DB - 1) / F::DB;
-    const int64_t blocks = p.batches * p.chunks * a.groups * c.group_blocks;
+    const int64_t blocks = p.batches * (p.chunks - 1) * a.groups * c.group_blocks;
     if (const int rc = start<scan_kernel<T, LS, kPacked, kAdjoint, kWide>>(blocks, F::kBlock,
                                                                         F::kFloats, c, st))
       return rc;
@@ -119,18 +119,27 @@ int gradient(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
   return start<scan_grad_kernel<T, LS, kPacked, kWide>>(blocks, L::kBlock, L::kFloats, a, st);
 }
 
+template <typename T, int LS, int NB, bool kWide>
+int token_of(const ScanArgs<T> &a, cudaStream_t st) {
+  const int64_t count = a.channels * ((a.sequences + NB - 1) / NB) * LS;
+  const int64_t blocks = (count + kScanThreads - 1) / kScanThreads;
+  if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  scan_step_kernel<T, LS, NB, kWide><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
+  return launched();
+}
+
+// Four entries a thread once that leaves every SM 2048 threads.
+template <typename T, int LS, bool kWide>
+int token(const ScanArgs<T> &a, cudaStream_t st) {
+  const int64_t threads = a.channels * a.sequences * LS;
+  return threads >= 4 * 2048 * (int64_t)num_sms() ? token_of<T, LS, 4, kWide>(a, st)
+                                                  : token_of<T, LS, 1, kWide>(a, st);
+}
+
 template <typename T, int LS>
 int by_lanes(ScanCall call, const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
-  if (call == kScanStep) {
-    const int64_t count = a.channels * a.sequences * LS;
-    const int64_t blocks = (count + kScanThreads - 1) / kScanThreads;
-    if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
-    if (a.wide_states && a.wide_bc)
-      scan_step_kernel<T, LS, true><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
-    else
-      scan_step_kernel<T, LS, false><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
-    return launched();
-  }
+  if (call == kScanStep)
+    return a.wide_states && a.wide_bc ? token<T, LS, true>(a, st) : token<T, LS, false>(a, st);
   if (call == kScan) {
     if (a.row_seq)
       return a.wide ? forward<T, LS, true, true>(p, a, st) : forward<T, LS, true, false>(p, a, st);
@@ -147,7 +156,7 @@ int run_scan(ScanCall call, const tcu_state_scan_args &s, cudaStream_t st) {
   const ScanArgs<T> a = args_of<T>(s, p, call);
   if (call != kScanStep && s.offsets && s.rows > 0) {
     row_sequence_kernel<<<(unsigned)((s.rows + 127) / 128), 128, 0, st>>>(
-        a.row_seq, s.offsets, s.sequences, s.rows);
+        a.row_seq, s.offsets, s.sequences, (int)s.rows);
     if (const int rc = launched()) return rc;
   }
   int rc = TCU_DFT_ERR_UNSUPPORTED;
