@@ -31,11 +31,14 @@ struct ConvArgs {
   const int32_t *slots;
   int64_t channels, num_slots;
   int rows, sequences, batches, silu;
-  int64_t runs;  // of kBlockRows * blocks rows in a batch entry
+  int runs;  // of kBlockRows * blocks rows in a batch entry
   int blocks;
 };
 
-constexpr int kThreads = 128;
+// A block: 32 threads along the channels, kItems items (runs, or batch
+// entries) below each other.  No division by a size of the call.
+constexpr int kItems = 4;
+constexpr int kThreads = 32 * kItems;
 constexpr int kBlockRows = 8;
 // Rows whose loads are on their way while as many are worked on: a multiple
 // of the width, so that slots are known, near eight.
@@ -83,14 +86,29 @@ struct Own {
     count = kWide ? V : (int)((a.channels - c + gap - 1) / gap);
   }
   __device__ __forceinline__ void params() {
+    float *to = reinterpret_cast<float *>(bias);
+    if constexpr (kWide) {  // the V rows of the weights are adjacent
+      constexpr int step = V * W % 4 == 0 ? 4 : 2;
+      Vec<float, step> all[V * W / step];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const bool in = kWide || v < count;
-      float *to = reinterpret_cast<float *>(bias);
-      to[v] = a.bias && in ? a.bias[c + v * gap] : 0.f;
+      for (int i = 0; i < V * W / step; ++i)
+        all[i] = reinterpret_cast<const Vec<float, step> *>(a.weight + c * W)[i];
 #pragma unroll
-      for (int k = 0; k < W; ++k)
-        reinterpret_cast<float *>(w[k])[v] = in ? a.weight[(c + v * gap) * W + k] : 0.f;
+      for (int v = 0; v < V; ++v) {
+        to[v] = a.bias ? a.bias[c + v] : 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+          reinterpret_cast<float *>(w[k])[v] = all[(v * W + k) / step].v[(v * W + k) % step];
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const bool in = v < count;
+        to[v] = a.bias && in ? a.bias[c + v * gap] : 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+          reinterpret_cast<float *>(w[k])[v] = in ? a.weight[(c + v * gap) * W + k] : 0.f;
+      }
     }
   }
   __device__ __forceinline__ Row row(const T *p) const {
@@ -152,24 +170,26 @@ struct Own {
 template <typename T, int V, int W, bool kWide>
 __global__ void __launch_bounds__(kThreads) conv_kernel(ConvArgs<T> a) {
   const int64_t cvs = (a.channels + V - 1) / V;
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t item = id / cvs, runs = a.runs * a.batches;
-  Own<T, V, W, kWide> own(a, id % cvs, cvs);
+  const int64_t cv = (int64_t)blockIdx.y * 32 + threadIdx.x;
+  const int item = (int)(blockIdx.x * kItems + threadIdx.y), runs = a.runs * a.batches;
+  if (cv >= cvs) return;
+  Own<T, V, W, kWide> own(a, cv, cvs);
   using Row = typename Own<T, V, W, kWide>::Row;
   constexpr int P = V / 2;
   const int64_t c = own.c;
   if (item >= runs) {
-    const int64_t rest = item - runs;
-    if (!a.last || rest >= (int64_t)a.sequences * (W - 1)) return;
+    const int rest = item - runs;
+    if (!a.last || rest >= a.sequences * (W - 1)) return;
     constexpr int kPast = W > 1 ? W - 1 : 1;  // W == 1 has no past and returned
     const Span s = span_at(a, rest / kPast);
     own.b = a.offsets ? 0 : s.seq;
-    const Row r = own.value(s, s.hi - s.lo - (W - 1) + (int)(rest % kPast));
-    r.template store<kWide>(a.last + rest * a.channels + c, own.count, own.gap);
+    const Row r = own.value(s, s.hi - s.lo - (W - 1) + rest % kPast);
+    r.template store<kWide>(a.last + (int64_t)rest * a.channels + c, own.count, own.gap);
     return;
   }
-  const int64_t b = own.b = item / a.runs, run = item % a.runs;
-  const int t0 = (int)run * (kBlockRows * a.blocks), t1 = min(t0 + kBlockRows * a.blocks, a.rows);
+  const int b = (int)((unsigned)item / (unsigned)a.runs), run = item - b * a.runs;
+  own.b = b;
+  const int t0 = run * (kBlockRows * a.blocks), t1 = min(t0 + kBlockRows * a.blocks, a.rows);
   own.params();
   for (int lo = t0; lo < t1;) {
     const Span s = span_of(a, b, lo);
@@ -225,9 +245,10 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(ConvArgs<T> a) {
 template <typename T, int V, int W, bool kWide>
 __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
   const int64_t cvs = (a.channels + V - 1) / V;
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t item = id / cvs, runs = a.runs * a.batches;
-  Own<T, V, W, kWide> own(a, id % cvs, cvs);
+  const int64_t cv = (int64_t)blockIdx.y * 32 + threadIdx.x;
+  const int item = (int)(blockIdx.x * kItems + threadIdx.y), runs = a.runs * a.batches;
+  if (cv >= cvs) return;
+  Own<T, V, W, kWide> own(a, cv, cvs);
   using Row = typename Own<T, V, W, kWide>::Row;
   constexpr int P = V / 2;
   const int64_t c = own.c;
@@ -241,13 +262,13 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
   };
   if (item >= runs) {
     // row i = k - (W-1) < 0 of sequence s: taps of its first rows
-    const int64_t rest = item - runs;
-    if (!a.dstate || rest >= (int64_t)a.sequences * (W - 1)) return;
+    const int rest = item - runs;
+    if (!a.dstate || rest >= a.sequences * (W - 1)) return;
     constexpr int kPast = W > 1 ? W - 1 : 1;
     const Span s = span_at(a, rest / kPast);
     own.b = a.offsets ? 0 : s.seq;
     own.params();
-    const int i = (int)(rest % kPast) - (W - 1), len = s.hi - s.lo;
+    const int i = rest % kPast - (W - 1), len = s.hi - s.lo;
     float2 x[W][P], dp[P], dx[P] = {};
     if (i >= len - (W - 1)) after(s, i - (len - (W - 1)), dx);
     own.window(s, 0, x);
@@ -265,11 +286,12 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
 #pragma unroll
           for (int n = 0; n < P; ++n) dx[n] = __ffma2_rn(own.w[m][n], dp[n], dx[n]);
     }
-    own.put(a.dstate + rest * a.channels + c, dx);
+    own.put(a.dstate + (int64_t)rest * a.channels + c, dx);
     return;
   }
-  const int64_t b = own.b = item / a.runs, run = item % a.runs;
-  const int t0 = (int)run * (kBlockRows * a.blocks), t1 = min(t0 + kBlockRows * a.blocks, a.rows);
+  const int b = (int)((unsigned)item / (unsigned)a.runs), run = item - b * a.runs;
+  own.b = b;
+  const int t0 = run * (kBlockRows * a.blocks), t1 = min(t0 + kBlockRows * a.blocks, a.rows);
   own.params();
   float2 dw[W][P] = {}, db[P] = {};
   for (int lo = t0; lo < t1;) {
@@ -347,7 +369,7 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
     }
     lo = hi;
   }
-  float *share = a.parts + item * a.channels * (W + 1);
+  float *share = a.parts + (int64_t)item * a.channels * (W + 1);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     if (!kWide && v >= own.count) continue;
@@ -361,10 +383,10 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
 template <typename T, int V, int W, bool kWide>
 __global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs<T> a) {
   const int64_t cvs = (a.channels + V - 1) / V;
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t b = id / cvs;
-  if (b >= a.sequences) return;
-  Own<T, V, W, kWide> own(a, id % cvs, cvs);
+  const int64_t cv = (int64_t)blockIdx.y * 32 + threadIdx.x;
+  const int b = (int)(blockIdx.x * kItems + threadIdx.y);
+  if (b >= a.sequences || cv >= cvs) return;
+  Own<T, V, W, kWide> own(a, cv, cvs);
   using Row = typename Own<T, V, W, kWide>::Row;
   constexpr int P = V / 2;
   const int64_t c = own.c, slot = a.slots ? a.slots[b] : b;
@@ -397,17 +419,17 @@ enum Call { kForward, kGrad, kStep };
 template <Call kCall, typename T, int V, int W, bool kWide>
 int launch(const ConvArgs<T> &a, cudaStream_t st) {
   const int64_t cvs = (a.channels + V - 1) / V;
-  int64_t items = a.runs * a.batches;
+  int64_t items = (int64_t)a.runs * a.batches;
   if (kCall == kStep) items = a.sequences;
   else if (kCall == kForward ? a.last != nullptr : a.dstate != nullptr)
     items += (int64_t)a.sequences * (W - 1);
-  const int64_t blocks = (items * cvs + kThreads - 1) / kThreads;
-  if (blocks == 0) return TCU_DFT_OK;
-  if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)blocks);
-  if constexpr (kCall == kForward) conv_kernel<T, V, W, kWide><<<grid, kThreads, 0, st>>>(a);
-  else if constexpr (kCall == kGrad) conv_grad_kernel<T, V, W, kWide><<<grid, kThreads, 0, st>>>(a);
-  else conv_step_kernel<T, V, W, kWide><<<grid, kThreads, 0, st>>>(a);
+  if (items == 0) return TCU_DFT_OK;
+  const int64_t down = (items + kItems - 1) / kItems, across = (cvs + 31) / 32;
+  if (items > INT32_MAX - kItems || across > 65535) return TCU_DFT_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)down, (unsigned)across), block(32, kItems);
+  if constexpr (kCall == kForward) conv_kernel<T, V, W, kWide><<<grid, block, 0, st>>>(a);
+  else if constexpr (kCall == kGrad) conv_grad_kernel<T, V, W, kWide><<<grid, block, 0, st>>>(a);
+  else conv_step_kernel<T, V, W, kWide><<<grid, block, 0, st>>>(a);
   return launched();
 }
 
@@ -481,11 +503,13 @@ int dispatch(Call call, const tcu_short_conv_args &s, cudaStream_t st) {
   a.sequences = s.sequences;
   a.batches = (int)sh.batches;
   a.silu = s.silu;
-  a.runs = sh.runs;
+  if (sh.runs * sh.batches > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  a.runs = (int)sh.runs;
   a.blocks = sh.blocks;
   if (call == kGrad) a.parts = static_cast<float *>(s.workspace);
   const int64_t batches = call == kStep ? s.sequences : sh.batches;
-  bool wide = s.channels % V == 0 && rows_aligned(s.x, s.type, batches, s.rows, word);
+  bool wide = s.channels % V == 0 && (uintptr_t)s.weight % 16 == 0 &&
+              rows_aligned(s.x, s.type, batches, s.rows, word);
   if (call == kGrad)
     wide = wide && rows_aligned(s.dy, s.type, batches, s.rows, word) &&
            rows_aligned(s.dx, s.type, batches, s.rows, word);

@@ -77,14 +77,12 @@ struct Place {
   int g, cb, nc;
   // of `chunks` chunks from `first` on
   __device__ __forceinline__ explicit Place(const ScanArgs<T> &a, int chunks, int first) {
-    const int blocks = a.groups * a.group_blocks;
-    const int64_t id = blockIdx.x;
-    const int blk = (int)(id % blocks);
-    const int64_t bk = id / blocks;
-    k = first + bk % chunks;
-    b = bk / chunks;
-    g = blk / a.group_blocks;
-    cb = blk % a.group_blocks;
+    const unsigned blocks = a.groups * a.group_blocks, bk = blockIdx.x / blocks;
+    const unsigned blk = blockIdx.x - bk * blocks;
+    b = bk / (unsigned)chunks;
+    k = first + (int)(bk - (unsigned)b * chunks);
+    g = (int)(blk / (unsigned)a.group_blocks);
+    cb = (int)blk - g * a.group_blocks;
     c0 = (int64_t)g * a.per_group + cb * DB;
     nc = min(DB, a.per_group - cb * DB);
     r0 = (int)k * a.chunk_rows;
@@ -627,93 +625,103 @@ __global__ void __launch_bounds__(64 * kPairs, kResident)
 }
 
 // carry[k] <- the state that enters chunk k (kBack: the adjoint that enters
-// it from below), from each chunk's own contribution in carry[k].
+// it from below), from each chunk's own contribution in carry[k].  One thread
+// a state; the chunks' loads go ahead in fours of the chain that joins them.
 template <typename T, bool kBack>
 __global__ void carry_kernel(ScanArgs<T> a) {
   const int64_t per = a.channels * a.states;
-  const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (id >= per * a.batches) return;
-  const int64_t b = id / per, at = id % per, c = at / a.states;
+  const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (at >= per) return;
+  const int64_t c = at / a.states;
   const float A2 = a.A[at] * kLog2e;
-  float h = 0.f;
-  for (int j = 0; j < a.chunks; ++j) {
-    const int k = kBack ? a.chunks - 1 - j : j;
-    const int r0 = k * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
-    float *p = a.carry + (b * a.chunks + k) * per + at;
-    // the last chunk of the walk has left nothing, and nothing needs it
-    if (j == a.chunks - 1) {
-      *p = h;
-      break;
+  for (int64_t b = blockIdx.y; b < a.batches; b += gridDim.y) {
+    float h = 0.f;
+    for (int j0 = 0; j0 < a.chunks; j0 += 4) {
+      float own[4], sum[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // the last chunk of the walk has left nothing, and nothing needs it
+        const int k = kBack ? a.chunks - 1 - (j0 + j) : j0 + j;
+        const bool in = j0 + j < a.chunks - 1;
+        own[j] = in ? a.carry[(b * a.chunks + k) * per + at] : 0.f;
+        sum[j] = in ? a.sum_d[(b * a.chunks + k) * a.channels + c] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (j0 + j >= a.chunks) break;
+        const int k = kBack ? a.chunks - 1 - (j0 + j) : j0 + j;
+        const int r0 = k * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
+        // does a sequence open (close, going back) within the chunk?
+        bool cut;
+        if (kBack) cut = r1 == a.rows || (a.row_seq && a.row_seq[r0] != a.row_seq[r1]);
+        else cut = r0 == 0 || (a.row_seq && a.row_seq[r0 - 1] != a.row_seq[r1 - 1]);
+        a.carry[(b * a.chunks + k) * per + at] = h;
+        h = cut || h == 0.f ? own[j] : fmaf(exp2_fast(A2 * sum[j]), h, own[j]);
+      }
     }
-    const float own = *p, decay = exp2_fast(A2 * a.sum_d[(b * a.chunks + k) * a.channels + c]);
-    // does a sequence open (close, going back) within the chunk?
-    bool cut;
-    if (kBack) cut = r1 == a.rows || (a.row_seq && a.row_seq[r0] != a.row_seq[r1]);
-    else cut = r0 == 0 || (a.row_seq && a.row_seq[r0 - 1] != a.row_seq[r1 - 1]);
-    *p = h;
-    h = cut || h == 0.f ? own : fmaf(decay, h, own);
   }
 }
 
-// One token: LS lanes per channel, 4 states each, the cache in place.  The
-// cache read and written is nearly all it does: 16 bytes a lane either way.
-// NB batch entries a thread, on their way at once, for one load of A.
+// One token: LS lanes per channel, 4 states each, the cache in place: 16
+// bytes a lane read and written, nearly all that it does.  NB batch entries
+// at once, on their way together; what is one value a row and channel (d, d u,
+// the gate) is done for one entry by each NB-th part of the lanes.
 template <typename T, int LS, int NB, bool kWide>
 __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(ScanArgs<T> a) {
-  const int64_t id = ((int64_t)blockIdx.x * kScanThreads + threadIdx.x) / LS;
-  const int sl = threadIdx.x % LS, n0 = sl * 4, n = min(4, a.states - n0);
-  const int64_t batches = (a.sequences + NB - 1) / NB;
-  const bool in = id < a.channels * batches;
-  const int64_t b0 = in ? id / a.channels : 0, c = in ? id % a.channels : 0;
-  const int64_t g = c / a.per_group * a.states + n0;
-  Raw<float, 4> h[NB], A;
-  Raw<T, 4> B[NB], C[NB];
-  float *cache[NB];
-  float u[NB], dt[NB], z[NB], o[NB];
-  A.template load<kWide>(a.A + c * a.states + n0, in ? n : 0);
-  const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
+  constexpr int kShare = LS / NB;  // lanes of a channel for one entry's values
+  const int64_t c = ((int64_t)blockIdx.x * kScanThreads + threadIdx.x) / LS;
+  const int lane = threadIdx.x % 32, sl = lane % LS, n0 = sl * 4, first = lane - sl;
+  const bool here = c < a.channels;
+  const int n = here ? min(4, a.states - n0) : 0;
+  const int64_t g = (unsigned)c / (unsigned)a.per_group * (int64_t)a.states + n0;
+  const int64_t entry = a.channels * a.states;
+  float *at = a.last + c * a.states + n0;
+  Raw<float, 4> A;
+  A.template load<kWide>(a.A + c * a.states + n0, n);
+  const float bias = here && a.dt_bias ? a.dt_bias[c] : 0.f;
+  const float skip = here && a.skip ? a.skip[c] : 0.f;
+  for (int b0 = blockIdx.y * NB; b0 < a.sequences; b0 += gridDim.y * NB) {
+    Raw<float, 4> h[NB];
+    Raw<T, 4> B[NB], C[NB];
+    float *cache[NB];
 #pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    const int64_t b = b0 + i * batches;
-    const bool row = in && b < a.sequences;
-    const int64_t slot = !row ? -1 : a.slots ? a.slots[b] : b;
-    const bool live = slot >= 0 && slot < a.num_slots;
-    cache[i] = live ? a.last + (slot * a.channels + c) * a.states + n0 : nullptr;
-    h[i].template load<kWide>(cache[i], live ? n : 0);
-    B[i].template load<kWide>(a.B.at(b, 0) + g, live ? n : 0);
-    C[i].template load<kWide>(a.C.at(b, 0) + g, live ? n : 0);
-    u[i] = live ? to_f(a.u.at(b, 0)[c]) : 0.f;
-    dt[i] = live ? to_f(a.dt.at(b, 0)[c]) : 0.f;
-    z[i] = live && a.gate.p ? to_f(a.gate.at(b, 0)[c]) : 0.f;
-  }
-#pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    const float d = step_of(a, dt[i], bias);
-    const float2 x = make_float2(d * u[i], d * u[i]), e = make_float2(d * kLog2e, d * kLog2e);
-    float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float2 r = __fmul2_rn(e, A.pair(j));
-      const float2 v = __ffma2_rn(make_float2(exp2_fast(r.x), exp2_fast(r.y)), h[i].pair(j),
-                                  __fmul2_rn(x, B[i].pair(j)));
-      h[i].set(j, v);
-      sum = __ffma2_rn(C[i].pair(j), v, sum);
+    for (int i = 0; i < NB; ++i) {
+      const int b = b0 + i;
+      const int slot = b >= a.sequences ? -1 : a.slots ? a.slots[b] : b;
+      const bool live = slot >= 0 && slot < a.num_slots;
+      cache[i] = live ? at + slot * entry : nullptr;
+      h[i].template load<kWide>(cache[i], live ? n : 0);
+      B[i].template load<kWide>(a.B.at(0, b) + g, live ? n : 0);
+      C[i].template load<kWide>(a.C.at(0, b) + g, live ? n : 0);
     }
-    o[i] = sum.x + sum.y;
-    if (cache[i]) h[i].template store<kWide>(cache[i], n);
-  }
+    const int mine = sl / kShare, b = b0 + mine;  // this lane's entry
+    const bool in = here && b < a.sequences;
+    const float u = in ? to_f(a.u.at(0, b)[c]) : 0.f;
+    const float z = in && a.gate.p ? to_f(a.gate.at(0, b)[c]) : 0.f;
+    const float d = step_of(a, in ? to_f(a.dt.at(0, b)[c]) : 0.f, bias), x = d * u;
+    float o[NB];
+    bool live = false;
 #pragma unroll
-  for (int s = LS / 2; s > 0; s /= 2)
+    for (int i = 0; i < NB; ++i) {
+      const float di = __shfl_sync(~0u, d, first + i * kShare) * kLog2e;
+      const float xi = __shfl_sync(~0u, x, first + i * kShare);
+      float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) o[i] += __shfl_xor_sync(~0u, o[i], s);
-  if (!in || sl != 0) return;
-#pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    const int64_t b = b0 + i * batches;
-    if (b >= a.sequences) break;
-    float y = fmaf(skip, u[i], o[i]);
-    if (a.gate.p) y *= silu(z[i]);
-    a.y.at(b, 0)[c] = from_f<T>(cache[i] ? y : 0.f);
+      for (int j = 0; j < 2; ++j) {
+        const float2 v = decay_add(__fmul2_rn(make_float2(di, di), A.pair(j)), h[i].pair(j),
+                                   __fmul2_rn(make_float2(xi, xi), B[i].pair(j)));
+        h[i].set(j, v);
+        sum = __ffma2_rn(C[i].pair(j), v, sum);
+      }
+      o[i] = sum.x + sum.y;
+      if (cache[i]) h[i].template store<kWide>(cache[i], n);
+      if (i == mine) live = cache[i] != nullptr;
+    }
+    reduce_scatter<NB, LS, 1>(o, lane);
+    if (!in || sl % kShare != 0) continue;
+    float y = fmaf(skip, u, o[0]);
+    if (a.gate.p) y *= silu(z);
+    a.y.at(0, b)[c] = from_f<T>(live ? y : 0.f);
   }
 }
 
@@ -1159,20 +1167,26 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
   if (warp == 0) tmem_dealloc(*reinterpret_cast<volatile uint32_t *>(smem), L::kColumns);
 }
 
-// dB and dC from the channel blocks' shares, in order.
+// dB and dC from the channel blocks' shares, in order: a block takes as many
+// rows as fit its threads, blockIdx.y the batch entries.
+constexpr int kSumThreads = 256;  // at least the values of a row and group: 2 * 128
 template <typename T>
-__global__ void sum_bc_kernel(ScanArgs<T> a) {
-  const int64_t per = (int64_t)a.groups * 2 * a.states, count = (int64_t)a.batches * a.rows * per;
-  const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (id >= count) return;
-  float s = 0.f;
-  for (int k = 0; k < a.group_blocks; ++k) s += a.bc_parts[k * count + id];
-  const int64_t row = id / per, in = id % per;
-  const int64_t b = row / a.rows;
-  const int t = (int)(row % a.rows);
-  const int g = (int)(in / (2 * a.states)), which = (int)(in / a.states % 2), n = (int)(in % a.states);
-  const Rows<T> &out = which ? a.dC : a.dB;
-  out.at(b, t)[(int64_t)g * a.states + n] = from_f<T>(s);
+__global__ void __launch_bounds__(kSumThreads) sum_bc_kernel(ScanArgs<T> a) {
+  const int per = 2 * a.states, down = threadIdx.x / per, at = threadIdx.x - down * per;
+  const int each = kSumThreads / per;  // rows and groups a block takes
+  const int which = at >= a.states, n = at - which * a.states;
+  const int64_t item = (int64_t)blockIdx.x * each + down;
+  if (down >= each || item >= (int64_t)a.rows * a.groups) return;
+  const int t = (int)((uint64_t)item / (unsigned)a.groups), g = (int)(item - (int64_t)t * a.groups);
+  const int64_t entry = (int64_t)a.rows * a.groups * per;
+  for (int64_t b = blockIdx.y; b < a.batches; b += gridDim.y) {
+    const float *from = a.bc_parts + b * entry + item * per + at;
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < a.group_blocks; ++k) s += from[k * a.batches * entry];
+    const Rows<T> &out = which ? a.dC : a.dB;
+    out.at(b, t)[(int64_t)g * a.states + n] = from_f<T>(s);
+  }
 }
 
 // ------------------------------------------------------------- host side

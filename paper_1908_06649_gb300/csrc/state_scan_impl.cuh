@@ -50,6 +50,9 @@ ScanArgs<T> args_of(const tcu_state_scan_args &s, const ScanPlan &p, ScanCall ca
   else
     for (const tcu_seq_rows *r : {&s.dy, &s.du, &s.ddt, &s.dgate})
       a.wide = a.wide && rows_aligned(*r, s.type, batches, rows, word);
+  if (step)  // one row an entry: entries step as rows do
+    for (Rows<const T> *r : {&a.u, &a.dt, &a.gate, &a.B, &a.C}) r->row = (int32_t)r->batch;
+  if (step) a.y.row = (int32_t)(a.y.batch = s.y.batch_stride);
   float *w = static_cast<float *>(s.workspace);
   a.carry = w;
   a.sum_d = a.carry + p.carry;
@@ -85,6 +88,35 @@ int start(int64_t blocks, int threads, int floats, const ScanArgs<T> &a, cudaStr
   return launched();
 }
 
+template <typename T, int LS, int NB, bool kWide>
+int token_of(const ScanArgs<T> &a, cudaStream_t st) {
+  const int64_t blocks = (a.channels * LS + kScanThreads - 1) / kScanThreads;
+  if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  const int entries = (a.sequences + NB - 1) / NB;
+  const dim3 grid((unsigned)blocks, (unsigned)std::min(entries, 65535));
+  scan_step_kernel<T, LS, NB, kWide><<<grid, kScanThreads, 0, st>>>(a);
+  return launched();
+}
+
+// Four entries a thread (two, where two lanes share a channel) once that
+// leaves every SM some 1000 threads.
+template <typename T, int LS, bool kWide>
+int token(const ScanArgs<T> &a, cudaStream_t st) {
+  constexpr int NB = LS < 4 ? 2 : 4;
+  const int64_t threads = a.channels * a.sequences * LS;
+  return threads >= NB * 1024 * (int64_t)num_sms() ? token_of<T, LS, NB, kWide>(a, st)
+                                                   : token_of<T, LS, 1, kWide>(a, st);
+}
+
+template <typename T, bool kBack>
+int carry(const ScanArgs<T> &a, cudaStream_t st) {
+  const int64_t blocks = (a.channels * a.states + 127) / 128;
+  if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)blocks, (unsigned)std::min(a.batches, 65535));
+  carry_kernel<T, kBack><<<grid, 128, 0, st>>>(a);
+  return launched();
+}
+
 template <typename T, int LS, bool kPacked, bool kWide>
 int forward(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
   const int64_t blocks = p.batches * a.groups * p.group_blocks;
@@ -93,9 +125,7 @@ int forward(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
     if (const int rc = start<scan_kernel<T, LS, kPacked, kState, kWide>>(blocks * (p.chunks - 1), Lay<LS, T, kWide>::kBlock, floats,
                                                                       a, st))
       return rc;
-    const int64_t count = a.channels * a.states * p.batches;
-    carry_kernel<T, false><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
-    if (const int rc = launched()) return rc;
+    if (const int rc = carry<T, false>(a, st)) return rc;
   }
   return start<scan_kernel<T, LS, kPacked, kOutputs, kWide>>(blocks * p.chunks, Lay<LS, T, kWide>::kBlock, floats, a, st);
 }
@@ -110,30 +140,11 @@ int gradient(const ScanPlan &p, const ScanArgs<T> &a, cudaStream_t st) {
     if (const int rc = start<scan_kernel<T, LS, kPacked, kAdjoint, kWide>>(blocks, F::kBlock,
                                                                         F::kFloats, c, st))
       return rc;
-    const int64_t count = a.channels * a.states * p.batches;
-    carry_kernel<T, true><<<(unsigned)((count + 127) / 128), 128, 0, st>>>(a);
-    if (const int rc = launched()) return rc;
+    if (const int rc = carry<T, true>(a, st)) return rc;
   }
   using L = GradLay<LS, T>;
   const int64_t blocks = p.batches * p.chunks * a.groups * p.group_blocks;
   return start<scan_grad_kernel<T, LS, kPacked, kWide>>(blocks, L::kBlock, L::kFloats, a, st);
-}
-
-template <typename T, int LS, int NB, bool kWide>
-int token_of(const ScanArgs<T> &a, cudaStream_t st) {
-  const int64_t count = a.channels * ((a.sequences + NB - 1) / NB) * LS;
-  const int64_t blocks = (count + kScanThreads - 1) / kScanThreads;
-  if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
-  scan_step_kernel<T, LS, NB, kWide><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
-  return launched();
-}
-
-// Four entries a thread once that leaves every SM 2048 threads.
-template <typename T, int LS, bool kWide>
-int token(const ScanArgs<T> &a, cudaStream_t st) {
-  const int64_t threads = a.channels * a.sequences * LS;
-  return threads >= 4 * 2048 * (int64_t)num_sms() ? token_of<T, LS, 4, kWide>(a, st)
-                                                  : token_of<T, LS, 1, kWide>(a, st);
 }
 
 template <typename T, int LS>
@@ -170,9 +181,14 @@ int run_scan(ScanCall call, const tcu_state_scan_args &s, cudaStream_t st) {
     case 32: rc = by_lanes<T, 32>(call, p, a, st); break;
   }
   if (rc != TCU_DFT_OK || call != kScanGrad) return rc;
-  const int64_t bc = p.batches * s.rows * s.groups * 2 * s.states;
-  if (bc > 0) sum_bc_kernel<T><<<(unsigned)((bc + 127) / 128), 128, 0, st>>>(a);
-  if ((rc = launched())) return rc;
+  if (!none) {
+    const int64_t each = kSumThreads / (2 * s.states);
+    const int64_t blocks = (s.rows * s.groups + each - 1) / each;
+    if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks, (unsigned)std::min<int64_t>(p.batches, 65535));
+    sum_bc_kernel<T><<<grid, kSumThreads, 0, st>>>(a);
+    if ((rc = launched())) return rc;
+  }
   const int64_t parts = none ? 0 : p.batches * p.chunks;
   Sum sums[3] = {{s.dA, a.A_parts, s.channels * s.states}};
   int count = 1;
