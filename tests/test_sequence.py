@@ -588,3 +588,18 @@ def test_offsets_out_of_order_stay_in_range(pkg):
         pkg.short_conv(c["x"], c["weight"], offsets=off, out=buf[10:80])
         assert (buf[:10] == 9).all() and (buf[80:] == 9).all()
     torch.cuda.synchronize()
+
+
+def test_no_step_leaves_the_state(pkg):
+    """d = 0 is a decay of exactly 1 and no input: the bits of the state stay,
+    over prompts (whole and in parts) and tokens."""
+    for rows in (40, 5000):
+        d = cuda(scan_inputs(torch.float32, (1, rows, 8), 16, 1, None))
+        zero = torch.zeros_like(d["dt"])
+        y, last = pkg.state_scan(d["u"], zero, d["A"], d["B"], d["C"], state=d["state"])
+        assert torch.equal(last, d["state"])
+        want = torch.einsum("cn,rn->rc", d["state"][0].double(), d["C"][0, :, 0].double())
+        close(y[0], want.cpu())
+    cache = d["state"].clone()
+    pkg.state_scan_step(d["u"][:, 0], zero[:, 0], d["A"], d["B"][:, 0], d["C"][:, 0], cache)
+    assert torch.equal(cache, d["state"])
