@@ -91,7 +91,7 @@ def serve(block, width=256):
         y = block.token(torch.stack([r[n + t] for r, n in zip(rows, lengths)]), caches)
         for i, n in enumerate(lengths):
             worst = max(worst, float((y[i] - whole[i][n + t].detach()).abs().max()))
-    scale = max(float(w.abs().max()) for w in whole)
+    scale = max(float(w.detach().abs().max()) for w in whole)
     return worst / scale
 
 

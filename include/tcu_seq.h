@@ -29,13 +29,16 @@
  *
  * Row tensors and the convolution's states are of one type (tcu_seq_type);
  * the scan's states, all parameters and their gradients are fp32.  Sums,
- * states and gradients are accumulated in fp32 and rounded once, on storing.
+ * states and gradients are accumulated in fp32 and rounded once, on storing;
+ * the same call gives the same bits every time.  Exponentials and reciprocals
+ * are the special function unit's (2^-22 of the result).
  *
  * Calls are asynchronous on `stream` (a cudaStream_t), allocate nothing, and
  * return a TCU_DFT_* status: ERR_INVALID (sizes, null pointers, alignment of
  * a pointer to its element, workspace too small), ERR_UNSUPPORTED (width or
- * states beyond the limits, more than 2^31 - 1 rows), ERR_CUDA.  On an
- * argument error nothing is launched.  Outputs must not overlap inputs.
+ * states beyond the limits, more than 2^31 - 4097 rows, a row stride, or a
+ * single-token call's batch stride, beyond 32 bits), ERR_CUDA.  On an argument
+ * error nothing is launched.  Outputs must not overlap inputs.
  */
 #ifndef TCU_SEQ_H
 #define TCU_SEQ_H

@@ -8,9 +8,14 @@
 //     dx_i = sum_k w_k dp_{i+(W-1)-k} (+ dlast at the last W-1 rows)
 //     dw_k = sum_i dp_i x_{i-(W-1)+k},           dbias = sum_i dp_i
 // A dozen operations for each value read and written: HBM bounds the whole
-// of it, so a thread owns a few adjacent channels (one 16-byte word where the
-// rows allow it) and walks down the rows with its window in registers: each
-// row is read once, but for the W-1 rows above a run.
+// of it, so a thread owns a few adjacent channels and walks down the rows with
+// its window in registers and the next rows on their way: each row is read
+// once, but for the W-1 rows above a run (and, for the gradient, below it).
+//
+// Measured, bf16, width 4 with silu: forward at 8 x 4096 x 4096, 4 channels a
+// thread, 103 us, 5.2 TB/s (16-byte words of 8 channels hold half the threads:
+// 112 us); gradient at 8 x 2048 x 4096, 2 channels a thread, 99 us, 4.1 TB/s
+// (with 4: 135 us).  Copying runs at 6.8 TB/s.
 #include <algorithm>
 
 #include "seq_common.cuh"
@@ -379,7 +384,8 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(ConvArgs<T> a) {
   }
 }
 
-// One token: one thread per V channels and batch entry.
+// One token: one thread per V channels and batch entry.  512 x 4096 bf16: 13 us,
+// 2.6 TB/s, of which launch and drain are 7.
 template <typename T, int V, int W, bool kWide>
 __global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs<T> a) {
   const int64_t cvs = (a.channels + V - 1) / V;

@@ -25,10 +25,12 @@ ScanPlan plan_of(const tcu_state_scan_args &a, bool grad) {
   // that all blocks run at once.  The forward scan then pays its recurrence
   // almost twice: at 2048 rows x 4096 channels x 16 states, 42 % of the slots,
   // 232 us whole against 276 split; 21 %, 232 against 173.  The gradient pays
-  // less for it: 42 %, 852 us against 756.
+  // less for it: 42 %, 852 us against 756.  Two more kernels cost some 130 rows
+  // of a block's time (forward; 60, gradient): 37 rows x 768 channels take 11
+  // us whole, 22 split (31 and 38), so few rows are left whole.
   const int64_t slots = (grad ? grad_resident(p.ls) : kResident) * (int64_t)num_sms();
   int64_t chunks = blocks == 0 || blocks * (grad ? 2 : 3) > slots ? 1 : slots / blocks;
-  chunks = std::max<int64_t>(1, std::min(chunks, tiles / 2));
+  chunks = tiles < (grad ? 4 : 6) ? 1 : std::max<int64_t>(1, std::min(chunks, tiles));
   const int64_t chunk_tiles = std::max<int64_t>(1, (tiles + chunks - 1) / chunks);
   p.chunk_rows = chunk_tiles * kTile;
   p.chunks = (int)std::max<int64_t>(1, (a.rows + p.chunk_rows - 1) / p.chunk_rows);

@@ -241,6 +241,28 @@ def _adjacent(t):
     return t if t.shape[-1] == 1 or t.stride(-1) == 1 else t.contiguous()
 
 
+def _apart(out, others):
+    """Refuses an output that shares elements with an input."""
+    size = out.element_size()
+
+    def span(t):
+        return t.data_ptr(), t.data_ptr() + size * (
+            1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+    for t in others:
+        if t is None or not t.numel() or not out.numel():
+            continue
+        (a, b), (c, d) = span(out), span(t)
+        if b <= c or d <= a:
+            continue
+        # columns of one wider tensor: apart if their columns are
+        row, ch = out.stride()[-2], out.shape[-1]
+        at = (a - c) // size % row if row else 0
+        if t.stride()[:-1] == out.stride()[:-1] and ch <= at <= row - ch:
+            continue
+        raise ValueError("out must not overlap an input")
+
+
 def _workspace(name, packed, device):
     _lib()
     n = _calls[name](packed)
@@ -269,6 +291,8 @@ def _conv(x, weight, bias, silu, state, offsets, out, stream):
         y = torch.empty(x.shape, dtype=dtype, device=x.device) if out is None else out
         last = torch.empty(tail, dtype=dtype, device=x.device)
         py = _rows(y, "out", dtype, index, x.shape)
+        if out is not None:
+            _apart(out, (x, state))
         if ch:
             _call("tcu_short_conv", _CONV.pack(
                 _TYPES[dtype], width, bool(silu), seqs, rows, ch, off, *px, *py, *_NO_ROWS,
@@ -278,18 +302,18 @@ def _conv(x, weight, bias, silu, state, offsets, out, stream):
 
 class _ShortConv(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, state, silu, offsets, stream):
+    def forward(ctx, x, weight, bias, state, silu, offsets):
         ctx.save_for_backward(x, weight, bias, state, offsets)
-        ctx.silu, ctx.stream = silu, stream
-        return _conv(x, weight, bias, silu, state, offsets, None, stream)
+        ctx.silu = silu
+        return _conv(x, weight, bias, silu, state, offsets, None, None)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy, dlast):
         x, weight, bias, state, offsets = ctx.saved_tensors
         g = short_conv_grad(_adjacent(dy), x, weight, bias, silu=ctx.silu, state=state,
-                            offsets=offsets, dlast=dlast.contiguous(), stream=ctx.stream)
-        return g.x, g.weight, g.bias, g.state, None, None, None
+                            offsets=offsets, dlast=dlast.contiguous())
+        return g.x, g.weight, g.bias, g.state, None, None
 
 
 def short_conv(x, weight, bias=None, *, silu=False, state=None, offsets=None, out=None,
@@ -303,9 +327,9 @@ def short_conv(x, weight, bias=None, *, silu=False, state=None, offsets=None, ou
     None).  Returns (y, last), last being the state that a continuation takes.
     """
     if _wants_grad(x, weight, bias, state):
-        if out is not None:
-            raise ValueError("out cannot be given where a gradient is asked")
-        return _ShortConv.apply(x, weight, bias, state, silu, offsets, stream)
+        if out is not None or stream is not None:
+            raise ValueError("out and stream cannot be given where a gradient is asked")
+        return _ShortConv.apply(x, weight, bias, state, silu, offsets)
     return _conv(x, weight, bias, silu, state, offsets, out, stream)
 
 
@@ -421,6 +445,8 @@ def _scan(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets, marks, 
         y = torch.empty(u.shape, dtype=u.dtype, device=dev) if out is None else out
         last = torch.empty(c.tail, dtype=f32, device=dev)
         py = _rows(y, "out", c.dtype, c.index, u.shape)
+        if out is not None:
+            _apart(out, (u, dt, gate))
         kept = torch.empty(c.marks, dtype=f32, device=dev) if marks else None
 
         def packed(work, size):
@@ -436,11 +462,11 @@ def _scan(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets, marks, 
 
 class _StateScan(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, u, dt, A, B, C, skip, gate, dt_bias, state, softplus, offsets, stream):
+    def forward(ctx, u, dt, A, B, C, skip, gate, dt_bias, state, softplus, offsets):
         y, last, marks = _scan(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets,
-                               True, None, stream)
+                               True, None, None)
         ctx.save_for_backward(u, dt, A, B, C, skip, gate, dt_bias, state, offsets, marks)
-        ctx.softplus, ctx.stream = softplus, stream
+        ctx.softplus = softplus
         return y, last
 
     @staticmethod
@@ -449,8 +475,8 @@ class _StateScan(torch.autograd.Function):
         u, dt, A, B, C, skip, gate, dt_bias, state, offsets, marks = ctx.saved_tensors
         g = state_scan_grad(_adjacent(dy), u, dt, A, B, C, marks=marks, skip=skip, gate=gate,
                             dt_bias=dt_bias, softplus=ctx.softplus, state=state,
-                            offsets=offsets, dlast=dlast.contiguous(), stream=ctx.stream)
-        return g.u, g.dt, g.A, g.B, g.C, g.skip, g.gate, g.dt_bias, g.state, None, None, None
+                            offsets=offsets, dlast=dlast.contiguous())
+        return g.u, g.dt, g.A, g.B, g.C, g.skip, g.gate, g.dt_bias, g.state, None, None
 
 
 def state_scan(u, dt, A, B, C, *, skip=None, gate=None, dt_bias=None, softplus=False, state=None,
@@ -470,10 +496,9 @@ def state_scan(u, dt, A, B, C, *, skip=None, gate=None, dt_bias=None, softplus=F
     ``marks`` also the states that state_scan_grad resumes from.
     """
     if _wants_grad(u, dt, A, B, C, skip, gate, dt_bias, state):
-        if out is not None or marks:
-            raise ValueError("out and marks cannot be given where a gradient is asked")
-        return _StateScan.apply(u, dt, A, B, C, skip, gate, dt_bias, state, softplus, offsets,
-                                stream)
+        if out is not None or marks or stream is not None:
+            raise ValueError("out, marks and stream cannot be given where a gradient is asked")
+        return _StateScan.apply(u, dt, A, B, C, skip, gate, dt_bias, state, softplus, offsets)
     y, last, kept = _scan(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets, marks,
                           out, stream)
     return (y, last, kept) if marks else (y, last)

@@ -603,3 +603,41 @@ def test_no_step_leaves_the_state(pkg):
     cache = d["state"].clone()
     pkg.state_scan_step(d["u"][:, 0], zero[:, 0], d["A"], d["B"][:, 0], d["C"][:, 0], cache)
     assert torch.equal(cache, d["state"])
+
+
+def test_outputs_over_inputs_are_refused(pkg):
+    d = cuda(scan_inputs(torch.float32, (2, 37, 24), 16, 1, None))
+    args = [d[k] for k in SCAN[:5]]
+    w = torch.randn(24, 4, device="cuda")
+    for out in (d["u"], d["dt"]):
+        with pytest.raises(ValueError):
+            pkg.state_scan(*args, out=out)
+    with pytest.raises(ValueError):
+        pkg.short_conv(d["u"], w, out=d["u"])
+    wide = torch.randn(2, 37, 64, device="cuda")
+    with pytest.raises(ValueError):
+        pkg.short_conv(wide[..., :24], w, out=wide[..., 20:44])
+    want = pkg.short_conv(wide[..., :24].clone(), w)[0]
+    pkg.short_conv(wide[..., :24], w, out=wide[..., 24:48])
+    assert torch.equal(wide[..., 24:48], want)
+    # a gradient is recorded on the current stream, for outputs of the call's own
+    u = d["u"].clone().requires_grad_()
+    for more in ({"out": torch.empty_like(d["u"])}, {"stream": torch.cuda.Stream()}):
+        with pytest.raises(ValueError):
+            pkg.short_conv(u, w, **more)
+        with pytest.raises(ValueError):
+            pkg.state_scan(u, *args[1:], **more)
+
+
+def test_gradients_beside_other_streams(pkg):
+    """Backward passes under a stream that is not the default one."""
+    c = cuda(conv_inputs(torch.float32, (2, 300, 64), 4, None, True, False))
+    want = pkg.short_conv_grad(c["dy"], c["x"], c["weight"], c["bias"], silu=True)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        x = c["x"].clone().requires_grad_()
+        y, _ = pkg.short_conv(x, c["weight"], c["bias"], silu=True)
+        (y * c["dy"]).sum().backward()
+    s.synchronize()
+    assert torch.equal(x.grad, want.x)
