@@ -104,7 +104,7 @@ def train(block, width=256, steps=8, rate=0.02):
     for _ in range(steps):
         y, _ = block.prompt(x)
         loss = (y.float() - target).square().mean()
-        losses.append(float(loss))
+        losses.append(float(loss.detach()))
         grads = torch.autograd.grad(loss, block.parameters())
         with torch.no_grad():
             for p, g in zip(block.parameters(), grads):

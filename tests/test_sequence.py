@@ -641,3 +641,41 @@ def test_gradients_beside_other_streams(pkg):
         (y * c["dy"]).sum().backward()
     s.synchronize()
     assert torch.equal(x.grad, want.x)
+
+
+def test_offsets_beyond_32_bits(pkg):
+    """Tensors of more than 2^31 elements: the last channels of the last rows,
+    and the last entries of a cache, as they are in small tensors."""
+    rows, ch = 70016, 32768
+    assert rows * ch > 2 ** 31
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    u = torch.empty(1, rows, ch, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    w = torch.randn(ch, 4, generator=gen, device="cuda")
+    y, last = pkg.short_conv(u, w, silu=True)
+    part = u[..., -64:].contiguous()
+    want, want_last = pkg.short_conv(part, w[-64:].contiguous(), silu=True)
+    assert torch.equal(y[..., -64:], want) and torch.equal(last[..., -64:], want_last)
+    g = pkg.short_conv_grad(y, u, w, silu=True)
+    h = pkg.short_conv_grad(want, part, w[-64:].contiguous(), silu=True)
+    close(g.x[:, -300:, -64:], h.x[:, -300:].cpu().double())
+    close(g.weight[-64:], h.weight.cpu().double())
+    del g, y
+    A = -torch.rand(ch, 2, generator=gen, device="cuda") - 0.5
+    B, C = (torch.randn(1, rows, 2, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    y, last = pkg.state_scan(u, u, A, B, C, softplus=True)
+    want, want_last = pkg.state_scan(part, part, A[-64:].contiguous(), B, C, softplus=True)
+    close(y[:, -300:, -64:], want[:, -300:].cpu().double())
+    close(last[:, -64:], want_last.cpu().double())
+    del u, y
+    entries, ch, n = 140000, 1024, 16
+    assert entries * ch * n > 2 ** 31
+    cache = torch.zeros(entries, ch, n, device="cuda")
+    small = torch.zeros(2, ch, n, device="cuda")
+    s = cuda(scan_inputs(torch.float32, (2, 1, ch), n, 1, None))
+    args = [s[k][:, 0] if s[k].dim() > 2 else s[k] for k in SCAN[:5]]
+    slots = torch.tensor([entries - 1, entries - 2], dtype=torch.int32, device="cuda")
+    for _ in range(2):
+        got = pkg.state_scan_step(*args, cache, softplus=True, slots=slots)
+        want = pkg.state_scan_step(*args, small, softplus=True)
+        assert torch.equal(got, want)
+    assert torch.equal(cache[slots.long()], small) and not cache[:-2].any()
