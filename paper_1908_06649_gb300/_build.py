@@ -24,7 +24,7 @@ SEQ_UNITS = ["short_conv.cu", "state_scan.cu", "state_scan_f32.cu",
              "state_scan_bf16.cu", "state_scan_f16.cu"]
 HEADERS = ["tcgen05.cuh", "group_kernel.cuh", "launch.h",
            "launch_impl.cuh", "host_plan.h", "seq_common.cuh",
-           "state_scan.cuh", "state_scan_impl.cuh"]
+           "seq_index.h", "state_scan.cuh", "state_scan_impl.cuh"]
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 HDR = os.path.join(INCLUDE, "tcu_dft.h")
 SEQ_HDR = os.path.join(INCLUDE, "tcu_seq.h")

@@ -43,6 +43,7 @@
 #include <algorithm>
 
 #include "seq_common.cuh"
+#include "seq_index.h"
 #include "tcgen05.cuh"
 
 namespace tcu {
@@ -92,7 +93,7 @@ struct Place {
     c0 = (int64_t)g * a.per_group + cb * DB;
     nc = min(DB, a.per_group - cb * DB);
     r0 = (int)k * a.chunk_rows;
-    r1 = min(r0 + a.chunk_rows, a.rows);
+    r1 = chunk_end(r0, a.chunk_rows, a.rows);
   }
 };
 
@@ -671,7 +672,7 @@ __global__ void carry_kernel(ScanArgs<T> a) {
       for (int j = 0; j < 4; ++j) {
         if (j0 + j >= a.chunks) break;
         const int k = kBack ? a.chunks - 1 - (j0 + j) : j0 + j;
-        const int r0 = k * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
+        const int r0 = k * a.chunk_rows, r1 = chunk_end(r0, a.chunk_rows, a.rows);
         // does a sequence open (close, going back) within the chunk?
         bool cut;
         if (kBack) cut = r1 == a.rows || (a.row_seq && a.row_seq[r0] != a.row_seq[r1]);
