@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include "../../include/tcu_seq.h"
+#include "seq_index.h"
 
 namespace tcu {
 namespace seq {
@@ -207,18 +208,6 @@ struct Rows {
     return p + b * batch + (int64_t)t * row;
   }
 };
-
-// The sequence that holds row t of a packed tensor: the last s with
-// offsets[s] <= t < offsets[s + 1], -1 if t is in none (values out of order
-// still give -1 <= s < count).
-__device__ __forceinline__ int sequence_of(const int32_t *offsets, int count, int t) {
-  int lo = 0, hi = count;  // offsets[lo] <= t unless lo == 0
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (offsets[mid + 1] <= t) lo = mid + 1; else hi = mid;
-  }
-  return lo < count && offsets[lo] <= t ? lo : -1;
-}
 
 // ------------------------------------------------------------- host side
 inline int type_size(int type) { return type == TCU_SEQ_F32 ? 4 : 2; }

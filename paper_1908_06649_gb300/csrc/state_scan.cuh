@@ -43,7 +43,6 @@
 #include <algorithm>
 
 #include "seq_common.cuh"
-#include "seq_index.h"
 #include "tcgen05.cuh"
 
 namespace tcu {

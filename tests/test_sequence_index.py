@@ -52,3 +52,48 @@ int main(int, char **argv) {
 def test_chunks_cover_the_rows(run, rows):
     out = run(CHUNKS)(rows)
     assert out.returncode == 0, out
+
+
+SEQUENCES = r"""
+#include <sys/mman.h>
+// `count` sequences, all empty but the last, which holds every row.  Pages that
+// stay untouched read as zeros.
+int main(int, char **argv) {
+  const int count = atoi(argv[1]), rows = 100;
+  const size_t bytes = ((size_t)count + 1) * 4;
+  void *mem = mmap(nullptr, bytes, PROT_READ | PROT_WRITE,
+                   MAP_PRIVATE | MAP_ANONYMOUS | MAP_NORESERVE, -1, 0);
+  if (mem == MAP_FAILED) return 3;
+  int32_t *offsets = (int32_t *)mem;
+  offsets[count] = rows;
+  for (int t = 0; t < rows; ++t)
+    if (sequence_of(offsets, count, t) != count - 1) return 1;
+  return sequence_of(offsets, count, 100) == -1 ? 0 : 2;
+}
+"""
+
+
+@pytest.mark.parametrize("count", [1, 2, 1000, 2 ** 30 + 5, 2 ** 31 - 1])
+def test_sequence_of_a_row_among_many(run, count):
+    out = run(SEQUENCES)(count)
+    assert out.returncode == 0, out
+
+
+ORDERS = r"""
+int main() {
+  const int32_t o[] = {0, 0, 3, 3, 7, 7};  // sequences 1 and 3 hold rows
+  const int want[] = {1, 1, 1, 3, 3, 3, 3, -1};
+  for (int t = 0; t < 8; ++t)
+    if (sequence_of(o, 5, t) != want[t]) return 1;
+  if (sequence_of(o, 0, 0) != -1) return 2;
+  const int32_t odd[] = {50, 10, 50, -5, 200};
+  for (int t = 0; t < 300; ++t)
+    if (sequence_of(odd, 4, t) < -1 || sequence_of(odd, 4, t) > 3) return 3;
+  return 0;
+}
+"""
+
+
+def test_sequence_of_a_row(run):
+    out = run(ORDERS)()
+    assert out.returncode == 0, out
