@@ -36,9 +36,10 @@
  * Calls are asynchronous on `stream` (a cudaStream_t), allocate nothing, and
  * return a TCU_DFT_* status: ERR_INVALID (sizes, null pointers, alignment of
  * a pointer to its element, workspace too small), ERR_UNSUPPORTED (width or
- * states beyond the limits, more than 2^31 - 4097 rows, a row stride, or a
- * single-token call's batch stride, beyond 32 bits), ERR_CUDA.  On an argument
- * error nothing is launched.  Outputs must not overlap inputs.
+ * states beyond the limits, more than 2^31 - 4097 rows, a row stride beyond 32
+ * bits; a single-token scan's batch stride beyond 32 bits, or more than
+ * 2^31 - 262141 entries), ERR_CUDA.  On an argument error nothing is launched.
+ * Outputs must not overlap inputs.
  */
 #ifndef TCU_SEQ_H
 #define TCU_SEQ_H

@@ -144,6 +144,7 @@ extern "C" int tcu_state_scan_step(const tcu_state_scan_args *a, void *stream) {
   if (a->rows != 1 || a->offsets || a->num_slots < 0 ||
       (!a->slots && a->num_slots < a->sequences) || !opt_ok(a->slots, 4))
     return TCU_DFT_ERR_INVALID;
+  if (a->sequences > kMostEntries) return TCU_DFT_ERR_UNSUPPORTED;
   for (const tcu_seq_rows *r : {&a->u, &a->dt, &a->gate, &a->y, &a->B, &a->C})
     if (r->batch_stride > INT32_MAX || r->batch_stride < INT32_MIN) return TCU_DFT_ERR_UNSUPPORTED;
   if (a->sequences == 0) return TCU_DFT_OK;

@@ -689,6 +689,10 @@ __global__ void carry_kernel(ScanArgs<T> a) {
 // the gate) is done for one entry by each NB-th part of the lanes.  512 entries x
 // 4096 channels x 16 states: 53 us, 5.4 TB/s; one entry at a time, with that
 // work in every lane, 83 us.
+//
+// Up to 65535 blocks below each other step by NB <= 4 entries each, counted in
+// 32 bits: kMostEntries leaves room for the step past the last one.
+constexpr int kMostEntries = INT32_MAX - 4 * 65535;
 template <typename T, int LS, int NB, bool kWide>
 __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(ScanArgs<T> a) {
   constexpr int kShare = LS / NB;  // lanes of a channel for one entry's values

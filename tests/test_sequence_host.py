@@ -189,3 +189,11 @@ def test_reference_conv_by_hand():
     w = torch.tensor([[10.0, 1.0]], dtype=torch.float64)
     y, last = ref.conv(x, w, state=torch.tensor([[[5.0]]], dtype=torch.float64))
     assert y.flatten().tolist() == [51.0, 12.0, 23.0] and last.item() == 3.0
+
+
+def test_token_scan_of_too_many_entries(seq):
+    """Entries are counted in 32 bits, in steps of up to four for each of 65535
+    blocks: beyond 2^31 - 1 - 4 * 65535 a step past the last one would wrap."""
+    for n in (2 ** 31 - 4 * 65535, 2 ** 31 - 1):
+        a = scan_args(seq, rows=1, sequences=n, slots=0x10000, num_slots=1)
+        assert seq._lib().tcu_state_scan_step(a, None) == UNSUPPORTED
