@@ -39,7 +39,8 @@
  * states beyond the limits, more than 2^31 - 4097 rows, a row stride beyond 32
  * bits; a single-token scan's batch stride beyond 32 bits, or more than
  * 2^31 - 262141 entries), ERR_CUDA.  On an argument error nothing is launched.
- * Outputs must not overlap inputs.
+ * Outputs must not overlap inputs or themselves; y of a single-token call may
+ * be its x, u, dt or gate, with the same strides.
  */
 #ifndef TCU_SEQ_H
 #define TCU_SEQ_H

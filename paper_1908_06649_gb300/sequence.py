@@ -7,7 +7,9 @@ length, channels) -- or packed: (rows, channels) with ``offsets``, an int32
 CUDA tensor of sequences + 1 row numbers from 0 to rows.  Any strides over
 batch and rows are taken as they are (a slice of a wider projection needs no
 copy); channels must be adjacent.  Parameters and the scan's states are
-float32.  Everything runs on torch's current stream, or on ``stream``.
+float32.  Everything runs on torch's current stream, or on ``stream``.  ``out``
+shares memory neither with an input nor with itself; only a single-token call
+may write over a row that it reads (x; u, dt or gate), all of it.
 
 ``short_conv`` and ``state_scan`` are differentiable: where a gradient is
 asked of an argument they record themselves with autograd.  The ``_grad``
@@ -241,26 +243,77 @@ def _adjacent(t):
     return t if t.shape[-1] == 1 or t.stride(-1) == 1 else t.contiguous()
 
 
-def _apart(out, others):
-    """Refuses an output that shares elements with an input."""
-    size = out.element_size()
+def _memory(t):
+    """Where the elements of t lie, in bytes: (first, [(count - 1, stride)] of the
+    dimensions that are not one run, length of a run)."""
+    size = t.element_size()
+    run, outer = size, []
+    for n, st in sorted(zip(t.shape, t.stride()), key=lambda d: d[1]):
+        if n == 1:
+            continue
+        if st * size == run and not outer:
+            run *= n
+        else:
+            outer.append((n - 1, st * size))
+    return t.data_ptr(), outer, run
 
-    def span(t):
-        return t.data_ptr(), t.data_ptr() + size * (
-            1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
 
-    for t in others:
-        if t is None or not t.numel() or not out.numel():
-            continue
-        (a, b), (c, d) = span(out), span(t)
-        if b <= c or d <= a:
-            continue
-        # columns of one wider tensor: apart if their columns are
-        row, ch = out.stride()[-2], out.shape[-1]
-        at = (a - c) // size % row if row else 0
-        if t.stride()[:-1] == out.stride()[:-1] and ch <= at <= row - ch:
-            continue
-        raise ValueError("out must not overlap an input")
+def _hits(terms, lo, hi, tries):
+    """Whether a sum of x_k c_k over terms (m_k, c_k), 0 <= x_k <= m_k, falls
+    into [lo, hi]: exact, from the largest c down, for layouts that nest two or
+    three tries a term.  True where it takes more tries than are left."""
+    terms = [t for t in terms if t[0] and t[1]]
+    if not terms:
+        return lo <= 0 <= hi
+    (m, c), rest = terms[0], terms[1:]
+    reach = sum(n * s for n, s in rest)
+    for x in range(max(0, -((reach - lo) // c)), min(m, hi // c) + 1):
+        tries[0] -= 1
+        if not rest or tries[0] < 0 or _hits(rest, lo - x * c, hi - x * c, tries):
+            return True
+    return False
+
+
+def _overlap(one, two):
+    """Whether two layouts share a byte."""
+    (a, over_a, run_a), (b, over_b, run_b) = one, two
+    top = b + sum(m * c for m, c in over_b)  # the second's runs, counted down from its last
+    if top + run_b <= a or a + sum(m * c for m, c in over_a) + run_a <= b:
+        return False
+    steps = {}
+    for m, c in over_a + over_b:
+        steps[c] = steps.get(c, 0) + m
+    terms = sorted(((m, c) for c, m in steps.items()), key=lambda t: -t[1])
+    return _hits(terms, top - a - run_a + 1, top - a + run_b - 1, [1 << 16])
+
+
+def _overlaps_itself(one):
+    """Whether two elements of a layout share a byte."""
+    _, outer, run = one
+    outer = sorted(outer, key=lambda t: -t[1])
+    for k, (m, c) in enumerate(outer):
+        rest = outer[k + 1:]  # at least one step of this dimension, any of the rest
+        base = c - sum(n * s for n, s in rest)
+        if _hits([(m - 1, c)] + [(2 * n, s) for n, s in rest], 1 - run - base, run - 1 - base,
+                 [1 << 16]):
+            return True
+    return False
+
+
+def _apart(out, inputs, in_place=()):
+    """Refuses an output that shares memory with an input or with itself; one of
+    in_place may be the output."""
+    if not out.numel():
+        return
+    to = _memory(out)
+    if _overlaps_itself(to):
+        raise ValueError("out must not overlap itself")
+    for t in in_place:
+        if t is not None and _memory(t) != to and _overlap(to, _memory(t)):
+            raise ValueError("out must be an input or not overlap it")
+    for t in inputs:
+        if t is not None and t.numel() and _overlap(to, _memory(t)):
+            raise ValueError("out must not overlap an input")
 
 
 def _workspace(name, packed, device):
@@ -292,7 +345,7 @@ def _conv(x, weight, bias, silu, state, offsets, out, stream):
         last = torch.empty(tail, dtype=dtype, device=x.device)
         py = _rows(y, "out", dtype, index, x.shape)
         if out is not None:
-            _apart(out, (x, state))
+            _apart(out, (x, weight, bias, state, offsets))
         if ch:
             _call("tcu_short_conv", _CONV.pack(
                 _TYPES[dtype], width, bool(silu), seqs, rows, ch, off, *px, *py, *_NO_ROWS,
@@ -385,6 +438,8 @@ def short_conv_step(x, state, weight, bias=None, *, silu=False, slots=None, out=
     with _On(index, stream) as st:
         y = torch.empty((batch, ch), dtype=dtype, device=x.device) if out is None else out
         py = _rows(y, "out", dtype, index, x.shape)
+        if out is not None:
+            _apart(out, (state, weight, bias, slots), in_place=(x,))
         if ch:
             _call("tcu_short_conv_step", _CONV.pack(
                 _TYPES[dtype], width, bool(silu), batch, 1, ch, 0, px[0], px[2], 0, py[0], py[2],
@@ -446,7 +501,7 @@ def _scan(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets, marks, 
         last = torch.empty(c.tail, dtype=f32, device=dev)
         py = _rows(y, "out", c.dtype, c.index, u.shape)
         if out is not None:
-            _apart(out, (u, dt, gate))
+            _apart(out, (u, dt, A, B, C, skip, gate, dt_bias, state, offsets))
         kept = torch.empty(c.marks, dtype=f32, device=dev) if marks else None
 
         def packed(work, size):
@@ -571,6 +626,8 @@ def state_scan_step(u, dt, A, B, C, state, *, skip=None, gate=None, dt_bias=None
     with _On(index, stream) as st:
         y = torch.empty((batch, ch), dtype=dtype, device=u.device) if out is None else out
         py = _rows(y, "out", dtype, index, shape)
+        if out is not None:
+            _apart(out, (A, B, C, state, skip, dt_bias, slots), in_place=(u, dt, gate))
         if ch:
             _call("tcu_state_scan_step", _SCAN.pack(
                 _TYPES[dtype], bool(softplus), batch, groups, 1, ch, states, 0,
