@@ -35,10 +35,11 @@
  *
  * Calls are asynchronous on `stream` (a cudaStream_t), allocate nothing, and
  * return a TCU_DFT_* status: ERR_INVALID (sizes, null pointers, alignment of
- * a pointer to its element, workspace too small), ERR_UNSUPPORTED (width or
- * states beyond the limits, more than 2^31 - 4097 rows, a row stride beyond 32
- * bits; a single-token scan's batch stride beyond 32 bits, or more than
- * 2^31 - 262141 entries), ERR_CUDA.  On an argument error nothing is launched.
+ * a pointer to its element, workspace too small, a single-token call's cache
+ * over another argument), ERR_UNSUPPORTED (width or states beyond the limits,
+ * more than 2^31 - 4097 rows, a row stride beyond 32 bits; a single-token
+ * scan's batch stride beyond 32 bits, or more than 2^31 - 262141 entries),
+ * ERR_CUDA.  On an argument error nothing is launched.
  * Outputs must not overlap inputs or themselves; y of a single-token call may
  * be its x, u, dt or gate, with the same strides.
  */

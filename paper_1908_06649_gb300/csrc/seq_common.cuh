@@ -233,6 +233,20 @@ inline bool row_fits(const tcu_seq_rows &r) {
 inline bool f32_ok(const void *p) { return p && (uintptr_t)p % 4 == 0; }
 inline bool opt_ok(const void *p, int size) { return (uintptr_t)p % size == 0; }
 
+// Whether the `bytes` at p, advanced in place, share one with `count` rows of
+// `run` bytes at q, `stride` bytes apart (of any size: these are the caller's).
+using wide_int = __int128;
+inline bool over(const void *p, wide_int bytes, const void *q, int64_t run, int64_t count = 1,
+                 int64_t stride = 0) {
+  if (!p || !q || bytes <= 0 || run <= 0 || count <= 0) return false;
+  const wide_int lo = (wide_int)(uintptr_t)p, hi = lo + bytes;
+  wide_int a = (wide_int)(uintptr_t)q, s = count > 1 ? stride : 0;
+  if (s < 0) a += s * (count - 1), s = -s;
+  // the first row that ends behind lo
+  const wide_int k = a + run > lo || s == 0 ? 0 : (lo - run - a) / s + 1;
+  return k < count && a + k * s < hi && a + k * s + run > lo;
+}
+
 inline int launched() {
   return cudaGetLastError() == cudaSuccess ? TCU_DFT_OK : TCU_DFT_ERR_CUDA;
 }

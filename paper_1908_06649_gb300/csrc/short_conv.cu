@@ -628,5 +628,13 @@ extern "C" int tcu_short_conv_step(const tcu_short_conv_args *a, void *stream) {
       (!row_ok(a->x, sz) || !row_ok(a->y, sz) ||
        (a->width > 1 && a->num_slots > 0 && (!a->last || (uintptr_t)a->last % sz))))
     return TCU_DFT_ERR_INVALID;
+  const wide_int cache = (wide_int)a->num_slots * (a->width - 1) * a->channels * sz;
+  for (const tcu_seq_rows *r : {&a->x, &a->y})
+    if (over(a->last, cache, r->ptr, a->channels * sz, a->sequences, r->batch_stride * sz))
+      return TCU_DFT_ERR_INVALID;
+  if (over(a->last, cache, a->weight, a->channels * a->width * 4) ||
+      over(a->last, cache, a->bias, a->channels * 4) ||
+      over(a->last, cache, a->slots, (int64_t)a->sequences * 4))
+    return TCU_DFT_ERR_INVALID;
   return by_type(kStep, *a, static_cast<cudaStream_t>(stream));
 }

@@ -150,5 +150,17 @@ extern "C" int tcu_state_scan_step(const tcu_state_scan_args *a, void *stream) {
   if (a->sequences == 0) return TCU_DFT_OK;
   if (!inputs_ok(*a) || !row_ok(a->y, type_size(a->type)) || (a->num_slots > 0 && !a->last))
     return TCU_DFT_ERR_INVALID;
+  const int64_t entry = a->channels * a->states * 4;
+  const wide_int cache = (wide_int)a->num_slots * entry;
+  const int64_t row = a->channels * type_size(a->type);
+  const int64_t coefficients = a->groups * a->states * type_size(a->type);
+  for (const tcu_seq_rows *r : {&a->u, &a->dt, &a->gate, &a->B, &a->C, &a->y})
+    if (over(a->last, cache, r->ptr, r == &a->B || r == &a->C ? coefficients : row, a->sequences,
+             r->batch_stride * type_size(a->type)))
+      return TCU_DFT_ERR_INVALID;
+  if (over(a->last, cache, a->A, entry) || over(a->last, cache, a->skip, a->channels * 4) ||
+      over(a->last, cache, a->dt_bias, a->channels * 4) ||
+      over(a->last, cache, a->slots, (int64_t)a->sequences * 4))
+    return TCU_DFT_ERR_INVALID;
   return by_type(kScanStep, *a, stream);
 }

@@ -150,3 +150,49 @@ def test_outputs_of_tokens(seq):
     for to in (past.view(-1)[:b * c].view(b, c), wide[1:, :c]):
         with pytest.raises(ValueError):
             seq.short_conv_step(wide[:b, :c], past, w, out=to)
+
+
+@pytest.mark.gpu
+def test_caches_over_other_arguments(seq):
+    """A cache that a token call advances shares memory with no other argument;
+    it may lie between the rows of one."""
+    from paper_1908_06649_gb300 import TcuDftError
+    b, c, n = 3, 16, 8
+    size = b * c * n
+    arena = torch.randn(8 * size, device="cuda")
+    ok = dict(u=torch.randn(b, c, device="cuda"), dt=torch.randn(b, c, device="cuda"),
+              A=-torch.rand(c, n, device="cuda"), B=torch.randn(b, n, device="cuda"),
+              C=torch.randn(b, n, device="cuda"), gate=torch.randn(b, c, device="cuda"),
+              skip=torch.randn(c, device="cuda"), dt_bias=torch.randn(c, device="cuda"),
+              slots=torch.arange(b, device="cuda").int())
+
+    def scan(cache, **change):
+        v = dict(ok, **change)
+        return seq.state_scan_step(*[v.pop(k) for k in "u dt A B C".split()], cache, **v)
+
+    def at(first, like):
+        return arena[first:first + like.numel()].view(like.shape)
+
+    first = arena[size:2 * size].view(b, c, n)
+    start = first.clone()
+    want = scan(start.clone())
+    for k, v in ok.items():
+        for where in (size - v.numel() + 1, size + 8, 2 * size - 1):
+            t = at(where, v) if k != "slots" else arena.view(torch.int32)[where:where + b]
+            with pytest.raises(TcuDftError):
+                scan(first, **{k: t})
+        t = at(2 * size, v) if k != "slots" else arena.view(torch.int32)[2 * size:2 * size + b]
+        t.copy_(v)
+        cache = arena[size:2 * size].view(b, c, n).copy_(start)
+        assert torch.equal(scan(cache, **{k: t}), want), k
+    # between the first and the second row of u
+    apart = arena[:b * 2 * size].view(b, 2 * size)[:, :c].copy_(ok["u"])
+    cache = arena[c:c + size].view(b, c, n).copy_(start)
+    assert torch.equal(scan(cache, u=apart), want)
+    with pytest.raises(TcuDftError):
+        scan(arena[2 * size - size + 1:2 * size + 1].view(b, c, n), u=apart)
+    x, w = torch.randn(b, c, device="cuda"), torch.randn(c, W, device="cuda")
+    past = arena[:b * (W - 1) * c].view(b, W - 1, c)
+    for x1, w1 in ((at(past.numel() - 1, x), w), (x, at(past.numel() - 1, w))):
+        with pytest.raises(TcuDftError):
+            seq.short_conv_step(x1, past, w1)
