@@ -597,6 +597,9 @@ def state_scan_grad(dy, u, dt, A, B, C, *, marks, skip=None, gate=None, dt_bias=
             work, n = _workspace("tcu_state_scan_grad_workspace", packed(0, 0), dev)
             _call("tcu_state_scan_grad", packed(ptr(work), n), st)
             del work
+        else:  # sums over no channels
+            g.B.zero_()
+            g.C.zero_()
     return g
 
 
