@@ -239,6 +239,13 @@ def _no_grad(*tensors):
         raise ValueError("the single-token calls have no gradient")
 
 
+def _written(t):
+    """A call has written t in place: operations that saved it for their
+    backward pass find its version changed (inference tensors have none)."""
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 def _adjacent(t):
     return t if t.shape[-1] == 1 or t.stride(-1) == 1 else t.contiguous()
 
@@ -350,6 +357,8 @@ def _conv(x, weight, bias, silu, state, offsets, out, stream):
             _call("tcu_short_conv", _CONV.pack(
                 _TYPES[dtype], width, bool(silu), seqs, rows, ch, off, *px, *py, *_NO_ROWS,
                 *_NO_ROWS, pw, pb, ps, 0, last.data_ptr(), 0, 0, 0, 0, 0, 0, 0), st)
+        if out is not None:
+            _written(out)
     return y, last
 
 
@@ -383,6 +392,8 @@ def short_conv(x, weight, bias=None, *, silu=False, state=None, offsets=None, ou
         if out is not None or stream is not None:
             raise ValueError("out and stream cannot be given where a gradient is asked")
         return _ShortConv.apply(x, weight, bias, state, silu, offsets)
+    if _wants_grad(out):
+        raise ValueError("out must not record a gradient")
     return _conv(x, weight, bias, silu, state, offsets, out, stream)
 
 
@@ -428,7 +439,7 @@ def short_conv_step(x, state, weight, bias=None, *, silu=False, slots=None, out=
     _tensor(x, "x")
     if x.dim() != 2 or x.dtype not in _TYPES or not x.is_cuda:
         raise ValueError("x must be a float32, bfloat16 or float16 CUDA tensor (batch, channels)")
-    _no_grad(x, weight, bias)
+    _no_grad(x, state, weight, bias, out)
     batch, ch = x.shape
     width, dtype, index = _width(weight), x.dtype, x.get_device()
     cache, entries, ps = _cache(state, slots, batch, (width - 1, ch), dtype, index)
@@ -444,6 +455,9 @@ def short_conv_step(x, state, weight, bias=None, *, silu=False, slots=None, out=
             _call("tcu_short_conv_step", _CONV.pack(
                 _TYPES[dtype], width, bool(silu), batch, 1, ch, 0, px[0], px[2], 0, py[0], py[2],
                 0, *_NO_ROWS, *_NO_ROWS, pw, pb, 0, 0, cache, 0, 0, 0, 0, 0, ps, entries), st)
+        _written(state)
+        if out is not None:
+            _written(out)
     return y
 
 
@@ -512,6 +526,8 @@ def _scan(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets, marks, 
             work, n = _workspace("tcu_state_scan_workspace", packed(0, 0), dev)
             _call("tcu_state_scan", packed(work.data_ptr() if n else 0, n), st)
             del work
+        if out is not None:
+            _written(out)
     return y, last, kept
 
 
@@ -554,6 +570,8 @@ def state_scan(u, dt, A, B, C, *, skip=None, gate=None, dt_bias=None, softplus=F
         if out is not None or marks or stream is not None:
             raise ValueError("out, marks and stream cannot be given where a gradient is asked")
         return _StateScan.apply(u, dt, A, B, C, skip, gate, dt_bias, state, softplus, offsets)
+    if _wants_grad(out):
+        raise ValueError("out must not record a gradient")
     y, last, kept = _scan(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets, marks,
                           out, stream)
     return (y, last, kept) if marks else (y, last)
@@ -613,7 +631,7 @@ def state_scan_step(u, dt, A, B, C, state, *, skip=None, gate=None, dt_bias=None
     _tensor(u, "u")
     if u.dim() != 2 or u.dtype not in _TYPES or not u.is_cuda:
         raise ValueError("u must be a float32, bfloat16 or float16 CUDA tensor (batch, channels)")
-    _no_grad(u, dt, A, B, C, skip, gate, dt_bias)
+    _no_grad(u, dt, A, B, C, state, skip, gate, dt_bias, out)
     batch, ch = shape = u.shape
     B, C = _grouped(B, "B", u), _grouped(C, "C", u)
     groups, states = _groups(B, ch)
@@ -637,4 +655,7 @@ def state_scan_step(u, dt, A, B, C, state, *, skip=None, gate=None, dt_bias=None
                 pu[0], pu[2], 0, pd[0], pd[2], 0, pz[0], pz[2], 0, py[0], py[2], 0,
                 pB[0], pB[2], 0, pC[0], pC[2], 0, pA, pk, pi, 0, 0, cache, 0, 0, *_NO_GRADS,
                 0, 0, ps, entries), st)
+        _written(state)
+        if out is not None:
+            _written(out)
     return y

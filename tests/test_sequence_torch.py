@@ -37,3 +37,59 @@ def test_gradients_of_no_channels_are_zeros(seq, packed):
     g = seq.state_scan_grad(u, u, u, A, B, C, marks=marks, offsets=off)
     assert g.B.shape == B.shape and (g.B == 0).all() and (g.C == 0).all()
     assert g.u.shape == u.shape and g.A.shape == A.shape
+
+
+@pytest.mark.gpu
+def test_caches_that_record_a_gradient(seq):
+    """A token call has no gradient: a cache or an output that would need one is
+    refused, as every other argument is; under no_grad it is advanced."""
+    a, state = tokens()
+    w, x = torch.randn(16, 4, device="cuda"), a["u"]
+    _, past = seq.short_conv(torch.randn(4, 6, 16, device="cuda"), w.clone().requires_grad_())
+    assert past.requires_grad
+    with pytest.raises(ValueError):
+        seq.short_conv_step(x, past, w)
+    with pytest.raises(ValueError):
+        seq.state_scan_step(**a, state=state.clone().requires_grad_())
+    for make in (lambda out: seq.short_conv_step(x, past.detach().clone(), w, out=out),
+                 lambda out: seq.state_scan_step(**a, state=state.clone(), out=out),
+                 lambda out: seq.short_conv(x[None], w, out=out[None]),
+                 lambda out: seq.state_scan(x[None], a["dt"][None], a["A"], a["B"][None],
+                                            a["C"][None], out=out[None])):
+        with pytest.raises(ValueError):
+            make(torch.zeros_like(x).requires_grad_())
+        with torch.no_grad():
+            make(torch.zeros_like(x).requires_grad_())
+    with torch.no_grad():
+        before = past.clone()
+        seq.short_conv_step(x, past, w)
+        assert torch.equal(past[:, :2], before[:, 1:]) and torch.equal(past[:, 2], x)
+
+
+@pytest.mark.gpu
+def test_writes_in_place_are_known_to_autograd(seq):
+    """What an operation has saved for its backward pass may not change under it:
+    as torch's own in-place operations, the calls raise the tensor's version."""
+    a, state = tokens()
+    w, x = torch.randn(16, 4, device="cuda"), a["u"]
+    past = torch.randn(4, 3, 16, device="cuda")
+    prompt = (x[None], a["dt"][None], a["A"], a["B"][None], a["C"][None])
+    out = torch.zeros_like(x)
+    for t, call in ((past, lambda: seq.short_conv_step(x, past, w)),
+                    (state, lambda: seq.state_scan_step(**a, state=state)),
+                    (out, lambda: seq.short_conv_step(x, past, w, out=out)),
+                    (out, lambda: seq.state_scan_step(**a, state=state, out=out)),
+                    (out, lambda: seq.short_conv(x[None], w, out=out[None])),
+                    (out, lambda: seq.state_scan(*prompt, out=out[None]))):
+        p = torch.ones_like(t).requires_grad_()
+        loss = (p * t).sum()  # saves t
+        seen = t._version
+        call()
+        assert t._version > seen
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    # inference tensors have no version, and serve as before
+    with torch.inference_mode():
+        cache, to = state.clone(), torch.zeros_like(x)
+        seq.state_scan_step(**a, state=cache, out=to)
+    seq.state_scan_step(**a, state=cache, out=to)
