@@ -93,3 +93,59 @@ def test_writes_in_place_are_known_to_autograd(seq):
         cache, to = state.clone(), torch.zeros_like(x)
         seq.state_scan_step(**a, state=cache, out=to)
     seq.state_scan_step(**a, state=cache, out=to)
+
+
+def every_call(seq, a, state, wrap):
+    """(argument, call) for each argument of each call, wrapped alone."""
+    x, w = a["u"], torch.randn(16, 4, device=a["u"].device)
+    past = torch.randn(4, 3, 16, device=x.device)
+    rows = {k: v[None] if k in ("u", "dt", "B", "C") else v for k, v in a.items()}
+    marks = torch.zeros(1, 1, 16, 8, device=x.device)
+    own = state[:1]
+
+    def with_one(call, args):
+        for k in args:
+            if args[k] is not None:
+                yield k, lambda k=k: call(**dict(args, **{k: wrap(args[k])}))
+
+    yield from with_one(seq.short_conv, dict(x=x[None], weight=w, state=past[:1]))
+    yield from with_one(seq.short_conv_grad,
+                        dict(dy=x[None], x=x[None], weight=w, state=past[:1], dlast=past[:1]))
+    yield from with_one(seq.short_conv_step, dict(x=x, state=past, weight=w))
+    yield from with_one(seq.state_scan, dict(rows, gate=rows["u"], state=own))
+    yield from with_one(seq.state_scan_grad, dict(rows, dy=rows["u"], marks=marks, gate=rows["u"],
+                                                  state=own, dlast=own))
+    yield from with_one(seq.state_scan_step, dict(a, state=state, gate=a["u"]))
+
+
+def forward_mode(seq, a, state):
+    from torch.autograd import forward_ad
+    with forward_ad.dual_level():
+        count = 0
+        for k, call in every_call(seq, a, state,
+                                  lambda t: forward_ad.make_dual(t, torch.ones_like(t))):
+            with pytest.raises(ValueError, match="forward-mode"):
+                call()
+            count += 1
+    assert count > 30
+    return count
+
+
+def test_forward_mode_is_refused(seq):
+    """Before anything else is looked at, the device included."""
+    gen = torch.Generator().manual_seed(0)
+    r = lambda *s: torch.randn(*s, generator=gen)  # noqa: E731
+    forward_mode(seq, dict(u=r(4, 16), dt=r(4, 16), A=-r(16, 8).abs(), B=r(4, 8), C=r(4, 8)),
+                 r(4, 16, 8))
+
+
+@pytest.mark.gpu
+def test_forward_mode_on_the_gpu(seq):
+    """A tangent would be lost without a word; without one, a dual level is
+    nothing to the calls."""
+    from torch.autograd import forward_ad
+    a, state = tokens()
+    forward_mode(seq, a, state)
+    want = seq.state_scan_step(**a, state=state.clone())
+    with forward_ad.dual_level():
+        assert torch.equal(seq.state_scan_step(**a, state=state.clone()), want)
