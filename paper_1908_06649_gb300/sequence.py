@@ -124,6 +124,8 @@ class _On:
         self.stream = stream
         self.index = index
         self.guards = ()
+        if stream is not None and stream.device.index != index:
+            raise ValueError("stream is of %s, the tensors are on cuda:%d" % (stream.device, index))
         if stream is not None or index != _current_device():
             self.guards = [torch.cuda.device(index)]
             if stream is not None:

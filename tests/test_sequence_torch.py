@@ -149,3 +149,36 @@ def test_forward_mode_on_the_gpu(seq):
     want = seq.state_scan_step(**a, state=state.clone())
     with forward_ad.dual_level():
         assert torch.equal(seq.state_scan_step(**a, state=state.clone()), want)
+
+
+class FakeStream:
+    cuda_stream = 0
+
+    def __init__(self, index):
+        self.device = torch.device("cuda", index)
+
+
+def test_a_stream_of_another_device_is_refused(seq):
+    """Its kernels would start on that device, on memory of this one.  Nothing
+    is entered or launched: no GPU is needed to be refused."""
+    with pytest.raises(ValueError, match="cuda:1"):
+        seq._On(0, FakeStream(1))
+    seq._On(1, FakeStream(1))
+
+
+@pytest.mark.gpu
+def test_a_stream_of_another_device_is_refused_by_every_call(seq):
+    a, state = tokens()
+    x, w, other = a["u"], torch.randn(16, 4, device="cuda"), FakeStream(1)
+    rows = [a[k][None] if k != "A" else a[k] for k in ("u", "dt", "A", "B", "C")]
+    marks = seq.state_scan(*rows, marks=True)[2]
+    before = state.clone()
+    for call in (lambda: seq.short_conv(x[None], w, stream=other),
+                 lambda: seq.short_conv_grad(x[None], x[None], w, stream=other),
+                 lambda: seq.short_conv_step(x, torch.zeros(4, 3, 16, device="cuda"), w, stream=other),
+                 lambda: seq.state_scan(*rows, stream=other),
+                 lambda: seq.state_scan_grad(x[None], *rows, marks=marks, stream=other),
+                 lambda: seq.state_scan_step(**a, state=state, stream=other)):
+        with pytest.raises(ValueError, match="cuda:1"):
+            call()
+    assert torch.equal(state, before) and torch.cuda.current_device() == 0
