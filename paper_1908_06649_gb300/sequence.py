@@ -19,6 +19,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
+import threading
 from collections import namedtuple
 
 import torch
@@ -83,21 +84,27 @@ _NO_ROWS = (0, 0, 0)
 
 _bound = None
 _calls = {}
+_binding = threading.Lock()
 
 
 def _lib():
-    global _bound
+    global _bound, _calls
     if _bound is None:
-        L = lib()
-        for name in SYMBOLS:
-            f = getattr(L, name)
-            args = ctypes.POINTER(_ConvArgs if "conv" in name else _ScanArgs)
-            f.argtypes = [args] if name.endswith("workspace") else [args, _vp]
-            f.restype = _i64 if name.endswith("workspace") else ctypes.c_int
-            f = _calls[name] = L[name]  # the same entry, for packed arguments
-            f.argtypes = [ctypes.c_char_p] if name.endswith("workspace") else [ctypes.c_char_p, _vp]
-            f.restype = _i64 if name.endswith("workspace") else ctypes.c_int
-        _bound = L
+        with _binding:
+            if _bound is None:
+                L, calls = lib(), {}
+                for name in SYMBOLS:
+                    f = getattr(L, name)
+                    args = ctypes.POINTER(_ConvArgs if "conv" in name else _ScanArgs)
+                    f.argtypes = [args] if name.endswith("workspace") else [args, _vp]
+                    f.restype = _i64 if name.endswith("workspace") else ctypes.c_int
+                    f = calls[name] = L[name]  # the same entry, for packed arguments
+                    f.argtypes = ([ctypes.c_char_p] if name.endswith("workspace")
+                                  else [ctypes.c_char_p, _vp])
+                    f.restype = _i64 if name.endswith("workspace") else ctypes.c_int
+                # published whole: other threads look entries up without the lock
+                _calls = calls
+                _bound = L
     return _bound
 
 

@@ -1,7 +1,7 @@
 """The sequence operators as citizens of torch: no channels, in-place writes
 that autograd has to know of, forward mode, streams, first use by threads."""
 import threading
-import types
+import threading
 
 import pytest
 import torch
@@ -182,3 +182,61 @@ def test_a_stream_of_another_device_is_refused_by_every_call(seq):
         with pytest.raises(ValueError, match="cuda:1"):
             call()
     assert torch.equal(state, before) and torch.cuda.current_device() == 0
+
+
+def test_entries_are_published_with_their_types(seq, monkeypatch):
+    """A second thread whose first call falls into the binding finds either no
+    entry or a finished one: an entry without types takes a stream's address
+    for a 32-bit number.  Here the other thread looks after every step of it."""
+    class Entry:
+        def __init__(self):
+            self.__dict__["types"] = set()
+
+        def __setattr__(self, name, value):
+            look()
+            self.types.add(name)
+            look()
+
+    class Library:
+        def __init__(self):
+            self.named = {}
+
+        def __getattr__(self, name):
+            if not name.startswith("tcu_"):
+                raise AttributeError(name)
+            return self.named.setdefault(name, Entry())
+
+        def __getitem__(self, name):
+            return Entry()
+
+    def look():
+        for name, f in dict(seq._calls).items():
+            assert f.types == {"argtypes", "restype"}, name
+
+    monkeypatch.setattr(seq, "_bound", None)
+    monkeypatch.setattr(seq, "_calls", {})
+    monkeypatch.setattr(seq, "lib", Library)
+    first = seq._lib()
+    look()
+    assert sorted(seq._calls) == sorted(seq.SYMBOLS) and seq._lib() is first
+
+
+def test_threads_share_one_binding(seq, monkeypatch):
+    real, made = seq.lib, []
+
+    def slow():
+        made.append(1)
+        started.wait(2)
+        return real()
+
+    started, got = threading.Event(), []
+    monkeypatch.setattr(seq, "_bound", None)
+    monkeypatch.setattr(seq, "_calls", {})
+    monkeypatch.setattr(seq, "lib", slow)
+    threads = [threading.Thread(target=lambda: got.append(seq._lib())) for _ in range(4)]
+    for t in threads:
+        t.start()
+    started.set()
+    for t in threads:
+        t.join()
+    assert len(made) == 1 and len(got) == 4 and all(g is got[0] for g in got)
