@@ -1,7 +1,6 @@
 """The sequence operators as citizens of torch: no channels, in-place writes
 that autograd has to know of, forward mode, streams, first use by threads."""
 import threading
-import threading
 
 import pytest
 import torch
