@@ -780,9 +780,14 @@ struct GradLay {
   static constexpr int kBC = kMark * NP;              // B or C of a tile
   static constexpr int kPairFloats = 2 * (3 * kPlane + 2 * kBC) + 2 * WC;
   static constexpr int kThreadFloats = 2 * E;         // a first warp's thread: mark, sum of dA
-  static constexpr int kFloats = 4 + 4 * kBC + kPairs * (kPairFloats + 32 * kThreadFloats);
+  static constexpr int kLaneFloats = 2 * V;           // a second warp's: sums of dskip, dbias
+  static constexpr int kLanesAt = 4 + 4 * kBC + kPairs * (kPairFloats + 32 * kThreadFloats);
+  static constexpr int kFloats = kLanesAt + kPairs * 32 * kLaneFloats;
 };
-constexpr int kFlush = 8;  // tiles whose shares of dA are summed before they join the rest
+// Tiles whose shares of dA, dskip and dbias are summed before they join the
+// rest: a thread's rows in one fp32 chain would lose a bit every time their
+// number grows fourfold (2^17 rows of equal terms: 1.6e-4 off, 1e-5 so).
+constexpr int kFlush = 8;
 constexpr int grad_channels(int ls) { return 4 * (32 / ls) * scan_ch(ls); }
 constexpr int grad_resident(int ls) { return ls <= 8 ? 2 : 1; }
 
@@ -837,6 +842,19 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
     float2 dskip[V / 2], dbias[V / 2];
 #pragma unroll
     for (int v = 0; v < V / 2; ++v) dskip[v] = dbias[v] = make_float2(0.f, 0.f);
+    // their sums over earlier tiles, this lane's alone
+    float4 *sums = reinterpret_cast<float4 *>(smem + L::kLanesAt) + pair * 32 * (V / 2) + lane;
+#pragma unroll
+    for (int v = 0; v < V / 2; ++v) sums[32 * v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto flush = [&]() {
+#pragma unroll
+      for (int v = 0; v < V / 2; ++v) {
+        const float4 s = sums[32 * v];
+        sums[32 * v] = make_float4(s.x + dskip[v].x, s.y + dskip[v].y, s.z + dbias[v].x,
+                                   s.w + dbias[v].y);
+        dskip[v] = dbias[v] = make_float2(0.f, 0.f);
+      }
+    };
     struct In {
       Raw<T, V, !kWide> u, dt, z, dy;
     };
@@ -966,6 +984,7 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
         if (to < 0 && i > 0) finish(in[j % 2], i - 1, pass);
         if (to > 0 && i + 1 < tiles) stage(in[j % 2], i + 1, pass);
       }
+      if (i % kFlush == 0) flush();
       if (i > 0) share_bc(i - 1);
       if (i + 1 < tiles) stage_bc(i + 1);
       pu -= (int64_t)kMark * a.u.row;
@@ -975,8 +994,11 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
       __syncthreads();
     }
     // a channel's shares lie in the lanes of its column
+    flush();
 #pragma unroll
     for (int k = 0; k < V / 2; ++k) {
+      const float4 sum = sums[32 * k];
+      dskip[k] = make_float2(sum.x, sum.y), dbias[k] = make_float2(sum.z, sum.w);
 #pragma unroll
       for (int s = L::COLS; s < 32; s *= 2) {
         dskip[k].x += __shfl_xor_sync(~0u, dskip[k].x, s);

@@ -36,3 +36,24 @@ def test_as_many_rows_as_there_can_be(pkg):
     part = 2 ** 28
     for first in range(64, rows, part):
         assert (y[first:first + part] == steady).all()
+
+
+def test_long_sums_of_parameter_gradients(pkg):
+    """Gradients of skip and dt_bias over 2^17 rows that are not split (160
+    sequences fill the card), all terms the same 0.7: a decay of e^-1000 leaves
+    q u = 0.7 of each row for the one, (C q B) u for the other.  A lane's sum goes
+    in two levels, 16 terms and then their 1024 sums; three exchanges between
+    lanes and 28 steps over sequences follow.  Each step rounds by 2^-24 at most."""
+    rows, seqs = 2 ** 17, 160
+    one = torch.ones(1, 1, 1, device="cuda").expand(seqs, rows, 1)
+    u = torch.full((1, 1, 1), 0.7, device="cuda").expand(seqs, rows, 1)
+    A = torch.full((1, 1), -1000.0, device="cuda")
+    skip, bias = torch.ones(1, device="cuda"), torch.zeros(1, device="cuda")
+    BC = one.unsqueeze(-1)
+    _, _, marks = pkg.state_scan(u, one, A, BC, BC, skip=skip, dt_bias=bias, marks=True)
+    g = pkg.state_scan_grad(one, u, one, A, BC, BC, skip=skip, dt_bias=bias, marks=marks)
+    want = float(u[0, 0, 0].double()) * rows * seqs
+    bound = (16 + rows // 128 + 3 + 28) * 2.0 ** -24 * want
+    assert abs(float(g.skip) - want) <= bound
+    assert abs(float(g.dt_bias) - want) <= bound
+    assert float(g.A) == 0 and (g.dt == u).all() and (g.B == u[..., None]).all()
