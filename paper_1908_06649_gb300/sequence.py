@@ -251,18 +251,21 @@ def _no_grad(*tensors):
 
 
 def _no_tangent(*tensors):
-    """Refuses forward-mode dual tensors, whose tangents a call would drop."""
-    if _forward._current_level >= 0:
-        for t in tensors:
-            if isinstance(t, torch.Tensor) and _forward.unpack_dual(t).tangent is not None:
-                raise ValueError("the sequence operators have no forward-mode derivative")
+    """Refuses forward-mode dual tensors, whose tangents a call would drop.
+    Called where a dual level is open."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and _forward.unpack_dual(t).tangent is not None:
+            raise ValueError("the sequence operators have no forward-mode derivative")
+
+
+_raise_version = torch.autograd.graph.increment_version
 
 
 def _written(t):
     """A call has written t in place: operations that saved it for their
     backward pass find its version changed (inference tensors have none)."""
     if not t.is_inference():
-        torch.autograd.graph.increment_version(t)
+        _raise_version(t)
 
 
 def _adjacent(t):
@@ -407,7 +410,8 @@ def short_conv(x, weight, bias=None, *, silu=False, state=None, offsets=None, ou
     channels), of x's type, holds the rows before each sequence (zeros if
     None).  Returns (y, last), last being the state that a continuation takes.
     """
-    _no_tangent(x, weight, bias, state, out)
+    if _forward._current_level >= 0:
+        _no_tangent(x, weight, bias, state, out)
     if _wants_grad(x, weight, bias, state):
         if out is not None or stream is not None:
             raise ValueError("out and stream cannot be given where a gradient is asked")
@@ -421,7 +425,8 @@ def short_conv_grad(dy, x, weight, bias=None, *, silu=False, state=None, offsets
                     dlast=None, stream=None):
     """Gradients of short_conv's (y, last) under dy and dlast (zeros if None):
     ConvGrads(x, weight, bias, state), the last two None where the argument is."""
-    _no_tangent(dy, x, weight, bias, state, dlast)
+    if _forward._current_level >= 0:
+        _no_tangent(dy, x, weight, bias, state, dlast)
     seqs, rows, ch, off = _layout(x, "x", offsets)
     width, dtype, index, dev = _width(weight), x.dtype, x.get_device(), x.device
     tail, f32 = (seqs, width - 1, ch), torch.float32
@@ -457,7 +462,8 @@ def short_conv_step(x, state, weight, bias=None, *, silu=False, slots=None, out=
     ``state`` (entries, width - 1, channels) is advanced in place, at entry
     slots[b] (int32) for row b, or entry b.  A slot outside the cache gives a
     row of zeros; no two rows may name the same one."""
-    _no_tangent(x, state, weight, bias, out)
+    if _forward._current_level >= 0:
+        _no_tangent(x, state, weight, bias, out)
     _tensor(x, "x")
     if x.dim() != 2 or x.dtype not in _TYPES or not x.is_cuda:
         raise ValueError("x must be a float32, bfloat16 or float16 CUDA tensor (batch, channels)")
@@ -588,7 +594,8 @@ def state_scan(u, dt, A, B, C, *, skip=None, gate=None, dt_bias=None, softplus=F
     Returns (y, last), last being the state that a continuation takes; with
     ``marks`` also the states that state_scan_grad resumes from.
     """
-    _no_tangent(u, dt, A, B, C, skip, gate, dt_bias, state, out)
+    if _forward._current_level >= 0:
+        _no_tangent(u, dt, A, B, C, skip, gate, dt_bias, state, out)
     if _wants_grad(u, dt, A, B, C, skip, gate, dt_bias, state):
         if out is not None or marks or stream is not None:
             raise ValueError("out, marks and stream cannot be given where a gradient is asked")
@@ -605,7 +612,8 @@ def state_scan_grad(dy, u, dt, A, B, C, *, marks, skip=None, gate=None, dt_bias=
     """Gradients of state_scan's (y, last) under dy and dlast (zeros if None),
     from the marks that state_scan kept of the same arguments: ScanGrads(u, dt,
     A, B, C, skip, gate, dt_bias, state), None where the argument is."""
-    _no_tangent(dy, u, dt, A, B, C, marks, skip, gate, dt_bias, state, dlast)
+    if _forward._current_level >= 0:
+        _no_tangent(dy, u, dt, A, B, C, marks, skip, gate, dt_bias, state, dlast)
     c = _ScanCall(u, dt, A, B, C, skip, gate, dt_bias, softplus, state, offsets)
     f32, dev, dtype, index, shape = torch.float32, u.device, c.dtype, c.index, u.shape
     pdy = _rows(dy, "dy", dtype, index, shape)
@@ -652,7 +660,8 @@ def state_scan_step(u, dt, A, B, C, state, *, skip=None, gate=None, dt_bias=None
     ``state`` (entries, channels, states) is advanced in place, at entry
     slots[b] (int32) for row b, or entry b.  A slot outside the cache gives a
     row of zeros; no two rows may name the same one."""
-    _no_tangent(u, dt, A, B, C, state, skip, gate, dt_bias, out)
+    if _forward._current_level >= 0:
+        _no_tangent(u, dt, A, B, C, state, skip, gate, dt_bias, out)
     _tensor(u, "u")
     if u.dim() != 2 or u.dtype not in _TYPES or not u.is_cuda:
         raise ValueError("u must be a float32, bfloat16 or float16 CUDA tensor (batch, channels)")
