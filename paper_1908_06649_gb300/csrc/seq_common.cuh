@@ -203,7 +203,7 @@ template <typename T>
 struct Rows {
   T *p;
   int64_t batch;
-  int32_t row;  // one 32-bit product for a row's address (row_fits)
+  int32_t row;  // one 32-bit product for a row's address (pitch_fits)
   __device__ __forceinline__ T *at(int64_t b, int32_t t) const {
     return p + b * batch + (int64_t)t * row;
   }
@@ -225,10 +225,11 @@ inline bool rows_aligned(const tcu_seq_rows &r, int type, int64_t batches, int64
 inline bool row_ok(const tcu_seq_rows &r, int size) {
   return r.ptr && (uintptr_t)r.ptr % size == 0;
 }
-// Rows, and a row's pitch, within 32 bits, with room to step past the end.
+// Rows, and the pitch of `rows` rows, within 32 bits, with room to step past
+// the end (one row's pitch is never taken, whatever it is cut to).
 constexpr int64_t kMostRows = INT32_MAX - 4096;
-inline bool row_fits(const tcu_seq_rows &r) {
-  return r.row_stride >= INT32_MIN && r.row_stride <= INT32_MAX;
+inline bool pitch_fits(int64_t rows, int64_t stride) {
+  return rows <= 1 || (stride >= INT32_MIN && stride <= INT32_MAX);
 }
 inline bool f32_ok(const void *p) { return p && (uintptr_t)p % 4 == 0; }
 inline bool opt_ok(const void *p, int size) { return (uintptr_t)p % size == 0; }

@@ -478,9 +478,10 @@ int check_sizes(const tcu_short_conv_args *a) {
   if (!a || a->type < TCU_SEQ_F32 || a->type > TCU_SEQ_F16 || a->sequences < 0 || a->rows < 0 ||
       a->channels < 1 || a->width < 1)
     return TCU_DFT_ERR_INVALID;
-  if (a->width > TCU_SEQ_MAX_WIDTH || a->rows > kMostRows || a->channels > INT32_MAX ||
-      !row_fits(a->x) || !row_fits(a->y) || !row_fits(a->dy) || !row_fits(a->dx))
+  if (a->width > TCU_SEQ_MAX_WIDTH || a->rows > kMostRows || a->channels > INT32_MAX)
     return TCU_DFT_ERR_UNSUPPORTED;
+  for (const tcu_seq_rows *r : {&a->x, &a->y, &a->dy, &a->dx})
+    if (!pitch_fits(a->rows, r->row_stride)) return TCU_DFT_ERR_UNSUPPORTED;
   return TCU_DFT_OK;
 }
 

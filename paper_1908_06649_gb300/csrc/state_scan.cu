@@ -62,7 +62,7 @@ int check_sizes(const tcu_state_scan_args *a) {
     return TCU_DFT_ERR_UNSUPPORTED;
   for (const tcu_seq_rows *r : {&a->u, &a->dt, &a->gate, &a->y, &a->B, &a->C, &a->dy, &a->du,
                                 &a->ddt, &a->dgate, &a->dB, &a->dC})
-    if (!row_fits(*r)) return TCU_DFT_ERR_UNSUPPORTED;
+    if (!pitch_fits(a->rows, r->row_stride)) return TCU_DFT_ERR_UNSUPPORTED;
   return TCU_DFT_OK;
 }
 
@@ -146,7 +146,7 @@ extern "C" int tcu_state_scan_step(const tcu_state_scan_args *a, void *stream) {
     return TCU_DFT_ERR_INVALID;
   if (a->sequences > kMostEntries) return TCU_DFT_ERR_UNSUPPORTED;
   for (const tcu_seq_rows *r : {&a->u, &a->dt, &a->gate, &a->y, &a->B, &a->C})
-    if (r->batch_stride > INT32_MAX || r->batch_stride < INT32_MIN) return TCU_DFT_ERR_UNSUPPORTED;
+    if (!pitch_fits(a->sequences, r->batch_stride)) return TCU_DFT_ERR_UNSUPPORTED;
   if (a->sequences == 0) return TCU_DFT_OK;
   if (!inputs_ok(*a) || !row_ok(a->y, type_size(a->type)) || (a->num_slots > 0 && !a->last))
     return TCU_DFT_ERR_INVALID;

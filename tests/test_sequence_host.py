@@ -197,3 +197,14 @@ def test_token_scan_of_too_many_entries(seq):
     for n in (2 ** 31 - 4 * 65535, 2 ** 31 - 1):
         a = scan_args(seq, rows=1, sequences=n, slots=0x10000, num_slots=1)
         assert seq._lib().tcu_state_scan_step(a, None) == UNSUPPORTED
+
+
+def test_pitches_beyond_32_bits_are_refused(seq):
+    far = seq._Rows(0x10000, 2 ** 33, 2 ** 31)
+    for k in ("x", "y", "dy", "dx"):
+        assert seq._lib().tcu_short_conv(conv_args(seq, **{k: far}), None) == UNSUPPORTED
+    for k in ("u", "dt", "gate", "y", "B", "C", "dB"):
+        assert seq._lib().tcu_state_scan(scan_args(seq, **{k: far}), None) == UNSUPPORTED
+    for k in ("u", "dt", "gate", "y", "B", "C"):
+        a = scan_args(seq, rows=1, slots=0x10000, num_slots=1, **{k: far})
+        assert seq._lib().tcu_state_scan_step(a, None) == UNSUPPORTED

@@ -57,3 +57,36 @@ def test_long_sums_of_parameter_gradients(pkg):
     assert abs(float(g.skip) - want) <= bound
     assert abs(float(g.dt_bias) - want) <= bound
     assert float(g.A) == 0 and (g.dt == u).all() and (g.B == u[..., None]).all()
+
+
+def test_strides_that_step_over_nothing(pkg):
+    """One row, or one entry of a token call, may lie at any pitch: it is never
+    taken a step.  (The token of one long sequence is a slice of this kind.)"""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    c, n, far = 40, 16, 2 ** 33 + 8
+    randn = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    u, dt, gate = randn(1, 1, c), randn(1, 1, c), randn(1, 1, c)
+    A, B, C, w = -randn(c, n).abs(), randn(1, 1, 1, n), randn(1, 1, 1, n), randn(c, 4)
+    apart = lambda t: t.as_strided(t.shape, (far, far) + t.stride()[2:])  # noqa: E731
+    state, past = randn(1, c, n), randn(1, 3, c)
+
+    def scan(f):
+        args = f(u), f(dt), A, f(B), f(C)
+        y, last, marks = pkg.state_scan(*args, gate=f(gate), state=state, marks=True)
+        g = pkg.state_scan_grad(f(u), *args, gate=f(gate), state=state, marks=marks)
+        return [y, last] + [v for v in g if v is not None]
+
+    def conv(f):
+        g = pkg.short_conv_grad(f(dt), f(u), w, state=past)
+        return list(pkg.short_conv(f(u), w, state=past)) + [v for v in g if v is not None]
+
+    def token(f):
+        cache, rows = state.clone(), past.clone()
+        one = lambda t: f(t)[:, 0]  # noqa: E731
+        y = pkg.state_scan_step(one(u), one(dt), A, one(B), one(C), cache, gate=one(gate),
+                                out=f(torch.empty_like(u))[:, 0])
+        return [y, cache, pkg.short_conv_step(one(u), rows, w), rows]
+
+    for call in (scan, conv, token):
+        for got, want in zip(call(apart), call(lambda t: t)):
+            assert torch.equal(got, want)
