@@ -38,8 +38,8 @@
  * a pointer to its element, workspace too small, a single-token call's cache
  * over another argument), ERR_UNSUPPORTED (width or states beyond the limits,
  * more than 2^31 - 4097 rows, a row stride beyond 32 bits; a single-token
- * scan's batch stride beyond 32 bits, or more than 2^31 - 262141 entries),
- * ERR_CUDA.  On an argument error nothing is launched.
+ * scan's batch stride beyond 32 bits, or more than 2^31 - 262141 entries; more
+ * than 4,194,240 channels of a convolution; a grid of 2^31 blocks), ERR_CUDA.  On an argument error nothing is launched.
  * Outputs must not overlap inputs or themselves; y of a single-token call may
  * be its x, u, dt or gate, with the same strides.
  */
@@ -126,6 +126,8 @@ int64_t tcu_state_scan_workspace(const tcu_state_scan_args *a);
 /* dy, marks and the scan's inputs -> du, ddt, dA, dB, dC [, dskip, dgate,
  * ddt_bias, dstate], through workspace. */
 int tcu_state_scan_grad(const tcu_state_scan_args *a, void *stream);
+/* Mostly shares of dB and dC, 1 byte for each row and channel at 16 states, 4
+ * at 32, 16 at 64 and 64 at 128. */
 int64_t tcu_state_scan_grad_workspace(const tcu_state_scan_args *a);
 /* One row per sequence (rows = 1, dense): u, dt, B, C -> y, and the cache
  * `last` (num_slots x channels x states) advanced in place; slots as for

@@ -2,8 +2,9 @@
 
 The library is a dozen translation units compiled in parallel -- the host
 plan/ABI units and the kernel units (one per radix, mixed radix, BF16, the
-element-wise grid kernels) -- linked into one shared object; the
-bounds-checked variant is the same sources with -DTCU_DFT_CHECKED.
+element-wise grid kernels, the sequence operators) -- linked into one shared
+object; in the bounds-checked variant the DFT's units are compiled with
+-DTCU_DFT_CHECKED.
 """
 from __future__ import annotations
 
@@ -18,8 +19,8 @@ UNITS = ["tcu_dft.cu", "host_tables.cu", "noalloc.cu", "grid_plan.cu",
          "kernels_mixed_r8.cu", "kernels_mixed_r16.cu", "kernels_mixed_r32.cu",
          "kernels_bf16_r8.cu", "kernels_bf16_r16.cu", "kernels_bf16_r32.cu",
          "grid_kernels.cu"]
-# the sequence operators: no index checks of their own, so both variants link
-# the same objects
+# the sequence operators have no bounds-checked form: both variants link the
+# same objects
 SEQ_UNITS = ["short_conv.cu", "state_scan.cu", "state_scan_f32.cu",
              "state_scan_bf16.cu", "state_scan_f16.cu"]
 HEADERS = ["tcgen05.cuh", "group_kernel.cuh", "launch.h",

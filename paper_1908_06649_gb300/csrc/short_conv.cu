@@ -41,7 +41,8 @@ struct ConvArgs {
 };
 
 // A block: 32 threads along the channels, kItems items (runs, or batch
-// entries) below each other.  No division by a size of the call.
+// entries) below each other.  A prompt's thread divides by a size of the call
+// once, to find its run.
 constexpr int kItems = 4;
 constexpr int kThreads = 32 * kItems;
 constexpr int kBlockRows = 8;
@@ -459,7 +460,7 @@ struct Shape {
   int blocks;  // of kBlockRows rows in a run
 };
 
-// Runs as long as eight blocks, so that few rows are read twice and few shares
+// Runs of up to 16 blocks of rows, so that few rows are read twice and few shares
 // of dw written, but short enough to give every SM its 1024 threads.
 Shape shape_of(const tcu_short_conv_args &a, int values) {
   Shape s;
@@ -471,7 +472,7 @@ Shape shape_of(const tcu_short_conv_args &a, int values) {
   return s;
 }
 
-// Values a thread of the gradient owns: rows in words of 8 or 16 bytes.
+// Values a thread of the gradient owns: rows in words of 4 or 8 bytes.
 constexpr int kGradValues = 2;
 
 int check_sizes(const tcu_short_conv_args *a) {

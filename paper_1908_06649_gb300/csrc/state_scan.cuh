@@ -762,9 +762,9 @@ __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(ScanArgs<T> a) 
 // d u, q for the next tile and the sums o, r, v (in their places) into du,
 // ddt, dgate for the one before.  Two blocks fill an SM and its tensor memory.
 //
-// Measured at 8 x 2048 rows x 4096 channels x 16 states, bf16: 1220 us, of which
-// the first warps alone take 1000: 285 of the 383 instructions a row and warp,
-// at 60 % of the issue slots.  FMA pipe alone: 360 us.  States kept every fourth
+// Measured at 8 x 2048 rows x 4096 channels x 16 states, bf16: 1224 us, of which
+// the first warps alone take 1000: three quarters of the 380 instructions a row
+// and warp, at 59 % of the issue slots.  FMA pipe alone: 360 us.  States kept every fourth
 // row in shared memory and recomputed twice instead of once: 3960 us.
 template <int LS_, typename T>
 struct GradLay {
@@ -1220,8 +1220,11 @@ __global__ void __launch_bounds__(256, grad_resident(LS)) scan_grad_kernel(ScanA
 }
 
 // dB and dC from the channel blocks' shares, in order: a block takes as many
-// rows as fit its threads, blockIdx.y the batch entries.  Shares are one fp32
-// value for 128 channels' two bytes, written and read once.
+// rows as fit its threads, blockIdx.y the batch entries.  A block's share is an
+// fp32 value for each state of dB and of dC, written and read once, for the 128
+// channels that it covers up to 16 states, 64, 32 and 16 up to 32, 64 and 128: 8
+// bytes times states / channels for each row and channel, 1 at 16 states and 64
+// at 128, where they are most of the gradient's traffic.
 constexpr int kSumThreads = 256;  // at least the values of a row and group: 2 * 128
 template <typename T>
 __global__ void __launch_bounds__(kSumThreads) sum_bc_kernel(ScanArgs<T> a) {

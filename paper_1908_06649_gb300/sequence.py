@@ -7,7 +7,9 @@ length, channels) -- or packed: (rows, channels) with ``offsets``, an int32
 CUDA tensor of sequences + 1 row numbers from 0 to rows.  Any strides over
 batch and rows are taken as they are (a slice of a wider projection needs no
 copy); channels must be adjacent.  Parameters and the scan's states are
-float32.  Everything runs on torch's current stream, or on ``stream``.  ``out``
+float32.  Everything runs on torch's current stream, or on ``stream``; ordering
+that against other streams that use the tensors (wait_stream, record_stream) is
+the caller's, as for any torch operation.  ``out``
 shares memory neither with an input nor with itself; only a single-token call
 may write over a row that it reads (x; u, dt or gate), all of it.
 
