@@ -331,19 +331,31 @@ def _overlaps_itself(one):
     return False
 
 
+def _span(t):
+    """The first byte of t's memory, and the first beyond it."""
+    first = t.data_ptr()
+    if t.is_contiguous():
+        return first, first + t.numel() * t.element_size()
+    return first, first + t.element_size() * (
+        1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+
 def _apart(out, inputs, in_place=()):
     """Refuses an output that shares memory with an input or with itself; one of
     in_place may be the output."""
     if not out.numel():
         return
-    to = _memory(out)
-    if _overlaps_itself(to):
+    if not out.is_contiguous() and _overlaps_itself(_memory(out)):
         raise ValueError("out must not overlap itself")
-    for t in in_place:
-        if t is not None and _memory(t) != to and _overlap(to, _memory(t)):
-            raise ValueError("out must be an input or not overlap it")
-    for t in inputs:
-        if t is not None and t.numel() and _overlap(to, _memory(t)):
+    lo, hi = _span(out)
+    for i, t in enumerate(in_place + inputs):
+        if t is None or not t.numel():
+            continue
+        a, b = _span(t)
+        if hi <= a or b <= lo:  # nearly always
+            continue
+        one, to = _memory(t), _memory(out)
+        if _overlap(to, one) and not (i < len(in_place) and one == to):
             raise ValueError("out must not overlap an input")
 
 
