@@ -357,7 +357,9 @@ def _plain_gated(s):
 
     x, open_f, open_a = rows(s["x"]), torch.sigmoid(rows(s["forget"])), torch.sigmoid(rows(s["admit"]))
     log = -rate * open_f
-    a, root = torch.exp(log), torch.sqrt(-torch.expm1(2 * log))
+    # decays near one in 64 bits: a recurrence of many rows multiplies their mean error
+    a = torch.exp(log.double()).float()
+    root = torch.sqrt(-torch.expm1(2 * log))
     new = root * open_a * x
     if dense:
         if s["state"] is not None:
