@@ -1,7 +1,7 @@
 /*
  * tcu_seq.h -- C ABI of the sequence operators of libtcu_dft.so: a short
- * causal convolution and a selective state-space scan, each over whole
- * prompts, with its gradient, and for one token.
+ * causal convolution, a selective state-space scan and a gated linear
+ * recurrence, each over whole prompts, with its gradient, and for one token.
  *
  * The 2-D convolutions and stencils of tcu_dft.h mix positions with weights
  * that are the same everywhere, so a DFT diagonalises them.  The scan's decay
@@ -14,9 +14,11 @@
  *                h_t[n] = exp(d_t A[n]) h_{t-1}[n] + d_t u_t B_t[n]
  *                o_t = sum_n C_t[n] h_t[n] + skip u_t
  *                y_t = o_t g_t sigma(g_t) with a gate, else o_t
+ *   recurrence   a_t = exp(-rate sigma(forget_t))
+ *                h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigma(admit_t) x_t,  y_t = h_t
  * per sequence and channel, sigma(v) = 1 / (1 + exp(-v)).
  *
- * Layout.  Row tensors (x, u, dt, gate, y, their gradients) hold one row of
+ * Layout.  Row tensors (x, u, dt, gate, forget, admit, y, their gradients) hold one row of
  * `channels` adjacent values per position; B and C one row of groups x states
  * adjacent values, group g serving channels [g channels/groups, (g+1)
  * channels/groups).  Every row tensor has its own strides, in elements,
@@ -28,7 +30,8 @@
  * order give unspecified results, never an access out of range.
  *
  * Row tensors and the convolution's states are of one type (tcu_seq_type);
- * the scan's states, all parameters and their gradients are fp32.  Sums,
+ * the states of scan and recurrence, all parameters and their gradients are
+ * fp32.  Sums,
  * states and gradients are accumulated in fp32 and rounded once, on storing;
  * the same call gives the same bits every time.  Exponentials and reciprocals
  * are the special function unit's (2^-22 of the result).
@@ -41,7 +44,7 @@
  * scan's batch stride beyond 32 bits, or more than 2^31 - 262141 entries; more
  * than 4,194,240 channels of a convolution; a grid of 2^31 blocks), ERR_CUDA.  On an argument error nothing is launched.
  * Outputs must not overlap inputs or themselves; y of a single-token call may
- * be its x, u, dt or gate, with the same strides.
+ * be its x, u, dt, gate, forget or admit, with the same strides.
  */
 #ifndef TCU_SEQ_H
 #define TCU_SEQ_H
@@ -133,6 +136,41 @@ int64_t tcu_state_scan_grad_workspace(const tcu_state_scan_args *a);
  * `last` (num_slots x channels x states) advanced in place; slots as for
  * tcu_short_conv_step. */
 int tcu_state_scan_step(const tcu_state_scan_args *a, void *stream);
+
+/* Gated linear recurrence, one state a channel.  rate: channels, positive;
+ * state / last / dlast / dstate: sequences x channels (NULL state: zeros).
+ * marks: the state that enters every TCU_SEQ_GATED_MARK-th row, batch entries
+ * x ceil(rows / TCU_SEQ_GATED_MARK) x channels, as the scan's.  Rows behind
+ * the last packed sequence are left as they are in y, and their gradients are
+ * zeros. */
+enum { TCU_SEQ_GATED_MARK = 8 };
+typedef struct {
+  int32_t type, sequences;
+  int64_t rows, channels;
+  const int32_t *offsets;
+  tcu_seq_rows x, forget, admit, y;
+  const float *rate, *state, *dlast;
+  float *last, *dstate, *marks;
+  tcu_seq_rows dy, dx, dforget, dadmit;
+  float *drate;
+  void *workspace;
+  int64_t workspace_bytes;
+  const int32_t *slots;
+  int64_t num_slots;
+} tcu_gated_scan_args;
+
+/* x, forget, admit, rate [, state, offsets] -> y [, last, marks], through
+ * workspace. */
+int tcu_gated_scan(const tcu_gated_scan_args *a, void *stream);
+int64_t tcu_gated_scan_workspace(const tcu_gated_scan_args *a);
+/* dy, marks and the recurrence's inputs [, dlast] -> dx, dforget, dadmit,
+ * drate [, dstate], through workspace. */
+int tcu_gated_scan_grad(const tcu_gated_scan_args *a, void *stream);
+int64_t tcu_gated_scan_grad_workspace(const tcu_gated_scan_args *a);
+/* One row per sequence (rows = 1, dense): x, forget, admit -> y, and the cache
+ * `last` (num_slots x channels) advanced in place; slots as for
+ * tcu_short_conv_step. */
+int tcu_gated_scan_step(const tcu_gated_scan_args *a, void *stream);
 
 #ifdef __cplusplus
 }

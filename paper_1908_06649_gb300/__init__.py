@@ -453,7 +453,8 @@ class StencilPlan:
 # The sequence operators (sequence.py) under the package's own name, loaded
 # when first asked for: importing the package does not import torch.
 _SEQUENCE = ("short_conv", "short_conv_grad", "short_conv_step", "state_scan",
-             "state_scan_grad", "state_scan_step")
+             "state_scan_grad", "state_scan_step", "gated_scan", "gated_scan_grad",
+             "gated_scan_step")
 
 
 def __getattr__(name):

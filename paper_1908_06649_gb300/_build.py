@@ -22,7 +22,7 @@ UNITS = ["tcu_dft.cu", "host_tables.cu", "noalloc.cu", "grid_plan.cu",
 # the sequence operators have no bounds-checked form: both variants link the
 # same objects
 SEQ_UNITS = ["short_conv.cu", "state_scan.cu", "state_scan_f32.cu",
-             "state_scan_bf16.cu", "state_scan_f16.cu"]
+             "state_scan_bf16.cu", "state_scan_f16.cu", "gated_scan.cu"]
 HEADERS = ["tcgen05.cuh", "group_kernel.cuh", "launch.h",
            "launch_impl.cuh", "host_plan.h", "seq_common.cuh",
            "seq_index.h", "state_scan.cuh", "state_scan_impl.cuh"]

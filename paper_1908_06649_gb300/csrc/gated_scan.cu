@@ -1,0 +1,646 @@
+// gated_scan.cu -- the gated linear recurrence, its gradient and its
+// single-token form (include/tcu_seq.h).
+//
+// Per sequence and channel, s(v) = 1 / (1 + exp(-v)):
+//     L_t = -rate s(forget_t),   a_t = exp(L_t),   m_t = sqrt(1 - a_t^2)
+//     h_t = a_t h_{t-1} + m_t s(admit_t) x_t,      y_t = h_t
+//     e_t = dy_t + a_{t+1} e_{t+1}  (the gradient of h_t; dlast enters at the end)
+//     dx_t = e_t m_t s(admit_t),   dadmit_t = dx_t x_t (1 - s(admit_t))
+//     dL_t = a_t e_t h_{t-1} - (a_t^2 / m_t) e_t s(admit_t) x_t
+//     dforget_t = dL_t L_t (1 - s(forget_t)),   drate = sum_t dL_t L_t / rate
+//     dstate = a_1 e_1
+// Some thirty operations for each value and four rows of memory (eight with
+// the gradient): HBM bounds it if rows are read once and enough of them are on
+// their way, so the recurrence is cut along time.  A thread owns two channels
+// of a run of 8 rows, all of whose loads are in flight at once; 8 warps below
+// each other make a tile of 64 rows.  The rows of a run compose to one map
+// h -> A h + H, maps of runs compose through shared memory, maps of tiles
+// through the shared memory of a cluster of up to 16 blocks, and then the rows,
+// still in registers, are walked once more from the state that enters.  What
+// composes with what is fixed by the sizes: the same call gives the same bits.
+// The gradient walks the tiles from the end, forward within a run from the
+// state that the forward pass kept of it, and back.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "seq_common.cuh"
+
+namespace tcu {
+namespace seq {
+
+__global__ void row_sequence_kernel(int32_t *row_seq, const int32_t *offsets, int count,
+                                    int rows);
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kRun = TCU_SEQ_GATED_MARK;  // rows of a thread
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kTile = kRun * kWarps;  // rows of a block at a time
+constexpr int kStrip = 64;            // channels of a block
+constexpr int kMostCluster = 16;
+
+template <typename T>
+struct GatedArgs {
+  Rows<const T> x, forget, admit, dy;
+  Rows<T> y, dx, dforget, dadmit;
+  const float *rate, *state, *dlast;
+  float *last, *dstate, *marks, *parts;
+  const int32_t *offsets, *row_seq, *slots;
+  int64_t channels, num_slots;
+  int rows, sequences, batches, runs;
+};
+
+// exp(L) and exp(L)^2 - 1 for L <= 0.  1 - a^2 loses what a lacks in its last
+// place where a is near one, so exp(L) - 1 is a Taylor sum of degree 6 there
+// (L > -1/4: the next term is 5e-8 of it).
+struct Decay {
+  float2 a, m;  // a, sqrt(1 - a^2)
+};
+__device__ __forceinline__ float sqrt_fast(float v) {
+  float y;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v));
+  return y;
+}
+__device__ __forceinline__ float2 splat(float v) { return make_float2(v, v); }
+__device__ __forceinline__ Decay decay2(float2 L) {
+  float2 p = __ffma2_rn(L, splat(1.f / 720), splat(1.f / 120));
+  p = __ffma2_rn(p, L, splat(1.f / 24));
+  p = __ffma2_rn(p, L, splat(1.f / 6));
+  p = __ffma2_rn(p, L, splat(0.5f));
+  p = __ffma2_rn(p, L, splat(1.f));
+  p = __fmul2_rn(p, L);
+  const float2 z = __fmul2_rn(L, splat(kLog2e));
+  Decay d;
+  d.a = make_float2(exp2_fast(z.x), exp2_fast(z.y));
+  const float2 q = __fadd2_rn(d.a, splat(-1.f)), r = __fadd2_rn(p, splat(1.f));
+  const bool near0 = L.x > -0.25f, near1 = L.y > -0.25f;
+  const float2 em = make_float2(near0 ? p.x : q.x, near1 ? p.y : q.y);
+  d.a = make_float2(near0 ? r.x : d.a.x, near1 ? r.y : d.a.y);
+  const float2 room = __fmul2_rn(em, __fadd2_rn(em, splat(2.f)));  // a^2 - 1
+  d.m = make_float2(sqrt_fast(-room.x), sqrt_fast(-room.y));
+  return d;
+}
+
+// h -> A h + H of two channels.  A map that does not depend on h (a sequence
+// opens in it) drops even an h that is not finite.
+struct Map {
+  float2 A, H;
+};
+__device__ __forceinline__ float2 apply(const Map &m, float2 h) {
+  const float2 v = __ffma2_rn(m.A, h, m.H);
+  return make_float2(m.A.x == 0.f ? m.H.x : v.x, m.A.y == 0.f ? m.H.y : v.y);
+}
+// first then second
+__device__ __forceinline__ Map compose(const Map &first, const Map &second) {
+  const float2 A = __fmul2_rn(second.A, first.A);
+  return {make_float2(second.A.x == 0.f ? 0.f : A.x, second.A.y == 0.f ? 0.f : A.y),
+          apply(second, first.H)};
+}
+
+// Where sequences open and close in the 8 rows from r0 (bit i: row r0 + i),
+// which rows lie in one, and the sequence of row r0 + lane.
+struct Marks8 {
+  uint32_t open, close, inside;
+  int seq;
+};
+template <bool kPacked, typename T>
+__device__ __forceinline__ Marks8 sequences_of(const GatedArgs<T> &a, int b, int r0, int lane) {
+  Marks8 m;
+  if constexpr (kPacked) {
+    const int t = r0 - 1 + lane;  // r0 < rows <= 2^31 - 4097
+    const int v = lane < kRun + 2 && t >= 0 && t < a.rows ? a.row_seq[t] : -2;
+    m.seq = __shfl_down_sync(~0u, v, 1);
+    const int next = __shfl_down_sync(~0u, v, 2);
+    const bool in = lane < kRun && m.seq >= 0;
+    m.open = __ballot_sync(~0u, in && m.seq != v);
+    m.close = __ballot_sync(~0u, in && m.seq != next);
+    m.inside = __ballot_sync(~0u, in);
+  } else {
+    m.open = r0 == 0 ? 1u : 0u;
+    m.close = a.rows - 1 - r0 < kRun ? 1u << (a.rows - 1 - r0) : 0u;
+    m.inside = a.rows - r0 < kRun ? (1u << (a.rows - r0)) - 1u : (1u << kRun) - 1u;
+    m.seq = b;
+  }
+  return m;
+}
+
+// Two values of a per-sequence array at channel c (count of them exist).
+template <bool kWide>
+__device__ __forceinline__ float2 pair_at(const float *p, int64_t at, int count) {
+  if constexpr (kWide)
+    return count > 0 ? *reinterpret_cast<const float2 *>(p + at) : make_float2(0.f, 0.f);
+  return make_float2(count > 0 ? p[at] : 0.f, count > 1 ? p[at + 1] : 0.f);
+}
+template <bool kWide>
+__device__ __forceinline__ void put_pair(float *p, int64_t at, int count, float2 v) {
+  if constexpr (kWide) {
+    if (count > 0) *reinterpret_cast<float2 *>(p + at) = v;
+    return;
+  }
+  if (count > 0) p[at] = v.x;
+  if (count > 1) p[at + 1] = v.y;
+}
+
+// Composes the maps of the block's warps and of the cluster's blocks, in the
+// order of warps and blocks (kBack: from the last of either); takes the value
+// that enters the cluster's rows and gives that which enters this warp's, and
+// through `carry` that which leaves the cluster's.
+struct Joint {
+  Map warps[2][kWarps][32];
+  Map blocks[2][kMostCluster][32];
+};
+template <bool kBack>
+__device__ __forceinline__ float2 join(Joint &s, int turn, const Map &own, float2 &carry, int warp,
+                                       int lane, int rank, int size) {
+  s.warps[turn][warp][lane] = own;
+  __syncthreads();
+  Map before{splat(1.f), splat(0.f)}, all{splat(1.f), splat(0.f)};
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    const int w = kBack ? kWarps - 1 - i : i;
+    if (w == warp) before = all;
+    all = compose(all, s.warps[turn][w][lane]);
+  }
+  float2 enters = carry;
+  if (size == 1) {
+    carry = apply(all, carry);
+  } else {
+    const cg::cluster_group cluster = cg::this_cluster();
+    for (int r = warp; r < size; r += kWarps)
+      *cluster.map_shared_rank(&s.blocks[turn][rank][lane], r) = all;
+    cluster.sync();
+    for (int i = 0; i < size; ++i) {
+      const int r = kBack ? size - 1 - i : i;
+      if (r == rank) enters = carry;
+      carry = apply(s.blocks[turn][r][lane], carry);
+    }
+  }
+  return apply(before, enters);
+}
+
+// An empty sequence ends in the state it starts from.
+template <bool kWide, typename T>
+__device__ __forceinline__ void empty_sequences(const GatedArgs<T> &a, float *to, const float *from,
+                                                int64_t c, int count, int first, int step) {
+  for (int64_t s = first; s < a.sequences; s += step)
+    if (a.offsets[s] >= a.offsets[s + 1])
+      put_pair<kWide>(to, s * a.channels + c, count,
+               from ? pair_at<kWide>(from, s * a.channels + c, count) : splat(0.f));
+}
+
+template <typename T, bool kPacked, bool kWide>
+__global__ void __launch_bounds__(kThreads, 2) gated_kernel(const GatedArgs<T> a, int size) {
+  __shared__ Joint joint;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int rank = (int)(blockIdx.x % size);
+  const int64_t c = (int64_t)(blockIdx.x / size) * kStrip + 2 * lane;
+  const int count = (int)max((int64_t)0, min((int64_t)2, a.channels - c));
+  const float2 rate = pair_at<kWide>(a.rate, c, count);
+  int turn = 0;
+  for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
+    float2 carry = splat(0.f);
+    if (!kPacked && a.state) carry = pair_at<kWide>(a.state, (int64_t)b * a.channels + c, count);
+    for (int64_t t0 = 0; t0 < a.rows; t0 += (int64_t)size * kTile) {
+      const int64_t first = t0 + (int64_t)rank * kTile + warp * kRun;
+      const int r0 = (int)min(first, (int64_t)a.rows);
+      const int n = min(kRun, a.rows - r0);
+      Raw<T, 2> x[kRun], f[kRun], g[kRun];
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        const int has = i < n ? count : 0;
+        f[i].template load<kWide>(a.forget.at(b, r0 + i) + c, has);
+        g[i].template load<kWide>(a.admit.at(b, r0 + i) + c, has);
+        x[i].template load<kWide>(a.x.at(b, r0 + i) + c, has);
+      }
+      Marks8 seqs{};
+      if (n > 0) seqs = sequences_of<kPacked>(a, b, r0, lane);
+      float2 keep[kRun], add[kRun];
+      Map run{splat(1.f), splat(0.f)};
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        const Decay d = decay2(__fmul2_rn(sigmoid2(f[i].pair(0)), make_float2(-rate.x, -rate.y)));
+        const bool in = seqs.inside >> i & 1;  // others pass on what they get
+        keep[i] = in ? d.a : splat(1.f);
+        add[i] = in ? __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g[i].pair(0))), x[i].pair(0))
+                    : splat(0.f);
+        if (kPacked && (seqs.open >> i & 1)) {
+          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
+          run = {splat(0.f), a.state ? pair_at<kWide>(a.state, s * a.channels + c, count) : splat(0.f)};
+        }
+        run = {__fmul2_rn(run.A, keep[i]), __ffma2_rn(run.H, keep[i], add[i])};
+      }
+      float2 h = join<false>(joint, turn, run, carry, warp, lane, rank, size);
+      turn ^= 1;
+      if (n <= 0) continue;
+      if (a.marks)
+        put_pair<kWide>(a.marks, ((int64_t)b * a.runs + r0 / kRun) * a.channels + c, count, h);
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        if (kPacked && (seqs.open >> i & 1)) {
+          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
+          h = a.state ? pair_at<kWide>(a.state, s * a.channels + c, count) : splat(0.f);
+        }
+        h = __ffma2_rn(h, keep[i], add[i]);
+        if (seqs.inside >> i & 1) {
+          Raw<T, 2> y;
+          y.set(0, h);
+          y.template store<kWide>(a.y.at(b, r0 + i) + c, count);
+        }
+        if (seqs.close >> i & 1) {
+          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
+          if (a.last) put_pair<kWide>(a.last, s * a.channels + c, count, h);
+        }
+      }
+    }
+  }
+  if (kPacked && a.last && blockIdx.y == 0)
+    empty_sequences<kWide>(a, a.last, a.state, c, count, rank * kWarps + warp, size * kWarps);
+  if (size > 1) cg::this_cluster().sync();  // no block leaves while others write to it
+}
+
+template <typename T, bool kPacked, bool kWide>
+__global__ void __launch_bounds__(kThreads, 2) gated_grad_kernel(const GatedArgs<T> a, int size) {
+  __shared__ Joint joint;
+  __shared__ float2 sums[kWarps][32];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int rank = (int)(blockIdx.x % size);
+  const int64_t c = (int64_t)(blockIdx.x / size) * kStrip + 2 * lane;
+  const int count = (int)max((int64_t)0, min((int64_t)2, a.channels - c));
+  const float2 rate = pair_at<kWide>(a.rate, c, count);
+  const int64_t step = (int64_t)size * kTile;
+  float2 drate = splat(0.f);
+  int turn = 0;
+  for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
+    float2 carry = splat(0.f);  // a_{t+1} e_{t+1} of the row below
+    if (!kPacked && a.dlast) carry = pair_at<kWide>(a.dlast, (int64_t)b * a.channels + c, count);
+    for (int64_t t0 = (a.rows - 1) / step * step; t0 >= 0; t0 -= step) {
+      const int64_t first = t0 + (int64_t)rank * kTile + warp * kRun;
+      const int r0 = (int)min(first, (int64_t)a.rows);
+      const int n = min(kRun, a.rows - r0);
+      Raw<T, 2> x[kRun], f[kRun], g[kRun], dy[kRun];
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        const int has = i < n ? count : 0;
+        f[i].template load<kWide>(a.forget.at(b, r0 + i) + c, has);
+        dy[i].template load<kWide>(a.dy.at(b, r0 + i) + c, has);
+        g[i].template load<kWide>(a.admit.at(b, r0 + i) + c, has);
+        x[i].template load<kWide>(a.x.at(b, r0 + i) + c, has);
+      }
+      Marks8 seqs{};
+      float2 h = splat(0.f);
+      if (n > 0) {
+        seqs = sequences_of<kPacked>(a, b, r0, lane);
+        h = pair_at<kWide>(a.marks, ((int64_t)b * a.runs + r0 / kRun) * a.channels + c, count);
+      }
+      // forward: decays, open gates and the state before each row
+      float2 keep[kRun], root[kRun], before[kRun];
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        const float2 L = __fmul2_rn(sigmoid2(f[i].pair(0)), make_float2(-rate.x, -rate.y));
+        const Decay d = decay2(L);
+        const bool in = seqs.inside >> i & 1;
+        keep[i] = in ? d.a : splat(1.f);
+        root[i] = d.m;
+        if (kPacked && (seqs.open >> i & 1)) {
+          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
+          h = a.state ? pair_at<kWide>(a.state, s * a.channels + c, count) : splat(0.f);
+        }
+        before[i] = h;
+        h = __ffma2_rn(h, keep[i],
+                       __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g[i].pair(0))), x[i].pair(0)));
+      }
+      Map run{splat(1.f), splat(0.f)};
+#pragma unroll
+      for (int i = kRun - 1; i >= 0; --i) {
+        if (kPacked && (seqs.close >> i & 1)) {
+          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
+          run = {splat(0.f), a.dlast ? pair_at<kWide>(a.dlast, s * a.channels + c, count) : splat(0.f)};
+        }
+        if (!(seqs.inside >> i & 1)) continue;
+        run = {__fmul2_rn(run.A, keep[i]), __fmul2_rn(__fadd2_rn(run.H, dy[i].pair(0)), keep[i])};
+        if (kPacked && (seqs.open >> i & 1)) run = {splat(0.f), splat(0.f)};
+      }
+      float2 e = join<true>(joint, turn, run, carry, warp, lane, rank, size);
+      turn ^= 1;
+      if (n <= 0) continue;
+      float2 share = splat(0.f);
+#pragma unroll
+      for (int i = kRun - 1; i >= 0; --i) {
+        if (i >= n) continue;
+        Raw<T, 2> out;
+        if (kPacked && !(seqs.inside >> i & 1)) {  // rows of no sequence
+          out.set(0, splat(0.f));
+          out.template store<kWide>(a.dx.at(b, r0 + i) + c, count);
+          out.template store<kWide>(a.dadmit.at(b, r0 + i) + c, count);
+          out.template store<kWide>(a.dforget.at(b, r0 + i) + c, count);
+          continue;
+        }
+        if (kPacked && (seqs.close >> i & 1)) {
+          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
+          e = a.dlast ? pair_at<kWide>(a.dlast, s * a.channels + c, count) : splat(0.f);
+        }
+        e = __fadd2_rn(e, dy[i].pair(0));
+        const float2 open = sigmoid2(f[i].pair(0)), way = sigmoid2(g[i].pair(0)), v = x[i].pair(0);
+        const float2 L = __fmul2_rn(open, make_float2(-rate.x, -rate.y));
+        const float2 ew = __fmul2_rn(e, way), dx = __fmul2_rn(ew, root[i]);
+        out.set(0, dx);
+        out.template store<kWide>(a.dx.at(b, r0 + i) + c, count);
+        const float2 shut = __ffma2_rn(way, splat(-1.f), splat(1.f));
+        out.set(0, __fmul2_rn(__fmul2_rn(dx, v), shut));
+        out.template store<kWide>(a.dadmit.at(b, r0 + i) + c, count);
+        // dL L; L / m goes to zero with L, as -sqrt(-L / 2)
+        const float2 lm = make_float2(root[i].x > 0.f ? L.x * rcp_fast(root[i].x) : 0.f,
+                                      root[i].y > 0.f ? L.y * rcp_fast(root[i].y) : 0.f);
+        const float2 k = keep[i];
+        const float2 one = __fmul2_rn(__fmul2_rn(__fmul2_rn(e, before[i]), k), L);
+        const float2 two = __fmul2_rn(__fmul2_rn(__fmul2_rn(ew, v), __fmul2_rn(k, k)), lm);
+        const float2 dL = __ffma2_rn(two, splat(-1.f), one);
+        share = __fadd2_rn(share, dL);
+        out.set(0, __fmul2_rn(dL, __ffma2_rn(open, splat(-1.f), splat(1.f))));
+        out.template store<kWide>(a.dforget.at(b, r0 + i) + c, count);
+        e = __fmul2_rn(e, k);
+        if ((seqs.open >> i & 1) && a.dstate) {
+          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
+          put_pair<kWide>(a.dstate, s * a.channels + c, count, e);
+        }
+      }
+      drate = __fadd2_rn(drate, share);
+    }
+  }
+  if (kPacked && a.dstate && blockIdx.y == 0)
+    empty_sequences<kWide>(a, a.dstate, a.dlast, c, count, rank * kWarps + warp, size * kWarps);
+  sums[warp][lane] = drate;
+  __syncthreads();
+  if (warp == 0) {
+    float2 s = splat(0.f);
+    for (int w = 0; w < kWarps; ++w) s = __fadd2_rn(s, sums[w][lane]);
+    // of L = -rate s(forget): d rate = dL L / rate
+    s = make_float2(s.x / rate.x, s.y / rate.y);
+    put_pair<kWide>(a.parts, ((int64_t)blockIdx.y * size + rank) * a.channels + c, count, s);
+  }
+  if (size > 1) cg::this_cluster().sync();
+}
+
+// One thread for two channels of an entry.
+template <typename T, bool kWide>
+__global__ void __launch_bounds__(128) gated_step_kernel(const GatedArgs<T> a) {
+  const int64_t c = 2 * ((int64_t)blockIdx.x * blockDim.x + threadIdx.x);
+  const int count = (int)max((int64_t)0, min((int64_t)2, a.channels - c));
+  if (count == 0) return;
+  const float2 rate = pair_at<kWide>(a.rate, c, count);
+  for (int64_t b = blockIdx.y; b < a.sequences; b += gridDim.y) {
+    const int64_t slot = a.slots ? a.slots[b] : b;
+    Raw<T, 2> x, f, g, y;
+    f.template load<kWide>(a.forget.p + b * a.forget.batch + c, count);
+    g.template load<kWide>(a.admit.p + b * a.admit.batch + c, count);
+    x.template load<kWide>(a.x.p + b * a.x.batch + c, count);
+    const bool held = slot >= 0 && slot < a.num_slots;
+    float2 h = splat(0.f);
+    if (held) {
+      const Decay d = decay2(__fmul2_rn(sigmoid2(f.pair(0)), make_float2(-rate.x, -rate.y)));
+      const int64_t at = slot * a.channels + c;
+      h = __ffma2_rn(pair_at<kWide>(a.last, at, count), d.a,
+                     __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g.pair(0))), x.pair(0)));
+      put_pair<kWide>(a.last, at, count, h);
+    }
+    y.set(0, h);
+    y.template store<kWide>(a.y.p + b * a.y.batch + c, count);
+  }
+}
+
+// ------------------------------------------------------------- host side
+struct GatedPlan {
+  int64_t batches, strips, size, entries;  // entries: blocks along the batch
+  int64_t row_seq, parts;                  // workspace, in words
+};
+
+GatedPlan plan_of(const tcu_gated_scan_args &a, bool grad) {
+  GatedPlan p{};
+  p.batches = a.offsets ? 1 : a.sequences;
+  p.strips = (a.channels + kStrip - 1) / kStrip;
+  p.entries = std::min<int64_t>(p.batches, 65535);
+  // Blocks of a cluster share a strip's rows: as many as rows give tiles,
+  // until the card has a few blocks for each place.
+  const int64_t tiles = (a.rows + kTile - 1) / kTile;
+  p.size = 1;
+  while (p.size < kMostCluster && p.size < tiles &&
+         p.strips * p.entries * p.size < 8 * (int64_t)num_sms())
+    p.size *= 2;
+  p.row_seq = a.offsets ? (a.rows + 3) / 4 * 4 : 0;
+  p.parts = grad ? p.entries * p.size * a.channels : 0;
+  return p;
+}
+
+template <typename T>
+GatedArgs<T> args_of(const tcu_gated_scan_args &s, const GatedPlan &p, bool step) {
+  GatedArgs<T> a{};
+  a.x = rows_of<const T>(s.x);
+  a.forget = rows_of<const T>(s.forget);
+  a.admit = rows_of<const T>(s.admit);
+  a.y = rows_of<T>(s.y);
+  a.dy = rows_of<const T>(s.dy);
+  a.dx = rows_of<T>(s.dx);
+  a.dforget = rows_of<T>(s.dforget);
+  a.dadmit = rows_of<T>(s.dadmit);
+  a.rate = s.rate;
+  a.state = s.state;
+  a.dlast = s.dlast;
+  a.last = s.last;
+  a.dstate = s.dstate;
+  a.marks = s.marks;
+  a.offsets = s.offsets;
+  a.slots = s.slots;
+  a.channels = s.channels;
+  a.num_slots = s.num_slots;
+  a.rows = (int)s.rows;
+  a.sequences = s.sequences;
+  a.batches = (int)p.batches;
+  a.runs = (int)((s.rows + kRun - 1) / kRun);
+  if (!step) {
+    int32_t *w = static_cast<int32_t *>(s.workspace);
+    a.row_seq = s.offsets ? w : nullptr;
+    a.parts = reinterpret_cast<float *>(w + p.row_seq);
+  }
+  return a;
+}
+
+enum Call { kPrompt, kGrad, kStep };
+
+template <typename K, typename T>
+int start(K kernel, const GatedPlan &p, const GatedArgs<T> &a, cudaStream_t st) {
+  if (p.strips * p.size > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(p.strips * p.size), (unsigned)p.entries);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)p.size;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.size > 1 ? 1 : 0;
+  cudaError_t e = cudaSuccess;
+  if (p.size > 8)
+    e = cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, a, (int)p.size);
+  if (e == cudaSuccess) return launched();
+  cudaGetLastError();
+  return TCU_DFT_ERR_CUDA;
+}
+
+template <typename T, bool kPacked, bool kWide>
+int run_rows(Call call, const GatedPlan &p, const GatedArgs<T> &a, cudaStream_t st) {
+  return call == kGrad ? start(gated_grad_kernel<T, kPacked, kWide>, p, a, st)
+                       : start(gated_kernel<T, kPacked, kWide>, p, a, st);
+}
+
+template <typename T>
+int run(Call call, const tcu_gated_scan_args &s, cudaStream_t st) {
+  const GatedPlan p = plan_of(s, call == kGrad);
+  GatedArgs<T> a = args_of<T>(s, p, call == kStep);
+  const int64_t batches = call == kStep ? s.sequences : p.batches;
+  bool wide = s.channels % 2 == 0;
+  for (const void *q : {(const void *)s.rate, (const void *)s.state, (const void *)s.dlast,
+                        (const void *)s.last, (const void *)s.dstate, (const void *)s.marks,
+                        (const void *)a.parts})
+    wide = wide && (uintptr_t)q % 8 == 0;
+  for (const tcu_seq_rows *r : {&s.x, &s.forget, &s.admit})
+    wide = wide && rows_aligned(*r, s.type, batches, s.rows, 2 * sizeof(T));
+  if (call != kGrad) wide = wide && rows_aligned(s.y, s.type, batches, s.rows, 2 * sizeof(T));
+  else
+    for (const tcu_seq_rows *r : {&s.dy, &s.dx, &s.dforget, &s.dadmit})
+      wide = wide && rows_aligned(*r, s.type, batches, s.rows, 2 * sizeof(T));
+  if (call == kStep) {
+    const int64_t blocks = (s.channels + 255) / 256;
+    if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks, (unsigned)std::min(s.sequences, 65535));
+    if (wide) gated_step_kernel<T, true><<<grid, 128, 0, st>>>(a);
+    else gated_step_kernel<T, false><<<grid, 128, 0, st>>>(a);
+    return launched();
+  }
+  const bool none = p.batches == 0 || s.rows == 0;
+  if (!none) {
+    if (s.offsets) {
+      row_sequence_kernel<<<(unsigned)((s.rows + 127) / 128), 128, 0, st>>>(
+          const_cast<int32_t *>(a.row_seq), s.offsets, s.sequences, (int)s.rows);
+      if (const int rc = launched()) return rc;
+    }
+    const int rc = s.offsets ? wide ? run_rows<T, true, true>(call, p, a, st)
+                                    : run_rows<T, true, false>(call, p, a, st)
+                   : wide    ? run_rows<T, false, true>(call, p, a, st)
+                             : run_rows<T, false, false>(call, p, a, st);
+    if (rc) return rc;
+  }
+  if (call != kGrad) return TCU_DFT_OK;
+  const Sum sum = {s.drate, a.parts, s.channels};
+  return sum_parts(&sum, 1, none ? 0 : p.entries * p.size, 0, st);
+}
+
+int by_type(Call call, const tcu_gated_scan_args &a, void *stream) {
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  switch (a.type) {
+    case TCU_SEQ_F32: return run<float>(call, a, st);
+    case TCU_SEQ_BF16: return run<bf16>(call, a, st);
+    default: return run<f16>(call, a, st);
+  }
+}
+
+int check_sizes(const tcu_gated_scan_args *a) {
+  if (!a || a->type < TCU_SEQ_F32 || a->type > TCU_SEQ_F16 || a->sequences < 0 || a->rows < 0 ||
+      a->channels < 1)
+    return TCU_DFT_ERR_INVALID;
+  if (a->rows > kMostRows || a->channels > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  for (const tcu_seq_rows *r :
+       {&a->x, &a->forget, &a->admit, &a->y, &a->dy, &a->dx, &a->dforget, &a->dadmit})
+    if (!pitch_fits(a->rows, r->row_stride)) return TCU_DFT_ERR_UNSUPPORTED;
+  return TCU_DFT_OK;
+}
+
+bool inputs_ok(const tcu_gated_scan_args &a) {
+  const int sz = type_size(a.type);
+  return f32_ok(a.rate) && opt_ok(a.state, 4) && opt_ok(a.last, 4) && opt_ok(a.marks, 4) &&
+         opt_ok(a.offsets, 4) && row_ok(a.x, sz) && row_ok(a.forget, sz) && row_ok(a.admit, sz);
+}
+
+bool workspace_ok(const tcu_gated_scan_args &a, const GatedPlan &p) {
+  const int64_t bytes = 4 * (p.row_seq + p.parts);
+  return a.workspace_bytes >= bytes && (bytes == 0 || f32_ok(a.workspace));
+}
+
+// Sequences without any row end in the state they start from.
+int no_rows(const tcu_gated_scan_args &a, float *to, const float *from, void *stream) {
+  if (!to || a.sequences == 0 || a.rows > 0) return TCU_DFT_OK;
+  const size_t bytes = (size_t)a.sequences * a.channels * 4;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = from ? cudaMemcpyAsync(to, from, bytes, cudaMemcpyDeviceToDevice, st)
+                             : cudaMemsetAsync(to, 0, bytes, st);
+  if (e == cudaSuccess) return TCU_DFT_OK;
+  cudaGetLastError();
+  return TCU_DFT_ERR_CUDA;
+}
+
+bool any_rows(const tcu_gated_scan_args &a) {
+  return a.rows > 0 && a.sequences + (a.offsets != nullptr) > 0;
+}
+
+}  // namespace
+}  // namespace seq
+}  // namespace tcu
+
+using namespace tcu::seq;
+
+extern "C" int64_t tcu_gated_scan_workspace(const tcu_gated_scan_args *a) {
+  if (check_sizes(a)) return -1;
+  return 4 * plan_of(*a, false).row_seq;
+}
+
+extern "C" int64_t tcu_gated_scan_grad_workspace(const tcu_gated_scan_args *a) {
+  if (check_sizes(a)) return -1;
+  const GatedPlan p = plan_of(*a, true);
+  return 4 * (p.row_seq + p.parts);
+}
+
+extern "C" int tcu_gated_scan(const tcu_gated_scan_args *a, void *stream) {
+  if (const int rc = check_sizes(a)) return rc;
+  if (any_rows(*a) && (!inputs_ok(*a) || !row_ok(a->y, type_size(a->type)) ||
+                       !workspace_ok(*a, plan_of(*a, false))))
+    return TCU_DFT_ERR_INVALID;
+  if (const int rc = no_rows(*a, a->last, a->state, stream)) return rc;
+  return by_type(kPrompt, *a, stream);
+}
+
+extern "C" int tcu_gated_scan_grad(const tcu_gated_scan_args *a, void *stream) {
+  if (const int rc = check_sizes(a)) return rc;
+  const int sz = type_size(a->type);
+  if (!f32_ok(a->drate) || !opt_ok(a->dlast, 4) || !opt_ok(a->dstate, 4)) return TCU_DFT_ERR_INVALID;
+  if (any_rows(*a) && (!inputs_ok(*a) || !a->marks || !row_ok(a->dy, sz) || !row_ok(a->dx, sz) ||
+                       !row_ok(a->dforget, sz) || !row_ok(a->dadmit, sz) ||
+                       !workspace_ok(*a, plan_of(*a, true))))
+    return TCU_DFT_ERR_INVALID;
+  if (const int rc = no_rows(*a, a->dstate, a->dlast, stream)) return rc;
+  return by_type(kGrad, *a, stream);
+}
+
+extern "C" int tcu_gated_scan_step(const tcu_gated_scan_args *a, void *stream) {
+  if (const int rc = check_sizes(a)) return rc;
+  if (a->rows != 1 || a->offsets || a->num_slots < 0 ||
+      (!a->slots && a->num_slots < a->sequences) || !opt_ok(a->slots, 4))
+    return TCU_DFT_ERR_INVALID;
+  if (a->sequences == 0) return TCU_DFT_OK;
+  const int sz = type_size(a->type);
+  if (!inputs_ok(*a) || !row_ok(a->y, sz) || (a->num_slots > 0 && !a->last))
+    return TCU_DFT_ERR_INVALID;
+  const int64_t entry = a->channels * 4;
+  const wide_int cache = (wide_int)a->num_slots * entry;
+  for (const tcu_seq_rows *r : {&a->x, &a->forget, &a->admit, &a->y})
+    if (over(a->last, cache, r->ptr, a->channels * sz, a->sequences, r->batch_stride * sz))
+      return TCU_DFT_ERR_INVALID;
+  if (over(a->last, cache, a->rate, entry) ||
+      over(a->last, cache, a->slots, (int64_t)a->sequences * 4))
+    return TCU_DFT_ERR_INVALID;
+  return by_type(kStep, *a, stream);
+}

@@ -1,20 +1,21 @@
 """Sequence operators (C ABI in include/tcu_seq.h): the short causal
-convolution and the selective state-space scan, over prompts, with their
-gradients, and for one token.
+convolution, the selective state-space scan and the gated linear recurrence,
+over prompts, with their gradients, and for one token.
 
 Rows are torch tensors of float32, bfloat16 or float16, dense -- (batch,
 length, channels) -- or packed: (rows, channels) with ``offsets``, an int32
 CUDA tensor of sequences + 1 row numbers from 0 to rows.  Any strides over
 batch and rows are taken as they are (a slice of a wider projection needs no
-copy); channels must be adjacent.  Parameters and the scan's states are
-float32.  Everything runs on torch's current stream, or on ``stream``; ordering
+copy); channels must be adjacent.  Parameters and the states of scan and
+recurrence are float32.  Everything runs on torch's current stream, or on ``stream``; ordering
 that against other streams that use the tensors (wait_stream, record_stream) is
 the caller's, as for any torch operation.  ``out``
 shares memory neither with an input nor with itself; only a single-token call
-may write over a row that it reads (x; u, dt or gate), all of it.
+may write over a row that it reads (x; u, dt or gate; forget or admit), all
+of it.
 
-``short_conv`` and ``state_scan`` are differentiable: where a gradient is
-asked of an argument they record themselves with autograd.  The ``_grad``
+``short_conv``, ``state_scan`` and ``gated_scan`` are differentiable: where a
+gradient is asked of an argument they record themselves with autograd.  The ``_grad``
 calls are what that runs; the ``_step`` calls have no gradient.
 """
 from __future__ import annotations
@@ -33,18 +34,21 @@ from . import OK, TcuDftError, lib
 MAX_WIDTH = 8
 MAX_STATES = 128
 MARK = 16  # rows from one state that the gradient resumes from to the next
+GATED_MARK = 8  # the same for the gated recurrence
 
 SYMBOLS = (
     "tcu_short_conv", "tcu_short_conv_grad", "tcu_short_conv_grad_workspace",
     "tcu_short_conv_step", "tcu_state_scan", "tcu_state_scan_workspace",
     "tcu_state_scan_grad", "tcu_state_scan_grad_workspace",
-    "tcu_state_scan_step",
+    "tcu_state_scan_step", "tcu_gated_scan", "tcu_gated_scan_workspace",
+    "tcu_gated_scan_grad", "tcu_gated_scan_grad_workspace", "tcu_gated_scan_step",
 )
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 ConvGrads = namedtuple("ConvGrads", "x weight bias state")
 ScanGrads = namedtuple("ScanGrads", "u dt A B C skip gate dt_bias state")
+GatedGrads = namedtuple("GatedGrads", "x forget admit rate state")
 
 _vp, _i64, _i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
 
@@ -77,11 +81,24 @@ class _ScanArgs(ctypes.Structure):
                 ("slots", _vp), ("num_slots", _i64)]
 
 
+class _GatedArgs(ctypes.Structure):
+    _fields_ = [("type", _i32), ("sequences", _i32), ("rows", _i64), ("channels", _i64),
+                ("offsets", _vp), ("x", _Rows), ("forget", _Rows), ("admit", _Rows), ("y", _Rows),
+                ("rate", _vp), ("state", _vp), ("dlast", _vp),
+                ("last", _vp), ("dstate", _vp), ("marks", _vp),
+                ("dy", _Rows), ("dx", _Rows), ("dforget", _Rows), ("dadmit", _Rows),
+                ("drate", _vp),
+                ("workspace", _vp), ("workspace_bytes", _i64),
+                ("slots", _vp), ("num_slots", _i64)]
+
+
 # The same structures for struct.pack: what a call costs on the host counts
 # where a token's kernel takes a few microseconds.
 _CONV = struct.Struct("4i2qP" + "P2q" * 4 + "P" * 8 + "Pq" * 2)
 _SCAN = struct.Struct("4i3qP" + "P2q" * 6 + "P" * 8 + "P2q" * 6 + "P" * 3 + "Pq" * 2)
+_GATED = struct.Struct("2i2qP" + "P2q" * 4 + "P" * 6 + "P2q" * 4 + "P" + "Pq" * 2)
 assert _CONV.size == ctypes.sizeof(_ConvArgs) and _SCAN.size == ctypes.sizeof(_ScanArgs)
+assert _GATED.size == ctypes.sizeof(_GatedArgs)
 _NO_ROWS = (0, 0, 0)
 
 _bound = None
@@ -97,7 +114,8 @@ def _lib():
                 L, calls = lib(), {}
                 for name in SYMBOLS:
                     f = getattr(L, name)
-                    args = ctypes.POINTER(_ConvArgs if "conv" in name else _ScanArgs)
+                    args = ctypes.POINTER(_ConvArgs if "conv" in name else
+                                          _GatedArgs if "gated" in name else _ScanArgs)
                     f.argtypes = [args] if name.endswith("workspace") else [args, _vp]
                     f.restype = _i64 if name.endswith("workspace") else ctypes.c_int
                     f = calls[name] = L[name]  # the same entry, for packed arguments
@@ -703,6 +721,157 @@ def state_scan_step(u, dt, A, B, C, state, *, skip=None, gate=None, dt_bias=None
                 pu[0], pu[2], 0, pd[0], pd[2], 0, pz[0], pz[2], 0, py[0], py[2], 0,
                 pB[0], pB[2], 0, pC[0], pC[2], 0, pA, pk, pi, 0, 0, cache, 0, 0, *_NO_GRADS,
                 0, 0, ps, entries), st)
+        _written(state)
+        if out is not None:
+            _written(out)
+    return y
+
+
+# --------------------------------------------------- gated linear recurrence
+class _GatedCall:
+    """The checked arguments that the recurrence and its gradient share."""
+
+    def __init__(self, x, forget, admit, rate, state, offsets):
+        seqs, rows, ch, off = _layout(x, "x", offsets)
+        f32, dtype, index, shape = torch.float32, x.dtype, x.get_device(), x.shape
+        self.index, self.dtype, self.channels, self.tail = index, dtype, ch, (seqs, ch)
+        self.head = (_TYPES[dtype], seqs, rows, ch, off, *_rows(x, "x", dtype, index, shape),
+                     *_rows(forget, "forget", dtype, index, shape),
+                     *_rows(admit, "admit", dtype, index, shape))
+        self.params = (_flat(rate, "rate", f32, index, (ch,)),
+                       _flat(state, "state", f32, index, self.tail))
+        batch = shape[0] if offsets is None else 1
+        self.marks = (batch, -(-rows // GATED_MARK), ch)
+
+
+_NO_GATED_GRADS = _NO_ROWS * 4 + (0,)
+
+
+def _gated(x, forget, admit, rate, state, offsets, marks, out, stream):
+    c = _GatedCall(x, forget, admit, rate, state, offsets)
+    f32, dev = torch.float32, x.device
+    with _On(c.index, stream) as st:
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
+        last = torch.empty(c.tail, dtype=f32, device=dev)
+        py = _rows(y, "out", c.dtype, c.index, x.shape)
+        if out is not None:
+            _apart(out, (x, forget, admit, rate, state, offsets))
+        kept = torch.empty(c.marks, dtype=f32, device=dev) if marks else None
+
+        def packed(work, size):
+            return _GATED.pack(*c.head, *py, *c.params, 0, last.data_ptr(), 0,
+                               kept.data_ptr() if marks else 0, *_NO_GATED_GRADS, work, size, 0, 0)
+
+        if c.channels:
+            work, n = None, 0
+            if offsets is not None:  # only packed rows take a workspace
+                work, n = _workspace("tcu_gated_scan_workspace", packed(0, 0), dev)
+            _call("tcu_gated_scan", packed(work.data_ptr() if n else 0, n), st)
+            del work
+        if out is not None:
+            _written(out)
+    return y, last, kept
+
+
+class _GatedScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, forget, admit, rate, state, offsets):
+        y, last, marks = _gated(x, forget, admit, rate, state, offsets, True, None, None)
+        ctx.save_for_backward(x, forget, admit, rate, state, offsets, marks)
+        return y, last
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dlast):
+        x, forget, admit, rate, state, offsets, marks = ctx.saved_tensors
+        g = gated_scan_grad(_adjacent(dy), x, forget, admit, rate, marks=marks, state=state,
+                            offsets=offsets, dlast=dlast.contiguous())
+        return g.x, g.forget, g.admit, g.rate, g.state, None
+
+
+def gated_scan(x, forget, admit, rate, *, state=None, offsets=None, marks=False, out=None,
+               stream=None):
+    """Gated linear recurrence over every sequence, one state a channel:
+
+        a_t = exp(-rate sigmoid(forget_t))
+        h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(admit_t) x_t
+
+    and y = h.  x, forget, admit: rows; rate: (channels,), positive; state:
+    (sequences, channels), zeros if None.
+
+    Returns (y, last), last being the state that a continuation takes; with
+    ``marks`` also the states that gated_scan_grad resumes from.  Rows behind
+    the last packed sequence are not written.
+    """
+    if _forward._current_level >= 0:
+        _no_tangent(x, forget, admit, rate, state, out)
+    if _wants_grad(x, forget, admit, rate, state):
+        if out is not None or marks or stream is not None:
+            raise ValueError("out, marks and stream cannot be given where a gradient is asked")
+        return _GatedScan.apply(x, forget, admit, rate, state, offsets)
+    if _wants_grad(out):
+        raise ValueError("out must not record a gradient")
+    y, last, kept = _gated(x, forget, admit, rate, state, offsets, marks, out, stream)
+    return (y, last, kept) if marks else (y, last)
+
+
+def gated_scan_grad(dy, x, forget, admit, rate, *, marks, state=None, offsets=None, dlast=None,
+                    stream=None):
+    """Gradients of gated_scan's (y, last) under dy and dlast (zeros if None),
+    from the marks that gated_scan kept of the same arguments: GatedGrads(x,
+    forget, admit, rate, state), None where the argument is.  Rows behind the
+    last packed sequence get zeros."""
+    if _forward._current_level >= 0:
+        _no_tangent(dy, x, forget, admit, rate, marks, state, dlast)
+    c = _GatedCall(x, forget, admit, rate, state, offsets)
+    f32, dev, dtype, index, shape = torch.float32, x.device, c.dtype, c.index, x.shape
+    pdy = _rows(dy, "dy", dtype, index, shape)
+    pm = _flat(marks, "marks", f32, index, c.marks)
+    pl = _flat(dlast, "dlast", f32, index, c.tail)
+    with _On(index, stream) as st:
+        g = GatedGrads(*(torch.empty(shape, dtype=dtype, device=dev) for _ in range(3)),
+                       torch.empty(rate.shape, dtype=f32, device=dev),
+                       None if state is None else torch.empty(c.tail, dtype=f32, device=dev))
+        outs = [v for t in g[:3] for v in _rows(t, "gradient", dtype, index, shape)]
+
+        def packed(work, size):
+            return _GATED.pack(*c.head, *_NO_ROWS, *c.params, pl, 0,
+                               0 if state is None else g.state.data_ptr(), pm, *pdy, *outs,
+                               g.rate.data_ptr(), work, size, 0, 0)
+
+        if c.channels:
+            work, n = _workspace("tcu_gated_scan_grad_workspace", packed(0, 0), dev)
+            _call("tcu_gated_scan_grad", packed(work.data_ptr() if n else 0, n), st)
+            del work
+    return g
+
+
+def gated_scan_step(x, forget, admit, rate, state, *, slots=None, out=None, stream=None):
+    """gated_scan for one more row of every sequence: x, forget, admit (batch,
+    channels) to y.  ``state`` (entries, channels) is advanced in place, at
+    entry slots[b] (int32) for row b, or entry b.  A slot outside the cache
+    gives a row of zeros; no two rows may name the same one."""
+    if _forward._current_level >= 0:
+        _no_tangent(x, forget, admit, rate, state, out)
+    _tensor(x, "x")
+    if x.dim() != 2 or x.dtype not in _TYPES or not x.is_cuda:
+        raise ValueError("x must be a float32, bfloat16 or float16 CUDA tensor (batch, channels)")
+    _no_grad(x, forget, admit, rate, state, out)
+    batch, ch = shape = x.shape
+    f32, dtype, index = torch.float32, x.dtype, x.get_device()
+    cache, entries, ps = _cache(state, slots, batch, (ch,), f32, index)
+    px, pf = _rows(x, "x", dtype, index, shape), _rows(forget, "forget", dtype, index, shape)
+    pg = _rows(admit, "admit", dtype, index, shape)
+    pr = _flat(rate, "rate", f32, index, (ch,))
+    with _On(index, stream) as st:
+        y = torch.empty((batch, ch), dtype=dtype, device=x.device) if out is None else out
+        py = _rows(y, "out", dtype, index, shape)
+        if out is not None:
+            _apart(out, (rate, state, slots), in_place=(x, forget, admit))
+        if ch:
+            _call("tcu_gated_scan_step", _GATED.pack(
+                _TYPES[dtype], batch, 1, ch, 0, px[0], px[2], 0, pf[0], pf[2], 0, pg[0], pg[2], 0,
+                py[0], py[2], 0, pr, 0, 0, cache, 0, 0, *_NO_GATED_GRADS, 0, 0, ps, entries), st)
         _written(state)
         if out is not None:
             _written(out)
