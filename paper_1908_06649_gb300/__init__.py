@@ -455,6 +455,9 @@ class StencilPlan:
 _SEQUENCE = ("short_conv", "short_conv_grad", "short_conv_step", "state_scan",
              "state_scan_grad", "state_scan_step", "gated_scan", "gated_scan_grad",
              "gated_scan_step")
+# and the attention operators (attention.py)
+_ATTENTION = ("norm_rotate", "norm_rotate_grad", "window_attention", "window_attention_grad",
+              "window_attention_step", "window_cache")
 
 
 def __getattr__(name):
@@ -462,5 +465,10 @@ def __getattr__(name):
         from . import sequence
         for n in _SEQUENCE:
             globals()[n] = getattr(sequence, n)
+        return globals()[name]
+    if name in _ATTENTION:
+        from . import attention
+        for n in _ATTENTION:
+            globals()[n] = getattr(attention, n)
         return globals()[name]
     raise AttributeError("module %r has no attribute %r" % (__name__, name))

@@ -19,16 +19,20 @@ UNITS = ["tcu_dft.cu", "host_tables.cu", "noalloc.cu", "grid_plan.cu",
          "kernels_mixed_r8.cu", "kernels_mixed_r16.cu", "kernels_mixed_r32.cu",
          "kernels_bf16_r8.cu", "kernels_bf16_r16.cu", "kernels_bf16_r32.cu",
          "grid_kernels.cu"]
-# the sequence operators have no bounds-checked form: both variants link the
+# the sequence and attention operators have no bounds-checked form: both variants link the
 # same objects
 SEQ_UNITS = ["short_conv.cu", "state_scan.cu", "state_scan_f32.cu",
-             "state_scan_bf16.cu", "state_scan_f16.cu", "gated_scan.cu"]
+             "state_scan_bf16.cu", "state_scan_f16.cu", "gated_scan.cu",
+             "norm_rotate.cu", "window_attention.cu", "window_attention_grad.cu",
+             "window_attention_step.cu"]
 HEADERS = ["tcgen05.cuh", "group_kernel.cuh", "launch.h",
            "launch_impl.cuh", "host_plan.h", "seq_common.cuh",
-           "seq_index.h", "state_scan.cuh", "state_scan_impl.cuh"]
+           "seq_index.h", "state_scan.cuh", "state_scan_impl.cuh",
+           "attn_common.cuh"]
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 HDR = os.path.join(INCLUDE, "tcu_dft.h")
 SEQ_HDR = os.path.join(INCLUDE, "tcu_seq.h")
+ATTN_HDR = os.path.join(INCLUDE, "tcu_attn.h")
 LIB_PATH = os.path.join(HERE, "libtcu_dft.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 # the bounds-checked variant: every shared-memory, tensor-memory and global
@@ -54,7 +58,7 @@ def nvcc() -> str:
 
 def _sources():
     return ([os.path.join(CSRC, u) for u in UNITS + SEQ_UNITS]
-            + [os.path.join(CSRC, h) for h in HEADERS] + [HDR, SEQ_HDR])
+            + [os.path.join(CSRC, h) for h in HEADERS] + [HDR, SEQ_HDR, ATTN_HDR])
 
 
 def build_variants(names=("release",), force: bool = False,

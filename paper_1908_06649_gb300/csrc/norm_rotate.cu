@@ -1,0 +1,433 @@
+// norm_rotate.cu -- the norm of each head of queries and keys with the rotation
+// by position, and its gradient (include/tcu_attn.h).
+//
+// Per head of d values x, with weights w:
+//     r = 1 / sqrt(sum x^2 / d + eps),   n = x r,   y = R (n w)
+// R turning pairs of values by position x rate; its gradient, g = R^T dy:
+//     dw = sum over rows and heads of g n
+//     dx = r g w - x r^3 (sum g w x) / d
+// Some ten operations for each value read and written: HBM bounds it.  A warp
+// owns a row, with a few lanes for each head; a lane holds the same pairs of
+// every head, so that a row's angles are formed once for all its heads, and
+// weights, rates and the shares of dw stay in registers.  Both values of a pair
+// are in the same lane: rows may be written over those that they come from.
+#include <algorithm>
+
+#include "../../include/tcu_attn.h"
+#include "seq_common.cuh"
+
+namespace tcu {
+namespace seq {
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+
+template <typename T>
+struct RotateArgs {
+  Rows<const T> q, k, dyq, dyk;
+  Rows<T> yq, yk, dq, dk;
+  const float *rates, *q_weight, *k_weight;
+  float *parts;  // [block]{q: dim, k: dim}
+  const int32_t *offsets, *positions;
+  int64_t rows, total;  // of a batch entry, of all
+  int sequences, heads, kv_heads, dim, turned;
+  int lanes;  // of a head, a power of two
+  float eps;
+};
+
+// A lane's part of a head: kParts parts of VP adjacent pairs, in two words of
+// VP values each.  Pairs that are turned with their partner `turned` values on
+// lie at (p, p + turned), others at (2p, 2p + VP).
+template <int VP>
+struct Part {
+  static constexpr int kParts = VP >= 4 ? 1 : 4 / VP;
+};
+
+template <typename T, int VP>
+__device__ __forceinline__ void load_word(const T *p, bool has, float *v) {
+  if (has) {
+    const Vec<T, VP> w = *reinterpret_cast<const Vec<T, VP> *>(p);
+#pragma unroll
+    for (int i = 0; i < VP; ++i) v[i] = to_f(w.v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VP; ++i) v[i] = 0.f;
+  }
+}
+template <typename T, int VP>
+__device__ __forceinline__ void store_word(T *p, bool has, const float *v) {
+  if (!has) return;
+  Vec<T, VP> w;
+#pragma unroll
+  for (int i = 0; i < VP; ++i) w.v[i] = from_f<T>(v[i]);
+  *reinterpret_cast<Vec<T, VP> *>(p) = w;
+}
+
+template <typename T, int VP, bool kInter>
+struct Lane {
+  static constexpr int kParts = Part<VP>::kParts;
+  int at[kParts][2];
+  bool has[kParts];
+  uint64_t turn[kParts][VP];  // turns of one position, in 2^-64
+
+  __device__ __forceinline__ void init(const RotateArgs<T> &a, int j) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      const int p = (j + k * a.lanes) * VP;
+      has[k] = p < a.dim / 2;
+      const bool apart = !kInter && p < a.turned;
+      at[k][0] = apart ? p : 2 * p;
+      at[k][1] = apart ? p + a.turned : 2 * p + VP;
+#pragma unroll
+      for (int i = 0; i < VP; ++i) {
+        turn[k][i] = 0;
+        if (p + i >= a.turned) continue;
+        // whole turns of a position change nothing; 2^64 of the rest, signed
+        const double t = (double)a.rates[p + i] * 0.15915494309189535;
+        const double f = fabs(t) - floor(fabs(t));
+        const uint64_t u = (uint64_t)(f * 18446744073709551616.0);
+        turn[k][i] = t < 0 ? 0 - u : u;
+      }
+    }
+  }
+  // cos and sin of the lane's angles at a position: the product wraps as turns do
+  __device__ __forceinline__ void angles(int64_t position, float (*c)[VP], float (*s)[VP]) const {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int i = 0; i < VP; ++i) {
+        const int32_t t = (int32_t)(uint32_t)(((uint64_t)position * turn[k][i]) >> 32);
+        sincospif((float)t * 4.656612873077393e-10f, &s[k][i], &c[k][i]);  // 2^-31
+      }
+  }
+  __device__ __forceinline__ void load(const T *head, bool in, float (*v)[2 * VP]) const {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      load_word<T, VP>(head + at[k][0], in && has[k], v[k]);
+      load_word<T, VP>(head + at[k][1], in && has[k], v[k] + VP);
+    }
+  }
+  __device__ __forceinline__ void store(T *head, bool in, const float (*v)[2 * VP]) const {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      store_word<T, VP>(head + at[k][0], in && has[k], v[k]);
+      store_word<T, VP>(head + at[k][1], in && has[k], v[k] + VP);
+    }
+  }
+  // turns by the angles (kBack: against them)
+  template <bool kBack>
+  static __device__ __forceinline__ void rotate(float (*v)[2 * VP], const float (*c)[VP],
+                                                const float (*s)[VP]) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int i = 0; i < VP; ++i) {
+        float &x = v[k][kInter ? 2 * i : i], &y = v[k][kInter ? 2 * i + 1 : VP + i];
+        const float sn = kBack ? -s[k][i] : s[k][i], a = x, b = y;
+        x = a * c[k][i] - b * sn;
+        y = a * sn + b * c[k][i];
+      }
+  }
+  __device__ __forceinline__ void weights(const float *w, float (*v)[2 * VP]) const {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int i = 0; i < 2 * VP; ++i)
+        v[k][i] = !has[k] ? 0.f : w ? w[at[k][i / VP] + i % VP] : 1.f;
+  }
+};
+
+__device__ __forceinline__ float sum_lanes(float v, int lanes) {
+  for (int m = 1; m < lanes; m *= 2) v += __shfl_xor_sync(~0u, v, m);
+  return v;
+}
+
+// The row's batch entry, number and position; false for a row of no sequence.
+template <typename T>
+__device__ __forceinline__ bool place_of(const RotateArgs<T> &a, int64_t id, int64_t &b, int &t,
+                                         int64_t &position) {
+  b = id / a.rows;
+  t = (int)(id - b * a.rows);
+  position = t;
+  if (a.offsets) {
+    const int s = sequence_of(a.offsets, a.sequences, t);
+    if (s < 0) return false;
+    position = t - a.offsets[s];
+  }
+  if (a.positions) position = a.positions[id];
+  return true;
+}
+
+template <typename T, int VP, bool kInter>
+__global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs<T> a) {
+  constexpr int kParts = Part<VP>::kParts;
+  const int lane = threadIdx.x % 32, per = 32 / a.lanes, sub = lane / a.lanes;
+  Lane<T, VP, kInter> own;
+  own.init(a, lane % a.lanes);
+  float wq[kParts][2 * VP], wk[kParts][2 * VP];
+  own.weights(a.q_weight, wq);
+  own.weights(a.k_weight, wk);
+  const float inv = 1.f / a.dim;
+  const int64_t step = (int64_t)gridDim.x * kWarps;
+  for (int64_t id = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; id < a.total; id += step) {
+    int64_t b, position;
+    int t;
+    if (!place_of(a, id, b, t, position)) continue;
+    float c[kParts][VP], s[kParts][VP];
+    own.angles(position, c, s);
+    auto heads = [&](const T *from, T *to, int count, const float (*w)[2 * VP]) {
+#pragma unroll 2
+      for (int h0 = 0; h0 < count; h0 += per) {
+        const int h = h0 + sub;
+        const bool in = h < count;
+        float v[kParts][2 * VP];
+        own.load(from + (int64_t)h * a.dim, in, v);
+        float squares = 0.f;
+#pragma unroll
+        for (int k = 0; k < kParts; ++k)
+#pragma unroll
+          for (int i = 0; i < 2 * VP; ++i) squares = fmaf(v[k][i], v[k][i], squares);
+        const float r = rsqrtf(fmaf(sum_lanes(squares, a.lanes), inv, a.eps));
+#pragma unroll
+        for (int k = 0; k < kParts; ++k)
+#pragma unroll
+          for (int i = 0; i < 2 * VP; ++i) v[k][i] *= r * w[k][i];
+        own.template rotate<false>(v, c, s);
+        own.store(to + (int64_t)h * a.dim, in, v);
+      }
+    };
+    heads(a.q.at(b, t), a.yq.at(b, t), a.heads, wq);
+    heads(a.k.at(b, t), a.yk.at(b, t), a.kv_heads, wk);
+  }
+}
+
+template <typename T, int VP, bool kInter>
+__global__ void __launch_bounds__(kThreads) rotate_grad_kernel(const RotateArgs<T> a) {
+  constexpr int kParts = Part<VP>::kParts;
+  __shared__ float sums[kWarps][2 * TCU_ATTN_MAX_NORM_DIM];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int per = 32 / a.lanes, sub = lane / a.lanes;
+  Lane<T, VP, kInter> own;
+  own.init(a, lane % a.lanes);
+  float dwq[kParts][2 * VP] = {}, dwk[kParts][2 * VP] = {};
+  const float inv = 1.f / a.dim;
+  const int64_t step = (int64_t)gridDim.x * kWarps;
+  for (int64_t id = (int64_t)blockIdx.x * kWarps + warp; id < a.total; id += step) {
+    int64_t b, position;
+    int t;
+    const bool row = place_of(a, id, b, t, position);
+    float c[kParts][VP], s[kParts][VP];
+    if (row) own.angles(position, c, s);
+    auto heads = [&](const T *from, const T *dy, T *to, int count, const float *weight,
+                     float (*dw)[2 * VP]) {
+      float w[kParts][2 * VP];
+      own.weights(weight, w);
+      for (int h0 = 0; h0 < count; h0 += per) {
+        const int h = h0 + sub;
+        const bool in = h < count;
+        float x[kParts][2 * VP], g[kParts][2 * VP];
+        own.load(from + (int64_t)h * a.dim, in && row, x);
+        own.load(dy + (int64_t)h * a.dim, in && row, g);
+        if (row) {
+          own.template rotate<true>(g, c, s);
+          float squares = 0.f, dot = 0.f;
+#pragma unroll
+          for (int k = 0; k < kParts; ++k)
+#pragma unroll
+            for (int i = 0; i < 2 * VP; ++i) {
+              squares = fmaf(x[k][i], x[k][i], squares);
+              dot = fmaf(g[k][i] * w[k][i], x[k][i], dot);
+            }
+          for (int m = 1; m < a.lanes; m *= 2) {
+            squares += __shfl_xor_sync(~0u, squares, m);
+            dot += __shfl_xor_sync(~0u, dot, m);
+          }
+          const float r = rsqrtf(fmaf(squares, inv, a.eps)), back = r * r * r * dot * inv;
+#pragma unroll
+          for (int k = 0; k < kParts; ++k)
+#pragma unroll
+            for (int i = 0; i < 2 * VP; ++i) {
+              dw[k][i] = fmaf(g[k][i], x[k][i] * r, dw[k][i]);
+              g[k][i] = fmaf(g[k][i] * w[k][i], r, -x[k][i] * back);
+            }
+        }
+        own.store(to + (int64_t)h * a.dim, in, g);  // zeros for a row of no sequence
+      }
+    };
+    heads(a.q.at(b, t), a.dyq.at(b, t), a.dq.at(b, t), a.heads, a.q_weight, dwq);
+    heads(a.k.at(b, t), a.dyk.at(b, t), a.dk.at(b, t), a.kv_heads, a.k_weight, dwk);
+  }
+  if (!a.parts) return;
+  // lanes of the same values, then warps, in a fixed order
+#pragma unroll
+  for (int k = 0; k < kParts; ++k)
+#pragma unroll
+    for (int i = 0; i < 2 * VP; ++i) {
+      float x = dwq[k][i], y = dwk[k][i];
+      for (int m = a.lanes; m < 32; m *= 2) {
+        x += __shfl_xor_sync(~0u, x, m);
+        y += __shfl_xor_sync(~0u, y, m);
+      }
+      if (sub == 0 && own.has[k]) {
+        const int at = own.at[k][i / VP] + i % VP;
+        sums[warp][at] = x;
+        sums[warp][a.dim + at] = y;
+      }
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * a.dim; i += kThreads) {
+    float x = 0.f;
+    for (int w = 0; w < kWarps; ++w) x += sums[w][i];
+    a.parts[(int64_t)blockIdx.x * 2 * a.dim + i] = x;
+  }
+}
+
+// ------------------------------------------------------------- host side
+// Blocks of a call: as many as the card holds at once, so that each sums its
+// shares of the weights' gradients over many rows.
+int64_t blocks_of(const tcu_norm_rotate_args &a, bool grad) {
+  const int64_t total = (a.offsets ? 1 : (int64_t)a.sequences) * a.rows;
+  return std::min<int64_t>((total + kWarps - 1) / kWarps, (grad ? 3 : 4) * num_sms());
+}
+
+template <typename T, int VP, bool kInter>
+int start(const tcu_norm_rotate_args &s, RotateArgs<T> a, bool grad, cudaStream_t st) {
+  const int words = (s.dim / 2 + VP - 1) / VP;
+  a.lanes = 1;
+  while (a.lanes < 32 && a.lanes < words) a.lanes *= 2;
+  const unsigned blocks = (unsigned)blocks_of(s, grad);
+  if (grad) rotate_grad_kernel<T, VP, kInter><<<blocks, kThreads, 0, st>>>(a);
+  else rotate_kernel<T, VP, kInter><<<blocks, kThreads, 0, st>>>(a);
+  return launched();
+}
+
+template <typename T, int VP>
+int by_order(const tcu_norm_rotate_args &s, const RotateArgs<T> &a, bool grad, cudaStream_t st) {
+  return s.interleaved ? start<T, VP, true>(s, a, grad, st) : start<T, VP, false>(s, a, grad, st);
+}
+
+template <typename T>
+int run(const tcu_norm_rotate_args &s, bool grad, cudaStream_t st) {
+  RotateArgs<T> a{};
+  a.q = rows_of<const T>(s.q);
+  a.k = rows_of<const T>(s.k);
+  a.rates = s.rates;
+  a.q_weight = s.q_weight;
+  a.k_weight = s.k_weight;
+  a.offsets = s.offsets;
+  a.positions = s.positions;
+  a.rows = s.rows;
+  const int64_t batches = s.offsets ? 1 : s.sequences;
+  a.total = batches * s.rows;
+  a.sequences = s.sequences;
+  a.heads = s.heads;
+  a.kv_heads = s.kv_heads;
+  a.dim = s.dim;
+  a.turned = s.turned;
+  a.eps = s.eps;
+  const tcu_seq_rows *rows[6] = {&s.q, &s.k, &s.y_q, &s.y_k};
+  int count = 4;
+  if (grad) {
+    a.dyq = rows_of<const T>(s.dy_q);
+    a.dyk = rows_of<const T>(s.dy_k);
+    a.dq = rows_of<T>(s.dq);
+    a.dk = rows_of<T>(s.dk);
+    a.parts = s.dq_weight || s.dk_weight ? static_cast<float *>(s.workspace) : nullptr;
+    rows[2] = &s.dy_q, rows[3] = &s.dy_k, rows[4] = &s.dq, rows[5] = &s.dk;
+    count = 6;
+  } else {
+    a.yq = rows_of<T>(s.y_q);
+    a.yk = rows_of<T>(s.y_k);
+  }
+  int rc = TCU_DFT_OK;
+  if (a.total > 0) {
+    // the longest words that keep pairs of one kind together and lie aligned
+    int vp = 16 / (int)sizeof(T);
+    auto fits = [&](int n) {
+      if (s.dim / 2 % n || s.turned % n) return false;
+      for (int i = 0; i < count; ++i)
+        if (!rows_aligned(*rows[i], s.type, batches, s.rows, n * (int)sizeof(T))) return false;
+      return true;
+    };
+    while (vp > 1 && !fits(vp)) vp /= 2;
+    switch (vp) {
+      case 8:
+        if constexpr (sizeof(T) == 2) rc = by_order<T, 8>(s, a, grad, st);
+        break;
+      case 4: rc = by_order<T, 4>(s, a, grad, st); break;
+      case 2: rc = by_order<T, 2>(s, a, grad, st); break;
+      default: rc = by_order<T, 1>(s, a, grad, st);
+    }
+  }
+  if (rc || !grad) return rc;
+  Sum sums[2];
+  int n = 0;
+  if (s.dq_weight) sums[n++] = {s.dq_weight, a.parts, s.dim};
+  if (s.dk_weight) sums[n++] = {s.dk_weight, a.parts + s.dim, s.dim};
+  return n ? sum_parts(sums, n, a.total > 0 ? blocks_of(s, true) : 0, 2 * s.dim, st) : TCU_DFT_OK;
+}
+
+int check_sizes(const tcu_norm_rotate_args *a) {
+  if (!a || a->type < TCU_SEQ_F32 || a->type > TCU_SEQ_F16 || a->sequences < 0 || a->rows < 0 ||
+      a->heads < 1 || a->kv_heads < 1 || a->dim < 2 || a->dim % 2 || a->turned < 1 ||
+      a->turned > a->dim / 2 || !(a->eps >= 0))
+    return TCU_DFT_ERR_INVALID;
+  if (a->rows > kMostRows || a->dim > TCU_ATTN_MAX_NORM_DIM || a->heads > (1 << 20) ||
+      a->kv_heads > (1 << 20))
+    return TCU_DFT_ERR_UNSUPPORTED;
+  for (const tcu_seq_rows *r : {&a->q, &a->k, &a->y_q, &a->y_k, &a->dy_q, &a->dy_k, &a->dq, &a->dk})
+    if (!pitch_fits(a->rows, r->row_stride)) return TCU_DFT_ERR_UNSUPPORTED;
+  return TCU_DFT_OK;
+}
+
+bool any_rows(const tcu_norm_rotate_args &a) {
+  return a.rows > 0 && a.sequences + (a.offsets != nullptr) > 0;
+}
+
+bool inputs_ok(const tcu_norm_rotate_args &a) {
+  const int sz = type_size(a.type);
+  return f32_ok(a.rates) && opt_ok(a.q_weight, 4) && opt_ok(a.k_weight, 4) &&
+         opt_ok(a.offsets, 4) && opt_ok(a.positions, 4) && row_ok(a.q, sz) && row_ok(a.k, sz);
+}
+
+int by_type(const tcu_norm_rotate_args &a, bool grad, void *stream) {
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  switch (a.type) {
+    case TCU_SEQ_F32: return run<float>(a, grad, st);
+    case TCU_SEQ_BF16: return run<bf16>(a, grad, st);
+    default: return run<f16>(a, grad, st);
+  }
+}
+
+}  // namespace
+}  // namespace seq
+}  // namespace tcu
+
+using namespace tcu::seq;
+
+extern "C" int64_t tcu_norm_rotate_grad_workspace(const tcu_norm_rotate_args *a) {
+  if (check_sizes(a)) return -1;
+  return a->dq_weight || a->dk_weight ? blocks_of(*a, true) * 2 * a->dim * 4 : 0;
+}
+
+extern "C" int tcu_norm_rotate(const tcu_norm_rotate_args *a, void *stream) {
+  if (const int rc = check_sizes(a)) return rc;
+  if (!any_rows(*a)) return TCU_DFT_OK;
+  const int sz = type_size(a->type);
+  if (!inputs_ok(*a) || !row_ok(a->y_q, sz) || !row_ok(a->y_k, sz)) return TCU_DFT_ERR_INVALID;
+  return by_type(*a, false, stream);
+}
+
+extern "C" int tcu_norm_rotate_grad(const tcu_norm_rotate_args *a, void *stream) {
+  if (const int rc = check_sizes(a)) return rc;
+  if (!opt_ok(a->dq_weight, 4) || !opt_ok(a->dk_weight, 4)) return TCU_DFT_ERR_INVALID;
+  const int sz = type_size(a->type);
+  if (any_rows(*a)) {
+    const int64_t bytes = tcu_norm_rotate_grad_workspace(a);
+    if (!inputs_ok(*a) || !row_ok(a->dy_q, sz) || !row_ok(a->dy_k, sz) || !row_ok(a->dq, sz) ||
+        !row_ok(a->dk, sz) || a->workspace_bytes < bytes || (bytes && !f32_ok(a->workspace)))
+      return TCU_DFT_ERR_INVALID;
+  }
+  return by_type(*a, true, stream);
+}

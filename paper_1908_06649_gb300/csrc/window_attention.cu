@@ -1,0 +1,389 @@
+// window_attention.cu -- attention over a sliding window and a sequence's first
+// tokens, for prompts (include/tcu_attn.h); entry points and the filling of
+// caches.
+//
+// A block owns 128 query rows of one head and walks over the tiles of 128
+// keys that any of them sees, first tokens' tiles first, with one pass over
+// the data: S = Q K^T and O += P V on the tensor cores (tcgen05, accumulators
+// in tensor memory), P = exp2(c S - m) between them in registers, a row a
+// thread, m a running maximum.  O is brought to a new maximum only where that
+// rose by more than 8 (P stays below 2^8, sums below 2^39: fp32 holds them);
+// P goes back to tensor memory over S, in the rows' type.
+//
+// Products bound it (4 dim flops a visible pair and head) with exponentials
+// close by: a tile's two products are 1,050 cycles of the tensor pipe, its
+// 16,384 exponentials 1,024 of the special function unit.  Within a block the
+// products, the exponentials and the products wait for each other; two blocks
+// share an SM (256 columns of tensor memory and 96 KB of tiles each), and one's
+// products run under the other's exponentials.
+#include <algorithm>
+
+#include "attn_common.cuh"
+
+namespace tcu {
+namespace seq {
+namespace {
+
+constexpr int kRows = 128;  // of a tile of queries, and of keys
+constexpr int kSoft = 128;  // threads: a row each
+constexpr int kThreads = kSoft + 32;
+
+struct PromptMaps {
+  CUtensorMap q, k, v;
+};
+
+template <int DP>
+struct PromptShared {
+  uint8_t q[kTileBytes<DP, kRows>], k[kTileBytes<DP, kRows>], v[kTileBytes<DP, kRows>];
+  uint64_t full_k, full_v, scores, weights, done;
+  uint32_t tmem;
+  int low, sink_at, sink_end, failed;
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 2)
+    attend_kernel(const __grid_constant__ PromptMaps maps, const AttendArgs a, const Rows<T> y) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  PromptShared<DP> &s = *reinterpret_cast<PromptShared<DP> *>(raw);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int64_t id = blockIdx.x;
+  const int tile = (int)(id % a.q_tiles);
+  const int head = (int)(id / a.q_tiles % a.heads), batch = (int)(id / a.q_tiles / a.heads);
+  const int kv = head / (a.heads / a.kv_heads);
+  const uint32_t full_k = smem_u32(&s.full_k), full_v = smem_u32(&s.full_v),
+                 scores = smem_u32(&s.scores), weights = smem_u32(&s.weights),
+                 done = smem_u32(&s.done);
+  if (threadIdx.x == 0) {
+    mbar_init(full_k, 1);
+    mbar_init(full_v, 1);
+    mbar_init(scores, 1);
+    mbar_init(weights, kSoft);
+    mbar_init(done, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    s.low = INT32_MAX;
+    s.sink_end = 0;
+    s.failed = 0;
+  }
+  if (warp == kSoft / 32) tmem_alloc(smem_u32(&s.tmem), 256);
+  Seen seen{-1, INT32_MAX, 0, 0};
+  if (threadIdx.x < kSoft) seen = seen_by(a, (int64_t)tile * kRows + threadIdx.x);
+  fence_before_sync();
+  __syncthreads();
+  fence_after_sync();
+  // the key tiles: those of the window, and before them those of first tokens
+  if (threadIdx.x < kSoft) {
+    const int low = __reduce_min_sync(~0u, seen.lo);
+    if (lane == 0) atomicMin(&s.low, low);
+  }
+  __syncthreads();
+  const int first = s.low / kRows;  // s.low == INT32_MAX: no row is in a sequence
+  // only the sequence that the tile's first row continues begins before them
+  if (threadIdx.x < kSoft && seen.s0 < seen.s1 && seen.s0 < (int64_t)first * kRows) {
+    atomicMax(&s.sink_end, min(seen.s1, first * kRows));
+    s.sink_at = seen.s0 / kRows;
+  }
+  __syncthreads();
+  const uint32_t tmem = s.tmem, tS = tmem, tO = tmem + 128;
+  const bool any = s.low != INT32_MAX;
+  const int sink_tiles = s.sink_end > 0 ? (s.sink_end - 1) / kRows - s.sink_at + 1 : 0;
+  const int sink_first = sink_tiles ? s.sink_at : 0;
+  const int tiles = any ? sink_tiles + tile - first + 1 : 0;
+  const auto key_tile = [&](int t) {
+    return t < sink_tiles ? sink_first + t : first + t - sink_tiles;
+  };
+  const float c = a.scale * kLog2e;
+
+  if (warp == kSoft / 32) {
+    const uint32_t q = smem_u32(s.q), k = smem_u32(s.k), v = smem_u32(s.v);
+    constexpr uint32_t bytes = kTileBytes<DP, kRows>;
+    bool ok = true;
+    int keys = 1, values = 1;  // tiles asked for
+    if (tiles > 0 && elect_one()) {
+      mbar_expect_tx(full_k, 2 * bytes);
+      load_tile<DP, kRows>(q, &maps.q, head, tile * kRows, batch, full_k);
+      load_tile<DP, kRows>(k, &maps.k, kv, key_tile(0) * kRows, batch, full_k);
+      mbar_expect_tx(full_v, bytes);
+      load_tile<DP, kRows>(v, &maps.v, kv, key_tile(0) * kRows, batch, full_v);
+    }
+    __syncwarp();
+    for (int t = 0; t < tiles && ok; ++t) {
+      const uint32_t ph = t & 1;
+      ok = mbar_wait_bounded(full_k, ph);
+      // the scores take the place of weights that the last product has read
+      if (t > 0) ok = ok && mbar_wait_bounded(done, ph ^ 1);
+      if (!ok) break;
+      fence_after_sync();
+      if (elect_one()) {
+        product_rows<T, DP, kRows>(tS, q, k);
+        mma_commit(scores);
+        if (t > 0) {
+          mbar_expect_tx(full_v, bytes);
+          load_tile<DP, kRows>(v, &maps.v, kv, key_tile(t) * kRows, batch, full_v);
+        }
+      }
+      __syncwarp();
+      values = t + 1;
+      ok = mbar_wait_bounded(scores, ph);
+      if (ok && t + 1 < tiles) {
+        if (elect_one()) {
+          mbar_expect_tx(full_k, bytes);
+          load_tile<DP, kRows>(k, &maps.k, kv, key_tile(t + 1) * kRows, batch, full_k);
+        }
+        __syncwarp();
+        keys = t + 2;
+      }
+      ok = ok && mbar_wait_bounded(full_v, ph) && mbar_wait_bounded(weights, ph);
+      if (!ok) break;
+      fence_after_sync();
+      if (elect_one()) {
+        product_values<T, DP, kRows>(tO, tS, v, t > 0);
+        mma_commit(done);
+      }
+      __syncwarp();
+    }
+    if (!ok) {  // copies in flight end before the block does
+      s.failed = 1;
+      mbar_wait_bounded(full_k, (keys - 1) & 1);
+      mbar_wait_bounded(full_v, (values - 1) & 1);
+    }
+  } else {
+    const uint32_t mine = (uint32_t)(warp * 32) << 16;
+    // packed rows outside [begin, end) are in no sequence
+    const int begin = a.offsets ? a.offsets[0] : 0;
+    const int end = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int t = 0; t < tiles && ok; ++t) {
+      const uint32_t ph = t & 1;
+      const int j0 = key_tile(t) * kRows;
+      ok = mbar_wait_bounded(scores, ph);
+      if (!ok) break;
+      fence_after_sync();
+      const bool whole = __all_sync(~0u, seen.whole(j0, j0 + kRows));
+      // two walks over the scores: a row of them does not fit the registers
+      float top = -INFINITY, top1 = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 128; k += 64) {
+        float v[64];
+        tmem_ld32x2(tS + mine + k, tS + mine + k + 32, v);
+        if (whole) {
+#pragma unroll
+          for (int j = 0; j < 64; j += 2) {
+            top = fmaxf(top, v[j]);
+            top1 = fmaxf(top1, v[j + 1]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 64; ++j)
+            if (seen.at(j0 + k + j)) top = fmaxf(top, v[j]);
+        }
+      }
+      top = fmaxf(top, top1) * c;
+      const bool rise = top > m + 8.f || (m == -INFINITY && top > m);
+      const float now = rise ? top : m;
+      if (__any_sync(~0u, rise)) {
+        const float by = m == -INFINITY ? 0.f : exp2_fast(m - now);
+        l *= by;
+        if (t > 0) {
+#pragma unroll 1
+          for (int k = 0; k < DP; k += 16) {
+            float o[16];
+            tmem_ld16(tO + mine + k, o);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] *= by;
+            tmem_st16(tO + mine + k, o);
+          }
+        }
+        m = now;
+      }
+      const float off = m == -INFINITY ? 0.f : m;  // a row that has seen nothing yet
+      float sum = 0.f, sum1 = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float v[32];
+        uint32_t w[16];
+        tmem_ld32(tS + mine + 32 * k, v);
+        if (!whole) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = seen.at(j0 + 32 * k + j) ? v[j] : -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float p = exp2_fast(fmaf(v[2 * j], c, -off));
+          const float r = exp2_fast(fmaf(v[2 * j + 1], c, -off));
+          sum += p;
+          sum1 += r;
+          w[j] = pack2<T>(p, r);
+        }
+        tmem_st16u(tS + mine + 16 * k, w);
+      }
+      l += sum + sum1;
+      if (j0 + kRows > end || j0 < begin) {
+        ok = mbar_wait_bounded(full_v, ph);
+        int b, e;
+        if (!sequence_at(a, (int64_t)j0 + threadIdx.x, b, e))
+          clear_row<DP, kRows>(smem_u32(s.v), threadIdx.x);
+        fence_proxy_async_shared();
+      }
+      tmem_wait_st();
+      fence_before_sync();
+      mbar_arrive(weights);
+    }
+    if (tiles > 0) ok = ok && mbar_wait_bounded(done, (tiles - 1) & 1);
+    fence_after_sync();
+    const bool row = seen.i >= 0;
+    const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : l > 0.f ? 1.f / l : l;
+    T *to = y.at(batch, row ? seen.i : 0) + (int64_t)head * a.dim;
+    if (tiles > 0) {
+#pragma unroll 1
+      for (int k = 0; k < DP; k += 32) {
+        float o[32];
+        tmem_ld32(tO + mine + k, o);
+        if (row) store_values(to, k, a.dim, o, by);
+      }
+    }
+    if (row && a.lse)
+      a.lse[((int64_t)batch * a.rows + seen.i) * a.heads + head] = (m + log2f(l)) * kLn2;
+    fence_before_sync();
+  }
+  __syncthreads();
+  if (warp == kSoft / 32) tmem_dealloc(tmem, 256);
+}
+
+template <typename T, int DP>
+int prompt(const tcu_window_attention_args &s, cudaStream_t st) {
+  AttendArgs a = attend_args(s);
+  const int64_t batches = attn_batches(s);
+  a.q_tiles = (s.rows + kRows - 1) / kRows;
+  const int64_t blocks = a.q_tiles * s.heads * batches;
+  if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  PromptMaps maps;
+  if (!attn_map(&maps.q, s.q, s.type, batches, s.rows, s.heads, s.dim, kRows) ||
+      !attn_map(&maps.k, s.k, s.type, batches, s.rows, s.kv_heads, s.dim, kRows) ||
+      !attn_map(&maps.v, s.v, s.type, batches, s.rows, s.kv_heads, s.dim, kRows))
+    return TCU_DFT_ERR_CUDA;
+  constexpr int bytes = sizeof(PromptShared<DP>);
+  if (cudaFuncSetAttribute(attend_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return TCU_DFT_ERR_CUDA;
+  }
+  attend_kernel<T, DP><<<(unsigned)blocks, kThreads, bytes, st>>>(maps, a, rows_of<T>(s.y));
+  return launched();
+}
+
+// ------------------------------------------------------------------- caches
+struct FillArgs {
+  Rows<const uint4> k, v;  // rows in 16-byte words
+  uint4 *cache_k, *cache_v;
+  const int32_t *offsets, *slots;
+  int64_t rows, num_slots;
+  int sequences, words, window, sinks;
+};
+
+// A warp for each row of an entry: the last position of the sequence that
+// belongs there.
+__global__ void __launch_bounds__(128) fill_kernel(const FillArgs a) {
+  const int64_t held = (int64_t)a.sinks + a.window;
+  const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
+  if (r >= held) return;
+  for (int64_t s = blockIdx.y; s < a.sequences; s += gridDim.y) {
+    int64_t begin = 0, n = a.rows;
+    if (a.offsets) {
+      begin = max(0, a.offsets[s]);
+      n = min(a.rows, (int64_t)a.offsets[s + 1]) - begin;
+    }
+    const int64_t slot = a.slots ? a.slots[s] : s;
+    int64_t p = r;
+    if (r >= a.sinks && n > held) p = n - 1 - (n - 1 - r) % a.window;
+    if (p >= n || slot < 0 || slot >= a.num_slots) continue;
+    const int64_t b = a.offsets ? 0 : s;
+    const uint4 *k = a.k.at(b, (int)(begin + p)), *v = a.v.at(b, (int)(begin + p));
+    uint4 *to_k = a.cache_k + (slot * held + r) * a.words;
+    uint4 *to_v = a.cache_v + (slot * held + r) * a.words;
+    for (int i = threadIdx.x % 32; i < a.words; i += 32) to_k[i] = k[i], to_v[i] = v[i];
+  }
+}
+
+Rows<const uint4> words_of(const tcu_seq_rows &r) {
+  return {static_cast<const uint4 *>(r.ptr), r.batch_stride / 8, (int32_t)(r.row_stride / 8)};
+}
+
+}  // namespace
+
+int check_attention(const tcu_window_attention_args *a) {
+  if (!a || a->type < TCU_SEQ_F32 || a->type > TCU_SEQ_F16 || a->sequences < 0 || a->rows < 0 ||
+      a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->dim < 1 || a->window < 1 ||
+      a->sinks < 0 || !(a->scale > 0) || a->scale > 1e30f)
+    return TCU_DFT_ERR_INVALID;
+  if (a->type == TCU_SEQ_F32 || a->dim > TCU_ATTN_MAX_DIM || a->dim % 8 || a->rows > kMostRows ||
+      a->heads > (1 << 20))
+    return TCU_DFT_ERR_UNSUPPORTED;
+  for (const tcu_seq_rows *r : {&a->q, &a->k, &a->v, &a->y, &a->dy, &a->dq, &a->dk, &a->dv})
+    if (!pitch_fits(a->rows, r->row_stride)) return TCU_DFT_ERR_UNSUPPORTED;
+  return opt_ok(a->offsets, 4) && opt_ok(a->lse, 4) && opt_ok(a->slots, 4) &&
+                 opt_ok(a->positions, 4)
+             ? TCU_DFT_OK
+             : TCU_DFT_ERR_INVALID;
+}
+
+}  // namespace seq
+}  // namespace tcu
+
+using namespace tcu::seq;
+
+extern "C" int tcu_window_attention(const tcu_window_attention_args *a, void *stream) {
+  if (const int rc = check_attention(a)) return rc;
+  const int64_t batches = attn_batches(*a);
+  if (a->rows == 0 || batches == 0) return TCU_DFT_OK;
+  const int64_t qs = (int64_t)a->heads * a->dim, ks = (int64_t)a->kv_heads * a->dim;
+  if (!attn_rows_ok(a->q, batches, a->rows, qs) || !attn_rows_ok(a->k, batches, a->rows, ks) ||
+      !attn_rows_ok(a->v, batches, a->rows, ks) || !attn_rows_ok(a->y, batches, a->rows, qs))
+    return TCU_DFT_ERR_INVALID;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (a->type == TCU_SEQ_BF16)
+    return a->dim <= 64 ? prompt<bf16, 64>(*a, st) : prompt<bf16, 128>(*a, st);
+  return a->dim <= 64 ? prompt<f16, 64>(*a, st) : prompt<f16, 128>(*a, st);
+}
+
+extern "C" int tcu_window_cache(const tcu_window_attention_args *a, void *stream) {
+  if (const int rc = check_attention(a)) return rc;
+  if (a->num_slots < 0 || (!a->slots && a->num_slots < a->sequences)) return TCU_DFT_ERR_INVALID;
+  if (a->rows == 0 || a->sequences == 0 || a->num_slots == 0) return TCU_DFT_OK;
+  const int64_t batches = attn_batches(*a), ks = (int64_t)a->kv_heads * a->dim;
+  if (!attn_rows_ok(a->k, batches, a->rows, ks) || !attn_rows_ok(a->v, batches, a->rows, ks) ||
+      !a->cache_k || !a->cache_v || (uintptr_t)a->cache_k % 16 || (uintptr_t)a->cache_v % 16)
+    return TCU_DFT_ERR_INVALID;
+  const int64_t held = (int64_t)a->sinks + a->window;
+  const wide_int bytes = (wide_int)a->num_slots * held * ks * 2;
+  for (const void *c : {a->cache_k, a->cache_v}) {
+    for (const tcu_seq_rows *r : {&a->k, &a->v})
+      for (int64_t b = 0; b < batches; ++b)
+        if (over(c, bytes, static_cast<const char *>(r->ptr) + b * r->batch_stride * 2, ks * 2,
+                 a->rows, r->row_stride * 2))
+          return TCU_DFT_ERR_INVALID;
+    if (over(c, bytes, a->slots, (int64_t)a->sequences * 4) ||
+        over(c, bytes, a->offsets, ((int64_t)a->sequences + 1) * 4))
+      return TCU_DFT_ERR_INVALID;
+  }
+  if (over(a->cache_k, bytes, a->cache_v, 1) || over(a->cache_v, bytes, a->cache_k, 1))
+    return TCU_DFT_ERR_INVALID;
+  FillArgs f{};
+  f.k = words_of(a->k);
+  f.v = words_of(a->v);
+  f.cache_k = static_cast<uint4 *>(a->cache_k);
+  f.cache_v = static_cast<uint4 *>(a->cache_v);
+  f.offsets = a->offsets;
+  f.slots = a->slots;
+  f.rows = a->rows;
+  f.num_slots = a->num_slots;
+  f.sequences = a->sequences;
+  f.words = (int)(ks / 8);
+  f.window = a->window;
+  f.sinks = a->sinks;
+  // rows of an entry that no sequence of this length reaches need no block
+  const int64_t reach = std::min(held, a->rows);
+  const dim3 grid((unsigned)((reach + 3) / 4), (unsigned)std::min(a->sequences, 65535));
+  fill_kernel<<<grid, 128, 0, static_cast<cudaStream_t>(stream)>>>(f);
+  return launched();
+}

@@ -11,11 +11,12 @@ U = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 **
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 
 
-def close(got, want, name="", inner=2e-5):
+def close(got, want, name="", inner=2e-5, terms=None):
     """The 2-norm of the error is within u + inner of the result's, inner being
     what the arithmetic before the rounding may be off; a value may lie on the
     other side of a rounding boundary, 2 u of itself, plus 5 inner of the
-    result's root mean square."""
+    result's root mean square -- or, where the sums of the terms' sizes are
+    given, u and 2e-5 of them: what rounding each term by at most u can do."""
     assert got.shape == want.shape, (name, got.shape, want.shape)
     if not want.numel():
         return
@@ -26,7 +27,8 @@ def close(got, want, name="", inner=2e-5):
     norm = w.norm()
     assert err.norm() <= (u + inner) * norm + 1e-30, (name, float(err.norm() / norm))
     rms = norm / w.numel() ** 0.5
-    over = err - (2 * u * w.abs() + 5 * inner * rms)
+    each = 5 * inner * rms if terms is None else (u + 2e-5) * terms.detach() + 1e-4 * rms
+    over = err - (2 * u * w.abs() + each)
     # numbers below the type's normal range are off by its smallest step
     assert over.max() <= torch.finfo(got.dtype).smallest_normal * u, (name, float(over.max()), float(rms))
 
@@ -145,3 +147,30 @@ def attention(q, k, v, window, sinks=0, scale=None, offsets=None):
         y = y.index_put(where, (torch.softmax(score, -1) @ vs).transpose(0, 1))
         lse = lse.index_put(where, torch.logsumexp(score, -1).T)
     return y, lse
+
+
+def attention_terms(q, k, v, dy, window, sinks=0, scale=None, offsets=None):
+    """For each value of the gradients the sum of the sizes of its terms that
+    are rounded before they are added: ds = p (dp - delta) once, and delta =
+    dy.y in each product of y, for dq and dk; p for dv."""
+    scale = q.shape[-1] ** -0.5 if scale is None else scale
+    group = q.shape[-2] // k.shape[-2]
+    out = [torch.zeros_like(t) for t in (q, k, v)]
+    for _, at in spans(q, offsets):
+        n = q[at].shape[0]
+        if not n:
+            continue
+        i = torch.arange(n)
+        qs, dys = q[at].transpose(0, 1), dy[at].transpose(0, 1)
+        ks, vs = (x[at].transpose(0, 1).repeat_interleave(group, 0) for x in (k, v))
+        score = (scale * qs @ ks.transpose(1, 2)).masked_fill(
+            ~visible(i[:, None], i, window, sinks), -math.inf)
+        p = torch.softmax(score, -1)
+        y = p @ vs
+        dp = dys @ vs.transpose(1, 2)
+        size = p * ((dp - (dys * y).sum(-1, keepdim=True)).abs()
+                    + (dys * y).abs().sum(-1, keepdim=True)) * scale
+        out[0][at] = (size @ ks.abs()).transpose(0, 1)
+        for t, x in ((out[1], size.transpose(1, 2) @ qs.abs()), (out[2], p.transpose(1, 2) @ dys.abs())):
+            t[at] = x.unflatten(0, (-1, group)).sum(1).transpose(0, 1)
+    return out
