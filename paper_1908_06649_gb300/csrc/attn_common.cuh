@@ -27,14 +27,23 @@ struct AttendArgs {
   int sequences, heads, kv_heads, dim, window, sinks;
   float scale;
   int64_t q_tiles, k_tiles;
+  int chunk, chunks, sink_tiles;  // gradient: how the rows that see first tokens are split
 };
 
 // ---------------------------------------------------------------- visibility
+// The bits of [lo, hi) among 0..31.
+__device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
+  const auto below = [](int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; };
+  return below(hi) & ~below(lo);
+}
+
 // The keys that row i of a batch entry sees: [lo, i] and [s0, s1), s1 <= lo.
 struct Seen {
   int i, lo, s0, s1;
-  __device__ __forceinline__ bool at(int j) const {
-    return (j >= lo && j <= i) || (j >= s0 && j < s1);
+  // which of [j0, j0 + 32), a bit each: a test of a constant bit and a selection
+  // for each score, where bounds compared for each take ten times as long
+  __device__ __forceinline__ uint32_t bits(int j0) const {
+    return bits_between(lo - j0, i + 1 - j0) | bits_between(s0 - j0, s1 - j0);
   }
   // whether all of [j0, j1) is seen
   __device__ __forceinline__ bool whole(int j0, int j1) const { return j0 >= lo && j1 - 1 <= i; }
@@ -106,15 +115,19 @@ __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b)
                desc_sw128(b + k / 4 * ROWS_B * 128 + k % 4 * 32, 16), id, k > 0);
 }
 
-// D[128, DP] (+)= A B, A of 128 x ROWS_B 16-bit values in tensor memory, B a
-// tile of ROWS_B rows.
+// D[128, DP] (+)= A B, A of 128 x ROWS_B 16-bit values in tensor memory, two to
+// a column, B a tile of ROWS_B rows.  A's halves lie where the 32-bit values
+// lay that they were formed from, in the first half of their columns: who
+// writes one has read them itself.
 template <typename T, int DP, int ROWS_B>
 __device__ __forceinline__ void product_values(uint32_t d, uint32_t a, uint32_t b, bool add) {
   constexpr uint32_t id = idesc_16<T>(128, DP, true);
 #pragma unroll
   for (int k = 0; k < ROWS_B / 16; ++k)
-    mma_f16_ts(d, a + k * 8, desc_sw128(b + k * 16 * 128, ROWS_B * 128), id, add || k > 0);
+    mma_f16_ts(d, a + k / (ROWS_B / 32) * (ROWS_B / 2) + k % (ROWS_B / 32) * 8, desc_sw128(b + k * 16 * 128, ROWS_B * 128), id, add || k > 0);
 }
+
+__device__ __forceinline__ float2 splat(float v) { return make_float2(v, v); }
 
 template <typename T>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -151,13 +164,14 @@ template <int DP, int ROWS>
 constexpr uint32_t kTileBytes = DP * ROWS * 2;
 
 // Zeroes row r of a tile: what lies behind the last sequence, or before the
-// first, may be no number, and zero times that is none either.
+// first, may be no number, and zero times that is none either.  Two threads
+// take half of the row each.
 template <int DP, int ROWS>
-__device__ __forceinline__ void clear_row(uint32_t tile, int r) {
+__device__ __forceinline__ void clear_row(uint32_t tile, int r, int half) {
 #pragma unroll
   for (int c = 0; c < DP / 64; ++c)
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 4 * half; k < 4 * half + 4; ++k)
       asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + c * ROWS * 128 + r * 128 +
                                                                      k * 16),
                    "r"(0)

@@ -25,7 +25,7 @@ namespace seq {
 namespace {
 
 constexpr int kRows = 128;  // of a tile of queries, and of keys
-constexpr int kSoft = 128;  // threads: a row each
+constexpr int kSoft = 256;  // threads: half of a row each
 constexpr int kThreads = kSoft + 32;
 
 struct PromptMaps {
@@ -37,6 +37,7 @@ struct PromptShared {
   uint8_t q[kTileBytes<DP, kRows>], k[kTileBytes<DP, kRows>], v[kTileBytes<DP, kRows>];
   uint64_t full_k, full_v, scores, weights, done;
   uint32_t tmem;
+  float tops[2][2][kRows], sums[2][kRows];  // of half a row
   int low, sink_at, sink_end, failed;
 };
 
@@ -66,7 +67,8 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
   if (warp == kSoft / 32) tmem_alloc(smem_u32(&s.tmem), 256);
   Seen seen{-1, INT32_MAX, 0, 0};
-  if (threadIdx.x < kSoft) seen = seen_by(a, (int64_t)tile * kRows + threadIdx.x);
+  const int own = threadIdx.x % kRows;  // row
+  if (threadIdx.x < kSoft) seen = seen_by(a, (int64_t)tile * kRows + own);
   fence_before_sync();
   __syncthreads();
   fence_after_sync();
@@ -147,7 +149,8 @@ __global__ void __launch_bounds__(kThreads, 2)
       mbar_wait_bounded(full_v, (values - 1) & 1);
     }
   } else {
-    const uint32_t mine = (uint32_t)(warp * 32) << 16;
+    const int half = threadIdx.x / kRows;  // of the row: 64 keys, and as many outputs
+    const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
     // packed rows outside [begin, end) are in no sequence
     const int begin = a.offsets ? a.offsets[0] : 0;
     const int end = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
@@ -155,38 +158,40 @@ __global__ void __launch_bounds__(kThreads, 2)
     bool ok = true;
     for (int t = 0; t < tiles && ok; ++t) {
       const uint32_t ph = t & 1;
-      const int j0 = key_tile(t) * kRows;
+      const int j0 = key_tile(t) * kRows + 64 * half;
       ok = mbar_wait_bounded(scores, ph);
-      if (!ok) break;
       fence_after_sync();
-      const bool whole = __all_sync(~0u, seen.whole(j0, j0 + kRows));
-      // two walks over the scores: a row of them does not fit the registers
-      float top = -INFINITY, top1 = -INFINITY;
+      float v[64];
+      tmem_ld32x2(tS + mine + 64 * half, tS + mine + 64 * half + 32, v);
+      if (!__all_sync(~0u, seen.whole(j0, j0 + 64))) {
+        const uint32_t bits0 = seen.bits(j0), bits1 = seen.bits(j0 + 32);
 #pragma unroll
-      for (int k = 0; k < 128; k += 64) {
-        float v[64];
-        tmem_ld32x2(tS + mine + k, tS + mine + k + 32, v);
-        if (whole) {
-#pragma unroll
-          for (int j = 0; j < 64; j += 2) {
-            top = fmaxf(top, v[j]);
-            top1 = fmaxf(top1, v[j + 1]);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 64; ++j)
-            if (seen.at(j0 + k + j)) top = fmaxf(top, v[j]);
+        for (int j = 0; j < 32; ++j) {
+          v[j] = bits0 >> j & 1 ? v[j] : -INFINITY;
+          v[32 + j] = bits1 >> j & 1 ? v[32 + j] : -INFINITY;
         }
       }
-      top = fmaxf(top, top1) * c;
+      float top = v[0], top1 = v[1], top2 = v[2], top3 = v[3];
+#pragma unroll
+      for (int j = 4; j < 64; j += 4) {
+        top = fmaxf(top, v[j]);
+        top1 = fmaxf(top1, v[j + 1]);
+        top2 = fmaxf(top2, v[j + 2]);
+        top3 = fmaxf(top3, v[j + 3]);
+      }
+      top = fmaxf(fmaxf(top, top1), fmaxf(top2, top3));
+      s.tops[ph][half][own] = top;
+      // the row's other half
+      asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
+      top = fmaxf(top, s.tops[ph][half ^ 1][own]) * c;
       const bool rise = top > m + 8.f || (m == -INFINITY && top > m);
-      const float now = rise ? top : m;
       if (__any_sync(~0u, rise)) {
+        const float now = rise ? top : m;
         const float by = m == -INFINITY ? 0.f : exp2_fast(m - now);
         l *= by;
         if (t > 0) {
 #pragma unroll 1
-          for (int k = 0; k < DP; k += 16) {
+          for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 16) {
             float o[16];
             tmem_ld16(tO + mine + k, o);
 #pragma unroll
@@ -196,33 +201,25 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
         m = now;
       }
-      const float off = m == -INFINITY ? 0.f : m;  // a row that has seen nothing yet
-      float sum = 0.f, sum1 = 0.f;
+      // a row that has seen nothing yet has no maximum
+      const float2 off = splat(m == -INFINITY ? 0.f : -m), by = splat(c);
+      float2 sum = splat(0.f);
+      uint32_t w[32];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float v[32];
-        uint32_t w[16];
-        tmem_ld32(tS + mine + 32 * k, v);
-        if (!whole) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = seen.at(j0 + 32 * k + j) ? v[j] : -INFINITY;
-        }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float p = exp2_fast(fmaf(v[2 * j], c, -off));
-          const float r = exp2_fast(fmaf(v[2 * j + 1], c, -off));
-          sum += p;
-          sum1 += r;
-          w[j] = pack2<T>(p, r);
-        }
-        tmem_st16u(tS + mine + 16 * k, w);
+      for (int j = 0; j < 32; ++j) {
+        const float2 z = __ffma2_rn(make_float2(v[2 * j], v[2 * j + 1]), by, off);
+        const float2 p = make_float2(exp2_fast(z.x), exp2_fast(z.y));
+        sum = __fadd2_rn(sum, p);
+        w[j] = pack2<T>(p.x, p.y);
       }
-      l += sum + sum1;
-      if (j0 + kRows > end || j0 < begin) {
-        ok = mbar_wait_bounded(full_v, ph);
+      tmem_st16u(tS + mine + 64 * half, w);
+      tmem_st16u(tS + mine + 64 * half + 16, w + 16);
+      l += sum.x + sum.y;
+      if (key_tile(t) * kRows + kRows > end || key_tile(t) * kRows < begin) {
+        ok = ok && mbar_wait_bounded(full_v, ph);
         int b, e;
-        if (!sequence_at(a, (int64_t)j0 + threadIdx.x, b, e))
-          clear_row<DP, kRows>(smem_u32(s.v), threadIdx.x);
+        if (!sequence_at(a, (int64_t)key_tile(t) * kRows + own, b, e))
+          clear_row<DP, kRows>(smem_u32(s.v), own, half);
         fence_proxy_async_shared();
       }
       tmem_wait_st();
@@ -231,18 +228,21 @@ __global__ void __launch_bounds__(kThreads, 2)
     }
     if (tiles > 0) ok = ok && mbar_wait_bounded(done, (tiles - 1) & 1);
     fence_after_sync();
+    s.sums[half][own] = l;
+    asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
+    l = s.sums[0][own] + s.sums[1][own];
     const bool row = seen.i >= 0;
     const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : l > 0.f ? 1.f / l : l;
     T *to = y.at(batch, row ? seen.i : 0) + (int64_t)head * a.dim;
     if (tiles > 0) {
 #pragma unroll 1
-      for (int k = 0; k < DP; k += 32) {
+      for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 32) {
         float o[32];
         tmem_ld32(tO + mine + k, o);
         if (row) store_values(to, k, a.dim, o, by);
       }
     }
-    if (row && a.lse)
+    if (row && half == 0 && a.lse)
       a.lse[((int64_t)batch * a.rows + seen.i) * a.heads + head] = (m + log2f(l)) * kLn2;
     fence_before_sync();
   }

@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kRows = 128;  // of the block
 constexpr int kStep = 64;   // of a tile that it walks over
-constexpr int kSoft = 128;
+constexpr int kSoft = 256;  // threads that form weights: two for each row
 
 // ------------------------------------------------------------------- delta
 // delta = dy.y of each row and head, 16 lanes a head; for fp16 the largest
@@ -118,7 +118,8 @@ __global__ void __launch_bounds__(kSoft + 32, 2)
   }
   if (warp == kSoft / 32) tmem_alloc(smem_u32(&s.tmem), 256);
   Seen seen{-1, INT32_MAX, 0, 0};
-  if (threadIdx.x < kSoft) seen = seen_by(a, (int64_t)tile * kRows + threadIdx.x);
+  const int own = threadIdx.x % kRows;
+  if (threadIdx.x < kSoft) seen = seen_by(a, (int64_t)tile * kRows + own);
   fence_before_sync();
   __syncthreads();
   fence_after_sync();
@@ -206,7 +207,8 @@ __global__ void __launch_bounds__(kSoft + 32, 2)
       if (keys > 1) mbar_wait_bounded(full_k + 8 * (keys & 1), ((keys - 2) >> 1) & 1);
     }
   } else {
-    const uint32_t mine = (uint32_t)(warp * 32) << 16;
+    const int half = threadIdx.x / kRows;  // of the row: 32 keys, and half of its dq
+    const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
     const int begin = a.offsets ? a.offsets[0] : 0;
     const int end = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
     const float lift = lift_of(most);
@@ -223,28 +225,32 @@ __global__ void __launch_bounds__(kSoft + 32, 2)
       ok = mbar_wait_bounded(scores, ph);
       if (!ok) break;
       fence_after_sync();
-      const bool whole = __all_sync(~0u, seen.whole(j0, j0 + kStep));
+      const int j1 = j0 + 32 * half;
+      float v[64];
+      uint32_t w[16];
+      tmem_ld32x2(tS + mine + 32 * half, tP + mine + 32 * half, v);
+      const float2 by = splat(c), minus = splat(-lse), up = splat(lift), less = splat(-delta);
 #pragma unroll
-      for (int k = 0; k < kStep; k += 32) {
-        float v[64];
-        uint32_t w[16];
-        tmem_ld32x2(tS + mine + k, tP + mine + k, v);
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          float x = exp2_fast(fmaf(v[j], c, -lse)) * fmaf(v[32 + j], lift, -delta);
-          float y = exp2_fast(fmaf(v[j + 1], c, -lse)) * fmaf(v[33 + j], lift, -delta);
-          if (!whole) {
-            x = seen.at(j0 + k + j) ? x : 0.f;
-            y = seen.at(j0 + k + j + 1) ? y : 0.f;
-          }
-          w[j / 2] = pack2<T>(x, y);
-        }
-        tmem_st16u(tS + mine + k / 2, w);
+      for (int j = 0; j < 32; j += 2) {
+        const float2 z = __ffma2_rn(make_float2(v[j], v[j + 1]), by, minus);
+        const float2 d = __ffma2_rn(make_float2(v[32 + j], v[33 + j]), up, less);
+        const float2 x = __fmul2_rn(make_float2(exp2_fast(z.x), exp2_fast(z.y)), d);
+        v[j] = x.x;
+        v[j + 1] = x.y;
       }
+      if (!__all_sync(~0u, seen.whole(j1, j1 + 32))) {
+        const uint32_t bits = seen.bits(j1);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = bits >> j & 1 ? v[j] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
+      tmem_st16u(tS + mine + 32 * half, w);
       if (j0 + kStep > end || j0 < begin) {
         int b, e;
-        if (threadIdx.x < kStep && !sequence_at(a, (int64_t)j0 + threadIdx.x, b, e))
-          clear_row<DP, kStep>(smem_u32(s.k[t & 1]), threadIdx.x);
+        const int r = threadIdx.x / 2;
+        if (r < kStep && !sequence_at(a, (int64_t)j0 + r, b, e))
+          clear_row<DP, kStep>(smem_u32(s.k[t & 1]), r, threadIdx.x % 2);
         fence_proxy_async_shared();
       }
       tmem_wait_st();
@@ -253,16 +259,14 @@ __global__ void __launch_bounds__(kSoft + 32, 2)
     }
     if (tiles > 0) ok = ok && mbar_wait_bounded(done, (tiles - 1) & 1);
     fence_after_sync();
-    const int64_t i = (int64_t)tile * kRows + threadIdx.x;
+    const int64_t i = (int64_t)tile * kRows + own;
     const bool row = i < a.rows;
     const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : a.scale / lift;
     T *to = dq.at(batch, row ? (int)i : 0) + (int64_t)head * a.dim;
 #pragma unroll 1
-    for (int k = 0; k < DP; k += 32) {
+    for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 32) {
       float o[32];
-      if (tiles > 0) {
-        tmem_ld32(tQ + mine + k, o);
-      }
+      if (tiles > 0) tmem_ld32(tQ + mine + k, o);
       if (tiles == 0 || seen.i < 0) {  // rows of no sequence
 #pragma unroll
         for (int j = 0; j < 32; ++j) o[j] = 0.f;
@@ -286,27 +290,64 @@ template <int DP>
 struct KeyShared {
   uint8_t k[kTileBytes<DP, kRows>], v[kTileBytes<DP, kRows>];
   uint8_t q[kStages][kTileBytes<DP, kStep>], dy[kStages][kTileBytes<DP, kStep>];
-  // of the query rows of a tile: [half][turn]
-  float lse[2][2][kStep], delta[2][2][kStep];
-  int low[2][2][kStep], begin[2][2][kStep], sink_end[2][2][kStep];
+  float4 lse[2][2][kStep / 4], delta[2][2][kStep / 4];  // of a tile's query rows: [side][turn]
   uint64_t full_kv, full[kStages], scores[2], weights[2], done[2];
   uint32_t tmem;
-  int last, failed;
+  int last, begin, failed;
 };
 
-// Two halves of 128 threads take the tiles of queries in turn: while one half
-// forms weights, the tensor cores work on the other's tile.
-template <typename T, int DP>
+// A tile of queries of one head among those that a block walks over.
+struct QueryTile {
+  int head, at;
+  __device__ __forceinline__ void forward(int by, int first, int end) {
+    at += by;
+    while (at >= end) at -= end - first, ++head;
+  }
+};
+
+// Two sides of 256 threads take the tiles of queries in turn: while one forms
+// weights, the tensor cores work on the other's tile.  Of a side's threads two
+// share a key, 32 queries each.
+//
+// Most keys are seen from a window's rows, first tokens from all rows of
+// their sequence.  So that no block walks over more tiles than twice another,
+// those beyond the first multiple of `chunk` that is `chunk` tiles or more
+// behind the key tile go, `chunk` at a time, to blocks of a launch before
+// (kFar), whose sums the key tile's block adds to its own, in order.  A chunk
+// has far first tokens of one sequence at most, that of its first row.
+template <typename T, int DP, bool kFar>
 __global__ void __launch_bounds__(2 * kSoft + 32, 1)
     dkv_kernel(const __grid_constant__ KeyMaps maps, const AttendArgs a, const Rows<T> dk,
-               const Rows<T> dv, const int *most) {
+               const Rows<T> dv, const int *most, float *far) {
   extern __shared__ __align__(1024) uint8_t raw[];
   KeyShared<DP> &s = *reinterpret_cast<KeyShared<DP> *>(raw);
   const int warp = threadIdx.x / 32;
-  const int64_t id = blockIdx.x;
-  const int tile = (int)(id % a.k_tiles);
-  const int kv = (int)(id / a.k_tiles % a.kv_heads), batch = (int)(id / a.k_tiles / a.kv_heads);
+  int64_t id = blockIdx.x;
+  const int kv = (int)(id % a.kv_heads);
+  id /= a.kv_heads;
   const int group = a.heads / a.kv_heads;
+  int tile, batch, first, end;  // tiles of queries: [first, end)
+  float *slot = far;
+  if constexpr (kFar) {
+    const int nth = (int)(id % a.sink_tiles);
+    id /= a.sink_tiles;
+    const int x = (int)(id % a.chunks);
+    batch = (int)(id / a.chunks);
+    slot += (int64_t)blockIdx.x * 2 * kRows * DP;
+    int b, e;
+    if (!sequence_at(a, (int64_t)x * a.chunk * kStep, b, e)) return;
+    tile = b / kRows + nth;
+    if ((int64_t)tile * kRows >= (int64_t)b + a.sinks || x < (2 * tile + 2 * a.chunk - 1) / a.chunk)
+      return;
+    first = x * a.chunk;
+    end = (int)min((int64_t)first + a.chunk, ((int64_t)e + kStep - 1) / kStep);
+  } else {  // early tiles, which are seen from most rows, before late ones
+    const int64_t batches = gridDim.x / a.kv_heads / a.k_tiles;
+    batch = (int)(id % batches);
+    tile = (int)(id / batches);
+    first = tile * (kRows / kStep);
+    end = 0;
+  }
   const uint32_t full_kv = smem_u32(&s.full_kv), full = smem_u32(s.full),
                  scores = smem_u32(s.scores), weights = smem_u32(s.weights), done = smem_u32(s.done);
   if (threadIdx.x == 0) {
@@ -325,41 +366,51 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
   fence_before_sync();
   __syncthreads();
   fence_after_sync();
-  const int64_t j64 = (int64_t)tile * kRows + threadIdx.x % kSoft;
-  if (threadIdx.x < kSoft) {  // the end of the rows that see this key
-    int begin, end, past = 0;
-    if (sequence_at(a, j64, begin, end)) {
-      const int j = (int)j64;
-      past = j - begin < a.sinks || end - j <= a.window ? end : j + a.window;
-    }
-    past = __reduce_max_sync(~0u, past);
-    if (threadIdx.x % 32 == 0) atomicMax(&s.last, past);
+  // this thread's key is seen from rows [j, past)
+  const int64_t j64 = (int64_t)tile * kRows + threadIdx.x % kRows;
+  const int j = (int)min(j64, (int64_t)INT32_MAX);
+  int begin = 0, past = 0;
+  {
+    int e;
+    if (sequence_at(a, j64, begin, e))
+      past = j - begin < a.sinks || e - j <= a.window ? e : j + a.window;
   }
-  __syncthreads();
+  int far_from = 0, far_to = 0;  // chunks that other blocks have summed
+  if constexpr (!kFar) {
+    const int top = __reduce_max_sync(~0u, past);
+    if (threadIdx.x % 32 == 0) atomicMax(&s.last, top);
+    __syncthreads();
+    if (past > 0 && past == s.last) s.begin = begin;
+    end = max(first, (s.last + kStep - 1) / kStep);
+    __syncthreads();
+    if (a.chunk > 0) {
+      far_from = (first + 2 * a.chunk - 1) / a.chunk;
+      far_to = (end + a.chunk - 1) / a.chunk;
+      end = min(end, far_from * a.chunk);
+    }
+  }
   const uint32_t tmem = s.tmem, tV = tmem + 256, tK = tV + DP;
-  const int first = tile * (kRows / kStep);
-  const int q_tiles = max(0, (s.last + kStep - 1) / kStep - first);
-  const int64_t n = (int64_t)q_tiles * group;
+  const int64_t n = (int64_t)max(0, end - first) * group;
   const float c = a.scale * kLog2e;
-  const auto head_of = [&](int64_t t) { return kv * group + (int)(t / q_tiles); };
-  const auto row_of = [&](int64_t t) { return (first + (int)(t % q_tiles)) * kStep; };
 
   if (warp == 2 * kSoft / 32) {
     const uint32_t k = smem_u32(s.k), v = smem_u32(s.v), q = smem_u32(s.q), dy = smem_u32(s.dy);
     constexpr uint32_t bytes = kTileBytes<DP, kStep>;
     bool ok = true;
     int64_t asked = 0;
-    const auto ask = [&](int64_t t) {
-      const uint32_t stage = (uint32_t)t % kStages;
+    QueryTile next{kv * group, first};
+    const auto ask = [&]() {
+      const uint32_t stage = (uint32_t)asked % kStages;
       if (elect_one()) {
         mbar_expect_tx(full + 8 * stage, 2 * bytes);
-        load_tile<DP, kStep>(q + stage * bytes, &maps.q, head_of(t), row_of(t), batch,
+        load_tile<DP, kStep>(q + stage * bytes, &maps.q, next.head, next.at * kStep, batch,
                              full + 8 * stage);
-        load_tile<DP, kStep>(dy + stage * bytes, &maps.dy, head_of(t), row_of(t), batch,
+        load_tile<DP, kStep>(dy + stage * bytes, &maps.dy, next.head, next.at * kStep, batch,
                              full + 8 * stage);
       }
       __syncwarp();
-      asked = t + 1;
+      ++asked;
+      next.forward(1, first, end);
     };
     if (n > 0) {
       if (elect_one()) {
@@ -368,36 +419,36 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
         load_tile<DP, kRows>(v, &maps.v, kv, tile * kRows, batch, full_kv);
       }
       __syncwarp();
-      ask(0);
-      if (n > 1) ask(1);
+      ask();
+      if (n > 1) ask();
       ok = mbar_wait_bounded(full_kv, 0);
     }
     for (int64_t t = 0; n > 0 && t <= n && ok; ++t) {
       if (t < n) {
-        const uint32_t half = t & 1, stage = (uint32_t)t % kStages;
-        // the half's tensor memory and the tiles of t - 2 have been read
-        if (t >= 2) ok = mbar_wait_bounded(done + 8 * half, ((t - 2) >> 1) & 1);
-        if (ok && t + 2 < n) ask(t + 2);
+        const uint32_t side = t & 1, stage = (uint32_t)t % kStages;
+        // the side's tensor memory and the tiles of t - 2 have been read
+        if (t >= 2) ok = mbar_wait_bounded(done + 8 * side, ((t - 2) >> 1) & 1);
+        if (ok && t + 2 < n) ask();
         ok = ok && mbar_wait_bounded(full + 8 * stage, (uint32_t)(t / kStages) & 1);
         if (!ok) break;
         fence_after_sync();
         if (elect_one()) {
-          product_rows<T, DP, kStep>(tmem + 128 * half, k, q + stage * bytes);
-          product_rows<T, DP, kStep>(tmem + 128 * half + kStep, v, dy + stage * bytes);
-          mma_commit(scores + 8 * half);
+          product_rows<T, DP, kStep>(tmem + 128 * side, k, q + stage * bytes);
+          product_rows<T, DP, kStep>(tmem + 128 * side + kStep, v, dy + stage * bytes);
+          mma_commit(scores + 8 * side);
         }
         __syncwarp();
       }
       if (t > 0) {
         const int64_t u = t - 1;
-        const uint32_t half = u & 1, stage = (uint32_t)u % kStages;
-        ok = mbar_wait_bounded(weights + 8 * half, (uint32_t)(u >> 1) & 1);
+        const uint32_t side = u & 1, stage = (uint32_t)u % kStages;
+        ok = mbar_wait_bounded(weights + 8 * side, (uint32_t)(u >> 1) & 1);
         if (!ok) break;
         fence_after_sync();
         if (elect_one()) {
-          product_values<T, DP, kStep>(tV, tmem + 128 * half, dy + stage * bytes, u > 0);
-          product_values<T, DP, kStep>(tK, tmem + 128 * half + kStep, q + stage * bytes, u > 0);
-          mma_commit(done + 8 * half);
+          product_values<T, DP, kStep>(tV, tmem + 128 * side, dy + stage * bytes, u > 0);
+          product_values<T, DP, kStep>(tK, tmem + 128 * side + kStep, q + stage * bytes, u > 0);
+          mma_commit(done + 8 * side);
         }
         __syncwarp();
       }
@@ -409,108 +460,149 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
         mbar_wait_bounded(full + 8 * ((uint32_t)u % kStages), (uint32_t)(u / kStages) & 1);
     }
   } else {
-    const int half = threadIdx.x / kSoft, own = threadIdx.x % kSoft;
+    const int side = threadIdx.x / kSoft, own = threadIdx.x % kSoft;
+    const int half = own / kRows;  // of the tile's queries
     const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
-    const uint32_t tS = tmem + 128 * half + mine, tP = tS + kStep;
-    const int begin = a.offsets ? a.offsets[0] : 0;
-    const int end = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
-    const int j = (int)min(j64, (int64_t)INT32_MAX);
+    const uint32_t tS = tmem + 128 * side + 32 * half + mine, tP = tS + kStep;
+    const int inside = a.offsets ? a.offsets[0] : 0;  // packed rows outside are in no sequence
+    const int outside = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
     const float lift = lift_of(most);
-    // what the next tile's query rows bring, a row a thread
+    // what the next tile's query rows bring, a row a thread: asked for a tile
+    // ahead, and not touched before it is needed
     float lse = 0.f, delta = 0.f;
-    Seen seen{-1, INT32_MAX, 0, 0};
+    QueryTile next{kv * group, first};
     const auto fetch = [&](int64_t t) {
-      if (own >= kStep || t >= n) return;
-      seen = seen_by(a, (int64_t)row_of(t) + own);
-      lse = delta = 0.f;
-      if (seen.i >= 0) {
-        const int64_t at = ((int64_t)batch * a.rows + seen.i) * a.heads + head_of(t);
-        lse = a.lse[at] * kLog2e;
-        delta = a.delta[at] * lift;
+      const int64_t i = (int64_t)next.at * kStep + own;
+      if (own < kStep && t < n && i < a.rows) {
+        const int64_t at = ((int64_t)batch * a.rows + i) * a.heads + next.head;
+        lse = a.lse[at];
+        delta = a.delta[at];
       }
     };
-    fetch(half);
+    if (n > 0 && side) next.forward(1, first, end);
+    fetch(side);
     bool ok = true;
-    for (int64_t t = half; t < n; t += 2) {
+    for (int64_t t = side; t < n; t += 2) {
       const int turn = (t >> 1) & 1;
       if (own < kStep) {
-        s.lse[half][turn][own] = lse;
-        s.delta[half][turn][own] = delta;
-        s.low[half][turn][own] = seen.lo;
-        s.begin[half][turn][own] = seen.s0;
-        s.sink_end[half][turn][own] = seen.s1;
+        reinterpret_cast<float *>(s.lse[side][turn])[own] = -lse * kLog2e;
+        reinterpret_cast<float *>(s.delta[side][turn])[own] = -delta * lift;
       }
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "n"(kSoft) : "memory");
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + side), "n"(kSoft) : "memory");
+      const int i0 = next.at * kStep, i1 = i0 + 32 * half;
+      next.forward(2, first, end);
       fetch(t + 2);
-      const int i0 = row_of(t);
-      ok = mbar_wait_bounded(scores + 8 * half, (uint32_t)(t >> 1) & 1);
+      ok = mbar_wait_bounded(scores + 8 * side, (uint32_t)(t >> 1) & 1);
       if (!ok) break;
       fence_after_sync();
-      // rows see more from below as they come: the last one's bound is the highest
-      const bool whole = __all_sync(~0u, j <= i0 && j >= s.low[half][turn][kStep - 1]);
+      float v[64];
+      tmem_ld32x2(tS, tP, v);
+      const float2 by = splat(c), up = splat(lift);
 #pragma unroll
-      for (int k = 0; k < kStep; k += 32) {
-        float v[64];
-        uint32_t w[16], d[16];
-        tmem_ld32x2(tS + k, tP + k, v);
+      for (int i = 0; i < 32; i += 4) {
+        const float4 l = s.lse[side][turn][8 * half + i / 4], d = s.delta[side][turn][8 * half + i / 4];
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+          const float2 z = __ffma2_rn(make_float2(v[i + k], v[i + k + 1]), by,
+                                      k ? make_float2(l.z, l.w) : make_float2(l.x, l.y));
+          const float2 x = __ffma2_rn(make_float2(v[32 + i + k], v[33 + i + k]), up,
+                                      k ? make_float2(d.z, d.w) : make_float2(d.x, d.y));
+          const float2 p = make_float2(exp2_fast(z.x), exp2_fast(z.y)), ds = __fmul2_rn(p, x);
+          v[i + k] = p.x;
+          v[i + k + 1] = p.y;
+          v[32 + i + k] = ds.x;
+          v[33 + i + k] = ds.y;
+        }
+      }
+      if (!__all_sync(~0u, j <= i1 && i1 + 32 <= past)) {
+        const uint32_t bits = bits_between(j - i1, past - i1);
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-          const int r = k + i;
-          float p = exp2_fast(fmaf(v[i], c, -s.lse[half][turn][r]));
-          float x = p * fmaf(v[32 + i], lift, -s.delta[half][turn][r]);
-          if (!whole) {
-            const bool at = (j >= s.low[half][turn][r] && j <= i0 + r) ||
-                            (j >= s.begin[half][turn][r] && j < s.sink_end[half][turn][r]);
-            p = at ? p : 0.f;
-            x = at ? x : 0.f;
-          }
-          v[i] = p;
-          v[32 + i] = x;
+          v[i] = bits >> i & 1 ? v[i] : 0.f;
+          v[32 + i] = bits >> i & 1 ? v[32 + i] : 0.f;
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          w[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
-          d[i] = pack2<T>(v[32 + 2 * i], v[33 + 2 * i]);
-        }
-        tmem_st16u(tS + k / 2, w);
-        tmem_st16u(tP + k / 2, d);
       }
-      if (i0 + kStep > end || i0 < begin) {
+      uint32_t w[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) w[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+      tmem_st16u(tS, w);
+      tmem_st16u(tP, w + 16);
+      if (i0 + kStep > outside || i0 < inside) {
         int b, e;
-        if (own < kStep && !sequence_at(a, (int64_t)i0 + own, b, e)) {
-          clear_row<DP, kStep>(smem_u32(s.q[t % kStages]), own);
-          clear_row<DP, kStep>(smem_u32(s.dy[t % kStages]), own);
-        }
+        const int r = own / 4, of = own % 4;
+        if (!sequence_at(a, (int64_t)i0 + r, b, e))
+          clear_row<DP, kStep>(smem_u32(of < 2 ? s.q[t % kStages] : s.dy[t % kStages]), r, of % 2);
         fence_proxy_async_shared();
       }
       tmem_wait_st();
       fence_before_sync();
-      mbar_arrive(weights + 8 * half);
+      mbar_arrive(weights + 8 * side);
     }
     // all products: the last tile's after the one's before, as a barrier may be
     // waited for only one phase ahead
     if (n > 1) ok = ok && mbar_wait_bounded(done + 8 * (n & 1), (uint32_t)((n - 2) >> 1) & 1);
     if (n > 0) ok = ok && mbar_wait_bounded(done + 8 * ((n - 1) & 1), (uint32_t)((n - 1) >> 1) & 1);
     fence_after_sync();
-    const bool row = j64 < a.rows;
-    const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : half ? a.scale / lift : 1.f;
-    T *to = (half ? dk : dv).at(batch, row ? j : 0) + (int64_t)kv * a.dim;
-    int b, e;
-    const bool in = sequence_at(a, j64, b, e);
+    // side 0 stores dv, side 1 dk, each thread half of a row
+    const int r = own % kRows;
+    const float bad = !ok || s.failed ? __int_as_float(0x7fffffff) : 1.f;
+    const float by = bad * (side ? a.scale / lift : 1.f);
+    const bool in = past > 0;
+    T *to = (side ? dk : dv).at(batch, j64 < a.rows ? j : 0) + (int64_t)kv * a.dim;
+    const int nth = kFar || !in ? 0 : tile - s.begin / kRows;
 #pragma unroll 1
-    for (int k = 0; k < DP; k += 32) {
+    for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 32) {
       float o[32];
-      if (n > 0) tmem_ld32((half ? tK : tV) + mine + k, o);
+      if (n > 0) tmem_ld32((side ? tK : tV) + mine + k, o);
       if (n == 0 || !in) {  // rows of no sequence
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = 0.f;
       }
-      if (row) store_values(to, k, a.dim, o, by);
+      const int64_t at = ((int64_t)side * kRows + r) * DP + k;
+      if constexpr (kFar) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+          *reinterpret_cast<float4 *>(slot + at + i) =
+              make_float4(o[i] * bad, o[i + 1] * bad, o[i + 2] * bad, o[i + 3] * bad);
+        continue;
+      }
+      if (in)
+        for (int x = far_from; x < far_to; ++x) {
+          const float *from = far + (((((int64_t)batch * a.chunks + x) * a.sink_tiles + nth) *
+                                      a.kv_heads + kv) * 2 * kRows * DP) + at;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 f = *reinterpret_cast<const float4 *>(from + i);
+            o[i] += f.x, o[i + 1] += f.y, o[i + 2] += f.z, o[i + 3] += f.w;
+          }
+        }
+      if (j64 < a.rows) store_values(to, k, a.dim, o, by);
     }
     fence_before_sync();
   }
   __syncthreads();
   if (warp == 2 * kSoft / 32) tmem_dealloc(tmem, 512);
+}
+
+// Tiles of queries to a chunk: what a key outside the first tokens is seen
+// from, 16 at least; 0 where nothing is split.  Past 256 first tokens most
+// blocks walk over a whole sequence, and need not be made alike.
+void split_rows(const tcu_window_attention_args &s, AttendArgs &a) {
+  const int64_t tiles = (s.rows + kStep - 1) / kStep;
+  const int64_t chunk = std::max<int64_t>(16, ((int64_t)a.window + kRows + kStep - 1) / kStep + 1);
+  a.chunk = a.chunks = a.sink_tiles = 0;
+  if (a.sinks == 0 || a.sinks > 256 || tiles <= chunk) return;
+  a.chunk = (int)chunk;
+  a.chunks = (int)((tiles + chunk - 1) / chunk);
+  a.sink_tiles = (a.sinks + kRows - 1) / kRows + (s.offsets ? 1 : 0);
+}
+int padded_dim(int dim) { return dim <= 64 ? 64 : 128; }
+// Floats of workspace: delta, then the largest |dy|, then the far sums, 16-byte aligned.
+int64_t far_offset(const tcu_window_attention_args &s) {
+  return (attn_batches(s) * s.rows * s.heads + 1 + 3) / 4 * 4;
+}
+int64_t far_blocks(const tcu_window_attention_args &s, const AttendArgs &a) {
+  return attn_batches(s) * a.chunks * a.sink_tiles * s.kv_heads;
 }
 
 template <typename K>
@@ -543,8 +635,13 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
       !map(&km.q, s.q, s.heads, kStep) || !map(&km.dy, s.dy, s.heads, kStep) ||
       !map(&km.k, s.k, s.kv_heads, kRows) || !map(&km.v, s.v, s.kv_heads, kRows))
     return TCU_DFT_ERR_CUDA;
-  if (!shared_bytes(dq_kernel<T, DP>, sizeof(QueryShared<DP>)) ||
-      !shared_bytes(dkv_kernel<T, DP>, sizeof(KeyShared<DP>)))
+  split_rows(s, a);
+  const int64_t far = far_blocks(s, a);
+  if (far > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  float *sums = delta + far_offset(s);
+  constexpr int q_bytes = sizeof(QueryShared<DP>), k_bytes = sizeof(KeyShared<DP>);
+  if (!shared_bytes(dq_kernel<T, DP>, q_bytes) || !shared_bytes(dkv_kernel<T, DP, false>, k_bytes) ||
+      !shared_bytes(dkv_kernel<T, DP, true>, k_bytes))
     return TCU_DFT_ERR_CUDA;
   const unsigned blocks = (unsigned)std::min<int64_t>((total + 15) / 16, 16 * (int64_t)num_sms());
   if (most && cudaMemsetAsync(most, 0, sizeof(int), st) != cudaSuccess) {
@@ -554,10 +651,15 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
   delta_kernel<T><<<blocks, 256, 0, st>>>(rows_of<const T>(s.y), rows_of<const T>(s.dy), delta, most,
                                           a, total);
   if (const int rc = launched()) return rc;
-  dkv_kernel<T, DP><<<(unsigned)k_blocks, 2 * kSoft + 32, sizeof(KeyShared<DP>), st>>>(
-      km, a, rows_of<T>(s.dk), rows_of<T>(s.dv), most);
+  if (far > 0) {
+    dkv_kernel<T, DP, true><<<(unsigned)far, 2 * kSoft + 32, k_bytes, st>>>(
+        km, a, rows_of<T>(s.dk), rows_of<T>(s.dv), most, sums);
+    if (const int rc = launched()) return rc;
+  }
+  dkv_kernel<T, DP, false><<<(unsigned)k_blocks, 2 * kSoft + 32, k_bytes, st>>>(
+      km, a, rows_of<T>(s.dk), rows_of<T>(s.dv), most, sums);
   if (const int rc = launched()) return rc;
-  dq_kernel<T, DP><<<(unsigned)q_blocks, kSoft + 32, sizeof(QueryShared<DP>), st>>>(
+  dq_kernel<T, DP><<<(unsigned)q_blocks, kSoft + 32, q_bytes, st>>>(
       qm, a, rows_of<T>(s.dq), most);
   return launched();
 }
@@ -570,7 +672,9 @@ using namespace tcu::seq;
 
 extern "C" int64_t tcu_window_attention_grad_workspace(const tcu_window_attention_args *a) {
   if (check_attention(a)) return -1;
-  return (attn_batches(*a) * a->rows * a->heads + 1) * 4;
+  AttendArgs g = attend_args(*a);
+  split_rows(*a, g);
+  return 4 * (far_offset(*a) + far_blocks(*a, g) * 2 * kRows * padded_dim(a->dim));
 }
 
 extern "C" int tcu_window_attention_grad(const tcu_window_attention_args *a, void *stream) {
@@ -582,7 +686,8 @@ extern "C" int tcu_window_attention_grad(const tcu_window_attention_args *a, voi
     if (!attn_rows_ok(*r, batches, a->rows, qs)) return TCU_DFT_ERR_INVALID;
   for (const tcu_seq_rows *r : {&a->k, &a->v, &a->dk, &a->dv})
     if (!attn_rows_ok(*r, batches, a->rows, ks)) return TCU_DFT_ERR_INVALID;
-  if (!a->lse || a->workspace_bytes < tcu_window_attention_grad_workspace(a) || !f32_ok(a->workspace))
+  if (!a->lse || a->workspace_bytes < tcu_window_attention_grad_workspace(a) || !f32_ok(a->workspace) ||
+      (uintptr_t)a->workspace % 16)
     return TCU_DFT_ERR_INVALID;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (a->type == TCU_SEQ_BF16)

@@ -81,6 +81,19 @@ def test_packed(tcu, dtype, kind, total, dim, window, sinks):
 
 
 @gpu
+@pytest.mark.parametrize("lengths,window,sinks", [
+    ([2600], 100, 3), ([700, 0, 1990, 50], 60, 130), ([100, 2300], 900, 4), ([1, 3000, 1], 30, 256),
+    ([2500], 20, 300)])
+def test_first_tokens_of_long_sequences(tcu, lengths, window, sinks):
+    """Gradients of keys that thousands of rows see, which blocks of their own
+    sum in part."""
+    a, dy = inputs(torch.bfloat16, (sum(lengths),), 2, 1, 64)
+    check(tcu, a, dy, window, sinks, offsets=offsets_of(lengths))
+    if len(lengths) == 1:
+        check(tcu, {n: t[None] for n, t in a.items()}, dy[None], window, sinks)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", HALF)
 def test_large_scores_and_scales(tcu, dtype):
     """Scores up to some hundreds: the running maximum rises again and again."""
