@@ -24,20 +24,21 @@ namespace tcu {
 namespace seq {
 namespace {
 
-constexpr int kRows = 128;  // of a tile of queries, and of keys
-constexpr int kSoft = 256;  // threads: half of a row each
+constexpr int kRows = 128;  // of a tile of queries
+constexpr int kStep = 64;   // of a tile of keys
+constexpr int kSoft = 128;  // threads that form weights: a row each
 constexpr int kThreads = kSoft + 32;
 
 struct PromptMaps {
-  CUtensorMap q, k, v;
+  CUtensorMap q, k, v;  // k and v in boxes of kStep rows
 };
 
 template <int DP>
 struct PromptShared {
-  uint8_t q[kTileBytes<DP, kRows>], k[kTileBytes<DP, kRows>], v[kTileBytes<DP, kRows>];
-  uint64_t full_k, full_v, scores, weights, done;
+  uint8_t q[kTileBytes<DP, kRows>];
+  uint8_t k[2][kTileBytes<DP, kStep>], v[2][kTileBytes<DP, kStep>];
+  uint64_t full_k[2], full_v[2], scores[2], weights[2], done;
   uint32_t tmem;
-  float tops[2][2][kRows], sums[2][kRows];  // of half a row
   int low, sink_at, sink_end, failed;
 };
 
@@ -51,14 +52,16 @@ __global__ void __launch_bounds__(kThreads, 2)
   const int tile = (int)(id % a.q_tiles);
   const int head = (int)(id / a.q_tiles % a.heads), batch = (int)(id / a.q_tiles / a.heads);
   const int kv = head / (a.heads / a.kv_heads);
-  const uint32_t full_k = smem_u32(&s.full_k), full_v = smem_u32(&s.full_v),
-                 scores = smem_u32(&s.scores), weights = smem_u32(&s.weights),
+  const uint32_t full_k = smem_u32(s.full_k), full_v = smem_u32(s.full_v),
+                 scores = smem_u32(s.scores), weights = smem_u32(s.weights),
                  done = smem_u32(&s.done);
   if (threadIdx.x == 0) {
-    mbar_init(full_k, 1);
-    mbar_init(full_v, 1);
-    mbar_init(scores, 1);
-    mbar_init(weights, kSoft);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(full_k + 8 * i, 1);
+      mbar_init(full_v + 8 * i, 1);
+      mbar_init(scores + 8 * i, 1);
+      mbar_init(weights + 8 * i, kSoft);
+    }
     mbar_init(done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.low = INT32_MAX;
@@ -67,8 +70,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
   if (warp == kSoft / 32) tmem_alloc(smem_u32(&s.tmem), 256);
   Seen seen{-1, INT32_MAX, 0, 0};
-  const int own = threadIdx.x % kRows;  // row
-  if (threadIdx.x < kSoft) seen = seen_by(a, (int64_t)tile * kRows + own);
+  if (threadIdx.x < kSoft) seen = seen_by(a, (int64_t)tile * kRows + threadIdx.x);
   fence_before_sync();
   __syncthreads();
   fence_after_sync();
@@ -78,91 +80,97 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (lane == 0) atomicMin(&s.low, low);
   }
   __syncthreads();
-  const int first = s.low / kRows;  // s.low == INT32_MAX: no row is in a sequence
+  const int first = s.low / kStep;  // s.low == INT32_MAX: no row is in a sequence
   // only the sequence that the tile's first row continues begins before them
-  if (threadIdx.x < kSoft && seen.s0 < seen.s1 && seen.s0 < (int64_t)first * kRows) {
-    atomicMax(&s.sink_end, min(seen.s1, first * kRows));
-    s.sink_at = seen.s0 / kRows;
+  if (threadIdx.x < kSoft && seen.s0 < seen.s1 && seen.s0 < (int64_t)first * kStep) {
+    atomicMax(&s.sink_end, min(seen.s1, first * kStep));
+    s.sink_at = seen.s0 / kStep;
   }
   __syncthreads();
-  const uint32_t tmem = s.tmem, tS = tmem, tO = tmem + 128;
+  const uint32_t tmem = s.tmem, tO = tmem + 2 * kStep;
   const bool any = s.low != INT32_MAX;
-  const int sink_tiles = s.sink_end > 0 ? (s.sink_end - 1) / kRows - s.sink_at + 1 : 0;
+  const int sink_tiles = s.sink_end > 0 ? (s.sink_end - 1) / kStep - s.sink_at + 1 : 0;
   const int sink_first = sink_tiles ? s.sink_at : 0;
-  const int tiles = any ? sink_tiles + tile - first + 1 : 0;
-  const auto key_tile = [&](int t) {
-    return t < sink_tiles ? sink_first + t : first + t - sink_tiles;
+  const int last = (int)min((int64_t)tile * 2 + 1, (a.rows - 1) / kStep);
+  const int tiles = any ? sink_tiles + last - first + 1 : 0;
+  const auto key_row = [&](int t) {
+    return (t < sink_tiles ? sink_first + t : first + t - sink_tiles) * kStep;
   };
   const float c = a.scale * kLog2e;
 
   if (warp == kSoft / 32) {
     const uint32_t q = smem_u32(s.q), k = smem_u32(s.k), v = smem_u32(s.v);
-    constexpr uint32_t bytes = kTileBytes<DP, kRows>;
+    constexpr uint32_t bytes = kTileBytes<DP, kStep>;
     bool ok = true;
-    int keys = 1, values = 1;  // tiles asked for
-    if (tiles > 0 && elect_one()) {
-      mbar_expect_tx(full_k, 2 * bytes);
-      load_tile<DP, kRows>(q, &maps.q, head, tile * kRows, batch, full_k);
-      load_tile<DP, kRows>(k, &maps.k, kv, key_tile(0) * kRows, batch, full_k);
-      mbar_expect_tx(full_v, bytes);
-      load_tile<DP, kRows>(v, &maps.v, kv, key_tile(0) * kRows, batch, full_v);
-    }
-    __syncwarp();
-    for (int t = 0; t < tiles && ok; ++t) {
-      const uint32_t ph = t & 1;
-      ok = mbar_wait_bounded(full_k, ph);
-      // the scores take the place of weights that the last product has read
-      if (t > 0) ok = ok && mbar_wait_bounded(done, ph ^ 1);
-      if (!ok) break;
-      fence_after_sync();
+    int keys = 0, values = 0;  // tiles asked for
+    const auto ask = [&](const CUtensorMap *map, uint32_t to, uint32_t full, int &count, bool with_q) {
+      if (count >= tiles) return;
+      const uint32_t stage = count & 1;
       if (elect_one()) {
-        product_rows<T, DP, kRows>(tS, q, k);
-        mma_commit(scores);
-        if (t > 0) {
-          mbar_expect_tx(full_v, bytes);
-          load_tile<DP, kRows>(v, &maps.v, kv, key_tile(t) * kRows, batch, full_v);
-        }
+        mbar_expect_tx(full + 8 * stage, bytes + (with_q ? kTileBytes<DP, kRows> : 0));
+        if (with_q) load_tile<DP, kRows>(q, &maps.q, head, tile * kRows, batch, full);
+        load_tile<DP, kStep>(to + stage * bytes, map, kv, key_row(count), batch, full + 8 * stage);
       }
       __syncwarp();
-      values = t + 1;
-      ok = mbar_wait_bounded(scores, ph);
-      if (ok && t + 1 < tiles) {
+      ++count;
+    };
+    ask(&maps.k, k, full_k, keys, true);
+    ask(&maps.k, k, full_k, keys, false);
+    ask(&maps.v, v, full_v, values, false);
+    ask(&maps.v, v, full_v, values, false);
+    // scores run a tile ahead of the weights: while those of one are formed,
+    // the next tile's are multiplied
+    for (int t = -1; t < tiles && ok; ++t) {
+      const uint32_t stage = t & 1, other = stage ^ 1;
+      if (t + 1 < tiles) {
+        ok = mbar_wait_bounded(full_k + 8 * other, ((t + 1) >> 1) & 1);
+        // they take the place of weights that the product of t - 1 has read
+        if (t > 0) {
+          ok = ok && mbar_wait_bounded(done, (t - 1) & 1);
+          if (ok) ask(&maps.v, v, full_v, values, false);
+        }
+        if (!ok) break;
+        fence_after_sync();
         if (elect_one()) {
-          mbar_expect_tx(full_k, bytes);
-          load_tile<DP, kRows>(k, &maps.k, kv, key_tile(t + 1) * kRows, batch, full_k);
+          product_rows<T, DP, kStep>(tmem + other * kStep, q, k + other * bytes);
+          mma_commit(scores + 8 * other);
         }
         __syncwarp();
-        keys = t + 2;
       }
-      ok = ok && mbar_wait_bounded(full_v, ph) && mbar_wait_bounded(weights, ph);
+      if (t < 0) continue;
+      ok = mbar_wait_bounded(scores + 8 * stage, (t >> 1) & 1);
+      if (ok) ask(&maps.k, k, full_k, keys, false);
+      ok = ok && mbar_wait_bounded(full_v + 8 * stage, (t >> 1) & 1) &&
+           mbar_wait_bounded(weights + 8 * stage, (t >> 1) & 1);
       if (!ok) break;
       fence_after_sync();
       if (elect_one()) {
-        product_values<T, DP, kRows>(tO, tS, v, t > 0);
+        product_values<T, DP, kStep>(tO, tmem + stage * kStep, v + stage * bytes, t > 0);
         mma_commit(done);
       }
       __syncwarp();
     }
     if (!ok) {  // copies in flight end before the block does
       s.failed = 1;
-      mbar_wait_bounded(full_k, (keys - 1) & 1);
-      mbar_wait_bounded(full_v, (values - 1) & 1);
+      for (int i = 1; i <= 2; ++i) {
+        if (keys >= i) mbar_wait_bounded(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
+        if (values >= i) mbar_wait_bounded(full_v + 8 * ((values - i) & 1), ((values - i) >> 1) & 1);
+      }
     }
   } else {
-    const int half = threadIdx.x / kRows;  // of the row: 64 keys, and as many outputs
-    const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
+    const uint32_t mine = (uint32_t)(warp * 32) << 16;
     // packed rows outside [begin, end) are in no sequence
     const int begin = a.offsets ? a.offsets[0] : 0;
     const int end = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     for (int t = 0; t < tiles && ok; ++t) {
-      const uint32_t ph = t & 1;
-      const int j0 = key_tile(t) * kRows + 64 * half;
-      ok = mbar_wait_bounded(scores, ph);
+      const int stage = t & 1, ph = (t >> 1) & 1, j0 = key_row(t);
+      const uint32_t tS = tmem + mine + kStep * stage;
+      ok = mbar_wait_bounded(scores + 8 * stage, ph);
       fence_after_sync();
       float v[64];
-      tmem_ld32x2(tS + mine + 64 * half, tS + mine + 64 * half + 32, v);
+      tmem_ld32x2(tS, tS + 32, v);
       if (!__all_sync(~0u, seen.whole(j0, j0 + 64))) {
         const uint32_t bits0 = seen.bits(j0), bits1 = seen.bits(j0 + 32);
 #pragma unroll
@@ -179,19 +187,17 @@ __global__ void __launch_bounds__(kThreads, 2)
         top2 = fmaxf(top2, v[j + 2]);
         top3 = fmaxf(top3, v[j + 3]);
       }
-      top = fmaxf(fmaxf(top, top1), fmaxf(top2, top3));
-      s.tops[ph][half][own] = top;
-      // the row's other half
-      asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
-      top = fmaxf(top, s.tops[ph][half ^ 1][own]) * c;
+      top = fmaxf(fmaxf(top, top1), fmaxf(top2, top3)) * c;
       const bool rise = top > m + 8.f || (m == -INFINITY && top > m);
       if (__any_sync(~0u, rise)) {
         const float now = rise ? top : m;
         const float by = m == -INFINITY ? 0.f : exp2_fast(m - now);
         l *= by;
         if (t > 0) {
+          ok = ok && mbar_wait_bounded(done, (t - 1) & 1);
+          fence_after_sync();
 #pragma unroll 1
-          for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 16) {
+          for (int k = 0; k < DP; k += 16) {
             float o[16];
             tmem_ld16(tO + mine + k, o);
 #pragma unroll
@@ -212,37 +218,38 @@ __global__ void __launch_bounds__(kThreads, 2)
         sum = __fadd2_rn(sum, p);
         w[j] = pack2<T>(p.x, p.y);
       }
-      tmem_st16u(tS + mine + 64 * half, w);
-      tmem_st16u(tS + mine + 64 * half + 16, w + 16);
+      tmem_st16u(tS, w);
+      tmem_st16u(tS + 32, w + 16);
       l += sum.x + sum.y;
-      if (key_tile(t) * kRows + kRows > end || key_tile(t) * kRows < begin) {
-        ok = ok && mbar_wait_bounded(full_v, ph);
+      if (j0 + kStep > end || j0 < begin) {
+        ok = ok && mbar_wait_bounded(full_v + 8 * stage, ph);
         int b, e;
-        if (!sequence_at(a, (int64_t)key_tile(t) * kRows + own, b, e))
-          clear_row<DP, kRows>(smem_u32(s.v), own, half);
+        const int r = threadIdx.x / 2;
+        if (!sequence_at(a, (int64_t)j0 + r, b, e))
+          clear_row<DP, kStep>(smem_u32(s.v[stage]), r, threadIdx.x % 2);
         fence_proxy_async_shared();
       }
+      // the product before the last, here, where `done` cannot be two phases on:
+      // a wait for a phase tells it from its neighbours only
+      if (t > 0 && t == tiles - 1) ok = ok && mbar_wait_bounded(done, (t - 1) & 1);
       tmem_wait_st();
       fence_before_sync();
-      mbar_arrive(weights);
+      mbar_arrive(weights + 8 * stage);
     }
     if (tiles > 0) ok = ok && mbar_wait_bounded(done, (tiles - 1) & 1);
     fence_after_sync();
-    s.sums[half][own] = l;
-    asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
-    l = s.sums[0][own] + s.sums[1][own];
     const bool row = seen.i >= 0;
     const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : l > 0.f ? 1.f / l : l;
     T *to = y.at(batch, row ? seen.i : 0) + (int64_t)head * a.dim;
     if (tiles > 0) {
 #pragma unroll 1
-      for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 32) {
+      for (int k = 0; k < DP; k += 32) {
         float o[32];
         tmem_ld32(tO + mine + k, o);
         if (row) store_values(to, k, a.dim, o, by);
       }
     }
-    if (row && half == 0 && a.lse)
+    if (row && a.lse)
       a.lse[((int64_t)batch * a.rows + seen.i) * a.heads + head] = (m + log2f(l)) * kLn2;
     fence_before_sync();
   }
@@ -259,8 +266,8 @@ int prompt(const tcu_window_attention_args &s, cudaStream_t st) {
   if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
   PromptMaps maps;
   if (!attn_map(&maps.q, s.q, s.type, batches, s.rows, s.heads, s.dim, kRows) ||
-      !attn_map(&maps.k, s.k, s.type, batches, s.rows, s.kv_heads, s.dim, kRows) ||
-      !attn_map(&maps.v, s.v, s.type, batches, s.rows, s.kv_heads, s.dim, kRows))
+      !attn_map(&maps.k, s.k, s.type, batches, s.rows, s.kv_heads, s.dim, kStep) ||
+      !attn_map(&maps.v, s.v, s.type, batches, s.rows, s.kv_heads, s.dim, kStep))
     return TCU_DFT_ERR_CUDA;
   constexpr int bytes = sizeof(PromptShared<DP>);
   if (cudaFuncSetAttribute(attend_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,

@@ -305,6 +305,15 @@ struct QueryTile {
   }
 };
 
+// The first chunk that a tile's first tokens leave to far blocks, and where
+// sums of a chunk and the nth tile of a sequence's first tokens lie.
+__device__ __forceinline__ int far_from(const AttendArgs &a, int tile) {
+  return (tile * (kRows / kStep) + 2 * a.chunk - 1) / a.chunk;
+}
+__device__ __forceinline__ int64_t slot_of(const AttendArgs &a, int batch, int x, int nth, int kv) {
+  return (((int64_t)batch * a.chunks + x) * a.sink_tiles + nth) * a.kv_heads + kv;
+}
+
 // Two sides of 256 threads take the tiles of queries in turn: while one forms
 // weights, the tensor cores work on the other's tile.  Of a side's threads two
 // share a key, 32 queries each.
@@ -312,41 +321,42 @@ struct QueryTile {
 // Most keys are seen from a window's rows, first tokens from all rows of
 // their sequence.  So that no block walks over more tiles than twice another,
 // those beyond the first multiple of `chunk` that is `chunk` tiles or more
-// behind the key tile go, `chunk` at a time, to blocks of a launch before
-// (kFar), whose sums the key tile's block adds to its own, in order.  A chunk
-// has far first tokens of one sequence at most, that of its first row.
-template <typename T, int DP, bool kFar>
+// behind the key tile go, `chunk` at a time, to blocks of their own, the first
+// `far_blocks` of the launch.  A chunk has far first tokens of one sequence at
+// most, that of its first row.  Such sums, and the key tile's own, go to
+// memory in fp32, [chunk][tile of first tokens], a key tile's own behind all far
+// ones, at its first far chunk; join_kernel adds them in order.
+template <typename T, int DP>
 __global__ void __launch_bounds__(2 * kSoft + 32, 1)
     dkv_kernel(const __grid_constant__ KeyMaps maps, const AttendArgs a, const Rows<T> dk,
-               const Rows<T> dv, const int *most, float *far) {
+               const Rows<T> dv, const int *most, float *sums, int far_blocks) {
   extern __shared__ __align__(1024) uint8_t raw[];
   KeyShared<DP> &s = *reinterpret_cast<KeyShared<DP> *>(raw);
   const int warp = threadIdx.x / 32;
-  int64_t id = blockIdx.x;
+  const bool is_far = blockIdx.x < far_blocks;
+  int64_t id = is_far ? blockIdx.x : blockIdx.x - far_blocks;
   const int kv = (int)(id % a.kv_heads);
   id /= a.kv_heads;
   const int group = a.heads / a.kv_heads;
-  int tile, batch, first, end;  // tiles of queries: [first, end)
-  float *slot = far;
-  if constexpr (kFar) {
+  int tile, batch, first, end = 0;  // tiles of queries: [first, end)
+  int64_t slot = -1;                // of fp32 sums
+  if (is_far) {
     const int nth = (int)(id % a.sink_tiles);
     id /= a.sink_tiles;
     const int x = (int)(id % a.chunks);
     batch = (int)(id / a.chunks);
-    slot += (int64_t)blockIdx.x * 2 * kRows * DP;
+    slot = blockIdx.x;
     int b, e;
     if (!sequence_at(a, (int64_t)x * a.chunk * kStep, b, e)) return;
     tile = b / kRows + nth;
-    if ((int64_t)tile * kRows >= (int64_t)b + a.sinks || x < (2 * tile + 2 * a.chunk - 1) / a.chunk)
-      return;
+    if ((int64_t)tile * kRows >= (int64_t)b + a.sinks || x < far_from(a, tile)) return;
     first = x * a.chunk;
     end = (int)min((int64_t)first + a.chunk, ((int64_t)e + kStep - 1) / kStep);
   } else {  // early tiles, which are seen from most rows, before late ones
-    const int64_t batches = gridDim.x / a.kv_heads / a.k_tiles;
+    const int64_t batches = (gridDim.x - far_blocks) / a.kv_heads / a.k_tiles;
     batch = (int)(id % batches);
     tile = (int)(id / batches);
     first = tile * (kRows / kStep);
-    end = 0;
   }
   const uint32_t full_kv = smem_u32(&s.full_kv), full = smem_u32(s.full),
                  scores = smem_u32(s.scores), weights = smem_u32(s.weights), done = smem_u32(s.done);
@@ -375,18 +385,17 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
     if (sequence_at(a, j64, begin, e))
       past = j - begin < a.sinks || e - j <= a.window ? e : j + a.window;
   }
-  int far_from = 0, far_to = 0;  // chunks that other blocks have summed
-  if constexpr (!kFar) {
+  if (!is_far) {
     const int top = __reduce_max_sync(~0u, past);
     if (threadIdx.x % 32 == 0) atomicMax(&s.last, top);
     __syncthreads();
     if (past > 0 && past == s.last) s.begin = begin;
     end = max(first, (s.last + kStep - 1) / kStep);
     __syncthreads();
-    if (a.chunk > 0) {
-      far_from = (first + 2 * a.chunk - 1) / a.chunk;
-      far_to = (end + a.chunk - 1) / a.chunk;
-      end = min(end, far_from * a.chunk);
+    if (a.chunk > 0 && end > far_from(a, tile) * a.chunk) {
+      const int x = far_from(a, tile);
+      end = x * a.chunk;
+      slot = far_blocks + slot_of(a, batch, x, tile - s.begin / kRows, kv);
     }
   }
   const uint32_t tmem = s.tmem, tV = tmem + 256, tK = tV + DP;
@@ -549,7 +558,6 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
     const float by = bad * (side ? a.scale / lift : 1.f);
     const bool in = past > 0;
     T *to = (side ? dk : dv).at(batch, j64 < a.rows ? j : 0) + (int64_t)kv * a.dim;
-    const int nth = kFar || !in ? 0 : tile - s.begin / kRows;
 #pragma unroll 1
     for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 32) {
       float o[32];
@@ -558,30 +566,67 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = 0.f;
       }
-      const int64_t at = ((int64_t)side * kRows + r) * DP + k;
-      if constexpr (kFar) {
+      if (slot >= 0) {
+        float *row = sums + ((slot * 2 + side) * kRows + r) * DP + k;
 #pragma unroll
         for (int i = 0; i < 32; i += 4)
-          *reinterpret_cast<float4 *>(slot + at + i) =
-              make_float4(o[i] * bad, o[i + 1] * bad, o[i + 2] * bad, o[i + 3] * bad);
-        continue;
+          *reinterpret_cast<float4 *>(row + i) =
+              make_float4(o[i] * by, o[i + 1] * by, o[i + 2] * by, o[i + 3] * by);
+      } else if (j64 < a.rows) {
+        store_values(to, k, a.dim, o, by);
       }
-      if (in)
-        for (int x = far_from; x < far_to; ++x) {
-          const float *from = far + (((((int64_t)batch * a.chunks + x) * a.sink_tiles + nth) *
-                                      a.kv_heads + kv) * 2 * kRows * DP) + at;
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const float4 f = *reinterpret_cast<const float4 *>(from + i);
-            o[i] += f.x, o[i + 1] += f.y, o[i + 2] += f.z, o[i + 3] += f.w;
-          }
-        }
-      if (j64 < a.rows) store_values(to, k, a.dim, o, by);
     }
     fence_before_sync();
   }
   __syncthreads();
   if (warp == 2 * kSoft / 32) tmem_dealloc(tmem, 512);
+}
+
+// The sums of key tiles that far blocks share, a block a tile, head and entry.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kRows) join_kernel(const AttendArgs a, const Rows<T> dk,
+                                                     const Rows<T> dv, const float *sums,
+                                                     int far_blocks) {
+  __shared__ int last, first;
+  int64_t id = blockIdx.x;
+  const int kv = (int)(id % a.kv_heads);
+  id /= a.kv_heads;
+  const int64_t batches = gridDim.x / a.kv_heads / a.k_tiles;
+  const int batch = (int)(id % batches), tile = (int)(id / batches);
+  const int64_t j = (int64_t)tile * kRows + threadIdx.x;
+  int begin = 0, e = 0, past = 0;
+  if (threadIdx.x == 0) last = 0;
+  __syncthreads();
+  if (sequence_at(a, j, begin, e))
+    past = j - begin < a.sinks || e - j <= a.window ? e : (int)j + a.window;
+  const int top = __reduce_max_sync(~0u, past);
+  if (threadIdx.x % 32 == 0) atomicMax(&last, top);
+  __syncthreads();
+  if (past > 0 && past == last) first = begin;
+  __syncthreads();
+  const int from = far_from(a, tile), end = (last + kStep - 1) / kStep;
+  if (end <= from * a.chunk) return;
+  const int to = (end + a.chunk - 1) / a.chunk, nth = tile - first / kRows;
+  // eight adjacent values of a row a thread at a time
+  for (int i = threadIdx.x; i < 2 * kRows * (DP / 8); i += kRows) {
+    const int c = i % (DP / 8) * 8, r = i / (DP / 8) % kRows, side = i / (DP / 8) / kRows;
+    if (c >= a.dim || (int64_t)tile * kRows + r >= a.rows) continue;
+    float v[8] = {};
+    for (int x = from - 1; x < to; ++x) {
+      const int64_t slot = x < from ? far_blocks + slot_of(a, batch, from, nth, kv)
+                                    : slot_of(a, batch, x, nth, kv);
+      const float4 *p =
+          reinterpret_cast<const float4 *>(sums + ((slot * 2 + side) * kRows + r) * DP + c);
+      const float4 f = p[0], g = p[1];
+      v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+      v[4] += g.x, v[5] += g.y, v[6] += g.z, v[7] += g.w;
+    }
+    uint4 w;
+    w.x = pack2<T>(v[0], v[1]), w.y = pack2<T>(v[2], v[3]);
+    w.z = pack2<T>(v[4], v[5]), w.w = pack2<T>(v[6], v[7]);
+    T *row = (side ? dk : dv).at(batch, tile * kRows + r) + (int64_t)kv * a.dim;
+    *reinterpret_cast<uint4 *>(row + c) = w;
+  }
 }
 
 // Tiles of queries to a chunk: what a key outside the first tokens is seen
@@ -637,11 +682,10 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
     return TCU_DFT_ERR_CUDA;
   split_rows(s, a);
   const int64_t far = far_blocks(s, a);
-  if (far > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
+  if (far + k_blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
   float *sums = delta + far_offset(s);
   constexpr int q_bytes = sizeof(QueryShared<DP>), k_bytes = sizeof(KeyShared<DP>);
-  if (!shared_bytes(dq_kernel<T, DP>, q_bytes) || !shared_bytes(dkv_kernel<T, DP, false>, k_bytes) ||
-      !shared_bytes(dkv_kernel<T, DP, true>, k_bytes))
+  if (!shared_bytes(dq_kernel<T, DP>, q_bytes) || !shared_bytes(dkv_kernel<T, DP>, k_bytes))
     return TCU_DFT_ERR_CUDA;
   const unsigned blocks = (unsigned)std::min<int64_t>((total + 15) / 16, 16 * (int64_t)num_sms());
   if (most && cudaMemsetAsync(most, 0, sizeof(int), st) != cudaSuccess) {
@@ -651,14 +695,14 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
   delta_kernel<T><<<blocks, 256, 0, st>>>(rows_of<const T>(s.y), rows_of<const T>(s.dy), delta, most,
                                           a, total);
   if (const int rc = launched()) return rc;
+  const Rows<T> dk = rows_of<T>(s.dk), dv = rows_of<T>(s.dv);
+  dkv_kernel<T, DP><<<(unsigned)(far + k_blocks), 2 * kSoft + 32, k_bytes, st>>>(km, a, dk, dv, most,
+                                                                             sums, (int)far);
+  if (const int rc = launched()) return rc;
   if (far > 0) {
-    dkv_kernel<T, DP, true><<<(unsigned)far, 2 * kSoft + 32, k_bytes, st>>>(
-        km, a, rows_of<T>(s.dk), rows_of<T>(s.dv), most, sums);
+    join_kernel<T, DP><<<(unsigned)k_blocks, kRows, 0, st>>>(a, dk, dv, sums, (int)far);
     if (const int rc = launched()) return rc;
   }
-  dkv_kernel<T, DP, false><<<(unsigned)k_blocks, 2 * kSoft + 32, k_bytes, st>>>(
-      km, a, rows_of<T>(s.dk), rows_of<T>(s.dv), most, sums);
-  if (const int rc = launched()) return rc;
   dq_kernel<T, DP><<<(unsigned)q_blocks, kSoft + 32, q_bytes, st>>>(
       qm, a, rows_of<T>(s.dq), most);
   return launched();
@@ -674,7 +718,7 @@ extern "C" int64_t tcu_window_attention_grad_workspace(const tcu_window_attentio
   if (check_attention(a)) return -1;
   AttendArgs g = attend_args(*a);
   split_rows(*a, g);
-  return 4 * (far_offset(*a) + far_blocks(*a, g) * 2 * kRows * padded_dim(a->dim));
+  return 4 * (far_offset(*a) + far_blocks(*a, g) * 4 * kRows * padded_dim(a->dim));
 }
 
 extern "C" int tcu_window_attention_grad(const tcu_window_attention_args *a, void *stream) {

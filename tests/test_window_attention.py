@@ -82,7 +82,7 @@ def test_packed(tcu, dtype, kind, total, dim, window, sinks):
 
 @gpu
 @pytest.mark.parametrize("lengths,window,sinks", [
-    ([2600], 100, 3), ([700, 0, 1990, 50], 60, 130), ([100, 2300], 900, 4), ([1, 3000, 1], 30, 256),
+    ([2600], 100, 3), ([2100, 2500], 60, 3), ([700, 0, 1990, 50], 60, 130), ([100, 2300], 900, 4), ([1, 3000, 1], 30, 256),
     ([2500], 20, 300)])
 def test_first_tokens_of_long_sequences(tcu, lengths, window, sinks):
     """Gradients of keys that thousands of rows see, which blocks of their own
