@@ -54,51 +54,60 @@ struct GatedArgs {
   int rows, sequences, batches, runs;
 };
 
-// exp(L) and exp(L)^2 - 1 for L <= 0.  1 - a^2 loses what a lacks in its last
-// place where a is near one, so exp(L) - 1 is a Taylor sum of degree 6 there
-// (L > -1/4: the next term is 5e-8 of it).
+// exp(L) and sqrt(1 - exp(L)^2) for L <= 0.  1 - a^2 loses what a lacks in its
+// last place where a is near one, so exp(L) - 1 is a Taylor sum of degree 6
+// for L > -kNear (the next term is 5e-8 of it); kAllNear: there is no other L.
+constexpr float kNear = 0.25f;
 struct Decay {
-  float2 a, m;  // a, sqrt(1 - a^2)
+  float2 a, m;
 };
-__device__ __forceinline__ float sqrt_fast(float v) {
+__device__ __forceinline__ float rsqrt_fast(float v) {
   float y;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v));
   return y;
 }
 __device__ __forceinline__ float2 splat(float v) { return make_float2(v, v); }
+template <bool kAllNear>
 __device__ __forceinline__ Decay decay2(float2 L) {
   float2 p = __ffma2_rn(L, splat(1.f / 720), splat(1.f / 120));
   p = __ffma2_rn(p, L, splat(1.f / 24));
   p = __ffma2_rn(p, L, splat(1.f / 6));
   p = __ffma2_rn(p, L, splat(0.5f));
   p = __ffma2_rn(p, L, splat(1.f));
-  p = __fmul2_rn(p, L);
-  const float2 z = __fmul2_rn(L, splat(kLog2e));
+  p = __fmul2_rn(p, L);  // exp(L) - 1
   Decay d;
-  d.a = make_float2(exp2_fast(z.x), exp2_fast(z.y));
-  const float2 q = __fadd2_rn(d.a, splat(-1.f)), r = __fadd2_rn(p, splat(1.f));
-  const bool near0 = L.x > -0.25f, near1 = L.y > -0.25f;
-  const float2 em = make_float2(near0 ? p.x : q.x, near1 ? p.y : q.y);
-  d.a = make_float2(near0 ? r.x : d.a.x, near1 ? r.y : d.a.y);
-  const float2 room = __fmul2_rn(em, __fadd2_rn(em, splat(2.f)));  // a^2 - 1
-  d.m = make_float2(sqrt_fast(-room.x), sqrt_fast(-room.y));
+  d.a = __fadd2_rn(p, splat(1.f));
+  if constexpr (!kAllNear) {
+    const float2 z = __fmul2_rn(L, splat(kLog2e));
+    const float2 e = make_float2(exp2_fast(z.x), exp2_fast(z.y)), q = __fadd2_rn(e, splat(-1.f));
+    if (!(L.x > -kNear)) p.x = q.x, d.a.x = e.x;
+    if (!(L.y > -kNear)) p.y = q.y, d.a.y = e.y;
+  }
+  // 1 - a^2, kept off zero, where its root's reciprocal is none
+  float2 r = __fmul2_rn(p, __ffma2_rn(p, splat(-1.f), splat(-2.f)));
+  r = make_float2(fmaxf(r.x, 1e-37f), fmaxf(r.y, 1e-37f));
+  d.m = __fmul2_rn(r, make_float2(rsqrt_fast(r.x), rsqrt_fast(r.y)));
   return d;
 }
 
-// h -> A h + H of two channels.  A map that does not depend on h (a sequence
-// opens in it) drops even an h that is not finite.
-struct Map {
+// h -> A h + H of two channels.  Where sequences open in rows (kPacked), a map
+// that does not depend on h drops even an h that is not finite.
+struct alignas(16) Map {
   float2 A, H;
 };
+template <bool kPacked>
 __device__ __forceinline__ float2 apply(const Map &m, float2 h) {
   const float2 v = __ffma2_rn(m.A, h, m.H);
+  if constexpr (!kPacked) return v;
   return make_float2(m.A.x == 0.f ? m.H.x : v.x, m.A.y == 0.f ? m.H.y : v.y);
 }
 // first then second
+template <bool kPacked>
 __device__ __forceinline__ Map compose(const Map &first, const Map &second) {
   const float2 A = __fmul2_rn(second.A, first.A);
+  if constexpr (!kPacked) return {A, apply<false>(second, first.H)};
   return {make_float2(second.A.x == 0.f ? 0.f : A.x, second.A.y == 0.f ? 0.f : A.y),
-          apply(second, first.H)};
+          apply<true>(second, first.H)};
 }
 
 // Where sequences open and close in the 8 rows from r0 (bit i: row r0 + i),
@@ -153,7 +162,7 @@ struct Joint {
   Map warps[2][kWarps][32];
   Map blocks[2][kMostCluster][32];
 };
-template <bool kBack>
+template <bool kBack, bool kPacked>
 __device__ __forceinline__ float2 join(Joint &s, int turn, const Map &own, float2 &carry, int warp,
                                        int lane, int rank, int size) {
   s.warps[turn][warp][lane] = own;
@@ -163,11 +172,11 @@ __device__ __forceinline__ float2 join(Joint &s, int turn, const Map &own, float
   for (int i = 0; i < kWarps; ++i) {
     const int w = kBack ? kWarps - 1 - i : i;
     if (w == warp) before = all;
-    all = compose(all, s.warps[turn][w][lane]);
+    all = compose<kPacked>(all, s.warps[turn][w][lane]);
   }
   float2 enters = carry;
   if (size == 1) {
-    carry = apply(all, carry);
+    carry = apply<kPacked>(all, carry);
   } else {
     const cg::cluster_group cluster = cg::this_cluster();
     for (int r = warp; r < size; r += kWarps)
@@ -176,10 +185,10 @@ __device__ __forceinline__ float2 join(Joint &s, int turn, const Map &own, float
     for (int i = 0; i < size; ++i) {
       const int r = kBack ? size - 1 - i : i;
       if (r == rank) enters = carry;
-      carry = apply(s.blocks[turn][r][lane], carry);
+      carry = apply<kPacked>(s.blocks[turn][r][lane], carry);
     }
   }
-  return apply(before, enters);
+  return apply<kPacked>(before, enters);
 }
 
 // An empty sequence ends in the state it starts from.
@@ -192,48 +201,160 @@ __device__ __forceinline__ void empty_sequences(const GatedArgs<T> &a, float *to
                from ? pair_at<kWide>(from, s * a.channels + c, count) : splat(0.f));
 }
 
-template <typename T, bool kPacked, bool kWide>
-__global__ void __launch_bounds__(kThreads, 2) gated_kernel(const GatedArgs<T> a, int size) {
-  __shared__ Joint joint;
+// ------------------------------------------------------------ rows on the way
+// A warp's ring of kStages tiles of 8 rows x 64 channels of kTensors row
+// tensors, filled by copies that nothing waits for until their rows are due:
+// 16 bytes at a time where rows are aligned so (kWide), 4 for other 32-bit
+// rows; 16-bit rows at odd places go through registers.
+template <typename T, int kTensors, int kStages>
+struct alignas(16) Ring {
+  T v[kStages][kTensors][kRun][kStrip];
+};
+template <int kBytes>
+__device__ __forceinline__ void copy_async(void *dst, const void *src, bool has) {
+  const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
+  if constexpr (kBytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(has ? 16 : 0)
+                 : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(src), "r"(has ? 4 : 0)
+                 : "memory");
+}
+// Rows [r0, r0 + n) of a strip whose first channel is c0; others are zeros.
+template <typename T, bool kWide>
+__device__ __forceinline__ void copy_rows(T (*to)[kStrip], const Rows<const T> &from, int64_t b,
+                                          int r0, int n, int64_t c0, int64_t channels, int lane) {
+  if constexpr (kWide) {
+    constexpr int per = 16 / sizeof(T), chunks = kStrip / per;
+    const int c = lane % chunks * per;
+    const bool in = c0 + c < channels;
+#pragma unroll
+    for (int i = 0; i < kRun * chunks / 32; ++i) {
+      const int r = lane / chunks + i * (32 / chunks);
+      const bool has = in && r < n;
+      copy_async<16>(&to[r][c], has ? from.at(b, r0 + r) + c0 + c : from.p, has);
+    }
+  } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int r = 0; r < kRun; ++r)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int c = lane + 32 * k;
+        const bool has = r < n && c0 + c < channels;
+        copy_async<4>(&to[r][c], has ? from.at(b, r0 + r) + c0 + c : from.p, has);
+      }
+  } else {
+    T v[kRun][2];
+#pragma unroll
+    for (int r = 0; r < kRun; ++r)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        v[r][k] = r < n && c0 + lane + 32 * k < channels ? from.at(b, r0 + r)[c0 + lane + 32 * k]
+                                                         : from_f<T>(0.f);
+#pragma unroll
+    for (int r = 0; r < kRun; ++r)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) to[r][lane + 32 * k] = v[r][k];
+  }
+}
+__device__ __forceinline__ void copies_commit() {
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+  __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ float2 pair_of(const T (*rows)[kStrip], int i, int lane) {
+  uint32_t w[Pair<T>::kWords];
+  const Vec<uint32_t, Pair<T>::kWords> v =
+      *reinterpret_cast<const Vec<uint32_t, Pair<T>::kWords> *>(&rows[i][2 * lane]);
+#pragma unroll
+  for (int k = 0; k < Pair<T>::kWords; ++k) w[k] = v.v[k];
+  return Pair<T>::get(w);
+}
+template <typename T, bool kWide>
+__device__ __forceinline__ void put_row(T *to, float2 v, int count) {
+  Raw<T, 2> out;
+  out.set(0, v);
+  out.template store<kWide>(to, count);
+}
+
+// Blocks an SM, and stages: what its shared memory holds, and the registers.
+template <typename T>
+struct Sizes {
+  static constexpr int kStages = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kBlocks = sizeof(T) == 2 ? 3 : 2, kGradBlocks = 2;
+};
+
+template <typename T>
+struct GatedShared {
+  Joint joint;
+  Ring<T, 3, Sizes<T>::kStages> ring[kWarps];
+};
+template <typename T>
+struct GradShared {
+  Joint joint;
+  float2 sums[kWarps][32];
+  Ring<T, 4, Sizes<T>::kStages> ring[kWarps];
+};
+
+template <typename T, bool kPacked, bool kWide, bool kAllNear>
+__device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T> &s, int size,
+                                           float2 rate) {
+  constexpr int kStages = Sizes<T>::kStages;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int rank = (int)(blockIdx.x % size);
-  const int64_t c = (int64_t)(blockIdx.x / size) * kStrip + 2 * lane;
+  const int64_t c0 = (int64_t)(blockIdx.x / size) * kStrip, c = c0 + 2 * lane;
   const int count = (int)max((int64_t)0, min((int64_t)2, a.channels - c));
-  const float2 rate = pair_at<kWide>(a.rate, c, count);
+  const float2 minus = make_float2(-rate.x, -rate.y);
+  const int64_t step = (int64_t)size * kTile;
+  auto &ring = s.ring[warp];
   int turn = 0;
   for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
     float2 carry = splat(0.f);
     if (!kPacked && a.state) carry = pair_at<kWide>(a.state, (int64_t)b * a.channels + c, count);
-    for (int64_t t0 = 0; t0 < a.rows; t0 += (int64_t)size * kTile) {
-      const int64_t first = t0 + (int64_t)rank * kTile + warp * kRun;
-      const int r0 = (int)min(first, (int64_t)a.rows);
+    const auto ask = [&](int64_t t0, int stage) {
+      const int r0 = (int)min(t0 + (int64_t)rank * kTile + warp * kRun, (int64_t)a.rows);
+      const int n = t0 < a.rows ? min(kRun, a.rows - r0) : 0;
+      copy_rows<T, kWide>(ring.v[stage][0], a.forget, b, r0, n, c0, a.channels, lane);
+      copy_rows<T, kWide>(ring.v[stage][1], a.admit, b, r0, n, c0, a.channels, lane);
+      copy_rows<T, kWide>(ring.v[stage][2], a.x, b, r0, n, c0, a.channels, lane);
+      copies_commit();
+    };
+    __syncwarp();
+    for (int i = 0; i < kStages - 1; ++i) ask(i * step, i);
+    int stage = 0;
+    for (int64_t t0 = 0; t0 < a.rows; t0 += step) {
+      const int64_t at = t0 + (int64_t)rank * kTile + warp * kRun;
+      const int r0 = (int)min(at, (int64_t)a.rows);
       const int n = min(kRun, a.rows - r0);
-      Raw<T, 2> x[kRun], f[kRun], g[kRun];
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        const int has = i < n ? count : 0;
-        f[i].template load<kWide>(a.forget.at(b, r0 + i) + c, has);
-        g[i].template load<kWide>(a.admit.at(b, r0 + i) + c, has);
-        x[i].template load<kWide>(a.x.at(b, r0 + i) + c, has);
-      }
+      __syncwarp();
+      ask(t0 + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
       Marks8 seqs{};
       if (n > 0) seqs = sequences_of<kPacked>(a, b, r0, lane);
+      copies_wait<kStages - 1>();
       float2 keep[kRun], add[kRun];
       Map run{splat(1.f), splat(0.f)};
 #pragma unroll
       for (int i = 0; i < kRun; ++i) {
-        const Decay d = decay2(__fmul2_rn(sigmoid2(f[i].pair(0)), make_float2(-rate.x, -rate.y)));
-        const bool in = seqs.inside >> i & 1;  // others pass on what they get
-        keep[i] = in ? d.a : splat(1.f);
-        add[i] = in ? __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g[i].pair(0))), x[i].pair(0))
-                    : splat(0.f);
-        if (kPacked && (seqs.open >> i & 1)) {
-          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
-          run = {splat(0.f), a.state ? pair_at<kWide>(a.state, s * a.channels + c, count) : splat(0.f)};
+        const float2 f = pair_of(ring.v[stage][0], i, lane), g = pair_of(ring.v[stage][1], i, lane),
+                     x = pair_of(ring.v[stage][2], i, lane);
+        const Decay d = decay2<kAllNear>(__fmul2_rn(sigmoid2(f), minus));
+        keep[i] = d.a;
+        add[i] = __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g)), x);
+        if constexpr (kPacked) {
+          if (!(seqs.inside >> i & 1)) keep[i] = splat(1.f), add[i] = splat(0.f);
+          if (seqs.open >> i & 1) {
+            const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+            run = {splat(0.f), a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f)};
+          }
         }
         run = {__fmul2_rn(run.A, keep[i]), __ffma2_rn(run.H, keep[i], add[i])};
       }
-      float2 h = join<false>(joint, turn, run, carry, warp, lane, rank, size);
+      stage = stage == kStages - 1 ? 0 : stage + 1;
+      float2 h = join<false, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size);
       turn ^= 1;
       if (n <= 0) continue;
       if (a.marks)
@@ -241,148 +362,182 @@ __global__ void __launch_bounds__(kThreads, 2) gated_kernel(const GatedArgs<T> a
 #pragma unroll
       for (int i = 0; i < kRun; ++i) {
         if (kPacked && (seqs.open >> i & 1)) {
-          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
-          h = a.state ? pair_at<kWide>(a.state, s * a.channels + c, count) : splat(0.f);
+          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+          h = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
         }
         h = __ffma2_rn(h, keep[i], add[i]);
-        if (seqs.inside >> i & 1) {
-          Raw<T, 2> y;
-          y.set(0, h);
-          y.template store<kWide>(a.y.at(b, r0 + i) + c, count);
-        }
+        if (seqs.inside >> i & 1) put_row<T, kWide>(a.y.at(b, r0 + i) + c, h, count);
         if (seqs.close >> i & 1) {
-          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
-          if (a.last) put_pair<kWide>(a.last, s * a.channels + c, count, h);
+          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+          if (a.last) put_pair<kWide>(a.last, q * a.channels + c, count, h);
         }
       }
     }
+    copies_wait<0>();
   }
   if (kPacked && a.last && blockIdx.y == 0)
     empty_sequences<kWide>(a, a.last, a.state, c, count, rank * kWarps + warp, size * kWarps);
   if (size > 1) cg::this_cluster().sync();  // no block leaves while others write to it
 }
 
+// The rate of each of the lane's channels, and whether no decay of the warp's
+// is far from one.
+template <bool kWide, typename T>
+__device__ __forceinline__ float2 rates(const GatedArgs<T> &a, int size, bool &near) {
+  const int64_t c = (int64_t)(blockIdx.x / size) * kStrip + 2 * (threadIdx.x % 32);
+  const float2 r = pair_at<kWide>(a.rate, c, (int)max((int64_t)0, min((int64_t)2, a.channels - c)));
+  near = __syncthreads_and(r.x < kNear && r.y < kNear);
+  return r;
+}
+
 template <typename T, bool kPacked, bool kWide>
-__global__ void __launch_bounds__(kThreads, 2) gated_grad_kernel(const GatedArgs<T> a, int size) {
-  __shared__ Joint joint;
-  __shared__ float2 sums[kWarps][32];
+__global__ void __launch_bounds__(kThreads, Sizes<T>::kBlocks)
+    gated_kernel(const GatedArgs<T> a, int size) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  GatedShared<T> &s = *reinterpret_cast<GatedShared<T> *>(raw);
+  bool near;
+  const float2 rate = rates<kWide>(a, size, near);
+  if (near) gated_rows<T, kPacked, kWide, true>(a, s, size, rate);
+  else gated_rows<T, kPacked, kWide, false>(a, s, size, rate);
+}
+
+template <typename T, bool kPacked, bool kWide, bool kAllNear>
+__device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &s, int size,
+                                          float2 rate) {
+  constexpr int kStages = Sizes<T>::kStages;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int rank = (int)(blockIdx.x % size);
-  const int64_t c = (int64_t)(blockIdx.x / size) * kStrip + 2 * lane;
+  const int64_t c0 = (int64_t)(blockIdx.x / size) * kStrip, c = c0 + 2 * lane;
   const int count = (int)max((int64_t)0, min((int64_t)2, a.channels - c));
-  const float2 rate = pair_at<kWide>(a.rate, c, count);
+  const float2 minus = make_float2(-rate.x, -rate.y);
   const int64_t step = (int64_t)size * kTile;
+  auto &ring = s.ring[warp];
   float2 drate = splat(0.f);
   int turn = 0;
   for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
     float2 carry = splat(0.f);  // a_{t+1} e_{t+1} of the row below
     if (!kPacked && a.dlast) carry = pair_at<kWide>(a.dlast, (int64_t)b * a.channels + c, count);
-    for (int64_t t0 = (a.rows - 1) / step * step; t0 >= 0; t0 -= step) {
-      const int64_t first = t0 + (int64_t)rank * kTile + warp * kRun;
-      const int r0 = (int)min(first, (int64_t)a.rows);
+    const auto ask = [&](int64_t t0, int stage) {
+      const int r0 = (int)min(max((int64_t)0, t0) + (int64_t)rank * kTile + warp * kRun, (int64_t)a.rows);
+      const int n = t0 >= 0 ? min(kRun, a.rows - r0) : 0;
+      copy_rows<T, kWide>(ring.v[stage][0], a.forget, b, r0, n, c0, a.channels, lane);
+      copy_rows<T, kWide>(ring.v[stage][1], a.admit, b, r0, n, c0, a.channels, lane);
+      copy_rows<T, kWide>(ring.v[stage][2], a.x, b, r0, n, c0, a.channels, lane);
+      copy_rows<T, kWide>(ring.v[stage][3], a.dy, b, r0, n, c0, a.channels, lane);
+      copies_commit();
+    };
+    const int64_t end = (a.rows - 1) / step * step;
+    __syncwarp();
+    for (int i = 0; i < kStages - 1; ++i) ask(end - i * step, i);
+    int stage = 0;
+    for (int64_t t0 = end; t0 >= 0; t0 -= step) {
+      const int64_t at = t0 + (int64_t)rank * kTile + warp * kRun;
+      const int r0 = (int)min(at, (int64_t)a.rows);
       const int n = min(kRun, a.rows - r0);
-      Raw<T, 2> x[kRun], f[kRun], g[kRun], dy[kRun];
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        const int has = i < n ? count : 0;
-        f[i].template load<kWide>(a.forget.at(b, r0 + i) + c, has);
-        dy[i].template load<kWide>(a.dy.at(b, r0 + i) + c, has);
-        g[i].template load<kWide>(a.admit.at(b, r0 + i) + c, has);
-        x[i].template load<kWide>(a.x.at(b, r0 + i) + c, has);
-      }
+      __syncwarp();
+      ask(t0 - (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
       Marks8 seqs{};
       float2 h = splat(0.f);
       if (n > 0) {
         seqs = sequences_of<kPacked>(a, b, r0, lane);
         h = pair_at<kWide>(a.marks, ((int64_t)b * a.runs + r0 / kRun) * a.channels + c, count);
       }
-      // forward: decays, open gates and the state before each row
+      copies_wait<kStages - 1>();
+      const auto &rows = ring.v[stage];
+      // forward: decays and the state before each row
       float2 keep[kRun], root[kRun], before[kRun];
 #pragma unroll
       for (int i = 0; i < kRun; ++i) {
-        const float2 L = __fmul2_rn(sigmoid2(f[i].pair(0)), make_float2(-rate.x, -rate.y));
-        const Decay d = decay2(L);
-        const bool in = seqs.inside >> i & 1;
-        keep[i] = in ? d.a : splat(1.f);
+        const Decay d = decay2<kAllNear>(__fmul2_rn(sigmoid2(pair_of(rows[0], i, lane)), minus));
+        keep[i] = d.a;
         root[i] = d.m;
         if (kPacked && (seqs.open >> i & 1)) {
-          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
-          h = a.state ? pair_at<kWide>(a.state, s * a.channels + c, count) : splat(0.f);
+          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+          h = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
         }
         before[i] = h;
-        h = __ffma2_rn(h, keep[i],
-                       __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g[i].pair(0))), x[i].pair(0)));
+        h = __ffma2_rn(h, d.a, __fmul2_rn(__fmul2_rn(d.m, sigmoid2(pair_of(rows[1], i, lane))),
+                                          pair_of(rows[2], i, lane)));
       }
       Map run{splat(1.f), splat(0.f)};
 #pragma unroll
       for (int i = kRun - 1; i >= 0; --i) {
         if (kPacked && (seqs.close >> i & 1)) {
-          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
-          run = {splat(0.f), a.dlast ? pair_at<kWide>(a.dlast, s * a.channels + c, count) : splat(0.f)};
+          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+          run = {splat(0.f), a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f)};
         }
         if (!(seqs.inside >> i & 1)) continue;
-        run = {__fmul2_rn(run.A, keep[i]), __fmul2_rn(__fadd2_rn(run.H, dy[i].pair(0)), keep[i])};
+        run = {__fmul2_rn(run.A, keep[i]),
+               __fmul2_rn(__fadd2_rn(run.H, pair_of(rows[3], i, lane)), keep[i])};
         if (kPacked && (seqs.open >> i & 1)) run = {splat(0.f), splat(0.f)};
       }
-      float2 e = join<true>(joint, turn, run, carry, warp, lane, rank, size);
+      float2 e = join<true, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size);
       turn ^= 1;
-      if (n <= 0) continue;
       float2 share = splat(0.f);
 #pragma unroll
       for (int i = kRun - 1; i >= 0; --i) {
         if (i >= n) continue;
-        Raw<T, 2> out;
+        T *dx = a.dx.at(b, r0 + i) + c, *dg = a.dadmit.at(b, r0 + i) + c,
+          *df = a.dforget.at(b, r0 + i) + c;
         if (kPacked && !(seqs.inside >> i & 1)) {  // rows of no sequence
-          out.set(0, splat(0.f));
-          out.template store<kWide>(a.dx.at(b, r0 + i) + c, count);
-          out.template store<kWide>(a.dadmit.at(b, r0 + i) + c, count);
-          out.template store<kWide>(a.dforget.at(b, r0 + i) + c, count);
+          put_row<T, kWide>(dx, splat(0.f), count);
+          put_row<T, kWide>(dg, splat(0.f), count);
+          put_row<T, kWide>(df, splat(0.f), count);
           continue;
         }
         if (kPacked && (seqs.close >> i & 1)) {
-          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
-          e = a.dlast ? pair_at<kWide>(a.dlast, s * a.channels + c, count) : splat(0.f);
+          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+          e = a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f);
         }
-        e = __fadd2_rn(e, dy[i].pair(0));
-        const float2 open = sigmoid2(f[i].pair(0)), way = sigmoid2(g[i].pair(0)), v = x[i].pair(0);
-        const float2 L = __fmul2_rn(open, make_float2(-rate.x, -rate.y));
-        const float2 ew = __fmul2_rn(e, way), dx = __fmul2_rn(ew, root[i]);
-        out.set(0, dx);
-        out.template store<kWide>(a.dx.at(b, r0 + i) + c, count);
-        const float2 shut = __ffma2_rn(way, splat(-1.f), splat(1.f));
-        out.set(0, __fmul2_rn(__fmul2_rn(dx, v), shut));
-        out.template store<kWide>(a.dadmit.at(b, r0 + i) + c, count);
-        // dL L; L / m goes to zero with L, as -sqrt(-L / 2)
-        const float2 lm = make_float2(root[i].x > 0.f ? L.x * rcp_fast(root[i].x) : 0.f,
-                                      root[i].y > 0.f ? L.y * rcp_fast(root[i].y) : 0.f);
-        const float2 k = keep[i];
-        const float2 one = __fmul2_rn(__fmul2_rn(__fmul2_rn(e, before[i]), k), L);
-        const float2 two = __fmul2_rn(__fmul2_rn(__fmul2_rn(ew, v), __fmul2_rn(k, k)), lm);
-        const float2 dL = __ffma2_rn(two, splat(-1.f), one);
+        e = __fadd2_rn(e, pair_of(rows[3], i, lane));
+        const float2 open = sigmoid2(pair_of(rows[0], i, lane)), way = sigmoid2(pair_of(rows[1], i, lane)),
+                     x = pair_of(rows[2], i, lane), k = keep[i];
+        const float2 L = __fmul2_rn(open, minus), ew = __fmul2_rn(e, way);
+        const float2 gx = __fmul2_rn(ew, root[i]);
+        put_row<T, kWide>(dx, gx, count);
+        const float2 gxx = __fmul2_rn(gx, x);
+        put_row<T, kWide>(dg, __ffma2_rn(gxx, __fmul2_rn(way, splat(-1.f)), gxx), count);
+        // dL L, with L / m, which goes to zero with L as -sqrt(-L / 2)
+        const float2 lm = __fmul2_rn(L, make_float2(rcp_fast(root[i].x), rcp_fast(root[i].y)));
+        const float2 one = __fmul2_rn(__fmul2_rn(e, before[i]), L);
+        const float2 two = __fmul2_rn(__fmul2_rn(__fmul2_rn(ew, x), k), lm);
+        const float2 dL = __fmul2_rn(k, __ffma2_rn(two, splat(-1.f), one));
         share = __fadd2_rn(share, dL);
-        out.set(0, __fmul2_rn(dL, __ffma2_rn(open, splat(-1.f), splat(1.f))));
-        out.template store<kWide>(a.dforget.at(b, r0 + i) + c, count);
+        put_row<T, kWide>(df, __ffma2_rn(dL, __fmul2_rn(open, splat(-1.f)), dL), count);
         e = __fmul2_rn(e, k);
         if ((seqs.open >> i & 1) && a.dstate) {
-          const int64_t s = __shfl_sync(~0u, seqs.seq, i);
-          put_pair<kWide>(a.dstate, s * a.channels + c, count, e);
+          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+          put_pair<kWide>(a.dstate, q * a.channels + c, count, e);
         }
       }
       drate = __fadd2_rn(drate, share);
+      stage = stage == kStages - 1 ? 0 : stage + 1;
     }
+    copies_wait<0>();
   }
   if (kPacked && a.dstate && blockIdx.y == 0)
     empty_sequences<kWide>(a, a.dstate, a.dlast, c, count, rank * kWarps + warp, size * kWarps);
-  sums[warp][lane] = drate;
+  s.sums[warp][lane] = drate;
   __syncthreads();
   if (warp == 0) {
-    float2 s = splat(0.f);
-    for (int w = 0; w < kWarps; ++w) s = __fadd2_rn(s, sums[w][lane]);
+    float2 sum = splat(0.f);
+    for (int w = 0; w < kWarps; ++w) sum = __fadd2_rn(sum, s.sums[w][lane]);
     // of L = -rate s(forget): d rate = dL L / rate
-    s = make_float2(s.x / rate.x, s.y / rate.y);
-    put_pair<kWide>(a.parts, ((int64_t)blockIdx.y * size + rank) * a.channels + c, count, s);
+    sum = make_float2(sum.x / rate.x, sum.y / rate.y);
+    put_pair<kWide>(a.parts, ((int64_t)blockIdx.y * size + rank) * a.channels + c, count, sum);
   }
   if (size > 1) cg::this_cluster().sync();
+}
+
+template <typename T, bool kPacked, bool kWide>
+__global__ void __launch_bounds__(kThreads, Sizes<T>::kGradBlocks)
+    gated_grad_kernel(const GatedArgs<T> a, int size) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  GradShared<T> &s = *reinterpret_cast<GradShared<T> *>(raw);
+  bool near;
+  const float2 rate = rates<kWide>(a, size, near);
+  if (near) grad_rows<T, kPacked, kWide, true>(a, s, size, rate);
+  else grad_rows<T, kPacked, kWide, false>(a, s, size, rate);
 }
 
 // One thread for two channels of an entry.
@@ -401,7 +556,7 @@ __global__ void __launch_bounds__(128) gated_step_kernel(const GatedArgs<T> a) {
     const bool held = slot >= 0 && slot < a.num_slots;
     float2 h = splat(0.f);
     if (held) {
-      const Decay d = decay2(__fmul2_rn(sigmoid2(f.pair(0)), make_float2(-rate.x, -rate.y)));
+      const Decay d = decay2<false>(__fmul2_rn(sigmoid2(f.pair(0)), make_float2(-rate.x, -rate.y)));
       const int64_t at = slot * a.channels + c;
       h = __ffma2_rn(pair_at<kWide>(a.last, at, count), d.a,
                      __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g.pair(0))), x.pair(0)));
@@ -414,7 +569,7 @@ __global__ void __launch_bounds__(128) gated_step_kernel(const GatedArgs<T> a) {
 
 // ------------------------------------------------------------- host side
 struct GatedPlan {
-  int64_t batches, strips, size, entries;  // entries: blocks along the batch
+  int64_t batches, strips, size, entries;  // blocks of a cluster, along the batch
   int64_t row_seq, parts;                  // workspace, in words
 };
 
@@ -423,12 +578,12 @@ GatedPlan plan_of(const tcu_gated_scan_args &a, bool grad) {
   p.batches = a.offsets ? 1 : a.sequences;
   p.strips = (a.channels + kStrip - 1) / kStrip;
   p.entries = std::min<int64_t>(p.batches, 65535);
-  // Blocks of a cluster share a strip's rows: as many as rows give tiles,
-  // until the card has a few blocks for each place.
+  // Blocks of a cluster share a strip's rows: as many as rows give tiles, while
+  // all blocks run at once.
   const int64_t tiles = (a.rows + kTile - 1) / kTile;
+  const int64_t places = (int64_t)num_sms() * (a.type != TCU_SEQ_F32 && !grad ? 3 : 2);
   p.size = 1;
-  while (p.size < kMostCluster && p.size < tiles &&
-         p.strips * p.entries * p.size < 8 * (int64_t)num_sms())
+  while (p.size < kMostCluster && p.size < tiles && 2 * p.strips * p.entries * p.size <= places)
     p.size *= 2;
   p.row_seq = a.offsets ? (a.rows + 3) / 4 * 4 : 0;
   p.parts = grad ? p.entries * p.size * a.channels : 0;
@@ -471,11 +626,12 @@ GatedArgs<T> args_of(const tcu_gated_scan_args &s, const GatedPlan &p, bool step
 enum Call { kPrompt, kGrad, kStep };
 
 template <typename K, typename T>
-int start(K kernel, const GatedPlan &p, const GatedArgs<T> &a, cudaStream_t st) {
+int start(K kernel, int bytes, const GatedPlan &p, const GatedArgs<T> &a, cudaStream_t st) {
   if (p.strips * p.size > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(p.strips * p.size), (unsigned)p.entries);
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = bytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -483,8 +639,9 @@ int start(K kernel, const GatedPlan &p, const GatedArgs<T> &a, cudaStream_t st) 
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.size > 1 ? 1 : 0;
-  cudaError_t e = cudaSuccess;
-  if (p.size > 8)
+  cudaError_t e = cudaFuncSetAttribute((const void *)kernel,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && p.size > 8)
     e = cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, a, (int)p.size);
   if (e == cudaSuccess) return launched();
@@ -494,8 +651,9 @@ int start(K kernel, const GatedPlan &p, const GatedArgs<T> &a, cudaStream_t st) 
 
 template <typename T, bool kPacked, bool kWide>
 int run_rows(Call call, const GatedPlan &p, const GatedArgs<T> &a, cudaStream_t st) {
-  return call == kGrad ? start(gated_grad_kernel<T, kPacked, kWide>, p, a, st)
-                       : start(gated_kernel<T, kPacked, kWide>, p, a, st);
+  return call == kGrad
+             ? start(gated_grad_kernel<T, kPacked, kWide>, (int)sizeof(GradShared<T>), p, a, st)
+             : start(gated_kernel<T, kPacked, kWide>, (int)sizeof(GatedShared<T>), p, a, st);
 }
 
 template <typename T>
@@ -503,17 +661,19 @@ int run(Call call, const tcu_gated_scan_args &s, cudaStream_t st) {
   const GatedPlan p = plan_of(s, call == kGrad);
   GatedArgs<T> a = args_of<T>(s, p, call == kStep);
   const int64_t batches = call == kStep ? s.sequences : p.batches;
-  bool wide = s.channels % 2 == 0;
+  // prompts are copied in 16 bytes, tokens read in pairs
+  const int word = call == kStep ? 2 * (int)sizeof(T) : 16;
+  bool wide = s.channels % (word / (int)sizeof(T)) == 0;
   for (const void *q : {(const void *)s.rate, (const void *)s.state, (const void *)s.dlast,
                         (const void *)s.last, (const void *)s.dstate, (const void *)s.marks,
                         (const void *)a.parts})
     wide = wide && (uintptr_t)q % 8 == 0;
   for (const tcu_seq_rows *r : {&s.x, &s.forget, &s.admit})
-    wide = wide && rows_aligned(*r, s.type, batches, s.rows, 2 * sizeof(T));
-  if (call != kGrad) wide = wide && rows_aligned(s.y, s.type, batches, s.rows, 2 * sizeof(T));
+    wide = wide && rows_aligned(*r, s.type, batches, s.rows, word);
+  if (call != kGrad) wide = wide && rows_aligned(s.y, s.type, batches, s.rows, word);
   else
     for (const tcu_seq_rows *r : {&s.dy, &s.dx, &s.dforget, &s.dadmit})
-      wide = wide && rows_aligned(*r, s.type, batches, s.rows, 2 * sizeof(T));
+      wide = wide && rows_aligned(*r, s.type, batches, s.rows, word);
   if (call == kStep) {
     const int64_t blocks = (s.channels + 255) / 256;
     if (blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;

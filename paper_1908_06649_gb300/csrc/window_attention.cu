@@ -27,7 +27,7 @@ namespace {
 constexpr int kRows = 128;  // of a tile of queries
 constexpr int kStep = 64;   // of a tile of keys
 constexpr int kSoft = 128;  // threads that form weights: a row each
-constexpr int kThreads = kSoft + 32;
+constexpr int kThreads = kSoft + 64;  // and a warp for products, one for copies
 
 struct PromptMaps {
   CUtensorMap q, k, v;  // k and v in boxes of kStep rows
@@ -37,7 +37,7 @@ template <int DP>
 struct PromptShared {
   uint8_t q[kTileBytes<DP, kRows>];
   uint8_t k[2][kTileBytes<DP, kStep>], v[2][kTileBytes<DP, kStep>];
-  uint64_t full_k[2], full_v[2], scores[2], weights[2], done;
+  uint64_t full_k[2], full_v[2], scores[2], weights[2], done[2];
   uint32_t tmem;
   int low, sink_at, sink_end, failed;
 };
@@ -54,15 +54,15 @@ __global__ void __launch_bounds__(kThreads, 2)
   const int kv = head / (a.heads / a.kv_heads);
   const uint32_t full_k = smem_u32(s.full_k), full_v = smem_u32(s.full_v),
                  scores = smem_u32(s.scores), weights = smem_u32(s.weights),
-                 done = smem_u32(&s.done);
+                 done = smem_u32(s.done);
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
+      mbar_init(done + 8 * i, 1);
       mbar_init(full_k + 8 * i, 1);
       mbar_init(full_v + 8 * i, 1);
       mbar_init(scores + 8 * i, 1);
       mbar_init(weights + 8 * i, kSoft);
     }
-    mbar_init(done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.low = INT32_MAX;
     s.sink_end = 0;
@@ -98,26 +98,41 @@ __global__ void __launch_bounds__(kThreads, 2)
   };
   const float c = a.scale * kLog2e;
 
-  if (warp == kSoft / 32) {
-    const uint32_t q = smem_u32(s.q), k = smem_u32(s.k), v = smem_u32(s.v);
-    constexpr uint32_t bytes = kTileBytes<DP, kStep>;
+  const uint32_t q = smem_u32(s.q), k = smem_u32(s.k), v = smem_u32(s.v);
+  constexpr uint32_t bytes = kTileBytes<DP, kStep>;
+  if (warp == kSoft / 32 + 1) {  // copies: two tiles ahead
     bool ok = true;
     int keys = 0, values = 0;  // tiles asked for
-    const auto ask = [&](const CUtensorMap *map, uint32_t to, uint32_t full, int &count, bool with_q) {
-      if (count >= tiles) return;
-      const uint32_t stage = count & 1;
+    for (int t = 0; t < tiles && ok; ++t) {
+      const uint32_t stage = t & 1;
+      // the scores of t - 2 have read its keys, the product of t - 2 its values
+      if (t > 1) ok = mbar_wait_bounded(scores + 8 * stage, ((t - 2) >> 1) & 1);
+      if (!ok) break;
       if (elect_one()) {
-        mbar_expect_tx(full + 8 * stage, bytes + (with_q ? kTileBytes<DP, kRows> : 0));
-        if (with_q) load_tile<DP, kRows>(q, &maps.q, head, tile * kRows, batch, full);
-        load_tile<DP, kStep>(to + stage * bytes, map, kv, key_row(count), batch, full + 8 * stage);
+        mbar_expect_tx(full_k + 8 * stage, bytes + (t == 0 ? kTileBytes<DP, kRows> : 0));
+        if (t == 0) load_tile<DP, kRows>(q, &maps.q, head, tile * kRows, batch, full_k);
+        load_tile<DP, kStep>(k + stage * bytes, &maps.k, kv, key_row(t), batch, full_k + 8 * stage);
       }
       __syncwarp();
-      ++count;
-    };
-    ask(&maps.k, k, full_k, keys, true);
-    ask(&maps.k, k, full_k, keys, false);
-    ask(&maps.v, v, full_v, values, false);
-    ask(&maps.v, v, full_v, values, false);
+      keys = t + 1;
+      if (t > 1) ok = mbar_wait_bounded(done + 8 * stage, ((t - 2) >> 1) & 1);
+      if (!ok) break;
+      if (elect_one()) {
+        mbar_expect_tx(full_v + 8 * stage, bytes);
+        load_tile<DP, kStep>(v + stage * bytes, &maps.v, kv, key_row(t), batch, full_v + 8 * stage);
+      }
+      __syncwarp();
+      values = t + 1;
+    }
+    if (!ok) {  // copies in flight end before the block does
+      s.failed = 1;
+      for (int i = 1; i <= 2; ++i) {
+        if (keys >= i) mbar_wait_bounded(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
+        if (values >= i) mbar_wait_bounded(full_v + 8 * ((values - i) & 1), ((values - i) >> 1) & 1);
+      }
+    }
+  } else if (warp == kSoft / 32) {  // products
+    bool ok = true;
     // scores run a tile ahead of the weights: while those of one are formed,
     // the next tile's are multiplied
     for (int t = -1; t < tiles && ok; ++t) {
@@ -125,10 +140,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (t + 1 < tiles) {
         ok = mbar_wait_bounded(full_k + 8 * other, ((t + 1) >> 1) & 1);
         // they take the place of weights that the product of t - 1 has read
-        if (t > 0) {
-          ok = ok && mbar_wait_bounded(done, (t - 1) & 1);
-          if (ok) ask(&maps.v, v, full_v, values, false);
-        }
+        if (t > 0) ok = ok && mbar_wait_bounded(done + 8 * other, ((t - 1) >> 1) & 1);
         if (!ok) break;
         fence_after_sync();
         if (elect_one()) {
@@ -138,25 +150,17 @@ __global__ void __launch_bounds__(kThreads, 2)
         __syncwarp();
       }
       if (t < 0) continue;
-      ok = mbar_wait_bounded(scores + 8 * stage, (t >> 1) & 1);
-      if (ok) ask(&maps.k, k, full_k, keys, false);
-      ok = ok && mbar_wait_bounded(full_v + 8 * stage, (t >> 1) & 1) &&
+      ok = mbar_wait_bounded(full_v + 8 * stage, (t >> 1) & 1) &&
            mbar_wait_bounded(weights + 8 * stage, (t >> 1) & 1);
       if (!ok) break;
       fence_after_sync();
       if (elect_one()) {
         product_values<T, DP, kStep>(tO, tmem + stage * kStep, v + stage * bytes, t > 0);
-        mma_commit(done);
+        mma_commit(done + 8 * stage);
       }
       __syncwarp();
     }
-    if (!ok) {  // copies in flight end before the block does
-      s.failed = 1;
-      for (int i = 1; i <= 2; ++i) {
-        if (keys >= i) mbar_wait_bounded(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
-        if (values >= i) mbar_wait_bounded(full_v + 8 * ((values - i) & 1), ((values - i) >> 1) & 1);
-      }
-    }
+    if (!ok) s.failed = 1;
   } else {
     const uint32_t mine = (uint32_t)(warp * 32) << 16;
     // packed rows outside [begin, end) are in no sequence
@@ -194,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         const float by = m == -INFINITY ? 0.f : exp2_fast(m - now);
         l *= by;
         if (t > 0) {
-          ok = ok && mbar_wait_bounded(done, (t - 1) & 1);
+          ok = ok && mbar_wait_bounded(done + 8 * (stage ^ 1), ((t - 1) >> 1) & 1);
           fence_after_sync();
 #pragma unroll 1
           for (int k = 0; k < DP; k += 16) {
@@ -229,14 +233,12 @@ __global__ void __launch_bounds__(kThreads, 2)
           clear_row<DP, kStep>(smem_u32(s.v[stage]), r, threadIdx.x % 2);
         fence_proxy_async_shared();
       }
-      // the product before the last, here, where `done` cannot be two phases on:
-      // a wait for a phase tells it from its neighbours only
-      if (t > 0 && t == tiles - 1) ok = ok && mbar_wait_bounded(done, (t - 1) & 1);
       tmem_wait_st();
       fence_before_sync();
       mbar_arrive(weights + 8 * stage);
     }
-    if (tiles > 0) ok = ok && mbar_wait_bounded(done, (tiles - 1) & 1);
+    // products end in order
+    if (tiles > 0) ok = ok && mbar_wait_bounded(done + 8 * ((tiles - 1) & 1), ((tiles - 1) >> 1) & 1);
     fence_after_sync();
     const bool row = seen.i >= 0;
     const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : l > 0.f ? 1.f / l : l;
