@@ -154,41 +154,42 @@ __device__ __forceinline__ void put_pair(float *p, int64_t at, int count, float2
   if (count > 1) p[at + 1] = v.y;
 }
 
-// Composes the maps of the block's warps and of the cluster's blocks, in the
-// order of warps and blocks (kBack: from the last of either); takes the value
-// that enters the cluster's rows and gives that which enters this warp's, and
-// through `carry` that which leaves the cluster's.
+// Gives a warp the value that enters its rows: the maps of the warps before it
+// (kBack: behind it) are applied to what enters the block's.  In a block of its
+// own that is what left the tile before, put down by the warp that came last
+// (`leaves`); in a cluster what left the cluster's rows before, `carry`, through
+// the maps of the blocks before it.
 struct Joint {
   Map warps[2][kWarps][32];
   Map blocks[2][kMostCluster][32];
+  float2 carry[2][32];
 };
 template <bool kBack, bool kPacked>
 __device__ __forceinline__ float2 join(Joint &s, int turn, const Map &own, float2 &carry, int warp,
                                        int lane, int rank, int size) {
   s.warps[turn][warp][lane] = own;
   __syncthreads();
-  Map before{splat(1.f), splat(0.f)}, all{splat(1.f), splat(0.f)};
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    const int w = kBack ? kWarps - 1 - i : i;
-    if (w == warp) before = all;
-    all = compose<kPacked>(all, s.warps[turn][w][lane]);
+  Map before{splat(1.f), splat(0.f)};
+  for (int w = kBack ? kWarps - 1 : 0; w != warp; w += kBack ? -1 : 1)
+    before = compose<kPacked>(before, s.warps[turn][w][lane]);
+  if (size == 1) return apply<kPacked>(before, s.carry[turn][lane]);
+  const cg::cluster_group cluster = cg::this_cluster();
+  if (warp == (kBack ? 0 : kWarps - 1)) {
+    const Map all = compose<kPacked>(before, own);
+    for (int r = 0; r < size; ++r) *cluster.map_shared_rank(&s.blocks[turn][rank][lane], r) = all;
   }
+  cluster.sync();
   float2 enters = carry;
-  if (size == 1) {
-    carry = apply<kPacked>(all, carry);
-  } else {
-    const cg::cluster_group cluster = cg::this_cluster();
-    for (int r = warp; r < size; r += kWarps)
-      *cluster.map_shared_rank(&s.blocks[turn][rank][lane], r) = all;
-    cluster.sync();
-    for (int i = 0; i < size; ++i) {
-      const int r = kBack ? size - 1 - i : i;
-      if (r == rank) enters = carry;
-      carry = apply<kPacked>(s.blocks[turn][r][lane], carry);
-    }
+  for (int i = 0; i < size; ++i) {
+    const int r = kBack ? size - 1 - i : i;
+    if (r == rank) enters = carry;
+    carry = apply<kPacked>(s.blocks[turn][r][lane], carry);
   }
   return apply<kPacked>(before, enters);
+}
+template <bool kBack>
+__device__ __forceinline__ void leaves(Joint &s, int turn, float2 h, int warp, int lane, int size) {
+  if (size == 1 && warp == (kBack ? 0 : kWarps - 1)) s.carry[turn][lane] = h;
 }
 
 // An empty sequence ends in the state it starts from.
@@ -220,43 +221,52 @@ __device__ __forceinline__ void copy_async(void *dst, const void *src, bool has)
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(src), "r"(has ? 4 : 0)
                  : "memory");
 }
-// Rows [r0, r0 + n) of a strip whose first channel is c0; others are zeros.
+// Where a lane's part of a run of rows is, n <= 8 of them (the others become
+// zeros), the first a row `pitch` values long apart.
 template <typename T, bool kWide>
-__device__ __forceinline__ void copy_rows(T (*to)[kStrip], const Rows<const T> &from, int64_t b,
-                                          int r0, int n, int64_t c0, int64_t channels, int lane) {
-  if constexpr (kWide) {
-    constexpr int per = 16 / sizeof(T), chunks = kStrip / per;
-    const int c = lane % chunks * per;
-    const bool in = c0 + c < channels;
-#pragma unroll
-    for (int i = 0; i < kRun * chunks / 32; ++i) {
-      const int r = lane / chunks + i * (32 / chunks);
-      const bool has = in && r < n;
-      copy_async<16>(&to[r][c], has ? from.at(b, r0 + r) + c0 + c : from.p, has);
-    }
-  } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int r = 0; r < kRun; ++r)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int c = lane + 32 * k;
-        const bool has = r < n && c0 + c < channels;
-        copy_async<4>(&to[r][c], has ? from.at(b, r0 + r) + c0 + c : from.p, has);
-      }
-  } else {
-    T v[kRun][2];
-#pragma unroll
-    for (int r = 0; r < kRun; ++r)
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        v[r][k] = r < n && c0 + lane + 32 * k < channels ? from.at(b, r0 + r)[c0 + lane + 32 * k]
-                                                         : from_f<T>(0.f);
-#pragma unroll
-    for (int r = 0; r < kRun; ++r)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) to[r][lane + 32 * k] = v[r][k];
+struct Source {
+  static constexpr int kPer = 16 / sizeof(T), kChunks = kStrip / kPer;
+  const T *p;
+  int64_t pitch;
+  __device__ __forceinline__ void init(const Rows<const T> &from, int64_t b, int r0, int64_t c0,
+                                       int lane) {
+    pitch = from.row;
+    p = from.p + b * from.batch + c0 + (kWide ? lane % kChunks * kPer : lane) +
+        ((int64_t)r0 + (kWide ? lane / kChunks : 0)) * pitch;
   }
-}
+  __device__ __forceinline__ void copy(T (*to)[kStrip], int n, int64_t c0, int64_t channels,
+                                       int lane) const {
+    if constexpr (kWide) {
+      constexpr int each = 32 / kChunks;
+      const int r = lane / kChunks, c = lane % kChunks * kPer;
+      const bool in = c0 + c < channels;
+      const T *q = p;
+#pragma unroll
+      for (int i = 0; i < kRun / each; ++i, q += each * pitch)
+        if (in) copy_async<16>(&to[r + i * each][c], r + i * each < n ? q : p, r + i * each < n);
+    } else if constexpr (sizeof(T) == 4) {
+      const T *q = p;
+#pragma unroll
+      for (int r = 0; r < kRun; ++r, q += pitch)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          if (c0 + lane + 32 * k < channels)
+            copy_async<4>(&to[r][lane + 32 * k], r < n ? q + 32 * k : p, r < n);
+    } else {
+      T v[kRun][2];
+      const T *q = p;
+#pragma unroll
+      for (int r = 0; r < kRun; ++r, q += pitch)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          v[r][k] = r < n && c0 + lane + 32 * k < channels ? q[32 * k] : from_f<T>(0.f);
+#pragma unroll
+      for (int r = 0; r < kRun; ++r)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) to[r][lane + 32 * k] = v[r][k];
+    }
+  }
+};
 __device__ __forceinline__ void copies_commit() {
   asm volatile("cp.async.commit_group;" ::: "memory");
 }
@@ -309,32 +319,47 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
   const int64_t c0 = (int64_t)(blockIdx.x / size) * kStrip, c = c0 + 2 * lane;
   const int count = (int)max((int64_t)0, min((int64_t)2, a.channels - c));
   const float2 minus = make_float2(-rate.x, -rate.y);
-  const int64_t step = (int64_t)size * kTile;
+  const int step = size * kTile;
   auto &ring = s.ring[warp];
   int turn = 0;
   for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
+    const int start = rank * kTile + warp * kRun;  // this warp's rows begin there, a step apart
     float2 carry = splat(0.f);
     if (!kPacked && a.state) carry = pair_at<kWide>(a.state, (int64_t)b * a.channels + c, count);
-    const auto ask = [&](int64_t t0, int stage) {
-      const int r0 = (int)min(t0 + (int64_t)rank * kTile + warp * kRun, (int64_t)a.rows);
-      const int n = t0 < a.rows ? min(kRun, a.rows - r0) : 0;
-      copy_rows<T, kWide>(ring.v[stage][0], a.forget, b, r0, n, c0, a.channels, lane);
-      copy_rows<T, kWide>(ring.v[stage][1], a.admit, b, r0, n, c0, a.channels, lane);
-      copy_rows<T, kWide>(ring.v[stage][2], a.x, b, r0, n, c0, a.channels, lane);
+    leaves<false>(s.joint, turn, carry, warp, lane, size);
+    Source<T, kWide> from[3];
+    from[0].init(a.forget, b, start, c0, lane);
+    from[1].init(a.admit, b, start, c0, lane);
+    from[2].init(a.x, b, start, c0, lane);
+    T *y = a.y.at(b, 0) + c + (int64_t)start * a.y.row;
+    float *mark = a.marks + ((int64_t)b * a.runs + start / kRun) * a.channels + c;
+    int ahead = start;  // row that is asked for next
+    const auto ask = [&](int stage) {
+      const int n = min(kRun, a.rows - ahead);
+      if (n > 0) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          from[k].copy(ring.v[stage][k], n, c0, a.channels, lane);
+          from[k].p += step * from[k].pitch;
+        }
+      }
+      ahead += step;
       copies_commit();
     };
     __syncwarp();
-    for (int i = 0; i < kStages - 1; ++i) ask(i * step, i);
+    for (int i = 0; i < kStages - 1; ++i) ask(i);
     int stage = 0;
-    for (int64_t t0 = 0; t0 < a.rows; t0 += step) {
-      const int64_t at = t0 + (int64_t)rank * kTile + warp * kRun;
-      const int r0 = (int)min(at, (int64_t)a.rows);
-      const int n = min(kRun, a.rows - r0);
+    for (int t0 = 0; t0 < a.rows; t0 += step) {
+      const int r0 = t0 + start, n = min(kRun, a.rows - r0);  // no row where n <= 0
       __syncwarp();
-      ask(t0 + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
+      ask(stage == 0 ? kStages - 1 : stage - 1);
       Marks8 seqs{};
       if (n > 0) seqs = sequences_of<kPacked>(a, b, r0, lane);
       copies_wait<kStages - 1>();
+      // a run of whole rows in which no sequence opens (dense: a row 0 takes
+      // the carry) or closes goes without a look at each row
+      const bool plain = seqs.inside == (1u << kRun) - 1 && seqs.close == 0 &&
+                         (!kPacked || seqs.open == 0);
       float2 keep[kRun], add[kRun];
       Map run{splat(1.f), splat(0.f)};
 #pragma unroll
@@ -344,34 +369,53 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
         const Decay d = decay2<kAllNear>(__fmul2_rn(sigmoid2(f), minus));
         keep[i] = d.a;
         add[i] = __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g)), x);
-        if constexpr (kPacked) {
+      }
+      if (kPacked && !plain) {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
           if (!(seqs.inside >> i & 1)) keep[i] = splat(1.f), add[i] = splat(0.f);
           if (seqs.open >> i & 1) {
             const int64_t q = __shfl_sync(~0u, seqs.seq, i);
             run = {splat(0.f), a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f)};
           }
+          run = {__fmul2_rn(run.A, keep[i]), __ffma2_rn(run.H, keep[i], add[i])};
         }
-        run = {__fmul2_rn(run.A, keep[i]), __ffma2_rn(run.H, keep[i], add[i])};
+      } else {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+          run = {__fmul2_rn(run.A, keep[i]), __ffma2_rn(run.H, keep[i], add[i])};
       }
       stage = stage == kStages - 1 ? 0 : stage + 1;
       float2 h = join<false, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size);
       turn ^= 1;
-      if (n <= 0) continue;
-      if (a.marks)
-        put_pair<kWide>(a.marks, ((int64_t)b * a.runs + r0 / kRun) * a.channels + c, count, h);
+      if (n > 0) {
+        if (a.marks) put_pair<kWide>(mark, 0, count, h);
+        T *to = y;
+        if (plain) {
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        if (kPacked && (seqs.open >> i & 1)) {
-          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-          h = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
-        }
-        h = __ffma2_rn(h, keep[i], add[i]);
-        if (seqs.inside >> i & 1) put_row<T, kWide>(a.y.at(b, r0 + i) + c, h, count);
-        if (seqs.close >> i & 1) {
-          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-          if (a.last) put_pair<kWide>(a.last, q * a.channels + c, count, h);
+          for (int i = 0; i < kRun; ++i, to += a.y.row) {
+            h = __ffma2_rn(h, keep[i], add[i]);
+            put_row<T, kWide>(to, h, count);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kRun; ++i, to += a.y.row) {
+            if (kPacked && (seqs.open >> i & 1)) {
+              const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+              h = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
+            }
+            h = __ffma2_rn(h, keep[i], add[i]);
+            if (seqs.inside >> i & 1) put_row<T, kWide>(to, h, count);
+            if (seqs.close >> i & 1) {
+              const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+              if (a.last) put_pair<kWide>(a.last, q * a.channels + c, count, h);
+            }
+          }
         }
       }
+      leaves<false>(s.joint, turn, h, warp, lane, size);
+      y += step * (int64_t)a.y.row;
+      mark += (int64_t)(step / kRun) * a.channels;
     }
     copies_wait<0>();
   }
@@ -410,39 +454,55 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
   const int64_t c0 = (int64_t)(blockIdx.x / size) * kStrip, c = c0 + 2 * lane;
   const int count = (int)max((int64_t)0, min((int64_t)2, a.channels - c));
   const float2 minus = make_float2(-rate.x, -rate.y);
-  const int64_t step = (int64_t)size * kTile;
+  const int step = size * kTile;
   auto &ring = s.ring[warp];
   float2 drate = splat(0.f);
   int turn = 0;
+  const int end = (a.rows - 1) / step * step;  // the last tile
   for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
+    const int start = end + rank * kTile + warp * kRun;
     float2 carry = splat(0.f);  // a_{t+1} e_{t+1} of the row below
     if (!kPacked && a.dlast) carry = pair_at<kWide>(a.dlast, (int64_t)b * a.channels + c, count);
-    const auto ask = [&](int64_t t0, int stage) {
-      const int r0 = (int)min(max((int64_t)0, t0) + (int64_t)rank * kTile + warp * kRun, (int64_t)a.rows);
-      const int n = t0 >= 0 ? min(kRun, a.rows - r0) : 0;
-      copy_rows<T, kWide>(ring.v[stage][0], a.forget, b, r0, n, c0, a.channels, lane);
-      copy_rows<T, kWide>(ring.v[stage][1], a.admit, b, r0, n, c0, a.channels, lane);
-      copy_rows<T, kWide>(ring.v[stage][2], a.x, b, r0, n, c0, a.channels, lane);
-      copy_rows<T, kWide>(ring.v[stage][3], a.dy, b, r0, n, c0, a.channels, lane);
+    leaves<true>(s.joint, turn, carry, warp, lane, size);
+    Source<T, kWide> from[4];
+    from[0].init(a.forget, b, start, c0, lane);
+    from[1].init(a.admit, b, start, c0, lane);
+    from[2].init(a.x, b, start, c0, lane);
+    from[3].init(a.dy, b, start, c0, lane);
+    // outputs: at the run's last row, walked upwards
+    T *to[3];
+    const Rows<T> *outs[3] = {&a.dx, &a.dadmit, &a.dforget};
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      to[k] = outs[k]->at(b, 0) + c + ((int64_t)start + kRun - 1) * outs[k]->row;
+    const float *mark = a.marks + ((int64_t)b * a.runs + start / kRun) * a.channels + c;
+    int ahead = start;
+    const auto ask = [&](int stage) {
+      const int n = min(kRun, a.rows - ahead);
+      if (n > 0 && ahead >= 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) from[k].copy(ring.v[stage][k], n, c0, a.channels, lane);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) from[k].p -= step * from[k].pitch;
+      ahead -= step;
       copies_commit();
     };
-    const int64_t end = (a.rows - 1) / step * step;
     __syncwarp();
-    for (int i = 0; i < kStages - 1; ++i) ask(end - i * step, i);
+    for (int i = 0; i < kStages - 1; ++i) ask(i);
     int stage = 0;
-    for (int64_t t0 = end; t0 >= 0; t0 -= step) {
-      const int64_t at = t0 + (int64_t)rank * kTile + warp * kRun;
-      const int r0 = (int)min(at, (int64_t)a.rows);
-      const int n = min(kRun, a.rows - r0);
+    for (int t0 = end; t0 >= 0; t0 -= step) {
+      const int r0 = t0 + rank * kTile + warp * kRun, n = min(kRun, a.rows - r0);
       __syncwarp();
-      ask(t0 - (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
+      ask(stage == 0 ? kStages - 1 : stage - 1);
       Marks8 seqs{};
       float2 h = splat(0.f);
       if (n > 0) {
         seqs = sequences_of<kPacked>(a, b, r0, lane);
-        h = pair_at<kWide>(a.marks, ((int64_t)b * a.runs + r0 / kRun) * a.channels + c, count);
+        h = pair_at<kWide>(mark, 0, count);
       }
       copies_wait<kStages - 1>();
+      const bool plain = seqs.inside == (1u << kRun) - 1 && seqs.close == 0 && seqs.open == 0;
       const auto &rows = ring.v[stage];
       // forward: decays and the state before each row
       float2 keep[kRun], root[kRun], before[kRun];
@@ -460,35 +520,29 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
                                           pair_of(rows[2], i, lane)));
       }
       Map run{splat(1.f), splat(0.f)};
+      if (plain) {
 #pragma unroll
-      for (int i = kRun - 1; i >= 0; --i) {
-        if (kPacked && (seqs.close >> i & 1)) {
-          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-          run = {splat(0.f), a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f)};
+        for (int i = kRun - 1; i >= 0; --i)
+          run = {__fmul2_rn(run.A, keep[i]),
+                 __fmul2_rn(__fadd2_rn(run.H, pair_of(rows[3], i, lane)), keep[i])};
+      } else {
+#pragma unroll
+        for (int i = kRun - 1; i >= 0; --i) {
+          if (kPacked && (seqs.close >> i & 1)) {
+            const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+            run = {splat(0.f), a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f)};
+          }
+          if (!(seqs.inside >> i & 1)) continue;
+          run = {__fmul2_rn(run.A, keep[i]),
+                 __fmul2_rn(__fadd2_rn(run.H, pair_of(rows[3], i, lane)), keep[i])};
+          if (kPacked && (seqs.open >> i & 1)) run = {splat(0.f), splat(0.f)};
         }
-        if (!(seqs.inside >> i & 1)) continue;
-        run = {__fmul2_rn(run.A, keep[i]),
-               __fmul2_rn(__fadd2_rn(run.H, pair_of(rows[3], i, lane)), keep[i])};
-        if (kPacked && (seqs.open >> i & 1)) run = {splat(0.f), splat(0.f)};
       }
       float2 e = join<true, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size);
       turn ^= 1;
       float2 share = splat(0.f);
-#pragma unroll
-      for (int i = kRun - 1; i >= 0; --i) {
-        if (i >= n) continue;
-        T *dx = a.dx.at(b, r0 + i) + c, *dg = a.dadmit.at(b, r0 + i) + c,
-          *df = a.dforget.at(b, r0 + i) + c;
-        if (kPacked && !(seqs.inside >> i & 1)) {  // rows of no sequence
-          put_row<T, kWide>(dx, splat(0.f), count);
-          put_row<T, kWide>(dg, splat(0.f), count);
-          put_row<T, kWide>(df, splat(0.f), count);
-          continue;
-        }
-        if (kPacked && (seqs.close >> i & 1)) {
-          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-          e = a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f);
-        }
+      // the gradients of row i from that of its state, e, which becomes the row above's
+      const auto row = [&](int i, T *dx, T *dg, T *df) {
         e = __fadd2_rn(e, pair_of(rows[3], i, lane));
         const float2 open = sigmoid2(pair_of(rows[0], i, lane)), way = sigmoid2(pair_of(rows[1], i, lane)),
                      x = pair_of(rows[2], i, lane), k = keep[i];
@@ -505,13 +559,39 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
         share = __fadd2_rn(share, dL);
         put_row<T, kWide>(df, __ffma2_rn(dL, __fmul2_rn(open, splat(-1.f)), dL), count);
         e = __fmul2_rn(e, k);
-        if ((seqs.open >> i & 1) && a.dstate) {
-          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-          put_pair<kWide>(a.dstate, q * a.channels + c, count, e);
+      };
+      T *dx = to[0], *dg = to[1], *df = to[2];
+      if (plain) {
+#pragma unroll
+        for (int i = kRun - 1; i >= 0; --i, dx -= a.dx.row, dg -= a.dadmit.row, df -= a.dforget.row)
+          row(i, dx, dg, df);
+      } else {
+#pragma unroll
+        for (int i = kRun - 1; i >= 0; --i, dx -= a.dx.row, dg -= a.dadmit.row, df -= a.dforget.row) {
+          if (i >= n) continue;
+          if (kPacked && !(seqs.inside >> i & 1)) {  // rows of no sequence
+            put_row<T, kWide>(dx, splat(0.f), count);
+            put_row<T, kWide>(dg, splat(0.f), count);
+            put_row<T, kWide>(df, splat(0.f), count);
+            continue;
+          }
+          if (kPacked && (seqs.close >> i & 1)) {
+            const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+            e = a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f);
+          }
+          row(i, dx, dg, df);
+          if ((seqs.open >> i & 1) && a.dstate) {
+            const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+            put_pair<kWide>(a.dstate, q * a.channels + c, count, e);
+          }
         }
       }
       drate = __fadd2_rn(drate, share);
+      leaves<true>(s.joint, turn, e, warp, lane, size);
       stage = stage == kStages - 1 ? 0 : stage + 1;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) to[k] -= step * (int64_t)outs[k]->row;
+      mark -= (int64_t)(step / kRun) * a.channels;
     }
     copies_wait<0>();
   }
@@ -578,12 +658,15 @@ GatedPlan plan_of(const tcu_gated_scan_args &a, bool grad) {
   p.batches = a.offsets ? 1 : a.sequences;
   p.strips = (a.channels + kStrip - 1) / kStrip;
   p.entries = std::min<int64_t>(p.batches, 65535);
-  // Blocks of a cluster share a strip's rows: as many as rows give tiles, while
-  // all blocks run at once.
+  // Blocks of a cluster share a strip's rows, where blocks are fewer than the
+  // card's places.  A tile takes 1.3 us, 2.5 with its cluster's exchange, and
+  // blocks of an SM slow each other down: 65536 x 1536, 24 strips, forward: 958,
+  // 497, 367, 402 us in clusters of 2, 4, 8, 16; 8192 x 256 x 2: 122, 67, 40, 32;
+  // 8 x 2048 x 4096, 512 strips: 124 us whole, 140 in clusters of 2.
   const int64_t tiles = (a.rows + kTile - 1) / kTile;
-  const int64_t places = (int64_t)num_sms() * (a.type != TCU_SEQ_F32 && !grad ? 3 : 2);
   p.size = 1;
-  while (p.size < kMostCluster && p.size < tiles && 2 * p.strips * p.entries * p.size <= places)
+  while (p.size < kMostCluster && p.size < tiles &&
+         4 * p.strips * p.entries * p.size <= 3 * (int64_t)num_sms())
     p.size *= 2;
   p.row_seq = a.offsets ? (a.rows + 3) / 4 * 4 : 0;
   p.parts = grad ? p.entries * p.size * a.channels : 0;

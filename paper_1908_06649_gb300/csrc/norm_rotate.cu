@@ -8,8 +8,7 @@
 //     dx = r g w - x r^3 (sum g w x) / d
 // Some ten operations for each value read and written: HBM bounds it.  A warp
 // owns a row, with a few lanes for each head; a lane holds the same pairs of
-// every head, so that a row's angles are formed once for all its heads, and
-// weights, rates and the shares of dw stay in registers.  Both values of a pair
+// every head, so that a row's angles are formed once for all its heads.  Both values of a pair
 // are in the same lane: rows may be written over those that they come from.
 #include <algorithm>
 
@@ -44,76 +43,70 @@ struct Part {
   static constexpr int kParts = VP >= 4 ? 1 : 4 / VP;
 };
 
+// A lane's values of a head as they lie in memory.
 template <typename T, int VP>
-__device__ __forceinline__ void load_word(const T *p, bool has, float *v) {
-  if (has) {
-    const Vec<T, VP> w = *reinterpret_cast<const Vec<T, VP> *>(p);
-#pragma unroll
-    for (int i = 0; i < VP; ++i) v[i] = to_f(w.v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < VP; ++i) v[i] = 0.f;
-  }
-}
-template <typename T, int VP>
-__device__ __forceinline__ void store_word(T *p, bool has, const float *v) {
-  if (!has) return;
-  Vec<T, VP> w;
-#pragma unroll
-  for (int i = 0; i < VP; ++i) w.v[i] = from_f<T>(v[i]);
-  *reinterpret_cast<Vec<T, VP> *>(p) = w;
-}
+struct Words {
+  Vec<T, VP> w[Part<VP>::kParts][2];
+};
 
 template <typename T, int VP, bool kInter>
 struct Lane {
   static constexpr int kParts = Part<VP>::kParts;
-  int at[kParts][2];
+  int first[kParts], at[kParts][2];  // pair, values
   bool has[kParts];
-  uint64_t turn[kParts][VP];  // turns of one position, in 2^-64
 
   __device__ __forceinline__ void init(const RotateArgs<T> &a, int j) {
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
       const int p = (j + k * a.lanes) * VP;
       has[k] = p < a.dim / 2;
+      first[k] = has[k] ? p : 0;
       const bool apart = !kInter && p < a.turned;
       at[k][0] = apart ? p : 2 * p;
       at[k][1] = apart ? p + a.turned : 2 * p + VP;
-#pragma unroll
-      for (int i = 0; i < VP; ++i) {
-        turn[k][i] = 0;
-        if (p + i >= a.turned) continue;
-        // whole turns of a position change nothing; 2^64 of the rest, signed
-        const double t = (double)a.rates[p + i] * 0.15915494309189535;
-        const double f = fabs(t) - floor(fabs(t));
-        const uint64_t u = (uint64_t)(f * 18446744073709551616.0);
-        turn[k][i] = t < 0 ? 0 - u : u;
-      }
     }
   }
   // cos and sin of the lane's angles at a position: the product wraps as turns do
-  __device__ __forceinline__ void angles(int64_t position, float (*c)[VP], float (*s)[VP]) const {
+  __device__ __forceinline__ void angles(const uint64_t *turns, int64_t position, float (*c)[VP],
+                                         float (*s)[VP]) const {
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
 #pragma unroll
       for (int i = 0; i < VP; ++i) {
-        const int32_t t = (int32_t)(uint32_t)(((uint64_t)position * turn[k][i]) >> 32);
+        const int32_t t = (int32_t)(uint32_t)(((uint64_t)position * turns[first[k] + i]) >> 32);
         sincospif((float)t * 4.656612873077393e-10f, &s[k][i], &c[k][i]);  // 2^-31
       }
   }
-  __device__ __forceinline__ void load(const T *head, bool in, float (*v)[2 * VP]) const {
+  __device__ __forceinline__ void load(const T *head, bool in, Words<T, VP> &v) const {
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-      load_word<T, VP>(head + at[k][0], in && has[k], v[k]);
-      load_word<T, VP>(head + at[k][1], in && has[k], v[k] + VP);
-    }
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (in && has[k]) {
+          v.w[k][j] = *reinterpret_cast<const Vec<T, VP> *>(head + at[k][j]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < VP; ++i) v.w[k][j].v[i] = from_f<T>(0.f);
+        }
+      }
+  }
+  static __device__ __forceinline__ void values(const Words<T, VP> &w, float (*v)[2 * VP]) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int i = 0; i < 2 * VP; ++i) v[k][i] = to_f(w.w[k][i / VP].v[i % VP]);
   }
   __device__ __forceinline__ void store(T *head, bool in, const float (*v)[2 * VP]) const {
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-      store_word<T, VP>(head + at[k][0], in && has[k], v[k]);
-      store_word<T, VP>(head + at[k][1], in && has[k], v[k] + VP);
-    }
+    for (int k = 0; k < kParts; ++k)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!in || !has[k]) continue;
+        Vec<T, VP> w;
+#pragma unroll
+        for (int i = 0; i < VP; ++i) w.v[i] = from_f<T>(v[k][j * VP + i]);
+        *reinterpret_cast<Vec<T, VP> *>(head + at[k][j]) = w;
+      }
   }
   // turns by the angles (kBack: against them)
   template <bool kBack>
@@ -159,15 +152,36 @@ __device__ __forceinline__ bool place_of(const RotateArgs<T> &a, int64_t id, int
   return true;
 }
 
+// The turns of one position, in 2^-64, of each pair of a head; whole turns
+// change nothing.
+constexpr int kPairs = TCU_ATTN_MAX_NORM_DIM / 2;
+template <typename T>
+__device__ __forceinline__ void fill_turns(const RotateArgs<T> &a, uint64_t *turns) {
+  for (int p = threadIdx.x; p < kPairs; p += kThreads) {
+    uint64_t u = 0;
+    if (p < a.turned) {
+      const double t = (double)a.rates[p] * 0.15915494309189535;
+      const double f = fabs(t) - floor(fabs(t));
+      u = (uint64_t)(f * 18446744073709551616.0);
+      if (t < 0) u = 0 - u;
+    }
+    turns[p] = u;
+  }
+  __syncthreads();
+}
+
+// Heads of a lane whose loads are on their way together.
+template <typename T, int VP>
+constexpr int kAtOnce = VP * sizeof(T) == 16 ? 4 : 2;
+
 template <typename T, int VP, bool kInter>
-__global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs<T> a) {
-  constexpr int kParts = Part<VP>::kParts;
+__global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const RotateArgs<T> a) {
+  constexpr int kParts = Part<VP>::kParts, kMany = kAtOnce<T, VP>;
+  __shared__ uint64_t turns[kPairs];
+  fill_turns(a, turns);
   const int lane = threadIdx.x % 32, per = 32 / a.lanes, sub = lane / a.lanes;
   Lane<T, VP, kInter> own;
   own.init(a, lane % a.lanes);
-  float wq[kParts][2 * VP], wk[kParts][2 * VP];
-  own.weights(a.q_weight, wq);
-  own.weights(a.k_weight, wk);
   const float inv = 1.f / a.dim;
   const int64_t step = (int64_t)gridDim.x * kWarps;
   for (int64_t id = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; id < a.total; id += step) {
@@ -175,42 +189,61 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs<T> a)
     int t;
     if (!place_of(a, id, b, t, position)) continue;
     float c[kParts][VP], s[kParts][VP];
-    own.angles(position, c, s);
-    auto heads = [&](const T *from, T *to, int count, const float (*w)[2 * VP]) {
-#pragma unroll 2
-      for (int h0 = 0; h0 < count; h0 += per) {
-        const int h = h0 + sub;
-        const bool in = h < count;
-        float v[kParts][2 * VP];
-        own.load(from + (int64_t)h * a.dim, in, v);
-        float squares = 0.f;
+    own.angles(turns, position, c, s);
+    auto heads = [&](const T *from, T *to, int count, const float *weight) {
+      float w[kParts][2 * VP];
+      own.weights(weight, w);
+      for (int h0 = sub; h0 - sub < count; h0 += kMany * per) {
+        Words<T, VP> words[kMany];
 #pragma unroll
-        for (int k = 0; k < kParts; ++k)
+        for (int m = 0; m < kMany; ++m)
+          own.load(from + (int64_t)(h0 + m * per) * a.dim, h0 + m * per < count, words[m]);
 #pragma unroll
-          for (int i = 0; i < 2 * VP; ++i) squares = fmaf(v[k][i], v[k][i], squares);
-        const float r = rsqrtf(fmaf(sum_lanes(squares, a.lanes), inv, a.eps));
+        for (int m = 0; m < kMany; ++m) {
+          if (h0 - sub + m * per >= count) break;  // the whole warp
+          float v[kParts][2 * VP];
+          own.values(words[m], v);
+          float squares = 0.f;
 #pragma unroll
-        for (int k = 0; k < kParts; ++k)
+          for (int k = 0; k < kParts; ++k)
 #pragma unroll
-          for (int i = 0; i < 2 * VP; ++i) v[k][i] *= r * w[k][i];
-        own.template rotate<false>(v, c, s);
-        own.store(to + (int64_t)h * a.dim, in, v);
+            for (int i = 0; i < 2 * VP; ++i) squares = fmaf(v[k][i], v[k][i], squares);
+          const float r = rsqrtf(fmaf(sum_lanes(squares, a.lanes), inv, a.eps));
+#pragma unroll
+          for (int k = 0; k < kParts; ++k)
+#pragma unroll
+            for (int i = 0; i < 2 * VP; ++i) v[k][i] *= r * w[k][i];
+          own.template rotate<false>(v, c, s);
+          own.store(to + (int64_t)(h0 + m * per) * a.dim, h0 + m * per < count, v);
+        }
       }
     };
-    heads(a.q.at(b, t), a.yq.at(b, t), a.heads, wq);
-    heads(a.k.at(b, t), a.yk.at(b, t), a.kv_heads, wk);
+    heads(a.q.at(b, t), a.yq.at(b, t), a.heads, a.q_weight);
+    heads(a.k.at(b, t), a.yk.at(b, t), a.kv_heads, a.k_weight);
   }
 }
 
+template <int VP>
+struct GradShared {
+  // each lane's shares of dw, [queries, keys][value][thread]
+  float shares[2][2 * VP * Part<VP>::kParts][kThreads];
+  float sums[kWarps][2 * TCU_ATTN_MAX_NORM_DIM];
+  uint64_t turns[kPairs];
+};
+
 template <typename T, int VP, bool kInter>
-__global__ void __launch_bounds__(kThreads) rotate_grad_kernel(const RotateArgs<T> a) {
-  constexpr int kParts = Part<VP>::kParts;
-  __shared__ float sums[kWarps][2 * TCU_ATTN_MAX_NORM_DIM];
+__global__ void __launch_bounds__(kThreads, 2) rotate_grad_kernel(const RotateArgs<T> a) {
+  constexpr int kParts = Part<VP>::kParts, kMany = kAtOnce<T, VP> / 2;
+  extern __shared__ __align__(16) uint8_t raw[];
+  GradShared<VP> &sh = *reinterpret_cast<GradShared<VP> *>(raw);
+  fill_turns(a, sh.turns);
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int per = 32 / a.lanes, sub = lane / a.lanes;
   Lane<T, VP, kInter> own;
   own.init(a, lane % a.lanes);
-  float dwq[kParts][2 * VP] = {}, dwk[kParts][2 * VP] = {};
+#pragma unroll
+  for (int i = 0; i < 2 * VP * kParts; ++i)
+    sh.shares[0][i][threadIdx.x] = sh.shares[1][i][threadIdx.x] = 0.f;
   const float inv = 1.f / a.dim;
   const int64_t step = (int64_t)gridDim.x * kWarps;
   for (int64_t id = (int64_t)blockIdx.x * kWarps + warp; id < a.total; id += step) {
@@ -218,45 +251,60 @@ __global__ void __launch_bounds__(kThreads) rotate_grad_kernel(const RotateArgs<
     int t;
     const bool row = place_of(a, id, b, t, position);
     float c[kParts][VP], s[kParts][VP];
-    if (row) own.angles(position, c, s);
-    auto heads = [&](const T *from, const T *dy, T *to, int count, const float *weight,
-                     float (*dw)[2 * VP]) {
-      float w[kParts][2 * VP];
+    if (row) own.angles(sh.turns, position, c, s);
+    auto heads = [&](const T *from, const T *dy, T *to, int count, const float *weight, int which) {
+      float w[kParts][2 * VP], dw[kParts][2 * VP] = {};
       own.weights(weight, w);
-      for (int h0 = 0; h0 < count; h0 += per) {
-        const int h = h0 + sub;
-        const bool in = h < count;
-        float x[kParts][2 * VP], g[kParts][2 * VP];
-        own.load(from + (int64_t)h * a.dim, in && row, x);
-        own.load(dy + (int64_t)h * a.dim, in && row, g);
-        if (row) {
-          own.template rotate<true>(g, c, s);
-          float squares = 0.f, dot = 0.f;
+      for (int h0 = sub; h0 - sub < count; h0 += kMany * per) {
+        Words<T, VP> xs[kMany], gs[kMany];
 #pragma unroll
-          for (int k = 0; k < kParts; ++k)
-#pragma unroll
-            for (int i = 0; i < 2 * VP; ++i) {
-              squares = fmaf(x[k][i], x[k][i], squares);
-              dot = fmaf(g[k][i] * w[k][i], x[k][i], dot);
-            }
-          for (int m = 1; m < a.lanes; m *= 2) {
-            squares += __shfl_xor_sync(~0u, squares, m);
-            dot += __shfl_xor_sync(~0u, dot, m);
-          }
-          const float r = rsqrtf(fmaf(squares, inv, a.eps)), back = r * r * r * dot * inv;
-#pragma unroll
-          for (int k = 0; k < kParts; ++k)
-#pragma unroll
-            for (int i = 0; i < 2 * VP; ++i) {
-              dw[k][i] = fmaf(g[k][i], x[k][i] * r, dw[k][i]);
-              g[k][i] = fmaf(g[k][i] * w[k][i], r, -x[k][i] * back);
-            }
+        for (int m = 0; m < kMany; ++m) {
+          const bool in = row && h0 + m * per < count;
+          own.load(from + (int64_t)(h0 + m * per) * a.dim, in, xs[m]);
+          own.load(dy + (int64_t)(h0 + m * per) * a.dim, in, gs[m]);
         }
-        own.store(to + (int64_t)h * a.dim, in, g);  // zeros for a row of no sequence
+#pragma unroll
+        for (int m = 0; m < kMany; ++m) {
+          if (h0 - sub + m * per >= count) break;  // the whole warp
+          float x[kParts][2 * VP], g[kParts][2 * VP];
+          own.values(xs[m], x);
+          own.values(gs[m], g);
+          if (row) {
+            own.template rotate<true>(g, c, s);
+            float squares = 0.f, dot = 0.f;
+#pragma unroll
+            for (int k = 0; k < kParts; ++k)
+#pragma unroll
+              for (int i = 0; i < 2 * VP; ++i) {
+                squares = fmaf(x[k][i], x[k][i], squares);
+                dot = fmaf(g[k][i] * w[k][i], x[k][i], dot);
+              }
+            for (int i = 1; i < a.lanes; i *= 2) {
+              squares += __shfl_xor_sync(~0u, squares, i);
+              dot += __shfl_xor_sync(~0u, dot, i);
+            }
+            const float r = rsqrtf(fmaf(squares, inv, a.eps)), back = r * r * r * dot * inv;
+#pragma unroll
+            for (int k = 0; k < kParts; ++k)
+#pragma unroll
+              for (int i = 0; i < 2 * VP; ++i) {
+                dw[k][i] = fmaf(g[k][i], x[k][i] * r, dw[k][i]);
+                g[k][i] = fmaf(g[k][i] * w[k][i], r, -x[k][i] * back);
+              }
+          }
+          // zeros for a row of no sequence
+          own.store(to + (int64_t)(h0 + m * per) * a.dim, h0 + m * per < count, g);
+        }
+      }
+      if (a.parts && row) {
+#pragma unroll
+        for (int k = 0; k < kParts; ++k)
+#pragma unroll
+          for (int i = 0; i < 2 * VP; ++i) sh.shares[which][k * 2 * VP + i][threadIdx.x] += dw[k][i];
       }
     };
-    heads(a.q.at(b, t), a.dyq.at(b, t), a.dq.at(b, t), a.heads, a.q_weight, dwq);
-    heads(a.k.at(b, t), a.dyk.at(b, t), a.dk.at(b, t), a.kv_heads, a.k_weight, dwk);
+    heads(a.q.at(b, t), a.dyq.at(b, t), a.dq.at(b, t), a.heads, a.q_weight, 0);
+    heads(a.k.at(b, t), a.dyk.at(b, t), a.dk.at(b, t), a.kv_heads, a.k_weight, 1);
   }
   if (!a.parts) return;
   // lanes of the same values, then warps, in a fixed order
@@ -264,21 +312,21 @@ __global__ void __launch_bounds__(kThreads) rotate_grad_kernel(const RotateArgs<
   for (int k = 0; k < kParts; ++k)
 #pragma unroll
     for (int i = 0; i < 2 * VP; ++i) {
-      float x = dwq[k][i], y = dwk[k][i];
+      float x = sh.shares[0][k * 2 * VP + i][threadIdx.x], y = sh.shares[1][k * 2 * VP + i][threadIdx.x];
       for (int m = a.lanes; m < 32; m *= 2) {
         x += __shfl_xor_sync(~0u, x, m);
         y += __shfl_xor_sync(~0u, y, m);
       }
       if (sub == 0 && own.has[k]) {
         const int at = own.at[k][i / VP] + i % VP;
-        sums[warp][at] = x;
-        sums[warp][a.dim + at] = y;
+        sh.sums[warp][at] = x;
+        sh.sums[warp][a.dim + at] = y;
       }
     }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * a.dim; i += kThreads) {
     float x = 0.f;
-    for (int w = 0; w < kWarps; ++w) x += sums[w][i];
+    for (int w = 0; w < kWarps; ++w) x += sh.sums[w][i];
     a.parts[(int64_t)blockIdx.x * 2 * a.dim + i] = x;
   }
 }
@@ -288,7 +336,7 @@ __global__ void __launch_bounds__(kThreads) rotate_grad_kernel(const RotateArgs<
 // shares of the weights' gradients over many rows.
 int64_t blocks_of(const tcu_norm_rotate_args &a, bool grad) {
   const int64_t total = (a.offsets ? 1 : (int64_t)a.sequences) * a.rows;
-  return std::min<int64_t>((total + kWarps - 1) / kWarps, (grad ? 3 : 4) * num_sms());
+  return std::min<int64_t>((total + kWarps - 1) / kWarps, 2 * num_sms());
 }
 
 template <typename T, int VP, bool kInter>
@@ -297,7 +345,14 @@ int start(const tcu_norm_rotate_args &s, RotateArgs<T> a, bool grad, cudaStream_
   a.lanes = 1;
   while (a.lanes < 32 && a.lanes < words) a.lanes *= 2;
   const unsigned blocks = (unsigned)blocks_of(s, grad);
-  if (grad) rotate_grad_kernel<T, VP, kInter><<<blocks, kThreads, 0, st>>>(a);
+  constexpr int bytes = sizeof(GradShared<VP>);
+  if (grad && cudaFuncSetAttribute(rotate_grad_kernel<T, VP, kInter>,
+                                   cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return TCU_DFT_ERR_CUDA;
+  }
+  if (grad) rotate_grad_kernel<T, VP, kInter><<<blocks, kThreads, bytes, st>>>(a);
   else rotate_kernel<T, VP, kInter><<<blocks, kThreads, 0, st>>>(a);
   return launched();
 }
