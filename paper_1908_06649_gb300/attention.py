@@ -184,13 +184,15 @@ class _RotateCall:
 def _rotate(q, k, rates, q_weight, k_weight, positions, offsets, eps, interleaved, out, stream):
     c = _RotateCall(q, k, rates, q_weight, k_weight, positions, offsets, eps, interleaved)
     with _On(c.index, stream) as st:
+        qs, ks = c.shapes
         if out is None:
-            yq, yk = (torch.empty(s, dtype=c.dtype, device=q.device) for s in c.shapes)
+            yq = torch.empty(qs, dtype=c.dtype, device=q.device)
+            yk = torch.empty(ks, dtype=c.dtype, device=q.device)
+            ys = _fresh(yq, qs) + _fresh(yk, ks)
         else:
             yq, yk = out
-        ys = (*_grouped_rows(yq, "out", c.dtype, c.index, c.shapes[0]),
-              *_grouped_rows(yk, "out", c.dtype, c.index, c.shapes[1]))
-        if out is not None:
+            ys = (_grouped_rows(yq, "out", c.dtype, c.index, qs)
+                  + _grouped_rows(yk, "out", c.dtype, c.index, ks))
             others = (rates, q_weight, k_weight, positions, offsets)
             _apart(yq, (k, *others), in_place=(q,))
             _apart(yk, (q, yq, *others), in_place=(k,))
@@ -284,15 +286,30 @@ _HALF = {torch.bfloat16: 1, torch.float16: 2}
 
 def _rows16(t, name, dtype, index, shape):
     """_grouped_rows of rows that 16-byte accesses and tensor maps reach."""
-    r = _grouped_rows(t, name, dtype, index, shape)
-    if not t.numel():
-        return r
-    values, many = shape[-1] * shape[-2], len(shape) == 4
-    rows, batch = (shape[1], shape[0]) if many else (shape[0], 1)
-    if (r[0] % 16 or (rows > 1 and (r[2] % 8 or r[2] < values))
-            or (batch > 1 and (r[1] % 8 or r[1] < values))):
+    if not isinstance(t, torch.Tensor):
+        _tensor(t, name)
+    st, ptr = t.stride(), t.data_ptr()
+    if len(st) == 4:
+        batch, rows, heads, dim = shape
+        b, r, h, d = st
+    else:
+        batch, (rows, heads, dim) = 1, shape
+        b, (r, h, d) = 0, st if len(st) == 3 else (0, 0, 0)
+    values = heads * dim
+    if (t.dtype is dtype and t.shape == shape and t.get_device() == index and (h == dim or heads == 1)
+            and d == 1 and ptr % 16 == 0 and (rows <= 1 or (r % 8 == 0 and r >= values))
+            and (batch <= 1 or (b % 8 == 0 and b >= values))):
+        return ptr, b, r
+    r = _grouped_rows(t, name, dtype, index, shape)  # raises what is wrong
+    if t.numel():
         raise ValueError("%s must hold its rows apart, each at a multiple of 16 bytes" % name)
     return r
+
+
+def _fresh(t, shape):
+    """A new tensor's rows."""
+    row = shape[-1] * shape[-2]
+    return (t.data_ptr(), shape[1] * row, row) if len(shape) == 4 else (t.data_ptr(), 0, row)
 
 
 def _bounds(window, sinks, scale, dim):
@@ -332,9 +349,12 @@ _NO_CACHE = (0, 0, 0, 0, 0)
 def _attend(q, k, v, window, sinks, scale, offsets, lse, out, stream):
     c = _AttentionCall(q, k, v, window, sinks, scale, offsets)
     with _On(c.index, stream) as st:
-        y = torch.empty(c.shapes[0], dtype=c.dtype, device=q.device) if out is None else out
-        py = _rows16(y, "out", c.dtype, c.index, c.shapes[0])
-        if out is not None:
+        if out is None:
+            y = torch.empty(c.shapes[0], dtype=c.dtype, device=q.device)
+            py = _fresh(y, c.shapes[0])
+        else:
+            y = out
+            py = _rows16(y, "out", c.dtype, c.index, c.shapes[0])
             _apart(out, (q, k, v, offsets))
         sums = torch.empty(c.shapes[0][:-1], dtype=torch.float32, device=q.device) if lse else None
         _call("tcu_window_attention", _ATTEND.pack(*c.sizes, *c.rows, *py, sums.data_ptr() if lse else 0,
@@ -460,9 +480,12 @@ def window_attention_step(q, k, v, cache_k, cache_v, positions, *, window, sinks
         _tensor(positions, "positions")
     pp = _flat(positions, "positions", torch.int32, c.index, (batch,))
     with _On(c.index, stream) as st:
-        y = torch.empty(c.shapes[0], dtype=c.dtype, device=q.device) if out is None else out
-        py = _rows16(y, "out", c.dtype, c.index, c.shapes[0])
-        if out is not None:
+        if out is None:
+            y = torch.empty(c.shapes[0], dtype=c.dtype, device=q.device)
+            py = _fresh(y, c.shapes[0])
+        else:
+            y = out
+            py = _rows16(y, "out", c.dtype, c.index, c.shapes[0])
             _apart(out, (q, k, v, cache_k, cache_v, positions, slots))
         t, _, heads, kv, dim, w, s, scale = c.sizes[:8]
         r = c.rows

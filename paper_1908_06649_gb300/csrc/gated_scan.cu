@@ -25,6 +25,7 @@
 #include <algorithm>
 
 #include "seq_common.cuh"
+#include "tcgen05.cuh"
 
 namespace tcu {
 namespace seq {
@@ -159,26 +160,55 @@ __device__ __forceinline__ void put_pair(float *p, int64_t at, int count, float2
 // own that is what left the tile before, put down by the warp that came last
 // (`leaves`); in a cluster what left the cluster's rows before, `carry`, through
 // the maps of the blocks before it.
+// Blocks send their maps to each other as stores that the receiver's mbarrier
+// counts; two sets of maps are enough, since a block sends the next but one
+// only when all have sent the next, and so have read the last.
 struct Joint {
   Map warps[2][kWarps][32];
   Map blocks[2][kMostCluster][32];
   float2 carry[2][32];
+  uint64_t arrived[2];
 };
+__device__ __forceinline__ void send_map(uint32_t to, const Map &m, uint32_t mbar) {
+  asm volatile(
+      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, "
+      "[%5];" ::"r"(to),
+      "f"(m.A.x), "f"(m.A.y), "f"(m.H.x), "f"(m.H.y), "r"(mbar)
+      : "memory");
+}
+__device__ __forceinline__ void expect_maps(Joint &s, int turn, int size) {
+  mbar_expect_tx(smem_u32(&s.arrived[turn]), size * 32 * (uint32_t)sizeof(Map));
+}
+__device__ __forceinline__ void start_joint(Joint &s, int size) {
+  if (size == 1) return;
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&s.arrived[0]), 1);
+    mbar_init(smem_u32(&s.arrived[1]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    expect_maps(s, 0, size);
+    expect_maps(s, 1, size);
+  }
+  cg::this_cluster().sync();
+}
 template <bool kBack, bool kPacked>
 __device__ __forceinline__ float2 join(Joint &s, int turn, const Map &own, float2 &carry, int warp,
-                                       int lane, int rank, int size) {
+                                       int lane, int rank, int size, int &phase) {
   s.warps[turn][warp][lane] = own;
   __syncthreads();
   Map before{splat(1.f), splat(0.f)};
   for (int w = kBack ? kWarps - 1 : 0; w != warp; w += kBack ? -1 : 1)
     before = compose<kPacked>(before, s.warps[turn][w][lane]);
   if (size == 1) return apply<kPacked>(before, s.carry[turn][lane]);
-  const cg::cluster_group cluster = cg::this_cluster();
   if (warp == (kBack ? 0 : kWarps - 1)) {
     const Map all = compose<kPacked>(before, own);
-    for (int r = 0; r < size; ++r) *cluster.map_shared_rank(&s.blocks[turn][rank][lane], r) = all;
+    const uint32_t to = smem_u32(&s.blocks[turn][rank][lane]), mbar = smem_u32(&s.arrived[turn]);
+    for (int r = 0; r < size; ++r) send_map(mapa_shared(to, r), all, mapa_shared(mbar, r));
   }
-  cluster.sync();
+  // phase: -1 once a wait has run out, and what follows is no number
+  if (phase >= 0 && !mbar_wait_cluster_bounded(smem_u32(&s.arrived[turn]), phase >> 1 & 1)) phase = -1;
+  if (phase < 0) return splat(__int_as_float(0x7fffffff));
+  ++phase;
+  if (threadIdx.x == 0) expect_maps(s, turn, size);
   float2 enters = carry;
   for (int i = 0; i < size; ++i) {
     const int r = kBack ? size - 1 - i : i;
@@ -321,7 +351,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
   const float2 minus = make_float2(-rate.x, -rate.y);
   const int step = size * kTile;
   auto &ring = s.ring[warp];
-  int turn = 0;
+  int turn = 0, phase = 0;
   for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
     const int start = rank * kTile + warp * kRun;  // this warp's rows begin there, a step apart
     float2 carry = splat(0.f);
@@ -386,7 +416,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
           run = {__fmul2_rn(run.A, keep[i]), __ffma2_rn(run.H, keep[i], add[i])};
       }
       stage = stage == kStages - 1 ? 0 : stage + 1;
-      float2 h = join<false, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size);
+      float2 h = join<false, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size, phase);
       turn ^= 1;
       if (n > 0) {
         if (a.marks) put_pair<kWide>(mark, 0, count, h);
@@ -421,7 +451,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
   }
   if (kPacked && a.last && blockIdx.y == 0)
     empty_sequences<kWide>(a, a.last, a.state, c, count, rank * kWarps + warp, size * kWarps);
-  if (size > 1) cg::this_cluster().sync();  // no block leaves while others write to it
+  if (size > 1) cg::this_cluster().sync();  // no block leaves while others send to it
 }
 
 // The rate of each of the lane's channels, and whether no decay of the warp's
@@ -439,6 +469,7 @@ __global__ void __launch_bounds__(kThreads, Sizes<T>::kBlocks)
     gated_kernel(const GatedArgs<T> a, int size) {
   extern __shared__ __align__(16) uint8_t raw[];
   GatedShared<T> &s = *reinterpret_cast<GatedShared<T> *>(raw);
+  start_joint(s.joint, size);
   bool near;
   const float2 rate = rates<kWide>(a, size, near);
   if (near) gated_rows<T, kPacked, kWide, true>(a, s, size, rate);
@@ -457,7 +488,7 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
   const int step = size * kTile;
   auto &ring = s.ring[warp];
   float2 drate = splat(0.f);
-  int turn = 0;
+  int turn = 0, phase = 0;
   const int end = (a.rows - 1) / step * step;  // the last tile
   for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
     const int start = end + rank * kTile + warp * kRun;
@@ -538,7 +569,7 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
           if (kPacked && (seqs.open >> i & 1)) run = {splat(0.f), splat(0.f)};
         }
       }
-      float2 e = join<true, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size);
+      float2 e = join<true, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size, phase);
       turn ^= 1;
       float2 share = splat(0.f);
       // the gradients of row i from that of its state, e, which becomes the row above's
@@ -614,6 +645,7 @@ __global__ void __launch_bounds__(kThreads, Sizes<T>::kGradBlocks)
     gated_grad_kernel(const GatedArgs<T> a, int size) {
   extern __shared__ __align__(16) uint8_t raw[];
   GradShared<T> &s = *reinterpret_cast<GradShared<T> *>(raw);
+  start_joint(s.joint, size);
   bool near;
   const float2 rate = rates<kWide>(a, size, near);
   if (near) grad_rows<T, kPacked, kWide, true>(a, s, size, rate);

@@ -8,8 +8,9 @@
 //     dx = r g w - x r^3 (sum g w x) / d
 // Some ten operations for each value read and written: HBM bounds it.  A warp
 // owns a row, with a few lanes for each head; a lane holds the same pairs of
-// every head, so that a row's angles are formed once for all its heads.  Both values of a pair
-// are in the same lane: rows may be written over those that they come from.
+// every head, so that a row's angles are formed once for all its heads.  Both
+// values of a pair are in the same lane: rows may be written over those that
+// they come from.
 #include <algorithm>
 
 #include "../../include/tcu_attn.h"
@@ -170,13 +171,20 @@ __device__ __forceinline__ void fill_turns(const RotateArgs<T> &a, uint64_t *tur
   __syncthreads();
 }
 
-// Heads of a lane whose loads are on their way together.
+// Heads of a lane whose loads are on their way together, and the longest word.
+// At 16384 rows x 40 heads x 128, bf16 (168 MB), forward: words of 8 values, 4
+// heads 67 us, 5 heads 82, of 4 values 85.  The gradient holds two tensors and
+// its sums beside them: words of 8 spill, 214 us; of 4, 4 heads 137 us, 2 heads
+// 171, 3 heads 146.
+template <int VP>
+constexpr int kAtOnce = VP >= 4 ? 4 : 2;
 template <typename T, int VP>
-constexpr int kAtOnce = VP * sizeof(T) == 16 ? 4 : 2;
+constexpr int kGradAtOnce = VP == 4 && sizeof(T) == 2 ? 4 : 2;
+constexpr int kGradWord = 4;
 
 template <typename T, int VP, bool kInter>
 __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const RotateArgs<T> a) {
-  constexpr int kParts = Part<VP>::kParts, kMany = kAtOnce<T, VP>;
+  constexpr int kParts = Part<VP>::kParts, kMany = kAtOnce<VP>;
   __shared__ uint64_t turns[kPairs];
   fill_turns(a, turns);
   const int lane = threadIdx.x % 32, per = 32 / a.lanes, sub = lane / a.lanes;
@@ -233,7 +241,7 @@ struct GradShared {
 
 template <typename T, int VP, bool kInter>
 __global__ void __launch_bounds__(kThreads, 2) rotate_grad_kernel(const RotateArgs<T> a) {
-  constexpr int kParts = Part<VP>::kParts, kMany = kAtOnce<T, VP> / 2;
+  constexpr int kParts = Part<VP>::kParts, kMany = kGradAtOnce<T, VP>;
   extern __shared__ __align__(16) uint8_t raw[];
   GradShared<VP> &sh = *reinterpret_cast<GradShared<VP> *>(raw);
   fill_turns(a, sh.turns);
@@ -346,14 +354,18 @@ int start(const tcu_norm_rotate_args &s, RotateArgs<T> a, bool grad, cudaStream_
   while (a.lanes < 32 && a.lanes < words) a.lanes *= 2;
   const unsigned blocks = (unsigned)blocks_of(s, grad);
   constexpr int bytes = sizeof(GradShared<VP>);
-  if (grad && cudaFuncSetAttribute(rotate_grad_kernel<T, VP, kInter>,
-                                   cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   bytes) != cudaSuccess) {
-    cudaGetLastError();
-    return TCU_DFT_ERR_CUDA;
+  if (!grad) {
+    rotate_kernel<T, VP, kInter><<<blocks, kThreads, 0, st>>>(a);
+    return launched();
   }
-  if (grad) rotate_grad_kernel<T, VP, kInter><<<blocks, kThreads, bytes, st>>>(a);
-  else rotate_kernel<T, VP, kInter><<<blocks, kThreads, 0, st>>>(a);
+  if constexpr (VP <= kGradWord) {
+    if (cudaFuncSetAttribute(rotate_grad_kernel<T, VP, kInter>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+      cudaGetLastError();
+      return TCU_DFT_ERR_CUDA;
+    }
+    rotate_grad_kernel<T, VP, kInter><<<blocks, kThreads, bytes, st>>>(a);
+  }
   return launched();
 }
 
@@ -398,7 +410,7 @@ int run(const tcu_norm_rotate_args &s, bool grad, cudaStream_t st) {
   int rc = TCU_DFT_OK;
   if (a.total > 0) {
     // the longest words that keep pairs of one kind together and lie aligned
-    int vp = 16 / (int)sizeof(T);
+    int vp = grad ? kGradWord : 16 / (int)sizeof(T);
     auto fits = [&](int n) {
       if (s.dim / 2 % n || s.turned % n) return false;
       for (int i = 0; i < count; ++i)
