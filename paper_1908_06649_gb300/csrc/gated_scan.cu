@@ -40,7 +40,10 @@ namespace cg = cooperative_groups;
 constexpr int kRun = TCU_SEQ_GATED_MARK;  // rows of a thread
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kTile = kRun * kWarps;  // rows of a block at a time
+constexpr int kTile = kRun * kWarps;  // rows of a block at a time, in the gradient
+// Forward a thread takes two runs below each other: a tile's exchange costs as
+// much as 64 rows' arithmetic.  The gradient's registers hold one.
+constexpr int kRuns = 2, kMine = kRuns * kRun, kLongTile = kRuns * kTile;
 constexpr int kStrip = 64;            // channels of a block
 constexpr int kMostCluster = 16;
 
@@ -324,8 +327,8 @@ __device__ __forceinline__ void put_row(T *to, float2 v, int count) {
 // Blocks an SM, and stages: what its shared memory holds, and the registers.
 template <typename T>
 struct Sizes {
-  static constexpr int kStages = sizeof(T) == 2 ? 2 : 1;
-  static constexpr int kBlocks = sizeof(T) == 2 ? 3 : 2, kGradBlocks = 2;
+  static constexpr int kStages = sizeof(T) == 2 ? 3 : 1, kGradStages = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kBlocks = 2, kGradBlocks = 2;
 };
 
 template <typename T>
@@ -337,7 +340,7 @@ template <typename T>
 struct GradShared {
   Joint joint;
   float2 sums[kWarps][32];
-  Ring<T, 4, Sizes<T>::kStages> ring[kWarps];
+  Ring<T, 4, Sizes<T>::kGradStages> ring[kWarps];
 };
 
 template <typename T, bool kPacked, bool kWide, bool kAllNear>
@@ -349,11 +352,11 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
   const int64_t c0 = (int64_t)(blockIdx.x / size) * kStrip, c = c0 + 2 * lane;
   const int count = (int)max((int64_t)0, min((int64_t)2, a.channels - c));
   const float2 minus = make_float2(-rate.x, -rate.y);
-  const int step = size * kTile;
+  const int step = size * kLongTile;
   auto &ring = s.ring[warp];
   int turn = 0, phase = 0;
   for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
-    const int start = rank * kTile + warp * kRun;  // this warp's rows begin there, a step apart
+    const int start = rank * kLongTile + warp * kMine;  // this warp's rows, a step apart
     float2 carry = splat(0.f);
     if (!kPacked && a.state) carry = pair_at<kWide>(a.state, (int64_t)b * a.channels + c, count);
     leaves<false>(s.joint, turn, carry, warp, lane, size);
@@ -363,81 +366,90 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
     from[2].init(a.x, b, start, c0, lane);
     T *y = a.y.at(b, 0) + c + (int64_t)start * a.y.row;
     float *mark = a.marks + ((int64_t)b * a.runs + start / kRun) * a.channels + c;
-    int ahead = start;  // row that is asked for next
+    int ahead = start, sub = 0;  // row that is asked for next, which of a tile's runs
     const auto ask = [&](int stage) {
       const int n = min(kRun, a.rows - ahead);
       if (n > 0) {
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          from[k].copy(ring.v[stage][k], n, c0, a.channels, lane);
-          from[k].p += step * from[k].pitch;
-        }
+        for (int k = 0; k < 3; ++k) from[k].copy(ring.v[stage][k], n, c0, a.channels, lane);
       }
-      ahead += step;
+      const int hop = sub == kRuns - 1 ? step - kMine + kRun : kRun;
+      sub = sub == kRuns - 1 ? 0 : sub + 1;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) from[k].p += hop * from[k].pitch;
+      ahead = a.rows - ahead > hop ? ahead + hop : a.rows;  // the sum may pass 2^31
       copies_commit();
     };
     __syncwarp();
-    for (int i = 0; i < kStages - 1; ++i) ask(i);
+    for (int i = 0; i < kStages; ++i) ask(i);
     int stage = 0;
     for (int t0 = 0; t0 < a.rows; t0 += step) {
-      const int r0 = t0 + start, n = min(kRun, a.rows - r0);  // no row where n <= 0
-      __syncwarp();
-      ask(stage == 0 ? kStages - 1 : stage - 1);
-      Marks8 seqs{};
-      if (n > 0) seqs = sequences_of<kPacked>(a, b, r0, lane);
-      copies_wait<kStages - 1>();
-      // a run of whole rows in which no sequence opens (dense: a row 0 takes
-      // the carry) or closes goes without a look at each row
-      const bool plain = seqs.inside == (1u << kRun) - 1 && seqs.close == 0 &&
-                         (!kPacked || seqs.open == 0);
-      float2 keep[kRun], add[kRun];
+      const int r0 = t0 + start;
+      float2 keep[kRuns][kRun], add[kRuns][kRun];
+      Marks8 seqs[kRuns];
+      bool plain[kRuns];
       Map run{splat(1.f), splat(0.f)};
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        const float2 f = pair_of(ring.v[stage][0], i, lane), g = pair_of(ring.v[stage][1], i, lane),
-                     x = pair_of(ring.v[stage][2], i, lane);
-        const Decay d = decay2<kAllNear>(__fmul2_rn(sigmoid2(f), minus));
-        keep[i] = d.a;
-        add[i] = __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g)), x);
-      }
-      if (kPacked && !plain) {
+      for (int u = 0; u < kRuns; ++u) {
+        seqs[u] = Marks8{};
+        if (r0 + u * kRun < a.rows) seqs[u] = sequences_of<kPacked>(a, b, r0 + u * kRun, lane);
+        copies_wait<kStages - 1>();
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-          if (!(seqs.inside >> i & 1)) keep[i] = splat(1.f), add[i] = splat(0.f);
-          if (seqs.open >> i & 1) {
-            const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-            run = {splat(0.f), a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f)};
-          }
-          run = {__fmul2_rn(run.A, keep[i]), __ffma2_rn(run.H, keep[i], add[i])};
+          const float2 f = pair_of(ring.v[stage][0], i, lane), g = pair_of(ring.v[stage][1], i, lane),
+                       x = pair_of(ring.v[stage][2], i, lane);
+          const Decay d = decay2<kAllNear>(__fmul2_rn(sigmoid2(f), minus));
+          keep[u][i] = d.a;
+          add[u][i] = __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g)), x);
         }
-      } else {
+        __syncwarp();
+        ask(stage);
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        // a run of whole rows in which no sequence opens (dense: a row 0 takes
+        // the carry) or closes goes without a look at each row
+        plain[u] = seqs[u].inside == (1u << kRun) - 1 && seqs[u].close == 0 &&
+                   (!kPacked || seqs[u].open == 0);
+        if (kPacked && !plain[u]) {
 #pragma unroll
-        for (int i = 0; i < kRun; ++i)
-          run = {__fmul2_rn(run.A, keep[i]), __ffma2_rn(run.H, keep[i], add[i])};
+          for (int i = 0; i < kRun; ++i) {
+            if (!(seqs[u].inside >> i & 1)) keep[u][i] = splat(1.f), add[u][i] = splat(0.f);
+            if (seqs[u].open >> i & 1) {
+              const int64_t q = __shfl_sync(~0u, seqs[u].seq, i);
+              run = {splat(0.f),
+                     a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f)};
+            }
+            run = {__fmul2_rn(run.A, keep[u][i]), __ffma2_rn(run.H, keep[u][i], add[u][i])};
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kRun; ++i)
+            run = {__fmul2_rn(run.A, keep[u][i]), __ffma2_rn(run.H, keep[u][i], add[u][i])};
+        }
       }
-      stage = stage == kStages - 1 ? 0 : stage + 1;
       float2 h = join<false, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size, phase);
       turn ^= 1;
-      if (n > 0) {
-        if (a.marks) put_pair<kWide>(mark, 0, count, h);
-        T *to = y;
-        if (plain) {
+      T *to = y;
+#pragma unroll
+      for (int u = 0; u < kRuns; ++u) {
+        if (r0 + u * kRun >= a.rows) break;
+        if (a.marks) put_pair<kWide>(mark + u * a.channels, 0, count, h);
+        if (plain[u]) {
 #pragma unroll
           for (int i = 0; i < kRun; ++i, to += a.y.row) {
-            h = __ffma2_rn(h, keep[i], add[i]);
+            h = __ffma2_rn(h, keep[u][i], add[u][i]);
             put_row<T, kWide>(to, h, count);
           }
         } else {
 #pragma unroll
           for (int i = 0; i < kRun; ++i, to += a.y.row) {
-            if (kPacked && (seqs.open >> i & 1)) {
-              const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+            if (kPacked && (seqs[u].open >> i & 1)) {
+              const int64_t q = __shfl_sync(~0u, seqs[u].seq, i);
               h = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
             }
-            h = __ffma2_rn(h, keep[i], add[i]);
-            if (seqs.inside >> i & 1) put_row<T, kWide>(to, h, count);
-            if (seqs.close >> i & 1) {
-              const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+            h = __ffma2_rn(h, keep[u][i], add[u][i]);
+            if (seqs[u].inside >> i & 1) put_row<T, kWide>(to, h, count);
+            if (seqs[u].close >> i & 1) {
+              const int64_t q = __shfl_sync(~0u, seqs[u].seq, i);
               if (a.last) put_pair<kWide>(a.last, q * a.channels + c, count, h);
             }
           }
@@ -479,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, Sizes<T>::kBlocks)
 template <typename T, bool kPacked, bool kWide, bool kAllNear>
 __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &s, int size,
                                           float2 rate) {
-  constexpr int kStages = Sizes<T>::kStages;
+  constexpr int kStages = Sizes<T>::kGradStages;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int rank = (int)(blockIdx.x % size);
   const int64_t c0 = (int64_t)(blockIdx.x / size) * kStrip, c = c0 + 2 * lane;
@@ -520,12 +532,10 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
       copies_commit();
     };
     __syncwarp();
-    for (int i = 0; i < kStages - 1; ++i) ask(i);
+    for (int i = 0; i < kStages; ++i) ask(i);
     int stage = 0;
     for (int t0 = end; t0 >= 0; t0 -= step) {
       const int r0 = t0 + rank * kTile + warp * kRun, n = min(kRun, a.rows - r0);
-      __syncwarp();
-      ask(stage == 0 ? kStages - 1 : stage - 1);
       Marks8 seqs{};
       float2 h = splat(0.f);
       if (n > 0) {
@@ -619,6 +629,8 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
       }
       drate = __fadd2_rn(drate, share);
       leaves<true>(s.joint, turn, e, warp, lane, size);
+      __syncwarp();
+      ask(stage);
       stage = stage == kStages - 1 ? 0 : stage + 1;
 #pragma unroll
       for (int k = 0; k < 3; ++k) to[k] -= step * (int64_t)outs[k]->row;
@@ -690,16 +702,21 @@ GatedPlan plan_of(const tcu_gated_scan_args &a, bool grad) {
   p.batches = a.offsets ? 1 : a.sequences;
   p.strips = (a.channels + kStrip - 1) / kStrip;
   p.entries = std::min<int64_t>(p.batches, 65535);
-  // Blocks of a cluster share a strip's rows, where blocks are fewer than the
-  // card's places.  A tile takes 1.3 us, 2.5 with its cluster's exchange, and
-  // blocks of an SM slow each other down: 65536 x 1536, 24 strips, forward: 958,
-  // 497, 367, 402 us in clusters of 2, 4, 8, 16; 8192 x 256 x 2: 122, 67, 40, 32;
-  // 8 x 2048 x 4096, 512 strips: 124 us whole, 140 in clusters of 2.
-  const int64_t tiles = (a.rows + kTile - 1) / kTile;
+  // Blocks of a cluster share a strip's rows, where strips are fewer than the
+  // card's places, two an SM: the largest size at which all clusters run at
+  // once.  Large clusters find fewer places, since each lies within one part of
+  // the card.  65536 x 1536, 24 strips, forward: 340, 279, 239, 295, 280 us in
+  // clusters of 4, 8, 9, 12, 16; 4121 x 1031 f32, 17 strips: 58, 47, 42, 34, 49;
+  // 8192 x 4096, 64 strips: 71, 79 us in clusters of 4, 8; 8 x 2048 x 4096, 512
+  // strips: 114 us whole, 121 in clusters of 2.
+  const int64_t tile = grad ? kTile : kLongTile, tiles = (a.rows + tile - 1) / tile;
+  const int64_t strips = p.strips * p.entries, sms = num_sms();
   p.size = 1;
-  while (p.size < kMostCluster && p.size < tiles &&
-         4 * p.strips * p.entries * p.size <= 3 * (int64_t)num_sms())
-    p.size *= 2;
+  for (const int size : {16, 12, 9, 8, 6, 4, 3, 2})
+    if (size <= tiles && strips * size <= (size > 4 ? sms * 29 / 20 : sms * 9 / 5)) {
+      p.size = size;
+      break;
+    }
   p.row_seq = a.offsets ? (a.rows + 3) / 4 * 4 : 0;
   p.parts = grad ? p.entries * p.size * a.channels : 0;
   return p;
