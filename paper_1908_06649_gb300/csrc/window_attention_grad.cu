@@ -85,15 +85,18 @@ template <int DP>
 struct QueryShared {
   uint8_t q[kTileBytes<DP, kRows>], dy[kTileBytes<DP, kRows>];
   uint8_t k[2][kTileBytes<DP, kStep>], v[kTileBytes<DP, kStep>];
-  uint64_t full_k[2], full_v, scores, weights, done;
+  uint64_t full_k[2], full_v, scores, weights, done[2];
   uint32_t tmem;
   int low, sink_at, sink_end, failed;
 };
 
+// Two blocks share an SM, which holds 228 KB, 1 KB beside each block's own.
+static_assert(2 * (sizeof(QueryShared<128>) + 1024) <= 228 * 1024, "two blocks an SM");
+
 template <typename T, int DP>
-__global__ void __launch_bounds__(kSoft + 32, 2)
+__global__ void __launch_bounds__(kSoft + 64, 2)
     dq_kernel(const __grid_constant__ QueryMaps maps, const AttendArgs a, const Rows<T> dq,
-              const int *most) {
+              const int *most, float *exact) {
   extern __shared__ __align__(1024) uint8_t raw[];
   QueryShared<DP> &s = *reinterpret_cast<QueryShared<DP> *>(raw);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -103,8 +106,9 @@ __global__ void __launch_bounds__(kSoft + 32, 2)
   const int kv = head / (a.heads / a.kv_heads);
   const uint32_t full_k = smem_u32(s.full_k), full_v = smem_u32(&s.full_v),
                  scores = smem_u32(&s.scores), weights = smem_u32(&s.weights),
-                 done = smem_u32(&s.done);
+                 done = smem_u32(s.done);
   if (threadIdx.x == 0) {
+    mbar_init(done + 8, 1);
     mbar_init(full_k, 1);
     mbar_init(full_k + 8, 1);
     mbar_init(full_v, 1);
@@ -145,79 +149,79 @@ __global__ void __launch_bounds__(kSoft + 32, 2)
   };
   const float c = a.scale * kLog2e;
 
-  if (warp == kSoft / 32) {
-    const uint32_t q = smem_u32(s.q), dy = smem_u32(s.dy), k = smem_u32(s.k), v = smem_u32(s.v);
-    constexpr uint32_t bytes = kTileBytes<DP, kStep>;
+  const uint32_t q = smem_u32(s.q), dy = smem_u32(s.dy), k = smem_u32(s.k), v = smem_u32(s.v);
+  constexpr uint32_t bytes = kTileBytes<DP, kStep>;
+  if (warp == kSoft / 32 + 1) {  // copies
     bool ok = true;
-    int keys = min(2, tiles), values = 1;  // tiles asked for
-    if (tiles > 0 && elect_one()) {
-      mbar_expect_tx(full_k, 2 * kTileBytes<DP, kRows> + bytes);
-      load_tile<DP, kRows>(q, &maps.q, head, tile * kRows, batch, full_k);
-      load_tile<DP, kStep>(k, &maps.k, kv, key_row(0), batch, full_k);
-      load_tile<DP, kRows>(dy, &maps.dy, head, tile * kRows, batch, full_k);
-      mbar_expect_tx(full_v, bytes);
-      load_tile<DP, kStep>(v, &maps.v, kv, key_row(0), batch, full_v);
-      if (tiles > 1) {
-        mbar_expect_tx(full_k + 8, bytes);
-        load_tile<DP, kStep>(k + bytes, &maps.k, kv, key_row(1), batch, full_k + 8);
+    int keys = 0, values = 0;  // tiles asked for
+    for (int t = 0; t < tiles && ok; ++t) {
+      const uint32_t stage = t & 1;
+      // dq of t - 2 has read its keys, the scores of t - 1 their values
+      if (t > 1) ok = mbar_wait_bounded(done + 8 * stage, ((t - 2) >> 1) & 1);
+      if (!ok) break;
+      if (elect_one()) {
+        mbar_expect_tx(full_k + 8 * stage, bytes + (t == 0 ? 2 * kTileBytes<DP, kRows> : 0));
+        if (t == 0) {
+          load_tile<DP, kRows>(q, &maps.q, head, tile * kRows, batch, full_k);
+          load_tile<DP, kRows>(dy, &maps.dy, head, tile * kRows, batch, full_k);
+        }
+        load_tile<DP, kStep>(k + stage * bytes, &maps.k, kv, key_row(t), batch, full_k + 8 * stage);
       }
+      __syncwarp();
+      keys = t + 1;
+      if (t > 0) ok = mbar_wait_bounded(scores, (t - 1) & 1);
+      if (!ok) break;
+      if (elect_one()) {
+        mbar_expect_tx(full_v, bytes);
+        load_tile<DP, kStep>(v, &maps.v, kv, key_row(t), batch, full_v);
+      }
+      __syncwarp();
+      values = t + 1;
     }
-    __syncwarp();
+    if (!ok) {  // copies in flight end before the block does
+      s.failed = 1;
+      if (values > 0) mbar_wait_bounded(full_v, (values - 1) & 1);
+      for (int i = 1; i <= 2; ++i)
+        if (keys >= i) mbar_wait_bounded(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
+    }
+  } else if (warp == kSoft / 32) {  // products
+    bool ok = true;
     for (int t = 0; t < tiles; ++t) {
-      const uint32_t ph = t & 1, stage = t & 1, other = stage ^ 1;
+      const uint32_t ph = t & 1, stage = t & 1;
       ok = mbar_wait_bounded(full_k + 8 * stage, (t >> 1) & 1) && mbar_wait_bounded(full_v, ph);
       // scores take the place of what the last product has read
-      if (t > 0) ok = ok && mbar_wait_bounded(done, ph ^ 1);
+      if (t > 0) ok = ok && mbar_wait_bounded(done + 8 * (stage ^ 1), ((t - 1) >> 1) & 1);
       if (!ok) break;
       fence_after_sync();
       if (elect_one()) {
-        if (t > 0 && t + 1 < tiles) {
-          mbar_expect_tx(full_k + 8 * other, bytes);
-          load_tile<DP, kStep>(k + other * bytes, &maps.k, kv, key_row(t + 1), batch,
-                               full_k + 8 * other);
-        }
         product_rows<T, DP, kStep>(tS, q, k + stage * bytes);
         product_rows<T, DP, kStep>(tP, dy, v);
         mma_commit(scores);
       }
       __syncwarp();
-      if (t > 0 && t + 1 < tiles) keys = t + 2;
-      ok = mbar_wait_bounded(scores, ph);
-      if (ok && t + 1 < tiles) {
-        if (elect_one()) {
-          mbar_expect_tx(full_v, bytes);
-          load_tile<DP, kStep>(v, &maps.v, kv, key_row(t + 1), batch, full_v);
-        }
-        __syncwarp();
-        values = t + 2;
-      }
-      ok = ok && mbar_wait_bounded(weights, ph);
+      ok = mbar_wait_bounded(weights, ph);
       if (!ok) break;
       fence_after_sync();
       if (elect_one()) {
         product_values<T, DP, kStep>(tQ, tS, k + stage * bytes, t > 0);
-        mma_commit(done);
+        mma_commit(done + 8 * stage);
       }
       __syncwarp();
     }
-    if (!ok) {  // copies in flight end before the block does
-      s.failed = 1;
-      mbar_wait_bounded(full_v, (values - 1) & 1);
-      mbar_wait_bounded(full_k + 8 * ((keys - 1) & 1), ((keys - 1) >> 1) & 1);
-      if (keys > 1) mbar_wait_bounded(full_k + 8 * (keys & 1), ((keys - 2) >> 1) & 1);
-    }
+    if (!ok) s.failed = 1;
   } else {
     const int half = threadIdx.x / kRows;  // of the row: 32 keys, and half of its dq
     const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
     const int begin = a.offsets ? a.offsets[0] : 0;
     const int end = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
     const float lift = lift_of(most);
+    const int64_t at = ((int64_t)batch * a.rows + max(0, seen.i)) * a.heads + head;
     float lse = 0.f, delta = 0.f;
     if (seen.i >= 0) {
-      const int64_t at = ((int64_t)batch * a.rows + seen.i) * a.heads + head;
       lse = a.lse[at] * kLog2e;
       delta = a.delta[at] * lift;
     }
+    float2 total = splat(0.f);
     bool ok = true;
     for (int t = 0; t < tiles; ++t) {
       const uint32_t ph = t & 1;
@@ -244,7 +248,10 @@ __global__ void __launch_bounds__(kSoft + 32, 2)
         for (int j = 0; j < 32; ++j) v[j] = bits >> j & 1 ? v[j] : 0.f;
       }
 #pragma unroll
-      for (int j = 0; j < 16; ++j) w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
+      for (int j = 0; j < 16; ++j) {
+        total = __fadd2_rn(total, make_float2(v[2 * j], v[2 * j + 1]));
+        w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
+      }
       tmem_st16u(tS + mine + 32 * half, w);
       if (j0 + kStep > end || j0 < begin) {
         int b, e;
@@ -257,8 +264,14 @@ __global__ void __launch_bounds__(kSoft + 32, 2)
       fence_before_sync();
       mbar_arrive(weights);
     }
-    if (tiles > 0) ok = ok && mbar_wait_bounded(done, (tiles - 1) & 1);
+    if (tiles > 0) ok = ok && mbar_wait_bounded(done + 8 * ((tiles - 1) & 1), ((tiles - 1) >> 1) & 1);
     fence_after_sync();
+    // a row's ds add up to nothing: what they do add up to is what delta, from
+    // the rounded y, is off by, and dk takes it without
+    float *sums = reinterpret_cast<float *>(s.k[0]);  // all products have been read
+    sums[threadIdx.x] = total.x + total.y;
+    asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
+    if (half == 0 && seen.i >= 0) exact[at] = (delta + sums[own] + sums[kRows + own]) / lift;
     const int64_t i = (int64_t)tile * kRows + own;
     const bool row = i < a.rows;
     const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : a.scale / lift;
@@ -291,7 +304,7 @@ struct KeyShared {
   uint8_t k[kTileBytes<DP, kRows>], v[kTileBytes<DP, kRows>];
   uint8_t q[kStages][kTileBytes<DP, kStep>], dy[kStages][kTileBytes<DP, kStep>];
   float4 lse[2][2][kStep / 4], delta[2][2][kStep / 4];  // of a tile's query rows: [side][turn]
-  uint64_t full_kv, full[kStages], scores[2], weights[2], done[2];
+  uint64_t full_kv, full[kStages], read[kStages], scores[2], weights[2], done[2];
   uint32_t tmem;
   int last, begin, failed;
 };
@@ -327,7 +340,7 @@ __device__ __forceinline__ int64_t slot_of(const AttendArgs &a, int batch, int x
 // memory in fp32, [chunk][tile of first tokens], a key tile's own behind all far
 // ones, at its first far chunk; join_kernel adds them in order.
 template <typename T, int DP>
-__global__ void __launch_bounds__(2 * kSoft + 32, 1)
+__global__ void __launch_bounds__(2 * kSoft + 64, 1)
     dkv_kernel(const __grid_constant__ KeyMaps maps, const AttendArgs a, const Rows<T> dk,
                const Rows<T> dv, const int *most, float *sums, int far_blocks) {
   extern __shared__ __align__(1024) uint8_t raw[];
@@ -359,10 +372,11 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
     first = tile * (kRows / kStep);
   }
   const uint32_t full_kv = smem_u32(&s.full_kv), full = smem_u32(s.full),
-                 scores = smem_u32(s.scores), weights = smem_u32(s.weights), done = smem_u32(s.done);
+                 scores = smem_u32(s.scores), weights = smem_u32(s.weights), done = smem_u32(s.done),
+                 read = smem_u32(s.read);
   if (threadIdx.x == 0) {
     mbar_init(full_kv, 1);
-    for (int i = 0; i < kStages; ++i) mbar_init(full + 8 * i, 1);
+    for (int i = 0; i < kStages; ++i) mbar_init(full + 8 * i, 1), mbar_init(read + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(scores + 8 * i, 1);
       mbar_init(weights + 8 * i, kSoft);
@@ -402,14 +416,26 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
   const int64_t n = (int64_t)max(0, end - first) * group;
   const float c = a.scale * kLog2e;
 
-  if (warp == 2 * kSoft / 32) {
-    const uint32_t k = smem_u32(s.k), v = smem_u32(s.v), q = smem_u32(s.q), dy = smem_u32(s.dy);
-    constexpr uint32_t bytes = kTileBytes<DP, kStep>;
+  const uint32_t k = smem_u32(s.k), v = smem_u32(s.v), q = smem_u32(s.q), dy = smem_u32(s.dy);
+  constexpr uint32_t bytes = kTileBytes<DP, kStep>;
+  if (warp == 2 * kSoft / 32 + 1) {  // copies
     bool ok = true;
     int64_t asked = 0;
     QueryTile next{kv * group, first};
-    const auto ask = [&]() {
+    if (n > 0) {
+      if (elect_one()) {
+        mbar_expect_tx(full_kv, 2 * kTileBytes<DP, kRows>);
+        load_tile<DP, kRows>(k, &maps.k, kv, tile * kRows, batch, full_kv);
+        load_tile<DP, kRows>(v, &maps.v, kv, tile * kRows, batch, full_kv);
+      }
+      __syncwarp();
+    }
+    for (; asked < n; ++asked, next.forward(1, first, end)) {
       const uint32_t stage = (uint32_t)asked % kStages;
+      // the products of the tile before in this place have read it
+      if (asked >= kStages)
+        ok = mbar_wait_bounded(read + 8 * stage, (uint32_t)(asked / kStages - 1) & 1);
+      if (!ok) break;
       if (elect_one()) {
         mbar_expect_tx(full + 8 * stage, 2 * bytes);
         load_tile<DP, kStep>(q + stage * bytes, &maps.q, next.head, next.at * kStep, batch,
@@ -418,27 +444,21 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
                              full + 8 * stage);
       }
       __syncwarp();
-      ++asked;
-      next.forward(1, first, end);
-    };
-    if (n > 0) {
-      if (elect_one()) {
-        mbar_expect_tx(full_kv, 2 * kTileBytes<DP, kRows>);
-        load_tile<DP, kRows>(k, &maps.k, kv, tile * kRows, batch, full_kv);
-        load_tile<DP, kRows>(v, &maps.v, kv, tile * kRows, batch, full_kv);
-      }
-      __syncwarp();
-      ask();
-      if (n > 1) ask();
-      ok = mbar_wait_bounded(full_kv, 0);
     }
+    if (!ok) {  // copies in flight end before the block does
+      s.failed = 1;
+      mbar_wait_bounded(full_kv, 0);
+      for (int64_t u = max((int64_t)0, asked - kStages); u < asked; ++u)
+        mbar_wait_bounded(full + 8 * ((uint32_t)u % kStages), (uint32_t)(u / kStages) & 1);
+    }
+  } else if (warp == 2 * kSoft / 32) {  // products
+    bool ok = n == 0 || mbar_wait_bounded(full_kv, 0);
     for (int64_t t = 0; n > 0 && t <= n && ok; ++t) {
       if (t < n) {
         const uint32_t side = t & 1, stage = (uint32_t)t % kStages;
-        // the side's tensor memory and the tiles of t - 2 have been read
-        if (t >= 2) ok = mbar_wait_bounded(done + 8 * side, ((t - 2) >> 1) & 1);
-        if (ok && t + 2 < n) ask();
-        ok = ok && mbar_wait_bounded(full + 8 * stage, (uint32_t)(t / kStages) & 1);
+        ok = mbar_wait_bounded(full + 8 * stage, (uint32_t)(t / kStages) & 1);
+        // the side's tensor memory has been read
+        if (t >= 2) ok = ok && mbar_wait_bounded(done + 8 * side, ((t - 2) >> 1) & 1);
         if (!ok) break;
         fence_after_sync();
         if (elect_one()) {
@@ -458,16 +478,12 @@ __global__ void __launch_bounds__(2 * kSoft + 32, 1)
           product_values<T, DP, kStep>(tV, tmem + 128 * side, dy + stage * bytes, u > 0);
           product_values<T, DP, kStep>(tK, tmem + 128 * side + kStep, q + stage * bytes, u > 0);
           mma_commit(done + 8 * side);
+          mma_commit(read + 8 * stage);
         }
         __syncwarp();
       }
     }
-    if (!ok) {  // copies in flight end before the block does
-      s.failed = 1;
-      mbar_wait_bounded(full_kv, 0);
-      for (int64_t u = max((int64_t)0, asked - kStages); u < asked; ++u)
-        mbar_wait_bounded(full + 8 * ((uint32_t)u % kStages), (uint32_t)(u / kStages) & 1);
-    }
+    if (!ok) s.failed = 1;
   } else {
     const int side = threadIdx.x / kSoft, own = threadIdx.x % kSoft;
     const int half = own / kRows;  // of the tile's queries
@@ -696,15 +712,14 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
                                           a, total);
   if (const int rc = launched()) return rc;
   const Rows<T> dk = rows_of<T>(s.dk), dv = rows_of<T>(s.dv);
-  dkv_kernel<T, DP><<<(unsigned)(far + k_blocks), 2 * kSoft + 32, k_bytes, st>>>(km, a, dk, dv, most,
+  dq_kernel<T, DP><<<(unsigned)q_blocks, kSoft + 64, q_bytes, st>>>(qm, a, rows_of<T>(s.dq), most,
+                                                                delta);
+  if (const int rc = launched()) return rc;
+  dkv_kernel<T, DP><<<(unsigned)(far + k_blocks), 2 * kSoft + 64, k_bytes, st>>>(km, a, dk, dv, most,
                                                                              sums, (int)far);
   if (const int rc = launched()) return rc;
-  if (far > 0) {
-    join_kernel<T, DP><<<(unsigned)k_blocks, kRows, 0, st>>>(a, dk, dv, sums, (int)far);
-    if (const int rc = launched()) return rc;
-  }
-  dq_kernel<T, DP><<<(unsigned)q_blocks, kSoft + 32, q_bytes, st>>>(
-      qm, a, rows_of<T>(s.dq), most);
+  if (far == 0) return TCU_DFT_OK;
+  join_kernel<T, DP><<<(unsigned)k_blocks, kRows, 0, st>>>(a, dk, dv, sums, (int)far);
   return launched();
 }
 
