@@ -400,9 +400,8 @@ def window_attention(q, k, v, *, window, sinks=0, scale=None, offsets=None, lse=
 
     Returns y, with ``lse`` also the log of each row's sum of exponentials
     (..., heads), which window_attention_grad takes.  Rows behind the last
-    packed sequence are not written.  A value of v that is not finite reaches
-    the rows that see it, and may reach others of the same packed tensor that
-    share a tile of 128 rows with it, where a window or sequence ends in it.
+    packed sequence are not written.  What is not finite reaches only the rows
+    that see it; such a value of v may leave no number in all of their result.
     """
     if _forward._current_level >= 0:
         _no_tangent(q, k, v, out)

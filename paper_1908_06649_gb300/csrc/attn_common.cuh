@@ -63,6 +63,16 @@ __device__ __forceinline__ bool sequence_at(const AttendArgs &a, int64_t i, int 
   return true;
 }
 
+// The rows that are in some sequence: [first, last), sequences following on
+// each other.
+struct Filled {
+  int first, last;
+  __device__ __forceinline__ explicit Filled(const AttendArgs &a)
+      : first(a.offsets ? a.offsets[0] : 0),
+        last(a.offsets ? a.offsets[a.sequences] : INT32_MAX) {}
+  __device__ __forceinline__ bool holds(int i) const { return i >= first && i < last; }
+};
+
 __device__ __forceinline__ Seen seen_by(const AttendArgs &a, int64_t i) {
   Seen v{-1, INT32_MAX, 0, 0};
   int begin, end;
@@ -163,19 +173,48 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, 
 template <int DP, int ROWS>
 constexpr uint32_t kTileBytes = DP * ROWS * 2;
 
-// Zeroes row r of a tile: what lies behind the last sequence, or before the
-// first, may be no number, and zero times that is none either.  Two threads
-// take half of the row each.
-template <int DP, int ROWS>
-__device__ __forceinline__ void clear_row(uint32_t tile, int r, int half) {
+// Looks over a tile of 64 rows from row j0 on, THREADS threads together (this
+// one is `own`): zeros in the place of 16-byte chunks with values that are not
+// finite, whose rows' bits go to `bad` (not null), and of rows in no sequence.
+// A weight of zero times such a value is none, and would carry it to rows that
+// do not see it.
+template <typename T, int DP, int THREADS>
+__device__ __forceinline__ void clean_tile(uint32_t tile, int own, int j0, const Filled &filled,
+                                           unsigned long long *bad) {
+  constexpr uint32_t kExponent = __is_same(T, f16) ? 0x7c007c00u : 0x7f807f80u;
+  constexpr uint32_t kOne = __is_same(T, f16) ? 0x04000400u : 0x00800080u;
+  constexpr int kChunks = 64 * (DP / 8) / THREADS, kBatch = kChunks < 8 ? kChunks : 8;
+  const auto flags = [](const uint4 &w) {  // an exponent of ones carries
+    return (((w.x & kExponent) + kOne) | ((w.y & kExponent) + kOne) | ((w.z & kExponent) + kOne) |
+            ((w.w & kExponent) + kOne)) & 0x80008000u;
+  };
+  const auto at = [&](int k) { return tile + (uint32_t)(own + k * THREADS) * 16; };
+  const auto load = [&](int k) {
+    uint4 w;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                 : "r"(at(k)));
+    return w;
+  };
+  // nearly always there is nothing to do: loads by the batch, one test
+  uint32_t any = 0;
+#pragma unroll 1
+  for (int k0 = 0; k0 < kChunks; k0 += kBatch) {
+    uint4 w[kBatch];
 #pragma unroll
-  for (int c = 0; c < DP / 64; ++c)
+    for (int k = 0; k < kBatch; ++k) w[k] = load(k0 + k);
 #pragma unroll
-    for (int k = 4 * half; k < 4 * half + 4; ++k)
-      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + c * ROWS * 128 + r * 128 +
-                                                                     k * 16),
-                   "r"(0)
-                   : "memory");
+    for (int k = 0; k < kBatch; ++k) any |= flags(w[k]);
+  }
+  if (!any && filled.holds(j0) && filled.holds(j0 + 63)) return;
+#pragma unroll 1
+  for (int k = 0; k < kChunks; ++k) {
+    const int r = (own + k * THREADS) / 8 % 64;
+    const bool odd = flags(load(k)) != 0;
+    if (odd && bad) atomicOr(bad, 1ull << r);
+    if (odd || !filled.holds(j0 + r))
+      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at(k)), "r"(0) : "memory");
+  }
 }
 __device__ __forceinline__ void fence_proxy_async_shared() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -27,7 +27,7 @@ namespace {
 constexpr int kRows = 128;  // of a tile of queries
 constexpr int kStep = 64;   // of a tile of keys
 constexpr int kSoft = 128;  // threads that form weights: a row each
-constexpr int kThreads = kSoft + 64;  // and a warp for products, one for copies
+constexpr int kThreads = kSoft + 96;  // and a warp each for products, copies, a look at values
 
 struct PromptMaps {
   CUtensorMap q, k, v;  // k and v in boxes of kStep rows
@@ -37,9 +37,10 @@ template <int DP>
 struct PromptShared {
   uint8_t q[kTileBytes<DP, kRows>];
   uint8_t k[2][kTileBytes<DP, kStep>], v[2][kTileBytes<DP, kStep>];
-  uint64_t full_k[2], full_v[2], scores[2], weights[2], done[2];
+  uint64_t full_k[2], landed[2], full_v[2], scores[2], weights[2], done[2];
+  unsigned long long bad[2];  // rows of values that are not finite, of a tile
   uint32_t tmem;
-  int low, sink_at, sink_end, failed;
+  int low, high, sink_at, sink_end, failed;
 };
 
 template <typename T, int DP>
@@ -54,17 +55,19 @@ __global__ void __launch_bounds__(kThreads, 2)
   const int kv = head / (a.heads / a.kv_heads);
   const uint32_t full_k = smem_u32(s.full_k), full_v = smem_u32(s.full_v),
                  scores = smem_u32(s.scores), weights = smem_u32(s.weights),
-                 done = smem_u32(s.done);
+                 done = smem_u32(s.done), landed = smem_u32(s.landed);
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(done + 8 * i, 1);
       mbar_init(full_k + 8 * i, 1);
-      mbar_init(full_v + 8 * i, 1);
+      mbar_init(landed + 8 * i, 1);
+      mbar_init(full_v + 8 * i, 32);
       mbar_init(scores + 8 * i, 1);
       mbar_init(weights + 8 * i, kSoft);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.low = INT32_MAX;
+    s.high = 0;
     s.sink_end = 0;
     s.failed = 0;
   }
@@ -77,7 +80,11 @@ __global__ void __launch_bounds__(kThreads, 2)
   // the key tiles: those of the window, and before them those of first tokens
   if (threadIdx.x < kSoft) {
     const int low = __reduce_min_sync(~0u, seen.lo);
-    if (lane == 0) atomicMin(&s.low, low);
+    const int high = __reduce_max_sync(~0u, seen.i >= 0 ? seen.lo : 0);
+    if (lane == 0) {
+      atomicMin(&s.low, low);
+      atomicMax(&s.high, high);
+    }
   }
   __syncthreads();
   const int first = s.low / kStep;  // s.low == INT32_MAX: no row is in a sequence
@@ -96,6 +103,8 @@ __global__ void __launch_bounds__(kThreads, 2)
   const auto key_row = [&](int t) {
     return (t < sink_tiles ? sink_first + t : first + t - sink_tiles) * kStep;
   };
+  // whether not all rows see all keys of a tile
+  const auto edge = [&](int j0) { return j0 < s.high || j0 + kStep - 1 > tile * kRows; };
   const float c = a.scale * kLog2e;
 
   const uint32_t q = smem_u32(s.q), k = smem_u32(s.k), v = smem_u32(s.v);
@@ -118,8 +127,8 @@ __global__ void __launch_bounds__(kThreads, 2)
       if (t > 1) ok = mbar_wait_bounded(done + 8 * stage, ((t - 2) >> 1) & 1);
       if (!ok) break;
       if (elect_one()) {
-        mbar_expect_tx(full_v + 8 * stage, bytes);
-        load_tile<DP, kStep>(v + stage * bytes, &maps.v, kv, key_row(t), batch, full_v + 8 * stage);
+        mbar_expect_tx(landed + 8 * stage, bytes);
+        load_tile<DP, kStep>(v + stage * bytes, &maps.v, kv, key_row(t), batch, landed + 8 * stage);
       }
       __syncwarp();
       values = t + 1;
@@ -128,8 +137,25 @@ __global__ void __launch_bounds__(kThreads, 2)
       s.failed = 1;
       for (int i = 1; i <= 2; ++i) {
         if (keys >= i) mbar_wait_bounded(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
-        if (values >= i) mbar_wait_bounded(full_v + 8 * ((values - i) & 1), ((values - i) >> 1) & 1);
+        if (values >= i) mbar_wait_bounded(landed + 8 * ((values - i) & 1), ((values - i) >> 1) & 1);
       }
+    }
+  } else if (warp == kSoft / 32 + 2) {  // a look at values that not all rows see
+    const Filled filled(a);
+    for (int t = 0; t < tiles; ++t) {
+      const uint32_t stage = t & 1;
+      if (!mbar_wait_bounded(landed + 8 * stage, (t >> 1) & 1)) {
+        s.failed = 1;
+        break;
+      }
+      if (edge(key_row(t))) {
+        // the marks of t - 2 have been read: its values have made room
+        if (lane == 0) s.bad[stage] = 0;
+        __syncwarp();
+        clean_tile<T, DP, 32>(v + stage * bytes, lane, key_row(t), filled, &s.bad[stage]);
+        fence_proxy_async_shared();
+      }
+      mbar_arrive(full_v + 8 * stage);
     }
   } else if (warp == kSoft / 32) {  // products
     bool ok = true;
@@ -163,9 +189,6 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (!ok) s.failed = 1;
   } else {
     const uint32_t mine = (uint32_t)(warp * 32) << 16;
-    // packed rows outside [begin, end) are in no sequence
-    const int begin = a.offsets ? a.offsets[0] : 0;
-    const int end = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     for (int t = 0; t < tiles && ok; ++t) {
@@ -175,12 +198,24 @@ __global__ void __launch_bounds__(kThreads, 2)
       fence_after_sync();
       float v[64];
       tmem_ld32x2(tS, tS + 32, v);
-      if (!__all_sync(~0u, seen.whole(j0, j0 + 64))) {
+      if (edge(j0)) {
+        // rows of values in no sequence, and those that are not finite, are gone;
+        // who sees one of the latter has no number for its result
+        ok = ok && mbar_wait_bounded(full_v + 8 * stage, ph);
+        const unsigned long long bad = s.bad[stage];
         const uint32_t bits0 = seen.bits(j0), bits1 = seen.bits(j0 + 32);
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           v[j] = bits0 >> j & 1 ? v[j] : -INFINITY;
           v[32 + j] = bits1 >> j & 1 ? v[32 + j] : -INFINITY;
+        }
+        if (bad) {
+          const uint32_t bad0 = bits0 & (uint32_t)bad, bad1 = bits1 & (uint32_t)(bad >> 32);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            v[j] = bad0 >> j & 1 ? __int_as_float(0x7fffffff) : v[j];
+            v[32 + j] = bad1 >> j & 1 ? __int_as_float(0x7fffffff) : v[32 + j];
+          }
         }
       }
       float top = v[0], top1 = v[1], top2 = v[2], top3 = v[3];
@@ -225,14 +260,6 @@ __global__ void __launch_bounds__(kThreads, 2)
       tmem_st16u(tS, w);
       tmem_st16u(tS + 32, w + 16);
       l += sum.x + sum.y;
-      if (j0 + kStep > end || j0 < begin) {
-        ok = ok && mbar_wait_bounded(full_v + 8 * stage, ph);
-        int b, e;
-        const int r = threadIdx.x / 2;
-        if (!sequence_at(a, (int64_t)j0 + r, b, e))
-          clear_row<DP, kStep>(smem_u32(s.v[stage]), r, threadIdx.x % 2);
-        fence_proxy_async_shared();
-      }
       tmem_wait_st();
       fence_before_sync();
       mbar_arrive(weights + 8 * stage);

@@ -87,7 +87,7 @@ struct QueryShared {
   uint8_t k[2][kTileBytes<DP, kStep>], v[kTileBytes<DP, kStep>];
   uint64_t full_k[2], full_v, scores, weights, done[2];
   uint32_t tmem;
-  int low, sink_at, sink_end, failed;
+  int low, high, sink_at, sink_end, failed;
 };
 
 // Two blocks share an SM, which holds 228 KB, 1 KB beside each block's own.
@@ -113,10 +113,11 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
     mbar_init(full_k + 8, 1);
     mbar_init(full_v, 1);
     mbar_init(scores, 1);
-    mbar_init(weights, kSoft);
+    mbar_init(weights, kSoft + 32);
     mbar_init(done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.low = INT32_MAX;
+    s.high = 0;
     s.sink_end = 0;
     s.failed = 0;
   }
@@ -129,7 +130,11 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
   fence_after_sync();
   if (threadIdx.x < kSoft) {
     const int low = __reduce_min_sync(~0u, seen.lo);
-    if (lane == 0) atomicMin(&s.low, low);
+    const int high = __reduce_max_sync(~0u, seen.i >= 0 ? seen.lo : 0);
+    if (lane == 0) {
+      atomicMin(&s.low, low);
+      atomicMax(&s.high, high);
+    }
   }
   __syncthreads();
   const int first = s.low / kStep;
@@ -149,11 +154,23 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
   };
   const float c = a.scale * kLog2e;
 
+  // whether not all rows see all keys of a tile
+  const auto edge = [&](int j0) { return j0 < s.high || j0 + kStep - 1 > tile * kRows; };
   const uint32_t q = smem_u32(s.q), dy = smem_u32(s.dy), k = smem_u32(s.k), v = smem_u32(s.v);
   constexpr uint32_t bytes = kTileBytes<DP, kStep>;
-  if (warp == kSoft / 32 + 1) {  // copies
+  if (warp == kSoft / 32 + 1) {  // copies, and a look at keys that not all rows see
+    const Filled filled(a);
     bool ok = true;
     int keys = 0, values = 0;  // tiles asked for
+    // after the scores: keys in no sequence, and those that are not finite, go
+    // (who sees one of the latter has no number for its lse)
+    const auto look = [&](int t) {
+      if (edge(key_row(t))) {
+        clean_tile<T, DP, 32>(k + (t & 1) * bytes, lane, key_row(t), filled, nullptr);
+        fence_proxy_async_shared();
+      }
+      mbar_arrive(weights);
+    };
     for (int t = 0; t < tiles && ok; ++t) {
       const uint32_t stage = t & 1;
       // dq of t - 2 has read its keys, the scores of t - 1 their values
@@ -177,6 +194,11 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
       }
       __syncwarp();
       values = t + 1;
+      if (t > 0) look(t - 1);
+    }
+    if (tiles > 0 && ok) {
+      ok = mbar_wait_bounded(scores, (tiles - 1) & 1);
+      look(tiles - 1);
     }
     if (!ok) {  // copies in flight end before the block does
       s.failed = 1;
@@ -212,8 +234,6 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
   } else {
     const int half = threadIdx.x / kRows;  // of the row: 32 keys, and half of its dq
     const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
-    const int begin = a.offsets ? a.offsets[0] : 0;
-    const int end = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
     const float lift = lift_of(most);
     const int64_t at = ((int64_t)batch * a.rows + max(0, seen.i)) * a.heads + head;
     float lse = 0.f, delta = 0.f;
@@ -253,13 +273,6 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
         w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
       }
       tmem_st16u(tS + mine + 32 * half, w);
-      if (j0 + kStep > end || j0 < begin) {
-        int b, e;
-        const int r = threadIdx.x / 2;
-        if (r < kStep && !sequence_at(a, (int64_t)j0 + r, b, e))
-          clear_row<DP, kStep>(smem_u32(s.k[t & 1]), r, threadIdx.x % 2);
-        fence_proxy_async_shared();
-      }
       tmem_wait_st();
       fence_before_sync();
       mbar_arrive(weights);
@@ -306,7 +319,7 @@ struct KeyShared {
   float4 lse[2][2][kStep / 4], delta[2][2][kStep / 4];  // of a tile's query rows: [side][turn]
   uint64_t full_kv, full[kStages], read[kStages], scores[2], weights[2], done[2];
   uint32_t tmem;
-  int last, begin, failed;
+  int last, begin, least, failed;
 };
 
 // A tile of queries of one head among those that a block walks over.
@@ -340,7 +353,7 @@ __device__ __forceinline__ int64_t slot_of(const AttendArgs &a, int batch, int x
 // memory in fp32, [chunk][tile of first tokens], a key tile's own behind all far
 // ones, at its first far chunk; join_kernel adds them in order.
 template <typename T, int DP>
-__global__ void __launch_bounds__(2 * kSoft + 64, 1)
+__global__ void __launch_bounds__(2 * kSoft + 128, 1)
     dkv_kernel(const __grid_constant__ KeyMaps maps, const AttendArgs a, const Rows<T> dk,
                const Rows<T> dv, const int *most, float *sums, int far_blocks) {
   extern __shared__ __align__(1024) uint8_t raw[];
@@ -379,11 +392,12 @@ __global__ void __launch_bounds__(2 * kSoft + 64, 1)
     for (int i = 0; i < kStages; ++i) mbar_init(full + 8 * i, 1), mbar_init(read + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(scores + 8 * i, 1);
-      mbar_init(weights + 8 * i, kSoft);
+      mbar_init(weights + 8 * i, kSoft + 64);
       mbar_init(done + 8 * i, 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.last = 0;
+    s.least = INT32_MAX;
     s.failed = 0;
   }
   if (warp == 2 * kSoft / 32) tmem_alloc(smem_u32(&s.tmem), 512);
@@ -399,7 +413,11 @@ __global__ void __launch_bounds__(2 * kSoft + 64, 1)
     if (sequence_at(a, j64, begin, e))
       past = j - begin < a.sinks || e - j <= a.window ? e : j + a.window;
   }
-  if (!is_far) {
+  const int least = __reduce_min_sync(~0u, past > 0 ? past : INT32_MAX);
+  if (threadIdx.x % 32 == 0) atomicMin(&s.least, least);
+  if (is_far) {
+    __syncthreads();
+  } else {
     const int top = __reduce_max_sync(~0u, past);
     if (threadIdx.x % 32 == 0) atomicMax(&s.last, top);
     __syncthreads();
@@ -418,7 +436,28 @@ __global__ void __launch_bounds__(2 * kSoft + 64, 1)
 
   const uint32_t k = smem_u32(s.k), v = smem_u32(s.v), q = smem_u32(s.q), dy = smem_u32(s.dy);
   constexpr uint32_t bytes = kTileBytes<DP, kStep>;
-  if (warp == 2 * kSoft / 32 + 1) {  // copies
+  // whether not all keys of the block are seen from all rows of a tile
+  const auto edge = [&](int i0) { return i0 < (tile + 1) * kRows - 1 || i0 + kStep > s.least; };
+  if (warp >= 2 * kSoft / 32 + 2) {
+    // a look at queries (one warp) and dy (another), after the scores: rows in no
+    // sequence, and those that are not finite, go; a key that one of the latter
+    // sees has no number for its gradients, dk through p or dp, dv through dp
+    const Filled filled(a);
+    const uint32_t from = warp == 2 * kSoft / 32 + 2 ? q : dy;
+    QueryTile next{kv * group, first};
+    for (int64_t t = 0; t < n; ++t, next.forward(1, first, end)) {
+      if (!mbar_wait_bounded(scores + 8 * (t & 1), (uint32_t)(t >> 1) & 1)) {
+        s.failed = 1;
+        break;
+      }
+      if (edge(next.at * kStep)) {
+        clean_tile<T, DP, 32>(from + (uint32_t)t % kStages * bytes, threadIdx.x % 32, next.at * kStep,
+                              filled, nullptr);
+        fence_proxy_async_shared();
+      }
+      mbar_arrive(weights + 8 * (t & 1));
+    }
+  } else if (warp == 2 * kSoft / 32 + 1) {  // copies
     bool ok = true;
     int64_t asked = 0;
     QueryTile next{kv * group, first};
@@ -489,8 +528,6 @@ __global__ void __launch_bounds__(2 * kSoft + 64, 1)
     const int half = own / kRows;  // of the tile's queries
     const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
     const uint32_t tS = tmem + 128 * side + 32 * half + mine, tP = tS + kStep;
-    const int inside = a.offsets ? a.offsets[0] : 0;  // packed rows outside are in no sequence
-    const int outside = a.offsets ? a.offsets[a.sequences] : INT32_MAX;
     const float lift = lift_of(most);
     // what the next tile's query rows bring, a row a thread: asked for a tile
     // ahead, and not touched before it is needed
@@ -539,11 +576,11 @@ __global__ void __launch_bounds__(2 * kSoft + 64, 1)
           v[33 + i + k] = ds.y;
         }
       }
-      if (!__all_sync(~0u, j <= i1 && i1 + 32 <= past)) {
+      if (edge(i0)) {
         const uint32_t bits = bits_between(j - i1, past - i1);
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-          v[i] = bits >> i & 1 ? v[i] : 0.f;
+          v[i] = bits >> i & 1 ? fmaf(v[32 + i], 0.f, v[i]) : 0.f;
           v[32 + i] = bits >> i & 1 ? v[32 + i] : 0.f;
         }
       }
@@ -552,13 +589,6 @@ __global__ void __launch_bounds__(2 * kSoft + 64, 1)
       for (int i = 0; i < 32; ++i) w[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
       tmem_st16u(tS, w);
       tmem_st16u(tP, w + 16);
-      if (i0 + kStep > outside || i0 < inside) {
-        int b, e;
-        const int r = own / 4, of = own % 4;
-        if (!sequence_at(a, (int64_t)i0 + r, b, e))
-          clear_row<DP, kStep>(smem_u32(of < 2 ? s.q[t % kStages] : s.dy[t % kStages]), r, of % 2);
-        fence_proxy_async_shared();
-      }
       tmem_wait_st();
       fence_before_sync();
       mbar_arrive(weights + 8 * side);
@@ -715,7 +745,7 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
   dq_kernel<T, DP><<<(unsigned)q_blocks, kSoft + 64, q_bytes, st>>>(qm, a, rows_of<T>(s.dq), most,
                                                                 delta);
   if (const int rc = launched()) return rc;
-  dkv_kernel<T, DP><<<(unsigned)(far + k_blocks), 2 * kSoft + 64, k_bytes, st>>>(km, a, dk, dv, most,
+  dkv_kernel<T, DP><<<(unsigned)(far + k_blocks), 2 * kSoft + 128, k_bytes, st>>>(km, a, dk, dv, most,
                                                                              sums, (int)far);
   if (const int rc = launched()) return rc;
   if (far == 0) return TCU_DFT_OK;

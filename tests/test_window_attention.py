@@ -198,6 +198,48 @@ def test_batch_entries_do_not_reach_each_other(tcu, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("where", [5, 63, 64, 200, 299])
+def test_what_is_not_finite_reaches_who_sees_it(tcu, dtype, bad, where):
+    """One row of k, v or q that is not finite, amid sequences that end inside
+    tiles: rows that do not see it keep their results and gradients, and rows
+    that see the value have no number."""
+    a, dy = inputs(dtype, (300,), 4, 2, 80)
+    lengths, more = [70, 130, 100], dict(window=40, sinks=2)
+    off = offsets_of(lengths).cuda()
+    c, dy = cuda(a), dy.cuda()
+    y, lse = tcu.window_attention(**c, offsets=off, lse=True, **more)
+    g = tcu.window_attention_grad(dy, **c, y=y, lse=lse, offsets=off, **more)
+    i = torch.arange(300)
+    begin = torch.repeat_interleave(torch.tensor([0, 70, 200]), torch.tensor(lengths))
+    sees = ref.visible((i - begin)[:, None], (i - begin)[None], 40, 2) & (begin[:, None] == begin)
+    sees = sees.cuda()
+    for name in ("v", "k", "q"):
+        d = {n: t.clone() for n, t in c.items()}
+        d[name][where] = bad
+        y2, lse2 = tcu.window_attention(**d, offsets=off, lse=True, **more)
+        touched = sees[:, where] if name != "q" else i.cuda() == where
+        assert torch.equal(y2[~touched], y[~touched]), name
+        if name == "v":
+            assert not y2[touched].isfinite().all(-1).any()
+        g2 = tcu.window_attention_grad(dy, **d, y=y2, lse=lse2, offsets=off, **more)
+        assert torch.equal(g2.q[~touched], g.q[~touched]), name
+        # keys that a touched row sees
+        reached = (sees & touched[:, None]).any(0)
+        assert torch.equal(g2.k[~reached], g.k[~reached]), name
+        assert torch.equal(g2.v[~reached], g.v[~reached]), name
+    e = dy.clone()
+    e[where] = bad
+    g2 = tcu.window_attention_grad(e, **c, y=y, lse=lse, offsets=off, **more)
+    rest = i.cuda() != where
+    assert torch.equal(g2.q[rest], g.q[rest])
+    assert torch.equal(g2.k[~sees[where]], g.k[~sees[where]])
+    assert torch.equal(g2.v[~sees[where]], g.v[~sees[where]])
+    assert not g2.v[sees[where]].isfinite().all(-1).any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALF)
 def test_rows_out_of_sight_may_be_anything(tcu, dtype):
     """Keys and values that no row of a tile sees are not read; keys that a
     row does not see do not reach it, whatever they are."""
