@@ -1,8 +1,8 @@
 """In-tree build of libtcu_dft.so for sm_103a (nvcc, no cmake).
 
-The library is a dozen translation units compiled in parallel -- the host
+The library is some two dozen translation units compiled in parallel -- the host
 plan/ABI units and the kernel units (one per radix, mixed radix, BF16, the
-element-wise grid kernels, the sequence operators) -- linked into one shared
+element-wise grid kernels, the sequence and attention operators) -- linked into one shared
 object; in the bounds-checked variant the DFT's units are compiled with
 -DTCU_DFT_CHECKED.
 """

@@ -453,3 +453,24 @@ def test_refusals_of_cuda_tensors(tcu):
                      lambda: tcu.gated_scan_step(x[:, 0], x[:, 0], dual[:, 0], rate, cache)):
             with pytest.raises(ValueError, match="forward-mode"):
                 call()
+
+
+@gpu
+def test_beyond_32_bits_of_elements(tcu):
+    """2.1e9 values a tensor: the end of a run is what a second call gives that
+    continues from the first's last state."""
+    rows, ch, cut = 525000, 4096, 524000
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.empty(1, rows, ch, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    rate = torch.full((ch,), 0.5, device="cuda")
+    y, last = tcu.gated_scan(x, x, x, rate)
+    _, state = tcu.gated_scan(x[:, :cut], x[:, :cut], x[:, :cut], rate)
+    end = x[:, cut:].clone()
+    z, stop, marks = tcu.gated_scan(end, end, end, rate, state=state, marks=True)
+    close(y[:, cut:], z.double().cpu(), inner=ref.U[torch.bfloat16] + 2e-5)
+    close(last, stop.double().cpu())
+    del y
+    _, _, kept = tcu.gated_scan(x, x, x, rate, marks=True)
+    g = tcu.gated_scan_grad(x, x, x, x, rate, marks=kept)
+    w = tcu.gated_scan_grad(end, end, end, end, rate, marks=marks, state=state)
+    close(g.forget[:, cut:], w.forget.double().cpu(), inner=ref.U[torch.bfloat16] + 2e-5)

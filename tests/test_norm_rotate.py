@@ -343,3 +343,20 @@ def test_refusals_of_tensors(tcu):
                      lambda: tcu.norm_rotate_grad(q, dual, q, q, rates)):
             with pytest.raises(ValueError, match="forward-mode"):
                 call()
+
+
+@gpu
+def test_beyond_32_bits_of_elements(tcu):
+    rows = 270000
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    q = torch.empty(1, rows, 64, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    k = q[:, :, :1].clone()
+    rates = 10000.0 ** (-torch.arange(64, device="cuda") / 64)
+    place = torch.arange(rows, dtype=torch.int32, device="cuda")
+    y, z = tcu.norm_rotate(q, k, rates)
+    end = [t[0, -100:].clone() for t in (q, k)]
+    y2, z2 = tcu.norm_rotate(*end, rates, positions=place[-100:])
+    assert torch.equal(y[0, -100:], y2) and torch.equal(z[0, -100:], z2)
+    g = tcu.norm_rotate_grad(q, k, q, k, rates)
+    w = tcu.norm_rotate_grad(*end, *end, rates, positions=place[-100:])
+    assert torch.equal(g.q[0, -100:], w.q) and torch.equal(g.k[0, -100:], w.k)

@@ -557,3 +557,35 @@ def test_refusals_of_tensors(tcu):
     before = ck._version
     tcu.window_attention_step(**ok)
     assert ck._version > before
+
+
+@gpu
+def test_beyond_32_bits_of_elements(tcu):
+    """2.2e9 values of q: the last rows are what a call on the last rows alone
+    gives; so are their gradients, but for rows whose later readers are cut."""
+    rows, heads, window, keep = 270000, 64, 100, 1000
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    q = torch.empty(1, rows, heads, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    k, v = (torch.empty(1, rows, 1, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+            for _ in range(2))
+    y, lse = tcu.window_attention(q, k, v, window=window, lse=True)
+    e = [t[:, rows - keep:].clone() for t in (q, k, v)]
+    z, s = tcu.window_attention(*e, window=window, lse=True)
+    u = U[torch.bfloat16]
+    close(y[:, window - keep:], z[:, window:].double().cpu(), inner=2 * u + 2e-5)
+    close(lse[:, window - keep:], s[:, window:].double().cpu())
+    g = tcu.window_attention_grad(q, q, k, v, y, lse, window=window)
+    w = tcu.window_attention_grad(e[0], *e, z, s, window=window)
+    close(g.q[:, window - keep:], w.q[:, window:].double().cpu(), inner=4 * u + 2e-5)
+    close(g.v[:, window - keep:], w.v[:, window:].double().cpu(), inner=4 * u + 2e-5)
+    # a cache beyond as many
+    del y, lse, g, q
+    cache = torch.empty(2, 2200, 8000, 1, 128, dtype=torch.bfloat16, device="cuda")
+    cache[:, 2199].normal_(generator=gen)
+    slot = torch.tensor([2199], dtype=torch.int32, device="cuda")
+    place = torch.tensor([9000], dtype=torch.int32, device="cuda")
+    token = [t[:, -1] for t in e]
+    far = tcu.window_attention_step(*token, *cache.unbind(0), place, window=8000, slots=slot)
+    near = cache[:, 2199:].clone()
+    got = tcu.window_attention_step(*token, *near.unbind(0), place, window=8000)
+    assert torch.equal(far, got)
