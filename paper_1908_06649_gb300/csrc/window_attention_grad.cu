@@ -86,9 +86,12 @@ struct QueryShared {
   uint8_t q[kTileBytes<DP, kRows>], dy[kTileBytes<DP, kRows>];
   uint8_t k[2][kTileBytes<DP, kStep>], v[kTileBytes<DP, kStep>];
   uint64_t full_k[2], full_v, scores, weights, done[2];
+  float sums[kRows];
   uint32_t tmem;
   int low, high, sink_at, sink_end, failed;
 };
+
+constexpr int kTwice = 4;
 
 // Two blocks share an SM, which holds 228 KB, 1 KB beside each block's own.
 static_assert(2 * (sizeof(QueryShared<128>) + 1024) <= 228 * 1024, "two blocks an SM");
@@ -152,6 +155,11 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
   const auto key_row = [&](int t) {
     return (t < sink_tiles ? sink_first + t : first + t - sink_tiles) * kStep;
   };
+  // delta from the rounded y is off by what it is rounded by, which counts where
+  // a row sees few keys and y is as large as they are: few tiles are walked over
+  // twice, and delta is the sum of p dp that the first walk finds
+  const int before = tiles <= kTwice ? tiles : 0, steps = before + tiles;
+  const auto row_at = [&](int t) { return key_row(t < before ? t : t - before); };
   const float c = a.scale * kLog2e;
 
   // whether not all rows see all keys of a tile
@@ -165,13 +173,13 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
     // after the scores: keys in no sequence, and those that are not finite, go
     // (who sees one of the latter has no number for its lse)
     const auto look = [&](int t) {
-      if (edge(key_row(t))) {
-        clean_tile<T, DP, 32>(k + (t & 1) * bytes, lane, key_row(t), filled, nullptr);
+      if (t >= before && edge(row_at(t))) {
+        clean_tile<T, DP, 32>(k + (t & 1) * bytes, lane, row_at(t), filled, nullptr);
         fence_proxy_async_shared();
       }
       mbar_arrive(weights);
     };
-    for (int t = 0; t < tiles && ok; ++t) {
+    for (int t = 0; t < steps && ok; ++t) {
       const uint32_t stage = t & 1;
       // dq of t - 2 has read its keys, the scores of t - 1 their values
       if (t > 1) ok = mbar_wait_bounded(done + 8 * stage, ((t - 2) >> 1) & 1);
@@ -182,7 +190,7 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
           load_tile<DP, kRows>(q, &maps.q, head, tile * kRows, batch, full_k);
           load_tile<DP, kRows>(dy, &maps.dy, head, tile * kRows, batch, full_k);
         }
-        load_tile<DP, kStep>(k + stage * bytes, &maps.k, kv, key_row(t), batch, full_k + 8 * stage);
+        load_tile<DP, kStep>(k + stage * bytes, &maps.k, kv, row_at(t), batch, full_k + 8 * stage);
       }
       __syncwarp();
       keys = t + 1;
@@ -190,15 +198,15 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
       if (!ok) break;
       if (elect_one()) {
         mbar_expect_tx(full_v, bytes);
-        load_tile<DP, kStep>(v, &maps.v, kv, key_row(t), batch, full_v);
+        load_tile<DP, kStep>(v, &maps.v, kv, row_at(t), batch, full_v);
       }
       __syncwarp();
       values = t + 1;
       if (t > 0) look(t - 1);
     }
-    if (tiles > 0 && ok) {
-      ok = mbar_wait_bounded(scores, (tiles - 1) & 1);
-      look(tiles - 1);
+    if (steps > 0 && ok) {
+      ok = mbar_wait_bounded(scores, (steps - 1) & 1);
+      look(steps - 1);
     }
     if (!ok) {  // copies in flight end before the block does
       s.failed = 1;
@@ -208,7 +216,7 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
     }
   } else if (warp == kSoft / 32) {  // products
     bool ok = true;
-    for (int t = 0; t < tiles; ++t) {
+    for (int t = 0; t < steps; ++t) {
       const uint32_t ph = t & 1, stage = t & 1;
       ok = mbar_wait_bounded(full_k + 8 * stage, (t >> 1) & 1) && mbar_wait_bounded(full_v, ph);
       // scores take the place of what the last product has read
@@ -225,7 +233,7 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
       if (!ok) break;
       fence_after_sync();
       if (elect_one()) {
-        product_values<T, DP, kStep>(tQ, tS, k + stage * bytes, t > 0);
+        if (t >= before) product_values<T, DP, kStep>(tQ, tS, k + stage * bytes, t > before);
         mma_commit(done + 8 * stage);
       }
       __syncwarp();
@@ -243,9 +251,9 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
     }
     float2 total = splat(0.f);
     bool ok = true;
-    for (int t = 0; t < tiles; ++t) {
+    for (int t = 0; t < steps; ++t) {
       const uint32_t ph = t & 1;
-      const int j0 = key_row(t);
+      const int j0 = row_at(t);
       ok = mbar_wait_bounded(scores, ph);
       if (!ok) break;
       fence_after_sync();
@@ -272,19 +280,26 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
         total = __fadd2_rn(total, make_float2(v[2 * j], v[2 * j + 1]));
         w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
       }
-      tmem_st16u(tS + mine + 32 * half, w);
+      if (t >= before) tmem_st16u(tS + mine + 32 * half, w);
+      if (t == before - 1) {  // both halves take their joint sum
+        if (half == 1) s.sums[own] = total.x + total.y;
+        asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
+        if (half == 0) s.sums[own] += total.x + total.y;
+        asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
+        delta += s.sums[own];
+        total = splat(0.f);
+      }
       tmem_wait_st();
       fence_before_sync();
       mbar_arrive(weights);
     }
-    if (tiles > 0) ok = ok && mbar_wait_bounded(done + 8 * ((tiles - 1) & 1), ((tiles - 1) >> 1) & 1);
+    if (steps > 0) ok = ok && mbar_wait_bounded(done + 8 * ((steps - 1) & 1), ((steps - 1) >> 1) & 1);
     fence_after_sync();
     // a row's ds add up to nothing: what they do add up to is what delta, from
     // the rounded y, is off by, and dk takes it without
-    float *sums = reinterpret_cast<float *>(s.k[0]);  // all products have been read
-    sums[threadIdx.x] = total.x + total.y;
+    if (half == 1) s.sums[own] = total.x + total.y;
     asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
-    if (half == 0 && seen.i >= 0) exact[at] = (delta + sums[own] + sums[kRows + own]) / lift;
+    if (half == 0 && seen.i >= 0) exact[at] = (delta + s.sums[own] + total.x + total.y) / lift;
     const int64_t i = (int64_t)tile * kRows + own;
     const bool row = i < a.rows;
     const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : a.scale / lift;
