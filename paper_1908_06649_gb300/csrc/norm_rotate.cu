@@ -67,15 +67,23 @@ struct Lane {
       at[k][1] = apart ? p + a.turned : 2 * p + VP;
     }
   }
+  // The lane's values in pairs, for packed arithmetic: a pair and its partner
+  // where they are adjacent (or VP is 1), else two values of a word, words in
+  // order.
+  static constexpr bool kTogether = kInter || VP == 1;
+  using Values = float2[kParts][VP];
+  struct Angles {
+    float c[kParts][VP], s[kParts][VP];
+  };
+
   // cos and sin of the lane's angles at a position: the product wraps as turns do
-  __device__ __forceinline__ void angles(const uint64_t *turns, int64_t position, float (*c)[VP],
-                                         float (*s)[VP]) const {
+  __device__ __forceinline__ void angles(const uint64_t *turns, int64_t position, Angles &a) const {
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
 #pragma unroll
       for (int i = 0; i < VP; ++i) {
         const int32_t t = (int32_t)(uint32_t)(((uint64_t)position * turns[first[k] + i]) >> 32);
-        sincospif((float)t * 4.656612873077393e-10f, &s[k][i], &c[k][i]);  // 2^-31
+        sincospif((float)t * 4.656612873077393e-10f, &a.s[k][i], &a.c[k][i]);  // 2^-31
       }
   }
   __device__ __forceinline__ void load(const T *head, bool in, Words<T, VP> &v) const {
@@ -91,44 +99,74 @@ struct Lane {
         }
       }
   }
-  static __device__ __forceinline__ void values(const Words<T, VP> &w, float (*v)[2 * VP]) {
+  static __device__ __forceinline__ void values(const Words<T, VP> &w, Values &v) {
 #pragma unroll
-    for (int k = 0; k < kParts; ++k)
+    for (int k = 0; k < kParts; ++k) {
+      if constexpr (VP == 1) {
+        v[k][0] = make_float2(to_f(w.w[k][0].v[0]), to_f(w.w[k][1].v[0]));
+      } else {
+        constexpr int kWords = Pair<T>::kWords;
 #pragma unroll
-      for (int i = 0; i < 2 * VP; ++i) v[k][i] = to_f(w.w[k][i / VP].v[i % VP]);
+        for (int i = 0; i < VP; ++i)
+          v[k][i] = Pair<T>::get(reinterpret_cast<const uint32_t *>(&w.w[k][i / (VP / 2)]) +
+                                 i % (VP / 2) * kWords);
+      }
+    }
   }
-  __device__ __forceinline__ void store(T *head, bool in, const float (*v)[2 * VP]) const {
+  __device__ __forceinline__ void store(T *head, bool in, const Values &v) const {
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!in || !has[k]) continue;
         Vec<T, VP> w;
+        if constexpr (VP == 1) {
+          w.v[0] = from_f<T>(j ? v[k][0].y : v[k][0].x);
+        } else {
 #pragma unroll
-        for (int i = 0; i < VP; ++i) w.v[i] = from_f<T>(v[k][j * VP + i]);
+          for (int i = 0; i < VP / 2; ++i)
+            Pair<T>::put(reinterpret_cast<uint32_t *>(&w) + i * Pair<T>::kWords, v[k][j * (VP / 2) + i]);
+        }
         *reinterpret_cast<Vec<T, VP> *>(head + at[k][j]) = w;
       }
   }
   // turns by the angles (kBack: against them)
   template <bool kBack>
-  static __device__ __forceinline__ void rotate(float (*v)[2 * VP], const float (*c)[VP],
-                                                const float (*s)[VP]) {
+  static __device__ __forceinline__ void rotate(Values &v, const Angles &a) {
 #pragma unroll
-    for (int k = 0; k < kParts; ++k)
+    for (int k = 0; k < kParts; ++k) {
+      if constexpr (kTogether) {
 #pragma unroll
-      for (int i = 0; i < VP; ++i) {
-        float &x = v[k][kInter ? 2 * i : i], &y = v[k][kInter ? 2 * i + 1 : VP + i];
-        const float sn = kBack ? -s[k][i] : s[k][i], a = x, b = y;
-        x = a * c[k][i] - b * sn;
-        y = a * sn + b * c[k][i];
+        for (int i = 0; i < VP; ++i) {
+          const float c = a.c[k][i], s = kBack ? -a.s[k][i] : a.s[k][i];
+          const float2 x = v[k][i];
+          v[k][i] = __ffma2_rn(x, make_float2(c, c), __fmul2_rn(make_float2(x.y, x.x), make_float2(-s, s)));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < VP / 2; ++i) {
+          const float2 c = make_float2(a.c[k][2 * i], a.c[k][2 * i + 1]);
+          const float2 s = make_float2(a.s[k][2 * i], a.s[k][2 * i + 1]), n = make_float2(-s.x, -s.y);
+          const float2 x = v[k][i], y = v[k][VP / 2 + i];
+          v[k][i] = __ffma2_rn(x, c, __fmul2_rn(y, kBack ? s : n));
+          v[k][VP / 2 + i] = __ffma2_rn(y, c, __fmul2_rn(x, kBack ? n : s));
+        }
       }
+    }
   }
-  __device__ __forceinline__ void weights(const float *w, float (*v)[2 * VP]) const {
+  // Where value j (0, 1) of pair i of part k lies in a head.
+  __device__ __forceinline__ int place(int k, int i, int j) const {
+    if constexpr (VP == 1) return at[k][j];
+    else return at[k][i / (VP / 2)] + 2 * (i % (VP / 2)) + j;
+  }
+  __device__ __forceinline__ void weights(const float *w, Values &v) const {
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
 #pragma unroll
-      for (int i = 0; i < 2 * VP; ++i)
-        v[k][i] = !has[k] ? 0.f : w ? w[at[k][i / VP] + i % VP] : 1.f;
+      for (int i = 0; i < VP; ++i)
+        v[k][i] = !has[k] ? make_float2(0.f, 0.f)
+                  : w     ? make_float2(w[place(k, i, 0)], w[place(k, i, 1)])
+                          : make_float2(1.f, 1.f);
   }
 };
 
@@ -188,7 +226,8 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const RotateArgs<T>
   __shared__ uint64_t turns[kPairs];
   fill_turns(a, turns);
   const int lane = threadIdx.x % 32, per = 32 / a.lanes, sub = lane / a.lanes;
-  Lane<T, VP, kInter> own;
+  using L = Lane<T, VP, kInter>;
+  L own;
   own.init(a, lane % a.lanes);
   const float inv = 1.f / a.dim;
   const int64_t step = (int64_t)gridDim.x * kWarps;
@@ -196,10 +235,10 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const RotateArgs<T>
     int64_t b, position;
     int t;
     if (!place_of(a, id, b, t, position)) continue;
-    float c[kParts][VP], s[kParts][VP];
-    own.angles(turns, position, c, s);
+    typename L::Angles angles;
+    own.angles(turns, position, angles);
     auto heads = [&](const T *from, T *to, int count, const float *weight) {
-      float w[kParts][2 * VP];
+      typename L::Values w;
       own.weights(weight, w);
       for (int h0 = sub; h0 - sub < count; h0 += kMany * per) {
         Words<T, VP> words[kMany];
@@ -209,19 +248,20 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const RotateArgs<T>
 #pragma unroll
         for (int m = 0; m < kMany; ++m) {
           if (h0 - sub + m * per >= count) break;  // the whole warp
-          float v[kParts][2 * VP];
+          typename L::Values v;
           own.values(words[m], v);
-          float squares = 0.f;
+          float2 squares = make_float2(0.f, 0.f);
 #pragma unroll
           for (int k = 0; k < kParts; ++k)
 #pragma unroll
-            for (int i = 0; i < 2 * VP; ++i) squares = fmaf(v[k][i], v[k][i], squares);
-          const float r = rsqrtf(fmaf(sum_lanes(squares, a.lanes), inv, a.eps));
+            for (int i = 0; i < VP; ++i) squares = __ffma2_rn(v[k][i], v[k][i], squares);
+          const float r = rsqrtf(fmaf(sum_lanes(squares.x + squares.y, a.lanes), inv, a.eps));
 #pragma unroll
           for (int k = 0; k < kParts; ++k)
 #pragma unroll
-            for (int i = 0; i < 2 * VP; ++i) v[k][i] *= r * w[k][i];
-          own.template rotate<false>(v, c, s);
+            for (int i = 0; i < VP; ++i)
+              v[k][i] = __fmul2_rn(__fmul2_rn(v[k][i], make_float2(r, r)), w[k][i]);
+          own.template rotate<false>(v, angles);
           own.store(to + (int64_t)(h0 + m * per) * a.dim, h0 + m * per < count, v);
         }
       }
@@ -247,7 +287,8 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_grad_kernel(const RotateAr
   fill_turns(a, sh.turns);
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int per = 32 / a.lanes, sub = lane / a.lanes;
-  Lane<T, VP, kInter> own;
+  using L = Lane<T, VP, kInter>;
+  L own;
   own.init(a, lane % a.lanes);
 #pragma unroll
   for (int i = 0; i < 2 * VP * kParts; ++i)
@@ -258,11 +299,15 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_grad_kernel(const RotateAr
     int64_t b, position;
     int t;
     const bool row = place_of(a, id, b, t, position);
-    float c[kParts][VP], s[kParts][VP];
-    if (row) own.angles(sh.turns, position, c, s);
+    typename L::Angles angles;
+    if (row) own.angles(sh.turns, position, angles);
     auto heads = [&](const T *from, const T *dy, T *to, int count, const float *weight, int which) {
-      float w[kParts][2 * VP], dw[kParts][2 * VP] = {};
+      typename L::Values w, dw;
       own.weights(weight, w);
+#pragma unroll
+      for (int k = 0; k < kParts; ++k)
+#pragma unroll
+        for (int i = 0; i < VP; ++i) dw[k][i] = make_float2(0.f, 0.f);
       for (int h0 = sub; h0 - sub < count; h0 += kMany * per) {
         Words<T, VP> xs[kMany], gs[kMany];
 #pragma unroll
@@ -274,30 +319,33 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_grad_kernel(const RotateAr
 #pragma unroll
         for (int m = 0; m < kMany; ++m) {
           if (h0 - sub + m * per >= count) break;  // the whole warp
-          float x[kParts][2 * VP], g[kParts][2 * VP];
+          typename L::Values x, g;
           own.values(xs[m], x);
           own.values(gs[m], g);
           if (row) {
-            own.template rotate<true>(g, c, s);
-            float squares = 0.f, dot = 0.f;
+            own.template rotate<true>(g, angles);
+            float2 squares = make_float2(0.f, 0.f), dots = make_float2(0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < kParts; ++k)
 #pragma unroll
-              for (int i = 0; i < 2 * VP; ++i) {
-                squares = fmaf(x[k][i], x[k][i], squares);
-                dot = fmaf(g[k][i] * w[k][i], x[k][i], dot);
+              for (int i = 0; i < VP; ++i) {
+                squares = __ffma2_rn(x[k][i], x[k][i], squares);
+                dots = __ffma2_rn(__fmul2_rn(g[k][i], w[k][i]), x[k][i], dots);
               }
+            float square = squares.x + squares.y, dot = dots.x + dots.y;
             for (int i = 1; i < a.lanes; i *= 2) {
-              squares += __shfl_xor_sync(~0u, squares, i);
+              square += __shfl_xor_sync(~0u, square, i);
               dot += __shfl_xor_sync(~0u, dot, i);
             }
-            const float r = rsqrtf(fmaf(squares, inv, a.eps)), back = r * r * r * dot * inv;
+            const float r = rsqrtf(fmaf(square, inv, a.eps)), back = -(r * r * dot * inv);
 #pragma unroll
             for (int k = 0; k < kParts; ++k)
 #pragma unroll
-              for (int i = 0; i < 2 * VP; ++i) {
-                dw[k][i] = fmaf(g[k][i], x[k][i] * r, dw[k][i]);
-                g[k][i] = fmaf(g[k][i] * w[k][i], r, -x[k][i] * back);
+              for (int i = 0; i < VP; ++i) {
+                const float2 n = __fmul2_rn(x[k][i], make_float2(r, r));
+                dw[k][i] = __ffma2_rn(g[k][i], n, dw[k][i]);
+                g[k][i] = __ffma2_rn(__fmul2_rn(g[k][i], w[k][i]), make_float2(r, r),
+                                     __fmul2_rn(n, make_float2(back, back)));
               }
           }
           // zeros for a row of no sequence
@@ -308,7 +356,10 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_grad_kernel(const RotateAr
 #pragma unroll
         for (int k = 0; k < kParts; ++k)
 #pragma unroll
-          for (int i = 0; i < 2 * VP; ++i) sh.shares[which][k * 2 * VP + i][threadIdx.x] += dw[k][i];
+          for (int i = 0; i < VP; ++i) {
+            sh.shares[which][2 * (k * VP + i)][threadIdx.x] += dw[k][i].x;
+            sh.shares[which][2 * (k * VP + i) + 1][threadIdx.x] += dw[k][i].y;
+          }
       }
     };
     heads(a.q.at(b, t), a.dyq.at(b, t), a.dq.at(b, t), a.heads, a.q_weight, 0);
@@ -320,15 +371,15 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_grad_kernel(const RotateAr
   for (int k = 0; k < kParts; ++k)
 #pragma unroll
     for (int i = 0; i < 2 * VP; ++i) {
-      float x = sh.shares[0][k * 2 * VP + i][threadIdx.x], y = sh.shares[1][k * 2 * VP + i][threadIdx.x];
+      const int at = k * 2 * VP + i;
+      float x = sh.shares[0][at][threadIdx.x], y = sh.shares[1][at][threadIdx.x];
       for (int m = a.lanes; m < 32; m *= 2) {
         x += __shfl_xor_sync(~0u, x, m);
         y += __shfl_xor_sync(~0u, y, m);
       }
       if (sub == 0 && own.has[k]) {
-        const int at = own.at[k][i / VP] + i % VP;
-        sh.sums[warp][at] = x;
-        sh.sums[warp][a.dim + at] = y;
+        sh.sums[warp][own.place(k, i / 2, i % 2)] = x;
+        sh.sums[warp][a.dim + own.place(k, i / 2, i % 2)] = y;
       }
     }
   __syncthreads();
