@@ -104,7 +104,8 @@ int64_t tcu_window_attention_grad_workspace(const tcu_window_attention_args *a);
  * gives a row of zeros and changes no cache; no two rows may name one entry. */
 int tcu_window_attention_step(const tcu_window_attention_args *a, void *stream);
 /* The rows of whole prompts k and v that the next token of each sequence
- * sees, into its entry. */
+ * sees, into its entry; entries outside [0, num_slots) are passed over, and no
+ * two sequences may name one. */
 int tcu_window_cache(const tcu_window_attention_args *a, void *stream);
 
 #ifdef __cplusplus

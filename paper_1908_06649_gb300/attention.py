@@ -115,19 +115,20 @@ def _workspace(name, packed, device):
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None, n
 
 
-def _heads(q, k, offsets, types, what, loose=False):
+def _heads(q, k, offsets, types, what, loose=False, name="q"):
     """(sequences, rows, heads, key heads, dim, address of offsets, shapes of
-    q and k); loose: three dimensions are rows even without offsets."""
-    _tensor(q, "q")
+    q and k); loose: three dimensions are rows even without offsets; name: q's."""
+    _tensor(q, name)
     _tensor(k, "k")
     if q.dtype not in types:
-        raise TypeError("q must be %s" % what)
+        raise TypeError("%s must be %s" % (name, what))
     if not q.is_cuda:
-        raise ValueError("q must be a CUDA tensor")
+        raise ValueError("%s must be a CUDA tensor" % name)
     shape = q.shape
     flat = offsets is not None or (loose and len(shape) == 3)
     if len(shape) != (3 if flat else 4):
-        raise ValueError("q must be (batch, length, heads, dim), or (rows, heads, dim) with offsets")
+        raise ValueError("%s must be (batch, length, heads, dim), or (rows, heads, dim) with "
+                         "offsets" % name)
     heads, dim = shape[-2:]
     if k.dim() != len(shape):
         raise ValueError("k must have %d dimensions, as q" % len(shape))
@@ -326,9 +327,9 @@ def _bounds(window, sinks, scale, dim):
 class _AttentionCall:
     """The checked arguments that the calls on rows share."""
 
-    def __init__(self, q, k, v, window, sinks, scale, offsets, tokens=False):
+    def __init__(self, q, k, v, window, sinks, scale, offsets, tokens=False, name="q"):
         seqs, rows, heads, kv, dim, off, qs, ks = _heads(q, k, offsets, _HALF, "bfloat16 or float16",
-                                                         loose=tokens)
+                                                         tokens, name)
         if heads % kv:
             raise ValueError("the %d heads of q must divide into the %d heads of k" % (heads, kv))
         if dim % 8 or not 8 <= dim <= MAX_DIM:
@@ -338,7 +339,7 @@ class _AttentionCall:
         self.index, self.dtype, self.shapes = index, dtype, (qs, ks)
         self.window, self.sinks, self.kv, self.dim = window, sinks, kv, dim
         self.sizes = (_HALF[dtype], seqs, heads, kv, dim, window, sinks, scale, rows, off)
-        self.rows = (*_rows16(q, "q", dtype, index, qs), *_rows16(k, "k", dtype, index, ks),
+        self.rows = (*_rows16(q, name, dtype, index, qs), *_rows16(k, "k", dtype, index, ks),
                      *_rows16(v, "v", dtype, index, ks))
 
 
@@ -502,11 +503,12 @@ def window_cache(k, v, cache_k, cache_v, *, window, sinks=0, offsets=None, slots
     """Fills entries of the caches that window_attention_step takes from whole
     prompts k and v: of each sequence the rows that its next token sees, at
     entry slots[s] (int32) for sequence s, or entry s.  Other rows of the
-    caches stay; slots outside them are passed over."""
+    caches stay; slots outside them are passed over; no two sequences may name
+    the same one."""
     if _forward._current_level >= 0:
         _no_tangent(k, v, cache_k, cache_v)
     _no_grad(k, v, cache_k, cache_v)
-    c = _AttentionCall(k, k, v, window, sinks, 1.0, offsets)
+    c = _AttentionCall(k, k, v, window, sinks, 1.0, offsets, name="k")
     pk, pv, ps, n = _caches(c, cache_k, cache_v, slots, c.sizes[1])
     with _On(c.index, stream) as st:
         _call("tcu_window_cache", _ATTEND.pack(*c.sizes, *c.rows, *_NO_ROWS, 0, *_NO_GRAD_ROWS,
