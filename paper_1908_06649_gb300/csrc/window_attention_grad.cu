@@ -17,8 +17,8 @@
 //
 // Products bound it, 10 dim flops a visible pair and head (14 as done here).
 // Measured, bf16, 4 x 2048 rows, 16 heads (4 of keys) x 128, window 1024 (1.3e11
-// flops): dq 112 us, dk and dv 145 us, delta 16 us: 0.47 PFLOP/s of what is
-// asked for, 0.66 of what is done.  Tiles of 64 rows read the other operand anew
+// flops): dq 116 us, dk and dv 150 us, delta 16 us, joining 8 us: 0.45 PFLOP/s of
+// what is asked for, 0.62 of what is done.  Tiles of 64 rows read the other operand anew
 // from shared memory for each product (55 to 60 cycles where 32 would do), and
 // tensor memory holds no larger ones beside the sums.
 #include <algorithm>
@@ -651,7 +651,9 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
   if (warp == 2 * kSoft / 32) tmem_dealloc(tmem, 512);
 }
 
-// The sums of key tiles that far blocks share, a block a tile, head and entry.
+// The sums of key tiles that far blocks share, eight blocks a tile, head and
+// entry: few tiles have any, and one block each took 45 us.
+constexpr int kJoin = 8;
 template <typename T, int DP>
 __global__ void __launch_bounds__(kRows) join_kernel(const AttendArgs a, const Rows<T> dk,
                                                      const Rows<T> dv, const float *sums,
@@ -677,7 +679,7 @@ __global__ void __launch_bounds__(kRows) join_kernel(const AttendArgs a, const R
   if (end <= from * a.chunk) return;
   const int to = (end + a.chunk - 1) / a.chunk, nth = tile - first / kRows;
   // eight adjacent values of a row a thread at a time
-  for (int i = threadIdx.x; i < 2 * kRows * (DP / 8); i += kRows) {
+  for (int i = blockIdx.y * kRows + threadIdx.x; i < 2 * kRows * (DP / 8); i += kJoin * kRows) {
     const int c = i % (DP / 8) * 8, r = i / (DP / 8) % kRows, side = i / (DP / 8) / kRows;
     if (c >= a.dim || (int64_t)tile * kRows + r >= a.rows) continue;
     float v[8] = {};
@@ -772,7 +774,7 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
                                                                              sums, (int)far);
   if (const int rc = launched()) return rc;
   if (far == 0) return TCU_DFT_OK;
-  join_kernel<T, DP><<<(unsigned)k_blocks, kRows, 0, st>>>(a, dk, dv, sums, (int)far);
+  join_kernel<T, DP><<<dim3((unsigned)k_blocks, kJoin), kRows, 0, st>>>(a, dk, dv, sums, (int)far);
   return launched();
 }
 
