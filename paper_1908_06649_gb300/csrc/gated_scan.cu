@@ -49,7 +49,7 @@ constexpr int kTile = kRun * kWarps;  // rows of a block at a time, in the gradi
 // Forward a thread takes two runs below each other: a tile's exchange costs as
 // much as 64 rows' arithmetic.  The gradient's registers hold one.
 constexpr int kRuns = 2, kMine = kRuns * kRun, kLongTile = kRuns * kTile;
-constexpr int kStrip = 64;            // channels of a block
+constexpr int kStrip = 64;  // channels of a block
 constexpr int kMostCluster = 16;
 
 template <typename T>
@@ -167,10 +167,10 @@ __device__ __forceinline__ void put_pair(float *p, int64_t at, int count, float2
 // (kBack: behind it) are applied to what enters the block's.  In a block of its
 // own that is what left the tile before, put down by the warp that came last
 // (`leaves`); in a cluster what left the cluster's rows before, `carry`, through
-// the maps of the blocks before it.
-// Blocks send their maps to each other as stores that the receiver's mbarrier
-// counts; two sets of maps are enough, since a block sends the next but one
-// only when all have sent the next, and so have read the last.
+// the maps of the blocks before it.  Blocks send their maps to each other as
+// stores that the receiver's mbarrier counts; two sets of maps are enough, since
+// a block sends the next but one only when all have sent the next, and so have
+// read the last.
 struct Joint {
   Map warps[2][kWarps][32];
   Map blocks[2][kMostCluster][32];
@@ -237,7 +237,7 @@ __device__ __forceinline__ void empty_sequences(const GatedArgs<T> &a, float *to
   for (int64_t s = first; s < a.sequences; s += step)
     if (a.offsets[s] >= a.offsets[s + 1])
       put_pair<kWide>(to, s * a.channels + c, count,
-               from ? pair_at<kWide>(from, s * a.channels + c, count) : splat(0.f));
+                      from ? pair_at<kWide>(from, s * a.channels + c, count) : splat(0.f));
 }
 
 // ------------------------------------------------------------ rows on the way
