@@ -29,7 +29,9 @@
  * call gives the same bits every time.  Angles are exact to 2^-32 turns at
  * any position: the turns of a position are a 64-bit product that wraps.
  *
- * Calls and statuses are as in tcu_seq.h.  Outputs must not overlap inputs or
+ * Calls and statuses are as in tcu_seq.h.  Every wait inside a kernel of
+ * attention ends after two seconds; what a block then stores is no number,
+ * while the call, which returned before, has given OK.  Outputs must not overlap inputs or
  * themselves, but y_q and y_k may be q and k, with the same strides.
  */
 #ifndef TCU_ATTN_H

@@ -43,6 +43,8 @@
  * more than 2^31 - 4097 rows, a row stride beyond 32 bits; a single-token
  * scan's batch stride beyond 32 bits, or more than 2^31 - 262141 entries; more
  * than 4,194,240 channels of a convolution; a grid of 2^31 blocks), ERR_CUDA.  On an argument error nothing is launched.
+ * A wait between blocks of the recurrence ends after two seconds; what is then
+ * stored is no number, while the call, which returned before, has given OK.
  * Outputs must not overlap inputs or themselves; y of a single-token call may
  * be its x, u, dt, gate, forget or admit, with the same strides.
  */

@@ -154,6 +154,13 @@ __device__ __forceinline__ void mbar_arrive(uint32_t addr) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 
+// A bounded wait of a whole warp, with one verdict for its lanes: a wait that
+// runs out for some of them and not for others would part the warp before
+// votes, elections and tensor-memory accesses that all lanes take together.
+__device__ __forceinline__ bool warp_waits(uint32_t addr, uint32_t parity) {
+  return __all_sync(~0u, mbar_wait_bounded(addr, parity));
+}
+
 // A box of 64 values x rows of one head: coordinates (value, head, row, batch).
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *map, int c0, int c1, int c2,
                                             int c3, uint32_t mbar) {

@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     for (int t = 0; t < tiles && ok; ++t) {
       const uint32_t stage = t & 1;
       // the scores of t - 2 have read its keys, the product of t - 2 its values
-      if (t > 1) ok = mbar_wait_bounded(scores + 8 * stage, ((t - 2) >> 1) & 1);
+      if (t > 1) ok = warp_waits(scores + 8 * stage, ((t - 2) >> 1) & 1);
       if (!ok) break;
       if (elect_one()) {
         mbar_expect_tx(full_k + 8 * stage, bytes + (t == 0 ? kTileBytes<DP, kRows> : 0));
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
       __syncwarp();
       keys = t + 1;
-      if (t > 1) ok = mbar_wait_bounded(done + 8 * stage, ((t - 2) >> 1) & 1);
+      if (t > 1) ok = warp_waits(done + 8 * stage, ((t - 2) >> 1) & 1);
       if (!ok) break;
       if (elect_one()) {
         mbar_expect_tx(landed + 8 * stage, bytes);
@@ -139,15 +139,15 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (!ok) {  // copies in flight end before the block does
       s.failed = 1;
       for (int i = 1; i <= 2; ++i) {
-        if (keys >= i) mbar_wait_bounded(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
-        if (values >= i) mbar_wait_bounded(landed + 8 * ((values - i) & 1), ((values - i) >> 1) & 1);
+        if (keys >= i) warp_waits(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
+        if (values >= i) warp_waits(landed + 8 * ((values - i) & 1), ((values - i) >> 1) & 1);
       }
     }
   } else if (warp == kSoft / 32 + 2) {  // a look at values that not all rows see
     const Filled filled(a);
     for (int t = 0; t < tiles; ++t) {
       const uint32_t stage = t & 1;
-      if (!mbar_wait_bounded(landed + 8 * stage, (t >> 1) & 1)) {
+      if (!warp_waits(landed + 8 * stage, (t >> 1) & 1)) {
         s.failed = 1;
         break;
       }
@@ -167,9 +167,9 @@ __global__ void __launch_bounds__(kThreads, 2)
     for (int t = -1; t < tiles && ok; ++t) {
       const uint32_t stage = t & 1, other = stage ^ 1;
       if (t + 1 < tiles) {
-        ok = mbar_wait_bounded(full_k + 8 * other, ((t + 1) >> 1) & 1);
+        ok = warp_waits(full_k + 8 * other, ((t + 1) >> 1) & 1);
         // they take the place of weights that the product of t - 1 has read
-        if (t > 0) ok = ok && mbar_wait_bounded(done + 8 * other, ((t - 1) >> 1) & 1);
+        if (t > 0) ok = ok && warp_waits(done + 8 * other, ((t - 1) >> 1) & 1);
         if (!ok) break;
         fence_after_sync();
         if (elect_one()) {
@@ -179,8 +179,8 @@ __global__ void __launch_bounds__(kThreads, 2)
         __syncwarp();
       }
       if (t < 0) continue;
-      ok = mbar_wait_bounded(full_v + 8 * stage, (t >> 1) & 1) &&
-           mbar_wait_bounded(weights + 8 * stage, (t >> 1) & 1);
+      ok = warp_waits(full_v + 8 * stage, (t >> 1) & 1) &&
+           warp_waits(weights + 8 * stage, (t >> 1) & 1);
       if (!ok) break;
       fence_after_sync();
       if (elect_one()) {
@@ -197,14 +197,14 @@ __global__ void __launch_bounds__(kThreads, 2)
     for (int t = 0; t < tiles && ok; ++t) {
       const int stage = t & 1, ph = (t >> 1) & 1, j0 = key_row(t);
       const uint32_t tS = tmem + mine + kStep * stage;
-      ok = mbar_wait_bounded(scores + 8 * stage, ph);
+      ok = warp_waits(scores + 8 * stage, ph);
       fence_after_sync();
       float v[64];
       tmem_ld32x2(tS, tS + 32, v);
       if (edge(j0)) {
         // rows of values in no sequence, and those that are not finite, are gone;
         // who sees one of the latter has no number for its result
-        ok = ok && mbar_wait_bounded(full_v + 8 * stage, ph);
+        ok = ok && warp_waits(full_v + 8 * stage, ph);
         const unsigned long long bad = s.bad[stage];
         const uint32_t bits0 = seen.bits(j0), bits1 = seen.bits(j0 + 32);
 #pragma unroll
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         const float by = m == -INFINITY ? 0.f : exp2_fast(m - now);
         l *= by;
         if (t > 0) {
-          ok = ok && mbar_wait_bounded(done + 8 * (stage ^ 1), ((t - 1) >> 1) & 1);
+          ok = ok && warp_waits(done + 8 * (stage ^ 1), ((t - 1) >> 1) & 1);
           fence_after_sync();
 #pragma unroll 1
           for (int k = 0; k < DP; k += 16) {
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       mbar_arrive(weights + 8 * stage);
     }
     // products end in order
-    if (tiles > 0) ok = ok && mbar_wait_bounded(done + 8 * ((tiles - 1) & 1), ((tiles - 1) >> 1) & 1);
+    if (tiles > 0) ok = ok && warp_waits(done + 8 * ((tiles - 1) & 1), ((tiles - 1) >> 1) & 1);
     fence_after_sync();
     const bool row = seen.i >= 0;
     const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : l > 0.f ? 1.f / l : l;

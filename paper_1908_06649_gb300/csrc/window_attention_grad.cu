@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
     for (int t = 0; t < steps && ok; ++t) {
       const uint32_t stage = t & 1;
       // dq of t - 2 has read its keys, the scores of t - 1 their values
-      if (t > 1) ok = mbar_wait_bounded(done + 8 * stage, ((t - 2) >> 1) & 1);
+      if (t > 1) ok = warp_waits(done + 8 * stage, ((t - 2) >> 1) & 1);
       if (!ok) break;
       if (elect_one()) {
         mbar_expect_tx(full_k + 8 * stage, bytes + (t == 0 ? 2 * kTileBytes<DP, kRows> : 0));
@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
       }
       __syncwarp();
       keys = t + 1;
-      if (t > 0) ok = mbar_wait_bounded(scores, (t - 1) & 1);
+      if (t > 0) ok = warp_waits(scores, (t - 1) & 1);
       if (!ok) break;
       if (elect_one()) {
         mbar_expect_tx(full_v, bytes);
@@ -213,22 +213,22 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
       if (t > 0) look(t - 1);
     }
     if (steps > 0 && ok) {
-      ok = mbar_wait_bounded(scores, (steps - 1) & 1);
+      ok = warp_waits(scores, (steps - 1) & 1);
       look(steps - 1);
     }
     if (!ok) {  // copies in flight end before the block does
       s.failed = 1;
-      if (values > 0) mbar_wait_bounded(full_v, (values - 1) & 1);
+      if (values > 0) warp_waits(full_v, (values - 1) & 1);
       for (int i = 1; i <= 2; ++i)
-        if (keys >= i) mbar_wait_bounded(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
+        if (keys >= i) warp_waits(full_k + 8 * ((keys - i) & 1), ((keys - i) >> 1) & 1);
     }
   } else if (warp == kSoft / 32) {  // products
     bool ok = true;
     for (int t = 0; t < steps; ++t) {
       const uint32_t ph = t & 1, stage = t & 1;
-      ok = mbar_wait_bounded(full_k + 8 * stage, (t >> 1) & 1) && mbar_wait_bounded(full_v, ph);
+      ok = warp_waits(full_k + 8 * stage, (t >> 1) & 1) && warp_waits(full_v, ph);
       // scores take the place of what the last product has read
-      if (t > 0) ok = ok && mbar_wait_bounded(done + 8 * (stage ^ 1), ((t - 1) >> 1) & 1);
+      if (t > 0) ok = ok && warp_waits(done + 8 * (stage ^ 1), ((t - 1) >> 1) & 1);
       if (!ok) break;
       fence_after_sync();
       if (elect_one()) {
@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
         mma_commit(scores);
       }
       __syncwarp();
-      ok = mbar_wait_bounded(weights, ph);
+      ok = warp_waits(weights, ph);
       if (!ok) break;
       fence_after_sync();
       if (elect_one()) {
@@ -262,8 +262,8 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
     for (int t = 0; t < steps; ++t) {
       const uint32_t ph = t & 1;
       const int j0 = row_at(t);
-      ok = mbar_wait_bounded(scores, ph);
-      if (!ok) break;
+      // a warp whose wait ran out goes on without waiting: others share its barriers
+      ok = ok && warp_waits(scores, ph);
       fence_after_sync();
       const int j1 = j0 + 32 * half;
       float v[64];
@@ -301,16 +301,18 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
       fence_before_sync();
       mbar_arrive(weights);
     }
-    if (steps > 0) ok = ok && mbar_wait_bounded(done + 8 * ((steps - 1) & 1), ((steps - 1) >> 1) & 1);
+    if (steps > 0) ok = ok && warp_waits(done + 8 * ((steps - 1) & 1), ((steps - 1) >> 1) & 1);
+    if (!ok) s.failed = 1;
     fence_after_sync();
     // a row's ds add up to nothing: what they do add up to is what delta, from
     // the rounded y, is off by, and dk takes it without
     if (half == 1) s.sums[own] = total.x + total.y;
     asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
-    if (half == 0 && seen.i >= 0) exact[at] = (delta + s.sums[own] + total.x + total.y) / lift;
+    const float bad = s.failed ? __int_as_float(0x7fffffff) : 1.f;  // no number
+    if (half == 0 && seen.i >= 0) exact[at] = bad * (delta + s.sums[own] + total.x + total.y) / lift;
     const int64_t i = (int64_t)tile * kRows + own;
     const bool row = i < a.rows;
-    const float by = !ok || s.failed ? __int_as_float(0x7fffffff) : a.scale / lift;
+    const float by = bad * a.scale / lift;
     T *to = dq.at(batch, row ? (int)i : 0) + (int64_t)head * a.dim;
 #pragma unroll 1
     for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 32) {
@@ -469,7 +471,7 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
     const uint32_t from = warp == 2 * kSoft / 32 + 2 ? q : dy;
     QueryTile next{kv * group, first};
     for (int64_t t = 0; t < n; ++t, next.forward(1, first, end)) {
-      if (!mbar_wait_bounded(scores + 8 * (t & 1), (uint32_t)(t >> 1) & 1)) {
+      if (!warp_waits(scores + 8 * (t & 1), (uint32_t)(t >> 1) & 1)) {
         s.failed = 1;
         break;
       }
@@ -496,7 +498,7 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
       const uint32_t stage = (uint32_t)asked % kStages;
       // the products of the tile before in this place have read it
       if (asked >= kStages)
-        ok = mbar_wait_bounded(read + 8 * stage, (uint32_t)(asked / kStages - 1) & 1);
+        ok = warp_waits(read + 8 * stage, (uint32_t)(asked / kStages - 1) & 1);
       if (!ok) break;
       if (elect_one()) {
         mbar_expect_tx(full + 8 * stage, 2 * bytes);
@@ -509,18 +511,18 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
     }
     if (!ok) {  // copies in flight end before the block does
       s.failed = 1;
-      mbar_wait_bounded(full_kv, 0);
+      warp_waits(full_kv, 0);
       for (int64_t u = max((int64_t)0, asked - kStages); u < asked; ++u)
-        mbar_wait_bounded(full + 8 * ((uint32_t)u % kStages), (uint32_t)(u / kStages) & 1);
+        warp_waits(full + 8 * ((uint32_t)u % kStages), (uint32_t)(u / kStages) & 1);
     }
   } else if (warp == 2 * kSoft / 32) {  // products
-    bool ok = n == 0 || mbar_wait_bounded(full_kv, 0);
+    bool ok = n == 0 || warp_waits(full_kv, 0);
     for (int64_t t = 0; n > 0 && t <= n && ok; ++t) {
       if (t < n) {
         const uint32_t side = t & 1, stage = (uint32_t)t % kStages;
-        ok = mbar_wait_bounded(full + 8 * stage, (uint32_t)(t / kStages) & 1);
+        ok = warp_waits(full + 8 * stage, (uint32_t)(t / kStages) & 1);
         // the side's tensor memory has been read
-        if (t >= 2) ok = ok && mbar_wait_bounded(done + 8 * side, ((t - 2) >> 1) & 1);
+        if (t >= 2) ok = ok && warp_waits(done + 8 * side, ((t - 2) >> 1) & 1);
         if (!ok) break;
         fence_after_sync();
         if (elect_one()) {
@@ -533,7 +535,7 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
       if (t > 0) {
         const int64_t u = t - 1;
         const uint32_t side = u & 1, stage = (uint32_t)u % kStages;
-        ok = mbar_wait_bounded(weights + 8 * side, (uint32_t)(u >> 1) & 1);
+        ok = warp_waits(weights + 8 * side, (uint32_t)(u >> 1) & 1);
         if (!ok) break;
         fence_after_sync();
         if (elect_one()) {
@@ -577,8 +579,8 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
       const int i0 = next.at * kStep, i1 = i0 + 32 * half;
       next.forward(2, first, end);
       fetch(t + 2);
-      ok = mbar_wait_bounded(scores + 8 * side, (uint32_t)(t >> 1) & 1);
-      if (!ok) break;
+      // a warp whose wait ran out goes on without waiting: others share its barriers
+      ok = ok && warp_waits(scores + 8 * side, (uint32_t)(t >> 1) & 1);
       fence_after_sync();
       float v[64];
       tmem_ld32x2(tS, tP, v);
@@ -618,12 +620,14 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
     }
     // all products: the last tile's after the one's before, as a barrier may be
     // waited for only one phase ahead
-    if (n > 1) ok = ok && mbar_wait_bounded(done + 8 * (n & 1), (uint32_t)((n - 2) >> 1) & 1);
-    if (n > 0) ok = ok && mbar_wait_bounded(done + 8 * ((n - 1) & 1), (uint32_t)((n - 1) >> 1) & 1);
+    if (n > 1) ok = ok && warp_waits(done + 8 * (n & 1), (uint32_t)((n - 2) >> 1) & 1);
+    if (n > 0) ok = ok && warp_waits(done + 8 * ((n - 1) & 1), (uint32_t)((n - 1) >> 1) & 1);
+    if (!ok) s.failed = 1;
+    asm volatile("bar.sync 3, %0;" ::"n"(2 * kSoft) : "memory");
     fence_after_sync();
     // side 0 stores dv, side 1 dk, each thread half of a row
     const int r = own % kRows;
-    const float bad = !ok || s.failed ? __int_as_float(0x7fffffff) : 1.f;
+    const float bad = s.failed ? __int_as_float(0x7fffffff) : 1.f;
     const float by = bad * (side ? a.scale / lift : 1.f);
     const bool in = past > 0;
     T *to = (side ? dk : dv).at(batch, j64 < a.rows ? j : 0) + (int64_t)kv * a.dim;
