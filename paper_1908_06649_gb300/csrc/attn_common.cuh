@@ -23,6 +23,8 @@ struct AttendArgs {
   const int32_t *offsets;
   float *lse;
   const float *delta;
+  float *sizes;     // gradient in fp16: of each row and head, the sum of |dy_c y_c|
+  uint32_t *peaks;  // and of each key, the bits of its largest term of ds
   int64_t rows;  // of a batch entry
   int sequences, heads, kv_heads, dim, window, sinks;
   float scale;

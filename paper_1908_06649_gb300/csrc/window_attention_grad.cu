@@ -33,55 +33,83 @@ constexpr int kRows = 128;  // of the block
 constexpr int kStep = 64;   // of a tile that it walks over
 constexpr int kSoft = 256;  // threads that form weights: two for each row
 
+// fp16 holds 2^-14 to 2^16 with all its bits, less than weights of long rows
+// and gradients of different sizes span.  So its p goes to dv's product times
+// 2^15, and ds times a power of two of its own for each row of an accumulator,
+// which brings the row's largest term near 2^6: in dq a row's, from the terms
+// seen so far, with the sums brought to a new one where a term passes 2^15; in
+// dk a key's, from the largest term of its column, which dq_kernel leaves.
+// What one row or key brings says nothing of another.  (bf16 has fp32's range.)
+template <typename T>
+constexpr bool kNarrow = __is_same(T, f16);
+constexpr int kWeightUp = 15, kTermUp = 6, kTermRoom = 8;
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
+// The power for terms whose largest has the biased exponent e, at least kLeast.
+constexpr int kLeast = 32;
+__device__ __forceinline__ float lift_of(int e) { return power_of_two(kTermUp + 127 - e); }
+// dq and dk form ds with deltas that differ by the rounding of y, and so not
+// from terms of the same size where ds is next to nothing: a term's size has
+// this part of p sum_c |dy_c y_c| added.
+constexpr float kSlack = 1.f / 512;
+
 // ------------------------------------------------------------------- delta
-// delta = dy.y of each row and head, 16 lanes a head; for fp16 the largest
-// |dy| of rows in a sequence too (atomics: the order of a maximum has no say).
+// delta = dy.y of each row and head, 16 lanes a head; for fp16 the sum of the
+// products' sizes too, and zeros for the largest terms of keys.
 template <typename T>
 __global__ void __launch_bounds__(256) delta_kernel(const Rows<const T> y, const Rows<const T> dy,
-                                                    float *delta, int *most, const AttendArgs a,
-                                                    int64_t total) {
-  constexpr bool kMost = __is_same(T, f16);
+                                                    float *delta, const AttendArgs a, int64_t total,
+                                                    int64_t keys) {
   const int64_t step = (int64_t)gridDim.x * 16;
   const int lane = threadIdx.x % 16;
-  float top = 0.f;
   for (int64_t pair = (int64_t)blockIdx.x * 16 + threadIdx.x / 32 * 2; pair < total; pair += step) {
     const int64_t id = pair + threadIdx.x / 16 % 2;
-    float sum = 0.f;
+    float sum = 0.f, size = 0.f;
     if (id < total && lane * 8 < a.dim) {
       const int64_t row = id / a.heads, b = row / a.rows, t = row - b * a.rows;
       const int64_t at = (id - row * a.heads) * a.dim + lane * 8;
       const Vec<T, 8> u = *reinterpret_cast<const Vec<T, 8> *>(y.at(b, (int)t) + at);
       const Vec<T, 8> v = *reinterpret_cast<const Vec<T, 8> *>(dy.at(b, (int)t) + at);
-      int begin, end;
-      const bool in = kMost && sequence_at(a, t, begin, end);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sum = fmaf(to_f(u.v[i]), to_f(v.v[i]), sum);
-        const float size = fabsf(to_f(v.v[i]));
-        if (in && size < INFINITY) top = fmaxf(top, size);
+        if constexpr (kNarrow<T>) size = fmaf(fabsf(to_f(u.v[i])), fabsf(to_f(v.v[i])), size);
       }
     }
 #pragma unroll
-    for (int m = 1; m < 16; m *= 2) sum += __shfl_xor_sync(~0u, sum, m);
-    if (lane == 0 && id < total) delta[id] = sum;
-  }
-  if constexpr (kMost) {
-    __shared__ int block;
-    if (threadIdx.x == 0) block = 0;
-    __syncthreads();
-    const int bits = __reduce_max_sync(~0u, __float_as_int(top));
-    if (threadIdx.x % 32 == 0) atomicMax(&block, bits);
-    __syncthreads();
-    if (threadIdx.x == 0 && block > 0) atomicMax(most, block);
+    for (int m = 1; m < 16; m *= 2) {
+      sum += __shfl_xor_sync(~0u, sum, m);
+      if constexpr (kNarrow<T>) size += __shfl_xor_sync(~0u, size, m);
+    }
+    if (lane == 0 && id < total) {
+      delta[id] = sum;
+      if constexpr (kNarrow<T>) {
+        a.sizes[id] = size;
+        if (id < keys) a.peaks[id] = 0;
+      }
+    }
   }
 }
 
-// A power of two that brings the largest |dy| to [1/2, 1): ds, rounded to fp16,
-// then loses nothing to its range at the small gradients of long rows (bf16
-// has fp32's range).
-__device__ __forceinline__ float lift_of(const int *most) {
-  const int e = most ? *most >> 23 : 0;
-  return e > 0 ? __int_as_float((253 - e) << 23) : 1.f;
+// The largest of 32 values, none below zero, of each of 32 columns, over the
+// warp's rows (a lane has one row): lane j leaves column j's, its upper 16
+// bits, in *to.  Halves of the columns change places five times.
+__device__ __forceinline__ void column_peaks(const float *m, int lane, uint32_t *to) {
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    w[i] = __byte_perm(__float_as_uint(m[2 * i]), __float_as_uint(m[2 * i + 1]), 0x7632);
+#pragma unroll
+  for (int n = 8; n >= 1; n /= 2) {
+    const bool upper = lane & 2 * n;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const uint32_t keep = upper ? w[i + n] : w[i], send = upper ? w[i] : w[i + n];
+      w[i] = __vmaxu2(keep, __shfl_xor_sync(~0u, send, 2 * n));
+    }
+  }
+  w[0] = __vmaxu2(w[0], __shfl_xor_sync(~0u, w[0], 1));
+  const uint32_t own = lane & 1 ? w[0] & 0xffff0000u : w[0] << 16;
+  if (own) atomicMax(to + lane, own);  // of all rows: the order of a maximum has no say
 }
 
 // ---------------------------------------------------------------------- dq
@@ -94,7 +122,10 @@ struct QueryShared {
   uint8_t q[kTileBytes<DP, kRows>], dy[kTileBytes<DP, kRows>];
   uint8_t k[2][kTileBytes<DP, kStep>], v[kTileBytes<DP, kStep>];
   uint64_t full_k[2], full_v, scores, weights, done[2];
-  float sums[kRows];
+  union {
+    float sums[kRows];
+    uint8_t tops[2][2][kRows];  // exponents of largest terms: [turn][half]
+  };
   uint32_t tmem;
   int low, high, sink_at, sink_end, failed;
 };
@@ -107,7 +138,7 @@ static_assert(2 * (sizeof(QueryShared<128>) + 1024) <= 228 * 1024, "two blocks a
 template <typename T, int DP>
 __global__ void __launch_bounds__(kSoft + 64, 2)
     dq_kernel(const __grid_constant__ QueryMaps maps, const AttendArgs a, const Rows<T> dq,
-              const int *most, float *exact) {
+              float *exact) {
   extern __shared__ __align__(1024) uint8_t raw[];
   QueryShared<DP> &s = *reinterpret_cast<QueryShared<DP> *>(raw);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -250,13 +281,15 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
   } else {
     const int half = threadIdx.x / kRows;  // of the row: 32 keys, and half of its dq
     const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
-    const float lift = lift_of(most);
     const int64_t at = ((int64_t)batch * a.rows + max(0, seen.i)) * a.heads + head;
-    float lse = 0.f, delta = 0.f;
+    float lse = 0.f, delta = 0.f, slack = 0.f;
     if (seen.i >= 0) {
       lse = a.lse[at] * kLog2e;
-      delta = a.delta[at] * lift;
+      delta = a.delta[at];
+      if constexpr (kNarrow<T>) slack = a.sizes[at] * kSlack;
     }
+    int top = kLeast;  // exponent that the row's terms are brought near 2^kTermUp from
+    float lift = 1.f;
     float2 total = splat(0.f);
     bool ok = true;
     for (int t = 0; t < steps; ++t) {
@@ -269,24 +302,62 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
       float v[64];
       uint32_t w[16];
       tmem_ld32x2(tS + mine + 32 * half, tP + mine + 32 * half, v);
-      const float2 by = splat(c), minus = splat(-lse), up = splat(lift), less = splat(-delta);
+      const float2 by = splat(c), minus = splat(-lse), less = splat(-delta);
 #pragma unroll
       for (int j = 0; j < 32; j += 2) {
         const float2 z = __ffma2_rn(make_float2(v[j], v[j + 1]), by, minus);
-        const float2 d = __ffma2_rn(make_float2(v[32 + j], v[33 + j]), up, less);
-        const float2 x = __fmul2_rn(make_float2(exp2_fast(z.x), exp2_fast(z.y)), d);
+        const float2 d = __fadd2_rn(make_float2(v[32 + j], v[33 + j]), less);
+        const float2 p = make_float2(exp2_fast(z.x), exp2_fast(z.y)), x = __fmul2_rn(p, d);
         v[j] = x.x;
         v[j + 1] = x.y;
+        if constexpr (kNarrow<T>) {  // the terms' sizes
+          const float2 m = __fmul2_rn(p, __fadd2_rn(make_float2(fabsf(d.x), fabsf(d.y)), splat(slack)));
+          v[32 + j] = m.x;
+          v[33 + j] = m.y;
+        }
       }
       if (!__all_sync(~0u, seen.whole(j1, j1 + 32))) {
         const uint32_t bits = seen.bits(j1);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = bits >> j & 1 ? v[j] : 0.f;
+        for (int j = 0; j < 32; ++j) {
+          v[j] = bits >> j & 1 ? v[j] : 0.f;
+          if constexpr (kNarrow<T>) v[32 + j] = bits >> j & 1 ? v[32 + j] : 0.f;
+        }
       }
+      if constexpr (kNarrow<T>) {
+        if (t >= before) {
+          column_peaks(v + 32, lane, a.peaks + ((int64_t)batch * a.kv_heads + kv) * a.rows + j1);
+          float most = v[32];
+#pragma unroll
+          for (int j = 1; j < 32; ++j) most = fmaxf(most, v[32 + j]);
+          int e = __float_as_int(most) >> 23;
+          s.tops[t & 1][half][own] = (uint8_t)e;
+          asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
+          e = max(e, (int)s.tops[t & 1][half ^ 1][own]);
+          const bool rise = t == before || e > top + kTermRoom;
+          if (t > before && __any_sync(~0u, rise)) {
+            // the product before has ended: the scores were asked for after it
+            const float less = rise ? power_of_two(max(top - e, -126)) : 1.f;
+#pragma unroll 1
+            for (int k = DP / 2 * half; k < DP / 2 * (half + 1); k += 16) {
+              float o[16];
+              tmem_ld16(tQ + mine + k, o);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] *= less;
+              tmem_st16(tQ + mine + k, o);
+            }
+          }
+          if (rise) top = max(e, kLeast);
+          lift = lift_of(top);
+        }
+      }
+      const float2 up = splat(lift);
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        total = __fadd2_rn(total, make_float2(v[2 * j], v[2 * j + 1]));
-        w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
+        float2 x = make_float2(v[2 * j], v[2 * j + 1]);
+        total = __fadd2_rn(total, x);
+        if constexpr (kNarrow<T>) x = __fmul2_rn(x, up);
+        w[j] = pack2<T>(x.x, x.y);
       }
       if (t >= before) tmem_st16u(tS + mine + 32 * half, w);
       if (t == before - 1) {  // both halves take their joint sum
@@ -296,6 +367,7 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
         asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
         delta += s.sums[own];
         total = splat(0.f);
+        if constexpr (kNarrow<T>) asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
       }
       tmem_wait_st();
       fence_before_sync();
@@ -306,10 +378,11 @@ __global__ void __launch_bounds__(kSoft + 64, 2)
     fence_after_sync();
     // a row's ds add up to nothing: what they do add up to is what delta, from
     // the rounded y, is off by, and dk takes it without
+    if constexpr (kNarrow<T>) asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
     if (half == 1) s.sums[own] = total.x + total.y;
     asm volatile("bar.sync 1, %0;" ::"n"(kSoft) : "memory");
     const float bad = s.failed ? __int_as_float(0x7fffffff) : 1.f;  // no number
-    if (half == 0 && seen.i >= 0) exact[at] = bad * (delta + s.sums[own] + total.x + total.y) / lift;
+    if (half == 0 && seen.i >= 0) exact[at] = bad * (delta + s.sums[own] + total.x + total.y);
     const int64_t i = (int64_t)tile * kRows + own;
     const bool row = i < a.rows;
     const float by = bad * a.scale / lift;
@@ -380,7 +453,7 @@ __device__ __forceinline__ int64_t slot_of(const AttendArgs &a, int batch, int x
 template <typename T, int DP>
 __global__ void __launch_bounds__(2 * kSoft + 128, 1)
     dkv_kernel(const __grid_constant__ KeyMaps maps, const AttendArgs a, const Rows<T> dk,
-               const Rows<T> dv, const int *most, float *sums, int far_blocks) {
+               const Rows<T> dv, float *sums, int far_blocks) {
   extern __shared__ __align__(1024) uint8_t raw[];
   KeyShared<DP> &s = *reinterpret_cast<KeyShared<DP> *>(raw);
   const int warp = threadIdx.x / 32;
@@ -553,7 +626,12 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
     const int half = own / kRows;  // of the tile's queries
     const uint32_t mine = (uint32_t)((warp % 4) * 32) << 16;
     const uint32_t tS = tmem + 128 * side + 32 * half + mine, tP = tS + kStep;
-    const float lift = lift_of(most);
+    float lift = 1.f;  // of the thread's key
+    if constexpr (kNarrow<T>)
+      if (past > 0) {
+        const uint32_t most = a.peaks[((int64_t)batch * a.kv_heads + kv) * a.rows + j];
+        lift = lift_of(max((int)(most >> 23), kLeast));
+      }
     // what the next tile's query rows bring, a row a thread: asked for a tile
     // ahead, and not touched before it is needed
     float lse = 0.f, delta = 0.f;
@@ -572,8 +650,9 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
     for (int64_t t = side; t < n; t += 2) {
       const int turn = (t >> 1) & 1;
       if (own < kStep) {
-        reinterpret_cast<float *>(s.lse[side][turn])[own] = -lse * kLog2e;
-        reinterpret_cast<float *>(s.delta[side][turn])[own] = -delta * lift;
+        reinterpret_cast<float *>(s.lse[side][turn])[own] =
+            fmaf(-lse, kLog2e, kNarrow<T> ? (float)kWeightUp : 0.f);
+        reinterpret_cast<float *>(s.delta[side][turn])[own] = -delta;
       }
       asm volatile("bar.sync %0, %1;" ::"r"(1 + side), "n"(kSoft) : "memory");
       const int i0 = next.at * kStep, i1 = i0 + 32 * half;
@@ -584,7 +663,7 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
       fence_after_sync();
       float v[64];
       tmem_ld32x2(tS, tP, v);
-      const float2 by = splat(c), up = splat(lift);
+      const float2 by = splat(c), up = splat(lift * power_of_two(-kWeightUp));
 #pragma unroll
       for (int i = 0; i < 32; i += 4) {
         const float4 l = s.lse[side][turn][8 * half + i / 4], d = s.delta[side][turn][8 * half + i / 4];
@@ -592,8 +671,9 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
         for (int k = 0; k < 4; k += 2) {
           const float2 z = __ffma2_rn(make_float2(v[i + k], v[i + k + 1]), by,
                                       k ? make_float2(l.z, l.w) : make_float2(l.x, l.y));
-          const float2 x = __ffma2_rn(make_float2(v[32 + i + k], v[33 + i + k]), up,
-                                      k ? make_float2(d.z, d.w) : make_float2(d.x, d.y));
+          float2 x = __fadd2_rn(make_float2(v[32 + i + k], v[33 + i + k]),
+                                k ? make_float2(d.z, d.w) : make_float2(d.x, d.y));
+          if constexpr (kNarrow<T>) x = __fmul2_rn(x, up);
           const float2 p = make_float2(exp2_fast(z.x), exp2_fast(z.y)), ds = __fmul2_rn(p, x);
           v[i + k] = p.x;
           v[i + k + 1] = p.y;
@@ -628,7 +708,7 @@ __global__ void __launch_bounds__(2 * kSoft + 128, 1)
     // side 0 stores dv, side 1 dk, each thread half of a row
     const int r = own % kRows;
     const float bad = s.failed ? __int_as_float(0x7fffffff) : 1.f;
-    const float by = bad * (side ? a.scale / lift : 1.f);
+    const float by = bad * (side ? a.scale / lift : kNarrow<T> ? power_of_two(-kWeightUp) : 1.f);
     const bool in = past > 0;
     T *to = (side ? dk : dv).at(batch, j64 < a.rows ? j : 0) + (int64_t)kv * a.dim;
 #pragma unroll 1
@@ -717,9 +797,12 @@ void split_rows(const tcu_window_attention_args &s, AttendArgs &a) {
   a.sink_tiles = (a.sinks + kRows - 1) / kRows + (s.offsets ? 1 : 0);
 }
 int padded_dim(int dim) { return dim <= 64 ? 64 : 128; }
-// Floats of workspace: delta, then the largest |dy|, then the far sums, 16-byte aligned.
+// Floats of workspace: delta, for fp16 the sums of sizes and the largest terms of
+// keys, then the far sums, 16-byte aligned.
 int64_t far_offset(const tcu_window_attention_args &s) {
-  return (attn_batches(s) * s.rows * s.heads + 1 + 3) / 4 * 4;
+  const int64_t rows = attn_batches(s) * s.rows;
+  const int64_t n = rows * s.heads + (s.type == TCU_SEQ_F16 ? rows * ((int64_t)s.heads + s.kv_heads) : 0);
+  return (n + 3) / 4 * 4;
 }
 int64_t far_blocks(const tcu_window_attention_args &s, const AttendArgs &a) {
   return attn_batches(s) * a.chunks * a.sink_tiles * s.kv_heads;
@@ -740,9 +823,10 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
   const int64_t batches = attn_batches(s);
   a.q_tiles = a.k_tiles = (s.rows + kRows - 1) / kRows;
   float *delta = static_cast<float *>(s.workspace);
-  a.delta = delta;
-  int *most = __is_same(T, f16) ? reinterpret_cast<int *>(delta + batches * s.rows * s.heads) : nullptr;
   const int64_t total = batches * s.rows * s.heads;
+  a.delta = delta;
+  a.sizes = delta + total;
+  a.peaks = reinterpret_cast<uint32_t *>(a.sizes + total);
   const int64_t q_blocks = a.q_tiles * s.heads * batches, k_blocks = a.k_tiles * s.kv_heads * batches;
   if (q_blocks > INT32_MAX) return TCU_DFT_ERR_UNSUPPORTED;
   QueryMaps qm;
@@ -763,19 +847,14 @@ int gradient(const tcu_window_attention_args &s, cudaStream_t st) {
   if (!shared_bytes(dq_kernel<T, DP>, q_bytes) || !shared_bytes(dkv_kernel<T, DP>, k_bytes))
     return TCU_DFT_ERR_CUDA;
   const unsigned blocks = (unsigned)std::min<int64_t>((total + 15) / 16, 16 * (int64_t)num_sms());
-  if (most && cudaMemsetAsync(most, 0, sizeof(int), st) != cudaSuccess) {
-    cudaGetLastError();
-    return TCU_DFT_ERR_CUDA;
-  }
-  delta_kernel<T><<<blocks, 256, 0, st>>>(rows_of<const T>(s.y), rows_of<const T>(s.dy), delta, most,
-                                          a, total);
+  delta_kernel<T><<<blocks, 256, 0, st>>>(rows_of<const T>(s.y), rows_of<const T>(s.dy), delta, a,
+                                          total, batches * s.rows * s.kv_heads);
   if (const int rc = launched()) return rc;
   const Rows<T> dk = rows_of<T>(s.dk), dv = rows_of<T>(s.dv);
-  dq_kernel<T, DP><<<(unsigned)q_blocks, kSoft + 64, q_bytes, st>>>(qm, a, rows_of<T>(s.dq), most,
-                                                                delta);
+  dq_kernel<T, DP><<<(unsigned)q_blocks, kSoft + 64, q_bytes, st>>>(qm, a, rows_of<T>(s.dq), delta);
   if (const int rc = launched()) return rc;
-  dkv_kernel<T, DP><<<(unsigned)(far + k_blocks), 2 * kSoft + 128, k_bytes, st>>>(km, a, dk, dv, most,
-                                                                             sums, (int)far);
+  dkv_kernel<T, DP><<<(unsigned)(far + k_blocks), 2 * kSoft + 128, k_bytes, st>>>(km, a, dk, dv, sums,
+                                                                             (int)far);
   if (const int rc = launched()) return rc;
   if (far == 0) return TCU_DFT_OK;
   join_kernel<T, DP><<<dim3((unsigned)k_blocks, kJoin), kRows, 0, st>>>(a, dk, dv, sums, (int)far);
