@@ -99,24 +99,26 @@ __device__ __forceinline__ Decay decay2(float2 L) {
   return d;
 }
 
-// h -> A h + H of two channels.  Where sequences open in rows (kPacked), a map
-// that does not depend on h drops even an h that is not finite.
+// h -> A h + H of two channels; kCut in the place of A: a sequence opens on the
+// way, and h goes no further, not even one that is not finite.  (A product of
+// decays that has become zero is no cut: it is the same sequence.)
 struct alignas(16) Map {
   float2 A, H;
 };
+constexpr float kCut = -1.f;
 template <bool kPacked>
 __device__ __forceinline__ float2 apply(const Map &m, float2 h) {
   const float2 v = __ffma2_rn(m.A, h, m.H);
   if constexpr (!kPacked) return v;
-  return make_float2(m.A.x == 0.f ? m.H.x : v.x, m.A.y == 0.f ? m.H.y : v.y);
+  return make_float2(m.A.x == kCut ? m.H.x : v.x, m.A.y == kCut ? m.H.y : v.y);
 }
 // first then second
 template <bool kPacked>
 __device__ __forceinline__ Map compose(const Map &first, const Map &second) {
   const float2 A = __fmul2_rn(second.A, first.A);
   if constexpr (!kPacked) return {A, apply<false>(second, first.H)};
-  return {make_float2(second.A.x == 0.f ? 0.f : A.x, second.A.y == 0.f ? 0.f : A.y),
-          apply<true>(second, first.H)};
+  const bool cut = first.A.x == kCut || second.A.x == kCut;  // of both channels
+  return {cut ? make_float2(kCut, kCut) : A, apply<true>(second, first.H)};
 }
 
 // Where sequences open and close in the 8 rows from r0 (bit i: row r0 + i),
@@ -394,6 +396,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
       Marks8 seqs[kRuns];
       bool plain[kRuns];
       Map run{splat(1.f), splat(0.f)};
+      uint32_t cut = 0;
 #pragma unroll
       for (int u = 0; u < kRuns; ++u) {
         seqs[u] = Marks8{};
@@ -415,13 +418,13 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
         plain[u] = seqs[u].inside == (1u << kRun) - 1 && seqs[u].close == 0 &&
                    (!kPacked || seqs[u].open == 0);
         if (kPacked && !plain[u]) {
+          cut |= seqs[u].open;
 #pragma unroll
           for (int i = 0; i < kRun; ++i) {
             if (!(seqs[u].inside >> i & 1)) keep[u][i] = splat(1.f), add[u][i] = splat(0.f);
             if (seqs[u].open >> i & 1) {
               const int64_t q = __shfl_sync(~0u, seqs[u].seq, i);
-              run = {splat(0.f),
-                     a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f)};
+              run.H = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
             }
             run = {__fmul2_rn(run.A, keep[u][i]), __ffma2_rn(run.H, keep[u][i], add[u][i])};
           }
@@ -431,6 +434,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
             run = {__fmul2_rn(run.A, keep[u][i]), __ffma2_rn(run.H, keep[u][i], add[u][i])};
         }
       }
+      if (kPacked && cut) run.A = splat(kCut);
       float2 h = join<false, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size, phase);
       turn ^= 1;
       T *to = y;
@@ -576,13 +580,14 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
         for (int i = kRun - 1; i >= 0; --i) {
           if (kPacked && (seqs.close >> i & 1)) {
             const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-            run = {splat(0.f), a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f)};
+            run.H = a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f);
           }
           if (!(seqs.inside >> i & 1)) continue;
           run = {__fmul2_rn(run.A, keep[i]),
                  __fmul2_rn(__fadd2_rn(run.H, pair_of(rows[3], i, lane)), keep[i])};
-          if (kPacked && (seqs.open >> i & 1)) run = {splat(0.f), splat(0.f)};
+          if (kPacked && (seqs.open >> i & 1)) run.H = splat(0.f);
         }
+        if (kPacked && (seqs.open | seqs.close)) run.A = splat(kCut);
       }
       float2 e = join<true, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size, phase);
       turn ^= 1;
