@@ -26,8 +26,9 @@
  * Statistics, sums and products are accumulated in fp32 and rounded once, on
  * storing; attention rounds its weights, and in the gradient the scores'
  * gradients, to the rows' type before the products that take them.  The same
- * call gives the same bits every time.  Angles are exact to 2^-32 turns at
- * any position: the turns of a position are a 64-bit product that wraps.
+ * call gives the same bits every time.  Angles are
+ * 2^-25 turns off at most, at any position: the turns of a position are a 64-bit
+ * product that wraps, 2^-31 off for rates up to 2^32, and round to fp32.
  *
  * Calls and statuses are as in tcu_seq.h.  Every wait inside a kernel of
  * attention ends after two seconds; what a block then stores is no number,

@@ -236,7 +236,7 @@ def norm_rotate(q, k, rates, *, q_weight=None, k_weight=None, positions=None, of
     are given: single tokens, for instance.
 
     Returns (q, k); ``out``, a pair, may be q and k themselves.  Angles are as
-    exact at position 2^31 as at one.  Rows behind the last packed sequence are
+    exact at position 2^31 as at one, for rates up to 2^32.  Rows behind the last packed sequence are
     not written.
     """
     if _forward._current_level >= 0:

@@ -79,7 +79,8 @@ struct Lane {
     float c[kParts][VP], s[kParts][VP];
   };
 
-  // cos and sin of the lane's angles at a position: the product wraps as turns do
+  // cos and sin of the lane's angles at a position: the product wraps as turns
+  // do; of its 32 bits fp32 keeps 24, 2^-26 turns
   __device__ __forceinline__ void angles(const uint64_t *turns, int64_t position, Angles &a) const {
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
@@ -195,17 +196,23 @@ __device__ __forceinline__ bool place_of(const RotateArgs<T> &a, int64_t id, int
 }
 
 // The turns of one position, in 2^-64, of each pair of a head; whole turns
-// change nothing.
+// change nothing.  1 / (2 pi) is taken in two parts, 2^-110 off, and the product
+// with the first in two, so that a position near 2^31 multiplies 2^-63 turns, not
+// the 2^-55 of one product (rates up to 2^32; larger ones lose what they are).
 constexpr int kPairs = TCU_ATTN_MAX_NORM_DIM / 2;
+__device__ __forceinline__ uint64_t fraction(double t) {
+  const double f = fabs(t) - floor(fabs(t));
+  const uint64_t u = (uint64_t)(f * 18446744073709551616.0);
+  return t < 0 ? 0 - u : u;
+}
 template <typename T>
 __device__ __forceinline__ void fill_turns(const RotateArgs<T> &a, uint64_t *turns) {
   for (int p = threadIdx.x; p < kPairs; p += kThreads) {
     uint64_t u = 0;
     if (p < a.turned) {
-      const double t = (double)a.rates[p] * 0.15915494309189535;
-      const double f = fabs(t) - floor(fabs(t));
-      u = (uint64_t)(f * 18446744073709551616.0);
-      if (t < 0) u = 0 - u;
+      constexpr double kTurn = 0.15915494309189535, kRest = -9.839338337591243e-18;
+      const double rate = a.rates[p], t = rate * kTurn;
+      u = fraction(t) + fraction(fma(rate, kRest, fma(rate, kTurn, -t)));
     }
     turns[p] = u;
   }
