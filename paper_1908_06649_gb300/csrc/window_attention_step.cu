@@ -137,7 +137,9 @@ struct Walk {
       for (int i = 0; i < DP / 8; ++i)
         o[i][0] *= by[0], o[i][1] *= by[0], o[i][2] *= by[1], o[i][3] *= by[1];
     }
-    uint32_t p[4];
+    // weights in two parts, what the first rounds off in the second: the products
+    // they add are hidden behind the rows on their way
+    uint32_t p[4], rest[4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float off = now[h] == -INFINITY ? 0.f : now[h];
@@ -146,8 +148,13 @@ struct Walk {
       for (int i = 0; i < 4; ++i) e[i] = exp2_fast(s[i / 2][2 * h + i % 2] - off);
       l[h] = l[h] * (m[h] == now[h] ? 1.f : by[h]) + (e[0] + e[1]) + (e[2] + e[3]);
       m[h] = now[h];
-      p[h] = pack2<T>(e[0], e[1]);
-      p[2 + h] = pack2<T>(e[2], e[3]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t w = pack2<T>(e[2 * i], e[2 * i + 1]);
+        const float2 taken = Pair<T>::get(&w);
+        p[2 * i + h] = w;
+        rest[2 * i + h] = pack2<T>(e[2 * i] - taken.x, e[2 * i + 1] - taken.y);
+      }
     }
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) {
@@ -155,6 +162,8 @@ struct Walk {
       ldmatrix4<true>(v + chunk_at<DP>((mat & 1) * 8 + r, 2 * i + (mat >> 1)), b);
       mma16<T>(o[2 * i], p, b[0], b[1]);
       mma16<T>(o[2 * i + 1], p, b[2], b[3]);
+      mma16<T>(o[2 * i], rest, b[0], b[1]);
+      mma16<T>(o[2 * i + 1], rest, b[2], b[3]);
     }
   }
 };
