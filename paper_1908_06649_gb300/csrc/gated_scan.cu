@@ -17,7 +17,7 @@
 // rows of a run compose to one map h -> A h + H, maps of warps through shared
 // memory, maps of blocks through a cluster of up to 16 that send them to each
 // other, and then the rows, still in registers, are walked once more from the
-// state that enters.  What composes with what is fixed by the sizes: the same
+// state that enters.  From run to run decays near one are held as a - 1.  What composes with what is fixed by the sizes: the same
 // call gives the same bits.  The gradient walks the tiles from the end, forward
 // within a run from the state that the forward pass kept of it, and back.
 //
@@ -63,19 +63,33 @@ struct GatedArgs {
   int rows, sequences, batches, runs;
 };
 
-// exp(L) and sqrt(1 - exp(L)^2) for L <= 0.  1 - a^2 loses what a lacks in its
-// last place where a is near one, so exp(L) - 1 is a Taylor sum of degree 6
-// for L > -kNear (the next term is 5e-8 of it); kAllNear: there is no other L.
+__device__ __forceinline__ float2 splat(float v) { return make_float2(v, v); }
+// For each value: v where h is finite, else w.
+__device__ __forceinline__ float2 if_finite(float2 h, float2 v, float2 w) {
+  return make_float2(fabsf(h.x) < INFINITY ? v.x : w.x, fabsf(h.y) < INFINITY ? v.y : w.y);
+}
+// Whether a value of the warp's is not finite.
+__device__ __forceinline__ bool any_odd(float2 v) {
+  return __any_sync(~0u, !(fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY));
+}
+
+// a = exp(L), a - 1 and m = sqrt(1 - a^2) for L <= 0.  1 - a^2 loses what a lacks in
+// its last place where a is near one, so a - 1 is a Taylor sum of degree 6 for L >
+// -kNear (the next term is 5e-8 of it); kAllNear: there is no other L.
+//
+// So does a state lose, at every row, where a gate hardly changes: an a within
+// 1e-5 of one, rounded to fp32, is off by 3e-3 of 1 - a, and the state remembers 1
+// / (1 - a) rows.  Within a run a is used as it is rounded (16 rows: 5e-7 of the
+// state); from run to run, and where a state is handed out or taken, a - 1 is.
 constexpr float kNear = 0.25f;
 struct Decay {
-  float2 a, m;
+  float2 a, less, m;
 };
 __device__ __forceinline__ float rsqrt_fast(float v) {
   float y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v));
   return y;
 }
-__device__ __forceinline__ float2 splat(float v) { return make_float2(v, v); }
 template <bool kAllNear>
 __device__ __forceinline__ Decay decay2(float2 L) {
   float2 p = __ffma2_rn(L, splat(1.f / 720), splat(1.f / 120));
@@ -83,7 +97,7 @@ __device__ __forceinline__ Decay decay2(float2 L) {
   p = __ffma2_rn(p, L, splat(1.f / 6));
   p = __ffma2_rn(p, L, splat(0.5f));
   p = __ffma2_rn(p, L, splat(1.f));
-  p = __fmul2_rn(p, L);  // exp(L) - 1
+  p = __fmul2_rn(p, L);
   Decay d;
   d.a = __fadd2_rn(p, splat(1.f));
   if constexpr (!kAllNear) {
@@ -92,34 +106,88 @@ __device__ __forceinline__ Decay decay2(float2 L) {
     if (!(L.x > -kNear)) p.x = q.x, d.a.x = e.x;
     if (!(L.y > -kNear)) p.y = q.y, d.a.y = e.y;
   }
+  d.less = p;
   // 1 - a^2, kept off zero, where its root's reciprocal is none
   float2 r = __fmul2_rn(p, __ffma2_rn(p, splat(-1.f), splat(-2.f)));
   r = make_float2(fmaxf(r.x, 1e-37f), fmaxf(r.y, 1e-37f));
   d.m = __fmul2_rn(r, make_float2(rsqrt_fast(r.x), rsqrt_fast(r.y)));
   return d;
 }
+// A decay in one word: a - 1, below zero, where it is near one, else itself.  In runs in which a sequence opens or closes, and on the way between
+// blocks.
+__device__ __forceinline__ float held(float a, float less) {
+  return a > 0.5f ? fminf(less, -1e-37f) : a;
+}
+__device__ __forceinline__ float2 held(const Decay &d) {
+  return make_float2(held(d.a.x, d.less.x), held(d.a.y, d.less.y));
+}
+__device__ __forceinline__ float near_one(float v) {  // one or zero
+  return v < 0.f ? 1.f : 0.f;
+}
+__device__ __forceinline__ float2 near_one(float2 v) { return make_float2(near_one(v.x), near_one(v.y)); }
+__device__ __forceinline__ float2 decay_of(float2 v) { return __fadd2_rn(near_one(v), v); }
+// a h + v, which carries an infinite h on only where kOdd
+template <bool kOdd>
+__device__ __forceinline__ float2 decayed(float2 a, float2 h, float2 v) {
+  const float2 w = __ffma2_rn(near_one(a), h, __ffma2_rn(a, h, v));
+  return kOdd ? if_finite(h, w, __ffma2_rn(decay_of(a), h, v)) : w;
+}
 
-// h -> A h + H of two channels; kCut in the place of A: a sequence opens on the
-// way, and h goes no further, not even one that is not finite.  (A product of
-// decays that has become zero is no cut: it is the same sequence.)
+// h -> (A + rest) h + H of two channels, rest what A lacks in its last place where
+// it is near one.  kCut in the place of A: a sequence opens on the way, and h goes
+// no further, not even one that is not finite.  (A product of decays that has
+// become zero is no cut: it is the same sequence.)
 struct alignas(16) Map {
   float2 A, H;
 };
 constexpr float kCut = -1.f;
 template <bool kPacked>
-__device__ __forceinline__ float2 apply(const Map &m, float2 h) {
-  const float2 v = __ffma2_rn(m.A, h, m.H);
+__device__ __forceinline__ float2 unless_cut(const Map &m, float2 v) {
   if constexpr (!kPacked) return v;
   return make_float2(m.A.x == kCut ? m.H.x : v.x, m.A.y == kCut ? m.H.y : v.y);
 }
-// first then second
-template <bool kPacked>
-__device__ __forceinline__ Map compose(const Map &first, const Map &second) {
-  const float2 A = __fmul2_rn(second.A, first.A);
-  if constexpr (!kPacked) return {A, apply<false>(second, first.H)};
-  const bool cut = first.A.x == kCut || second.A.x == kCut;  // of both channels
-  return {cut ? make_float2(kCut, kCut) : A, apply<true>(second, first.H)};
+template <bool kPacked, bool kOdd>
+__device__ __forceinline__ float2 apply(const Map &m, float2 rest, float2 h) {
+  float2 v = __ffma2_rn(m.A, h, __ffma2_rn(rest, h, m.H));
+  if constexpr (kOdd) v = if_finite(h, v, __ffma2_rn(m.A, h, m.H));
+  return unless_cut<kPacked>(m, v);
 }
+// Rows and maps that follow on each other: the product of decays (kAllNear: one
+// and `less`) and that less one.
+template <bool kAllNear>
+struct Path {
+  float2 A, less, H;
+  bool cut;  // in both channels
+  __device__ __forceinline__ Path() : A(splat(1.f)), less(splat(0.f)), H(splat(0.f)), cut(false) {}
+  __device__ __forceinline__ void decay(const Decay &d) {
+    if constexpr (!kAllNear) A = __fmul2_rn(A, d.a);
+    less = __fadd2_rn(less, __ffma2_rn(less, d.less, d.less));
+  }
+  // (H is the caller's)
+  __device__ __forceinline__ void decay(const Map &m, float2 rest) {
+    const float2 p = __fadd2_rn(__fadd2_rn(m.A, splat(-1.f)), rest);
+    A = __fmul2_rn(A, m.A);
+    less = __fadd2_rn(less, __ffma2_rn(less, p, p));
+    cut = cut || m.A.x == kCut;
+  }
+  template <bool kPacked>
+  __device__ __forceinline__ Map map(float2 &rest) const {
+    const float2 near = __fadd2_rn(less, splat(1.f));
+    rest = __fadd2_rn(less, __ffma2_rn(near, splat(-1.f), splat(1.f)));
+    Map m{near, H};
+    if constexpr (!kAllNear) {
+      if (!(A.x > 0.5f)) m.A.x = A.x, rest.x = 0.f;
+      if (!(A.y > 0.5f)) m.A.y = A.y, rest.y = 0.f;
+    }
+    if (kPacked && cut) m.A = splat(kCut);
+    return m;
+  }
+  // the same with A in one word
+  template <bool kPacked>
+  __device__ __forceinline__ Map message() const {
+    return {kPacked && cut ? splat(kCut) : make_float2(held(A.x, less.x), held(A.y, less.y)), H};
+  }
+};
 
 // Where sequences open and close in the 8 rows from r0 (bit i: row r0 + i),
 // which rows lie in one, and the sequence of row r0 + lane.
@@ -167,15 +235,17 @@ __device__ __forceinline__ void put_pair(float *p, int64_t at, int count, float2
 
 // Gives a warp the value that enters its rows: the maps of the warps before it
 // (kBack: behind it) are applied to what enters the block's.  In a block of its
-// own that is what left the tile before, put down by the warp that came last
-// (`leaves`); in a cluster what left the cluster's rows before, `carry`, through
+// own that is what left the tile before, as its maps give it and not the walk
+// over its rows, put down by the warp that comes last (`leaves`: ahead of the
+// first tile); in a cluster what left the cluster's rows before, `carry`, through
 // the maps of the blocks before it.  Blocks send their maps to each other as
 // stores that the receiver's mbarrier counts; two sets of maps are enough, since
 // a block sends the next but one only when all have sent the next, and so have
 // read the last.
 struct Joint {
   Map warps[2][kWarps][32];
-  Map blocks[2][kMostCluster][32];
+  float2 rests[2][kWarps][32];
+  Map blocks[2][kMostCluster][32];  // A in one word: what counts is how many words are sent
   float2 carry[2][32];
   uint64_t arrived[2];
 };
@@ -200,32 +270,82 @@ __device__ __forceinline__ void start_joint(Joint &s, int size) {
   }
   cg::this_cluster().sync();
 }
-template <bool kBack, bool kPacked>
-__device__ __forceinline__ float2 join(Joint &s, int turn, const Map &own, float2 &carry, int warp,
-                                       int lane, int rank, int size, int &phase) {
-  s.warps[turn][warp][lane] = own;
-  __syncthreads();
-  Map before{splat(1.f), splat(0.f)};
-  for (int w = kBack ? kWarps - 1 : 0; w != warp; w += kBack ? -1 : 1)
-    before = compose<kPacked>(before, s.warps[turn][w][lane]);
-  if (size == 1) return apply<kPacked>(before, s.carry[turn][lane]);
-  if (warp == (kBack ? 0 : kWarps - 1)) {
-    const Map all = compose<kPacked>(before, own);
-    const uint32_t to = smem_u32(&s.blocks[turn][rank][lane]), mbar = smem_u32(&s.arrived[turn]);
-    for (int r = 0; r < size; ++r) send_map(mapa_shared(to, r), all, mapa_shared(mbar, r));
-  }
-  // phase: -1 once a wait has run out, and what follows is no number
-  if (phase >= 0 && !mbar_wait_cluster_bounded(smem_u32(&s.arrived[turn]), phase >> 1 & 1)) phase = -1;
-  if (phase < 0) return splat(__int_as_float(0x7fffffff));
-  ++phase;
-  if (threadIdx.x == 0) expect_maps(s, turn, size);
+// h through the maps of the warps before (behind) this one.
+template <bool kBack, bool kPacked, bool kOdd>
+__device__ __forceinline__ float2 through_warps(const Joint &s, int turn, float2 h, int warp, int lane) {
+  constexpr int first = kBack ? kWarps - 1 : 0, by = kBack ? -1 : 1;
+#pragma unroll 2
+  for (int w = first; w != warp; w += by)
+    h = apply<kPacked, kOdd>(s.warps[turn][w][lane], s.rests[turn][w][lane], h);
+  return h;
+}
+// carry through the maps of all blocks; what enters this one.
+template <bool kBack, bool kPacked, bool kOdd>
+__device__ __forceinline__ float2 through_blocks(const Joint &s, int turn, float2 &carry, int lane,
+                                                 int rank, int size) {
   float2 enters = carry;
   for (int i = 0; i < size; ++i) {
     const int r = kBack ? size - 1 - i : i;
     if (r == rank) enters = carry;
-    carry = apply<kPacked>(s.blocks[turn][r][lane], carry);
+    const Map m = s.blocks[turn][r][lane];
+    carry = unless_cut<kPacked>(m, decayed<kOdd>(m.A, carry, m.H));
   }
-  return apply<kPacked>(before, enters);
+  return enters;
+}
+template <bool kPacked>
+__device__ __forceinline__ float2 apply_any(const Map &m, float2 rest, float2 h) {
+  const float2 v = apply<kPacked, false>(m, rest, h);
+  return any_odd(v) ? apply<kPacked, true>(m, rest, h) : v;
+}
+template <bool kBack, bool kPacked, bool kAllNear>
+__device__ __forceinline__ float2 join(Joint &s, int turn, const Path<kAllNear> &own, float2 &carry,
+                                       int warp, int lane, int rank, int size, int &phase) {
+  float2 rest;
+  const Map mine = own.template map<kPacked>(rest);
+  s.warps[turn][warp][lane] = mine;
+  s.rests[turn][warp][lane] = rest;
+  __syncthreads();
+  constexpr int first = kBack ? kWarps - 1 : 0, by = kBack ? -1 : 1;
+  const bool last = warp == kWarps - 1 - first;
+  if (size == 1) {
+    const float2 from = s.carry[turn][lane];
+    float2 enters = through_warps<kBack, kPacked, false>(s, turn, from, warp, lane);
+    if (any_odd(enters)) enters = through_warps<kBack, kPacked, true>(s, turn, from, warp, lane);
+    if (last) s.carry[turn ^ 1][lane] = apply_any<kPacked>(mine, rest, enters);
+    return enters;
+  }
+  if (last) {
+    Path<false> path;
+#pragma unroll 2
+    for (int w = first; w != warp; w += by) {
+      path.decay(s.warps[turn][w][lane], s.rests[turn][w][lane]);
+      path.H = apply<kPacked, false>(s.warps[turn][w][lane], s.rests[turn][w][lane], path.H);
+    }
+    path.decay(mine, rest);
+    path.H = apply<kPacked, false>(mine, rest, path.H);
+    if (any_odd(path.H))
+      path.H = apply<kPacked, true>(
+          mine, rest, through_warps<kBack, kPacked, true>(s, turn, splat(0.f), warp, lane));
+    const Map all = path.template message<kPacked>();
+    const uint32_t to = smem_u32(&s.blocks[turn][rank][lane]), mbar = smem_u32(&s.arrived[turn]);
+    for (int r = 0; r < size; ++r) send_map(mapa_shared(to, r), all, mapa_shared(mbar, r));
+  }
+  // phase: -1 once a wait has run out, for the whole warp, and what follows is no
+  // number
+  if (phase >= 0 && !__all_sync(~0u, mbar_wait_cluster_bounded(smem_u32(&s.arrived[turn]), phase >> 1 & 1)))
+    phase = -1;
+  if (phase < 0) return splat(__int_as_float(0x7fffffff));
+  ++phase;
+  if (threadIdx.x == 0) expect_maps(s, turn, size);
+  const float2 from = carry;
+  float2 enters = through_blocks<kBack, kPacked, false>(s, turn, carry, lane, rank, size);
+  enters = through_warps<kBack, kPacked, false>(s, turn, enters, warp, lane);
+  if (any_odd(__ffma2_rn(carry, splat(0.f), enters))) {
+    carry = from;
+    enters = through_blocks<kBack, kPacked, true>(s, turn, carry, lane, rank, size);
+    enters = through_warps<kBack, kPacked, true>(s, turn, enters, warp, lane);
+  }
+  return enters;
 }
 template <bool kBack>
 __device__ __forceinline__ void leaves(Joint &s, int turn, float2 h, int warp, int lane, int size) {
@@ -251,6 +371,15 @@ template <typename T, int kTensors, int kStages>
 struct alignas(16) Ring {
   T v[kStages][kTensors][kRun][kStrip];
 };
+// Zeros for channels behind the last, which no copy brings: numbers, so that
+// what is not finite is looked for in all of a warp's values.
+template <typename R>
+__device__ __forceinline__ void clear_ring(R &ring, int64_t c0, int64_t channels, int lane) {
+  if (c0 + kStrip <= channels) return;
+  uint4 *at = reinterpret_cast<uint4 *>(&ring);
+  for (int i = lane; i < (int)(sizeof(R) / 16); i += 32) at[i] = make_uint4(0, 0, 0, 0);
+  __syncwarp();
+}
 template <int kBytes>
 __device__ __forceinline__ void copy_async(void *dst, const void *src, bool has) {
   const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
@@ -361,6 +490,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
   const float2 minus = make_float2(-rate.x, -rate.y);
   const int step = size * kLongTile;
   auto &ring = s.ring[warp];
+  clear_ring(ring, c0, a.channels, lane);
   int turn = 0, phase = 0;
   for (int b = blockIdx.y; b < a.batches; b += gridDim.y) {
     const int start = rank * kLongTile + warp * kMine;  // this warp's rows, a step apart
@@ -393,48 +523,58 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
     for (int t0 = 0; t0 < a.rows; t0 += step) {
       const int r0 = t0 + start;
       float2 keep[kRuns][kRun], add[kRuns][kRun];
-      Marks8 seqs[kRuns];
+      Marks8 seqs[kRuns] = {};
       bool plain[kRuns];
-      Map run{splat(1.f), splat(0.f)};
-      uint32_t cut = 0;
+      Path<kAllNear> run;
+      const auto opens = [&](int u, int i) {  // what enters the sequence that opens in a row
+        const int64_t q = __shfl_sync(~0u, seqs[u].seq, i);
+        return a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
+      };
 #pragma unroll
       for (int u = 0; u < kRuns; ++u) {
-        seqs[u] = Marks8{};
         if (r0 + u * kRun < a.rows) seqs[u] = sequences_of<kPacked>(a, b, r0 + u * kRun, lane);
-        copies_wait<kStages - 1>();
-#pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-          const float2 f = pair_of(ring.v[stage][0], i, lane), g = pair_of(ring.v[stage][1], i, lane),
-                       x = pair_of(ring.v[stage][2], i, lane);
-          const Decay d = decay2<kAllNear>(__fmul2_rn(sigmoid2(f), minus));
-          keep[u][i] = d.a;
-          add[u][i] = __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g)), x);
-        }
-        __syncwarp();
-        ask(stage);
-        stage = stage == kStages - 1 ? 0 : stage + 1;
         // a run of whole rows in which no sequence opens (dense: a row 0 takes
         // the carry) or closes goes without a look at each row
         plain[u] = seqs[u].inside == (1u << kRun) - 1 && seqs[u].close == 0 &&
                    (!kPacked || seqs[u].open == 0);
-        if (kPacked && !plain[u]) {
-          cut |= seqs[u].open;
+        run.cut = run.cut || (kPacked && seqs[u].open);
+        copies_wait<kStages - 1>();
+        const auto gates = [&](int u, int i) {
+          const float2 f = pair_of(ring.v[stage][0], i, lane), g = pair_of(ring.v[stage][1], i, lane),
+                       x = pair_of(ring.v[stage][2], i, lane);
+          const Decay d = decay2<kAllNear>(__fmul2_rn(sigmoid2(f), minus));
+          add[u][i] = __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g)), x);
+          return d;
+        };
+        if (plain[u]) {
 #pragma unroll
           for (int i = 0; i < kRun; ++i) {
-            if (!(seqs[u].inside >> i & 1)) keep[u][i] = splat(1.f), add[u][i] = splat(0.f);
-            if (seqs[u].open >> i & 1) {
-              const int64_t q = __shfl_sync(~0u, seqs[u].seq, i);
-              run.H = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
-            }
-            run = {__fmul2_rn(run.A, keep[u][i]), __ffma2_rn(run.H, keep[u][i], add[u][i])};
+            const Decay d = gates(u, i);
+            keep[u][i] = d.a;
+            run.decay(d);
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < kRun; ++i)
-            run = {__fmul2_rn(run.A, keep[u][i]), __ffma2_rn(run.H, keep[u][i], add[u][i])};
+          for (int i = 0; i < kRun; ++i) {
+            const Decay d = gates(u, i);
+            keep[u][i] = held(d);
+            if (seqs[u].inside >> i & 1) run.decay(d);
+          }
+        }
+        __syncwarp();
+        ask(stage);
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        if (plain[u]) {
+#pragma unroll
+          for (int i = 0; i < kRun; ++i) run.H = __ffma2_rn(run.H, keep[u][i], add[u][i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kRun; ++i) {
+            if (kPacked && (seqs[u].open >> i & 1)) run.H = opens(u, i);
+            if (seqs[u].inside >> i & 1) run.H = decayed<true>(keep[u][i], run.H, add[u][i]);
+          }
         }
       }
-      if (kPacked && cut) run.A = splat(kCut);
       float2 h = join<false, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size, phase);
       turn ^= 1;
       T *to = y;
@@ -451,12 +591,10 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
         } else {
 #pragma unroll
           for (int i = 0; i < kRun; ++i, to += a.y.row) {
-            if (kPacked && (seqs[u].open >> i & 1)) {
-              const int64_t q = __shfl_sync(~0u, seqs[u].seq, i);
-              h = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
-            }
-            h = __ffma2_rn(h, keep[u][i], add[u][i]);
-            if (seqs[u].inside >> i & 1) put_row<T, kWide>(to, h, count);
+            if (kPacked && (seqs[u].open >> i & 1)) h = opens(u, i);
+            if (!(seqs[u].inside >> i & 1)) continue;
+            h = decayed<true>(keep[u][i], h, add[u][i]);
+            put_row<T, kWide>(to, h, count);
             if (seqs[u].close >> i & 1) {
               const int64_t q = __shfl_sync(~0u, seqs[u].seq, i);
               if (a.last) put_pair<kWide>(a.last, q * a.channels + c, count, h);
@@ -464,7 +602,6 @@ __device__ __forceinline__ void gated_rows(const GatedArgs<T> &a, GatedShared<T>
           }
         }
       }
-      leaves<false>(s.joint, turn, h, warp, lane, size);
       y += step * (int64_t)a.y.row;
       mark += (int64_t)(step / kRun) * a.channels;
     }
@@ -508,6 +645,7 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
   const float2 minus = make_float2(-rate.x, -rate.y);
   const int step = size * kTile;
   auto &ring = s.ring[warp];
+  clear_ring(ring, c0, a.channels, lane);
   float2 drate = splat(0.f);
   int turn = 0, phase = 0;
   const int end = (a.rows - 1) / step * step;  // the last tile
@@ -556,47 +694,60 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
       const auto &rows = ring.v[stage];
       // forward: decays and the state before each row
       float2 keep[kRun], root[kRun], before[kRun];
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) {
+      Path<kAllNear> run;
+      run.cut = kPacked && (seqs.open | seqs.close);
+      const auto gates = [&](int i) {
         const Decay d = decay2<kAllNear>(__fmul2_rn(sigmoid2(pair_of(rows[0], i, lane)), minus));
-        keep[i] = d.a;
         root[i] = d.m;
-        if (kPacked && (seqs.open >> i & 1)) {
-          const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-          h = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
-        }
         before[i] = h;
         h = __ffma2_rn(h, d.a, __fmul2_rn(__fmul2_rn(d.m, sigmoid2(pair_of(rows[1], i, lane))),
                                           pair_of(rows[2], i, lane)));
+        return d;
+      };
+      if (plain) {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+          const Decay d = gates(i);
+          keep[i] = d.a;
+          run.decay(d);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+          if (kPacked && (seqs.open >> i & 1)) {
+            const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+            h = a.state ? pair_at<kWide>(a.state, q * a.channels + c, count) : splat(0.f);
+          }
+          const Decay d = gates(i);
+          keep[i] = held(d);
+          if (seqs.inside >> i & 1) run.decay(d);
+        }
       }
-      Map run{splat(1.f), splat(0.f)};
+      const auto closes = [&](int i) {  // what enters the sequence that ends in a row
+        const int64_t q = __shfl_sync(~0u, seqs.seq, i);
+        return a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f);
+      };
       if (plain) {
 #pragma unroll
         for (int i = kRun - 1; i >= 0; --i)
-          run = {__fmul2_rn(run.A, keep[i]),
-                 __fmul2_rn(__fadd2_rn(run.H, pair_of(rows[3], i, lane)), keep[i])};
+          run.H = __fmul2_rn(__fadd2_rn(run.H, pair_of(rows[3], i, lane)), keep[i]);
       } else {
 #pragma unroll
         for (int i = kRun - 1; i >= 0; --i) {
-          if (kPacked && (seqs.close >> i & 1)) {
-            const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-            run.H = a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f);
-          }
+          if (kPacked && (seqs.close >> i & 1)) run.H = closes(i);
           if (!(seqs.inside >> i & 1)) continue;
-          run = {__fmul2_rn(run.A, keep[i]),
-                 __fmul2_rn(__fadd2_rn(run.H, pair_of(rows[3], i, lane)), keep[i])};
+          run.H = decayed<true>(keep[i], __fadd2_rn(run.H, pair_of(rows[3], i, lane)), splat(0.f));
           if (kPacked && (seqs.open >> i & 1)) run.H = splat(0.f);
         }
-        if (kPacked && (seqs.open | seqs.close)) run.A = splat(kCut);
       }
       float2 e = join<true, kPacked>(s.joint, turn, run, carry, warp, lane, rank, size, phase);
       turn ^= 1;
       float2 share = splat(0.f);
-      // the gradients of row i from that of its state, e, which becomes the row above's
-      const auto row = [&](int i, T *dx, T *dg, T *df) {
+      // the gradients of row i, of decay k, from that of its state, e
+      const auto row = [&](int i, float2 k, T *dx, T *dg, T *df) {
         e = __fadd2_rn(e, pair_of(rows[3], i, lane));
         const float2 open = sigmoid2(pair_of(rows[0], i, lane)), way = sigmoid2(pair_of(rows[1], i, lane)),
-                     x = pair_of(rows[2], i, lane), k = keep[i];
+                     x = pair_of(rows[2], i, lane);
         const float2 L = __fmul2_rn(open, minus), ew = __fmul2_rn(e, way);
         const float2 gx = __fmul2_rn(ew, root[i]);
         put_row<T, kWide>(dx, gx, count);
@@ -609,13 +760,14 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
         const float2 dL = __fmul2_rn(k, __ffma2_rn(two, splat(-1.f), one));
         share = __fadd2_rn(share, dL);
         put_row<T, kWide>(df, __ffma2_rn(dL, __fmul2_rn(open, splat(-1.f)), dL), count);
-        e = __fmul2_rn(e, k);
       };
       T *dx = to[0], *dg = to[1], *df = to[2];
       if (plain) {
 #pragma unroll
-        for (int i = kRun - 1; i >= 0; --i, dx -= a.dx.row, dg -= a.dadmit.row, df -= a.dforget.row)
-          row(i, dx, dg, df);
+        for (int i = kRun - 1; i >= 0; --i, dx -= a.dx.row, dg -= a.dadmit.row, df -= a.dforget.row) {
+          row(i, keep[i], dx, dg, df);
+          e = __fmul2_rn(e, keep[i]);  // the row above's
+        }
       } else {
 #pragma unroll
         for (int i = kRun - 1; i >= 0; --i, dx -= a.dx.row, dg -= a.dadmit.row, df -= a.dforget.row) {
@@ -626,11 +778,9 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
             put_row<T, kWide>(df, splat(0.f), count);
             continue;
           }
-          if (kPacked && (seqs.close >> i & 1)) {
-            const int64_t q = __shfl_sync(~0u, seqs.seq, i);
-            e = a.dlast ? pair_at<kWide>(a.dlast, q * a.channels + c, count) : splat(0.f);
-          }
-          row(i, dx, dg, df);
+          if (kPacked && (seqs.close >> i & 1)) e = closes(i);
+          row(i, decay_of(keep[i]), dx, dg, df);
+          e = decayed<true>(keep[i], e, splat(0.f));
           if ((seqs.open >> i & 1) && a.dstate) {
             const int64_t q = __shfl_sync(~0u, seqs.seq, i);
             put_pair<kWide>(a.dstate, q * a.channels + c, count, e);
@@ -638,7 +788,6 @@ __device__ __forceinline__ void grad_rows(const GatedArgs<T> &a, GradShared<T> &
         }
       }
       drate = __fadd2_rn(drate, share);
-      leaves<true>(s.joint, turn, e, warp, lane, size);
       __syncwarp();
       ask(stage);
       stage = stage == kStages - 1 ? 0 : stage + 1;
@@ -687,13 +836,13 @@ __global__ void __launch_bounds__(128) gated_step_kernel(const GatedArgs<T> a) {
     f.template load<kWide>(a.forget.p + b * a.forget.batch + c, count);
     g.template load<kWide>(a.admit.p + b * a.admit.batch + c, count);
     x.template load<kWide>(a.x.p + b * a.x.batch + c, count);
-    const bool held = slot >= 0 && slot < a.num_slots;
+    const bool found = slot >= 0 && slot < a.num_slots;
     float2 h = splat(0.f);
-    if (held) {
+    if (found) {
       const Decay d = decay2<false>(__fmul2_rn(sigmoid2(f.pair(0)), make_float2(-rate.x, -rate.y)));
       const int64_t at = slot * a.channels + c;
-      h = __ffma2_rn(pair_at<kWide>(a.last, at, count), d.a,
-                     __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g.pair(0))), x.pair(0)));
+      const float2 add = __fmul2_rn(__fmul2_rn(d.m, sigmoid2(g.pair(0))), x.pair(0));
+      h = decayed<true>(held(d), pair_at<kWide>(a.last, at, count), add);
       put_pair<kWide>(a.last, at, count, h);
     }
     y.set(0, h);

@@ -1,4 +1,4 @@
-"""The waits of the attention kernels, read in their sources: none is cut short
+"""The waits of the attention kernels and the recurrence, read in their sources: none is cut short
 on a GPU to see what follows.
 
 A wait ends after two seconds.  Where it runs out for some threads and not for
@@ -27,6 +27,12 @@ def test_waits_have_one_verdict_a_warp(name):
     assert "while (true)" not in text
     body = re.search(r"bool warp_waits\([^{]*\{(.*?)\n\}", source("attn_common.cuh"), re.S).group(1)
     assert "__all_sync(~0u, mbar_wait_bounded(" in body
+
+
+def test_waits_of_the_recurrence_have_one_verdict_a_warp():
+    text = source("gated_scan.cu")
+    waits = re.findall(r"[^\n]*\bmbar_(?:try_)?wait\w*\([^\n]*", text)
+    assert len(waits) == 1 and "__all_sync(~0u, mbar_wait_cluster_bounded(" in waits[0]
 
 
 def test_no_thread_leaves_others_at_a_barrier():

@@ -1,4 +1,5 @@
-"""The gated recurrence where states are not finite."""
+"""The gated recurrence at the ends of its range: states that are not finite,
+decays next to one and far from it."""
 import pytest
 import torch
 
@@ -58,3 +59,99 @@ def test_what_is_not_finite_stays_in_its_sequence(tcu, bad, channels):
         assert torch.equal(b.x[:50], g.x[:50]) and torch.equal(b.x[750:], g.x[750:]), where
         assert not b.x[50:748].isfinite().any(), where
         assert torch.equal(b.state[::2], g.state[::2]) and not b.state[1].isfinite().any()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["clusters", "blocks", "packed"])
+def test_gates_that_hardly_change(tcu, kind):
+    """Constant gates and decays within 5e-6 to 5e-4 of one over 30000 rows: a
+    decay that is off in its last place, 2^-25 of one, is so at every row, and
+    a state remembers 1 / (1 - a) of them.  Held as a - 1 it is 2^-22 of that
+    off, as the special function unit's results are, and the state as much: with
+    an input of the same sign and a factor of four for what multiplies it,
+    1e-6; 2e-5 holds it, and the gradients."""
+    rows, ch, batch = 30000, 64, 300 if kind == "blocks" else 1
+    lengths = [rows] if kind != "packed" else [300, rows - 5000, 0, 4000, 700]
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    x, dy = r(batch, rows, ch) + 1, r(batch, rows, ch) + 1
+    forget, admit = (torch.zeros(1, 1, ch, device="cuda") + g for g in (0.0, 1.0))
+    forget, admit = forget.repeat(batch, rows, 1), admit.repeat(batch, rows, 1)
+    rate = torch.logspace(-5, -3, ch, device="cuda")
+    seqs = batch if kind != "packed" else len(lengths)
+    state, dlast = r(seqs, ch), r(seqs, ch)
+    more = {}
+    if kind == "packed":
+        x, dy, forget, admit = x[0], dy[0], forget[0], admit[0]
+        more["offsets"] = offsets_of(lengths).cuda()
+    y, last, marks = tcu.gated_scan(x, forget, admit, rate, state=state, marks=True, **more)
+    g = tcu.gated_scan_grad(dy, x, forget, admit, rate, marks=marks, state=state, dlast=dlast, **more)
+    off = [0]
+    for n in lengths:
+        off.append(off[-1] + n)
+    for s in (0, batch - 1) if kind == "blocks" else range(seqs):  # of the blocks' entries two
+        at = slice(off[s], off[s + 1]) if kind == "packed" else s
+        if kind == "packed" and not lengths[s]:
+            assert torch.equal(last[s], state[s]) and torch.equal(g.state[s], dlast[s])
+            continue
+        n = lengths[s] if kind == "packed" else rows
+        xs, dys = x[at].double(), dy[at].double()
+        log = -rate.double() / 2
+        keep, room, way = torch.exp(log), torch.sqrt(-torch.expm1(2 * log)), torch.sigmoid(admit[at][0].double())
+        new = room * way * xs
+        h, before, hs = state[s].double(), torch.empty_like(xs), torch.empty_like(xs)
+        for t in range(n):
+            before[t] = h
+            h = keep * h + new[t]
+            hs[t] = h
+        e, carry = torch.empty_like(xs), dlast[s].double()
+        for t in reversed(range(n)):
+            e[t] = dys[t] + carry
+            carry = keep * e[t]
+        dlog = keep * e * before - keep ** 2 / room * e * way * xs
+        for j in range(0, ch, 9):  # each on its own: their sizes differ
+            for got, want, name in (
+                    (y[at], hs, "y"), (g.x[at], e * room * way, "dx"), (g.forget[at], dlog * log / 2, "dforget"),
+                    (g.admit[at], e * room * xs * way * (1 - way), "dadmit")):
+                close(got[..., j], want[..., j].cpu(), (name, s, j))
+        close(last[s], h.cpu(), "last")
+        close(g.state[s], carry.cpu(), "dstate")
+    if batch == 1 and kind != "packed":
+        close(g.rate, (dlog * log / rate).sum(0).cpu(), "drate")
+
+
+@gpu
+def test_tokens_of_gates_that_hardly_change(tcu):
+    """The same, a token at a time."""
+    ch, steps = 64, 3000
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.randn(steps, 1, ch, generator=gen, device="cuda") + 1
+    gate = torch.zeros(1, ch, device="cuda")
+    rate = torch.logspace(-4, 0, ch, device="cuda")
+    state = torch.randn(1, ch, generator=gen, device="cuda") * 100
+    log = -rate.double() / 2
+    keep, room = torch.exp(log), torch.sqrt(-torch.expm1(2 * log))
+    want = state.double()
+    for t in range(steps):
+        tcu.gated_scan_step(x[t], gate, gate, rate, state)
+        want = keep * want + room / 2 * x[t].double()
+    for j in range(ch):
+        close(state[0, j:j + 1], want[0, j:j + 1].cpu(), j)
+
+
+@gpu
+def test_decays_far_from_one(tcu):
+    """Rates that leave nothing of a state beside rates that leave nearly all of
+    it: what a row forgets does not stay as a rounding of what it was."""
+    ch = 64
+    gen = torch.Generator().manual_seed(0)
+    x = randn(gen, 1, 400, ch) * 10.0 ** -torch.arange(400)[:, None].div(20, rounding_mode="floor")
+    forget, admit = randn(gen, 1, 400, ch) + 2, randn(gen, 1, 400, ch)
+    rate = torch.logspace(0.5, 1.5, ch)
+    rate[1::2] = torch.logspace(-3, -1, ch // 2)
+    a = dict(x=x, forget=forget, admit=admit, rate=rate, state=randn(gen, 1, ch) * 1e4)
+    y, _ = ref.gated(**{k: v.double() for k, v in a.items()})
+    got, _ = tcu.gated_scan(**cuda(a))
+    for t in range(0, 400, 20):  # inputs of one size at a time
+        for part in (slice(0, None, 2), slice(1, None, 2)):
+            close(got[0, t + 10:t + 20, part], y[0, t + 10:t + 20, part], (t, part))
