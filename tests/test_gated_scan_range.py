@@ -155,3 +155,54 @@ def test_decays_far_from_one(tcu):
     for t in range(0, 400, 20):  # inputs of one size at a time
         for part in (slice(0, None, 2), slice(1, None, 2)):
             close(got[0, t + 10:t + 20, part], y[0, t + 10:t + 20, part], (t, part))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("share", [16, 12, 9, 8, 6, 4, 3, 2])
+def test_all_sizes_of_clusters(tcu, dtype, packed, share):
+    """Channels for which a strip's rows are shared by 16, 12, 9, 8, 6, 4, 3 or 2
+    blocks, over rows that take several exchanges between them, in sequences
+    that open in different ones; some strips against the definition."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    strips = (sms * 29 // 20 if share > 4 else sms * 9 // 5) // share
+    ch, lengths = strips * 64, [5200] if not packed else [700, 0, 1, 2900, 133, 1466]
+    rows, seqs = sum(lengths), len(lengths)
+    gen = torch.Generator(device="cuda").manual_seed(share)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    x, f, i, dy = (r(rows, ch).to(dtype) for _ in range(4))
+    rate, state, dlast = torch.exp(r(ch) - 3), r(seqs, ch), r(seqs, ch)
+    args = (x, f, i) if packed else (x[None], f[None], i[None])
+    more = dict(offsets=offsets_of(lengths).cuda()) if packed else {}
+    y, last, marks = tcu.gated_scan(*args, rate, state=state, marks=True, **more)
+    g = tcu.gated_scan_grad(dy if packed else dy[None], *args, rate, marks=marks, state=state,
+                            dlast=dlast, **more)
+    some = torch.cat([torch.arange(64) + 64 * s for s in sorted({0, strips // 2, strips - 1})]).cuda()
+    x, f, i, dy, dlast = (t[:, some].double() for t in (x, f, i, dy, dlast))
+    log = -rate[some].double() * torch.sigmoid(f)
+    keep, room, way = torch.exp(log), torch.sqrt(-torch.expm1(2 * log)), torch.sigmoid(i)
+    before, hs, e = (torch.empty_like(keep) for _ in range(3))
+    ends, starts, at = [], [], 0
+    for s, n in enumerate(lengths):
+        h = state[s, some].double()
+        for t in range(at, at + n):
+            before[t] = h
+            h = keep[t] * h + room[t] * way[t] * x[t]
+            hs[t] = h
+        ends.append(h)
+        carry = dlast[s]
+        for t in reversed(range(at, at + n)):
+            e[t] = dy[t] + carry
+            carry = keep[t] * e[t]
+        starts.append(carry)
+        at += n
+    dlog = keep * e * before - keep ** 2 / room * e * way * x
+    rows_of = lambda t: (t if packed else t[0])[:, some]  # noqa: E731
+    close(rows_of(y), hs.cpu(), "y")
+    close(last[:, some], torch.stack(ends).cpu(), "last")
+    close(rows_of(g.x), (e * room * way).cpu(), "dx")
+    close(rows_of(g.admit), (e * room * x * way * (1 - way)).cpu(), "dadmit")
+    close(rows_of(g.forget), (dlog * log * (1 - torch.sigmoid(f))).cpu(), "dforget")
+    close(g.rate[some], (dlog * log / rate[some]).sum(0).cpu(), "drate")
+    close(g.state[:, some], torch.stack(starts).cpu(), "dstate")
