@@ -28,7 +28,8 @@
  * gradients, to the rows' type before the products that take them.  The same
  * call gives the same bits every time.  Angles are
  * 2^-25 turns off at most, at any position: the turns of a position are a 64-bit
- * product that wraps, 2^-31 off for rates up to 2^32, and round to fp32.
+ * product that wraps, 2^-31 off for rates up to 2^32, and round to fp32.  Pairs
+ * whose rate is not finite become no numbers.
  *
  * Calls and statuses are as in tcu_seq.h.  Every wait inside a kernel of
  * attention ends after two seconds; what a block then stores is no number,

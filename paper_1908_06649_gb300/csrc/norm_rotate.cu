@@ -39,6 +39,37 @@ struct RotateArgs {
   float eps;
 };
 
+// The turns of one position, in 2^-64, of each pair of a head; whole turns
+// change nothing.  1 / (2 pi) is taken in two parts, 2^-110 off, and the product
+// with the first in two, so that a position near 2^31 multiplies 2^-63 turns, not
+// the 2^-55 of one product (rates up to 2^32; larger ones lose what they are).
+constexpr int kPairs = TCU_ATTN_MAX_NORM_DIM / 2;
+struct Turns {
+  uint64_t of_one[kPairs];
+  float unit[kPairs];  // half turns of the upper 32 bits' unit; no number where the rate is none
+};
+__device__ __forceinline__ uint64_t fraction(double t) {
+  const double f = fabs(t) - floor(fabs(t));
+  const uint64_t u = (uint64_t)(f * 18446744073709551616.0);
+  return t < 0 ? 0 - u : u;
+}
+template <typename T>
+__device__ __forceinline__ void fill_turns(const RotateArgs<T> &a, Turns &turns) {
+  for (int p = threadIdx.x; p < kPairs; p += kThreads) {
+    uint64_t u = 0;
+    float unit = 4.656612873077393e-10f;  // 2^-31
+    if (p < a.turned) {
+      constexpr double kTurn = 0.15915494309189535, kRest = -9.839338337591243e-18;
+      const double rate = a.rates[p], t = rate * kTurn;
+      if (fabs(rate) < INFINITY) u = fraction(t) + fraction(fma(rate, kRest, fma(rate, kTurn, -t)));
+      else unit = __int_as_float(0x7fffffff);
+    }
+    turns.of_one[p] = u;
+    turns.unit[p] = unit;
+  }
+  __syncthreads();
+}
+
 // A lane's part of a head: kParts parts of VP adjacent pairs, in two words of
 // VP values each.  Pairs that are turned with their partner `turned` values on
 // lie at (p, p + turned), others at (2p, 2p + VP).
@@ -81,13 +112,14 @@ struct Lane {
 
   // cos and sin of the lane's angles at a position: the product wraps as turns
   // do; of its 32 bits fp32 keeps 24, 2^-26 turns
-  __device__ __forceinline__ void angles(const uint64_t *turns, int64_t position, Angles &a) const {
+  __device__ __forceinline__ void angles(const Turns &turns, int64_t position, Angles &a) const {
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
 #pragma unroll
       for (int i = 0; i < VP; ++i) {
-        const int32_t t = (int32_t)(uint32_t)(((uint64_t)position * turns[first[k] + i]) >> 32);
-        sincospif((float)t * 4.656612873077393e-10f, &a.s[k][i], &a.c[k][i]);  // 2^-31
+        const int p = first[k] + i;
+        const int32_t t = (int32_t)(uint32_t)(((uint64_t)position * turns.of_one[p]) >> 32);
+        sincospif((float)t * turns.unit[p], &a.s[k][i], &a.c[k][i]);
       }
   }
   __device__ __forceinline__ void load(const T *head, bool in, Words<T, VP> &v) const {
@@ -195,30 +227,6 @@ __device__ __forceinline__ bool place_of(const RotateArgs<T> &a, int64_t id, int
   return true;
 }
 
-// The turns of one position, in 2^-64, of each pair of a head; whole turns
-// change nothing.  1 / (2 pi) is taken in two parts, 2^-110 off, and the product
-// with the first in two, so that a position near 2^31 multiplies 2^-63 turns, not
-// the 2^-55 of one product (rates up to 2^32; larger ones lose what they are).
-constexpr int kPairs = TCU_ATTN_MAX_NORM_DIM / 2;
-__device__ __forceinline__ uint64_t fraction(double t) {
-  const double f = fabs(t) - floor(fabs(t));
-  const uint64_t u = (uint64_t)(f * 18446744073709551616.0);
-  return t < 0 ? 0 - u : u;
-}
-template <typename T>
-__device__ __forceinline__ void fill_turns(const RotateArgs<T> &a, uint64_t *turns) {
-  for (int p = threadIdx.x; p < kPairs; p += kThreads) {
-    uint64_t u = 0;
-    if (p < a.turned) {
-      constexpr double kTurn = 0.15915494309189535, kRest = -9.839338337591243e-18;
-      const double rate = a.rates[p], t = rate * kTurn;
-      u = fraction(t) + fraction(fma(rate, kRest, fma(rate, kTurn, -t)));
-    }
-    turns[p] = u;
-  }
-  __syncthreads();
-}
-
 // Heads of a lane whose loads are on their way together, and the longest word.
 // At 16384 rows x 40 heads x 128, bf16 (168 MB), forward: words of 8 values, 4
 // heads 67 us, 5 heads 82, of 4 values 85.  The gradient holds two tensors and
@@ -233,7 +241,7 @@ constexpr int kGradWord = 4;
 template <typename T, int VP, bool kInter>
 __global__ void __launch_bounds__(kThreads, 2) rotate_kernel(const RotateArgs<T> a) {
   constexpr int kParts = Part<VP>::kParts, kMany = kAtOnce<VP>;
-  __shared__ uint64_t turns[kPairs];
+  __shared__ Turns turns;
   fill_turns(a, turns);
   const int lane = threadIdx.x % 32, per = 32 / a.lanes, sub = lane / a.lanes;
   using L = Lane<T, VP, kInter>;
@@ -286,7 +294,7 @@ struct GradShared {
   // each lane's shares of dw, [queries, keys][value][thread]
   float shares[2][2 * VP * Part<VP>::kParts][kThreads];
   float sums[kWarps][2 * TCU_ATTN_MAX_NORM_DIM];
-  uint64_t turns[kPairs];
+  Turns turns;
 };
 
 template <typename T, int VP, bool kInter>

@@ -79,6 +79,27 @@ def test_angles(tcu, interleaved):
         assert a.abs().max() <= 8.3e-7 and (b - 1).abs().max() <= 8.3e-7
 
 
+@gpu
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim", [128, 18, 6])
+def test_rates_that_are_no_numbers(tcu, bad, interleaved, dim):
+    """Their pairs come out as no numbers, the others as they were."""
+    n = dim // 2 - 1
+    gen = torch.Generator().manual_seed(0)
+    q, dq = torch.randn(2, 5, 3, 2, dim, generator=gen).cuda().unbind(0)
+    rates = torch.rand(n, generator=gen).cuda()
+    place = torch.tensor([0, 1, -4, 70000, 2 ** 31 - 1], dtype=torch.int32).cuda()[:, None].repeat(1, 3)
+    want, _ = tcu.norm_rotate(q, q, rates, positions=place, interleaved=interleaved)
+    rates[n - 1] = bad
+    got, _ = tcu.norm_rotate(q, q, rates, positions=place, interleaved=interleaved)
+    g = tcu.norm_rotate_grad(dq, dq, q, q, rates, positions=place, interleaved=interleaved)
+    gone = torch.zeros(dim, dtype=torch.bool)
+    gone[[2 * n - 2, 2 * n - 1] if interleaved else [n - 1, 2 * n - 1]] = True
+    assert got[..., gone].isnan().all() and torch.equal(got[..., ~gone], want[..., ~gone])
+    assert g.q[..., gone].isnan().all()
+
+
 def test_reference():
     assert abs(float(over_two_pi()) - 1 / (2 * math.pi)) < 1e-17
     cos, sin = angles([0, 3, -2], [0.5, 2.0])
