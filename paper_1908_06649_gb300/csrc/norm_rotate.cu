@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 2) rotate_grad_kernel(const RotateAr
 // ------------------------------------------------------------- host side
 // Blocks of a call: as many as the card holds at once, so that each sums its
 // shares of the weights' gradients over many rows.
-int64_t blocks_of(const tcu_norm_rotate_args &a, bool grad) {
+int64_t blocks_of(const tcu_norm_rotate_args &a) {
   const int64_t total = (a.offsets ? 1 : (int64_t)a.sequences) * a.rows;
   return std::min<int64_t>((total + kWarps - 1) / kWarps, 2 * num_sms());
 }
@@ -421,7 +421,7 @@ int start(const tcu_norm_rotate_args &s, RotateArgs<T> a, bool grad, cudaStream_
   const int words = (s.dim / 2 + VP - 1) / VP;
   a.lanes = 1;
   while (a.lanes < 32 && a.lanes < words) a.lanes *= 2;
-  const unsigned blocks = (unsigned)blocks_of(s, grad);
+  const unsigned blocks = (unsigned)blocks_of(s);
   constexpr int bytes = sizeof(GradShared<VP>);
   if (!grad) {
     rotate_kernel<T, VP, kInter><<<blocks, kThreads, 0, st>>>(a);
@@ -501,7 +501,7 @@ int run(const tcu_norm_rotate_args &s, bool grad, cudaStream_t st) {
   int n = 0;
   if (s.dq_weight) sums[n++] = {s.dq_weight, a.parts, s.dim};
   if (s.dk_weight) sums[n++] = {s.dk_weight, a.parts + s.dim, s.dim};
-  return n ? sum_parts(sums, n, a.total > 0 ? blocks_of(s, true) : 0, 2 * s.dim, st) : TCU_DFT_OK;
+  return n ? sum_parts(sums, n, a.total > 0 ? blocks_of(s) : 0, 2 * s.dim, st) : TCU_DFT_OK;
 }
 
 int check_sizes(const tcu_norm_rotate_args *a) {
@@ -544,7 +544,7 @@ using namespace tcu::seq;
 
 extern "C" int64_t tcu_norm_rotate_grad_workspace(const tcu_norm_rotate_args *a) {
   if (check_sizes(a)) return -1;
-  return a->dq_weight || a->dk_weight ? blocks_of(*a, true) * 2 * a->dim * 4 : 0;
+  return a->dq_weight || a->dk_weight ? blocks_of(*a) * 2 * a->dim * 4 : 0;
 }
 
 extern "C" int tcu_norm_rotate(const tcu_norm_rotate_args *a, void *stream) {
