@@ -24,17 +24,19 @@
  * left as they are in outputs, and their gradients are zeros.
  *
  * Statistics, sums and products are accumulated in fp32 and rounded once, on
- * storing; attention rounds its weights, and in the gradient the scores'
- * gradients, to the rows' type before the products that take them.  The same
- * call gives the same bits every time.  Angles are
- * 2^-25 turns off at most, at any position: the turns of a position are a 64-bit
- * product that wraps, 2^-31 off for rates up to 2^32, and round to fp32.  Pairs
- * whose rate is not finite become no numbers.
+ * storing; attention over prompts rounds its weights, and in the gradient the
+ * scores' gradients, to the rows' type before the products that take them (fp16:
+ * times powers of two for each row or key, so that nothing is lost to its range;
+ * single tokens: in two parts).  The same call gives the same bits every time.
+ * Angles are 2^-25 turns off at most, at any position: the turns of a position
+ * are a 64-bit product that wraps, 2^-31 off for rates up to 2^32, and round to
+ * fp32.  Pairs whose rate is not finite become no numbers.
  *
  * Calls and statuses are as in tcu_seq.h.  Every wait inside a kernel of
  * attention ends after two seconds; what a block then stores is no number,
- * while the call, which returned before, has given OK.  Outputs must not overlap inputs or
- * themselves, but y_q and y_k may be q and k, with the same strides.
+ * while the call, which returned before, has given OK.  Outputs must not
+ * overlap inputs or themselves, but y_q and y_k may be q and k, with the same
+ * strides.
  */
 #ifndef TCU_ATTN_H
 #define TCU_ATTN_H

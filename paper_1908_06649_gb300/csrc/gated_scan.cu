@@ -21,10 +21,11 @@
 // call gives the same bits.  The gradient walks the tiles from the end, forward
 // within a run from the state that the forward pass kept of it, and back.
 //
-// Measured, bf16: forward 8 x 2048 x 4096 (537 MB) 114 us, 4.7 TB/s, gradient
-// (933 MB) 222 us, 4.2 TB/s; forward 65536 x 1536 (805 MB) 238 us, 3.4 TB/s.
+// Measured, bf16: forward 8 x 2048 x 4096 (537 MB) 119 us, 4.5 TB/s, gradient
+// (933 MB) 228 us, 4.1 TB/s; forward 65536 x 1536 (805 MB) 259 us, 3.1 TB/s.
 // Copying runs at 6.8 TB/s.  58 % of the issue slots are in use at two blocks an
-// SM: latency of the exchange and of short chains is what is left.
+// SM: latency of the exchange and of short chains is what is left.  With decays
+// rounded from run to run the same took 114, 222 and 238 us.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -864,10 +865,10 @@ GatedPlan plan_of(const tcu_gated_scan_args &a, bool grad) {
   // Blocks of a cluster share a strip's rows, where strips are fewer than the
   // card's places, two an SM: the largest size at which all clusters run at
   // once.  Large clusters find fewer places, since each lies within one part of
-  // the card.  65536 x 1536, 24 strips, forward: 340, 279, 239, 295, 280 us in
-  // clusters of 4, 8, 9, 12, 16; 4121 x 1031 f32, 17 strips: 58, 47, 42, 34, 49;
-  // 8192 x 4096, 64 strips: 71, 79 us in clusters of 4, 8; 8 x 2048 x 4096, 512
-  // strips: 114 us whole, 121 in clusters of 2.
+  // the card.  65536 x 1536, 24 strips, forward: 371, 302, 261, 320, 306 us in
+  // clusters of 4, 8, 9, 12, 16; 4121 x 1031 f32, packed, 17 strips: 70, 53, 48,
+  // 42, 60; 8192 x 4096, 64 strips: 78, 87 us in clusters of 4, 8; 8 x 2048 x 4096,
+  // 512 strips: 124 us whole, 134 in clusters of 2 (launch included).
   const int64_t tile = grad ? kTile : kLongTile, tiles = (a.rows + tile - 1) / tile;
   const int64_t strips = p.strips * p.entries, sms = num_sms();
   p.size = 1;

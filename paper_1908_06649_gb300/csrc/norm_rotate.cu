@@ -12,8 +12,8 @@
 // values of a pair are in the same lane: rows may be written over those that
 // they come from.
 //
-// Measured, bf16, 16384 rows x 40 heads x 128: forward (336 MB) 65 us, 5.2 TB/s;
-// gradient (503 MB) 121 us with the sum of its shares, 4.2 TB/s.
+// Measured, bf16, 16384 rows x 40 heads x 128: forward (336 MB) 60 us, 5.6 TB/s;
+// gradient (503 MB) 110 us and 10 for the sum of its shares, 4.2 TB/s.
 #include <algorithm>
 
 #include "../../include/tcu_attn.h"
@@ -228,10 +228,10 @@ __device__ __forceinline__ bool place_of(const RotateArgs<T> &a, int64_t id, int
 }
 
 // Heads of a lane whose loads are on their way together, and the longest word.
-// At 16384 rows x 40 heads x 128, bf16 (168 MB), forward: words of 8 values, 4
-// heads 67 us, 5 heads 82, of 4 values 85.  The gradient holds two tensors and
-// its sums beside them: words of 8 spill, 214 us; of 4, 4 heads 137 us, 2 heads
-// 171, 3 heads 146.
+// At 16384 rows x 40 heads x 128, bf16 (168 MB), launches included, forward: words
+// of 8 values, 4 heads 66 us, 5 heads 68, of 4 values 83.  The gradient holds two
+// tensors and its sums beside them: words of 4, 4 heads 123 us, 2 heads 140, 3
+// heads 136; words of 8 146.  Three blocks an SM: 91 and 146.
 template <int VP>
 constexpr int kAtOnce = VP >= 4 ? 4 : 2;
 template <typename T, int VP>

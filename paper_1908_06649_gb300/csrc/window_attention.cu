@@ -14,11 +14,12 @@
 // scores and products for weights, so scores run a tile ahead, in two places,
 // and two blocks share an SM (256 columns of tensor memory, 96 KB of tiles
 // each).  A warp each issues products, copies, and looks over values that not
-// all rows see; at 128 keys a tile, one place for scores and two threads a row
-// the same call took 1,007 us for 808, with copies issued between products 904.
+// all rows see.
 //
 // Measured, bf16: 32768 rows, 32 heads (8 of keys) x 128, window 2048, 4 first
-// tokens (1.07e12 flops): 845 us, 1.26 PFLOP/s, 67 % of cuBLAS's burst rate.
+// tokens (1.07e12 flops): 886 us, 1.21 PFLOP/s, 64 % of cuBLAS's burst rate.  Before
+// values were looked over it was 808, with copies issued between the products 904,
+// with 128 keys a tile, one place for scores and two threads a row 1,007.
 #include <algorithm>
 
 #include "attn_common.cuh"

@@ -17,10 +17,11 @@
 //
 // Products bound it, 10 dim flops a visible pair and head (14 as done here).
 // Measured, bf16, 4 x 2048 rows, 16 heads (4 of keys) x 128, window 1024 (1.3e11
-// flops): dq 116 us, dk and dv 150 us, delta 16 us, joining 8 us: 0.45 PFLOP/s
-// of what is asked for, 0.62 of what is done.  Tiles of 64 rows read the other
+// flops): dq 120 us, dk and dv 153 us, delta 16 us, joining 8 us: 0.44 PFLOP/s
+// of what is asked for, 0.61 of what is done.  Tiles of 64 rows read the other
 // operand anew from shared memory for each product (55 to 60 cycles where 32
-// would do), and tensor memory holds no larger ones beside the sums.
+// would do), and tensor memory holds no larger ones beside the sums.  At 640
+// threads dkv_kernel has 96 registers, and spills 100 to 140 bytes of them.
 #include <algorithm>
 
 #include "attn_common.cuh"

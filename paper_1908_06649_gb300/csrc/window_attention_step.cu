@@ -12,7 +12,10 @@
 // through shared memory in the order of warps and blocks.
 //
 // Measured, bf16: 64 tokens, 32 heads (8 of keys) x 128, 2052 rows an entry (538
-// MB) 88 us, 6.1 TB/s, 90 % of the copy rate; one token of 1028 rows 11 us.
+// MB) 90 us, 6.0 TB/s, 88 % of the copy rate (weights in one part: 88); one token of
+// 1028 rows 11 us, five round trips to memory that wait for each other (slot,
+// position, q, the new row, which is taken and stored first, the cache) and the
+// barriers of a cluster.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -359,9 +362,10 @@ int step(const tcu_window_attention_args &s, cudaStream_t st) {
   a.head_groups = (s.heads / s.kv_heads + kHeads - 1) / kHeads;
   a.c = s.scale * kLog2e;
   // Blocks of a cluster share an entry's rows, where blocks are fewer than SMs
-  // and a warp still has a few tiles: a block costs some 10 us beside its rows.
-  // 64 entries x 8 key heads x 2052 rows: 90 us whole, 107 in clusters of 2, 121
-  // of 4; 16 x 2 x 4100 rows of 64 values: 33 us whole, 12 in clusters of 8.
+  // and a warp still has a few tiles: a block costs some 10 us beside its rows (the
+  // chain above).  Launch included, 64 entries x 8 key heads x 2052 rows: 109 us
+  // whole, 126 in clusters of 2, 138 of 4; 16 x 2 x 4100 rows of 64 values: 37 us
+  // whole, 19 in clusters of 8.
   const int64_t blocks = (int64_t)a.head_groups * s.kv_heads * s.sequences;
   const int64_t tiles = ((int64_t)s.window + s.sinks + kTile - 1) / kTile;
   int size = 1;
