@@ -198,3 +198,42 @@ def test_gradients_are_rounded_twice(tcu, dtype, length, window, sinks):
     for n, got, exact in zip(g._fields, g, grads):
         off = float((got.cpu().double() - exact).norm() / exact.norm() / U[dtype])
         assert off <= 0.75, (n, off)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("lengths,window,sinks", [([2600], 100, 3), ([700, 0, 1990, 50], 60, 130),
+                                                  ([100, 2300], 900, 4)])
+def test_first_tokens_of_long_sequences(tcu, dtype, lengths, window, sinks):
+    """Keys that thousands of rows see, whose sums are formed in parts: late
+    rows' dy a thousandth of early ones', sequences of other sizes."""
+    a, dy = inputs(dtype, (sum(lengths),), 4, 2, 64)
+    off = offsets_of(lengths)
+    parts = []
+    for s, n in enumerate(lengths):
+        at = slice(off[s].item(), off[s + 1].item())
+        dy[at] *= 2.0 ** (8 if s % 2 else -2)
+        dy[at.start + n // 2:at.stop] *= 2.0 ** -10
+        parts += [(slice(at.start, at.start + n // 2),), (slice(at.start + n // 2, at.stop),)] if n else []
+    check_parts(tcu, a, dy, window, sinks, dict(q=parts, k=parts, v=parts), off)
+
+
+@gpu
+def test_captured_calls_of_other_sizes(tcu):
+    """One graph, replayed for inputs of other sizes: nothing is kept from one
+    replay for the next."""
+    a, dy = inputs(torch.float16, (2, 300), 4, 2, 64)
+    c, more = cuda(a), dict(window=60, sinks=2)
+    dy = dy.cuda()
+    y, lse = tcu.window_attention(**c, lse=True, **more)
+    static, graph = dy.clone(), torch.cuda.CUDAGraph()
+    tcu.window_attention_grad(static, **c, y=y, lse=lse, **more)
+    with torch.cuda.graph(graph):
+        g = tcu.window_attention_grad(static, **c, y=y, lse=lse, **more)
+    for e in (12, -6, 12, 0):
+        static.copy_(dy * 2.0 ** e)
+        graph.replay()
+        want = tcu.window_attention_grad(static, **c, y=y, lse=lse, **more)
+        torch.cuda.synchronize()
+        for x, w in zip(g, want):
+            assert torch.equal(x, w), e
